@@ -292,6 +292,60 @@ RPX_API rpx_status_t rpx_attn_backward(const rpx_attn_desc_t* desc, const void* 
 RPX_API size_t rpx_attn_backward_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_tokens);
 
 /*
+ * Norm of queries and keys per head and rotation by position, in one pass (the attention calls of this library take q and
+ * k with both already applied; the paper's video prompts are positioned on three axes: time, height, width).  For every
+ * token t and head h, with the weight w of that tensor (q_weight or k_weight, [head_dim]):
+ *     y = x * (mean(x^2) + eps)^(-1/2) * w                     (y = x when the two weights are NULL)
+ *     a_i = positions[pair_axis[i]][t] * inv_freq[i]           for the pairs i < rot_dim / 2
+ *     out_i              = y_i cos a_i - y_{i+rot_dim/2} sin a_i
+ *     out_{i+rot_dim/2}  = y_{i+rot_dim/2} cos a_i + y_i sin a_i,      out_j = y_j for j >= rot_dim
+ * Sums and products are float32, the angles are reduced in 64 bits (any int32 position), and the result is rounded once.
+ *   desc->rot_dim: a multiple of 16, 16 .. head_dim; head_dim 64 or 128; any head counts >= 1
+ *   desc->pair_axis: HOST array of rot_dim / 2 axis numbers < num_axes (1 .. 8), or NULL: every pair takes axis 0
+ *   q [n_tokens][num_q_heads][head_dim], k [n_tokens][num_kv_heads][head_dim] with token strides in elements, such as
+ *       views of one fused projection; q_weight, k_weight: element type of q and k, both or neither NULL
+ *   positions device int32 [num_axes][pos_axis_stride], pos_axis_stride >= n_tokens; inv_freq device float32 [rot_dim / 2]
+ *   q_out, k_out with token strides; each may be its input itself (same pointer and stride), otherwise no output
+ *       overlaps an input or the other output
+ */
+typedef struct {
+    int32_t num_q_heads;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    int32_t rot_dim;
+    int32_t num_axes;
+    const uint8_t* pair_axis; /* host */
+    float eps;                /* >= 0 */
+    rpx_dtype_t dtype;        /* element type of q, k, the weights and the outputs */
+} rpx_rope_desc_t;
+
+RPX_API rpx_status_t rpx_qk_norm_rope(const rpx_rope_desc_t* desc, const void* q, const void* k, int64_t q_tok_stride,
+                                      int64_t k_tok_stride, const void* q_weight, const void* k_weight,
+                                      const int32_t* positions, int64_t pos_axis_stride, const float* inv_freq,
+                                      int64_t n_tokens, void* q_out, void* k_out, int64_t q_out_tok_stride,
+                                      int64_t k_out_tok_stride, void* cuda_stream);
+
+/*
+ * Backward of rpx_qk_norm_rope (Section 3.2: the training actor's passes are differentiated).  dq, dk are the gradients with
+ * respect to its outputs as rpx_attn_backward leaves them: float32, contiguous.  With g = the transposed rotation of the
+ * gradient, u = x * (mean(x^2) + eps)^(-1/2) and r that factor:
+ *     dw = sum over tokens and heads of g u,      dx = r (g w - u mean(g w u))          (dx = g without weights)
+ *   dq_in, dk_in: gradients with respect to q and k, desc->dtype, token strides in elements, no overlap with any input
+ *   dq_weight, dk_weight: float32 [head_dim], both or neither NULL, only with weights; accumulate_dw == 0: written,
+ *       != 0: added to.  n_tokens == 0 writes zeros (or adds nothing).
+ *   workspace: rpx_qk_norm_rope_backward_workspace_bytes, needed when dq_weight and dk_weight are given
+ * Sums run in a fixed order: the same call gives the same bits.
+ */
+RPX_API rpx_status_t rpx_qk_norm_rope_backward(const rpx_rope_desc_t* desc, const void* q, const void* k, int64_t q_tok_stride,
+                                               int64_t k_tok_stride, const void* q_weight, const void* k_weight,
+                                               const int32_t* positions, int64_t pos_axis_stride, const float* inv_freq,
+                                               const float* dq, const float* dk, int64_t n_tokens, void* dq_in, void* dk_in,
+                                               int64_t dq_in_tok_stride, int64_t dk_in_tok_stride, float* dq_weight,
+                                               float* dk_weight, int32_t accumulate_dw, void* workspace,
+                                               size_t workspace_bytes, void* cuda_stream);
+RPX_API size_t rpx_qk_norm_rope_backward_workspace_bytes(const rpx_rope_desc_t* desc, int64_t n_tokens);
+
+/*
  * Allocation-free variant of rpx_token_logprobs (the paper has no counterpart: this entry point
  * exists for deployment, not for the method).  It is meant for callers that cannot give the
  * library a workspace because they cannot allocate one: a scoring hook that runs inside an

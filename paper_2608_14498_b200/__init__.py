@@ -13,8 +13,11 @@ from .binding import (  # noqa: F401
     get_sm_budget,
     library_path,
     load_library,
+    mrope_pair_axis,
     prefix_attn,
     prefix_attn_workspace_bytes,
+    qk_norm_rope,
+    qk_norm_rope_backward,
     selftest_bounded_wait,
     set_lm_head_pairing,
     set_sm_budget,

@@ -34,6 +34,9 @@ EXPORTS = (
     "rpx_get_lm_head_pairing",
     "rpx_attn_backward",
     "rpx_attn_backward_workspace_bytes",
+    "rpx_qk_norm_rope",
+    "rpx_qk_norm_rope_backward",
+    "rpx_qk_norm_rope_backward_workspace_bytes",
     "rpx_prefix_attn_workspace_bytes",
     "rpx_suffix_attn_workspace_bytes",
     "rpx_token_logprobs_workspace_bytes",
@@ -69,6 +72,19 @@ class KvCache(ctypes.Structure):
         ("block_size", ctypes.c_int32),
         ("block_table", ctypes.c_void_p),
         ("block_table_stride", ctypes.c_int32),
+    ]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32),
+        ("pair_axis", ctypes.c_char_p),
+        ("eps", ctypes.c_float),
+        ("dtype", ctypes.c_int32),
     ]
 
 
@@ -118,6 +134,13 @@ def load_library():
                                       i64, i32, vp, vp, vp, i32, vp, sz, vp, vp]
     lib.rpx_attn_backward_workspace_bytes.restype = sz
     lib.rpx_attn_backward_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i64]
+    lib.rpx_qk_norm_rope.restype = i32
+    lib.rpx_qk_norm_rope.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, i64, i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, i64, vp]
+    lib.rpx_qk_norm_rope_backward.restype = i32
+    lib.rpx_qk_norm_rope_backward.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, i64, i64, vp, vp, vp, i64, vp, vp, vp, i64, vp,
+                                              vp, i64, i64, vp, vp, i32, vp, sz, vp]
+    lib.rpx_qk_norm_rope_backward_workspace_bytes.restype = sz
+    lib.rpx_qk_norm_rope_backward_workspace_bytes.argtypes = [ctypes.POINTER(RopeDesc), i64]
     lib.rpx_prefix_attn_workspace_bytes.restype = sz
     lib.rpx_prefix_attn_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i64]
     lib.rpx_suffix_attn_workspace_bytes.restype = sz
@@ -544,3 +567,112 @@ def token_logprobs_merge(all_stats, target_ids, vocab_total: int, logprobs=None,
     if rc != 0:
         raise RpxError(rc, "rpx_token_logprobs_merge")
     return (logprobs, lse) if return_lse else logprobs
+
+
+# ------------------------------------------------------------------ norm + rotation in front of the attention calls
+def mrope_pair_axis(sections, interleaved: bool = False):
+    """Axis of every rotary pair for positions on several axes: ``sections[a]`` pairs for axis a, one run after the other,
+    or - ``interleaved`` - the axes taking turns while they have pairs left (pair i goes to axis i mod n) and axis 0
+    taking every other pair."""
+    n, total = len(sections), sum(sections)
+    if n < 1 or any(s < 0 for s in sections):
+        raise ValueError("sections are pair counts, one per axis")
+    if not interleaved:
+        return [a for a, s in enumerate(sections) for _ in range(s)]
+    axes = [i % n if i // n < sections[i % n] else 0 for i in range(total)]
+    if [axes.count(a) for a in range(n)] != list(sections):
+        raise ValueError("these sections cannot take turns: an axis other than 0 has more pairs than there are turns")
+    return axes
+
+
+def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) -> RopeDesc:
+    torch = _torch()
+    code = _dtype_code(q)
+    if k.dtype != q.dtype or any(w is not None and w.dtype != q.dtype for w in (q_weight, k_weight)):
+        raise TypeError("q, k and the norm weights must share an element type")
+    if positions.dtype != torch.int32 or inv_freq.dtype != torch.float32:
+        raise TypeError("positions are int32 and inv_freq float32")
+    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        raise ValueError("expected q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim]")
+    n, d = q.shape[0], q.shape[2]
+    if positions.dim() not in (1, 2) or positions.shape[-1] != n or (n > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions are [tokens] or [axes, tokens] with contiguous tokens")
+    if inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq is a contiguous [rot_dim / 2] tensor")
+    for w in (q_weight, k_weight):
+        if w is not None and (tuple(w.shape) != (d,) or not w.is_contiguous()):
+            raise ValueError("norm weights are contiguous [head_dim] tensors")
+    rot = 2 * inv_freq.shape[0]
+    if pair_axis is not None and len(pair_axis) != rot // 2:
+        raise ValueError("pair_axis has one axis number per entry of inv_freq")
+    return RopeDesc(q.shape[1], k.shape[1], d, rot, positions.shape[0] if positions.dim() == 2 else 1,
+                    bytes(pair_axis) if pair_axis is not None else None, float(eps), code)
+
+
+def _axis_stride(positions) -> int:
+    n = positions.shape[-1]
+    return positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else n
+
+
+def _rope_out(given, like):
+    if given is None:
+        return _torch().empty(tuple(like.shape), dtype=like.dtype, device=like.device)
+    if given.shape != like.shape or given.dtype != like.dtype:
+        raise ValueError("an output has the shape and element type of its input")
+    return given
+
+
+@_in_call_context
+def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, pair_axis=None, eps: float = 1e-6, q_out=None,
+                 k_out=None, stream=None):
+    """rpx_qk_norm_rope: RMS norm per head (with weights) and rotation by position of queries and keys, in one pass.
+
+    q [T, H_q, d], k [T, H_kv, d]; positions int32 [T] or [axes, T]; inv_freq float32 [rot_dim / 2]; pair_axis: the axis of
+    each pair (see ``mrope_pair_axis``), None = axis 0; weights [d] or both None (rotation only).  ``q_out`` / ``k_out``
+    may be q / k themselves.  Returns (q_out, k_out)."""
+    lib = load_library()
+    desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)
+    q_out, k_out = _rope_out(q_out, q), _rope_out(k_out, k)
+    rc = lib.rpx_qk_norm_rope(ctypes.byref(desc), _ptr(q), _ptr(k), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
+                              _ptr(k_weight), _ptr(positions), _axis_stride(positions), _ptr(inv_freq), q.shape[0],
+                              _ptr(q_out), _ptr(k_out), _tok_stride(q_out), _tok_stride(k_out), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_qk_norm_rope")
+    return q_out, k_out
+
+
+@_in_call_context
+def qk_norm_rope_backward(q, k, dq, dk, positions, inv_freq, q_weight=None, k_weight=None, pair_axis=None, eps: float = 1e-6,
+                          dq_in=None, dk_in=None, dq_weight=None, dk_weight=None, accumulate_dw: bool = False,
+                          workspace=None, stream=None):
+    """rpx_qk_norm_rope_backward: from float32 dq, dk with respect to the outputs (as ``attn_backward`` returns them) to the
+    gradients of q, k (their element type) and of the norm weights (float32, added to the given buffers with
+    ``accumulate_dw``).  Returns (dq_in, dk_in, dq_weight, dk_weight), the last two None without weights."""
+    torch = _torch()
+    lib = load_library()
+    desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)
+    for g, x in ((dq, q), (dk, k)):
+        if g.dtype != torch.float32 or g.shape != x.shape or not g.is_contiguous():
+            raise ValueError("dq and dk are contiguous float32 tensors of the shapes of q and k")
+    dq_in, dk_in = _rope_out(dq_in, q), _rope_out(dk_in, k)
+    d = q.shape[2]
+    ws = None
+    if q_weight is not None:
+        if accumulate_dw and (dq_weight is None or dk_weight is None):
+            raise ValueError("accumulate_dw needs the dq_weight and dk_weight buffers to add to")
+        if dq_weight is None:
+            dq_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+        if dk_weight is None:
+            dk_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+        for w in (dq_weight, dk_weight):
+            if w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous():
+                raise ValueError("weight gradients are contiguous float32 [head_dim] tensors")
+        ws = _workspace(int(lib.rpx_qk_norm_rope_backward_workspace_bytes(ctypes.byref(desc), q.shape[0])), q.device, workspace)
+    rc = lib.rpx_qk_norm_rope_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
+                                       _ptr(k_weight), _ptr(positions), _axis_stride(positions), _ptr(inv_freq), _ptr(dq),
+                                       _ptr(dk), q.shape[0], _ptr(dq_in), _ptr(dk_in), _tok_stride(dq_in), _tok_stride(dk_in),
+                                       _ptr(dq_weight), _ptr(dk_weight), 1 if accumulate_dw else 0, _ptr(ws),
+                                       ws.numel() * ws.element_size() if ws is not None else 0, _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_qk_norm_rope_backward")
+    return dq_in, dk_in, dq_weight, dk_weight

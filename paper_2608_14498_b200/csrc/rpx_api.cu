@@ -368,6 +368,120 @@ rpx_status_t rpx_attn_backward(const rpx_attn_desc_t* desc, const void* q, const
     return launch_attention_backward(a);
 }
 
+}  // extern "C"
+
+namespace {
+
+// Checks shared by rpx_qk_norm_rope and its backward; `out_*` are the tensors the call writes.
+rpx_status_t check_rope(const RopeArgs& a) {
+    const rpx_rope_desc_t* d = a.desc;
+    if (d == nullptr) return RPX_ERR_NULL;
+    if (d->dtype != RPX_BF16 && d->dtype != RPX_F32) return RPX_ERR_DTYPE;
+    if (d->head_dim != 64 && d->head_dim != 128) return RPX_ERR_SHAPE;
+    if (d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->num_q_heads > 65536 || d->num_kv_heads > 65536) return RPX_ERR_SHAPE;
+    if (d->rot_dim < 16 || d->rot_dim > d->head_dim || d->rot_dim % 16 != 0) return RPX_ERR_SHAPE;
+    if (d->num_axes < 1 || d->num_axes > 8 || !(d->eps >= 0.f)) return RPX_ERR_SHAPE;
+    if (d->pair_axis != nullptr)
+        for (int i = 0; i < d->rot_dim / 2; ++i)
+            if (d->pair_axis[i] >= d->num_axes) return RPX_ERR_SHAPE;
+    if (a.n_tokens < 0 || a.n_tokens >= INT32_MAX) return RPX_ERR_SHAPE;
+    if ((a.q_weight == nullptr) != (a.k_weight == nullptr)) return RPX_ERR_NULL;
+    if (a.n_tokens == 0) return RPX_OK;
+    if (a.q == nullptr || a.k == nullptr || a.positions == nullptr || a.inv_freq == nullptr || a.q_out == nullptr ||
+        a.k_out == nullptr)
+        return RPX_ERR_NULL;
+    const int64_t q_row = static_cast<int64_t>(d->num_q_heads) * d->head_dim;
+    const int64_t kv_row = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
+    if (a.q_tok_stride < q_row || a.k_tok_stride < kv_row || a.q_out_tok_stride < q_row || a.k_out_tok_stride < kv_row ||
+        a.pos_axis_stride < a.n_tokens)
+        return RPX_ERR_SHAPE;
+    if (a.q_tok_stride % 8 || a.k_tok_stride % 8 || a.q_out_tok_stride % 8 || a.k_out_tok_stride % 8) return RPX_ERR_ALIGN;
+    if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.q_weight) || !aligned16(a.k_weight) || !aligned16(a.q_out) ||
+        !aligned16(a.k_out) || !aligned16(a.dq) || !aligned16(a.dk))
+        return RPX_ERR_ALIGN;
+    return RPX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+rpx_status_t rpx_qk_norm_rope(const rpx_rope_desc_t* desc, const void* q, const void* k, int64_t q_tok_stride,
+                              int64_t k_tok_stride, const void* q_weight, const void* k_weight, const int32_t* positions,
+                              int64_t pos_axis_stride, const float* inv_freq, int64_t n_tokens, void* q_out, void* k_out,
+                              int64_t q_out_tok_stride, int64_t k_out_tok_stride, void* cuda_stream) {
+    RopeArgs a;
+    a.desc = desc;
+    a.q = q;
+    a.k = k;
+    a.q_tok_stride = q_tok_stride;
+    a.k_tok_stride = k_tok_stride;
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.positions = positions;
+    a.pos_axis_stride = pos_axis_stride;
+    a.inv_freq = inv_freq;
+    a.n_tokens = n_tokens;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.q_out_tok_stride = q_out_tok_stride;
+    a.k_out_tok_stride = k_out_tok_stride;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rpx_status_t rc = check_rope(a)) return rc;
+    if (n_tokens == 0) return RPX_OK;
+    if (rpx_status_t rc = check_arch()) return rc;
+    return launch_qk_rope(a);
+}
+
+size_t rpx_qk_norm_rope_backward_workspace_bytes(const rpx_rope_desc_t* desc, int64_t n_tokens) {
+    if (desc == nullptr || n_tokens < 0 || desc->head_dim <= 0) return 0;
+    return align_up(rope_backward_workspace(desc->head_dim), kWsAlign);
+}
+
+rpx_status_t rpx_qk_norm_rope_backward(const rpx_rope_desc_t* desc, const void* q, const void* k, int64_t q_tok_stride,
+                                       int64_t k_tok_stride, const void* q_weight, const void* k_weight,
+                                       const int32_t* positions, int64_t pos_axis_stride, const float* inv_freq,
+                                       const float* dq, const float* dk, int64_t n_tokens, void* dq_in, void* dk_in,
+                                       int64_t dq_in_tok_stride, int64_t dk_in_tok_stride, float* dq_weight, float* dk_weight,
+                                       int32_t accumulate_dw, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    RopeArgs a;
+    a.desc = desc;
+    a.q = q;
+    a.k = k;
+    a.q_tok_stride = q_tok_stride;
+    a.k_tok_stride = k_tok_stride;
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.positions = positions;
+    a.pos_axis_stride = pos_axis_stride;
+    a.inv_freq = inv_freq;
+    a.n_tokens = n_tokens;
+    a.q_out = dq_in;
+    a.k_out = dk_in;
+    a.q_out_tok_stride = dq_in_tok_stride;
+    a.k_out_tok_stride = dk_in_tok_stride;
+    a.dq = dq;
+    a.dk = dk;
+    a.dq_weight = dq_weight;
+    a.dk_weight = dk_weight;
+    a.accumulate_dw = accumulate_dw != 0;
+    a.workspace = workspace;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rpx_status_t rc = check_rope(a)) return rc;
+    if ((dq_weight == nullptr) != (dk_weight == nullptr)) return RPX_ERR_NULL;
+    if (dq_weight != nullptr && q_weight == nullptr) return RPX_ERR_NULL;  // no weights, no gradient of them
+    if (n_tokens > 0 && (dq == nullptr || dk == nullptr)) return RPX_ERR_NULL;
+    if (dq_weight != nullptr) {
+        if (workspace == nullptr || workspace_bytes < rpx_qk_norm_rope_backward_workspace_bytes(desc, n_tokens))
+            return RPX_ERR_WORKSPACE;
+        if (!aligned_ws(workspace)) return RPX_ERR_ALIGN;
+    } else if (n_tokens == 0) {
+        return RPX_OK;
+    }
+    if (rpx_status_t rc = check_arch()) return rc;
+    return launch_qk_rope_backward(a);
+}
+
 rpx_status_t rpx_selftest_bounded_wait(int64_t limit_cycles, int32_t* device_status, void* cuda_stream) {
     if (device_status == nullptr) return RPX_ERR_NULL;
     if (limit_cycles <= 0 || limit_cycles > 2000000000ll) return RPX_ERR_SHAPE;

@@ -118,6 +118,28 @@ struct AttnBwdArgs {
 };
 rpx_status_t launch_attention_backward(const AttnBwdArgs& a);
 
+struct RopeArgs {
+    const rpx_rope_desc_t* desc;
+    const void *q, *k;
+    int64_t q_tok_stride, k_tok_stride;
+    const void *q_weight, *k_weight;     // both or neither NULL
+    const int32_t* positions;
+    int64_t pos_axis_stride;
+    const float* inv_freq;
+    int64_t n_tokens;
+    void *q_out, *k_out;                 // forward: the results; backward: gradients with respect to q and k
+    int64_t q_out_tok_stride, k_out_tok_stride;
+    const float *dq = nullptr, *dk = nullptr;          // backward only
+    float *dq_weight = nullptr, *dk_weight = nullptr;  // backward only, nullable
+    bool accumulate_dw = false;
+    void* workspace = nullptr;           // backward: one partial row per CTA
+    cudaStream_t stream;
+};
+constexpr int kRopeBwdCtasPerSm = 2, kRopeBwdMaxCtas = 512;
+size_t rope_backward_workspace(int32_t head_dim);
+rpx_status_t launch_qk_rope(const RopeArgs& a);
+rpx_status_t launch_qk_rope_backward(const RopeArgs& a);
+
 rpx_status_t launch_bounded_wait_selftest(long long limit_cycles, int32_t* status, cudaStream_t stream);
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }

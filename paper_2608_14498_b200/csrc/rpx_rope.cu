@@ -1,0 +1,453 @@
+// Per-head RMS norm of queries and keys with the rotation by multi-axis positions in the same pass, and its backward.
+//
+//   u = x * r,  r = (mean(x^2) + eps)^(-1/2),  y = u * w     (both steps left out when the weights are NULL)
+//   pair i = (i, i + rot/2) of the first rot elements is turned by theta_i = position[axis(i)] * inv_freq[i]:
+//   out_i = y_i cos - y_{i+rot/2} sin,  out_{i+rot/2} = y_{i+rot/2} cos + y_i sin;  the elements from rot on pass through
+//
+// backward, with g = (transposed rotation) dout:
+//   dw = sum over tokens and heads of g * u,   dx = r * (g w - u * mean(g w u))
+//
+// Bound by memory: 2 + 2 bytes per value forward in bf16, 2 + 4 + 2 backward (the gradients that arrive are float32).
+// A row of head_dim values is held by head_dim / 16 lanes, each with TWO 8-element chunks: the two that the rotation
+// pairs up (p and p + rot/16; beyond rot two neighbours), so neither half ever moves between lanes and the only
+// exchange is the sum of squares.  A warp keeps one token: its rot/2 angles are computed once, two per lane, and read
+// back from shared memory as the lane's eight (cos, sin) pairs for all of the token's heads.
+#include <cuda_bf16.h>
+
+#include "rpx_internal.h"
+
+namespace rpx {
+
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kMaxPairs = 64;
+
+struct Params {
+    const void *q, *k;
+    void *q_out, *k_out;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;  // elements between tokens
+    const void *q_weight, *k_weight;  // [D], or NULL
+    const int32_t* positions;         // [axes][pos_stride]
+    int64_t pos_stride;
+    const float* inv_freq;            // [rot / 2]
+    int64_t n_tokens;
+    int32_t num_q_heads, num_kv_heads, rot;
+    int32_t units_q, units, units_per_warp, warps_per_token;  // a unit = the rows one warp holds at once
+    float eps;
+    const float *dq, *dk;             // backward: [tokens][heads][D] contiguous
+    float* dw_partial;                // backward: [grid][2][D], or NULL
+    uint8_t axis[kMaxPairs];
+};
+
+// cos and sin of this token's angles.  The angle is reduced in 64 bits (position * frequency loses whole radians in 32
+// bits at far positions): in units of half a turn, brought into [-1, 1], which 32 bits hold to 2^-25 of a half turn.
+__device__ __forceinline__ void token_angles(const Params& p, int64_t token, int lane, float2* cs) {
+    for (int i = lane; i < (p.rot >> 1); i += 32) {
+        const double pos = static_cast<double>(__ldg(p.positions + p.axis[i] * p.pos_stride + token));
+        const double half_turns = pos * (static_cast<double>(__ldg(p.inv_freq + i)) * 0.31830988618379067154);
+        const float x = static_cast<float>(half_turns - 2.0 * rint(half_turns * 0.5));
+        float s, c;
+        sincospif(x, &s, &c);
+        cs[i] = make_float2(c, s);
+    }
+    __syncwarp();
+}
+
+struct Bf16 {
+    typedef __nv_bfloat16 Elem;
+    typedef uint4 Raw;  // 8 elements
+    static __device__ __forceinline__ Raw load(const Elem* p) { return *reinterpret_cast<const uint4*>(p); }
+    static __device__ __forceinline__ Raw zero() { return make_uint4(0u, 0u, 0u, 0u); }
+    static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    // the one rounding of the pass: results to bf16, nearest-even
+    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+struct F32 {
+    typedef float Elem;
+    struct Raw { float4 a, b; };
+    static __device__ __forceinline__ Raw load(const Elem* p) {
+        const float4* v = reinterpret_cast<const float4*>(p);
+        return Raw{v[0], v[1]};
+    }
+    static __device__ __forceinline__ Raw zero() {
+        return Raw{make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+    }
+    static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
+        x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
+        x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
+    }
+    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8]) {
+        float4* v = reinterpret_cast<float4*>(p);
+        v[0] = make_float4(x[0], x[1], x[2], x[3]);
+        v[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+};
+
+// Sum over the lanes that hold one row.
+template <int kLanes>
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    return x;
+}
+
+// What a lane keeps for a whole token: where its two chunks lie in a row and the angles of its eight pairs.
+template <int D>
+struct LaneMap {
+    static constexpr int kLanes = D / 16;      // lanes per row
+    static constexpr int kRows = 32 / kLanes;  // rows (heads) a warp holds at once: one unit
+    int row, off_a, off_b;
+    bool turned;
+    __device__ __forceinline__ LaneMap(int lane, int rot) {
+        const int c = lane % kLanes, n = rot / 16;
+        row = lane / kLanes;
+        turned = c < n;
+        off_a = 8 * (turned ? c : 2 * n + 2 * (c - n));
+        off_b = turned ? off_a + rot / 2 : off_a + 8;
+    }
+    __device__ __forceinline__ void angles(const float2* cs, float (&c)[8], float (&s)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            c[i] = 1.f;
+            s[i] = 0.f;
+        }
+        if (turned) {
+            const float4* v = reinterpret_cast<const float4*>(cs + off_a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 w = v[i];
+                c[2 * i] = w.x; s[2 * i] = w.y; c[2 * i + 1] = w.z; s[2 * i + 1] = w.w;
+            }
+        }
+    }
+};
+
+template <class T, int D, bool kNorm>
+__global__ void __launch_bounds__(kWarps * 32) qk_rope_kernel(const __grid_constant__ Params p) {
+    typedef LaneMap<D> Map;
+    typedef typename T::Elem Elem;
+    constexpr int kUnroll = sizeof(Elem) == 2 ? 4 : 2;  // units whose loads are in flight together
+    __shared__ __align__(16) float2 cs_all[kWarps][kMaxPairs];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
+    const int64_t token = task / p.warps_per_token;
+    if (token >= p.n_tokens) return;
+    const int32_t u_begin = static_cast<int32_t>(task - token * p.warps_per_token) * p.units_per_warp;
+    const int32_t u_end = min(p.units, u_begin + p.units_per_warp);
+    const Map map(lane, p.rot);
+    float c[8], s[8];
+    token_angles(p, token, lane, cs_all[warp]);
+    map.angles(cs_all[warp], c, s);
+
+    auto run = [&](const Elem* src, Elem* dst, const Elem* weight, int32_t heads, int32_t u0, int32_t u1) {
+        if (u0 >= u1) return;
+        float wa[8], wb[8];
+        if (kNorm) {
+            T::unpack(T::load(weight + map.off_a), wa);
+            T::unpack(T::load(weight + map.off_b), wb);
+        }
+        for (int32_t u = u0; u < u1; u += kUnroll) {
+            typename T::Raw ra[kUnroll], rb[kUnroll];
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                const int32_t head = (u + k) * Map::kRows + map.row;
+                const bool there = u + k < u1 && head < heads;
+                ra[k] = there ? T::load(src + head * D + map.off_a) : T::zero();
+                rb[k] = there ? T::load(src + head * D + map.off_b) : T::zero();
+            }
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                if (u + k >= u1) break;
+                const int32_t head = (u + k) * Map::kRows + map.row;
+                float a[8], b[8];
+                T::unpack(ra[k], a);
+                T::unpack(rb[k], b);
+                if (kNorm) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+                    const float r = rsqrtf(row_sum<Map::kLanes>(ss) * (1.f / D) + p.eps);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        a[i] = a[i] * r * wa[i];
+                        b[i] = b[i] * r * wb[i];
+                    }
+                }
+                if (map.turned) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = a[i], y = b[i];
+                        a[i] = fmaf(x, c[i], -y * s[i]);
+                        b[i] = fmaf(y, c[i], x * s[i]);
+                    }
+                }
+                if (head < heads) {
+                    T::store(dst + head * D + map.off_a, a);
+                    T::store(dst + head * D + map.off_b, b);
+                }
+            }
+        }
+    };
+    run(static_cast<const Elem*>(p.q) + token * p.q_stride, static_cast<Elem*>(p.q_out) + token * p.q_out_stride,
+        static_cast<const Elem*>(p.q_weight), p.num_q_heads, u_begin, min(u_end, p.units_q));
+    run(static_cast<const Elem*>(p.k) + token * p.k_stride, static_cast<Elem*>(p.k_out) + token * p.k_out_stride,
+        static_cast<const Elem*>(p.k_weight), p.num_kv_heads, max(u_begin, p.units_q) - p.units_q, u_end - p.units_q);
+}
+
+// Backward.  The warps stride over (token, part) tasks and keep their sums of the weight gradient in registers; a CTA
+// leaves one partial row per tensor, which dw_reduce_kernel adds up in a fixed order: the same result from run to run.
+template <class T, int D, bool kNorm>
+__global__ void __launch_bounds__(kWarps * 32) qk_rope_bwd_kernel(const __grid_constant__ Params p) {
+    typedef LaneMap<D> Map;
+    typedef typename T::Elem Elem;
+    constexpr int kUnroll = 2;
+    __shared__ __align__(16) float2 cs_all[kWarps][kMaxPairs];
+    __shared__ float dw_all[kNorm ? kWarps : 1][2][D];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Map map(lane, p.rot);
+    const int64_t n_tasks = p.n_tokens * p.warps_per_token;
+    float dwa[2][8], dwb[2][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dwa[t][i] = dwb[t][i] = 0.f;
+
+    for (int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp; task < n_tasks;
+         task += static_cast<int64_t>(gridDim.x) * kWarps) {
+        const int64_t token = task / p.warps_per_token;
+        const int32_t u_begin = static_cast<int32_t>(task - token * p.warps_per_token) * p.units_per_warp;
+        const int32_t u_end = min(p.units, u_begin + p.units_per_warp);
+        float c[8], s[8];
+        __syncwarp();  // the previous task's angles have been read
+        token_angles(p, token, lane, cs_all[warp]);
+        map.angles(cs_all[warp], c, s);
+
+        auto run = [&](const Elem* src, const float* grad, Elem* dst, const Elem* weight, int32_t heads, int32_t u0, int32_t u1,
+                       float (&da)[8], float (&db)[8]) {
+            if (u0 >= u1) return;
+            float wa[8], wb[8];
+            if (kNorm) {
+                T::unpack(T::load(weight + map.off_a), wa);
+                T::unpack(T::load(weight + map.off_b), wb);
+            }
+            for (int32_t u = u0; u < u1; u += kUnroll) {
+                typename T::Raw ra[kUnroll], rb[kUnroll];
+                F32::Raw ga[kUnroll], gb[kUnroll];
+#pragma unroll
+                for (int k = 0; k < kUnroll; ++k) {
+                    const int32_t head = (u + k) * Map::kRows + map.row;
+                    const bool there = u + k < u1 && head < heads;
+                    if (kNorm) {
+                        ra[k] = there ? T::load(src + head * D + map.off_a) : T::zero();
+                        rb[k] = there ? T::load(src + head * D + map.off_b) : T::zero();
+                    }
+                    ga[k] = there ? F32::load(grad + head * D + map.off_a) : F32::zero();
+                    gb[k] = there ? F32::load(grad + head * D + map.off_b) : F32::zero();
+                }
+#pragma unroll
+                for (int k = 0; k < kUnroll; ++k) {
+                    if (u + k >= u1) break;
+                    const int32_t head = (u + k) * Map::kRows + map.row;
+                    float g[8], h[8];
+                    F32::unpack(ga[k], g);
+                    F32::unpack(gb[k], h);
+                    if (map.turned) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float x = g[i], y = h[i];
+                            g[i] = fmaf(x, c[i], y * s[i]);
+                            h[i] = fmaf(y, c[i], -x * s[i]);
+                        }
+                    }
+                    if (kNorm) {
+                        float a[8], b[8];
+                        T::unpack(ra[k], a);
+                        T::unpack(rb[k], b);
+                        float ss = 0.f, dot = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+                            dot = fmaf(g[i] * wa[i], a[i], fmaf(h[i] * wb[i], b[i], dot));
+                        }
+                        ss = row_sum<Map::kLanes>(ss);
+                        dot = row_sum<Map::kLanes>(dot);
+                        // a row past the last head has zero gradient and adds nothing; its r is not used (eps may be 0)
+                        const float r = head < heads ? rsqrtf(ss * (1.f / D) + p.eps) : 0.f;
+                        const float m = dot * r * (1.f / D);  // mean(g w u)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float ua = a[i] * r, ub = b[i] * r;
+                            da[i] = fmaf(g[i], ua, da[i]);
+                            db[i] = fmaf(h[i], ub, db[i]);
+                            g[i] = r * fmaf(-ua, m, g[i] * wa[i]);
+                            h[i] = r * fmaf(-ub, m, h[i] * wb[i]);
+                        }
+                    }
+                    if (head < heads) {
+                        T::store(dst + head * D + map.off_a, g);
+                        T::store(dst + head * D + map.off_b, h);
+                    }
+                }
+            }
+        };
+        run(static_cast<const Elem*>(p.q) + token * p.q_stride, p.dq + token * p.num_q_heads * D,
+            static_cast<Elem*>(p.q_out) + token * p.q_out_stride, static_cast<const Elem*>(p.q_weight), p.num_q_heads, u_begin,
+            min(u_end, p.units_q), dwa[0], dwb[0]);
+        run(static_cast<const Elem*>(p.k) + token * p.k_stride, p.dk + token * p.num_kv_heads * D,
+            static_cast<Elem*>(p.k_out) + token * p.k_out_stride, static_cast<const Elem*>(p.k_weight), p.num_kv_heads,
+            max(u_begin, p.units_q) - p.units_q, u_end - p.units_q, dwa[1], dwb[1]);
+    }
+    if (kNorm && p.dw_partial != nullptr) {
+        // over the rows of the warp, then over the warps of the CTA
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float x = dwa[t][i], y = dwb[t][i];
+#pragma unroll
+                for (int off = Map::kLanes; off < 32; off <<= 1) {
+                    x += __shfl_xor_sync(0xffffffffu, x, off);
+                    y += __shfl_xor_sync(0xffffffffu, y, off);
+                }
+                if (map.row == 0) {
+                    dw_all[warp][t][map.off_a + i] = x;
+                    dw_all[warp][t][map.off_b + i] = y;
+                }
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * D; i += kWarps * 32) {
+            float x = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) x += dw_all[w][i / D][i % D];
+            p.dw_partial[static_cast<int64_t>(blockIdx.x) * 2 * D + i] = x;
+        }
+    }
+}
+
+// dw[t][i] (+)= sum over the CTAs' partials, in 64 bits: one warp per column.
+__global__ void dw_reduce_kernel(const float* __restrict__ partial, int n, int d, float* dq_weight, float* dk_weight, int accumulate) {
+    const int col = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+    if (col >= 2 * d) return;
+    double x = 0.0;
+    for (int i = lane; i < n; i += 32) x += static_cast<double>(partial[static_cast<int64_t>(i) * 2 * d + col]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    float* dst = col < d ? dq_weight + col : dk_weight + (col - d);
+    if (lane == 0) *dst = accumulate ? static_cast<float>(static_cast<double>(*dst) + x) : static_cast<float>(x);
+}
+
+// Units per warp: a token's heads are spread over several warps only while the tokens alone do not fill the SMs (16 warps
+// each), because every warp works out its token's angles again.
+void split_heads(Params& p, int head_dim, int sms) {
+    const int rows = 32 / (head_dim / 16);
+    p.units_q = (p.num_q_heads + rows - 1) / rows;
+    p.units = p.units_q + (p.num_kv_heads + rows - 1) / rows;
+    int64_t want = p.n_tokens > 0 ? (static_cast<int64_t>(sms) * 16 + p.n_tokens - 1) / p.n_tokens : 1;
+    if (want > p.units) want = p.units;
+    p.units_per_warp = static_cast<int32_t>((p.units + want - 1) / want);
+    p.warps_per_token = (p.units + p.units_per_warp - 1) / p.units_per_warp;
+}
+
+template <class T, int D>
+rpx_status_t launch_forward(const Params& p, cudaStream_t stream) {
+    const int64_t blocks = (p.n_tokens * p.warps_per_token + kWarps - 1) / kWarps;
+    if (blocks > INT32_MAX) return RPX_ERR_SHAPE;
+    if (p.q_weight != nullptr) qk_rope_kernel<T, D, true><<<static_cast<unsigned>(blocks), kWarps * 32, 0, stream>>>(p);
+    else qk_rope_kernel<T, D, false><<<static_cast<unsigned>(blocks), kWarps * 32, 0, stream>>>(p);
+    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+}
+
+template <class T, int D>
+rpx_status_t launch_backward(const Params& p, const RopeArgs& a, int sms) {
+    int64_t blocks = (p.n_tokens * p.warps_per_token + kWarps - 1) / kWarps;
+    const int64_t cap = static_cast<int64_t>(sms) * kRopeBwdCtasPerSm;
+    if (blocks > cap) blocks = cap;
+    if (p.q_weight == nullptr) {
+        qk_rope_bwd_kernel<T, D, false><<<static_cast<unsigned>(blocks), kWarps * 32, 0, a.stream>>>(p);
+        return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+    }
+    if (blocks > 0) qk_rope_bwd_kernel<T, D, true><<<static_cast<unsigned>(blocks), kWarps * 32, 0, a.stream>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
+    if (p.dw_partial == nullptr) return RPX_OK;
+    dw_reduce_kernel<<<2 * D / 8, 256, 0, a.stream>>>(p.dw_partial, static_cast<int>(blocks), D, a.dq_weight, a.dk_weight,
+                                                      a.accumulate_dw ? 1 : 0);
+    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+}
+
+}  // namespace
+
+namespace {
+
+Params make_params(const RopeArgs& a, int sms) {
+    Params p;
+    p.q = a.q;
+    p.k = a.k;
+    p.q_out = a.q_out;
+    p.k_out = a.k_out;
+    p.q_stride = a.q_tok_stride;
+    p.k_stride = a.k_tok_stride;
+    p.q_out_stride = a.q_out_tok_stride;
+    p.k_out_stride = a.k_out_tok_stride;
+    p.q_weight = a.q_weight;
+    p.k_weight = a.k_weight;
+    p.positions = a.positions;
+    p.pos_stride = a.pos_axis_stride;
+    p.inv_freq = a.inv_freq;
+    p.n_tokens = a.n_tokens;
+    p.num_q_heads = a.desc->num_q_heads;
+    p.num_kv_heads = a.desc->num_kv_heads;
+    p.rot = a.desc->rot_dim;
+    p.eps = a.desc->eps;
+    p.dq = a.dq;
+    p.dk = a.dk;
+    p.dw_partial = a.dq_weight != nullptr ? static_cast<float*>(a.workspace) : nullptr;
+    for (int i = 0; i < kMaxPairs; ++i)
+        p.axis[i] = a.desc->pair_axis != nullptr && i < p.rot / 2 ? a.desc->pair_axis[i] : 0;
+    split_heads(p, a.desc->head_dim, sms);
+    return p;
+}
+
+}  // namespace
+
+size_t rope_backward_workspace(int32_t head_dim) {
+    return static_cast<size_t>(kRopeBwdMaxCtas) * 2 * head_dim * sizeof(float);
+}
+
+rpx_status_t launch_qk_rope(const RopeArgs& a) {
+    const int sms = sm_count();
+    if (sms <= 0) return RPX_ERR_CUDA;
+    const Params p = make_params(a, sms);
+    const bool bf16 = a.desc->dtype == RPX_BF16;
+    if (a.desc->head_dim == 128) return bf16 ? launch_forward<Bf16, 128>(p, a.stream) : launch_forward<F32, 128>(p, a.stream);
+    return bf16 ? launch_forward<Bf16, 64>(p, a.stream) : launch_forward<F32, 64>(p, a.stream);
+}
+
+rpx_status_t launch_qk_rope_backward(const RopeArgs& a) {
+    int sms = sm_count();
+    if (sms <= 0) return RPX_ERR_CUDA;
+    if (sms > kRopeBwdMaxCtas / kRopeBwdCtasPerSm) sms = kRopeBwdMaxCtas / kRopeBwdCtasPerSm;
+    const Params p = make_params(a, sms);
+    const bool bf16 = a.desc->dtype == RPX_BF16;
+    if (a.desc->head_dim == 128) return bf16 ? launch_backward<Bf16, 128>(p, a, sms) : launch_backward<F32, 128>(p, a, sms);
+    return bf16 ? launch_backward<Bf16, 64>(p, a, sms) : launch_backward<F32, 64>(p, a, sms);
+}
+
+}  // namespace rpx
