@@ -165,6 +165,35 @@ RPX_API rpx_status_t rpx_chunk_attn(const rpx_attn_desc_t* desc, const void* q, 
                             size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
 
 /*
+ * Attention of a tree of drafted tokens over the cache (an extension: drafting and verifying several continuations of a
+ * cached prefix in one pass; a tree of one node is a decoding step).  Sequence s owns tokens cu_seqlens_tree[s] ..
+ * cu_seqlens_tree[s+1]-1, its nodes; node i attends to the cached_lens[s] keys in the cache, to its ancestors in the tree
+ * and to itself.
+ *   parents: device int32 [total_tree_tokens], per node the number WITHIN its sequence of the node it continues
+ *       (0 <= parent < i), -1: it continues the cached prefix, below -1: the node is not in use (padding).  A node not in
+ *       use has out = 0 and lse = -inf, is nobody's ancestor, and its k, v may hold anything.  A parent that is not an
+ *       earlier node in use sets RPX_ERR_DEVICE_DATA in *device_status; that node and those behind it count as not in use.
+ *   cached_lens device int32 [batch]: any length, 0 included.  Slots of the cache behind it may hold anything.
+ *   q, k, v, strides, out, lse, cache: as in rpx_suffix_attn.  The tree's K, V are not stored: rpx_cache_append stores
+ *       those of the accepted path.  Values of nodes in use are finite: a non-finite one reaches all rows of its sequence.
+ *   max_tree_len: upper bound of a sequence's nodes, at most RPX_TREE_MAX_NODES; a longer sequence is reported
+ *       (RPX_ERR_DEVICE_DATA) and skipped, as is one whose offsets leave the packed tensors or the block table.
+ *   max_cached_len: upper bound of cached_lens (sizes the grid only)
+ *   workspace: rpx_tree_attn_workspace_bytes with the same total_tree_tokens, batch and max_tree_len
+ * Results do not depend on the order in which the GPU runs the pieces: the same call gives the same bits.  Trees of up to
+ * 128 nodes are not capped by rpx_set_sm_budget.
+ */
+#define RPX_TREE_MAX_NODES 1024
+RPX_API rpx_status_t rpx_tree_attn(const rpx_attn_desc_t* desc, const void* q, const void* k, const void* v,
+                                   int64_t q_tok_stride, int64_t k_tok_stride, int64_t v_tok_stride,
+                                   const int32_t* cu_seqlens_tree, const int32_t* parents, const int32_t* cached_lens,
+                                   int32_t batch, int64_t total_tree_tokens, int32_t max_tree_len, int32_t max_cached_len,
+                                   const rpx_kv_cache_t* cache, void* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
+RPX_API size_t rpx_tree_attn_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_tree_tokens, int32_t batch,
+                                             int32_t max_tree_len);
+
+/*
  * Fused LM-head log-probabilities (Section 3.1: Phase 1 yields the log-probabilities of the prefix
  * positions, Phase 2 those of the suffix; Table 4, row on prefix log-probabilities).  For every row n:
  *     z_v = hidden[n,:] . w_vocab[v,:]          (never stored)

@@ -31,5 +31,7 @@ from .binding import (  # noqa: F401
     token_logprobs_shard,
     token_logprobs_static,
     token_logprobs_workspace_bytes,
+    tree_attn,
+    tree_attn_workspace_bytes,
     version,
 )

@@ -17,11 +17,14 @@ _lib = None
 RPX_BF16, RPX_F32 = 0, 1
 BLOCK_SIZE = 16
 STATIC_SCRATCH_BYTES = 8 << 20
+TREE_MAX_NODES = 1024
 
 EXPORTS = (
     "rpx_prefix_attn",
     "rpx_suffix_attn",
     "rpx_chunk_attn",
+    "rpx_tree_attn",
+    "rpx_tree_attn_workspace_bytes",
     "rpx_token_logprobs",
     "rpx_token_logprobs_entropy",
     "rpx_token_logprobs_shard",
@@ -113,6 +116,11 @@ def load_library():
     lib.rpx_chunk_attn.restype = i32
     lib.rpx_chunk_attn.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, i64, i64, i64, vp, vp, i32, i64, i32,
                                     i32, ctypes.POINTER(KvCache), vp, vp, vp, sz, vp, vp]
+    lib.rpx_tree_attn.restype = i32
+    lib.rpx_tree_attn.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, i64, i64, i64, vp, vp, vp, i32, i64, i32, i32,
+                                  ctypes.POINTER(KvCache), vp, vp, vp, sz, vp, vp]
+    lib.rpx_tree_attn_workspace_bytes.restype = sz
+    lib.rpx_tree_attn_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i64, i32, i32]
     lib.rpx_token_logprobs.restype = i32
     lib.rpx_token_logprobs.argtypes = [vp, i64, vp, vp, i64, i32, i32, i32, vp, vp, vp, sz, vp, vp]
     lib.rpx_token_logprobs_entropy.restype = i32
@@ -377,6 +385,44 @@ def chunk_attn(q, k, v, cu_seqlens_chunk, cached_lens, max_chunk_len: int, max_c
                              _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_chunk_attn")
+    return (out, lse) if return_lse else out
+
+
+def tree_attn_workspace_bytes(num_q_heads, num_kv_heads, head_dim, dtype_code, total_tokens, batch, max_tree_len) -> int:
+    d = AttnDesc(num_q_heads, num_kv_heads, head_dim, 0.0, dtype_code)
+    return int(load_library().rpx_tree_attn_workspace_bytes(ctypes.byref(d), int(total_tokens), int(batch), int(max_tree_len)))
+
+
+@_in_call_context
+def tree_attn(q, k, v, cu_seqlens_tree, parents, cached_lens, max_tree_len: int, max_cached_len: int, cache: Tuple,
+              softmax_scale: float = 0.0, out=None, lse=None, return_lse: bool = False, workspace=None, device_status=None,
+              stream=None):
+    """rpx_tree_attn: nodes of a tree of drafted tokens over [cached keys ; ancestors and itself]; one node per sequence is a
+    decoding step.
+
+    parents int32 [T]: the node (numbered within its sequence) each node continues, -1 = the cached prefix, -2 = padding
+    (out 0, lse -inf).  Other arguments as in ``suffix_attn``."""
+    torch = _torch()
+    lib = load_library()
+    desc = _desc(q, k, softmax_scale)
+    total, batch = q.shape[0], cu_seqlens_tree.shape[0] - 1
+    if any(t.dtype != torch.int32 or not t.is_contiguous() for t in (cu_seqlens_tree, parents, cached_lens)):
+        raise TypeError("cu_seqlens_tree, parents and cached_lens are contiguous int32 tensors")
+    if parents.shape[0] != total or cached_lens.shape[0] != batch:
+        raise ValueError("parents has one entry per token and cached_lens one per sequence")
+    if out is None:
+        out = torch.empty((total, q.shape[1], q.shape[2]), dtype=q.dtype, device=q.device)
+    if lse is None and return_lse:
+        lse = torch.empty((total, q.shape[1]), dtype=torch.float32, device=q.device)
+    ws = _workspace(int(lib.rpx_tree_attn_workspace_bytes(ctypes.byref(desc), total, batch, int(max_tree_len))), q.device,
+                    workspace)
+    cs = _cache_struct(cache)
+    rc = lib.rpx_tree_attn(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _tok_stride(q), _tok_stride(k), _tok_stride(v),
+                           _ptr(cu_seqlens_tree), _ptr(parents), _ptr(cached_lens), batch, total, int(max_tree_len),
+                           int(max_cached_len), ctypes.byref(cs), _ptr(out), _ptr(lse), _ptr(ws),
+                           ws.numel() * ws.element_size(), _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_tree_attn")
     return (out, lse) if return_lse else out
 
 

@@ -39,15 +39,39 @@ rpx_status_t check_cache(const rpx_kv_cache_t* c, int32_t batch) {
     return RPX_OK;
 }
 
-// Shared body of the two attention entry points.  prefix_lens == NULL selects the prefix pass.
+// Workspace of a tree pass.  Streaming form: its own.  Otherwise the suffix pass's, then the ancestor sets, then (bf16) the
+// tree's values with unused rows cleared.
+struct TreeWorkspace {
+    bool streams;
+    size_t sets_off, values_off, bytes;
+};
+TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t max_tree) {
+    TreeWorkspace w = {};
+    if (d == nullptr || tokens <= 0 || batch <= 0 || max_tree <= 0 || d->num_kv_heads <= 0) return w;
+    w.streams = d->dtype == RPX_BF16 && tree_streams(max_tree, d->num_q_heads / d->num_kv_heads);
+    if (w.streams) {
+        w.bytes = align_up(tree_stream_workspace(batch, d->head_dim), kWsAlign);
+        return w;
+    }
+    w.sets_off = align_up(attn_workspace(d, tokens, true), kWsAlign);
+    w.values_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
+    w.bytes = w.values_off;
+    if (d->dtype == RPX_BF16) w.bytes += align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
+    return w;
+}
+
+// Shared body of the attention entry points.  prefix_lens == NULL selects the prefix pass, parents != NULL
+// (with is_suffix) a tree of drafted tokens.
 rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const void* k, const void* v,
                            int64_t q_tok_stride, int64_t k_tok_stride, int64_t v_tok_stride, const int32_t* cu_seqlens,
                            const int32_t* prefix_lens, bool is_suffix, bool append_cache, int32_t batch, int64_t total_tokens,
                            int32_t max_q_len, int32_t max_prefix_len, const rpx_kv_cache_t* cache, void* out, float* lse,
-                           void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream) {
+                           void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream,
+                           bool is_tree = false, const int32_t* parents = nullptr) {
     if (rpx_status_t rc = check_attn_desc(desc)) return rc;
     if (batch < 0 || total_tokens < 0 || max_q_len < 0 || max_prefix_len < 0) return RPX_ERR_SHAPE;
     if (total_tokens >= INT32_MAX) return RPX_ERR_SHAPE;
+    if (is_tree && max_q_len > RPX_TREE_MAX_NODES) return RPX_ERR_SHAPE;
     if (is_suffix) {
         if (cache == nullptr) return RPX_ERR_NULL;
         if (batch > 0 && prefix_lens == nullptr) return RPX_ERR_NULL;
@@ -56,12 +80,14 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
         if (rpx_status_t rc = check_cache(cache, batch)) return rc;
     if (batch == 0 || total_tokens == 0 || max_q_len == 0) return RPX_OK;
     if (q == nullptr || k == nullptr || v == nullptr || out == nullptr || cu_seqlens == nullptr) return RPX_ERR_NULL;
+    if (is_tree && parents == nullptr) return RPX_ERR_NULL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return RPX_ERR_ALIGN;
     const int64_t q_row = static_cast<int64_t>(desc->num_q_heads) * desc->head_dim;
     const int64_t kv_row = static_cast<int64_t>(desc->num_kv_heads) * desc->head_dim;
     if (q_tok_stride < q_row || k_tok_stride < kv_row || v_tok_stride < kv_row) return RPX_ERR_SHAPE;
     if (q_tok_stride % 8 || k_tok_stride % 8 || v_tok_stride % 8) return RPX_ERR_ALIGN;
-    const size_t need = attn_workspace(desc, total_tokens, is_suffix);
+    const TreeWorkspace tree_ws = is_tree ? tree_workspace(desc, total_tokens, batch, max_q_len) : TreeWorkspace{};
+    const size_t need = is_tree ? tree_ws.bytes : attn_workspace(desc, total_tokens, is_suffix);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return RPX_ERR_WORKSPACE;
     if (need > 0 && !aligned_ws(workspace)) return RPX_ERR_ALIGN;
     if (rpx_status_t rc = check_arch()) return rc;
@@ -93,6 +119,43 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
     a.lse = lse;
     a.device_status = device_status;
     a.stream = stream;
+    if (is_tree) {
+        TreeArgs t;
+        t.num_q_heads = desc->num_q_heads;
+        t.num_kv_heads = desc->num_kv_heads;
+        t.head_dim = desc->head_dim;
+        t.softmax_scale = desc->softmax_scale;
+        t.q = q;
+        t.k = k;
+        t.v = v;
+        t.q_tok_stride = q_tok_stride;
+        t.k_tok_stride = k_tok_stride;
+        t.v_tok_stride = v_tok_stride;
+        t.cu_seqlens = cu_seqlens;
+        t.parents = parents;
+        t.cached_lens = prefix_lens;
+        t.batch = batch;
+        t.total_tokens = total_tokens;
+        t.max_tree = max_q_len;
+        t.max_cached = max_prefix_len;
+        t.cache = cache;
+        t.out = out;
+        t.lse = lse;
+        t.workspace = workspace;
+        t.device_status = device_status;
+        t.stream = stream;
+        if (tree_ws.streams) return launch_tree_stream(t);
+        uint8_t* ws = static_cast<uint8_t*>(workspace);
+        uint32_t* sets = reinterpret_cast<uint32_t*>(ws + tree_ws.sets_off);
+        void* values = desc->dtype == RPX_BF16 ? ws + tree_ws.values_off : nullptr;
+        if (rpx_status_t rc = launch_tree_sets(t, sets, values)) return rc;
+        a.tree_sets = sets;
+        a.tree_words = tree_set_words(max_q_len);
+        if (values != nullptr) {
+            a.v = values;
+            a.v_tok_stride = kv_row;
+        }
+    }
     // fp32 tensors take the fp32 CUDA-core path; out is then float32 and 16-byte alignment is all the tensors need
     if (desc->dtype == RPX_F32) return launch_attention_f32(a);
     return launch_attention(a);
@@ -139,6 +202,21 @@ rpx_status_t rpx_chunk_attn(const rpx_attn_desc_t* desc, const void* q, const vo
 
 size_t rpx_suffix_attn_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_suffix_tokens) {
     return attn_workspace(desc, total_suffix_tokens, true);
+}
+
+rpx_status_t rpx_tree_attn(const rpx_attn_desc_t* desc, const void* q, const void* k, const void* v, int64_t q_tok_stride,
+                           int64_t k_tok_stride, int64_t v_tok_stride, const int32_t* cu_seqlens_tree, const int32_t* parents,
+                           const int32_t* cached_lens, int32_t batch, int64_t total_tree_tokens, int32_t max_tree_len,
+                           int32_t max_cached_len, const rpx_kv_cache_t* cache, void* out, float* lse, void* workspace,
+                           size_t workspace_bytes, int32_t* device_status, void* cuda_stream) {
+    return run_attention(desc, q, k, v, q_tok_stride, k_tok_stride, v_tok_stride, cu_seqlens_tree, cached_lens, true, false,
+                         batch, total_tree_tokens, max_tree_len, max_cached_len, cache, out, lse, workspace, workspace_bytes,
+                         device_status, cuda_stream, true, parents);
+}
+
+size_t rpx_tree_attn_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_tree_tokens, int32_t batch,
+                                     int32_t max_tree_len) {
+    return tree_workspace(desc, total_tree_tokens, batch, max_tree_len).bytes;
 }
 
 size_t rpx_token_logprobs_workspace_bytes(int64_t n_tokens, int32_t hidden_dim, int32_t vocab, rpx_dtype_t dtype) {

@@ -37,6 +37,8 @@ struct Params {
     int32_t block_table_stride;
     int32_t num_blocks;
     int32_t write_cache;         // store this call's K/V behind the cached prefix
+    const uint32_t* tree_sets;   // nullable: [tokens][tree_words], the self keys each query token may see
+    int32_t tree_words;
     float scale_log2;
     float* out;                  // [tokens][H_q][d]
     float* lse;                  // nullable
@@ -58,11 +60,11 @@ __global__ void __launch_bounds__(kRowsPerCta * 32) attn_f32_kernel(const Params
     const int32_t kv_head = head / p.group;
     const int32_t tok0 = __ldg(p.cu_seqlens + seq);
     const int32_t len_q = __ldg(p.cu_seqlens + seq + 1) - tok0;
-    const int32_t len_p = p.prefix_lens != nullptr ? __ldg(p.prefix_lens + seq) : 0;
+    const int32_t len_p = p.prefix_lens != nullptr && !(p.tree_sets != nullptr && len_q == 0) ? __ldg(p.prefix_lens + seq) : 0;
     // the same checks as the tensor-core path: offsets that leave the packed tensors, more pages than a row of the
     // block table, a sequence longer than the caller's bound, an append that does not start on a page edge
     const int64_t table_tokens = static_cast<int64_t>(len_p) + (p.write_cache != 0 ? len_q : 0);
-    bool bad = tok0 < 0 || len_q < 0 || static_cast<int64_t>(tok0) + len_q > p.total_tokens || len_p < 0 ||
+    bool bad = tok0 < 0 || len_q < 0 || (p.tree_sets != nullptr && len_q > p.row_bound) || static_cast<int64_t>(tok0) + len_q > p.total_tokens || len_p < 0 ||
                (p.block_table != nullptr && (table_tokens + kPage - 1) / kPage > p.block_table_stride);
     bool flag = bad || (!bad && len_q > p.row_bound);
     const bool write = p.write_cache != 0 && !bad && (len_p % kPage) == 0;
@@ -76,6 +78,13 @@ __global__ void __launch_bounds__(kRowsPerCta * 32) attn_f32_kernel(const Params
         atomicCAS(p.status, 0, RPX_ERR_DEVICE_DATA);
 
     const int64_t tok = static_cast<int64_t>(tok0) + i;
+    const uint32_t* set = p.tree_sets != nullptr ? p.tree_sets + tok * p.tree_words : nullptr;
+    if (set != nullptr && ((__ldg(set + (i >> 5)) >> (i & 31)) & 1u) == 0u) {  // a node that is not in use
+#pragma unroll
+        for (int u = 0; u < U; ++u) p.out[(tok * p.num_q_heads + head) * D + u * 32 + lane] = 0.f;
+        if (p.lse != nullptr && lane == 0) p.lse[tok * p.num_q_heads + head] = -CUDART_INF_F;
+        return;
+    }
     float qv[U], acc[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -114,6 +123,7 @@ __global__ void __launch_bounds__(kRowsPerCta * 32) attn_f32_kernel(const Params
     }
     // ---- the call's own keys, causal
     for (int32_t j = 0; j <= i; ++j) {
+        if (set != nullptr && ((__ldg(set + (j >> 5)) >> (j & 31)) & 1u) == 0u) continue;  // not an ancestor
         const int64_t t = static_cast<int64_t>(tok0) + j;
         float kr[U], vr[U];
 #pragma unroll
@@ -165,7 +175,10 @@ rpx_status_t launch_attention_f32(const AttnArgs& a) {
     p.num_kv_heads = a.num_kv_heads;
     p.group = a.num_q_heads / a.num_kv_heads;
     p.total_tokens = a.total_tokens;
-    p.row_bound = (a.max_q_len + 255) / 256 * 256;  // the bf16 path's bound: whole pairs of 128-row tiles
+    p.tree_sets = a.tree_sets;
+    p.tree_words = a.tree_words;
+    // the bf16 path's bound: whole pairs of 128-row tiles, or a tree's own bound
+    p.row_bound = a.tree_sets != nullptr ? a.max_q_len : (a.max_q_len + 255) / 256 * 256;
     p.k_cache = a.cache != nullptr ? static_cast<__nv_bfloat16*>(a.cache->k_cache) : nullptr;
     p.v_cache = a.cache != nullptr ? static_cast<__nv_bfloat16*>(a.cache->v_cache) : nullptr;
     p.block_table = a.cache != nullptr ? a.cache->block_table : nullptr;

@@ -1,0 +1,748 @@
+// Attention of a tree of drafted tokens over [cached prefix ; ancestors in the tree], for few rows: the streaming form.
+//
+// For node i of a sequence, query head h and KV head g = h / group, over the cached keys 0 .. len - 1 and the nodes j on
+// the path from i to its root (i included):   out = sum_j softmax_j(scale * q . k_j) v_j.
+//
+// With few nodes (one is a decoding step) this is bound by reading the cache: every cached K and V is read once per block of
+// up to 64 rows (row = node * group + head within the KV head's group), 512 bytes per key against rows * 512 flops.  So
+// the work is laid out along the keys.  All key tiles (64 keys) of all (sequence, KV head, row block) segments are
+// numbered in a line, and every CTA of one resident wave takes an equal piece of that line: a single long sequence
+// spreads over all SMs as evenly as a ragged batch does.  A CTA that holds a whole segment writes its rows; pieces of a
+// segment leave (maximum, sum, un-normalised row) in the workspace and tree_join_kernel adds them up in the order of the
+// keys, so results do not depend on which CTA ran when.
+//   warp 4     : producer; one TMA box per 16-token page and tensor (both 64-element halves of its rows in one box,
+//                128-byte swizzle), three stages of 64 keys of K and V
+//   warps 0-3  : S = Q K^T and O += P V with mma.sync (16 rows x 8 keys x 16): at these row counts the tensor rate is not
+//                what bounds, and a 16-row tile wastes least of it.  A block is 16, 32 or 64 rows; the four warps are
+//                kRowTiles row tiles x 4 / kRowTiles ranges of the tile's keys, and join their ranges in shared memory
+//                at the end of a segment.
+// Scores are kept in log2 units, the running maximum is raised lazily (by steps of at least 2^8), sums are fp32.
+#include <math_constants.h>
+
+#include "rpx_internal.h"
+#include "rpx_ptx.cuh"
+
+namespace rpx {
+
+namespace {
+
+constexpr int kPage = 16, kTile = 64, kStages = 3;
+constexpr int kWarps = 4;  // consumer warps
+constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kCtasPerSm = 2;
+constexpr int kMinTiles = 2;     // key tiles a CTA takes at least: below that the join costs more than the spread gains
+constexpr int kMaxNodes = 128;   // nodes per sequence this form takes (their ancestor sets live in shared memory)
+constexpr int kMaskWords = kMaxNodes / 32;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRaise = 8.0f;
+
+struct Params {
+    const __nv_bfloat16* q;
+    int64_t q_stride;
+    const int32_t *cu, *parents, *lens;
+    const int32_t* block_table;
+    int32_t block_table_stride, num_blocks;
+    int32_t batch, num_q_heads, num_kv_heads, group, max_tree;
+    int64_t total_tokens;
+    int32_t ctas;          // CTAs the line of tiles is cut for (the grid)
+    float scale_log2;
+    __nv_bfloat16* out;    // [tokens][H_q][D]
+    float* lse;            // nullable
+    int64_t* seq_tile0;    // workspace [batch + 1]: number of the sequence's first tile; the last entry is the total
+    float2* part_ml;       // workspace [ctas][2][rows per block]
+    float* part_o;         // workspace [ctas][2][rows per block][D]
+    int32_t* status;
+};
+
+struct Ctl {
+    uint64_t full[kStages], empty[kStages];
+    int64_t warp_sum[kWarps + 1];
+    int64_t start_off;
+    int32_t start_seq;
+    uint32_t issued;  // tiles the producer has asked for
+    uint32_t abort_flag, drain_flag, data_error;
+    float2 ml[kWarps][16];
+    uint32_t anc[kMaxNodes][kMaskWords];  // ancestors and itself; all zero for a node that is not in use
+};
+
+template <int D>
+struct Layout {
+    static constexpr int kPageBytes = kPage * D * 2;
+    static constexpr int kTensorBytes = kTile * D * 2;
+    static constexpr int kStageBytes = 2 * kTensorBytes;
+    static constexpr int kCtlOff = kStages * kStageBytes;
+    static constexpr size_t kSmemBytes = kCtlOff + sizeof(Ctl);
+};
+
+// shared-memory offset of 16-byte chunk c of key r within a tile: pages of [half][16 rows][128 bytes], swizzled
+template <int D>
+__device__ __forceinline__ uint32_t key_off(int r, int c) {
+    return (r >> 4) * Layout<D>::kPageBytes + (c >> 3) * (kPage * 128) + (r & 15) * 128 + (((c & 7) ^ (r & 7)) << 4);
+}
+
+struct Seq {
+    int32_t tok0, n, len;         // first token, nodes, cached tokens
+    int32_t cached_tiles, tiles;  // key tiles of one segment: cached ones, then the tree's own
+    int32_t blocks;               // row blocks
+    __device__ __forceinline__ int64_t work(const Params& p) const { return static_cast<int64_t>(tiles) * blocks * p.num_kv_heads; }
+};
+
+// Offsets that leave the packed tensors or the block table, and a tree larger than the caller's bound, make a sequence
+// count as empty (its rows are left as they were) and are reported.
+template <int kRows>
+__device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* data_error) {
+    Seq q;
+    q.tok0 = __ldg(p.cu + s);
+    q.n = __ldg(p.cu + s + 1) - q.tok0;
+    q.len = __ldg(p.lens + s);
+    const bool bad = q.tok0 < 0 || q.n < 0 || static_cast<int64_t>(q.tok0) + q.n > p.total_tokens || q.n > p.max_tree ||
+                     (q.n > 0 && (q.len < 0 || (static_cast<int64_t>(q.len) + kPage - 1) / kPage > p.block_table_stride));
+    if (bad) {
+        if (data_error != nullptr) *data_error = 1;
+        q.n = 0;
+    }
+    if (q.n == 0) q.len = 0;
+    q.cached_tiles = q.len / kTile + (q.len % kTile != 0 ? 1 : 0);
+    q.tiles = q.n > 0 ? q.cached_tiles + (q.n + kTile - 1) / kTile : 0;
+    q.blocks = (q.n * p.group + kRows - 1) / kRows;
+    return q;
+}
+
+// The line of `total` tiles is cut into `pieces` nearly equal pieces, piece c = [begin(c), begin(c + 1)).
+__device__ __forceinline__ int64_t pieces_of(int64_t total, int32_t ctas) {
+    const int64_t most = total / kMinTiles;
+    return most < 1 ? 1 : most < ctas ? most : ctas;
+}
+__device__ __forceinline__ int64_t piece_begin(int64_t total, int64_t pieces, int64_t c) { return total * c / pieces; }
+__device__ __forceinline__ int64_t piece_of(int64_t total, int64_t pieces, int64_t tile) {
+    return ((tile + 1) * pieces - 1) / total;
+}
+
+__device__ __forceinline__ int64_t warp_scan(int64_t x, int lane) {  // inclusive
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
+// Inclusive sum over the CTA's threads; `all` receives the total.
+__device__ __forceinline__ int64_t block_scan(int64_t x, Ctl* ctl, int warp, int lane, int64_t* all) {
+    x = warp_scan(x, lane);
+    __syncthreads();
+    if (lane == 31) ctl->warp_sum[warp] = x;
+    __syncthreads();
+    int64_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w <= kWarps; ++w) {
+        const int64_t v = ctl->warp_sum[w];
+        if (w < warp) before += v;
+        total += v;
+    }
+    *all = total;
+    return x + before;
+}
+
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// Walks the pieces of segments inside this CTA's part of the line; every warp walks it alike.
+template <int kRows>
+struct Walk {
+    int32_t s, head, block, t0, t1;  // current segment: sequence, KV head, row block, key tiles [t0, t1)
+    Seq q;
+    int64_t pos, end, off;
+    bool have;
+    __device__ __forceinline__ Walk(int32_t s0, int64_t off0, int64_t begin, int64_t end_) : s(s0), pos(begin), end(end_), off(off0), have(false) {}
+    __device__ __forceinline__ bool next(const Params& p) {
+        while (pos < end && s < p.batch) {
+            if (!have) {
+                q = read_seq<kRows>(p, s, nullptr);
+                have = true;
+            }
+            if (off >= q.work(p)) {
+                ++s;
+                off = 0;
+                have = false;
+                continue;
+            }
+            const int32_t seg = static_cast<int32_t>(off / q.tiles);
+            t0 = static_cast<int32_t>(off - static_cast<int64_t>(seg) * q.tiles);
+            t1 = static_cast<int32_t>(min(static_cast<int64_t>(q.tiles), t0 + (end - pos)));
+            head = seg / q.blocks;
+            block = seg - head * q.blocks;
+            pos += t1 - t0;
+            off += t1 - t0;
+            return true;
+        }
+        return false;
+    }
+};
+
+template <int D, int kRowTiles>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                   const __grid_constant__ CUtensorMap tmap_kc, const __grid_constant__ CUtensorMap tmap_vc, const Params p) {
+    using L = Layout<D>;
+    constexpr int kRows = 16 * kRowTiles;
+    constexpr int kRanges = kWarps / kRowTiles;  // key ranges of a tile the warps work on side by side
+    constexpr int kSteps = kTile / kRanges / 16; // 16-key steps of one range
+    extern __shared__ __align__(1024) uint8_t smem[];
+    if ((smem_u32(smem) & 1023u) != 0u) {  // swizzled pages need 1024-byte alignment; never expected
+        if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, RPX_ERR_CUDA);
+        return;
+    }
+    Ctl* ctl = reinterpret_cast<Ctl*>(smem + L::kCtlOff);
+    volatile uint32_t* abort_flag = &ctl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&ctl->full[i], 1);
+            mbar_init(&ctl->empty[i], kWarps);
+        }
+        ctl->abort_flag = ctl->drain_flag = ctl->data_error = 0;
+        ctl->issued = 0;
+        ctl->start_seq = p.batch;
+        ctl->start_off = 0;
+        fence_barrier_init();
+    }
+    __syncthreads();
+
+    // ---- this CTA's piece of the line: the total first, then the sequence that holds the piece's first tile
+    uint32_t* report = blockIdx.x == 0 ? &ctl->data_error : nullptr;
+    int64_t total = 0, all = 0, first_work = 0, first_sum = 0;
+    for (int32_t base = 0; base < p.batch; base += kThreads) {
+        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
+        const int64_t w = s < p.batch ? read_seq<kRows>(p, s, report).work(p) : 0;
+        const int64_t sum = block_scan(w, ctl, warp, lane, &all);
+        if (base == 0) {
+            first_work = w;
+            first_sum = sum;
+        }
+        total += all;
+    }
+    const int64_t pieces = pieces_of(total, p.ctas);
+    const int64_t cta = blockIdx.x;
+    const int64_t begin = cta < pieces ? piece_begin(total, pieces, cta) : 0;
+    const int64_t end = cta < pieces ? piece_begin(total, pieces, cta + 1) : 0;
+    int64_t carry = 0;
+    for (int32_t base = 0; base < p.batch; base += kThreads) {
+        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
+        int64_t w = first_work, sum = first_sum;
+        if (base > 0 || p.batch > kThreads) {
+            w = s < p.batch ? read_seq<kRows>(p, s, nullptr).work(p) : 0;
+            sum = block_scan(w, ctl, warp, lane, &all);
+        }
+        const int64_t before = carry + sum - w;
+        if (s < p.batch) {
+            if (begin >= before && begin < before + w) {
+                ctl->start_seq = s;
+                ctl->start_off = begin - before;
+            }
+            if (blockIdx.x == 0) p.seq_tile0[s] = before;
+        }
+        carry += all;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.seq_tile0[p.batch] = total;
+    __syncthreads();
+
+    Walk<kRows> walk(ctl->start_seq, ctl->start_off, begin, end);
+    uint32_t it = 0;  // tiles this warp has been through (ring position)
+    bool ok = true;
+
+    if (warp == kWarps) {
+        // =========================================================== producer
+        while (ok && walk.next(p)) {
+            const int32_t pg = lane & 3;
+            const int32_t* table = p.block_table + static_cast<int64_t>(walk.s) * p.block_table_stride;
+            const int32_t pages = (walk.q.len + kPage - 1) / kPage;
+            auto read_block = [&](int32_t t) { return t * 4 + pg < pages ? __ldg(table + t * 4 + pg) : 0; };
+            int32_t next_block = walk.t0 < walk.q.cached_tiles ? read_block(walk.t0) : 0;
+            for (int32_t t = walk.t0; t < walk.t1; ++t, ++it) {
+                const uint32_t st = it % kStages;
+                if (!mbar_wait(&ctl->empty[st], ((it / kStages) & 1u) ^ 1u, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                uint8_t* dst = smem + st * L::kStageBytes + (lane >> 2) * L::kTensorBytes + pg * L::kPageBytes;
+                const bool cached = t < walk.q.cached_tiles;
+                int32_t block = next_block;
+                const int32_t own = t - walk.q.cached_tiles;  // the tree's own tile number
+                const int32_t boxes = cached ? min(4, pages - t * 4) : min(4, (walk.q.n - own * kTile + kPage - 1) / kPage);
+                if (cached) {
+                    if (block < 0 || block >= p.num_blocks) {
+                        ctl->data_error = 1;
+                        block = 0;
+                    }
+                    if (t + 1 < walk.q.cached_tiles && t + 1 < walk.t1) next_block = read_block(t + 1);
+                }
+                if (lane == 0) mbar_arrive_expect_tx(&ctl->full[st], static_cast<uint32_t>(boxes) * 2 * L::kPageBytes);
+                __syncwarp();  // the byte count is armed before any copy can complete
+                if (lane < 8 && pg < boxes) {  // lanes 0-3: the pages of K, lanes 4-7: those of V
+                    if (cached) tma_load_5d(dst, lane < 4 ? &tmap_kc : &tmap_vc, &ctl->full[st], 0, 0, 0, walk.head, block);
+                    else tma_load_4d(dst, lane < 4 ? &tmap_k : &tmap_v, &ctl->full[st], 0, walk.q.tok0 + own * kTile + pg * kPage, 0, walk.head);
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) ctl->issued = it;
+    } else {
+        // =========================================================== consumers
+        // After a wait that ran out (ok == false) a warp goes through the rest of its walk without waiting: every warp
+        // still meets the others at the same barriers, and the outputs of the call are undefined anyway.
+        const int rt = warp % kRowTiles, range = warp / kRowTiles;
+        const int gid = lane >> 2, tid = lane & 3;
+        while (walk.next(p)) {
+            const Seq q = walk.q;
+            const int32_t rows = q.n * p.group, row0 = walk.block * kRows;
+            // ---- Q of the warp's 16 rows, as A operands
+            uint32_t qf[D / 16][4];
+            int32_t node[2];
+            {
+                const __nv_bfloat16* src[2];
+                bool there[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int32_t r = row0 + rt * 16 + gid + 8 * u;
+                    there[u] = r < rows;
+                    node[u] = there[u] ? r / p.group : 0;
+                    src[u] = p.q + (static_cast<int64_t>(q.tok0) + node[u]) * p.q_stride +
+                             (static_cast<int64_t>(walk.head) * p.group + (there[u] ? r - node[u] * p.group : 0)) * D + 2 * tid;
+                }
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        qf[ks][e] = there[e & 1] ? __ldg(reinterpret_cast<const uint32_t*>(src[e & 1] + ks * 16 + 8 * (e >> 1))) : 0u;
+            }
+            // ---- the tree's ancestor sets, where this piece reaches its keys
+            const bool has_own = walk.t1 > q.cached_tiles;
+            if (has_own) {
+                for (int32_t j = threadIdx.x; j < q.n; j += 32 * kWarps) {
+                    uint32_t bits[kMaskWords];
+#pragma unroll
+                    for (int w = 0; w < kMaskWords; ++w) bits[w] = 0u;
+                    int32_t at = j;
+                    bool good = true, used = true;
+                    while (at >= 0) {
+#pragma unroll
+                        for (int w = 0; w < kMaskWords; ++w)
+                            if (w == (at >> 5)) bits[w] |= 1u << (at & 31);
+                        const int32_t up = __ldg(p.parents + q.tok0 + at);
+                        if (up < -1 && at == j) used = false;          // padding
+                        else if (up < -1 || up >= at) good = false;    // hangs on padding, or on a later node
+                        if (up >= at) break;
+                        at = up;
+                    }
+                    if (!good) ctl->data_error = 1;
+#pragma unroll
+                    for (int w = 0; w < kMaskWords; ++w) ctl->anc[j][w] = good && used ? bits[w] : 0u;
+                }
+                consumer_sync();
+            }
+            // Probabilities are rounded to bf16 for the P V product.  Over few keys that rounding is not averaged away, so
+            // short segments carry P as two bf16 terms (2^-17).
+            const bool two_terms = q.tiles <= 4;
+            float o[D / 8][4];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+            float run_max[2] = {-CUDART_INF_F, -CUDART_INF_F}, run_sum[2] = {0.f, 0.f};
+
+            for (int32_t t = walk.t0; t < walk.t1; ++t, ++it) {
+                const uint32_t st = it % kStages;
+                if (ok) ok = mbar_wait(&ctl->full[st], (it / kStages) & 1u, abort_flag);
+                uint8_t* stage = smem + st * L::kStageBytes;
+                const uint32_t k_addr = smem_u32(stage), v_addr = k_addr + L::kTensorBytes;
+                const bool own = t >= q.cached_tiles;
+                const int32_t first = (own ? t - q.cached_tiles : t) * kTile;  // number of the tile's first key
+                const int32_t keys = min(kTile, (own ? q.n : q.len) - first);  // keys the tile holds
+                // V rows behind the last key, and those of unused nodes, may hold anything: a probability of 0 must not
+                // meet a NaN there, so they are cleared (up to the next 16-key step; steps beyond it are not computed)
+                const bool clear = own || (keys & 15) != 0;
+                if (clear) {
+                    const int32_t r = threadIdx.x >> 1;
+                    if (r < ((keys + 15) & ~15) &&
+                        (r >= keys || (own && ((ctl->anc[first + r][(first + r) >> 5] >> ((first + r) & 31)) & 1u) == 0u))) {
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c)
+                            *reinterpret_cast<uint4*>(stage + L::kTensorBytes + key_off<D>(r, (threadIdx.x & 1) * (D / 16) + c)) =
+                                make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    consumer_sync();
+                }
+                // ---- scores of the warp's 16 rows and its range's keys
+                const int32_t range0 = range * kSteps * 16;
+                if (range0 < keys) {
+                    float sc[2 * kSteps][4];
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j) {
+                        const int32_t k0 = range0 + j * 16;
+                        if (k0 >= keys) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sc[2 * j][e] = sc[2 * j + 1][e] = -CUDART_INF_F;
+                            continue;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[2 * j][e] = sc[2 * j + 1][e] = 0.f;
+                        const int32_t r = k0 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks) {
+                            uint32_t b[4];
+                            ldsm_x4(k_addr + key_off<D>(r, 2 * ks + ((lane >> 3) & 1)), b);
+                            mma_16x8x16(sc[2 * j], qf[ks], b[0], b[1]);
+                            mma_16x8x16(sc[2 * j + 1], qf[ks], b[2], b[3]);
+                        }
+                    }
+                    if (own) {
+#pragma unroll
+                        for (int i = 0; i < 2 * kSteps; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int32_t j = first + range0 + 8 * i + 2 * tid + (e & 1);
+                                if (j >= q.n || ((ctl->anc[node[e >> 1]][j >> 5] >> (j & 31)) & 1u) == 0u) sc[i][e] = -CUDART_INF_F;
+                            }
+                    } else if (keys < kTile) {
+#pragma unroll
+                        for (int i = 0; i < 2 * kSteps; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (range0 + 8 * i + 2 * tid + (e & 1) >= keys) sc[i][e] = -CUDART_INF_F;
+                    }
+                    // ---- online softmax; a row is spread over four lanes
+                    float alpha[2], base[2];
+                    bool grow = false;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float m = fmaxf(sc[0][2 * u], sc[0][2 * u + 1]);
+#pragma unroll
+                        for (int i = 1; i < 2 * kSteps; ++i) m = fmaxf(m, fmaxf(sc[i][2 * u], sc[i][2 * u + 1]));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2)) * p.scale_log2;
+                        const bool up = m > run_max[u] + kRaise;
+                        const float to = up ? m : run_max[u];
+                        alpha[u] = up ? fast_exp2(run_max[u] - to) : 1.f;
+                        grow |= up;
+                        run_max[u] = to;
+                        base[u] = to == -CUDART_INF_F ? 0.f : to;  // a row that has seen no key yet
+                        run_sum[u] *= alpha[u];
+                    }
+                    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[i][e] *= alpha[e >> 1];
+                    }
+#pragma unroll
+                    for (int j = 0; j < kSteps; ++j) {
+                        const int32_t k0 = range0 + j * 16;
+                        if (k0 >= keys) break;
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {  // operand word e: row half e & 1, key half e >> 1
+                            const int i = 2 * j + (e >> 1), u = e & 1;
+                            const float x = fast_exp2(fmaf(sc[i][2 * u], p.scale_log2, -base[u]));
+                            const float y = fast_exp2(fmaf(sc[i][2 * u + 1], p.scale_log2, -base[u]));
+                            run_sum[u] += x + y;
+                            hi[e] = pack_bf16x2(x, y);
+                            lo[e] = pack_bf16x2(x - __uint_as_float(hi[e] << 16), y - __uint_as_float(hi[e] & 0xffff0000u));
+                        }
+                        const int32_t r = k0 + (lane & 15);
+#pragma unroll
+                        for (int dp = 0; dp < D / 16; ++dp) {
+                            uint32_t b[4];
+                            ldsm_x4_trans(v_addr + key_off<D>(r, 2 * dp + (lane >> 4)), b);
+                            mma_16x8x16(o[2 * dp], hi, b[0], b[1]);
+                            mma_16x8x16(o[2 * dp + 1], hi, b[2], b[3]);
+                            if (two_terms) {
+                                mma_16x8x16(o[2 * dp], lo, b[0], b[1]);
+                                mma_16x8x16(o[2 * dp + 1], lo, b[2], b[3]);
+                            }
+                        }
+                    }
+                }
+                if (t + 1 < walk.t1) {  // the last tile's stage first serves the join below
+                    if (clear) fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl->empty[st]);
+                }
+            }
+            // ---- join the warps' key ranges in the last tile's stage and hand the rows on
+            const uint32_t last = (it - 1) % kStages;
+            float* joined = reinterpret_cast<float*>(smem + last * L::kStageBytes);  // [warp][16][D]: as large as the stage
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                run_sum[u] += __shfl_xor_sync(0xffffffffu, run_sum[u], 1);
+                run_sum[u] += __shfl_xor_sync(0xffffffffu, run_sum[u], 2);
+                if (tid == 0) ctl->ml[warp][gid + 8 * u] = make_float2(run_max[u], run_sum[u]);
+            }
+            consumer_sync();  // nobody reads the tile any more
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)  // columns xor 8 * (row % 8): the eight rows of a store hit different banks
+                    *reinterpret_cast<float2*>(joined + (warp * 16 + gid + 8 * u) * D + ((8 * i + 2 * tid) ^ (gid << 3))) =
+                        make_float2(o[i][2 * u], o[i][2 * u + 1]);
+            consumer_sync();
+            const bool whole = walk.t0 == 0 && walk.t1 == q.tiles;
+            const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kRows;
+            for (int32_t i = threadIdx.x; i < kRows * (D / 4); i += 32 * kWarps) {
+                const int32_t r = i / (D / 4), c = (i % (D / 4)) * 4, rr = r & 15;
+                if (row0 + r >= rows) break;
+                float top = -CUDART_INF_F;
+#pragma unroll
+                for (int w = 0; w < kRanges; ++w) top = fmaxf(top, ctl->ml[(r >> 4) + w * kRowTiles][rr].x);
+                float sum = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kRanges; ++w) {
+                    const float2 ml = ctl->ml[(r >> 4) + w * kRowTiles][rr];
+                    // a range that saw no key contributes nothing (and its maximum is no number to subtract)
+                    const float f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
+                    const float4 v = *reinterpret_cast<const float4*>(joined + (((r >> 4) + w * kRowTiles) * 16 + rr) * D + (c ^ ((rr & 7) << 3)));
+                    sum = fmaf(f, ml.y, sum);
+                    acc.x = fmaf(f, v.x, acc.x);
+                    acc.y = fmaf(f, v.y, acc.y);
+                    acc.z = fmaf(f, v.z, acc.z);
+                    acc.w = fmaf(f, v.w, acc.w);
+                }
+                const int32_t nd = (row0 + r) / p.group;
+                // a piece that reaches the tree's own keys knows whether the row's node is in use
+                const bool unused = walk.t1 == q.tiles && ((ctl->anc[nd][nd >> 5] >> (nd & 31)) & 1u) == 0u;
+                if (whole) {
+                    const int64_t row = (static_cast<int64_t>(q.tok0) + nd) * p.num_q_heads + walk.head * p.group + (row0 + r - nd * p.group);
+                    const float inv = unused ? 0.f : 1.f / sum;
+                    uint2 w;
+                    w.x = unused ? 0u : pack_bf16x2(acc.x * inv, acc.y * inv);
+                    w.y = unused ? 0u : pack_bf16x2(acc.z * inv, acc.w * inv);
+                    *reinterpret_cast<uint2*>(p.out + row * D + c) = w;
+                    if (c == 0 && p.lse != nullptr) p.lse[row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
+                } else {
+                    *reinterpret_cast<float4*>(p.part_o + (slot + r) * D + c) = acc;
+                    if (c == 0) p.part_ml[slot + r] = make_float2(top, unused ? -1.f : sum);  // a negative sum marks an unused node
+                }
+            }
+            fence_proxy_async_smem();  // plain stores to the stage, before the next copy into it
+            consumer_sync();
+            if (lane == 0) mbar_arrive(&ctl->empty[last]);
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && ctl->abort_flag != 0u) {  // copies still in flight get a moment to land before the memory is released
+        const uint32_t n = ctl->issued, first = n > kStages ? n - kStages : 0u;
+        for (uint32_t i = first; i < n; ++i)
+            mbar_wait(&ctl->full[i % kStages], (i / kStages) & 1u, &ctl->drain_flag, kDrainLimitCycles);
+    }
+    if (threadIdx.x == 0 && p.status != nullptr) {
+        if (ctl->abort_flag != 0u) atomicCAS(p.status, 0, RPX_ERR_TIMEOUT);
+        else if (ctl->data_error != 0u) atomicCAS(p.status, 0, RPX_ERR_DEVICE_DATA);
+    }
+}
+
+// Adds up the pieces of every row whose segment was cut: one warp per (node, query head), pieces in the order of the keys.
+constexpr int kJoinRows = 8;
+template <int D, int kRows>
+__global__ void __launch_bounds__(kJoinRows * 32) tree_join_kernel(const Params p, int32_t chunks) {
+    constexpr int kCols = D / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int32_t s = blockIdx.x / chunks;
+    const Seq q = read_seq<kRows>(p, s, nullptr);
+    const int32_t i = (blockIdx.x - s * chunks) * kJoinRows + warp;
+    if (i >= q.n * p.num_q_heads) return;
+    const int32_t node = i / p.num_q_heads, head = i - node * p.num_q_heads;
+    const int32_t kv_head = head / p.group, r = node * p.group + head - kv_head * p.group;
+    const int64_t total = p.seq_tile0[p.batch], pieces = pieces_of(total, p.ctas);
+    const int64_t tile0 = p.seq_tile0[s] + (static_cast<int64_t>(kv_head) * q.blocks + r / kRows) * q.tiles;
+    const int64_t c0 = piece_of(total, pieces, tile0), c1 = piece_of(total, pieces, tile0 + q.tiles - 1);
+    if (c0 == c1) return;  // written whole
+    const int32_t row = r % kRows;
+    auto slot = [&](int64_t c) { return (c * 2 + (c == c0 ? 1 : 0)) * kRows + row; };
+    float top = -CUDART_INF_F;
+    for (int64_t c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, p.part_ml[slot(c)].x);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const bool unused = p.part_ml[slot(c1)].y < 0.f;
+    float sum = 0.f, acc[kCols];
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
+    if (!unused) {
+#pragma unroll 4
+        for (int64_t c = c0; c <= c1; ++c) {
+            const float2 ml = p.part_ml[slot(c)];
+            const float f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
+            const float* src = p.part_o + slot(c) * D + lane * kCols;
+            sum = fmaf(f, ml.y, sum);
+            if (kCols == 4) {
+                const float4 v = *reinterpret_cast<const float4*>(src);
+                acc[0] = fmaf(f, v.x, acc[0]);
+                acc[1] = fmaf(f, v.y, acc[1]);
+                acc[2] = fmaf(f, v.z, acc[2]);
+                acc[3] = fmaf(f, v.w, acc[3]);
+            } else {
+                const float2 v = *reinterpret_cast<const float2*>(src);
+                acc[0] = fmaf(f, v.x, acc[0]);
+                acc[1] = fmaf(f, v.y, acc[1]);
+            }
+        }
+    }
+    const float inv = unused ? 0.f : 1.f / sum;
+    const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
+    uint32_t w[kCols / 2];
+#pragma unroll
+    for (int k = 0; k < kCols / 2; ++k) w[k] = unused ? 0u : pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + out_row * D + lane * kCols);
+#pragma unroll
+    for (int k = 0; k < kCols / 2; ++k) dst[k] = w[k];
+    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
+}
+
+constexpr int kMaxCtas = 148 * kCtasPerSm;  // the workspace is sized for this many pieces
+
+// Rows per block: the smallest of 16, 32 and 64 that holds a tree's rows of one KV head.
+int rows_per_block(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+
+template <int D, int kRowTiles>
+rpx_status_t launch_stream(const TreeArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tkc,
+                           const CUtensorMap& tvc, Params p) {
+    using L = Layout<D>;
+    constexpr int kRows = 16 * kRowTiles;
+    auto* kernel = tree_stream_kernel<D, kRowTiles>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess)
+        return RPX_ERR_CUDA;
+    uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+    p.seq_tile0 = reinterpret_cast<int64_t*>(ws);
+    ws += align_up(static_cast<size_t>(a.batch + 1) * sizeof(int64_t), 256);
+    p.part_ml = reinterpret_cast<float2*>(ws);
+    ws += align_up(static_cast<size_t>(kMaxCtas) * 2 * kRows * sizeof(float2), 256);
+    p.part_o = reinterpret_cast<float*>(ws);
+    kernel<<<static_cast<unsigned>(p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);
+    if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
+    const int64_t chunks = (static_cast<int64_t>(a.max_tree) * a.num_q_heads + kJoinRows - 1) / kJoinRows;
+    if (chunks * a.batch > INT32_MAX) return RPX_ERR_SHAPE;
+    tree_join_kernel<D, kRows><<<static_cast<unsigned>(chunks * a.batch), kJoinRows * 32, 0, a.stream>>>(p, static_cast<int32_t>(chunks));
+    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+}
+
+template <int D>
+rpx_status_t launch_stream_d(const TreeArgs& a) {
+    CUtensorMap tk, tv, tkc, tvc;
+    {
+        // the tree's own K, V: 16 tokens of one head as a page: (64 elements, token, half, head)
+        const uint64_t dims[4] = {64, static_cast<uint64_t>(a.total_tokens), D / 64, static_cast<uint64_t>(a.num_kv_heads)};
+        const uint64_t ks[3] = {static_cast<uint64_t>(a.k_tok_stride) * 2, 128, D * 2ull};
+        const uint64_t vs[3] = {static_cast<uint64_t>(a.v_tok_stride) * 2, 128, D * 2ull};
+        const uint32_t box[4] = {64, kPage, D / 64, 1};
+        if (rpx_status_t rc = encode_tmap_bf16(&tk, a.k, 4, dims, ks, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&tv, a.v, 4, dims, vs, box)) return rc;
+    }
+    {
+        const uint64_t dims[5] = {64, kPage, D / 64, static_cast<uint64_t>(a.num_kv_heads), static_cast<uint64_t>(a.cache->num_blocks)};
+        const uint64_t strides[4] = {D * 2ull, 128, kPage * D * 2ull, static_cast<uint64_t>(a.num_kv_heads) * kPage * D * 2ull};
+        const uint32_t box[5] = {64, kPage, D / 64, 1, 1};
+        if (rpx_status_t rc = encode_tmap_bf16(&tkc, a.cache->k_cache, 5, dims, strides, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&tvc, a.cache->v_cache, 5, dims, strides, box)) return rc;
+    }
+    Params p;
+    p.q = static_cast<const __nv_bfloat16*>(a.q);
+    p.q_stride = a.q_tok_stride;
+    p.cu = a.cu_seqlens;
+    p.parents = a.parents;
+    p.lens = a.cached_lens;
+    p.block_table = a.cache->block_table;
+    p.block_table_stride = a.cache->block_table_stride;
+    p.num_blocks = static_cast<int32_t>(a.cache->num_blocks);
+    p.batch = a.batch;
+    p.num_q_heads = a.num_q_heads;
+    p.num_kv_heads = a.num_kv_heads;
+    p.group = a.num_q_heads / a.num_kv_heads;
+    p.max_tree = a.max_tree;
+    p.total_tokens = a.total_tokens;
+    const int sms = sm_count();
+    if (sms <= 0) return RPX_ERR_CUDA;
+    // (the SM budget is left out of this: where the line of tiles is cut decides the order of the sums, and this pass does
+    // not hold an SM for longer than its share of one read of the cache)
+    p.ctas = sms * kCtasPerSm < kMaxCtas ? sms * kCtasPerSm : kMaxCtas;
+    const float scale = a.softmax_scale > 0.f ? a.softmax_scale : 1.0f / sqrtf(static_cast<float>(D));
+    p.scale_log2 = scale * kLog2e;
+    p.out = static_cast<__nv_bfloat16*>(a.out);
+    p.lse = a.lse;
+    p.status = a.device_status;
+    switch (rows_per_block(static_cast<int64_t>(a.max_tree) * p.group)) {
+        case 16: return launch_stream<D, 1>(a, tk, tv, tkc, tvc, p);
+        case 32: return launch_stream<D, 2>(a, tk, tv, tkc, tvc, p);
+        default: return launch_stream<D, 4>(a, tk, tv, tkc, tvc, p);
+    }
+}
+
+// ------------------------------------------------------------------ ancestor sets and values for the other forms
+// One warp per token: its ancestor set as mask words (lane w holds word w while all lanes walk the path to the root), all
+// zero for a node that is not in use or a token of no sequence; and, for the tensor-core form, a copy of the tree's V with
+// those rows cleared (a probability of 0 must not meet what they hold).
+constexpr int kSetWarps = 8;
+__global__ void __launch_bounds__(kSetWarps * 32)
+tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ parents, int32_t batch, int64_t total_tokens,
+                 int32_t max_tree, int32_t words, uint32_t* sets, const __nv_bfloat16* v, int64_t v_stride, int32_t v_chunks,
+                 __nv_bfloat16* v_copy, int32_t* status) {
+    const int lane = threadIdx.x & 31;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * kSetWarps + (threadIdx.x >> 5);
+    if (token >= total_tokens) return;
+    int32_t lo = 0, hi = batch;  // the last sequence that starts at or before the token
+    while (lo < hi) {
+        const int32_t mid = (lo + hi + 1) >> 1;
+        if (mid < batch && __ldg(cu + mid) <= token) lo = mid;
+        else hi = mid - 1;
+    }
+    const int32_t tok0 = __ldg(cu + lo);
+    const int64_t n = static_cast<int64_t>(__ldg(cu + lo + 1)) - tok0;
+    const bool inside = tok0 >= 0 && tok0 <= token && token < tok0 + n && tok0 + n <= total_tokens && n <= max_tree;
+    uint32_t bits = 0u;
+    bool good = true, used = inside;
+    int32_t at = inside ? static_cast<int32_t>(token - tok0) : -1;
+    const int32_t self = at;
+    while (at >= 0) {
+        if ((at >> 5) == lane) bits |= 1u << (at & 31);
+        const int32_t up = __ldg(parents + tok0 + at);
+        if (up < -1 && at == self) used = false;
+        else if (up < -1 || up >= at) good = false;
+        if (up >= at) break;
+        at = up;
+    }
+    if (!good && lane == 0 && status != nullptr) atomicCAS(status, 0, RPX_ERR_DEVICE_DATA);
+    used = used && good;
+    if (lane < words) sets[token * words + lane] = used ? bits : 0u;
+    if (v_copy != nullptr) {
+        const uint4* src = reinterpret_cast<const uint4*>(v + token * v_stride);
+        uint4* dst = reinterpret_cast<uint4*>(v_copy) + token * v_chunks;
+        for (int32_t i = lane; i < v_chunks; i += 32) dst[i] = used ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+}  // namespace
+
+int32_t tree_set_words(int32_t max_tree) { return (max_tree + 127) / 128 * 4; }
+
+rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy) {
+    const int64_t blocks = (a.total_tokens + kSetWarps - 1) / kSetWarps;
+    tree_sets_kernel<<<static_cast<unsigned>(blocks), kSetWarps * 32, 0, a.stream>>>(
+        a.cu_seqlens, a.parents, a.batch, a.total_tokens, a.max_tree, tree_set_words(a.max_tree), sets,
+        static_cast<const __nv_bfloat16*>(a.v), a.v_tok_stride, a.num_kv_heads * a.head_dim / 8,
+        static_cast<__nv_bfloat16*>(v_copy), a.device_status);
+    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+}
+
+bool tree_streams(int32_t max_tree, int32_t group) {
+    (void)group;
+    return max_tree <= kMaxNodes;
+}
+
+size_t tree_stream_workspace(int32_t batch, int32_t head_dim) {
+    return align_up(static_cast<size_t>(batch + 1) * sizeof(int64_t), 256) + align_up(static_cast<size_t>(kMaxCtas) * 2 * 64 * sizeof(float2), 256) +
+           static_cast<size_t>(kMaxCtas) * 2 * 64 * head_dim * sizeof(float);
+}
+
+rpx_status_t launch_tree_stream(const TreeArgs& a) {
+    return a.head_dim == 128 ? launch_stream_d<128>(a) : launch_stream_d<64>(a);
+}
+
+}  // namespace rpx

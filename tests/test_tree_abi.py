@@ -1,0 +1,56 @@
+"""Host-only checks of the tree attention entry point: refusals before any launch, legal no-ops, workspace sizes."""
+import ctypes
+
+import pytest
+
+from paper_2608_14498_b200 import binding as B
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2608_14498_b200 import build
+
+    build.build()
+    return B.load_library()
+
+
+GOOD = B.AttnDesc(4, 2, 128, 0.0, B.RPX_BF16)
+CACHE = B.KvCache(0x1000, 0x1000, 8, 16, 0x1000, 4)
+
+
+def call(lib, desc=GOOD, q=0x1000, k=0x1000, v=0x1000, strides=(512, 256, 256), cu=0x1000, parents=0x1000, lens=0x1000,
+         batch=1, total=16, max_tree=16, max_cached=64, cache=CACHE, out=0x1000, ws=0x1000, ws_bytes=1 << 30):
+    return lib.rpx_tree_attn(ctypes.byref(desc) if desc is not None else None, q, k, v, *strides, cu, parents, lens, batch,
+                             total, max_tree, max_cached, ctypes.byref(cache) if cache is not None else None, out, None, ws,
+                             ws_bytes, None, None)
+
+
+def test_refusals(lib):
+    assert call(lib, desc=None) == -1
+    for bad in (dict(q=None), dict(k=None), dict(v=None), dict(cu=None), dict(parents=None), dict(lens=None), dict(out=None),
+                dict(cache=None), dict(cache=B.KvCache(None, 0x1000, 8, 16, 0x1000, 4))):
+        assert call(lib, **bad) == -1, bad
+    for bad in (dict(desc=B.AttnDesc(4, 3, 128, 0.0, 0)), dict(desc=B.AttnDesc(4, 2, 80, 0.0, 0)), dict(total=-1),
+                dict(batch=-1), dict(max_tree=-1), dict(max_tree=B.TREE_MAX_NODES + 1), dict(strides=(256, 256, 256)),
+                dict(cache=B.KvCache(0x1000, 0x1000, 8, 32, 0x1000, 4))):
+        assert call(lib, **bad) == -2, bad
+    assert call(lib, desc=B.AttnDesc(4, 2, 128, 0.0, 9)) == -3
+    for bad in (dict(q=0x1008), dict(out=0x1004), dict(strides=(516, 256, 256)), dict(ws=0x1010)):
+        assert call(lib, **bad) == -4, bad
+    assert call(lib, ws=None) == -5
+    assert call(lib, ws_bytes=64) == -5
+    # nothing to do
+    assert call(lib, batch=0, q=None, lens=None, ws=None) == 0
+    assert call(lib, total=0, q=None, ws=None) == 0
+    assert call(lib, max_tree=0, q=None, ws=None) == 0
+
+
+def test_workspace_sizes(lib):
+    small = B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 64, 8, 8)
+    assert 0 < small < 32 << 20 and small % 256 == 0
+    wide = B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 8 * 200, 8, 200)
+    # ancestor sets (8 words each) and a copy of the values come on top of the suffix pass's workspace
+    assert wide == B.suffix_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 1600) + 1600 * 8 * 4 + 1600 * 4 * 128 * 2
+    f32 = B.tree_attn_workspace_bytes(4, 2, 64, B.RPX_F32, 10, 2, 5)
+    assert f32 == 256 + 256  # the attention call's piece, and 10 sets of 4 words
+    assert B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 0, 8, 8) == 0
