@@ -70,7 +70,8 @@ enum {
     RPX_ERR_ARCH = -6,        /* current device is not compute capability 10.x               */
     RPX_ERR_CUDA = -7,        /* a CUDA runtime/driver call failed                           */
     RPX_ERR_DEVICE_DATA = -8, /* (device_status) out-of-range id found in device data        */
-    RPX_ERR_TIMEOUT = -9      /* (device_status) a bounded kernel-side wait expired          */
+    RPX_ERR_TIMEOUT = -9,     /* (device_status) a bounded kernel-side wait expired          */
+    RPX_ERR_NO_PAGES = -10    /* (device_status) the page pool has too few free pages        */
 };
 
 typedef enum { RPX_BF16 = 0, RPX_F32 = 1 } rpx_dtype_t;
@@ -319,6 +320,96 @@ RPX_API rpx_status_t rpx_attn_backward(const rpx_attn_desc_t* desc, const void* 
                                        void* workspace, size_t workspace_bytes, int32_t* device_status,
                                        void* cuda_stream);
 RPX_API size_t rpx_attn_backward_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_tokens);
+
+/*
+ * Pages of the cache, shared and moved on the device (the paper keeps the boundary KV of a prompt for all of its responses,
+ * Table 4; these calls keep the books when sequences branch, end and leave holes).  A pool has num_blocks pages; all layers
+ * of a model share the books, each with its own k_cache, v_cache.
+ *   ref_counts  device int32 [num_blocks]: how many table entries hold the page; 0 = free
+ *   block_table device int32 [rows][block_table_stride], of which the first table_cols columns are used: the pages a row
+ *               holds, in order from column 0, then -1
+ *   lens        device int32 [rows]: cached tokens of the row, at most 16 times its pages
+ * Several rows may hold the same page.  All decisions go by numbers (lowest free page first, requests in their order), so
+ * the same call leaves the same table.  Calls that touch one pool are issued on one stream, or ordered by the caller.
+ */
+typedef struct {
+    int32_t* block_table;
+    int32_t block_table_stride;
+    int32_t table_cols;
+    int32_t rows;
+    int32_t* lens;
+    int32_t* ref_counts;
+    int32_t num_blocks;
+} rpx_page_pool_t;
+
+/*
+ * Gives up the pages of `n` rows (device int32 [n]; a row listed twice is given up once): counts go down by one per entry,
+ * the entries become -1, lens 0.  A row number outside the table, or an entry nobody was counted for, is reported
+ * (RPX_ERR_DEVICE_DATA) and skipped.
+ */
+RPX_API rpx_status_t rpx_pages_free(const rpx_page_pool_t* pool, const int32_t* rows, int32_t n, int32_t* device_status,
+                                    void* cuda_stream);
+
+/*
+ * Branches sequences.  Request i (of n; src_rows, dst_rows device int32 [n]), with room for extra_tokens more:
+ *   src != dst  row dst, which holds no pages, becomes a branch of row src (-1: of nothing, a new sequence): it shares src's
+ *               whole pages (counts go up by one), gets fresh pages from there on up to lens[src] + extra_tokens, and
+ *               lens[dst] = lens[src].  If src's last page is partial, (copy_src[i], copy_dst[i]) = (that page, the branch's
+ *               own): the caller copies it in every layer (rpx_cache_copy_pages).  Otherwise, and for every refused
+ *               request, both are -1.
+ *   src == dst  the row keeps its pages and gets fresh ones up to lens + extra_tokens.
+ * All rows are read as they were before the call: a row is dst of one request only, and a row that is branched into is no
+ * request's src.  Requests that break this, rows outside the table, a dst that holds pages, a src that does not hold what
+ * its lens says, or more pages than table_cols are reported (RPX_ERR_DEVICE_DATA) and change nothing.  Fresh pages are taken
+ * in the order of the requests; one that needs more than are left, and every later one that needs any, is reported
+ * (RPX_ERR_NO_PAGES) and changes nothing.
+ *   workspace: rpx_pages_fork_workspace_bytes, 256-byte aligned
+ */
+RPX_API rpx_status_t rpx_pages_fork(const rpx_page_pool_t* pool, const int32_t* src_rows, const int32_t* dst_rows, int32_t n,
+                                    int32_t extra_tokens, int32_t* copy_src, int32_t* copy_dst, void* workspace,
+                                    size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
+RPX_API size_t rpx_pages_fork_workspace_bytes(const rpx_page_pool_t* pool, int32_t n);
+
+/*
+ * Moves the live pages to the low end of the pool: with L of them, the live pages numbered L and above go, in order, to the
+ * free numbers below L, and everything from L on is free.  Writes the new table and counts (block_table_out with its own
+ * stride, ref_counts_out: the pool's own arrays, or others that do not overlap them; columns beyond table_cols are not
+ * written), the list of moves copy_src, copy_dst (device int32 [num_blocks / 2], -1 behind the last move) for
+ * rpx_cache_copy_pages, and L to *n_live (device int32).  pool->lens is not used.  A table entry that names a free page, or
+ * none of the pool's, is reported (RPX_ERR_DEVICE_DATA) and becomes -1.
+ *   workspace: rpx_pages_compact_workspace_bytes, 256-byte aligned
+ */
+RPX_API rpx_status_t rpx_pages_compact(const rpx_page_pool_t* pool, int32_t* block_table_out, int32_t block_table_out_stride,
+                                       int32_t* ref_counts_out, int32_t* copy_src, int32_t* copy_dst, int32_t* n_live,
+                                       void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
+RPX_API size_t rpx_pages_compact_workspace_bytes(const rpx_page_pool_t* pool);
+
+/*
+ * Copies whole pages within the pools of `layers` layers: page src[i] to page dst[i] of K and of V, i < n (device int32 [n];
+ * pairs of -1 are skipped).  No dst may appear twice or be a src of another pair (the lists of the two calls above never do).
+ *   k_cache, v_cache: bf16 [layers][num_blocks][num_kv_heads][16][head_dim], layer_stride elements between layers
+ *   (a multiple of 8; for one layer any).  Page numbers outside the pool are reported and skipped.
+ */
+RPX_API rpx_status_t rpx_cache_copy_pages(void* k_cache, void* v_cache, int32_t layers, int64_t layer_stride, int64_t num_blocks,
+                                          int32_t num_kv_heads, int32_t head_dim, const int32_t* src, const int32_t* dst,
+                                          int64_t n, int32_t* device_status, void* cuda_stream);
+
+/*
+ * Stores K and V of chosen tokens behind the cached ones (after rpx_tree_attn: those of the accepted path).  Sequence s
+ * gets m = cu_append[s+1] - cu_append[s] tokens at positions cached_lens[s] .. cached_lens[s] + m - 1: the tokens
+ * token_ids[cu_append[s] + i] of k and v (device int32 [n_token_ids]), or, with token_ids == NULL, the tokens
+ * cu_append[s] + i themselves (n_token_ids is not used then).  cached_lens is not changed.
+ *   k, v [total_tokens][num_kv_heads][head_dim], RPX_BF16, or RPX_F32 (rounded to nearest-even as the prefix pass does)
+ *   max_append: upper bound of m (a sequence with more is reported and skipped).  Positions need not start a page; slots of
+ *   other positions are left as they are.  A sequence whose offsets or table do not fit, and a token or page number out of
+ *   range, is reported (RPX_ERR_DEVICE_DATA) and not stored.  Two sequences must not store into the same slot (a page that
+ *   rows share is never one that is still filled: rpx_pages_fork gives every branch its own).
+ */
+RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_tok_stride, int64_t v_tok_stride,
+                                      int64_t total_tokens, int32_t num_kv_heads, int32_t head_dim, rpx_dtype_t dtype,
+                                      const int32_t* token_ids, int64_t n_token_ids, const int32_t* cu_append,
+                                      const int32_t* cached_lens, int32_t batch, int32_t max_append,
+                                      const rpx_kv_cache_t* cache, int32_t* device_status, void* cuda_stream);
 
 /*
  * Norm of queries and keys per head and rotation by position, in one pass (the attention calls of this library take q and

@@ -8,12 +8,17 @@ from .binding import (  # noqa: F401
     RpxError,
     attn_backward,
     attn_backward_workspace_bytes,
+    cache_append,
+    cache_copy_pages,
     chunk_attn,
     get_lm_head_pairing,
     get_sm_budget,
     library_path,
     load_library,
     mrope_pair_axis,
+    pages_compact,
+    pages_fork,
+    pages_free,
     prefix_attn,
     prefix_attn_workspace_bytes,
     qk_norm_rope,

@@ -37,6 +37,13 @@ EXPORTS = (
     "rpx_get_lm_head_pairing",
     "rpx_attn_backward",
     "rpx_attn_backward_workspace_bytes",
+    "rpx_pages_free",
+    "rpx_pages_fork",
+    "rpx_pages_fork_workspace_bytes",
+    "rpx_pages_compact",
+    "rpx_pages_compact_workspace_bytes",
+    "rpx_cache_copy_pages",
+    "rpx_cache_append",
     "rpx_qk_norm_rope",
     "rpx_qk_norm_rope_backward",
     "rpx_qk_norm_rope_backward_workspace_bytes",
@@ -75,6 +82,18 @@ class KvCache(ctypes.Structure):
         ("block_size", ctypes.c_int32),
         ("block_table", ctypes.c_void_p),
         ("block_table_stride", ctypes.c_int32),
+    ]
+
+
+class PagePool(ctypes.Structure):
+    _fields_ = [
+        ("block_table", ctypes.c_void_p),
+        ("block_table_stride", ctypes.c_int32),
+        ("table_cols", ctypes.c_int32),
+        ("rows", ctypes.c_int32),
+        ("lens", ctypes.c_void_p),
+        ("ref_counts", ctypes.c_void_p),
+        ("num_blocks", ctypes.c_int32),
     ]
 
 
@@ -142,6 +161,22 @@ def load_library():
                                       i64, i32, vp, vp, vp, i32, vp, sz, vp, vp]
     lib.rpx_attn_backward_workspace_bytes.restype = sz
     lib.rpx_attn_backward_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i64]
+    pool = ctypes.POINTER(PagePool)
+    lib.rpx_pages_free.restype = i32
+    lib.rpx_pages_free.argtypes = [pool, vp, i32, vp, vp]
+    lib.rpx_pages_fork.restype = i32
+    lib.rpx_pages_fork.argtypes = [pool, vp, vp, i32, i32, vp, vp, vp, sz, vp, vp]
+    lib.rpx_pages_fork_workspace_bytes.restype = sz
+    lib.rpx_pages_fork_workspace_bytes.argtypes = [pool, i32]
+    lib.rpx_pages_compact.restype = i32
+    lib.rpx_pages_compact.argtypes = [pool, vp, i32, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.rpx_pages_compact_workspace_bytes.restype = sz
+    lib.rpx_pages_compact_workspace_bytes.argtypes = [pool]
+    lib.rpx_cache_copy_pages.restype = i32
+    lib.rpx_cache_copy_pages.argtypes = [vp, vp, i32, i64, i64, i32, i32, vp, vp, i64, vp, vp]
+    lib.rpx_cache_append.restype = i32
+    lib.rpx_cache_append.argtypes = [vp, vp, i64, i64, i64, i32, i32, i32, vp, i64, vp, vp, i32, i32, ctypes.POINTER(KvCache), vp,
+                                     vp]
     lib.rpx_qk_norm_rope.restype = i32
     lib.rpx_qk_norm_rope.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, i64, i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, i64, vp]
     lib.rpx_qk_norm_rope_backward.restype = i32
@@ -722,3 +757,139 @@ def qk_norm_rope_backward(q, k, dq, dk, positions, inv_freq, q_weight=None, k_we
     if rc != 0:
         raise RpxError(rc, "rpx_qk_norm_rope_backward")
     return dq_in, dk_in, dq_weight, dk_weight
+
+
+# ------------------------------------------------------------------ pages of the cache
+def _page_pool(block_table, lens, ref_counts) -> PagePool:
+    torch = _torch()
+    for t in (block_table, lens, ref_counts):
+        if t is not None and t.dtype != torch.int32:
+            raise TypeError("block_table, lens and ref_counts are int32")
+    if block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table is [rows, pages] with contiguous rows")
+    if not ref_counts.is_contiguous() or (lens is not None and (not lens.is_contiguous() or lens.shape[0] != block_table.shape[0])):
+        raise ValueError("ref_counts [num_blocks] and lens [rows] are contiguous")
+    rows, cols = block_table.shape
+    return PagePool(block_table.data_ptr(), block_table.stride(0) if rows > 1 else cols, cols, rows, _ptr(lens),
+                    ref_counts.data_ptr(), ref_counts.shape[0])
+
+
+def _row_list(t):
+    if t.dtype != _torch().int32 or t.dim() != 1 or not t.is_contiguous():
+        raise TypeError("row, page and token lists are contiguous int32 tensors")
+    return t
+
+
+@_in_call_context
+def pages_free(block_table, lens, ref_counts, rows, device_status=None, stream=None) -> None:
+    """rpx_pages_free: the listed rows give up their pages (reference counts go down, entries become -1, lens 0)."""
+    pool = _page_pool(block_table, lens, ref_counts)
+    rc = load_library().rpx_pages_free(ctypes.byref(pool), _ptr(_row_list(rows)), rows.shape[0], _ptr(device_status),
+                                       _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_pages_free")
+
+
+@_in_call_context
+def pages_fork(block_table, lens, ref_counts, src_rows, dst_rows, extra_tokens: int = 0, copy_src=None, copy_dst=None,
+               workspace=None, device_status=None, stream=None):
+    """rpx_pages_fork: empty rows ``dst`` become branches of rows ``src`` (-1: new sequences; src == dst: the row grows), whole
+    pages shared, with fresh pages for the partial last one and ``extra_tokens`` more.
+
+    Returns (copy_src, copy_dst) int32 [n]: the partial pages to copy in every layer (``cache_copy_pages``), -1 where none."""
+    torch = _torch()
+    lib = load_library()
+    pool = _page_pool(block_table, lens, ref_counts)
+    n = _row_list(src_rows).shape[0]
+    if _row_list(dst_rows).shape[0] != n:
+        raise ValueError("src_rows and dst_rows have one entry per request")
+    if copy_src is None:
+        copy_src = torch.empty((n,), dtype=torch.int32, device=block_table.device)
+    if copy_dst is None:
+        copy_dst = torch.empty((n,), dtype=torch.int32, device=block_table.device)
+    if _row_list(copy_src).shape[0] < n or _row_list(copy_dst).shape[0] < n:
+        raise ValueError("copy_src and copy_dst have one entry per request")
+    ws = _workspace(int(lib.rpx_pages_fork_workspace_bytes(ctypes.byref(pool), n)), block_table.device, workspace)
+    rc = lib.rpx_pages_fork(ctypes.byref(pool), _ptr(src_rows), _ptr(dst_rows), n, int(extra_tokens), _ptr(copy_src),
+                            _ptr(copy_dst), _ptr(ws), ws.numel() * ws.element_size(), _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_pages_fork")
+    return copy_src, copy_dst
+
+
+@_in_call_context
+def pages_compact(block_table, ref_counts, table_out=None, ref_counts_out=None, copy_src=None, copy_dst=None, n_live=None,
+                  workspace=None, device_status=None, stream=None):
+    """rpx_pages_compact: live pages move to the low end of the pool; the table and the counts are rewritten, in place unless
+    outputs are given.
+
+    Returns (copy_src, copy_dst, n_live): the moves for ``cache_copy_pages`` (int32 [num_blocks // 2], -1 behind the last) and
+    the number of live pages (int32 [1])."""
+    torch = _torch()
+    lib = load_library()
+    pool = _page_pool(block_table, None, ref_counts)
+    table_out = block_table if table_out is None else table_out
+    ref_counts_out = ref_counts if ref_counts_out is None else ref_counts_out
+    out = _page_pool(table_out, None, ref_counts_out)
+    if table_out.shape != block_table.shape or ref_counts_out.shape != ref_counts.shape:
+        raise ValueError("table_out and ref_counts_out have the shapes of block_table and ref_counts")
+    moves, dev = ref_counts.shape[0] // 2, block_table.device
+    if copy_src is None:
+        copy_src = torch.empty((moves,), dtype=torch.int32, device=dev)
+    if copy_dst is None:
+        copy_dst = torch.empty((moves,), dtype=torch.int32, device=dev)
+    if n_live is None:
+        n_live = torch.empty((1,), dtype=torch.int32, device=dev)
+    if _row_list(copy_src).shape[0] < moves or _row_list(copy_dst).shape[0] < moves or _row_list(n_live).shape[0] < 1:
+        raise ValueError("copy_src and copy_dst have num_blocks // 2 entries, n_live one")
+    ws = _workspace(int(lib.rpx_pages_compact_workspace_bytes(ctypes.byref(pool))), dev, workspace)
+    rc = lib.rpx_pages_compact(ctypes.byref(pool), out.block_table, out.block_table_stride, out.ref_counts, _ptr(copy_src),
+                               _ptr(copy_dst), _ptr(n_live), _ptr(ws), ws.numel() * ws.element_size(), _ptr(device_status),
+                               _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_pages_compact")
+    return copy_src, copy_dst, n_live
+
+
+@_in_call_context
+def cache_copy_pages(k_cache, v_cache, src, dst, device_status=None, stream=None) -> None:
+    """rpx_cache_copy_pages: page src[i] -> page dst[i] of both pools (pairs of -1 skipped).
+
+    Pools bfloat16 [num_blocks, H_kv, 16, d], or [layers, num_blocks, H_kv, 16, d] for all layers at once."""
+    torch = _torch()
+    if k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16:
+        raise TypeError("cache pools are bfloat16")
+    if k_cache.shape != v_cache.shape or k_cache.dim() not in (4, 5) or k_cache.shape[-2] != BLOCK_SIZE:
+        raise ValueError("cache pools are [(layers,) blocks, kv_heads, 16, head_dim], K and V alike")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("cache pools must be contiguous")
+    layers = k_cache.shape[0] if k_cache.dim() == 5 else 1
+    blocks, heads, _, d = k_cache.shape[-4:]
+    n = _row_list(src).shape[0]
+    if _row_list(dst).shape[0] != n:
+        raise ValueError("src and dst have one entry per pair")
+    rc = load_library().rpx_cache_copy_pages(_ptr(k_cache), _ptr(v_cache), layers, blocks * heads * BLOCK_SIZE * d, blocks, heads,
+                                             d, _ptr(src), _ptr(dst), n, _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_cache_copy_pages")
+
+
+@_in_call_context
+def cache_append(k, v, cu_append, cached_lens, max_append: int, cache: Tuple, token_ids=None, device_status=None,
+                 stream=None) -> None:
+    """rpx_cache_append: K and V of tokens ``token_ids[cu_append[s]:cu_append[s + 1]]`` (or of the tokens of that range
+    themselves) are stored at positions cached_lens[s], cached_lens[s] + 1, .. of sequence s; cached_lens stays as it is."""
+    cs = _cache_struct(cache)
+    if v.shape != k.shape or v.dtype != k.dtype or tuple(cache[0].shape[1:]) != (k.shape[1], BLOCK_SIZE, k.shape[2]):
+        raise ValueError("k and v are [tokens, kv_heads, head_dim] tensors that fit the cache pools")
+    batch = _row_list(cached_lens).shape[0]
+    if _row_list(cu_append).shape[0] != batch + 1 or cache[2].shape[0] < batch:
+        raise ValueError("cu_append has one entry more than cached_lens, and the block table a row for each sequence")
+    if token_ids is not None:
+        _row_list(token_ids)
+    rc = load_library().rpx_cache_append(_ptr(k), _ptr(v), _tok_stride(k), _tok_stride(v), k.shape[0], k.shape[1], k.shape[2],
+                                         _dtype_code(k), _ptr(token_ids), token_ids.shape[0] if token_ids is not None else 0,
+                                         _ptr(cu_append), _ptr(cached_lens), batch, int(max_append), ctypes.byref(cs),
+                                         _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_cache_append")

@@ -560,6 +560,153 @@ rpx_status_t rpx_qk_norm_rope_backward(const rpx_rope_desc_t* desc, const void* 
     return launch_qk_rope_backward(a);
 }
 
+}  // extern "C"
+
+namespace {
+
+rpx_status_t check_pool(const rpx_page_pool_t* p, bool with_lens) {
+    if (p == nullptr) return RPX_ERR_NULL;
+    if (p->rows < 0 || p->table_cols < 0 || p->block_table_stride < p->table_cols || p->num_blocks < 0) return RPX_ERR_SHAPE;
+    if (p->rows > 0 && p->table_cols > 0 && p->block_table == nullptr) return RPX_ERR_NULL;
+    if (p->rows > 0 && with_lens && p->lens == nullptr) return RPX_ERR_NULL;
+    if (p->num_blocks > 0 && p->ref_counts == nullptr) return RPX_ERR_NULL;
+    return RPX_OK;
+}
+
+PageArgs page_args(const rpx_page_pool_t* p, int32_t* device_status, void* cuda_stream) {
+    PageArgs a;
+    a.block_table = p->block_table;
+    a.block_table_stride = p->block_table_stride;
+    a.table_cols = p->table_cols;
+    a.rows = p->rows;
+    a.lens = p->lens;
+    a.ref_counts = p->ref_counts;
+    a.num_blocks = p->num_blocks;
+    a.device_status = device_status;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    return a;
+}
+
+rpx_status_t check_workspace(const void* workspace, size_t have, size_t need) {
+    if (workspace == nullptr || have < need) return RPX_ERR_WORKSPACE;
+    return aligned_ws(workspace) ? RPX_OK : RPX_ERR_ALIGN;
+}
+
+}  // namespace
+
+extern "C" {
+
+rpx_status_t rpx_pages_free(const rpx_page_pool_t* pool, const int32_t* rows, int32_t n, int32_t* device_status, void* cuda_stream) {
+    if (rpx_status_t rc = check_pool(pool, true)) return rc;
+    if (n < 0) return RPX_ERR_SHAPE;
+    if (n == 0) return RPX_OK;
+    if (rows == nullptr) return RPX_ERR_NULL;
+    if (rpx_status_t rc = check_arch()) return rc;
+    return launch_pages_free(page_args(pool, device_status, cuda_stream), rows, n);
+}
+
+size_t rpx_pages_fork_workspace_bytes(const rpx_page_pool_t* pool, int32_t n) {
+    if (pool == nullptr || n < 0 || pool->rows < 0 || pool->num_blocks < 0) return 0;
+    return align_up(pages_fork_workspace(n, pool->rows, pool->num_blocks), kWsAlign);
+}
+
+rpx_status_t rpx_pages_fork(const rpx_page_pool_t* pool, const int32_t* src_rows, const int32_t* dst_rows, int32_t n,
+                            int32_t extra_tokens, int32_t* copy_src, int32_t* copy_dst, void* workspace, size_t workspace_bytes,
+                            int32_t* device_status, void* cuda_stream) {
+    if (rpx_status_t rc = check_pool(pool, true)) return rc;
+    if (n < 0 || n > (1 << 30) || extra_tokens < 0) return RPX_ERR_SHAPE;
+    if (n == 0) return RPX_OK;
+    if (src_rows == nullptr || dst_rows == nullptr || copy_src == nullptr || copy_dst == nullptr) return RPX_ERR_NULL;
+    if (rpx_status_t rc = check_workspace(workspace, workspace_bytes, rpx_pages_fork_workspace_bytes(pool, n))) return rc;
+    if (rpx_status_t rc = check_arch()) return rc;
+    return launch_pages_fork(page_args(pool, device_status, cuda_stream), src_rows, dst_rows, n, extra_tokens, copy_src, copy_dst, workspace);
+}
+
+size_t rpx_pages_compact_workspace_bytes(const rpx_page_pool_t* pool) {
+    if (pool == nullptr || pool->num_blocks < 0) return 0;
+    return align_up(pages_compact_workspace(pool->num_blocks), kWsAlign);
+}
+
+rpx_status_t rpx_pages_compact(const rpx_page_pool_t* pool, int32_t* block_table_out, int32_t block_table_out_stride,
+                               int32_t* ref_counts_out, int32_t* copy_src, int32_t* copy_dst, int32_t* n_live, void* workspace,
+                               size_t workspace_bytes, int32_t* device_status, void* cuda_stream) {
+    if (rpx_status_t rc = check_pool(pool, false)) return rc;
+    if (pool->num_blocks == 0) return RPX_ERR_SHAPE;
+    if (block_table_out_stride < pool->table_cols) return RPX_ERR_SHAPE;
+    if (pool->rows > 0 && pool->table_cols > 0 && block_table_out == nullptr) return RPX_ERR_NULL;
+    if (ref_counts_out == nullptr || n_live == nullptr) return RPX_ERR_NULL;
+    if (pool->num_blocks > 1 && (copy_src == nullptr || copy_dst == nullptr)) return RPX_ERR_NULL;
+    if (rpx_status_t rc = check_workspace(workspace, workspace_bytes, rpx_pages_compact_workspace_bytes(pool))) return rc;
+    if (rpx_status_t rc = check_arch()) return rc;
+    return launch_pages_compact(page_args(pool, device_status, cuda_stream), block_table_out, block_table_out_stride, ref_counts_out, copy_src, copy_dst,
+                                n_live, workspace);
+}
+
+rpx_status_t rpx_cache_copy_pages(void* k_cache, void* v_cache, int32_t layers, int64_t layer_stride, int64_t num_blocks,
+                                  int32_t num_kv_heads, int32_t head_dim, const int32_t* src, const int32_t* dst, int64_t n,
+                                  int32_t* device_status, void* cuda_stream) {
+    if (layers < 0 || num_blocks < 0 || num_blocks > INT32_MAX || n < 0 || n > INT32_MAX || num_kv_heads <= 0 || num_kv_heads > 65536)
+        return RPX_ERR_SHAPE;
+    if (head_dim != 64 && head_dim != 128) return RPX_ERR_SHAPE;
+    if (layers > 1 && layer_stride < num_blocks * num_kv_heads * 16 * head_dim) return RPX_ERR_SHAPE;
+    if (n == 0 || layers == 0) return RPX_OK;
+    if (k_cache == nullptr || v_cache == nullptr || src == nullptr || dst == nullptr) return RPX_ERR_NULL;
+    if (!aligned16(k_cache) || !aligned16(v_cache) || (layers > 1 && layer_stride % 8 != 0)) return RPX_ERR_ALIGN;
+    if (rpx_status_t rc = check_arch()) return rc;
+    CopyPagesArgs a;
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    a.layer_stride = layer_stride;
+    a.layers = layers;
+    a.num_blocks = static_cast<int32_t>(num_blocks);
+    a.num_kv_heads = num_kv_heads;
+    a.head_dim = head_dim;
+    a.src = src;
+    a.dst = dst;
+    a.n = n;
+    a.device_status = device_status;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    return launch_copy_pages(a);
+}
+
+rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_tok_stride, int64_t v_tok_stride, int64_t total_tokens,
+                              int32_t num_kv_heads, int32_t head_dim, rpx_dtype_t dtype, const int32_t* token_ids,
+                              int64_t n_token_ids, const int32_t* cu_append, const int32_t* cached_lens, int32_t batch,
+                              int32_t max_append, const rpx_kv_cache_t* cache, int32_t* device_status, void* cuda_stream) {
+    if (cache == nullptr) return RPX_ERR_NULL;
+    if (dtype != RPX_BF16 && dtype != RPX_F32) return RPX_ERR_DTYPE;
+    if (head_dim != 64 && head_dim != 128) return RPX_ERR_SHAPE;
+    if (num_kv_heads <= 0 || num_kv_heads > 65536 || batch < 0 || max_append < 0 || total_tokens < 0 || total_tokens >= INT32_MAX ||
+        n_token_ids < 0 || n_token_ids >= INT32_MAX)
+        return RPX_ERR_SHAPE;
+    if (rpx_status_t rc = check_cache(cache, batch)) return rc;
+    if (batch == 0 || max_append == 0 || total_tokens == 0) return RPX_OK;
+    if (k == nullptr || v == nullptr || cu_append == nullptr || cached_lens == nullptr) return RPX_ERR_NULL;
+    const int64_t row = static_cast<int64_t>(num_kv_heads) * head_dim;
+    if (k_tok_stride < row || v_tok_stride < row) return RPX_ERR_SHAPE;
+    if (!aligned16(k) || !aligned16(v) || k_tok_stride % 8 || v_tok_stride % 8) return RPX_ERR_ALIGN;
+    if (rpx_status_t rc = check_arch()) return rc;
+    AppendArgs a;
+    a.k = k;
+    a.v = v;
+    a.k_tok_stride = k_tok_stride;
+    a.v_tok_stride = v_tok_stride;
+    a.num_kv_heads = num_kv_heads;
+    a.head_dim = head_dim;
+    a.dtype = dtype;
+    a.token_ids = token_ids;
+    a.cu = cu_append;
+    a.cached_lens = cached_lens;
+    a.batch = batch;
+    a.max_append = max_append;
+    a.total_tokens = total_tokens;
+    a.n_listed = token_ids != nullptr ? n_token_ids : total_tokens;
+    a.cache = *cache;
+    a.device_status = device_status;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    return launch_append(a);
+}
+
 rpx_status_t rpx_selftest_bounded_wait(int64_t limit_cycles, int32_t* device_status, void* cuda_stream) {
     if (device_status == nullptr) return RPX_ERR_NULL;
     if (limit_cycles <= 0 || limit_cycles > 2000000000ll) return RPX_ERR_SHAPE;
@@ -579,6 +726,7 @@ const char* rpx_status_string(rpx_status_t status) {
         case RPX_ERR_CUDA: return "a CUDA call failed";
         case RPX_ERR_DEVICE_DATA: return "out-of-range id in device data";
         case RPX_ERR_TIMEOUT: return "a bounded kernel-side wait expired";
+        case RPX_ERR_NO_PAGES: return "the page pool has too few free pages";
         default: return "unknown status";
     }
 }

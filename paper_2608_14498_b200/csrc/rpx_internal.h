@@ -144,6 +144,50 @@ int32_t tree_set_words(int32_t max_tree);            // 32-bit words of one ance
 // Ancestor sets [tokens][tree_set_words] and, with v_copy (bf16 [tokens][H_kv][d]), the values with unused rows cleared.
 rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy);
 
+struct PageArgs {
+    int32_t* block_table;        // [rows][block_table_stride]
+    int32_t block_table_stride, table_cols, rows;
+    int32_t* lens;               // [rows] cached tokens (free, fork)
+    int32_t* ref_counts;         // [num_blocks]
+    int32_t num_blocks;
+    int32_t* device_status;
+    cudaStream_t stream;
+};
+rpx_status_t launch_pages_free(const PageArgs& a, const int32_t* rows, int32_t n);
+size_t pages_fork_workspace(int32_t n, int32_t rows, int32_t num_blocks);
+rpx_status_t launch_pages_fork(const PageArgs& a, const int32_t* src_rows, const int32_t* dst_rows, int32_t n, int32_t extra,
+                               int32_t* copy_src, int32_t* copy_dst, void* workspace);
+size_t pages_compact_workspace(int32_t num_blocks);
+rpx_status_t launch_pages_compact(const PageArgs& a, int32_t* table_out, int64_t table_out_stride, int32_t* ref_counts_out,
+                                  int32_t* copy_src, int32_t* copy_dst, int32_t* n_live, void* workspace);
+
+struct CopyPagesArgs {
+    void *k_cache, *v_cache;
+    int64_t layer_stride;        // elements between layers, a multiple of 8
+    int32_t layers, num_blocks, num_kv_heads, head_dim;
+    const int32_t *src, *dst;    // [n]
+    int64_t n;
+    int32_t* device_status;
+    cudaStream_t stream;
+};
+rpx_status_t launch_copy_pages(const CopyPagesArgs& a);
+
+struct AppendArgs {
+    const void *k, *v;
+    int64_t k_tok_stride, v_tok_stride;
+    int32_t num_kv_heads, head_dim;
+    rpx_dtype_t dtype;
+    const int32_t* token_ids;    // nullable
+    const int32_t* cu;           // [batch + 1]
+    const int32_t* cached_lens;
+    int32_t batch, max_append;
+    int64_t total_tokens, n_listed;  // tokens of k and v; entries cu may reach (of token_ids, or tokens)
+    rpx_kv_cache_t cache;
+    int32_t* device_status;
+    cudaStream_t stream;
+};
+rpx_status_t launch_append(const AppendArgs& a);
+
 struct RopeArgs {
     const rpx_rope_desc_t* desc;
     const void *q, *k;

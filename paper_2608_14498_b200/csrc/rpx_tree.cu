@@ -733,7 +733,7 @@ rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy) {
 
 bool tree_streams(int32_t max_tree, int32_t group) {
     (void)group;
-    return max_tree <= kMaxNodes;
+    return max_tree <= kMaxNodes && max_tree * group <= 32;
 }
 
 size_t tree_stream_workspace(int32_t batch, int32_t head_dim) {
