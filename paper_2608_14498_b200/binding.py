@@ -217,10 +217,16 @@ def version() -> int:
 
 
 # ------------------------------------------------------------------ helpers (torch side)
-def _torch():
-    import torch
+_torch_module = None
 
-    return torch
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
@@ -238,8 +244,9 @@ def _ptr(t) -> Optional[int]:
 
 def _stream_ptr(stream) -> int:
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _tok_stride(t) -> int:
@@ -272,6 +279,8 @@ def _in_call_context(fn):
         torch = _torch()
         first = args[0] if args else next(iter(kwargs.values()))
         stream = kwargs.get("stream")
+        if stream is None and first.device.index == torch.cuda.current_device():
+            return fn(*args, **kwargs)  # the usual case, without the cost of entering a context
         with torch.cuda.device(first.device):
             if stream is None:
                 return fn(*args, **kwargs)
