@@ -180,9 +180,10 @@ RPX_API rpx_status_t rpx_chunk_attn(const rpx_attn_desc_t* desc, const void* q, 
  *   max_tree_len: upper bound of a sequence's nodes, at most RPX_TREE_MAX_NODES; a longer sequence is reported
  *       (RPX_ERR_DEVICE_DATA) and skipped, as is one whose offsets leave the packed tensors or the block table.
  *   max_cached_len: upper bound of cached_lens (sizes the grid only)
+ *   num_q_heads / num_kv_heads: any up to 128; above, RPX_BF16 trees have at most 128 nodes (RPX_ERR_SHAPE)
  *   workspace: rpx_tree_attn_workspace_bytes with the same total_tree_tokens, batch and max_tree_len
- * Results do not depend on the order in which the GPU runs the pieces: the same call gives the same bits.  Trees of up to
- * 128 nodes are not capped by rpx_set_sm_budget.
+ * Results do not depend on the order in which the GPU runs the pieces: the same call gives the same bits.  RPX_BF16 calls are
+ * not capped by rpx_set_sm_budget.
  */
 #define RPX_TREE_MAX_NODES 1024
 RPX_API rpx_status_t rpx_tree_attn(const rpx_attn_desc_t* desc, const void* q, const void* k, const void* v,

@@ -14,7 +14,7 @@ _ROOT = os.path.dirname(_HERE)
 _CSRC = os.path.join(_HERE, "csrc")
 _OUT = os.path.join(_HERE, "librpx.so")
 SOURCES = ["rpx_api.cu", "rpx_host.cu", "rpx_logprobs.cu", "rpx_logprobs_bwd.cu", "rpx_attn.cu", "rpx_attn_bwd.cu", "rpx_attn_f32.cu",
-           "rpx_rope.cu", "rpx_tree.cu", "rpx_pages.cu"]
+           "rpx_rope.cu", "rpx_tree.cu", "rpx_tree_tile.cu", "rpx_pages.cu"]
 
 
 def _nvcc() -> str:

@@ -39,8 +39,8 @@ rpx_status_t check_cache(const rpx_kv_cache_t* c, int32_t batch) {
     return RPX_OK;
 }
 
-// Workspace of a tree pass.  Streaming form: its own.  Otherwise the suffix pass's, then the ancestor sets, then (bf16) the
-// tree's values with unused rows cleared.
+// Workspace of a tree pass.  Streaming form: its own.  Tensor-core form: its own, the ancestor sets, and the tree's values
+// with unused rows cleared.  float32: the attention call's piece and the sets.
 struct TreeWorkspace {
     bool streams;
     size_t sets_off, values_off, bytes;
@@ -48,12 +48,14 @@ struct TreeWorkspace {
 TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t max_tree) {
     TreeWorkspace w = {};
     if (d == nullptr || tokens <= 0 || batch <= 0 || max_tree <= 0 || d->num_kv_heads <= 0) return w;
-    w.streams = d->dtype == RPX_BF16 && tree_streams(max_tree, d->num_q_heads / d->num_kv_heads);
+    const int32_t group = d->num_q_heads / d->num_kv_heads;
+    w.streams = d->dtype == RPX_BF16 && tree_streams(max_tree, group);
     if (w.streams) {
         w.bytes = align_up(tree_stream_workspace(batch, d->head_dim), kWsAlign);
         return w;
     }
-    w.sets_off = align_up(attn_workspace(d, tokens, true), kWsAlign);
+    const size_t own = d->dtype == RPX_F32 ? attn_workspace(d, tokens, true) : group > 128 ? 0 : tree_tile_workspace(batch, d->head_dim, max_tree, group);
+    w.sets_off = align_up(own, kWsAlign);
     w.values_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
     w.bytes = w.values_off;
     if (d->dtype == RPX_BF16) w.bytes += align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
@@ -72,6 +74,11 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
     if (batch < 0 || total_tokens < 0 || max_q_len < 0 || max_prefix_len < 0) return RPX_ERR_SHAPE;
     if (total_tokens >= INT32_MAX) return RPX_ERR_SHAPE;
     if (is_tree && max_q_len > RPX_TREE_MAX_NODES) return RPX_ERR_SHAPE;
+    // the tensor-core form keeps the heads of a KV head in one 128-row tile; the streaming form takes larger groups, but
+    // not every tree
+    if (is_tree && desc->dtype == RPX_BF16 && desc->num_q_heads / desc->num_kv_heads > 128 && max_q_len > 0 &&
+        !tree_streams(max_q_len, desc->num_q_heads / desc->num_kv_heads))
+        return RPX_ERR_SHAPE;
     if (is_suffix) {
         if (cache == nullptr) return RPX_ERR_NULL;
         if (batch > 0 && prefix_lens == nullptr) return RPX_ERR_NULL;
@@ -149,12 +156,9 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
         uint32_t* sets = reinterpret_cast<uint32_t*>(ws + tree_ws.sets_off);
         void* values = desc->dtype == RPX_BF16 ? ws + tree_ws.values_off : nullptr;
         if (rpx_status_t rc = launch_tree_sets(t, sets, values)) return rc;
+        if (desc->dtype == RPX_BF16) return launch_tree_tile(t, sets, values);
         a.tree_sets = sets;
         a.tree_words = tree_set_words(max_q_len);
-        if (values != nullptr) {
-            a.v = values;
-            a.v_tok_stride = kv_row;
-        }
     }
     // fp32 tensors take the fp32 CUDA-core path; out is then float32 and 16-byte alignment is all the tensors need
     if (desc->dtype == RPX_F32) return launch_attention_f32(a);

@@ -116,9 +116,6 @@ struct Params {
     float2* part_ml;              // [n_splits][tokens][H_q]: (row maximum in log2 units, row sum)
     uint32_t* split_cnt;          // [tokens][H_q], zero before the launch: arrivals per 32-row group
     int64_t total_tokens;
-    const uint32_t* tree_sets;    // kTree: [tokens][tree_words], the self keys each query token may see
-    int32_t tree_words;           // a multiple of 4
-    int32_t max_tree;             // kTree: the caller's bound; a longer sequence is reported and skipped
     float scale_log2;
     float inv_scale_log2;
     void* out;                    // bf16 [tokens][H_q][D] (fp32 tensors take the CUDA-core kernel)
@@ -147,16 +144,14 @@ struct Item {
 // Offsets that do not describe a range inside the packed tensors (a negative length, an end beyond total_tokens, a
 // negative cached length, more pages than a row of the block table holds) are reported and the item is handed on
 // empty, so nothing is read or written through them.
-template <bool kTree>
 __device__ __forceinline__ int4 fetch_item(const Params& p, int32_t idx, uint32_t* data_error) {
     const int32_t seq = ((idx / p.n_splits) % (p.batch * p.item_heads)) / p.item_heads;
     const int32_t tok0 = __ldg(p.cu_seqlens + seq);
     int32_t len_q = __ldg(p.cu_seqlens + seq + 1) - tok0;
     int32_t len_p = p.prefix_lens != nullptr ? __ldg(p.prefix_lens + seq) : 0;
-    if (kTree && len_q == 0) len_p = 0;  // no rows: whatever its cached length says
     // pages the block table must hold for this sequence: its cached prefix, plus its own tokens where they are stored
     const int64_t table_tokens = static_cast<int64_t>(len_p) + (p.write_cache != 0 ? len_q : 0);
-    if (tok0 < 0 || len_q < 0 || static_cast<int64_t>(tok0) + len_q > p.total_tokens || len_p < 0 || (kTree && len_q > p.max_tree) ||
+    if (tok0 < 0 || len_q < 0 || static_cast<int64_t>(tok0) + len_q > p.total_tokens || len_p < 0 ||
         (p.block_table != nullptr && (table_tokens + kPage - 1) / kPage > p.block_table_stride)) {
         *data_error = 1;
         len_q = 0;
@@ -206,9 +201,8 @@ __device__ __forceinline__ Item decode_item(const Params& p, int4 rec) {
 }
 
 // kFastSteps: also instantiate the branch-free form of the softmax step (see there); the launcher picks it for the
-// prefix pass.  kTree: the self keys a row sees are its ancestors in a tree of drafted tokens (all at or before its own
-// position, so the causal tile bounds hold) instead of every one at or before it; rows of unused nodes get 0 and -inf.
-template <int D, bool kFastSteps, bool kTree>
+// prefix pass.
+template <int D, bool kFastSteps>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
             const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_kc,
@@ -295,7 +289,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
             int4 rec = make_int4(-1, 0, 0, 0);
             if (lane == 0) {
                 const int32_t idx = static_cast<int32_t>(atomicAdd(p.next_item, 1u));
-                if (idx < p.n_items) rec = fetch_item<kTree>(p, idx, &ctl->data_error);
+                if (idx < p.n_items) rec = fetch_item(p, idx, &ctl->data_error);
                 ctl->item_rec[ring] = rec;
                 mbar_arrive(&ctl->item_full[ring]);
             }
@@ -622,14 +616,6 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
                 q_local = q0 + t * kTileQ + row;
                 row_head = head;
             }
-            const uint32_t* my_set = nullptr;  // kTree: this row's ancestor set; NULL for padding rows
-            bool row_used = true;
-            if constexpr (kTree) {
-                if (row_in_tile && q_local < len_q) {
-                    my_set = p.tree_sets + (static_cast<int64_t>(tok0) + q_local) * p.tree_words;
-                    row_used = ((__ldg(my_set + (q_local >> 5)) >> (q_local & 31)) & 1u) != 0u;
-                }
-            }
             const uint32_t lane_addr = (quarter * 32u) << 16;
             const int32_t my_tiles = n_tile0 + t * x1;
             const uint32_t my_s = tmem_base + t * 128 + lane_addr;        // this thread's lane of S_t / P_t
@@ -668,16 +654,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
                 bool rescale = false;
                 auto body = [&](auto fast_tag) {
                 constexpr bool kFast = decltype(fast_tag)::value;
-                if (kTree && j >= n_prefix_tiles) {
-                    uint4 set = make_uint4(0u, 0u, 0u, 0u);
-                    if (my_set != nullptr) set = __ldg(reinterpret_cast<const uint4*>(my_set) + (j - n_prefix_tiles));
-                    const uint32_t bits[4] = {set.x, set.y, set.z, set.w};
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (((bits[c] >> i) & 1u) == 0u) sc[c][i] = 0xff800000u;  // -inf
-                } else if (!kFast && n_vis < kTileK) {
+                if (!kFast && n_vis < kTileK) {
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c)
 #pragma unroll
@@ -707,14 +684,11 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
                 rescale = j > 0 && __any_sync(0xffffffffu, grow);
                 run_sum *= alpha;
                 run_max = new_max;
-                // a tree's row may not have seen any key yet: its (all masked) scores then need a finite number to be
-                // compared with; what it adds up, at most 2^-125 each, goes with the first rescale
-                const float ref_max = kTree && run_max == -CUDART_INF_F ? 0.f : run_max;
                 // ---- P = 2^(x - max) as packed bf16 pairs over the first 64 columns of S_t
                 const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2);
-                const uint64_t neg_max2 = f2_pack(-ref_max, -ref_max);
-                const uint64_t magic_max2 = f2_pack(12582912.f - ref_max, 12582912.f - ref_max);
-                const float min_score = (ref_max - 125.f) * p.inv_scale_log2;
+                const uint64_t neg_max2 = f2_pack(-run_max, -run_max);
+                const uint64_t magic_max2 = f2_pack(12582912.f - run_max, 12582912.f - run_max);
+                const float min_score = (run_max - 125.f) * p.inv_scale_log2;
                 uint64_t part2[4] = {0ull, 0ull, 0ull, 0ull};  // four packed accumulators = eight chains
                 // kSplit also writes the second bf16 term of each probability (what the first term's
                 // rounding dropped) to columns 64..127, four words at a time to keep it in registers.
@@ -826,7 +800,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
                         uint32_t w[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            w[i] = kTree && !row_used ? 0u : pack_bf16x2(__uint_as_float(r[2 * i]) * inv, __uint_as_float(r[2 * i + 1]) * inv);
+                            w[i] = pack_bf16x2(__uint_as_float(r[2 * i]) * inv, __uint_as_float(r[2 * i + 1]) * inv);
                         if (wide) {
                             st_global_v8(dst, w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
                             st_global_v8(dst + 16, w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]);
@@ -912,7 +886,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
                                 }
                                 store_chunk(ra, c);
                             }
-                            if (p.lse != nullptr) p.lse[rh] = kTree && !row_used ? -CUDART_INF_F : (top + log2f(total)) * kLn2;
+                            if (p.lse != nullptr) p.lse[rh] = (top + log2f(total)) * kLn2;
                         }
                     }
                 } else {
@@ -935,8 +909,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ 
                     store_chunk(rb, c + 1);
                 }
                 if (row_valid && p.lse != nullptr)
-                    p.lse[static_cast<int64_t>(tok0 + q_local) * p.num_q_heads + row_head] =
-                        kTree && !row_used ? -CUDART_INF_F : (run_max + log2f(run_sum)) * kLn2;
+                    p.lse[static_cast<int64_t>(tok0 + q_local) * p.num_q_heads + row_head] = (run_max + log2f(run_sum)) * kLn2;
                 }
             }
         }
@@ -1006,9 +979,6 @@ rpx_status_t launch_attention_d(const AttnArgs& a) {
     p.item_heads = pack ? a.num_kv_heads : a.num_q_heads;
     p.n_pairs = (a.max_q_len + 2 * tile_tokens - 1) / (2 * tile_tokens);
     const float scale = a.softmax_scale > 0.f ? a.softmax_scale : 1.0f / sqrtf(static_cast<float>(D));
-    p.tree_sets = a.tree_sets;
-    p.tree_words = a.tree_words;
-    p.max_tree = a.max_q_len;
     p.scale_log2 = scale * kLog2e;
     p.inv_scale_log2 = 1.0f / p.scale_log2;
     p.out = a.out;
@@ -1058,9 +1028,7 @@ rpx_status_t launch_attention_d(const AttnArgs& a) {
     const int64_t grid = n_items < sms ? n_items : sms;  // persistent: one CTA per SM
     if (cudaMemsetAsync(a.item_counter, 0, sizeof(uint32_t), a.stream) != cudaSuccess) return RPX_ERR_CUDA;
     // the prefix pass (no cached tiles) runs the instance with the branch-free softmax step
-    auto* kernel = a.prefix_lens == nullptr ? attn_kernel<D, true, false>
-                   : a.tree_sets != nullptr ? attn_kernel<D, false, true>
-                                            : attn_kernel<D, false, false>;
+    auto* kernel = a.prefix_lens == nullptr ? attn_kernel<D, true> : attn_kernel<D, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) !=
         cudaSuccess)
         return RPX_ERR_CUDA;

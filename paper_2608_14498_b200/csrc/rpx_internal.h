@@ -42,7 +42,8 @@ struct AttnArgs {
     bool append_cache = false;         // chunked prefill: read the earlier chunks AND append this one
     uint32_t* item_counter = nullptr;  // 4 bytes of workspace: the kernel's work-item counter (zeroed by the launcher)
     void* split_ws = nullptr;          // suffix pass only: room for split-KV partials (attn_split_workspace bytes), or NULL
-    // tree of drafted tokens instead of causal rows: ancestor set of every token, tree_words words each (launch_tree_sets)
+    // launch_attention_f32 only: a tree of drafted tokens instead of causal rows: ancestor set of every token, tree_words
+    // words each (launch_tree_sets)
     const uint32_t* tree_sets = nullptr;
     int32_t tree_words = 0;
     void* out;                         // bf16 (launch_attention) or float32 (launch_attention_f32)
@@ -140,6 +141,9 @@ struct TreeArgs {
 bool tree_streams(int32_t max_tree, int32_t group);  // whether the streaming form takes trees of this size
 size_t tree_stream_workspace(int32_t batch, int32_t head_dim);
 rpx_status_t launch_tree_stream(const TreeArgs& a);  // bf16
+size_t tree_tile_workspace(int32_t batch, int32_t head_dim, int32_t max_tree, int32_t group);
+// bf16; sets and values as launch_tree_sets leaves them, launched directly before on the same stream
+rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const void* values);
 int32_t tree_set_words(int32_t max_tree);            // 32-bit words of one ancestor set, a multiple of 4
 // Ancestor sets [tokens][tree_set_words] and, with v_copy (bf16 [tokens][H_kv][d]), the values with unused rows cleared.
 rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy);

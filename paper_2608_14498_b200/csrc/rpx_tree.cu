@@ -5,11 +5,8 @@
 //
 // With few nodes (one is a decoding step) this is bound by reading the cache: every cached K and V is read once per block of
 // up to 64 rows (row = node * group + head within the KV head's group), 512 bytes per key against rows * 512 flops.  So
-// the work is laid out along the keys.  All key tiles (64 keys) of all (sequence, KV head, row block) segments are
-// numbered in a line, and every CTA of one resident wave takes an equal piece of that line: a single long sequence
-// spreads over all SMs as evenly as a ragged batch does.  A CTA that holds a whole segment writes its rows; pieces of a
-// segment leave (maximum, sum, un-normalised row) in the workspace and tree_join_kernel adds them up in the order of the
-// keys, so results do not depend on which CTA ran when.
+// the work is laid out along the keys (rpx_tree.cuh): a single long sequence spreads over all SMs as evenly as a ragged
+// batch does.
 //   warp 4     : producer; one TMA box per 16-token page and tensor (both 64-element halves of its rows in one box,
 //                128-byte swizzle), three stages of 64 keys of K and V
 //   warps 0-3  : S = Q K^T and O += P V with mma.sync (16 rows x 8 keys x 16): at these row counts the tensor rate is not
@@ -17,49 +14,24 @@
 //                kRowTiles row tiles x 4 / kRowTiles ranges of the tile's keys, and join their ranges in shared memory
 //                at the end of a segment.
 // Scores are kept in log2 units, the running maximum is raised lazily (by steps of at least 2^8), sums are fp32.
-#include <math_constants.h>
-
-#include "rpx_internal.h"
-#include "rpx_ptx.cuh"
+#include "rpx_tree.cuh"
 
 namespace rpx {
 
 namespace {
 
-constexpr int kPage = 16, kTile = 64, kStages = 3;
+using namespace tree;
+
+constexpr int kTile = 64, kStages = 3;
 constexpr int kWarps = 4;  // consumer warps
 constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kCtasPerSm = 2;
-constexpr int kMinTiles = 2;     // key tiles a CTA takes at least: below that the join costs more than the spread gains
 constexpr int kMaxNodes = 128;   // nodes per sequence this form takes (their ancestor sets live in shared memory)
 constexpr int kMaskWords = kMaxNodes / 32;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kRaise = 8.0f;
-
-struct Params {
-    const __nv_bfloat16* q;
-    int64_t q_stride;
-    const int32_t *cu, *parents, *lens;
-    const int32_t* block_table;
-    int32_t block_table_stride, num_blocks;
-    int32_t batch, num_q_heads, num_kv_heads, group, max_tree;
-    int64_t total_tokens;
-    int32_t ctas;          // CTAs the line of tiles is cut for (the grid)
-    float scale_log2;
-    __nv_bfloat16* out;    // [tokens][H_q][D]
-    float* lse;            // nullable
-    int64_t* seq_tile0;    // workspace [batch + 1]: number of the sequence's first tile; the last entry is the total
-    float2* part_ml;       // workspace [ctas][2][rows per block]
-    float* part_o;         // workspace [ctas][2][rows per block][D]
-    int32_t* status;
-};
 
 struct Ctl {
     uint64_t full[kStages], empty[kStages];
-    int64_t warp_sum[kWarps + 1];
-    int64_t start_off;
-    int32_t start_seq;
+    Start start;
     uint32_t issued;  // tiles the producer has asked for
     uint32_t abort_flag, drain_flag, data_error;
     float2 ml[kWarps][16];
@@ -81,103 +53,7 @@ __device__ __forceinline__ uint32_t key_off(int r, int c) {
     return (r >> 4) * Layout<D>::kPageBytes + (c >> 3) * (kPage * 128) + (r & 15) * 128 + (((c & 7) ^ (r & 7)) << 4);
 }
 
-struct Seq {
-    int32_t tok0, n, len;         // first token, nodes, cached tokens
-    int32_t cached_tiles, tiles;  // key tiles of one segment: cached ones, then the tree's own
-    int32_t blocks;               // row blocks
-    __device__ __forceinline__ int64_t work(const Params& p) const { return static_cast<int64_t>(tiles) * blocks * p.num_kv_heads; }
-};
-
-// Offsets that leave the packed tensors or the block table, and a tree larger than the caller's bound, make a sequence
-// count as empty (its rows are left as they were) and are reported.
-template <int kRows>
-__device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* data_error) {
-    Seq q;
-    q.tok0 = __ldg(p.cu + s);
-    q.n = __ldg(p.cu + s + 1) - q.tok0;
-    q.len = __ldg(p.lens + s);
-    const bool bad = q.tok0 < 0 || q.n < 0 || static_cast<int64_t>(q.tok0) + q.n > p.total_tokens || q.n > p.max_tree ||
-                     (q.n > 0 && (q.len < 0 || (static_cast<int64_t>(q.len) + kPage - 1) / kPage > p.block_table_stride));
-    if (bad) {
-        if (data_error != nullptr) *data_error = 1;
-        q.n = 0;
-    }
-    if (q.n == 0) q.len = 0;
-    q.cached_tiles = q.len / kTile + (q.len % kTile != 0 ? 1 : 0);
-    q.tiles = q.n > 0 ? q.cached_tiles + (q.n + kTile - 1) / kTile : 0;
-    q.blocks = (q.n * p.group + kRows - 1) / kRows;
-    return q;
-}
-
-// The line of `total` tiles is cut into `pieces` nearly equal pieces, piece c = [begin(c), begin(c + 1)).
-__device__ __forceinline__ int64_t pieces_of(int64_t total, int32_t ctas) {
-    const int64_t most = total / kMinTiles;
-    return most < 1 ? 1 : most < ctas ? most : ctas;
-}
-__device__ __forceinline__ int64_t piece_begin(int64_t total, int64_t pieces, int64_t c) { return total * c / pieces; }
-__device__ __forceinline__ int64_t piece_of(int64_t total, int64_t pieces, int64_t tile) {
-    return ((tile + 1) * pieces - 1) / total;
-}
-
-__device__ __forceinline__ int64_t warp_scan(int64_t x, int lane) {  // inclusive
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, off);
-        if (lane >= off) x += y;
-    }
-    return x;
-}
-// Inclusive sum over the CTA's threads; `all` receives the total.
-__device__ __forceinline__ int64_t block_scan(int64_t x, Ctl* ctl, int warp, int lane, int64_t* all) {
-    x = warp_scan(x, lane);
-    __syncthreads();
-    if (lane == 31) ctl->warp_sum[warp] = x;
-    __syncthreads();
-    int64_t before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w <= kWarps; ++w) {
-        const int64_t v = ctl->warp_sum[w];
-        if (w < warp) before += v;
-        total += v;
-    }
-    *all = total;
-    return x + before;
-}
-
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-
-// Walks the pieces of segments inside this CTA's part of the line; every warp walks it alike.
-template <int kRows>
-struct Walk {
-    int32_t s, head, block, t0, t1;  // current segment: sequence, KV head, row block, key tiles [t0, t1)
-    Seq q;
-    int64_t pos, end, off;
-    bool have;
-    __device__ __forceinline__ Walk(int32_t s0, int64_t off0, int64_t begin, int64_t end_) : s(s0), pos(begin), end(end_), off(off0), have(false) {}
-    __device__ __forceinline__ bool next(const Params& p) {
-        while (pos < end && s < p.batch) {
-            if (!have) {
-                q = read_seq<kRows>(p, s, nullptr);
-                have = true;
-            }
-            if (off >= q.work(p)) {
-                ++s;
-                off = 0;
-                have = false;
-                continue;
-            }
-            const int32_t seg = static_cast<int32_t>(off / q.tiles);
-            t0 = static_cast<int32_t>(off - static_cast<int64_t>(seg) * q.tiles);
-            t1 = static_cast<int32_t>(min(static_cast<int64_t>(q.tiles), t0 + (end - pos)));
-            head = seg / q.blocks;
-            block = seg - head * q.blocks;
-            pos += t1 - t0;
-            off += t1 - t0;
-            return true;
-        }
-        return false;
-    }
-};
 
 template <int D, int kRowTiles>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
@@ -185,6 +61,7 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                    const __grid_constant__ CUtensorMap tmap_kc, const __grid_constant__ CUtensorMap tmap_vc, const Params p) {
     using L = Layout<D>;
     constexpr int kRows = 16 * kRowTiles;
+    using Cut = RowCut<kRows>;
     constexpr int kRanges = kWarps / kRowTiles;  // key ranges of a tile the warps work on side by side
     constexpr int kSteps = kTile / kRanges / 16; // 16-key steps of one range
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -202,51 +79,12 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         }
         ctl->abort_flag = ctl->drain_flag = ctl->data_error = 0;
         ctl->issued = 0;
-        ctl->start_seq = p.batch;
-        ctl->start_off = 0;
         fence_barrier_init();
     }
     __syncthreads();
 
-    // ---- this CTA's piece of the line: the total first, then the sequence that holds the piece's first tile
-    uint32_t* report = blockIdx.x == 0 ? &ctl->data_error : nullptr;
-    int64_t total = 0, all = 0, first_work = 0, first_sum = 0;
-    for (int32_t base = 0; base < p.batch; base += kThreads) {
-        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
-        const int64_t w = s < p.batch ? read_seq<kRows>(p, s, report).work(p) : 0;
-        const int64_t sum = block_scan(w, ctl, warp, lane, &all);
-        if (base == 0) {
-            first_work = w;
-            first_sum = sum;
-        }
-        total += all;
-    }
-    const int64_t pieces = pieces_of(total, p.ctas);
-    const int64_t cta = blockIdx.x;
-    const int64_t begin = cta < pieces ? piece_begin(total, pieces, cta) : 0;
-    const int64_t end = cta < pieces ? piece_begin(total, pieces, cta + 1) : 0;
-    int64_t carry = 0;
-    for (int32_t base = 0; base < p.batch; base += kThreads) {
-        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
-        int64_t w = first_work, sum = first_sum;
-        if (base > 0 || p.batch > kThreads) {
-            w = s < p.batch ? read_seq<kRows>(p, s, nullptr).work(p) : 0;
-            sum = block_scan(w, ctl, warp, lane, &all);
-        }
-        const int64_t before = carry + sum - w;
-        if (s < p.batch) {
-            if (begin >= before && begin < before + w) {
-                ctl->start_seq = s;
-                ctl->start_off = begin - before;
-            }
-            if (blockIdx.x == 0) p.seq_tile0[s] = before;
-        }
-        carry += all;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.seq_tile0[p.batch] = total;
-    __syncthreads();
-
-    Walk<kRows> walk(ctl->start_seq, ctl->start_off, begin, end);
+    find_piece<Cut, kWarps + 1>(p, &ctl->start, &ctl->data_error);
+    Walk<Cut> walk(p, &ctl->start);
     uint32_t it = 0;  // tiles this warp has been through (ring position)
     bool ok = true;
 
@@ -540,63 +378,6 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
 }
 
-// Adds up the pieces of every row whose segment was cut: one warp per (node, query head), pieces in the order of the keys.
-constexpr int kJoinRows = 8;
-template <int D, int kRows>
-__global__ void __launch_bounds__(kJoinRows * 32) tree_join_kernel(const Params p, int32_t chunks) {
-    constexpr int kCols = D / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int32_t s = blockIdx.x / chunks;
-    const Seq q = read_seq<kRows>(p, s, nullptr);
-    const int32_t i = (blockIdx.x - s * chunks) * kJoinRows + warp;
-    if (i >= q.n * p.num_q_heads) return;
-    const int32_t node = i / p.num_q_heads, head = i - node * p.num_q_heads;
-    const int32_t kv_head = head / p.group, r = node * p.group + head - kv_head * p.group;
-    const int64_t total = p.seq_tile0[p.batch], pieces = pieces_of(total, p.ctas);
-    const int64_t tile0 = p.seq_tile0[s] + (static_cast<int64_t>(kv_head) * q.blocks + r / kRows) * q.tiles;
-    const int64_t c0 = piece_of(total, pieces, tile0), c1 = piece_of(total, pieces, tile0 + q.tiles - 1);
-    if (c0 == c1) return;  // written whole
-    const int32_t row = r % kRows;
-    auto slot = [&](int64_t c) { return (c * 2 + (c == c0 ? 1 : 0)) * kRows + row; };
-    float top = -CUDART_INF_F;
-    for (int64_t c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, p.part_ml[slot(c)].x);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const bool unused = p.part_ml[slot(c1)].y < 0.f;
-    float sum = 0.f, acc[kCols];
-#pragma unroll
-    for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
-    if (!unused) {
-#pragma unroll 4
-        for (int64_t c = c0; c <= c1; ++c) {
-            const float2 ml = p.part_ml[slot(c)];
-            const float f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
-            const float* src = p.part_o + slot(c) * D + lane * kCols;
-            sum = fmaf(f, ml.y, sum);
-            if (kCols == 4) {
-                const float4 v = *reinterpret_cast<const float4*>(src);
-                acc[0] = fmaf(f, v.x, acc[0]);
-                acc[1] = fmaf(f, v.y, acc[1]);
-                acc[2] = fmaf(f, v.z, acc[2]);
-                acc[3] = fmaf(f, v.w, acc[3]);
-            } else {
-                const float2 v = *reinterpret_cast<const float2*>(src);
-                acc[0] = fmaf(f, v.x, acc[0]);
-                acc[1] = fmaf(f, v.y, acc[1]);
-            }
-        }
-    }
-    const float inv = unused ? 0.f : 1.f / sum;
-    const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
-    uint32_t w[kCols / 2];
-#pragma unroll
-    for (int k = 0; k < kCols / 2; ++k) w[k] = unused ? 0u : pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
-    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + out_row * D + lane * kCols);
-#pragma unroll
-    for (int k = 0; k < kCols / 2; ++k) dst[k] = w[k];
-    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
-}
-
 constexpr int kMaxCtas = 148 * kCtasPerSm;  // the workspace is sized for this many pieces
 
 // Rows per block: the smallest of 16, 32 and 64 that holds a tree's rows of one KV head.
@@ -606,22 +387,14 @@ template <int D, int kRowTiles>
 rpx_status_t launch_stream(const TreeArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tkc,
                            const CUtensorMap& tvc, Params p) {
     using L = Layout<D>;
-    constexpr int kRows = 16 * kRowTiles;
+    using Cut = RowCut<16 * kRowTiles>;
     auto* kernel = tree_stream_kernel<D, kRowTiles>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess)
         return RPX_ERR_CUDA;
-    uint8_t* ws = static_cast<uint8_t*>(a.workspace);
-    p.seq_tile0 = reinterpret_cast<int64_t*>(ws);
-    ws += align_up(static_cast<size_t>(a.batch + 1) * sizeof(int64_t), 256);
-    p.part_ml = reinterpret_cast<float2*>(ws);
-    ws += align_up(static_cast<size_t>(kMaxCtas) * 2 * kRows * sizeof(float2), 256);
-    p.part_o = reinterpret_cast<float*>(ws);
+    carve_workspace<Cut>(p, a.workspace);
     kernel<<<static_cast<unsigned>(p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);
     if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
-    const int64_t chunks = (static_cast<int64_t>(a.max_tree) * a.num_q_heads + kJoinRows - 1) / kJoinRows;
-    if (chunks * a.batch > INT32_MAX) return RPX_ERR_SHAPE;
-    tree_join_kernel<D, kRows><<<static_cast<unsigned>(chunks * a.batch), kJoinRows * 32, 0, a.stream>>>(p, static_cast<int32_t>(chunks));
-    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+    return launch_join<D, Cut>(p, a.max_tree, a.stream);
 }
 
 template <int D>
@@ -643,31 +416,12 @@ rpx_status_t launch_stream_d(const TreeArgs& a) {
         if (rpx_status_t rc = encode_tmap_bf16(&tkc, a.cache->k_cache, 5, dims, strides, box)) return rc;
         if (rpx_status_t rc = encode_tmap_bf16(&tvc, a.cache->v_cache, 5, dims, strides, box)) return rc;
     }
-    Params p;
-    p.q = static_cast<const __nv_bfloat16*>(a.q);
-    p.q_stride = a.q_tok_stride;
-    p.cu = a.cu_seqlens;
-    p.parents = a.parents;
-    p.lens = a.cached_lens;
-    p.block_table = a.cache->block_table;
-    p.block_table_stride = a.cache->block_table_stride;
-    p.num_blocks = static_cast<int32_t>(a.cache->num_blocks);
-    p.batch = a.batch;
-    p.num_q_heads = a.num_q_heads;
-    p.num_kv_heads = a.num_kv_heads;
-    p.group = a.num_q_heads / a.num_kv_heads;
-    p.max_tree = a.max_tree;
-    p.total_tokens = a.total_tokens;
+    Params p = make_params(a);
     const int sms = sm_count();
     if (sms <= 0) return RPX_ERR_CUDA;
     // (the SM budget is left out of this: where the line of tiles is cut decides the order of the sums, and this pass does
     // not hold an SM for longer than its share of one read of the cache)
     p.ctas = sms * kCtasPerSm < kMaxCtas ? sms * kCtasPerSm : kMaxCtas;
-    const float scale = a.softmax_scale > 0.f ? a.softmax_scale : 1.0f / sqrtf(static_cast<float>(D));
-    p.scale_log2 = scale * kLog2e;
-    p.out = static_cast<__nv_bfloat16*>(a.out);
-    p.lse = a.lse;
-    p.status = a.device_status;
     switch (rows_per_block(static_cast<int64_t>(a.max_tree) * p.group)) {
         case 16: return launch_stream<D, 1>(a, tk, tv, tkc, tvc, p);
         case 32: return launch_stream<D, 2>(a, tk, tv, tkc, tvc, p);
@@ -684,6 +438,7 @@ __global__ void __launch_bounds__(kSetWarps * 32)
 tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ parents, int32_t batch, int64_t total_tokens,
                  int32_t max_tree, int32_t words, uint32_t* sets, const __nv_bfloat16* v, int64_t v_stride, int32_t v_chunks,
                  __nv_bfloat16* v_copy, int32_t* status) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the attention kernel may start on its cached tiles
     const int lane = threadIdx.x & 31;
     const int64_t token = static_cast<int64_t>(blockIdx.x) * kSetWarps + (threadIdx.x >> 5);
     if (token >= total_tokens) return;
@@ -731,15 +486,14 @@ rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy) {
     return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
 }
 
+// The streaming form is bound by reading the cache up to 32 rows per block (94 % of that bound at 15 rows, 80 % at 30,
+// 8192 cached tokens); 64-row blocks are bound by mma.sync (41 us against 13 % of it for 56 rows over 8 x 4096 tokens), and
+// the tensor-core form is faster from there on.  It takes trees of any size but groups of at most 128 heads.
 bool tree_streams(int32_t max_tree, int32_t group) {
-    (void)group;
-    return max_tree <= kMaxNodes && max_tree * group <= 32;
+    return max_tree <= kMaxNodes && (static_cast<int64_t>(max_tree) * group <= 32 || group > 128);
 }
 
-size_t tree_stream_workspace(int32_t batch, int32_t head_dim) {
-    return align_up(static_cast<size_t>(batch + 1) * sizeof(int64_t), 256) + align_up(static_cast<size_t>(kMaxCtas) * 2 * 64 * sizeof(float2), 256) +
-           static_cast<size_t>(kMaxCtas) * 2 * 64 * head_dim * sizeof(float);
-}
+size_t tree_stream_workspace(int32_t batch, int32_t head_dim) { return join_workspace<RowCut<64>>(batch, kMaxCtas, head_dim); }
 
 rpx_status_t launch_tree_stream(const TreeArgs& a) {
     return a.head_dim == 128 ? launch_stream_d<128>(a) : launch_stream_d<64>(a);

@@ -1,0 +1,380 @@
+// What the two forms of tree attention share: how the work is cut.
+//
+// All key tiles of all (sequence, head, row block) segments are numbered in a line; the line is cut into nearly equal
+// pieces, one per CTA of a resident wave.  A segment that lies in one piece is written by its CTA; of a segment that is
+// cut, every piece leaves its rows' (maximum in log2 units, sum) and un-normalised outputs in the workspace, and the
+// join adds them up in the order of the keys.  The cut goes by lengths alone, so the same call gives the same bits.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "rpx_internal.h"
+#include "rpx_ptx.cuh"
+
+namespace rpx {
+namespace tree {
+
+constexpr int kPage = 16;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRaise = 8.0f;  // a row's running maximum is raised when a score passes it by this much (log2 units)
+
+struct Params {
+    const __nv_bfloat16* q;
+    int64_t q_stride;
+    const int32_t *cu, *parents, *lens;
+    const int32_t* block_table;
+    int32_t block_table_stride, num_blocks;
+    int32_t batch, num_q_heads, num_kv_heads, group, max_tree;
+    int64_t total_tokens;
+    int32_t ctas;          // pieces the line is cut into at most (the grid)
+    int32_t tile_nodes;    // tensor-core form: nodes per query tile of 128 rows (128 / group)
+    const __nv_bfloat16 *k_cache, *v_cache;
+    const uint32_t* sets;  // tensor-core form: ancestor sets [tokens][set_words]
+    int32_t set_words;
+    float scale_log2;
+    __nv_bfloat16* out;    // [tokens][H_q][D]
+    float* lse;            // nullable
+    int64_t* seq_tile0;    // workspace [batch + 1]: number of the sequence's first tile; the last entry is the total
+    float2* part_ml;       // workspace [ctas][2][rows per block]; a negative sum marks a node that is not in use
+    float* part_o;         // workspace [ctas][2][rows per block][D]
+    int32_t* status;
+};
+
+// How a form cuts: keys per tile, rows of a block (in the workspace), blocks of a sequence, a row's place in its block.
+template <int kRows_>
+struct RowCut {  // blocks of kRows rows, row = node * group + head within the KV head's group
+    static constexpr int kTile = 64, kRows = kRows_, kMinTiles = 2;
+    static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) { return (n * p.group + kRows - 1) / kRows; }
+    static __device__ __forceinline__ void place(const Params& p, int32_t node, int32_t h, int32_t* block, int32_t* row) {
+        const int32_t r = node * p.group + h;
+        *block = r / kRows;
+        *row = r % kRows;
+    }
+};
+template <int kTiles>
+struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
+    static constexpr int kTile = 128, kRows = 128 * kTiles, kMinTiles = 2;
+    static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) {
+        return (n + kTiles * p.tile_nodes - 1) / (kTiles * p.tile_nodes);
+    }
+    static __device__ __forceinline__ void place(const Params& p, int32_t node, int32_t h, int32_t* block, int32_t* row) {
+        const int32_t tile = node / p.tile_nodes;
+        *block = tile / kTiles;
+        *row = (tile % kTiles) * 128 + (node - tile * p.tile_nodes) * p.group + h;
+    }
+};
+
+struct Seq {
+    int32_t tok0, n, len;         // first token, nodes, cached tokens
+    int32_t cached_tiles, tiles;  // key tiles of one segment: cached ones, then the tree's own
+    int32_t blocks;               // row blocks
+    __device__ __forceinline__ int64_t work(const Params& p) const { return static_cast<int64_t>(tiles) * blocks * p.num_kv_heads; }
+};
+
+// Offsets that leave the packed tensors or the block table, and a tree larger than the caller's bound, make a sequence
+// count as empty (its rows are left as they were) and are reported.
+template <class Cut>
+__device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* data_error) {
+    Seq q;
+    q.tok0 = __ldg(p.cu + s);
+    q.n = __ldg(p.cu + s + 1) - q.tok0;
+    q.len = __ldg(p.lens + s);
+    const bool bad = q.tok0 < 0 || q.n < 0 || static_cast<int64_t>(q.tok0) + q.n > p.total_tokens || q.n > p.max_tree ||
+                     (q.n > 0 && (q.len < 0 || (static_cast<int64_t>(q.len) + kPage - 1) / kPage > p.block_table_stride));
+    if (bad) {
+        if (data_error != nullptr) *data_error = 1;
+        q.n = 0;
+    }
+    if (q.n == 0) q.len = 0;
+    q.cached_tiles = q.len / Cut::kTile + (q.len % Cut::kTile != 0 ? 1 : 0);
+    q.tiles = q.n > 0 ? q.cached_tiles + (q.n + Cut::kTile - 1) / Cut::kTile : 0;
+    q.blocks = Cut::blocks(p, q.n);
+    if (q.work(p) > INT32_MAX) {  // beyond any memory; the walk counts a sequence's tiles in 32 bits
+        if (data_error != nullptr) *data_error = 1;
+        q.n = q.len = q.cached_tiles = q.tiles = q.blocks = 0;
+    }
+    return q;
+}
+
+// The line of `total` tiles is cut into pieces of piece_tiles() tiles (the last ones may be short or empty).
+template <class Cut>
+__device__ __forceinline__ int64_t piece_tiles(int64_t total, int32_t ctas) {
+    const int64_t even = (total + ctas - 1) / ctas;
+    return even > Cut::kMinTiles ? even : Cut::kMinTiles;
+}
+__device__ __forceinline__ int32_t piece_of(int64_t tile, int64_t size) {
+    if ((tile >> 31) == 0 && (size >> 31) == 0) return static_cast<int32_t>(static_cast<uint32_t>(tile) / static_cast<uint32_t>(size));
+    return static_cast<int32_t>(tile / size);
+}
+
+__device__ __forceinline__ int64_t warp_scan(int64_t x, int lane) {  // inclusive
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
+// Inclusive sum over the CTA's kWarps warps; `all` receives the total.
+template <int kWarps>
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* warp_sum, int64_t* all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    x = warp_scan(x, lane);
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = x;
+    __syncthreads();
+    int64_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const int64_t v = warp_sum[w];
+        if (w < warp) before += v;
+        total += v;
+    }
+    *all = total;
+    return x + before;
+}
+
+// Where a CTA's piece starts (in shared memory).
+struct Start {
+    int64_t warp_sum[16];
+    int32_t seq, off;  // its first tile: sequence, and tile within that sequence's work
+    int32_t tiles;     // how many
+};
+
+// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also leaves every sequence's first tile in
+// the workspace and reports bad offsets.
+template <class Cut, int kWarps>
+__device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32_t* data_error) {
+    constexpr int kThreads = 32 * kWarps;
+    uint32_t* report = blockIdx.x == 0 ? data_error : nullptr;
+    if (threadIdx.x == 0) {
+        start->seq = p.batch;
+        start->off = 0;
+    }
+    int64_t total = 0, all = 0, first_work = 0, first_sum = 0;
+    for (int32_t base = 0; base < p.batch; base += kThreads) {
+        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
+        const int64_t w = s < p.batch ? read_seq<Cut>(p, s, report).work(p) : 0;
+        const int64_t sum = block_scan<kWarps>(w, start->warp_sum, &all);
+        if (base == 0) {
+            first_work = w;
+            first_sum = sum;
+        }
+        total += all;
+    }
+    const int64_t size = piece_tiles<Cut>(total, p.ctas);
+    const int64_t begin = min(total, size * static_cast<int64_t>(blockIdx.x)), end = min(total, begin + size);
+    int64_t carry = 0;
+    for (int32_t base = 0; base < p.batch; base += kThreads) {
+        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
+        int64_t w = first_work, sum = first_sum;
+        if (p.batch > kThreads) {
+            w = s < p.batch ? read_seq<Cut>(p, s, nullptr).work(p) : 0;
+            sum = block_scan<kWarps>(w, start->warp_sum, &all);
+        }
+        const int64_t before = carry + sum - w;
+        if (s < p.batch) {
+            if (begin < end && begin >= before && begin < before + w) {
+                start->seq = s;
+                start->off = static_cast<int32_t>(begin - before);
+            }
+            if (blockIdx.x == 0) p.seq_tile0[s] = before;
+        }
+        carry += all;
+    }
+    if (threadIdx.x == 0) {
+        start->tiles = static_cast<int32_t>(end - begin);
+        if (blockIdx.x == 0) p.seq_tile0[p.batch] = total;
+    }
+    __syncthreads();
+}
+
+// Walks the pieces of segments inside this CTA's part of the line; every warp walks it alike.
+template <class Cut>
+struct Walk {
+    int32_t s, head, block, t0, t1;  // current segment: sequence, KV head, row block, key tiles [t0, t1)
+    int32_t left;                    // tiles of the piece behind t1
+    Seq q;
+    __device__ __forceinline__ Walk(const Params& p, const Start* start) : s(start->seq), head(0), block(0), t0(0), t1(0), left(start->tiles), q() {
+        if (left == 0) return;
+        q = read_seq<Cut>(p, s, nullptr);
+        const int32_t seg = start->off / q.tiles;
+        t1 = start->off - seg * q.tiles;
+        head = seg / q.blocks;
+        block = seg - head * q.blocks;
+    }
+    __device__ __forceinline__ bool next(const Params& p) {
+        if (left == 0) return false;
+        if (t1 == q.tiles) {
+            t1 = 0;
+            if (++block == q.blocks) {
+                block = 0;
+                if (++head == p.num_kv_heads) {
+                    head = 0;
+                    do {
+                        if (++s >= p.batch) return false;  // (not reached: the piece ends before the line does)
+                        q = read_seq<Cut>(p, s, nullptr);
+                    } while (q.n == 0);
+                }
+            }
+        }
+        t0 = t1;
+        t1 = min(q.tiles, t0 + left);
+        left -= t1 - t0;
+        return true;
+    }
+};
+
+// Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  kSplit warps share a row (one
+// long sequence is cut into dozens of pieces for a handful of rows): each takes every kSplit-th piece.
+constexpr int kJoinWarps = 8;
+template <int D, class Cut, int kSplit>
+__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params p, int32_t chunks) {
+    constexpr int kCols = D / 32;
+    __shared__ float partial[kSplit > 1 ? kJoinWarps : 1][D];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % kSplit;
+    const int32_t s = blockIdx.x / chunks;
+    const Seq q = read_seq<Cut>(p, s, nullptr);
+    const int32_t i = (blockIdx.x - s * chunks) * (kJoinWarps / kSplit) + warp / kSplit;
+    const bool there = i < q.n * p.num_q_heads;
+    int32_t node = 0, head = 0, c0 = 0, c1 = 0, row = 0;
+    if (there) {
+        node = i / p.num_q_heads;
+        head = i - node * p.num_q_heads;
+        const int32_t kv_head = head / p.group;
+        int32_t block;
+        Cut::place(p, node, head - kv_head * p.group, &block, &row);
+        const int64_t size = piece_tiles<Cut>(p.seq_tile0[p.batch], p.ctas);
+        const int64_t tile0 = p.seq_tile0[s] + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.tiles;
+        c0 = piece_of(tile0, size);
+        c1 = piece_of(tile0 + q.tiles - 1, size);
+    }
+    const bool cut = c0 != c1;  // otherwise the row was written whole
+    if (kSplit == 1 && !cut) return;
+    // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
+    auto slot = [&](int32_t c) { return (static_cast<int64_t>(c) * 2 + (c == c0 ? 1 : 0)) * Cut::kRows + row; };
+    float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
+    bool unused = false;
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
+    if (cut) {
+        for (int32_t c = c0 + lane; c <= c1; c += 32) {
+            const float2 ml = p.part_ml[slot(c)];
+            top = fmaxf(top, ml.x);
+            if (c == c1) unused = ml.y < 0.f;
+        }
+        unused = __any_sync(0xffffffffu, unused);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        if (!unused) {
+            for (int32_t base = c0; base <= c1; base += 32) {
+                float f = 0.f;  // this lane's piece's factor
+                if (base + lane <= c1) {
+                    const float2 ml = p.part_ml[slot(base + lane)];
+                    f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
+                    sum = fmaf(f, ml.y, sum);
+                }
+                const int32_t n = min(32, c1 - base + 1);
+#pragma unroll 4
+                for (int32_t j = sub; j < n; j += kSplit) {
+                    const float fj = __shfl_sync(0xffffffffu, f, j);
+                    const float* src = p.part_o + slot(base + j) * D + lane * kCols;
+                    if (kCols == 4) {
+                        const float4 v = *reinterpret_cast<const float4*>(src);
+                        acc[0] = fmaf(fj, v.x, acc[0]);
+                        acc[1] = fmaf(fj, v.y, acc[1]);
+                        acc[kCols - 2] = fmaf(fj, v.z, acc[kCols - 2]);
+                        acc[kCols - 1] = fmaf(fj, v.w, acc[kCols - 1]);
+                    } else {
+                        const float2 v = *reinterpret_cast<const float2*>(src);
+                        acc[0] = fmaf(fj, v.x, acc[0]);
+                        acc[1] = fmaf(fj, v.y, acc[1]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        }
+    }
+    if (kSplit > 1) {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) partial[warp][lane * kCols + k] = acc[k];
+        __syncthreads();
+        if (sub != 0 || !cut) return;
+#pragma unroll
+        for (int w = 1; w < kSplit; ++w)
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) acc[k] += partial[warp + w][lane * kCols + k];
+    }
+    const float inv = unused ? 0.f : 1.f / sum;
+    const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
+    uint32_t w[kCols / 2];
+#pragma unroll
+    for (int k = 0; k < kCols / 2; ++k) w[k] = unused ? 0u : pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + out_row * D + lane * kCols);
+#pragma unroll
+    for (int k = 0; k < kCols / 2; ++k) dst[k] = w[k];
+    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
+}
+
+template <int D, class Cut, int kSplit>
+rpx_status_t launch_join_split(const Params& p, int32_t max_tree, cudaStream_t stream) {
+    const int64_t chunks = (static_cast<int64_t>(max_tree) * p.num_q_heads * kSplit + kJoinWarps - 1) / kJoinWarps;
+    if (chunks * p.batch > INT32_MAX) return RPX_ERR_SHAPE;
+    tree_join_kernel<D, Cut, kSplit><<<static_cast<unsigned>(chunks * p.batch), kJoinWarps * 32, 0, stream>>>(p, static_cast<int32_t>(chunks));
+    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+}
+template <int D, class Cut>
+rpx_status_t launch_join(const Params& p, int32_t max_tree, cudaStream_t stream) {
+    // more than 8 pieces per segment: four warps a row
+    const int64_t segments = static_cast<int64_t>(p.batch) * p.num_kv_heads * Cut::blocks(p, max_tree);
+    return p.ctas > 8 * segments ? launch_join_split<D, Cut, 4>(p, max_tree, stream) : launch_join_split<D, Cut, 1>(p, max_tree, stream);
+}
+
+// The pass's workspace: sequences' first tiles, then the pieces' rows.
+template <class Cut>
+inline size_t join_workspace(int32_t batch, int32_t ctas, int32_t head_dim) {
+    const size_t rows = static_cast<size_t>(ctas) * 2 * Cut::kRows;
+    return align_up(static_cast<size_t>(batch + 1) * sizeof(int64_t), 256) + align_up(rows * sizeof(float2), 256) + rows * head_dim * sizeof(float);
+}
+template <class Cut>
+inline void carve_workspace(Params& p, void* workspace) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.seq_tile0 = reinterpret_cast<int64_t*>(ws);
+    ws += align_up(static_cast<size_t>(p.batch + 1) * sizeof(int64_t), 256);
+    p.part_ml = reinterpret_cast<float2*>(ws);
+    ws += align_up(static_cast<size_t>(p.ctas) * 2 * Cut::kRows * sizeof(float2), 256);
+    p.part_o = reinterpret_cast<float*>(ws);
+}
+
+inline Params make_params(const TreeArgs& a) {
+    Params p = {};
+    p.q = static_cast<const __nv_bfloat16*>(a.q);
+    p.q_stride = a.q_tok_stride;
+    p.cu = a.cu_seqlens;
+    p.parents = a.parents;
+    p.lens = a.cached_lens;
+    p.block_table = a.cache->block_table;
+    p.block_table_stride = a.cache->block_table_stride;
+    p.num_blocks = static_cast<int32_t>(a.cache->num_blocks);
+    p.k_cache = static_cast<const __nv_bfloat16*>(a.cache->k_cache);
+    p.v_cache = static_cast<const __nv_bfloat16*>(a.cache->v_cache);
+    p.batch = a.batch;
+    p.num_q_heads = a.num_q_heads;
+    p.num_kv_heads = a.num_kv_heads;
+    p.group = a.num_q_heads / a.num_kv_heads;
+    p.tile_nodes = p.group <= 128 ? 128 / p.group : 1;
+    p.max_tree = a.max_tree;
+    p.total_tokens = a.total_tokens;
+    const float scale = a.softmax_scale > 0.f ? a.softmax_scale : 1.0f / sqrtf(static_cast<float>(a.head_dim));
+    p.scale_log2 = scale * kLog2e;
+    p.out = static_cast<__nv_bfloat16*>(a.out);
+    p.lse = a.lse;
+    p.status = a.device_status;
+    return p;
+}
+
+}  // namespace tree
+}  // namespace rpx

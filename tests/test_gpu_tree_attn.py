@@ -148,6 +148,11 @@ CASES = [
     ([1024, 100], [256, 31], 16, 1, 128),
     ([50], [1024], 6, 2, 64),
     ([900, 4000], [150, 140], 5, 5, 128),
+    ([300, 60], [3, 2], 160, 1, 64),
+    ([128, 256, 384, 5000], [18, 18, 17, 9], 28, 4, 128),
+    ([9000], [30], 40, 8, 128),
+    ([140, 0, 12000, 260], [25, 26, 60, 51], 40, 8, 128),
+    ([2000] * 20, [40] * 20, 8, 2, 64),
 ]
 
 
