@@ -11,7 +11,7 @@
 //                    output of its own, and the warps of buffer 0 join the two straight out of TMEM at the end.
 //   warps 0-3, 4-7 : softmax of buffer 0, 1: thread = row = TMEM lane
 //   warp  8        : producer: Q once per segment, K and V through rings of their own (K runs a tile ahead, so it is not
-//                    held up behind a V slot), one TMA box per 16-token page and 64-element half
+//                    held up behind a V slot), one TMA box per 16-token page
 //   warp  9        : issues S_t = Q K^T (smem x smem -> TMEM) and O_t += P_t V (P as bf16 over S_t's first 64 columns)
 //   warps 10, 11   : only take part in the register hand-over
 // The tree's own V tiles come from a copy in which rows of unused nodes are zero, and ancestor sets as bit masks; a small
@@ -60,8 +60,12 @@ struct Ctl {
     float2 ml[kTile];
 };
 
-__device__ __forceinline__ uint32_t swz_off(int r, int cc) {
-    return static_cast<uint32_t>((cc >> 3) * (kTile * 128) + r * 128 + (((cc & 7) ^ (r & 7)) << 4));
+// Key tiles lie as [group of 8 keys][half][8 rows][128 bytes], swizzled: a 16-token page (two groups, both halves) is one
+// 4 KB TMA box, and to the tensor core the groups are evenly spaced, which is all that its descriptors need.  (With a box
+// per page and half, 32 boxes of 2 KB a tile, the loads took 3800 clocks per 64 KB tile whatever the pass did with them.)
+template <int D>
+__device__ __forceinline__ uint32_t key_off(int r, int c) {  // of 16-byte chunk c of key r
+    return static_cast<uint32_t>(((r >> 3) * (D / 64) + (c >> 3)) * 1024 + (r & 7) * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
 // Waits until the kernel launched before this one has finished and its writes are visible.
@@ -138,8 +142,8 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             ++segments;
             const int32_t* table = p.block_table + static_cast<int64_t>(walk.s) * p.block_table_stride;
             const int32_t pages = (q.len + kPage - 1) / kPage;
-            // lane pg + 8 hf fetches half hf of page pg of a tile; block ids are read a tile ahead
-            const int pg = lane & 7, hf = lane >> 3;
+            // lane pg fetches page pg of a tile; block ids are read a tile ahead
+            const int pg = lane & 7;
             auto read_block = [&](int32_t t) {
                 int32_t b = t < q.cached_tiles && t * kPages + pg < pages ? __ldg(table + t * kPages + pg) : 0;
                 if (b < 0 || b >= p.num_blocks) {
@@ -155,11 +159,10 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         wait_for_sets();
                         have_sets = true;
                     }
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(full, L::kTensorBytes);
-                        for (int h = 0; h < L::kHalves; ++h)
-                            tma_load_3d(dst + h * L::kHalfBytes, is_v ? &tmap_v : &tmap_k, full, h * 64, walk.head, q.tok0 + own * kTile);
-                    }
+                    if (lane == 0) mbar_arrive_expect_tx(full, L::kTensorBytes);
+                    __syncwarp();
+                    if (lane < kTile / 8)  // tokens start anywhere: a box per 8
+                        tma_load_4d(dst + lane * (8 * D * 2), is_v ? &tmap_v : &tmap_k, full, 0, q.tok0 + own * kTile + lane * 8, 0, walk.head);
                     return;
                 }
                 // K behind the last key may be anything (its scores are masked); V may not: what a probability of 0 meets
@@ -174,7 +177,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         const int32_t r = first + i / (D / 8), c = i % (D / 8);
                         uint4 x = make_uint4(0u, 0u, 0u, 0u);
                         if (r < rows) x = __ldg(src + (r - first) * (D / 8) + c);
-                        *reinterpret_cast<uint4*>(dst + swz_off(r, c)) = x;
+                        *reinterpret_cast<uint4*>(dst + key_off<D>(r, c)) = x;
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
@@ -184,8 +187,8 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     else mbar_arrive(full);
                 }
                 __syncwarp();  // the byte count is armed before any copy can complete
-                if (hf < L::kHalves && pg < boxes)
-                    tma_load_4d(dst + hf * L::kHalfBytes + pg * (kPage * 128), is_v ? &tmap_vc : &tmap_kc, full, hf * 64, 0, walk.head, block);
+                if (lane < boxes)
+                    tma_load_4d(dst + pg * (kPage * D * 2), is_v ? &tmap_vc : &tmap_kc, full, 0, 0, 0, (block * p.num_kv_heads + walk.head) * 2);
             };
             const int32_t n = walk.t1 - walk.t0;
             int32_t block_now = read_block(walk.t0), block_before = 0;
@@ -225,8 +228,8 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             constexpr uint32_t idesc_qk = make_idesc_bf16(kTile, kTile, false, false);
             constexpr uint32_t idesc_pv = make_idesc_bf16(kTile, D, false, true);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem), 16, 1024);
-            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem + L::kKOff), 16, 1024);             // K-major
-            const uint64_t v_desc = make_smem_desc_sw128(smem_u32(smem + L::kVOff), L::kHalfBytes, 1024);  // MN-major
+            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem + L::kKOff), 16, L::kHalves * 1024);    // K-major
+            const uint64_t v_desc = make_smem_desc_sw128(smem_u32(smem + L::kVOff), 1024, L::kHalves * 1024);  // MN-major
             bool ok = true;
             uint32_t segments = 0, nk = 0, nv = 0;
             uint32_t steps[2] = {0, 0};  // steps of each buffer so far (barrier parity)
@@ -236,8 +239,10 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             auto issue_qk = [&](int t, int tile, uint32_t i) {
                 const uint64_t kd = k_desc + static_cast<uint64_t>((i % L::kSlotsK) * (L::kTensorBytes >> 4));
                 const uint64_t qd = q_desc + static_cast<uint64_t>(tile * (L::kTensorBytes >> 4));
-                if (D == 128) umma_ss_k128_overwrite(tmem_base + t * 128, qd, kd, idesc_qk);
-                else umma_ss_k64_overwrite(tmem_base + t * 128, qd, kd, idesc_qk);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)  // 16 columns = 32 bytes of a 128-byte row
+                    umma_bf16_ss(tmem_base + t * 128, qd + (ks >> 2) * (L::kHalfBytes >> 4) + 2 * (ks & 3), kd + (ks >> 2) * 64 + 2 * (ks & 3),
+                                 idesc_qk, ks != 0);
                 umma_commit(&ctl->s_full[t]);
             };
             // waits for the probabilities of a buffer's next step and issues their product with V
@@ -248,8 +253,13 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 if (first && used[t] > 0 && !mbar_wait(&ctl->o_free[t], (used[t] - 1) & 1u, abort_flag)) return false;
                 tc_fence_after_sync();
                 const uint64_t vd = v_desc + static_cast<uint64_t>((i % L::kSlotsV) * (L::kTensorBytes >> 4));
-                umma_ts_k128(tmem_base + 256 + t * 128, tmem_base + t * 128, vd, idesc_pv, first ? 0u : 1u);
-                if (two_terms) umma_ts_k128(tmem_base + 256 + t * 128, tmem_base + t * 128 + 64, vd, idesc_pv, 1u);
+#pragma unroll
+                for (int ks = 0; ks < kTile / 16; ++ks)  // 16 keys = 8 columns of P = two groups of V
+                    umma_bf16_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + 8 * ks, vd + ks * (L::kHalves * 128), idesc_pv, !first || ks != 0);
+                if (two_terms)
+#pragma unroll
+                    for (int ks = 0; ks < kTile / 16; ++ks)
+                        umma_bf16_ts(tmem_base + 256 + t * 128, tmem_base + t * 128 + 64 + 8 * ks, vd + ks * (L::kHalves * 128), idesc_pv, 1u);
                 return true;
             };
             while (ok && walk.next(p)) {
@@ -577,16 +587,19 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* va
         if (rpx_status_t rc = encode_tmap_bf16(&tq, a.q, 3, dims, strides, box)) return rc;
     }
     {
-        const uint64_t dims[3] = {D, heads, tokens};
-        const uint64_t ks[2] = {D * 2ull, static_cast<uint64_t>(a.k_tok_stride) * 2}, vs[2] = {D * 2ull, heads * D * 2ull};
-        const uint32_t box[3] = {64, 1, kTile};
-        if (rpx_status_t rc = encode_tmap_bf16(&tk, a.k, 3, dims, ks, box)) return rc;
-        if (rpx_status_t rc = encode_tmap_bf16(&tv, values, 3, dims, vs, box)) return rc;
+        const uint64_t dims[4] = {64, tokens, D / 64, heads};
+        const uint64_t ks[3] = {static_cast<uint64_t>(a.k_tok_stride) * 2, 128, D * 2ull}, vs[3] = {heads * D * 2ull, 128, D * 2ull};
+        const uint32_t box[4] = {64, 8, D / 64, 1};
+        if (rpx_status_t rc = encode_tmap_bf16(&tk, a.k, 4, dims, ks, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&tv, values, 4, dims, vs, box)) return rc;
     }
     {
-        const uint64_t dims[4] = {D, kPage, heads, static_cast<uint64_t>(a.cache->num_blocks)};
-        const uint64_t strides[3] = {D * 2ull, kPage * D * 2ull, heads * kPage * D * 2ull};
-        const uint32_t box[4] = {64, kPage, 1, 1};
+        // the pool as groups of 8 keys: two per page and head
+        const uint64_t groups = static_cast<uint64_t>(a.cache->num_blocks) * heads * 2;
+        if (groups > INT32_MAX) return RPX_ERR_SHAPE;
+        const uint64_t dims[4] = {64, 8, D / 64, groups};
+        const uint64_t strides[3] = {D * 2ull, 128, 8 * D * 2ull};
+        const uint32_t box[4] = {64, 8, D / 64, 2};
         if (rpx_status_t rc = encode_tmap_bf16(&tkc, a.cache->k_cache, 4, dims, strides, box)) return rc;
         if (rpx_status_t rc = encode_tmap_bf16(&tvc, a.cache->v_cache, 4, dims, strides, box)) return rc;
     }
