@@ -32,6 +32,9 @@ constexpr int kThreads = 32 * 12;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;  // 256 * 208 + 128 * 88 <= 384 * 168, what the launch has
 constexpr uint32_t kTmemCols = 512;
+constexpr int kPolyPairsOf4 = 1;  // of every 4 pairs of exponentials, how many go to the FMA pipe
+// 2^f on [-1/2, 1/2], least maximum of the relative error among quartics (2.6e-6; iteratively reweighted least squares)
+constexpr float kExp2_0 = 0.99999926f, kExp2_1 = 0.69312181f, kExp2_2 = 0.24024745f, kExp2_3 = 0.05591786f, kExp2_4 = 0.0095701f;
 constexpr int kMaxCtas = 148;
 
 template <int D, bool kPaired>
@@ -173,12 +176,18 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     const int32_t ragged = __shfl_sync(0xffffffffu, block, boxes);
                     const uint4* src = reinterpret_cast<const uint4*>(p.v_cache + (static_cast<int64_t>(ragged) * p.num_kv_heads + walk.head) * kPage * D);
                     const int32_t first = boxes * kPage;
-                    for (int32_t i = lane; i < (kTile - first) * (D / 8); i += 32) {
-                        const int32_t r = first + i / (D / 8), c = i % (D / 8);
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if (r < rows) x = __ldg(src + (r - first) * (D / 8) + c);
-                        *reinterpret_cast<uint4*>(dst + key_off<D>(r, c)) = x;
+                    uint4 x[kPage * D / 8 / 32];
+#pragma unroll
+                    for (int i = 0; i < kPage * D / 8 / 32; ++i) {  // the page, all loads in flight together
+                        const int32_t r = (lane + 32 * i) / (D / 8);
+                        x[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (first + r < rows) x[i] = __ldg(src + lane + 32 * i);
                     }
+#pragma unroll
+                    for (int i = 0; i < kPage * D / 8 / 32; ++i)
+                        *reinterpret_cast<uint4*>(dst + key_off<D>(first + (lane + 32 * i) / (D / 8), (lane + 32 * i) % (D / 8))) = x[i];
+                    for (int32_t i = lane; i < (kTile - first - kPage) * (D / 8); i += 32)
+                        *reinterpret_cast<uint4*>(dst + key_off<D>(first + kPage + i / (D / 8), i % (D / 8))) = make_uint4(0u, 0u, 0u, 0u);
                     fence_proxy_async_smem();
                     __syncwarp();
                 }
@@ -421,9 +430,11 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 run_max = new_max;
                 const float base = run_max == -CUDART_INF_F ? 0.f : run_max;  // a row that has seen no key yet
                 // ---- P = 2^(x - max): bf16 pairs over the first 64 columns of S_t, for short segments (one or two tiles,
-                // where the rounding is not averaged over many keys) a second term in the other 64.  The exponentials all
-                // go to the special-function unit: a cubic on the FMA pipe would be off by 1e-4, which the float32 lse shows.
+                // where the rounding is not averaged over many keys) a second term in the other 64.  A quarter of the
+                // exponentials is taken off the special-function unit (16 a clock, as long as the two products of a query
+                // tile take); a cubic would do for P, but its 1e-4 shows in the float32 lse.
                 const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2), base2 = f2_pack(-base, -base);
+                const uint64_t magic = f2_pack(12582912.f, 12582912.f);  // 1.5 * 2^23: adding it rounds to an integer
                 uint64_t part[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -433,7 +444,25 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     for (int i = 0; i < 32; i += 2) {
                         float x0, x1;
                         f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[c][i]), __uint_as_float(sc[c][i + 1])), scale2, base2), x0, x1);
-                        const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
+                        float e0, e1;
+                        if (((i / 2) & 3) < kPolyPairsOf4) {
+                            // x = n + f, |f| <= 1/2; 2^f by a quartic, 2^n into the exponent field
+                            const uint64_t x = f2_pack(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+                            const uint64_t shifted = f2_add(x, magic);
+                            const uint64_t f = f2_sub(x, f2_sub(shifted, magic));
+                            uint64_t y = f2_fma(f2_pack(kExp2_4, kExp2_4), f, f2_pack(kExp2_3, kExp2_3));
+                            y = f2_fma(y, f, f2_pack(kExp2_2, kExp2_2));
+                            y = f2_fma(y, f, f2_pack(kExp2_1, kExp2_1));
+                            y = f2_fma(y, f, f2_pack(kExp2_0, kExp2_0));
+                            float y0, y1, s0, s1;
+                            f2_unpack(y, y0, y1);
+                            f2_unpack(shifted, s0, s1);
+                            e0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(s0) << 23));
+                            e1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(s1) << 23));
+                        } else {
+                            e0 = fast_exp2(x0);
+                            e1 = fast_exp2(x1);
+                        }
                         part[(i / 2) % 4] = f2_add(part[(i / 2) % 4], f2_pack(e0, e1));
                         packed[i >> 1] = pack_bf16x2(e0, e1);
                         if constexpr (kTwoTerms) {  // what the first term dropped
