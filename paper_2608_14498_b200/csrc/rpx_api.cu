@@ -39,11 +39,11 @@ rpx_status_t check_cache(const rpx_kv_cache_t* c, int32_t batch) {
     return RPX_OK;
 }
 
-// Workspace of a tree pass.  Streaming form: its own.  Tensor-core form: its own, the ancestor sets, and the tree's values
-// with unused rows cleared.  float32: the attention call's piece and the sets.
+// Workspace of a tree pass.  Streaming form: its own.  Tensor-core form: its own, the ancestor sets, the tokens' sequences,
+// and the tree's values with unused rows cleared.  float32: the attention call's piece and the sets.
 struct TreeWorkspace {
     bool streams;
-    size_t sets_off, values_off, bytes;
+    size_t sets_off, seq_off, values_off, bytes;
 };
 TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t max_tree) {
     TreeWorkspace w = {};
@@ -56,9 +56,12 @@ TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t b
     }
     const size_t own = d->dtype == RPX_F32 ? attn_workspace(d, tokens, true) : group > 128 ? 0 : tree_tile_workspace(batch, d->head_dim, max_tree, group);
     w.sets_off = align_up(own, kWsAlign);
-    w.values_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
-    w.bytes = w.values_off;
-    if (d->dtype == RPX_BF16) w.bytes += align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
+    w.seq_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
+    w.bytes = w.seq_off;
+    if (d->dtype == RPX_BF16) {
+        w.values_off = w.seq_off + align_up(static_cast<size_t>(tokens) * sizeof(int32_t), kWsAlign);
+        w.bytes = w.values_off + align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
+    }
     return w;
 }
 
@@ -154,9 +157,13 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
         if (tree_ws.streams) return launch_tree_stream(t);
         uint8_t* ws = static_cast<uint8_t*>(workspace);
         uint32_t* sets = reinterpret_cast<uint32_t*>(ws + tree_ws.sets_off);
-        void* values = desc->dtype == RPX_BF16 ? ws + tree_ws.values_off : nullptr;
-        if (rpx_status_t rc = launch_tree_sets(t, sets, values)) return rc;
-        if (desc->dtype == RPX_BF16) return launch_tree_tile(t, sets, values);
+        if (desc->dtype == RPX_BF16) {
+            int32_t* token_seq = reinterpret_cast<int32_t*>(ws + tree_ws.seq_off);
+            void* values = ws + tree_ws.values_off;
+            if (rpx_status_t rc = launch_tree_sets(t, sets, token_seq, values)) return rc;
+            return launch_tree_tile(t, sets, token_seq, values);
+        }
+        if (rpx_status_t rc = launch_tree_sets(t, sets, nullptr, nullptr)) return rc;
         a.tree_sets = sets;
         a.tree_words = tree_set_words(max_q_len);
     }

@@ -1,6 +1,6 @@
 // What the two forms of tree attention share: how the work is cut.
 //
-// All key tiles of all (sequence, head, row block) segments are numbered in a line; the line is cut into nearly equal
+// All key tiles of all (sequence, head, row block) segments lie in a line; the line is cut into equal
 // pieces, one per CTA of a resident wave.  A segment that lies in one piece is written by its CTA; of a segment that is
 // cut, every piece leaves its rows' (maximum in log2 units, sum) and un-normalised outputs in the workspace, and the
 // join adds them up in the order of the keys.  The cut goes by lengths alone, so the same call gives the same bits.
@@ -32,20 +32,24 @@ struct Params {
     int32_t tile_nodes;    // tensor-core form: nodes per query tile of 128 rows (128 / group)
     const __nv_bfloat16 *k_cache, *v_cache;
     const uint32_t* sets;  // tensor-core form: ancestor sets [tokens][set_words]
+    const int32_t* token_seq;  // tensor-core form: each token's sequence, -1 for none
     int32_t set_words;
     float scale_log2;
     __nv_bfloat16* out;    // [tokens][H_q][D]
     float* lse;            // nullable
-    int64_t* seq_tile0;    // workspace [batch + 1]: number of the sequence's first tile; the last entry is the total
+    int64_t* seq_unit0;    // workspace [batch + 1]: number of the sequence's first unit; the last entry is the total
     float2* part_ml;       // workspace [ctas][2][rows per block]; a negative sum marks a node that is not in use
     float* part_o;         // workspace [ctas][2][rows per block][D]
     int32_t* status;
 };
 
-// How a form cuts: keys per tile, rows of a block (in the workspace), blocks of a sequence, a row's place in its block.
+// How a form cuts: keys per tile, rows of a block (in the workspace), blocks of a sequence, a row's place in its block, and
+// the weight of a block's key tiles: the line is measured in units of these, and a tile belongs to the piece that holds its
+// first unit.  All blocks but a sequence's last have the same weight.
 template <int kRows_>
 struct RowCut {  // blocks of kRows rows, row = node * group + head within the KV head's group
-    static constexpr int kTile = 64, kRows = kRows_, kMinTiles = 2;
+    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 2;
+    static __device__ __forceinline__ int32_t weight(const Params&, int32_t, int32_t) { return 1; }
     static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) { return (n * p.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ void place(const Params& p, int32_t node, int32_t h, int32_t* block, int32_t* row) {
         const int32_t r = node * p.group + h;
@@ -55,7 +59,14 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
 };
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
-    static constexpr int kTile = 128, kRows = 128 * kTiles, kMinTiles = 2;
+    static constexpr int kTile = 128, kRows = 128 * kTiles;
+    // a key tile against two query tiles takes about 3500 clocks, against one 2600
+    static constexpr int kPairWeight = 4, kOneWeight = 3;
+    static constexpr int kMinUnits = kTiles == 1 ? 2 : 2 * kPairWeight;
+    static __device__ __forceinline__ int32_t weight(const Params& p, int32_t n, int32_t block) {
+        if (kTiles == 1) return 1;
+        return n - block * kTiles * p.tile_nodes > p.tile_nodes ? kPairWeight : kOneWeight;
+    }
     static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) {
         return (n + kTiles * p.tile_nodes - 1) / (kTiles * p.tile_nodes);
     }
@@ -70,7 +81,12 @@ struct Seq {
     int32_t tok0, n, len;         // first token, nodes, cached tokens
     int32_t cached_tiles, tiles;  // key tiles of one segment: cached ones, then the tree's own
     int32_t blocks;               // row blocks
-    __device__ __forceinline__ int64_t work(const Params& p) const { return static_cast<int64_t>(tiles) * blocks * p.num_kv_heads; }
+    int32_t weight, last_weight;  // of the key tiles of all blocks but the last, and of the last
+    __device__ __forceinline__ int64_t head_work() const {
+        return static_cast<int64_t>(tiles) * (static_cast<int64_t>(blocks - 1) * weight + last_weight);
+    }
+    __device__ __forceinline__ int64_t work(const Params& p) const { return n > 0 ? head_work() * p.num_kv_heads : 0; }
+    __device__ __forceinline__ int32_t block_weight(int32_t block) const { return block + 1 < blocks ? weight : last_weight; }
 };
 
 // Offsets that leave the packed tensors or the block table, and a tree larger than the caller's bound, make a sequence
@@ -91,22 +107,25 @@ __device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* da
     q.cached_tiles = q.len / Cut::kTile + (q.len % Cut::kTile != 0 ? 1 : 0);
     q.tiles = q.n > 0 ? q.cached_tiles + (q.n + Cut::kTile - 1) / Cut::kTile : 0;
     q.blocks = Cut::blocks(p, q.n);
-    if (q.work(p) > INT32_MAX) {  // beyond any memory; the walk counts a sequence's tiles in 32 bits
+    q.weight = Cut::weight(p, q.n, 0);
+    q.last_weight = q.n > 0 ? Cut::weight(p, q.n, q.blocks - 1) : q.weight;
+    if (q.work(p) > INT32_MAX) {  // beyond any memory; the walk counts a sequence's units in 32 bits
         if (data_error != nullptr) *data_error = 1;
         q.n = q.len = q.cached_tiles = q.tiles = q.blocks = 0;
     }
     return q;
 }
 
-// The line of `total` tiles is cut into pieces of piece_tiles() tiles (the last ones may be short or empty).
+// The line of `total` units is cut into pieces of piece_units() units (the last ones may be short or empty; none is shorter
+// than a tile's weight otherwise, so each of a segment's pieces holds a tile).
 template <class Cut>
-__device__ __forceinline__ int64_t piece_tiles(int64_t total, int32_t ctas) {
-    const int64_t even = (total + ctas - 1) / ctas;
-    return even > Cut::kMinTiles ? even : Cut::kMinTiles;
+__device__ __forceinline__ int64_t piece_units(int64_t total, int32_t ctas) {
+    const int64_t even = (total >> 31) == 0 ? (static_cast<uint32_t>(total) + ctas - 1u) / static_cast<uint32_t>(ctas) : (total + ctas - 1) / ctas;
+    return even > Cut::kMinUnits ? even : Cut::kMinUnits;
 }
-__device__ __forceinline__ int32_t piece_of(int64_t tile, int64_t size) {
-    if ((tile >> 31) == 0 && (size >> 31) == 0) return static_cast<int32_t>(static_cast<uint32_t>(tile) / static_cast<uint32_t>(size));
-    return static_cast<int32_t>(tile / size);
+__device__ __forceinline__ int32_t piece_of(int64_t unit, int64_t size) {
+    if ((unit >> 31) == 0 && (size >> 31) == 0) return static_cast<int32_t>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(size));
+    return static_cast<int32_t>(unit / size);
 }
 
 __device__ __forceinline__ int64_t warp_scan(int64_t x, int lane) {  // inclusive
@@ -139,11 +158,11 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* warp_sum, int6
 // Where a CTA's piece starts (in shared memory).
 struct Start {
     int64_t warp_sum[16];
-    int32_t seq, off;  // its first tile: sequence, and tile within that sequence's work
-    int32_t tiles;     // how many
+    int32_t seq, off;  // its first unit: sequence, and unit within that sequence's work
+    int32_t units;     // how many
 };
 
-// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also leaves every sequence's first tile in
+// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also leaves every sequence's first unit in
 // the workspace and reports bad offsets.
 template <class Cut, int kWarps>
 __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32_t* data_error) {
@@ -164,7 +183,7 @@ __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32
         }
         total += all;
     }
-    const int64_t size = piece_tiles<Cut>(total, p.ctas);
+    const int64_t size = piece_units<Cut>(total, p.ctas);
     const int64_t begin = min(total, size * static_cast<int64_t>(blockIdx.x)), end = min(total, begin + size);
     int64_t carry = 0;
     for (int32_t base = 0; base < p.batch; base += kThreads) {
@@ -180,13 +199,13 @@ __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32
                 start->seq = s;
                 start->off = static_cast<int32_t>(begin - before);
             }
-            if (blockIdx.x == 0) p.seq_tile0[s] = before;
+            if (blockIdx.x == 0) p.seq_unit0[s] = before;
         }
         carry += all;
     }
     if (threadIdx.x == 0) {
-        start->tiles = static_cast<int32_t>(end - begin);
-        if (blockIdx.x == 0) p.seq_tile0[p.batch] = total;
+        start->units = static_cast<int32_t>(end - begin);
+        if (blockIdx.x == 0) p.seq_unit0[p.batch] = total;
     }
     __syncthreads();
 }
@@ -195,18 +214,22 @@ __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32
 template <class Cut>
 struct Walk {
     int32_t s, head, block, t0, t1;  // current segment: sequence, KV head, row block, key tiles [t0, t1)
-    int32_t left;                    // tiles of the piece behind t1
+    int32_t left;                    // units of the piece behind t1
     Seq q;
-    __device__ __forceinline__ Walk(const Params& p, const Start* start) : s(start->seq), head(0), block(0), t0(0), t1(0), left(start->tiles), q() {
+    __device__ __forceinline__ Walk(const Params& p, const Start* start) : s(start->seq), head(0), block(0), t0(0), t1(0), left(start->units), q() {
         if (left == 0) return;
         q = read_seq<Cut>(p, s, nullptr);
-        const int32_t seg = start->off / q.tiles;
-        t1 = start->off - seg * q.tiles;
-        head = seg / q.blocks;
-        block = seg - head * q.blocks;
+        const int32_t per_head = static_cast<int32_t>(q.head_work()), per_block = q.tiles * q.weight;
+        head = start->off / per_head;
+        int32_t off = start->off - head * per_head;
+        block = min(off / per_block, q.blocks - 1);
+        off -= block * per_block;
+        const int32_t w = q.block_weight(block);
+        t1 = (off + w - 1) / w;
+        left -= t1 * w - off;
     }
     __device__ __forceinline__ bool next(const Params& p) {
-        if (left == 0) return false;
+        if (left <= 0) return false;
         if (t1 == q.tiles) {
             t1 = 0;
             if (++block == q.blocks) {
@@ -220,36 +243,55 @@ struct Walk {
                 }
             }
         }
+        const int32_t w = q.block_weight(block);
         t0 = t1;
-        t1 = min(q.tiles, t0 + left);
-        left -= t1 - t0;
+        t1 = min(q.tiles, t0 + (left + w - 1) / w);
+        left -= (t1 - t0) * w;
         return true;
     }
 };
 
 // Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  kSplit warps share a row (one
-// long sequence is cut into dozens of pieces for a handful of rows): each takes every kSplit-th piece.
+// long sequence is cut into dozens of pieces for a handful of rows): each takes every kSplit-th piece.  Rows are numbered
+// within their sequence (chunks blocks each), or over all tokens where token_seq names each token's sequence.  Launched on
+// top of the attention kernel: it reads the lengths and waits for that kernel only then.
 constexpr int kJoinWarps = 8;
 template <int D, class Cut, int kSplit>
-__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params p, int32_t chunks) {
+__global__ void __launch_bounds__(kJoinWarps * 32, 5) tree_join_kernel(const Params p, int32_t chunks) {
     constexpr int kCols = D / 32;
     __shared__ float partial[kSplit > 1 ? kJoinWarps : 1][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % kSplit;
-    const int32_t s = blockIdx.x / chunks;
-    const Seq q = read_seq<Cut>(p, s, nullptr);
-    const int32_t i = (blockIdx.x - s * chunks) * (kJoinWarps / kSplit) + warp / kSplit;
-    const bool there = i < q.n * p.num_q_heads;
-    int32_t node = 0, head = 0, c0 = 0, c1 = 0, row = 0;
-    if (there) {
+    int32_t s, node = 0, head = 0;
+    Seq q;
+    bool there;
+    if (p.token_seq != nullptr) {
+        const int64_t i = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / kSplit) + warp / kSplit;
+        const int64_t token = i / p.num_q_heads;
+        there = token < p.total_tokens;
+        s = there ? p.token_seq[token] : -1;
+        there = s >= 0;
+        q = read_seq<Cut>(p, there ? s : 0, nullptr);
+        node = static_cast<int32_t>(token - q.tok0);
+        head = static_cast<int32_t>(i - token * p.num_q_heads);
+        there = there && node < q.n;
+    } else {
+        s = blockIdx.x / chunks;
+        q = read_seq<Cut>(p, s, nullptr);
+        const int32_t i = (blockIdx.x - s * chunks) * (kJoinWarps / kSplit) + warp / kSplit;
+        there = i < q.n * p.num_q_heads;
         node = i / p.num_q_heads;
         head = i - node * p.num_q_heads;
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int32_t c0 = 0, c1 = 0, row = 0;
+    if (there) {
         const int32_t kv_head = head / p.group;
         int32_t block;
         Cut::place(p, node, head - kv_head * p.group, &block, &row);
-        const int64_t size = piece_tiles<Cut>(p.seq_tile0[p.batch], p.ctas);
-        const int64_t tile0 = p.seq_tile0[s] + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.tiles;
-        c0 = piece_of(tile0, size);
-        c1 = piece_of(tile0 + q.tiles - 1, size);
+        const int64_t size = piece_units<Cut>(p.seq_unit0[p.batch], p.ctas);
+        const int64_t unit0 = p.seq_unit0[s] + kv_head * q.head_work() + static_cast<int64_t>(block) * q.tiles * q.weight;
+        c0 = piece_of(unit0, size);
+        c1 = piece_of(unit0 + static_cast<int64_t>(q.tiles - 1) * q.block_weight(block), size);
     }
     const bool cut = c0 != c1;  // otherwise the row was written whole
     if (kSplit == 1 && !cut) return;
@@ -260,7 +302,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params
 #pragma unroll
     for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
     if (cut) {
-        for (int32_t c = c0 + lane; c <= c1; c += 32) {
+        const float2 mine = c0 + lane <= c1 ? p.part_ml[slot(c0 + lane)] : make_float2(-CUDART_INF_F, 0.f);
+        top = mine.x;
+        unused = c0 + lane == c1 && mine.y < 0.f;
+        for (int32_t c = c0 + 32 + lane; c <= c1; c += 32) {
             const float2 ml = p.part_ml[slot(c)];
             top = fmaxf(top, ml.x);
             if (c == c1) unused = ml.y < 0.f;
@@ -272,7 +317,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params
             for (int32_t base = c0; base <= c1; base += 32) {
                 float f = 0.f;  // this lane's piece's factor
                 if (base + lane <= c1) {
-                    const float2 ml = p.part_ml[slot(base + lane)];
+                    const float2 ml = base == c0 ? mine : p.part_ml[slot(base + lane)];
                     f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
                     sum = fmaf(f, ml.y, sum);
                 }
@@ -314,17 +359,34 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params
 #pragma unroll
     for (int k = 0; k < kCols / 2; ++k) w[k] = unused ? 0u : pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
     uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + out_row * D + lane * kCols);
-#pragma unroll
-    for (int k = 0; k < kCols / 2; ++k) dst[k] = w[k];
+    if (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[kCols / 2 - 1]);
+    else *dst = w[0];
     if (lane == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
+}
+
+// Launches a kernel that may start before the one in front of it has ended (it waits by itself where it has to).
+template <class Kernel, class... Args>
+rpx_status_t launch_on_top(Kernel* kernel, unsigned grid, unsigned threads, size_t smem, cudaStream_t stream, const Args&... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(grid);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...) == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
 }
 
 template <int D, class Cut, int kSplit>
 rpx_status_t launch_join_split(const Params& p, int32_t max_tree, cudaStream_t stream) {
     const int64_t chunks = (static_cast<int64_t>(max_tree) * p.num_q_heads * kSplit + kJoinWarps - 1) / kJoinWarps;
-    if (chunks * p.batch > INT32_MAX) return RPX_ERR_SHAPE;
-    tree_join_kernel<D, Cut, kSplit><<<static_cast<unsigned>(chunks * p.batch), kJoinWarps * 32, 0, stream>>>(p, static_cast<int32_t>(chunks));
-    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+    const int64_t by_tokens = (p.total_tokens * p.num_q_heads * kSplit + kJoinWarps - 1) / kJoinWarps;
+    const int64_t grid = p.token_seq != nullptr ? by_tokens : chunks * p.batch;
+    if (grid > INT32_MAX) return RPX_ERR_SHAPE;
+    return launch_on_top(tree_join_kernel<D, Cut, kSplit>, static_cast<unsigned>(grid), kJoinWarps * 32, 0, stream, p, static_cast<int32_t>(chunks));
 }
 template <int D, class Cut>
 rpx_status_t launch_join(const Params& p, int32_t max_tree, cudaStream_t stream) {
@@ -333,7 +395,7 @@ rpx_status_t launch_join(const Params& p, int32_t max_tree, cudaStream_t stream)
     return p.ctas > 8 * segments ? launch_join_split<D, Cut, 4>(p, max_tree, stream) : launch_join_split<D, Cut, 1>(p, max_tree, stream);
 }
 
-// The pass's workspace: sequences' first tiles, then the pieces' rows.
+// The pass's workspace: sequences' first units, then the pieces' rows.
 template <class Cut>
 inline size_t join_workspace(int32_t batch, int32_t ctas, int32_t head_dim) {
     const size_t rows = static_cast<size_t>(ctas) * 2 * Cut::kRows;
@@ -342,7 +404,7 @@ inline size_t join_workspace(int32_t batch, int32_t ctas, int32_t head_dim) {
 template <class Cut>
 inline void carve_workspace(Params& p, void* workspace) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    p.seq_tile0 = reinterpret_cast<int64_t*>(ws);
+    p.seq_unit0 = reinterpret_cast<int64_t*>(ws);
     ws += align_up(static_cast<size_t>(p.batch + 1) * sizeof(int64_t), 256);
     p.part_ml = reinterpret_cast<float2*>(ws);
     ws += align_up(static_cast<size_t>(p.ctas) * 2 * Cut::kRows * sizeof(float2), 256);

@@ -8,7 +8,7 @@
 // behind the products of another.  So there are always two score buffers in flight:
 //   two query tiles  the buffers are the query tiles, both walk every key tile;
 //   one query tile   the buffers take turns: buffer t walks the key tiles t, t + 2, .. with a running maximum, sum and
-//                    output of its own, and the warps of buffer 0 join the two straight out of TMEM at the end.
+//                    output of its own, and both buffers' warps add the two up straight out of TMEM at the end.
 //   warps 0-3, 4-7 : softmax of buffer 0, 1: thread = row = TMEM lane
 //   warp  8        : producer: Q once per segment, K and V through rings of their own (K runs a tile ahead, so it is not
 //                    held up behind a V slot), one TMA box per 16-token page
@@ -56,11 +56,11 @@ struct Ctl {
     uint64_t p_ready[2];  // softmax -> tensor core
     uint64_t o_done[2];   // tensor core -> softmax: the segment's last product into O_t
     uint64_t o_free[2];   // softmax -> tensor core: O_t has been read
-    uint64_t ml_ready;    // buffer 1's maxima and sums are in `ml`
+    uint64_t ml_ready;    // both buffers' maxima and sums are in `ml`
     uint64_t drain;
     Start start;
     uint32_t tmem_base, abort_flag, drain_flag, data_error;
-    float2 ml[kTile];
+    float2 ml[2][kTile];
 };
 
 // Key tiles lie as [group of 8 keys][half][8 rows][128 bytes], swizzled: a 16-token page (two groups, both halves) is one
@@ -102,9 +102,9 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             mbar_init(&ctl->s_full[t], 1);
             mbar_init(&ctl->p_ready[t], 4);
             mbar_init(&ctl->o_done[t], 1);
-            mbar_init(&ctl->o_free[t], 4);
+            mbar_init(&ctl->o_free[t], 8);
         }
-        mbar_init(&ctl->ml_ready, 4);
+        mbar_init(&ctl->ml_ready, 8);
         mbar_init(&ctl->drain, 1);
         ctl->abort_flag = ctl->drain_flag = ctl->data_error = 0;
         fence_barrier_init();
@@ -355,7 +355,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         const uint32_t my_s = tmem_base + t * 128 + lane_addr, my_o = tmem_base + 256 + t * 128 + lane_addr;
         uint32_t steps = 0;              // this buffer's steps so far
         uint32_t used[2] = {0, 0};       // segments in which each buffer took part
-        uint32_t joined = 0;             // segments in which buffer 0 took buffer 1's share
+        uint32_t turns = 0;              // segments in which the buffers took turns
         bool ok = true, have_sets = false;
         while (ok && walk.next(p)) {
             const Seq q = walk.q;
@@ -499,35 +499,37 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             if (two_terms) run_steps(std::true_type{});
             else run_steps(std::false_type{});
             if (!ok) break;
-            // ---- the segment's rows
+            // ---- the segment's rows.  Two query tiles: each buffer's warps write their own.  One: the warps of both buffers
+            // add the two outputs up, one half of the columns each.
             const bool with_1 = paired || n > 1;  // buffer 1 took part
-            if (t == 1 && !with_1) continue;
-            ok = mbar_wait(&ctl->o_done[t], used[t] & 1u, abort_flag);
-            if (!ok) break;
-            tc_fence_after_sync();
             float f0 = 1.f, f1 = 0.f, top = run_max, sum = run_sum;
-            const bool takes_1 = t == 0 && !paired && with_1;
-            if (t == 1 && !paired) {  // buffer 0's warps take it from here
-                ctl->ml[row] = make_float2(run_max, run_sum);
+            if (paired) {
+                ok = mbar_wait(&ctl->o_done[t], used[t] & 1u, abort_flag);
+            } else {
+                // (whoever has let go of O_0 has read the maxima and sums of the segment before)
+                ok = used[0] == 0 || mbar_wait(&ctl->o_free[0], (used[0] - 1) & 1u, abort_flag);
+                if (!ok) break;
+                ctl->ml[t][row] = make_float2(run_max, run_sum);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl->ml_ready);
-                ++used[0];
-                ++used[1];
-                continue;
+                ok = mbar_wait(&ctl->ml_ready, turns & 1u, abort_flag) && mbar_wait(&ctl->o_done[0], used[0] & 1u, abort_flag) &&
+                     (!with_1 || mbar_wait(&ctl->o_done[1], used[1] & 1u, abort_flag));
+                ++turns;
+                if (ok) {
+                    const float2 a = ctl->ml[0][row], b = ctl->ml[1][row];
+                    top = fmaxf(a.x, b.x);
+                    f0 = a.x == -CUDART_INF_F ? 0.f : fast_exp2(a.x - top);
+                    f1 = b.x == -CUDART_INF_F ? 0.f : fast_exp2(b.x - top);
+                    sum = f0 * a.y + f1 * b.y;
+                }
             }
-            if (takes_1) {
-                ok = mbar_wait(&ctl->o_done[1], used[1] & 1u, abort_flag) && mbar_wait(&ctl->ml_ready, joined & 1u, abort_flag);
-                if (!ok) break;
-                tc_fence_after_sync();
-                ++joined;
-                const float2 ml = ctl->ml[row];
-                top = fmaxf(run_max, ml.x);
-                f0 = run_max == -CUDART_INF_F ? 0.f : fast_exp2(run_max - top);
-                f1 = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
-                sum = f0 * run_sum + f1 * ml.y;
-            }
+            if (!ok) break;
+            tc_fence_after_sync();
             ++used[0];
             if (with_1) ++used[1];
+            const bool adds = !paired && with_1;
+            const uint32_t o_addr = tmem_base + 256 + (paired ? t * 128 : 0) + lane_addr;
+            const int c_begin = paired || t == 0 ? 0 : D / 64, c_end = paired || t == 1 ? D / 32 : D / 64;
             const bool whole = walk.t0 == 0 && walk.t1 == q.tiles;
             const bool unused = walk.t1 == q.tiles && !row_used;
             const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
@@ -535,20 +537,25 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             const float inv = 1.f / sum;
             const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0u;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = c_begin; c < c_end; ++c) {
                 uint32_t a[32], b[32];
-                tmem_ld32(my_o + c * 32, a);
-                if (takes_1) tmem_ld32(my_o + 128 + c * 32, b);
+                tmem_ld32(o_addr + c * 32, a);
+                if (adds) tmem_ld32(o_addr + 128 + c * 32, b);
                 tmem_ld_wait();
-                if (c == D / 32 - 1) {  // O is out of TMEM: the next segment's first product may overwrite it
+                if (c == c_end - 1) {  // O is out of TMEM: the next segment's first product may overwrite it
                     tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&ctl->o_free[t]);
-                        if (takes_1) mbar_arrive(&ctl->o_free[1]);
+                    if (lane == 0) {  // eight arrivals: four warps twice, or all eight
+                        if (paired) {
+                            mbar_arrive(&ctl->o_free[t]);
+                            mbar_arrive(&ctl->o_free[t]);
+                        } else {
+                            mbar_arrive(&ctl->o_free[0]);
+                            if (adds) mbar_arrive(&ctl->o_free[1]);
+                        }
                     }
                 }
-                if (takes_1) {
+                if (adds) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         a[i] = __float_as_uint(fmaf(f0, __uint_as_float(a[i]), f1 * __uint_as_float(b[i])));
@@ -576,13 +583,14 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                                      a[8 * i + 6], a[8 * i + 7]);
                 }
             }
-            if (row_valid) {
+            if (row_valid && (paired || t == 0)) {
                 if (!whole) p.part_ml[slot] = make_float2(top, unused ? -1.f : sum);
                 else if (p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
             }
         }
     }
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join may take this CTA's place and wait
     tc_fence_before_sync();
     __syncthreads();
     if (warp == kMmaWarp) {
@@ -597,11 +605,12 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 }
 
 template <int D, bool kPaired>
-rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* values) {
+rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const int32_t* token_seq, const void* values) {
     using L = Layout<D, kPaired>;
     using Cut = NodeCut<L::kQTiles>;
     Params p = make_params(a);
     p.sets = sets;
+    p.token_seq = token_seq;
     p.set_words = tree_set_words(a.max_tree);
     const int sms = sm_count();
     if (sms <= 0) return RPX_ERR_CUDA;
@@ -636,17 +645,7 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* va
     static_assert(smem <= 232448, "shared memory of one CTA");
     auto* kernel = tree_tile_kernel<D, kPaired>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return RPX_ERR_CUDA;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>(p.ctas));
-    config.blockDim = dim3(kThreads);
-    config.dynamicSmemBytes = smem;
-    config.stream = a.stream;
-    config.attrs = attr;
-    config.numAttrs = 1;
-    if (cudaLaunchKernelEx(&config, kernel, tq, tk, tv, tkc, tvc, static_cast<const Params>(p)) != cudaSuccess) return RPX_ERR_CUDA;
+    if (rpx_status_t rc = launch_on_top(kernel, static_cast<unsigned>(p.ctas), kThreads, smem, a.stream, tq, tk, tv, tkc, tvc, p)) return rc;
     return launch_join<D, Cut>(p, a.max_tree, a.stream);
 }
 
@@ -659,10 +658,10 @@ size_t tree_tile_workspace(int32_t batch, int32_t head_dim, int32_t max_tree, in
     return paired(max_tree, group) ? join_workspace<NodeCut<2>>(batch, kMaxCtas, head_dim) : join_workspace<NodeCut<1>>(batch, kMaxCtas, head_dim);
 }
 
-rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const void* values) {
+rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const int32_t* token_seq, const void* values) {
     if (paired(a.max_tree, a.num_q_heads / a.num_kv_heads))
-        return a.head_dim == 128 ? launch_tile<128, true>(a, sets, values) : launch_tile<64, true>(a, sets, values);
-    return a.head_dim == 128 ? launch_tile<128, false>(a, sets, values) : launch_tile<64, false>(a, sets, values);
+        return a.head_dim == 128 ? launch_tile<128, true>(a, sets, token_seq, values) : launch_tile<64, true>(a, sets, token_seq, values);
+    return a.head_dim == 128 ? launch_tile<128, false>(a, sets, token_seq, values) : launch_tile<64, false>(a, sets, token_seq, values);
 }
 
 }  // namespace rpx
