@@ -39,11 +39,11 @@ rpx_status_t check_cache(const rpx_kv_cache_t* c, int32_t batch) {
     return RPX_OK;
 }
 
-// Workspace of a tree pass.  Streaming form: its own.  Tensor-core form: its own, the ancestor sets, the tokens' sequences,
-// and the tree's values with unused rows cleared.  float32: the attention call's piece and the sets.
+// Workspace of a tree pass.  Streaming form: its own.  Tensor-core form: its own, the ancestor sets, and the tree's values
+// with unused rows cleared.  float32: the attention call's piece and the sets.
 struct TreeWorkspace {
     bool streams;
-    size_t sets_off, seq_off, values_off, bytes;
+    size_t sets_off, values_off, bytes;
 };
 TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t max_tree) {
     TreeWorkspace w = {};
@@ -51,17 +51,14 @@ TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t b
     const int32_t group = d->num_q_heads / d->num_kv_heads;
     w.streams = d->dtype == RPX_BF16 && tree_streams(max_tree, group);
     if (w.streams) {
-        w.bytes = align_up(tree_stream_workspace(batch, d->head_dim), kWsAlign);
+        w.bytes = align_up(tree_stream_workspace(d->head_dim), kWsAlign);
         return w;
     }
-    const size_t own = d->dtype == RPX_F32 ? attn_workspace(d, tokens, true) : group > 128 ? 0 : tree_tile_workspace(batch, d->head_dim, max_tree, group);
+    const size_t own = d->dtype == RPX_F32 ? attn_workspace(d, tokens, true) : group > 128 ? 0 : tree_tile_workspace(d->head_dim, max_tree, group);
     w.sets_off = align_up(own, kWsAlign);
-    w.seq_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
-    w.bytes = w.seq_off;
-    if (d->dtype == RPX_BF16) {
-        w.values_off = w.seq_off + align_up(static_cast<size_t>(tokens) * sizeof(int32_t), kWsAlign);
-        w.bytes = w.values_off + align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
-    }
+    w.values_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
+    w.bytes = w.values_off;
+    if (d->dtype == RPX_BF16) w.bytes += align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
     return w;
 }
 
@@ -158,12 +155,11 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
         uint8_t* ws = static_cast<uint8_t*>(workspace);
         uint32_t* sets = reinterpret_cast<uint32_t*>(ws + tree_ws.sets_off);
         if (desc->dtype == RPX_BF16) {
-            int32_t* token_seq = reinterpret_cast<int32_t*>(ws + tree_ws.seq_off);
             void* values = ws + tree_ws.values_off;
-            if (rpx_status_t rc = launch_tree_sets(t, sets, token_seq, values)) return rc;
-            return launch_tree_tile(t, sets, token_seq, values);
+            if (rpx_status_t rc = launch_tree_sets(t, sets, values)) return rc;
+            return launch_tree_tile(t, sets, values);
         }
-        if (rpx_status_t rc = launch_tree_sets(t, sets, nullptr, nullptr)) return rc;
+        if (rpx_status_t rc = launch_tree_sets(t, sets, nullptr)) return rc;
         a.tree_sets = sets;
         a.tree_words = tree_set_words(max_q_len);
     }

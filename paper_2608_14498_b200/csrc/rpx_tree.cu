@@ -124,6 +124,7 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
         }
         if (lane == 0) ctl->issued = it;
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // every load is on its way: the join may start soon
     } else {
         // =========================================================== consumers
         // After a wait that ran out (ok == false) a warp goes through the rest of its walk without waiting: every warp
@@ -366,7 +367,6 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (lane == 0) mbar_arrive(&ctl->empty[last]);
         }
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join may take this CTA's place and wait
     __syncthreads();
     if (threadIdx.x == 0 && ctl->abort_flag != 0u) {  // copies still in flight get a moment to land before the memory is released
         const uint32_t n = ctl->issued, first = n > kStages ? n - kStages : 0u;
@@ -395,7 +395,7 @@ rpx_status_t launch_stream(const TreeArgs& a, const CUtensorMap& tk, const CUten
     carve_workspace<Cut>(p, a.workspace);
     kernel<<<static_cast<unsigned>(p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);
     if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
-    return launch_join<D, Cut>(p, a.max_tree, a.stream);
+    return launch_join<D, Cut>(p, a.stream);
 }
 
 template <int D>
@@ -432,12 +432,12 @@ rpx_status_t launch_stream_d(const TreeArgs& a) {
 
 // ------------------------------------------------------------------ ancestor sets and values for the other forms
 // One warp per token: its ancestor set as mask words (lane w holds word w while all lanes walk the path to the root), all
-// zero for a node that is not in use or a token of no sequence; and, for the tensor-core form, the token's sequence and a
-// copy of the tree's V with those rows cleared (a probability of 0 must not meet what they hold).
+// zero for a node that is not in use or a token of no sequence; and, for the tensor-core form, a copy of the
+// tree's V with those rows cleared (a probability of 0 must not meet what they hold).
 constexpr int kSetWarps = 8;
 __global__ void __launch_bounds__(kSetWarps * 32)
 tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ parents, int32_t batch, int64_t total_tokens,
-                 int32_t max_tree, int32_t words, uint32_t* sets, int32_t* token_seq, const __nv_bfloat16* v, int64_t v_stride, int32_t v_chunks,
+                 int32_t max_tree, int32_t words, uint32_t* sets, const __nv_bfloat16* v, int64_t v_stride, int32_t v_chunks,
                  __nv_bfloat16* v_copy, int32_t* status) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the attention kernel may start on its cached tiles
     const int lane = threadIdx.x & 31;
@@ -467,7 +467,6 @@ tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ par
     if (!good && lane == 0 && status != nullptr) atomicCAS(status, 0, RPX_ERR_DEVICE_DATA);
     used = used && good;
     if (lane < words) sets[token * words + lane] = used ? bits : 0u;
-    if (token_seq != nullptr && lane == 0) token_seq[token] = inside ? lo : -1;
     if (v_copy != nullptr) {
         const uint4* src = reinterpret_cast<const uint4*>(v + token * v_stride);
         uint4* dst = reinterpret_cast<uint4*>(v_copy) + token * v_chunks;
@@ -479,10 +478,10 @@ tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ par
 
 int32_t tree_set_words(int32_t max_tree) { return (max_tree + 127) / 128 * 4; }
 
-rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, int32_t* token_seq, void* v_copy) {
+rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy) {
     const int64_t blocks = (a.total_tokens + kSetWarps - 1) / kSetWarps;
     tree_sets_kernel<<<static_cast<unsigned>(blocks), kSetWarps * 32, 0, a.stream>>>(
-        a.cu_seqlens, a.parents, a.batch, a.total_tokens, a.max_tree, tree_set_words(a.max_tree), sets, token_seq,
+        a.cu_seqlens, a.parents, a.batch, a.total_tokens, a.max_tree, tree_set_words(a.max_tree), sets,
         static_cast<const __nv_bfloat16*>(a.v), a.v_tok_stride, a.num_kv_heads * a.head_dim / 8,
         static_cast<__nv_bfloat16*>(v_copy), a.device_status);
     return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
@@ -495,7 +494,7 @@ bool tree_streams(int32_t max_tree, int32_t group) {
     return max_tree <= kMaxNodes && (static_cast<int64_t>(max_tree) * group <= 32 || group > 128);
 }
 
-size_t tree_stream_workspace(int32_t batch, int32_t head_dim) { return join_workspace<RowCut<64>>(batch, kMaxCtas, head_dim); }
+size_t tree_stream_workspace(int32_t head_dim) { return join_workspace<RowCut<64>>(kMaxCtas, head_dim); }
 
 rpx_status_t launch_tree_stream(const TreeArgs& a) {
     return a.head_dim == 128 ? launch_stream_d<128>(a) : launch_stream_d<64>(a);

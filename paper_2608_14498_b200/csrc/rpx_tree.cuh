@@ -32,12 +32,10 @@ struct Params {
     int32_t tile_nodes;    // tensor-core form: nodes per query tile of 128 rows (128 / group)
     const __nv_bfloat16 *k_cache, *v_cache;
     const uint32_t* sets;  // tensor-core form: ancestor sets [tokens][set_words]
-    const int32_t* token_seq;  // tensor-core form: each token's sequence, -1 for none
     int32_t set_words;
     float scale_log2;
     __nv_bfloat16* out;    // [tokens][H_q][D]
     float* lse;            // nullable
-    int64_t* seq_unit0;    // workspace [batch + 1]: number of the sequence's first unit; the last entry is the total
     float2* part_ml;       // workspace [ctas][2][rows per block]; a negative sum marks a node that is not in use
     float* part_o;         // workspace [ctas][2][rows per block][D]
     int32_t* status;
@@ -162,8 +160,8 @@ struct Start {
     int32_t units;     // how many
 };
 
-// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also leaves every sequence's first unit in
-// the workspace and reports bad offsets.
+// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also
+// reports bad offsets.
 template <class Cut, int kWarps>
 __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32_t* data_error) {
     constexpr int kThreads = 32 * kWarps;
@@ -199,13 +197,11 @@ __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32
                 start->seq = s;
                 start->off = static_cast<int32_t>(begin - before);
             }
-            if (blockIdx.x == 0) p.seq_unit0[s] = before;
         }
         carry += all;
     }
     if (threadIdx.x == 0) {
         start->units = static_cast<int32_t>(end - begin);
-        if (blockIdx.x == 0) p.seq_unit0[p.batch] = total;
     }
     __syncthreads();
 }
@@ -251,117 +247,151 @@ struct Walk {
     }
 };
 
-// Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  kSplit warps share a row (one
-// long sequence is cut into dozens of pieces for a handful of rows): each takes every kSplit-th piece.  Rows are numbered
-// within their sequence (chunks blocks each), or over all tokens where token_seq names each token's sequence.  Launched on
-// top of the attention kernel: it reads the lengths and waits for that kernel only then.
+// Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  kSplit == 1: a warp takes the rows
+// of one token and KV head, kJoinRows at a time.  Otherwise, for few rows: the eight warps of a block take one row, each every
+// eighth piece.  The kernel is launched on top of the attention kernel: what the lengths alone tell it works out before it waits, and after
+// that one round of loads is left.
 constexpr int kJoinWarps = 8;
+
 template <int D, class Cut, int kSplit>
-__global__ void __launch_bounds__(kJoinWarps * 32, 5) tree_join_kernel(const Params p, int32_t chunks) {
-    constexpr int kCols = D / 32;
-    __shared__ float partial[kSplit > 1 ? kJoinWarps : 1][D];
+__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params p) {
+    constexpr int kCols = D / 32, kJoinRows = kSplit > 1 ? 1 : 4;  // rows whose loads are in flight together
+    __shared__ float part_acc[kSplit > 1 ? kJoinWarps : 1][kJoinRows][D];
+    __shared__ float2 part_row[kSplit > 1 ? kJoinWarps : 1][kJoinRows];  // (maximum, sum); a negative sum: not in use
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % kSplit;
-    int32_t s, node = 0, head = 0;
-    Seq q;
-    bool there;
-    if (p.token_seq != nullptr) {
-        const int64_t i = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / kSplit) + warp / kSplit;
-        const int64_t token = i / p.num_q_heads;
-        there = token < p.total_tokens;
-        s = there ? p.token_seq[token] : -1;
-        there = s >= 0;
-        q = read_seq<Cut>(p, there ? s : 0, nullptr);
-        node = static_cast<int32_t>(token - q.tok0);
-        head = static_cast<int32_t>(i - token * p.num_q_heads);
-        there = there && node < q.n;
-    } else {
-        s = blockIdx.x / chunks;
-        q = read_seq<Cut>(p, s, nullptr);
-        const int32_t i = (blockIdx.x - s * chunks) * (kJoinWarps / kSplit) + warp / kSplit;
-        there = i < q.n * p.num_q_heads;
-        node = i / p.num_q_heads;
-        head = i - node * p.num_q_heads;
+    const int64_t task = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / kSplit) + warp / kSplit;
+    const int32_t tasks = kSplit > 1 ? p.num_q_heads : p.num_kv_heads;  // of a token
+    const int64_t token = task / tasks;
+    const int32_t head = static_cast<int32_t>(task - token * tasks), kv_head = kSplit > 1 ? head / p.group : head;
+    const int32_t h_begin = kSplit > 1 ? head - kv_head * p.group : 0, h_end = kSplit > 1 ? h_begin + 1 : p.group;
+    // ---- the token's sequence (the last that starts at or before it), the units in front of it and in all
+    int32_t s = 0;
+    for (int32_t hi = p.batch - 1; s < hi;) {
+        const int32_t mid = (s + hi + 1) >> 1;
+        if (__ldg(p.cu + mid) <= token) s = mid;
+        else hi = mid - 1;
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    int32_t c0 = 0, c1 = 0, row = 0;
-    if (there) {
-        const int32_t kv_head = head / p.group;
-        int32_t block;
-        Cut::place(p, node, head - kv_head * p.group, &block, &row);
-        const int64_t size = piece_units<Cut>(p.seq_unit0[p.batch], p.ctas);
-        const int64_t unit0 = p.seq_unit0[s] + kv_head * q.head_work() + static_cast<int64_t>(block) * q.tiles * q.weight;
-        c0 = piece_of(unit0, size);
-        c1 = piece_of(unit0 + static_cast<int64_t>(q.tiles - 1) * q.block_weight(block), size);
+    int64_t before = 0, total = 0;
+    for (int32_t i = lane; i < p.batch; i += 32) {
+        const int64_t w = read_seq<Cut>(p, i, nullptr).work(p);
+        total += w;
+        if (i < s) before += w;
     }
-    const bool cut = c0 != c1;  // otherwise the row was written whole
-    if (kSplit == 1 && !cut) return;
-    // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
-    auto slot = [&](int32_t c) { return (static_cast<int64_t>(c) * 2 + (c == c0 ? 1 : 0)) * Cut::kRows + row; };
-    float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
-    bool unused = false;
 #pragma unroll
-    for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
-    if (cut) {
-        const float2 mine = c0 + lane <= c1 ? p.part_ml[slot(c0 + lane)] : make_float2(-CUDART_INF_F, 0.f);
-        top = mine.x;
-        unused = c0 + lane == c1 && mine.y < 0.f;
-        for (int32_t c = c0 + 32 + lane; c <= c1; c += 32) {
-            const float2 ml = p.part_ml[slot(c)];
-            top = fmaxf(top, ml.x);
-            if (c == c1) unused = ml.y < 0.f;
+    for (int off = 16; off > 0; off >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, off);
+        before += __shfl_xor_sync(0xffffffffu, before, off);
+    }
+    const Seq q = read_seq<Cut>(p, s, nullptr);
+    const int32_t node = static_cast<int32_t>(token - q.tok0);
+    const bool inside = token < p.total_tokens && token >= q.tok0 && node < q.n;
+    const int64_t size = piece_units<Cut>(total, p.ctas);
+    before += kv_head * q.head_work();
+    for (int32_t h0 = h_begin; h0 < h_end; h0 += kJoinRows) {
+        int32_t c0[kJoinRows], n[kJoinRows], row[kJoinRows], most = 0;  // first piece, pieces (0: nothing to do), place in a slot
+#pragma unroll
+        for (int k = 0; k < kJoinRows; ++k) {
+            c0[k] = n[k] = row[k] = 0;
+            if (inside && h0 + k < h_end) {
+                int32_t block;
+                Cut::place(p, node, h0 + k, &block, &row[k]);
+                const int64_t unit0 = before + static_cast<int64_t>(block) * q.tiles * q.weight;
+                c0[k] = piece_of(unit0, size);
+                n[k] = piece_of(unit0 + static_cast<int64_t>(q.tiles - 1) * q.block_weight(block), size) - c0[k] + 1;
+                if (n[k] == 1) n[k] = 0;  // written whole
+                most = max(most, n[k]);
+            }
         }
-        unused = __any_sync(0xffffffffu, unused);
+        if (h0 == h_begin) asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (kSplit == 1 && most == 0) continue;
+        float top[kJoinRows], sum[kJoinRows], acc[kJoinRows][kCols];
+        bool unused[kJoinRows];
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-        if (!unused) {
-            for (int32_t base = c0; base <= c1; base += 32) {
-                float f = 0.f;  // this lane's piece's factor
-                if (base + lane <= c1) {
-                    const float2 ml = base == c0 ? mine : p.part_ml[slot(base + lane)];
-                    f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top);
-                    sum = fmaf(f, ml.y, sum);
-                }
-                const int32_t n = min(32, c1 - base + 1);
-#pragma unroll 4
-                for (int32_t j = sub; j < n; j += kSplit) {
-                    const float fj = __shfl_sync(0xffffffffu, f, j);
-                    const float* src = p.part_o + slot(base + j) * D + lane * kCols;
+        for (int k = 0; k < kJoinRows; ++k) {
+            top[k] = -CUDART_INF_F;
+            sum[k] = 0.f;
+            unused[k] = false;
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) acc[k][e] = 0.f;
+        }
+#pragma unroll (kSplit > 1 ? 8 : 2)
+        for (int32_t j = sub; j < most; j += kSplit) {
+            float2 ml[kJoinRows];
+            float4 v[kJoinRows];
+#pragma unroll
+            for (int k = 0; k < kJoinRows; ++k) {
+                ml[k] = make_float2(-CUDART_INF_F, 0.f);
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (j < n[k]) {
+                    // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
+                    const int64_t at = (static_cast<int64_t>(c0[k] + j) * 2 + (j == 0 ? 1 : 0)) * Cut::kRows + row[k];
+                    ml[k] = p.part_ml[at];
                     if (kCols == 4) {
-                        const float4 v = *reinterpret_cast<const float4*>(src);
-                        acc[0] = fmaf(fj, v.x, acc[0]);
-                        acc[1] = fmaf(fj, v.y, acc[1]);
-                        acc[kCols - 2] = fmaf(fj, v.z, acc[kCols - 2]);
-                        acc[kCols - 1] = fmaf(fj, v.w, acc[kCols - 1]);
+                        v[k] = *reinterpret_cast<const float4*>(p.part_o + at * D + lane * kCols);
                     } else {
-                        const float2 v = *reinterpret_cast<const float2*>(src);
-                        acc[0] = fmaf(fj, v.x, acc[0]);
-                        acc[1] = fmaf(fj, v.y, acc[1]);
+                        const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + lane * kCols);
+                        v[k].x = x.x;
+                        v[k].y = x.y;
                     }
                 }
             }
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            for (int k = 0; k < kJoinRows; ++k) {
+                unused[k] |= ml[k].y < 0.f;
+                if (ml[k].x == -CUDART_INF_F) continue;  // no key seen
+                const float to = fmaxf(top[k], ml[k].x);
+                const float keep = fast_exp2(top[k] - to), f = fast_exp2(ml[k].x - to);
+                top[k] = to;
+                sum[k] = fmaf(sum[k], keep, f * ml[k].y);
+                const float x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) acc[k][e] = fmaf(acc[k][e], keep, f * x[e]);
+            }
+        }
+        if (kSplit > 1) {
+#pragma unroll
+            for (int k = 0; k < kJoinRows; ++k) {
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) part_acc[warp][k][lane * kCols + e] = acc[k][e];
+                if (lane == 0) part_row[warp][k] = make_float2(top[k], unused[k] ? -1.f : sum[k]);
+            }
+            __syncthreads();
+            // the first warp finishes the row
+#pragma unroll
+            for (int k = 0; k < kJoinRows; ++k) {
+                if (warp != 0) continue;
+                top[k] = -CUDART_INF_F;
+                sum[k] = 0.f;
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) acc[k][e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < kJoinWarps; ++w) top[k] = fmaxf(top[k], part_row[w][k].x);
+#pragma unroll
+                for (int w = 0; w < kJoinWarps; ++w) {
+                    const float2 ml = part_row[w][k];
+                    unused[k] |= ml.y < 0.f;
+                    const float f = ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - top[k]);
+                    sum[k] = fmaf(f, ml.y, sum[k]);
+#pragma unroll
+                    for (int e = 0; e < kCols; ++e) acc[k][e] = fmaf(f, part_acc[w][k][lane * kCols + e], acc[k][e]);
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int k = 0; k < kJoinRows; ++k) {
+            if (n[k] == 0 || (kSplit > 1 && warp != 0)) continue;
+            const float inv = unused[k] ? 0.f : 1.f / sum[k];
+            const int64_t out_row = token * p.num_q_heads + kv_head * p.group + h0 + k;
+            uint32_t w[kCols / 2];
+#pragma unroll
+            for (int e = 0; e < kCols / 2; ++e) w[e] = unused[k] ? 0u : pack_bf16x2(acc[k][2 * e] * inv, acc[k][2 * e + 1] * inv);
+            uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + out_row * D + lane * kCols);
+            if (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[kCols / 2 - 1]);
+            else *dst = w[0];
+            if (lane == 0 && p.lse != nullptr) p.lse[out_row] = unused[k] ? -CUDART_INF_F : (top[k] + log2f(sum[k])) * kLn2;
         }
     }
-    if (kSplit > 1) {
-#pragma unroll
-        for (int k = 0; k < kCols; ++k) partial[warp][lane * kCols + k] = acc[k];
-        __syncthreads();
-        if (sub != 0 || !cut) return;
-#pragma unroll
-        for (int w = 1; w < kSplit; ++w)
-#pragma unroll
-            for (int k = 0; k < kCols; ++k) acc[k] += partial[warp + w][lane * kCols + k];
-    }
-    const float inv = unused ? 0.f : 1.f / sum;
-    const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
-    uint32_t w[kCols / 2];
-#pragma unroll
-    for (int k = 0; k < kCols / 2; ++k) w[k] = unused ? 0u : pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
-    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + out_row * D + lane * kCols);
-    if (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[kCols / 2 - 1]);
-    else *dst = w[0];
-    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
 }
 
 // Launches a kernel that may start before the one in front of it has ended (it waits by itself where it has to).
@@ -381,31 +411,27 @@ rpx_status_t launch_on_top(Kernel* kernel, unsigned grid, unsigned threads, size
 }
 
 template <int D, class Cut, int kSplit>
-rpx_status_t launch_join_split(const Params& p, int32_t max_tree, cudaStream_t stream) {
-    const int64_t chunks = (static_cast<int64_t>(max_tree) * p.num_q_heads * kSplit + kJoinWarps - 1) / kJoinWarps;
-    const int64_t by_tokens = (p.total_tokens * p.num_q_heads * kSplit + kJoinWarps - 1) / kJoinWarps;
-    const int64_t grid = p.token_seq != nullptr ? by_tokens : chunks * p.batch;
+rpx_status_t launch_join_split(const Params& p, cudaStream_t stream) {
+    const int64_t grid = (p.total_tokens * (kSplit > 1 ? p.num_q_heads : p.num_kv_heads) * kSplit + kJoinWarps - 1) / kJoinWarps;
     if (grid > INT32_MAX) return RPX_ERR_SHAPE;
-    return launch_on_top(tree_join_kernel<D, Cut, kSplit>, static_cast<unsigned>(grid), kJoinWarps * 32, 0, stream, p, static_cast<int32_t>(chunks));
+    return launch_on_top(tree_join_kernel<D, Cut, kSplit>, static_cast<unsigned>(grid), kJoinWarps * 32, 0, stream, p);
 }
 template <int D, class Cut>
-rpx_status_t launch_join(const Params& p, int32_t max_tree, cudaStream_t stream) {
-    // more than 8 pieces per segment: four warps a row
-    const int64_t segments = static_cast<int64_t>(p.batch) * p.num_kv_heads * Cut::blocks(p, max_tree);
-    return p.ctas > 8 * segments ? launch_join_split<D, Cut, 4>(p, max_tree, stream) : launch_join_split<D, Cut, 1>(p, max_tree, stream);
+rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
+    // one warp a row group needs some thousands of them to be quick (and not every row may have been cut): up to 4096 rows, a
+    // block a row
+    return p.total_tokens * p.num_q_heads <= 4096 ? launch_join_split<D, Cut, kJoinWarps>(p, stream) : launch_join_split<D, Cut, 1>(p, stream);
 }
 
-// The pass's workspace: sequences' first units, then the pieces' rows.
+// The pass's workspace: the pieces' rows.
 template <class Cut>
-inline size_t join_workspace(int32_t batch, int32_t ctas, int32_t head_dim) {
+inline size_t join_workspace(int32_t ctas, int32_t head_dim) {
     const size_t rows = static_cast<size_t>(ctas) * 2 * Cut::kRows;
-    return align_up(static_cast<size_t>(batch + 1) * sizeof(int64_t), 256) + align_up(rows * sizeof(float2), 256) + rows * head_dim * sizeof(float);
+    return align_up(rows * sizeof(float2), 256) + rows * head_dim * sizeof(float);
 }
 template <class Cut>
 inline void carve_workspace(Params& p, void* workspace) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    p.seq_unit0 = reinterpret_cast<int64_t*>(ws);
-    ws += align_up(static_cast<size_t>(p.batch + 1) * sizeof(int64_t), 256);
     p.part_ml = reinterpret_cast<float2*>(ws);
     ws += align_up(static_cast<size_t>(p.ctas) * 2 * Cut::kRows * sizeof(float2), 256);
     p.part_o = reinterpret_cast<float*>(ws);

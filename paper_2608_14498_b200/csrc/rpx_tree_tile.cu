@@ -344,6 +344,9 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             }
         }
         __syncwarp();
+        // What is left is the last segment's output: once every CTA is there, the join may start on the SMs that are free.
+        // (Earlier, and it would crowd the SMs that finish first.)
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     } else if (warp > kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     } else {
@@ -590,7 +593,6 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         }
     }
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join may take this CTA's place and wait
     tc_fence_before_sync();
     __syncthreads();
     if (warp == kMmaWarp) {
@@ -605,12 +607,11 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 }
 
 template <int D, bool kPaired>
-rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const int32_t* token_seq, const void* values) {
+rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* values) {
     using L = Layout<D, kPaired>;
     using Cut = NodeCut<L::kQTiles>;
     Params p = make_params(a);
     p.sets = sets;
-    p.token_seq = token_seq;
     p.set_words = tree_set_words(a.max_tree);
     const int sms = sm_count();
     if (sms <= 0) return RPX_ERR_CUDA;
@@ -646,7 +647,7 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const int32_t*
     auto* kernel = tree_tile_kernel<D, kPaired>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return RPX_ERR_CUDA;
     if (rpx_status_t rc = launch_on_top(kernel, static_cast<unsigned>(p.ctas), kThreads, smem, a.stream, tq, tk, tv, tkc, tvc, p)) return rc;
-    return launch_join<D, Cut>(p, a.max_tree, a.stream);
+    return launch_join<D, Cut>(p, a.stream);
 }
 
 // One query tile holds the rows of every tree: the buffers take turns throughout and the second Q tile's room goes to V.
@@ -654,14 +655,14 @@ bool paired(int32_t max_tree, int32_t group) { return max_tree > 128 / group; }
 
 }  // namespace
 
-size_t tree_tile_workspace(int32_t batch, int32_t head_dim, int32_t max_tree, int32_t group) {
-    return paired(max_tree, group) ? join_workspace<NodeCut<2>>(batch, kMaxCtas, head_dim) : join_workspace<NodeCut<1>>(batch, kMaxCtas, head_dim);
+size_t tree_tile_workspace(int32_t head_dim, int32_t max_tree, int32_t group) {
+    return paired(max_tree, group) ? join_workspace<NodeCut<2>>(kMaxCtas, head_dim) : join_workspace<NodeCut<1>>(kMaxCtas, head_dim);
 }
 
-rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const int32_t* token_seq, const void* values) {
+rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const void* values) {
     if (paired(a.max_tree, a.num_q_heads / a.num_kv_heads))
-        return a.head_dim == 128 ? launch_tile<128, true>(a, sets, token_seq, values) : launch_tile<64, true>(a, sets, token_seq, values);
-    return a.head_dim == 128 ? launch_tile<128, false>(a, sets, token_seq, values) : launch_tile<64, false>(a, sets, token_seq, values);
+        return a.head_dim == 128 ? launch_tile<128, true>(a, sets, values) : launch_tile<64, true>(a, sets, values);
+    return a.head_dim == 128 ? launch_tile<128, false>(a, sets, values) : launch_tile<64, false>(a, sets, values);
 }
 
 }  // namespace rpx
