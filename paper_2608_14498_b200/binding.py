@@ -250,13 +250,14 @@ def _stream_ptr(stream) -> int:
 
 
 def _tok_stride(t) -> int:
-    if t.dim() != 3:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3:
         raise ValueError("expected a [tokens, heads, head_dim] tensor")
-    if t.shape[0] <= 1:
-        return t.shape[1] * t.shape[2]
-    if t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+    if shape[0] <= 1:
+        return shape[1] * shape[2]
+    if stride[2] != 1 or stride[1] != shape[2]:
         raise ValueError("expected a [tokens, heads, head_dim] tensor with contiguous heads")
-    return t.stride(0)
+    return stride[0]
 
 
 def _workspace(nbytes: int, device, workspace):
@@ -448,23 +449,24 @@ def tree_attn(q, k, v, cu_seqlens_tree, parents, cached_lens, max_tree_len: int,
     (out 0, lse -inf).  Other arguments as in ``suffix_attn``."""
     torch = _torch()
     lib = load_library()
-    desc = _desc(q, k, softmax_scale)
-    total, batch = q.shape[0], cu_seqlens_tree.shape[0] - 1
-    if any(t.dtype != torch.int32 or not t.is_contiguous() for t in (cu_seqlens_tree, parents, cached_lens)):
-        raise TypeError("cu_seqlens_tree, parents and cached_lens are contiguous int32 tensors")
+    desc = ctypes.byref(_desc(q, k, softmax_scale))
+    total, heads, _ = q.shape
+    batch = cu_seqlens_tree.shape[0] - 1
+    for t in (cu_seqlens_tree, parents, cached_lens):
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError("cu_seqlens_tree, parents and cached_lens are contiguous int32 tensors")
     if parents.shape[0] != total or cached_lens.shape[0] != batch:
         raise ValueError("parents has one entry per token and cached_lens one per sequence")
     if out is None:
-        out = torch.empty((total, q.shape[1], q.shape[2]), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and return_lse:
-        lse = torch.empty((total, q.shape[1]), dtype=torch.float32, device=q.device)
-    ws = _workspace(int(lib.rpx_tree_attn_workspace_bytes(ctypes.byref(desc), total, batch, int(max_tree_len))), q.device,
-                    workspace)
-    cs = _cache_struct(cache)
-    rc = lib.rpx_tree_attn(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _tok_stride(q), _tok_stride(k), _tok_stride(v),
-                           _ptr(cu_seqlens_tree), _ptr(parents), _ptr(cached_lens), batch, total, int(max_tree_len),
-                           int(max_cached_len), ctypes.byref(cs), _ptr(out), _ptr(lse), _ptr(ws),
-                           ws.numel() * ws.element_size(), _ptr(device_status), _stream_ptr(stream))
+        lse = torch.empty((total, heads), dtype=torch.float32, device=q.device)
+    need = lib.rpx_tree_attn_workspace_bytes(desc, total, batch, max_tree_len)
+    ws = _workspace(need, q.device, workspace)
+    rc = lib.rpx_tree_attn(desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), _tok_stride(q), _tok_stride(k), _tok_stride(v),
+                           cu_seqlens_tree.data_ptr(), parents.data_ptr(), cached_lens.data_ptr(), batch, total, max_tree_len,
+                           max_cached_len, ctypes.byref(_cache_struct(cache)), out.data_ptr(), _ptr(lse), ws.data_ptr(),
+                           ws.nbytes, _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_tree_attn")
     return (out, lse) if return_lse else out
@@ -677,36 +679,42 @@ def mrope_pair_axis(sections, interleaved: bool = False):
 
 def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) -> RopeDesc:
     torch = _torch()
+    dtype = q.dtype
     code = _dtype_code(q)
-    if k.dtype != q.dtype or any(w is not None and w.dtype != q.dtype for w in (q_weight, k_weight)):
+    if k.dtype != dtype:
         raise TypeError("q, k and the norm weights must share an element type")
     if positions.dtype != torch.int32 or inv_freq.dtype != torch.float32:
         raise TypeError("positions are int32 and inv_freq float32")
-    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+    q_shape, k_shape, pos_shape = q.shape, k.shape, positions.shape
+    if len(q_shape) != 3 or len(k_shape) != 3 or k_shape[0] != q_shape[0] or k_shape[2] != q_shape[2]:
         raise ValueError("expected q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim]")
-    n, d = q.shape[0], q.shape[2]
-    if positions.dim() not in (1, 2) or positions.shape[-1] != n or (n > 1 and positions.stride(-1) != 1):
+    n, hq, d = q_shape
+    axes = pos_shape[0] if len(pos_shape) == 2 else 1
+    if len(pos_shape) not in (1, 2) or pos_shape[-1] != n or (n > 1 and positions.stride(-1) != 1):
         raise ValueError("positions are [tokens] or [axes, tokens] with contiguous tokens")
     if inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq is a contiguous [rot_dim / 2] tensor")
     for w in (q_weight, k_weight):
-        if w is not None and (tuple(w.shape) != (d,) or not w.is_contiguous()):
-            raise ValueError("norm weights are contiguous [head_dim] tensors")
-    rot = 2 * inv_freq.shape[0]
-    if pair_axis is not None and len(pair_axis) != rot // 2:
-        raise ValueError("pair_axis has one axis number per entry of inv_freq")
-    return RopeDesc(q.shape[1], k.shape[1], d, rot, positions.shape[0] if positions.dim() == 2 else 1,
-                    bytes(pair_axis) if pair_axis is not None else None, float(eps), code)
+        if w is not None:
+            if w.dtype != dtype:
+                raise TypeError("q, k and the norm weights must share an element type")
+            if w.dim() != 1 or w.shape[0] != d or not w.is_contiguous():
+                raise ValueError("norm weights are contiguous [head_dim] tensors")
+    pairs = inv_freq.shape[0]
+    if pair_axis is not None:
+        if len(pair_axis) != pairs:
+            raise ValueError("pair_axis has one axis number per entry of inv_freq")
+        pair_axis = bytes(pair_axis)
+    return RopeDesc(hq, k_shape[1], d, 2 * pairs, axes, pair_axis, eps, code)
 
 
 def _axis_stride(positions) -> int:
-    n = positions.shape[-1]
-    return positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else n
+    return positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else positions.shape[-1]
 
 
 def _rope_out(given, like):
     if given is None:
-        return _torch().empty(tuple(like.shape), dtype=like.dtype, device=like.device)
+        return _torch().empty_like(like, memory_format=_torch().contiguous_format)
     if given.shape != like.shape or given.dtype != like.dtype:
         raise ValueError("an output has the shape and element type of its input")
     return given
@@ -723,9 +731,9 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, pair_a
     lib = load_library()
     desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)
     q_out, k_out = _rope_out(q_out, q), _rope_out(k_out, k)
-    rc = lib.rpx_qk_norm_rope(ctypes.byref(desc), _ptr(q), _ptr(k), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
-                              _ptr(k_weight), _ptr(positions), _axis_stride(positions), _ptr(inv_freq), q.shape[0],
-                              _ptr(q_out), _ptr(k_out), _tok_stride(q_out), _tok_stride(k_out), _stream_ptr(stream))
+    rc = lib.rpx_qk_norm_rope(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
+                              _ptr(k_weight), positions.data_ptr(), _axis_stride(positions), inv_freq.data_ptr(), q.shape[0],
+                              q_out.data_ptr(), k_out.data_ptr(), _tok_stride(q_out), _tok_stride(k_out), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_qk_norm_rope")
     return q_out, k_out

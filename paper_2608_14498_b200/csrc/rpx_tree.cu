@@ -390,11 +390,12 @@ rpx_status_t launch_stream(const TreeArgs& a, const CUtensorMap& tk, const CUten
     using L = Layout<D>;
     using Cut = RowCut<16 * kRowTiles>;
     auto* kernel = tree_stream_kernel<D, kRowTiles>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess)
-        return RPX_ERR_CUDA;
+    if (rpx_status_t rc = allow_smem(reinterpret_cast<const void*>(kernel), L::kSmemBytes)) return rc;
     carve_workspace<Cut>(p, a.workspace);
-    kernel<<<static_cast<unsigned>(p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);
+    const int64_t whole = whole_grid<Cut>(p, a.max_cached);
+    kernel<<<static_cast<unsigned>(whole > 0 ? whole : p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);
     if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
+    if (whole > 0) return RPX_OK;
     return launch_join<D, Cut>(p, a.stream);
 }
 

@@ -29,6 +29,7 @@ struct Params {
     int32_t batch, num_q_heads, num_kv_heads, group, max_tree;
     int64_t total_tokens;
     int32_t ctas;          // pieces the line is cut into at most (the grid)
+    int32_t whole_blocks;  // > 0: short sequences, a CTA per segment (this many blocks per head) and nothing to join
     int32_t tile_nodes;    // tensor-core form: nodes per query tile of 128 rows (128 / group)
     const __nv_bfloat16 *k_cache, *v_cache;
     const uint32_t* sets;  // tensor-core form: ancestor sets [tokens][set_words]
@@ -46,7 +47,7 @@ struct Params {
 // first unit.  All blocks but a sequence's last have the same weight.
 template <int kRows_>
 struct RowCut {  // blocks of kRows rows, row = node * group + head within the KV head's group
-    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 2;
+    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 2, kWholeTiles = 12;
     static __device__ __forceinline__ int32_t weight(const Params&, int32_t, int32_t) { return 1; }
     static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) { return (n * p.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ void place(const Params& p, int32_t node, int32_t h, int32_t* block, int32_t* row) {
@@ -57,7 +58,7 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
 };
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
-    static constexpr int kTile = 128, kRows = 128 * kTiles;
+    static constexpr int kTile = 128, kRows = 128 * kTiles, kWholeTiles = 6;
     // a key tile against two query tiles takes about 3500 clocks, against one 2600
     static constexpr int kPairWeight = 4, kOneWeight = 3;
     static constexpr int kMinUnits = kTiles == 1 ? 2 : 2 * kPairWeight;
@@ -165,6 +166,19 @@ struct Start {
 template <class Cut, int kWarps>
 __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32_t* data_error) {
     constexpr int kThreads = 32 * kWarps;
+    if (p.whole_blocks > 0) {
+        if (threadIdx.x == 0) {
+            const int32_t per_seq = p.num_kv_heads * p.whole_blocks, s = blockIdx.x / per_seq, i = blockIdx.x - s * per_seq;
+            const int32_t head = i / p.whole_blocks, block = i - head * p.whole_blocks;
+            const Seq q = read_seq<Cut>(p, s, i == 0 ? data_error : nullptr);
+            const bool there = q.n > 0 && block < q.blocks;
+            start->seq = s;
+            start->off = there ? static_cast<int32_t>(head * q.head_work()) + block * q.tiles * q.weight : 0;
+            start->units = there ? q.tiles * q.block_weight(block) : 0;
+        }
+        __syncthreads();
+        return;
+    }
     uint32_t* report = blockIdx.x == 0 ? data_error : nullptr;
     if (threadIdx.x == 0) {
         start->seq = p.batch;
@@ -421,6 +435,18 @@ rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
     // one warp a row group needs some thousands of them to be quick (and not every row may have been cut): up to 4096 rows, a
     // block a row
     return p.total_tokens * p.num_q_heads <= 4096 ? launch_join_split<D, Cut, kJoinWarps>(p, stream) : launch_join_split<D, Cut, 1>(p, stream);
+}
+
+// Short sequences are not cut: one CTA walks a segment of up to kWholeTiles key tiles in less time than the join takes.  Goes
+// by the caller's bound; a longer sequence is only slower.  Returns the grid (and sets whole_blocks), or 0.
+template <class Cut>
+inline int64_t whole_grid(Params& p, int32_t max_cached) {
+    const int64_t tiles = (static_cast<int64_t>(max_cached) + Cut::kTile - 1) / Cut::kTile + (p.max_tree + Cut::kTile - 1) / Cut::kTile;
+    const int32_t blocks = Cut::blocks(p, p.max_tree);
+    const int64_t grid = static_cast<int64_t>(p.batch) * p.num_kv_heads * blocks;
+    if (tiles > Cut::kWholeTiles || grid > INT32_MAX) return 0;
+    p.whole_blocks = blocks;
+    return grid;
 }
 
 // The pass's workspace: the pieces' rows.
