@@ -51,10 +51,10 @@ TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t b
     const int32_t group = d->num_q_heads / d->num_kv_heads;
     w.streams = d->dtype == RPX_BF16 && tree_streams(max_tree, group);
     if (w.streams) {
-        w.bytes = align_up(tree_stream_workspace(d->head_dim), kWsAlign);
+        w.bytes = align_up(tree_stream_workspace(batch, d->head_dim), kWsAlign);
         return w;
     }
-    const size_t own = d->dtype == RPX_F32 ? attn_workspace(d, tokens, true) : group > 128 ? 0 : tree_tile_workspace(d->head_dim, max_tree, group);
+    const size_t own = d->dtype == RPX_F32 ? attn_workspace(d, tokens, true) : group > 128 ? 0 : tree_tile_workspace(batch, d->head_dim, max_tree, group);
     w.sets_off = align_up(own, kWsAlign);
     w.values_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
     w.bytes = w.values_off;

@@ -141,9 +141,9 @@ struct TreeArgs {
     cudaStream_t stream;
 };
 bool tree_streams(int32_t max_tree, int32_t group);  // whether the streaming form takes trees of this size
-size_t tree_stream_workspace(int32_t head_dim);
+size_t tree_stream_workspace(int32_t batch, int32_t head_dim);
 rpx_status_t launch_tree_stream(const TreeArgs& a);  // bf16
-size_t tree_tile_workspace(int32_t head_dim, int32_t max_tree, int32_t group);
+size_t tree_tile_workspace(int32_t batch, int32_t head_dim, int32_t max_tree, int32_t group);
 // bf16; sets and values as launch_tree_sets leaves them, launched directly before on the same stream
 rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const void* values);
 int32_t tree_set_words(int32_t max_tree);            // 32-bit words of one ancestor set, a multiple of 4

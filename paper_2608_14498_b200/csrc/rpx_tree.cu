@@ -495,7 +495,7 @@ bool tree_streams(int32_t max_tree, int32_t group) {
     return max_tree <= kMaxNodes && (static_cast<int64_t>(max_tree) * group <= 32 || group > 128);
 }
 
-size_t tree_stream_workspace(int32_t head_dim) { return join_workspace<RowCut<64>>(kMaxCtas, head_dim); }
+size_t tree_stream_workspace(int32_t batch, int32_t head_dim) { return join_workspace<RowCut<64>>(batch, kMaxCtas, head_dim); }
 
 rpx_status_t launch_tree_stream(const TreeArgs& a) {
     return a.head_dim == 128 ? launch_stream_d<128>(a) : launch_stream_d<64>(a);

@@ -37,6 +37,7 @@ struct Params {
     float scale_log2;
     __nv_bfloat16* out;    // [tokens][H_q][D]
     float* lse;            // nullable
+    int64_t* seq_unit0;    // workspace [batch + 1]: number of the sequence's first unit; the last entry is the total
     float2* part_ml;       // workspace [ctas][2][rows per block]; a negative sum marks a node that is not in use
     float* part_o;         // workspace [ctas][2][rows per block][D]
     int32_t* status;
@@ -161,8 +162,8 @@ struct Start {
     int32_t units;     // how many
 };
 
-// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also
-// reports bad offsets.
+// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also leaves every sequence's first unit in
+// the workspace and reports bad offsets.
 template <class Cut, int kWarps>
 __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32_t* data_error) {
     constexpr int kThreads = 32 * kWarps;
@@ -211,11 +212,13 @@ __device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32
                 start->seq = s;
                 start->off = static_cast<int32_t>(begin - before);
             }
+            if (blockIdx.x == 0) p.seq_unit0[s] = before;
         }
         carry += all;
     }
     if (threadIdx.x == 0) {
         start->units = static_cast<int32_t>(end - begin);
+        if (blockIdx.x == 0) p.seq_unit0[p.batch] = total;
     }
     __syncthreads();
 }
@@ -261,63 +264,40 @@ struct Walk {
     }
 };
 
-// Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  kSplit == 1: a warp takes the rows
-// of one token and KV head, kJoinRows at a time.  Otherwise, for few rows: the eight warps of a block take one row, each every
-// eighth piece.  The kernel is launched on top of the attention kernel: what the lengths alone tell it works out before it waits, and after
-// that one round of loads is left.
+// Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  A warp takes kJoinRows rows (node,
+// query head) of a sequence side by side, or, where a handful of rows has dozens of pieces, the eight warps of a block one row,
+// each every eighth piece.  Launched on top of the attention kernel: the lengths are read before the wait for it.
 constexpr int kJoinWarps = 8;
 
-template <int D, class Cut, int kSplit>
-__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params p) {
-    constexpr int kCols = D / 32, kJoinRows = kSplit > 1 ? 1 : 4;  // rows whose loads are in flight together
+template <int D, class Cut, int kSplit, int kJoinRows>
+__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params p, int32_t chunks) {
+    constexpr int kCols = D / 32;
     __shared__ float part_acc[kSplit > 1 ? kJoinWarps : 1][kJoinRows][D];
     __shared__ float2 part_row[kSplit > 1 ? kJoinWarps : 1][kJoinRows];  // (maximum, sum); a negative sum: not in use
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % kSplit;
-    const int64_t task = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / kSplit) + warp / kSplit;
-    const int32_t tasks = kSplit > 1 ? p.num_q_heads : p.num_kv_heads;  // of a token
-    const int64_t token = task / tasks;
-    const int32_t head = static_cast<int32_t>(task - token * tasks), kv_head = kSplit > 1 ? head / p.group : head;
-    const int32_t h_begin = kSplit > 1 ? head - kv_head * p.group : 0, h_end = kSplit > 1 ? h_begin + 1 : p.group;
-    // ---- the token's sequence (the last that starts at or before it), the units in front of it and in all
-    int32_t s = 0;
-    for (int32_t hi = p.batch - 1; s < hi;) {
-        const int32_t mid = (s + hi + 1) >> 1;
-        if (__ldg(p.cu + mid) <= token) s = mid;
-        else hi = mid - 1;
-    }
-    int64_t before = 0, total = 0;
-    for (int32_t i = lane; i < p.batch; i += 32) {
-        const int64_t w = read_seq<Cut>(p, i, nullptr).work(p);
-        total += w;
-        if (i < s) before += w;
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        total += __shfl_xor_sync(0xffffffffu, total, off);
-        before += __shfl_xor_sync(0xffffffffu, before, off);
-    }
+    const int32_t s = blockIdx.x / chunks;
     const Seq q = read_seq<Cut>(p, s, nullptr);
-    const int32_t node = static_cast<int32_t>(token - q.tok0);
-    const bool inside = token < p.total_tokens && token >= q.tok0 && node < q.n;
-    const int64_t size = piece_units<Cut>(total, p.ctas);
-    before += kv_head * q.head_work();
-    for (int32_t h0 = h_begin; h0 < h_end; h0 += kJoinRows) {
+    const int32_t row_begin = ((blockIdx.x - s * chunks) * (kJoinWarps / kSplit) + warp / kSplit) * kJoinRows, rows = q.n * p.num_q_heads;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (row_begin >= rows && kSplit == 1) return;
+    const int64_t size = piece_units<Cut>(p.seq_unit0[p.batch], p.ctas), seq0 = p.seq_unit0[s];
+    {
         int32_t c0[kJoinRows], n[kJoinRows], row[kJoinRows], most = 0;  // first piece, pieces (0: nothing to do), place in a slot
 #pragma unroll
         for (int k = 0; k < kJoinRows; ++k) {
             c0[k] = n[k] = row[k] = 0;
-            if (inside && h0 + k < h_end) {
+            if (row_begin + k < rows) {
+                const int32_t node = (row_begin + k) / p.num_q_heads, head = row_begin + k - node * p.num_q_heads, kv_head = head / p.group;
                 int32_t block;
-                Cut::place(p, node, h0 + k, &block, &row[k]);
-                const int64_t unit0 = before + static_cast<int64_t>(block) * q.tiles * q.weight;
+                Cut::place(p, node, head - kv_head * p.group, &block, &row[k]);
+                const int64_t unit0 = seq0 + kv_head * q.head_work() + static_cast<int64_t>(block) * q.tiles * q.weight;
                 c0[k] = piece_of(unit0, size);
                 n[k] = piece_of(unit0 + static_cast<int64_t>(q.tiles - 1) * q.block_weight(block), size) - c0[k] + 1;
                 if (n[k] == 1) n[k] = 0;  // written whole
                 most = max(most, n[k]);
             }
         }
-        if (h0 == h_begin) asm volatile("griddepcontrol.wait;" ::: "memory");
-        if (kSplit == 1 && most == 0) continue;
+        if (kSplit == 1 && most == 0) return;
         float top[kJoinRows], sum[kJoinRows], acc[kJoinRows][kCols];
         bool unused[kJoinRows];
 #pragma unroll
@@ -396,7 +376,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params
         for (int k = 0; k < kJoinRows; ++k) {
             if (n[k] == 0 || (kSplit > 1 && warp != 0)) continue;
             const float inv = unused[k] ? 0.f : 1.f / sum[k];
-            const int64_t out_row = token * p.num_q_heads + kv_head * p.group + h0 + k;
+            const int64_t out_row = static_cast<int64_t>(q.tok0) * p.num_q_heads + row_begin + k;
             uint32_t w[kCols / 2];
 #pragma unroll
             for (int e = 0; e < kCols / 2; ++e) w[e] = unused[k] ? 0u : pack_bf16x2(acc[k][2 * e] * inv, acc[k][2 * e + 1] * inv);
@@ -424,17 +404,36 @@ rpx_status_t launch_on_top(Kernel* kernel, unsigned grid, unsigned threads, size
     return cudaLaunchKernelEx(&config, kernel, args...) == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
 }
 
-template <int D, class Cut, int kSplit>
+template <int D, class Cut, int kSplit, int kJoinRows>
 rpx_status_t launch_join_split(const Params& p, cudaStream_t stream) {
-    const int64_t grid = (p.total_tokens * (kSplit > 1 ? p.num_q_heads : p.num_kv_heads) * kSplit + kJoinWarps - 1) / kJoinWarps;
-    if (grid > INT32_MAX) return RPX_ERR_SHAPE;
-    return launch_on_top(tree_join_kernel<D, Cut, kSplit>, static_cast<unsigned>(grid), kJoinWarps * 32, 0, stream, p);
+    constexpr int per_block = kJoinWarps / kSplit * kJoinRows;
+    const int64_t chunks = (static_cast<int64_t>(p.max_tree) * p.num_q_heads + per_block - 1) / per_block;
+    if (chunks * p.batch > INT32_MAX) return RPX_ERR_SHAPE;
+    return launch_on_top(tree_join_kernel<D, Cut, kSplit, kJoinRows>, static_cast<unsigned>(chunks * p.batch), kJoinWarps * 32, 0, stream, p,
+                         static_cast<int32_t>(chunks));
 }
 template <int D, class Cut>
 rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
-    // one warp a row group needs some thousands of them to be quick (and not every row may have been cut): up to 4096 rows, a
-    // block a row
-    return p.total_tokens * p.num_q_heads <= 4096 ? launch_join_split<D, Cut, kJoinWarps>(p, stream) : launch_join_split<D, Cut, 1>(p, stream);
+    // more than 8 pieces per segment: a block a row; more rows than the SMs hold warps: four rows a warp
+    const int64_t segments = static_cast<int64_t>(p.batch) * p.num_kv_heads * Cut::blocks(p, p.max_tree);
+    if (p.ctas > 8 * segments) return launch_join_split<D, Cut, kJoinWarps, 1>(p, stream);
+    return p.total_tokens * p.num_q_heads > 6144 ? launch_join_split<D, Cut, 1, 4>(p, stream) : launch_join_split<D, Cut, 1, 1>(p, stream);
+}
+
+// The pass's workspace: sequences' first units, then the pieces' rows.
+template <class Cut>
+inline size_t join_workspace(int32_t batch, int32_t ctas, int32_t head_dim) {
+    const size_t rows = static_cast<size_t>(ctas) * 2 * Cut::kRows;
+    return align_up(static_cast<size_t>(batch + 1) * sizeof(int64_t), 256) + align_up(rows * sizeof(float2), 256) + rows * head_dim * sizeof(float);
+}
+template <class Cut>
+inline void carve_workspace(Params& p, void* workspace) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.seq_unit0 = reinterpret_cast<int64_t*>(ws);
+    ws += align_up(static_cast<size_t>(p.batch + 1) * sizeof(int64_t), 256);
+    p.part_ml = reinterpret_cast<float2*>(ws);
+    ws += align_up(static_cast<size_t>(p.ctas) * 2 * Cut::kRows * sizeof(float2), 256);
+    p.part_o = reinterpret_cast<float*>(ws);
 }
 
 // Short sequences are not cut: one CTA walks a segment of up to kWholeTiles key tiles in less time than the join takes.  Goes
@@ -447,20 +446,6 @@ inline int64_t whole_grid(Params& p, int32_t max_cached) {
     if (tiles > Cut::kWholeTiles || grid > INT32_MAX) return 0;
     p.whole_blocks = blocks;
     return grid;
-}
-
-// The pass's workspace: the pieces' rows.
-template <class Cut>
-inline size_t join_workspace(int32_t ctas, int32_t head_dim) {
-    const size_t rows = static_cast<size_t>(ctas) * 2 * Cut::kRows;
-    return align_up(rows * sizeof(float2), 256) + rows * head_dim * sizeof(float);
-}
-template <class Cut>
-inline void carve_workspace(Params& p, void* workspace) {
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    p.part_ml = reinterpret_cast<float2*>(ws);
-    ws += align_up(static_cast<size_t>(p.ctas) * 2 * Cut::kRows * sizeof(float2), 256);
-    p.part_o = reinterpret_cast<float*>(ws);
 }
 
 inline Params make_params(const TreeArgs& a) {

@@ -658,8 +658,8 @@ bool paired(int32_t max_tree, int32_t group) { return max_tree > 128 / group; }
 
 }  // namespace
 
-size_t tree_tile_workspace(int32_t head_dim, int32_t max_tree, int32_t group) {
-    return paired(max_tree, group) ? join_workspace<NodeCut<2>>(kMaxCtas, head_dim) : join_workspace<NodeCut<1>>(kMaxCtas, head_dim);
+size_t tree_tile_workspace(int32_t batch, int32_t head_dim, int32_t max_tree, int32_t group) {
+    return paired(max_tree, group) ? join_workspace<NodeCut<2>>(batch, kMaxCtas, head_dim) : join_workspace<NodeCut<1>>(batch, kMaxCtas, head_dim);
 }
 
 rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const void* values) {
