@@ -270,7 +270,7 @@ struct Walk {
 constexpr int kJoinWarps = 8;
 
 template <int D, class Cut, int kSplit, int kJoinRows>
-__global__ void __launch_bounds__(kJoinWarps * 32) tree_join_kernel(const Params p, int32_t chunks) {
+__global__ void __launch_bounds__(kJoinWarps * 32, kSplit > 1 ? 2 : 4) tree_join_kernel(const Params p, int32_t chunks) {
     constexpr int kCols = D / 32;
     __shared__ float part_acc[kSplit > 1 ? kJoinWarps : 1][kJoinRows][D];
     __shared__ float2 part_row[kSplit > 1 ? kJoinWarps : 1][kJoinRows];  // (maximum, sum); a negative sum: not in use
@@ -414,10 +414,10 @@ rpx_status_t launch_join_split(const Params& p, cudaStream_t stream) {
 }
 template <int D, class Cut>
 rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
-    // more than 8 pieces per segment: a block a row; more rows than the SMs hold warps: four rows a warp
+    // more than 8 pieces per segment: a block a row; more rows than the SMs hold warps: two rows a warp
     const int64_t segments = static_cast<int64_t>(p.batch) * p.num_kv_heads * Cut::blocks(p, p.max_tree);
     if (p.ctas > 8 * segments) return launch_join_split<D, Cut, kJoinWarps, 1>(p, stream);
-    return p.total_tokens * p.num_q_heads > 6144 ? launch_join_split<D, Cut, 1, 4>(p, stream) : launch_join_split<D, Cut, 1, 1>(p, stream);
+    return p.total_tokens * p.num_q_heads > 6144 ? launch_join_split<D, Cut, 1, 2>(p, stream) : launch_join_split<D, Cut, 1, 1>(p, stream);
 }
 
 // The pass's workspace: sequences' first units, then the pieces' rows.
