@@ -31,7 +31,6 @@ constexpr int kMaskWords = kMaxNodes / 32;
 
 struct Ctl {
     uint64_t full[kStages], empty[kStages];
-    Start start;
     uint32_t issued;  // tiles the producer has asked for
     uint32_t abort_flag, drain_flag, data_error;
     float2 ml[kWarps][16];
@@ -82,9 +81,7 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         fence_barrier_init();
     }
     __syncthreads();
-
-    find_piece<Cut, kWarps + 1>(p, &ctl->start, &ctl->data_error);
-    Walk<Cut> walk(p, &ctl->start);
+    Walk<Cut> walk(p, find_piece<Cut>(p, &ctl->data_error));
     uint32_t it = 0;  // tiles this warp has been through (ring position)
     bool ok = true;
 
@@ -441,25 +438,44 @@ tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ par
                  int32_t max_tree, int32_t words, uint32_t* sets, const __nv_bfloat16* v, int64_t v_stride, int32_t v_chunks,
                  __nv_bfloat16* v_copy, int32_t* status) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the attention kernel may start on its cached tiles
+    // Parents of the sequence that the block's first token is in: the walk is a chain of dependent reads (192 nodes in
+    // steps of three: 10 us from global memory, which kept the attention kernel off the SMs).
+    __shared__ int32_t staged[RPX_TREE_MAX_NODES];
     const int lane = threadIdx.x & 31;
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * kSetWarps + (threadIdx.x >> 5);
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kSetWarps, token = first + (threadIdx.x >> 5);
+    auto sequence_of = [&](int64_t t) {  // the last that starts at or before the token
+        int32_t lo = 0, hi = batch - 1;
+        while (lo < hi) {
+            const int32_t mid = (lo + hi + 1) >> 1;
+            if (__ldg(cu + mid) <= t) lo = mid;
+            else hi = mid - 1;
+        }
+        return lo;
+    };
+    auto inside_of = [&](int64_t t, int32_t begin, int64_t n) {
+        return begin >= 0 && begin <= t && t < begin + n && begin + n <= total_tokens && n <= max_tree;
+    };
+    const int32_t s0 = sequence_of(first), begin0 = __ldg(cu + s0);
+    const int64_t n0 = static_cast<int64_t>(__ldg(cu + s0 + 1)) - begin0;
+    if (inside_of(first, begin0, n0))
+        for (int32_t i = threadIdx.x; i < n0; i += kSetWarps * 32) staged[i] = __ldg(parents + begin0 + i);
+    __syncthreads();
     if (token >= total_tokens) return;
-    int32_t lo = 0, hi = batch;  // the last sequence that starts at or before the token
-    while (lo < hi) {
-        const int32_t mid = (lo + hi + 1) >> 1;
-        if (mid < batch && __ldg(cu + mid) <= token) lo = mid;
-        else hi = mid - 1;
+    int32_t tok0 = begin0;
+    int64_t n = n0;
+    if (token >= begin0 + n0) {
+        const int32_t s = sequence_of(token);
+        tok0 = __ldg(cu + s);
+        n = static_cast<int64_t>(__ldg(cu + s + 1)) - tok0;
     }
-    const int32_t tok0 = __ldg(cu + lo);
-    const int64_t n = static_cast<int64_t>(__ldg(cu + lo + 1)) - tok0;
-    const bool inside = tok0 >= 0 && tok0 <= token && token < tok0 + n && tok0 + n <= total_tokens && n <= max_tree;
+    const bool inside = inside_of(token, tok0, n), is_staged = tok0 == begin0 && n == n0 && inside_of(first, begin0, n0);
     uint32_t bits = 0u;
     bool good = true, used = inside;
     int32_t at = inside ? static_cast<int32_t>(token - tok0) : -1;
     const int32_t self = at;
     while (at >= 0) {
         if ((at >> 5) == lane) bits |= 1u << (at & 31);
-        const int32_t up = __ldg(parents + tok0 + at);
+        const int32_t up = is_staged ? staged[at] : __ldg(parents + tok0 + at);
         if (up < -1 && at == self) used = false;
         else if (up < -1 || up >= at) good = false;
         if (up >= at) break;

@@ -136,91 +136,62 @@ __device__ __forceinline__ int64_t warp_scan(int64_t x, int lane) {  // inclusiv
     }
     return x;
 }
-// Inclusive sum over the CTA's kWarps warps; `all` receives the total.
-template <int kWarps>
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* warp_sum, int64_t* all) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    x = warp_scan(x, lane);
-    __syncthreads();
-    if (lane == 31) warp_sum[warp] = x;
-    __syncthreads();
-    int64_t before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        const int64_t v = warp_sum[w];
-        if (w < warp) before += v;
-        total += v;
-    }
-    *all = total;
-    return x + before;
-}
-
-// Where a CTA's piece starts (in shared memory).
-struct Start {
-    int64_t warp_sum[16];
-    int32_t seq, off;  // its first unit: sequence, and unit within that sequence's work
-    int32_t units;     // how many
+// A piece: its first unit (sequence, and unit within that sequence's work) and how many units it has.
+struct Piece {
+    int32_t seq, off, units;
 };
 
-// Finds this CTA's piece; called by all its threads, ends with a barrier.  CTA 0 also leaves every sequence's first unit in
-// the workspace and reports bad offsets.
-template <class Cut, int kWarps>
-__device__ __forceinline__ void find_piece(const Params& p, Start* start, uint32_t* data_error) {
-    constexpr int kThreads = 32 * kWarps;
+// Finds this CTA's piece; every warp of it works it out by itself (32 sequences a step), so nothing is waited for.  CTA 0's
+// first warp also leaves every sequence's first unit in the workspace, and reports bad offsets.
+template <class Cut>
+__device__ __forceinline__ Piece find_piece(const Params& p, uint32_t* data_error) {
+    const int lane = threadIdx.x & 31;
+    const bool scribe = blockIdx.x == 0 && threadIdx.x < 32;
+    Piece piece = {p.batch, 0, 0};
     if (p.whole_blocks > 0) {
-        if (threadIdx.x == 0) {
-            const int32_t per_seq = p.num_kv_heads * p.whole_blocks, s = blockIdx.x / per_seq, i = blockIdx.x - s * per_seq;
-            const int32_t head = i / p.whole_blocks, block = i - head * p.whole_blocks;
-            const Seq q = read_seq<Cut>(p, s, i == 0 ? data_error : nullptr);
-            const bool there = q.n > 0 && block < q.blocks;
-            start->seq = s;
-            start->off = there ? static_cast<int32_t>(head * q.head_work()) + block * q.tiles * q.weight : 0;
-            start->units = there ? q.tiles * q.block_weight(block) : 0;
+        const int32_t per_seq = p.num_kv_heads * p.whole_blocks, s = blockIdx.x / per_seq, i = blockIdx.x - s * per_seq;
+        const int32_t head = i / p.whole_blocks, block = i - head * p.whole_blocks;
+        const Seq q = read_seq<Cut>(p, s, i == 0 ? data_error : nullptr);
+        if (q.n > 0 && block < q.blocks) {
+            piece.seq = s;
+            piece.off = static_cast<int32_t>(head * q.head_work()) + block * q.tiles * q.weight;
+            piece.units = q.tiles * q.block_weight(block);
         }
-        __syncthreads();
-        return;
+        return piece;
     }
-    uint32_t* report = blockIdx.x == 0 ? data_error : nullptr;
-    if (threadIdx.x == 0) {
-        start->seq = p.batch;
-        start->off = 0;
-    }
-    int64_t total = 0, all = 0, first_work = 0, first_sum = 0;
-    for (int32_t base = 0; base < p.batch; base += kThreads) {
-        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
-        const int64_t w = s < p.batch ? read_seq<Cut>(p, s, report).work(p) : 0;
-        const int64_t sum = block_scan<kWarps>(w, start->warp_sum, &all);
+    int64_t total = 0, first_work = 0, first_sum = 0;
+    for (int32_t base = 0; base < p.batch; base += 32) {
+        const int64_t w = base + lane < p.batch ? read_seq<Cut>(p, base + lane, scribe ? data_error : nullptr).work(p) : 0;
+        const int64_t sum = total + warp_scan(w, lane);
         if (base == 0) {
             first_work = w;
             first_sum = sum;
         }
-        total += all;
+        total = __shfl_sync(0xffffffffu, sum, 31);
     }
     const int64_t size = piece_units<Cut>(total, p.ctas);
     const int64_t begin = min(total, size * static_cast<int64_t>(blockIdx.x)), end = min(total, begin + size);
     int64_t carry = 0;
-    for (int32_t base = 0; base < p.batch; base += kThreads) {
-        const int32_t s = base + static_cast<int32_t>(threadIdx.x);
+    for (int32_t base = 0; base < p.batch; base += 32) {
         int64_t w = first_work, sum = first_sum;
-        if (p.batch > kThreads) {
-            w = s < p.batch ? read_seq<Cut>(p, s, nullptr).work(p) : 0;
-            sum = block_scan<kWarps>(w, start->warp_sum, &all);
+        if (base > 0) {
+            w = base + lane < p.batch ? read_seq<Cut>(p, base + lane, nullptr).work(p) : 0;
+            sum = carry + warp_scan(w, lane);
         }
-        const int64_t before = carry + sum - w;
-        if (s < p.batch) {
-            if (begin < end && begin >= before && begin < before + w) {
-                start->seq = s;
-                start->off = static_cast<int32_t>(begin - before);
-            }
-            if (blockIdx.x == 0) p.seq_unit0[s] = before;
+        const int64_t before = sum - w;
+        const uint32_t found = __ballot_sync(0xffffffffu, begin < end && begin >= before && begin < sum);
+        if (found != 0u) {
+            const int src = __ffs(static_cast<int>(found)) - 1;
+            piece.seq = base + src;
+            piece.off = static_cast<int32_t>(begin - __shfl_sync(0xffffffffu, before, src));
+            piece.units = static_cast<int32_t>(end - begin);
+            if (!scribe) break;
         }
-        carry += all;
+        if (scribe && base + lane < p.batch) p.seq_unit0[base + lane] = before;
+        carry = __shfl_sync(0xffffffffu, sum, 31);
     }
-    if (threadIdx.x == 0) {
-        start->units = static_cast<int32_t>(end - begin);
-        if (blockIdx.x == 0) p.seq_unit0[p.batch] = total;
-    }
-    __syncthreads();
+    if (scribe && lane == 0) p.seq_unit0[p.batch] = total;
+    return piece;
 }
 
 // Walks the pieces of segments inside this CTA's part of the line; every warp walks it alike.
@@ -229,12 +200,12 @@ struct Walk {
     int32_t s, head, block, t0, t1;  // current segment: sequence, KV head, row block, key tiles [t0, t1)
     int32_t left;                    // units of the piece behind t1
     Seq q;
-    __device__ __forceinline__ Walk(const Params& p, const Start* start) : s(start->seq), head(0), block(0), t0(0), t1(0), left(start->units), q() {
+    __device__ __forceinline__ Walk(const Params& p, const Piece& piece) : s(piece.seq), head(0), block(0), t0(0), t1(0), left(piece.units), q() {
         if (left == 0) return;
         q = read_seq<Cut>(p, s, nullptr);
         const int32_t per_head = static_cast<int32_t>(q.head_work()), per_block = q.tiles * q.weight;
-        head = start->off / per_head;
-        int32_t off = start->off - head * per_head;
+        head = piece.off / per_head;
+        int32_t off = piece.off - head * per_head;
         block = min(off / per_block, q.blocks - 1);
         off -= block * per_block;
         const int32_t w = q.block_weight(block);
@@ -266,7 +237,7 @@ struct Walk {
 
 // Adds up the pieces of every row whose segment was cut, in an order that the lengths fix.  A warp takes kJoinRows rows (node,
 // query head) of a sequence side by side, or, where a handful of rows has dozens of pieces, the eight warps of a block one row,
-// each every eighth piece.  Launched on top of the attention kernel: the lengths are read before the wait for it.
+// each every eighth piece.  Launched on top of the attention kernel.
 constexpr int kJoinWarps = 8;
 
 template <int D, class Cut, int kSplit, int kJoinRows>
@@ -276,11 +247,12 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kSplit > 1 ? 2 : 4) tree_join
     __shared__ float2 part_row[kSplit > 1 ? kJoinWarps : 1][kJoinRows];  // (maximum, sum); a negative sum: not in use
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % kSplit;
     const int32_t s = blockIdx.x / chunks;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t total = p.seq_unit0[p.batch], seq0 = p.seq_unit0[s];  // (in flight together with the lengths)
     const Seq q = read_seq<Cut>(p, s, nullptr);
     const int32_t row_begin = ((blockIdx.x - s * chunks) * (kJoinWarps / kSplit) + warp / kSplit) * kJoinRows, rows = q.n * p.num_q_heads;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (row_begin >= rows && kSplit == 1) return;
-    const int64_t size = piece_units<Cut>(p.seq_unit0[p.batch], p.ctas), seq0 = p.seq_unit0[s];
+    const int64_t size = piece_units<Cut>(total, p.ctas);
     {
         int32_t c0[kJoinRows], n[kJoinRows], row[kJoinRows], most = 0;  // first piece, pieces (0: nothing to do), place in a slot
 #pragma unroll

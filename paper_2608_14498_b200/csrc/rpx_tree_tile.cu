@@ -58,7 +58,6 @@ struct Ctl {
     uint64_t o_free[2];   // softmax -> tensor core: O_t has been read
     uint64_t ml_ready;    // both buffers' maxima and sums are in `ml`
     uint64_t drain;
-    Start start;
     uint32_t tmem_base, abort_flag, drain_flag, data_error;
     float2 ml[2][kTile];
 };
@@ -113,12 +112,11 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         tmem_alloc(&ctl->tmem_base, kTmemCols);
         tmem_relinquish();
     }
-    find_piece<Cut, 12>(p, &ctl->start, &ctl->data_error);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = ctl->tmem_base;  // S_t at columns 128 t, O_t at 256 + 128 t
-    Walk<Cut> walk(p, &ctl->start);
+    Walk<Cut> walk(p, find_piece<Cut>(p, &ctl->data_error));
     // Every role walks the piece's segments alike.  A block whose nodes fit one query tile lets the buffers take turns.
     auto nodes_in_block = [&]() { return min(walk.q.n - walk.block * L::kQTiles * p.tile_nodes, L::kQTiles * p.tile_nodes); };
 
