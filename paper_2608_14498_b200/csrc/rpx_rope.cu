@@ -108,7 +108,7 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// What a lane keeps for a whole token: where its two chunks lie in a row and the angles of its eight pairs.
+// Where a lane's two chunks lie in a row.
 template <int D>
 struct LaneMap {
     static constexpr int kLanes = D / 16;      // lanes per row
@@ -122,205 +122,247 @@ struct LaneMap {
         off_a = 8 * (turned ? c : 2 * n + 2 * (c - n));
         off_b = turned ? off_a + rot / 2 : off_a + 8;
     }
-    __device__ __forceinline__ void angles(const float2* cs, float (&c)[8], float (&s)[8]) const {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            c[i] = 1.f;
-            s[i] = 0.f;
-        }
-        if (turned) {
-            const float4* v = reinterpret_cast<const float4*>(cs + off_a);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 w = v[i];
-                c[2 * i] = w.x; s[2 * i] = w.y; c[2 * i + 1] = w.z; s[2 * i + 1] = w.w;
-            }
-        }
-    }
 };
 
+// Eight consecutive (cos, sin) pairs, or eight floats, out of shared memory.
+__device__ __forceinline__ void read_angles(const float2* cs, float (&c)[8], float (&s)[8]) {
+    const float4* v = reinterpret_cast<const float4*>(cs);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 w = v[i];
+        c[2 * i] = w.x; s[2 * i] = w.y; c[2 * i + 1] = w.z; s[2 * i + 1] = w.w;
+    }
+}
+__device__ __forceinline__ void read8(const float* p, float (&x)[8]) {
+    const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+    x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+}
+
+// The weights as float32 in shared memory; called by the whole block, ends with a barrier.
+template <class T, int D>
+__device__ __forceinline__ void stage_weights(const Params& p, float (*w)[D]) {
+    for (int i = threadIdx.x; i < 2 * D / 8; i += kWarps * 32) {
+        float x[8];
+        T::unpack(T::load(static_cast<const typename T::Elem*>(i < D / 8 ? p.q_weight : p.k_weight) + (i % (D / 8)) * 8), x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[i / (D / 8)][(i % (D / 8)) * 8 + e] = x[e];
+    }
+    __syncthreads();
+}
+
+// The loads run a batch ahead of the arithmetic, the first batch in front of the angles: a warp always has rows in flight.
 template <class T, int D, bool kNorm>
-__global__ void __launch_bounds__(kWarps * 32) qk_rope_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3 : 2) qk_rope_kernel(const __grid_constant__ Params p) {
     typedef LaneMap<D> Map;
     typedef typename T::Elem Elem;
-    constexpr int kUnroll = sizeof(Elem) == 2 ? 4 : 2;  // units whose loads are in flight together
+    constexpr int kUnroll = sizeof(Elem) == 2 ? 2 : 1;  // units of a batch
     __shared__ __align__(16) float2 cs_all[kWarps][kMaxPairs];
+    __shared__ __align__(16) float weight[kNorm ? 2 : 1][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
     const int64_t token = task / p.warps_per_token;
-    if (token >= p.n_tokens) return;
     const int32_t u_begin = static_cast<int32_t>(task - token * p.warps_per_token) * p.units_per_warp;
-    const int32_t u_end = min(p.units, u_begin + p.units_per_warp);
+    const int32_t u_end = token < p.n_tokens ? min(p.units, u_begin + p.units_per_warp) : 0;
     const Map map(lane, p.rot);
-    float c[8], s[8];
-    token_angles(p, token, lane, cs_all[warp]);
-    map.angles(cs_all[warp], c, s);
+    const Elem* const q = static_cast<const Elem*>(p.q) + token * p.q_stride;
+    const Elem* const k = static_cast<const Elem*>(p.k) + token * p.k_stride;
 
-    auto run = [&](const Elem* src, Elem* dst, const Elem* weight, int32_t heads, int32_t u0, int32_t u1) {
-        if (u0 >= u1) return;
-        float wa[8], wb[8];
-        if (kNorm) {
-            T::unpack(T::load(weight + map.off_a), wa);
-            T::unpack(T::load(weight + map.off_b), wb);
-        }
-        for (int32_t u = u0; u < u1; u += kUnroll) {
-            typename T::Raw ra[kUnroll], rb[kUnroll];
+    typename T::Raw now[kUnroll][2], next[kUnroll][2];
+    auto load = [&](typename T::Raw (&raw)[kUnroll][2], int32_t u0) {
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                const int32_t head = (u + k) * Map::kRows + map.row;
-                const bool there = u + k < u1 && head < heads;
-                ra[k] = there ? T::load(src + head * D + map.off_a) : T::zero();
-                rb[k] = there ? T::load(src + head * D + map.off_b) : T::zero();
-            }
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                if (u + k >= u1) break;
-                const int32_t head = (u + k) * Map::kRows + map.row;
-                float a[8], b[8];
-                T::unpack(ra[k], a);
-                T::unpack(rb[k], b);
-                if (kNorm) {
-                    float ss = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-                    const float r = rsqrtf(row_sum<Map::kLanes>(ss) * (1.f / D) + p.eps);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        a[i] = a[i] * r * wa[i];
-                        b[i] = b[i] * r * wb[i];
-                    }
-                }
-                if (map.turned) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x = a[i], y = b[i];
-                        a[i] = fmaf(x, c[i], -y * s[i]);
-                        b[i] = fmaf(y, c[i], x * s[i]);
-                    }
-                }
-                if (head < heads) {
-                    T::store(dst + head * D + map.off_a, a);
-                    T::store(dst + head * D + map.off_b, b);
-                }
-            }
+        for (int i = 0; i < kUnroll; ++i) {
+            const bool is_q = u0 + i < p.units_q;
+            const int32_t head = (u0 + i - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
+            const Elem* src = (is_q ? q : k) + head * D;
+            const bool there = u0 + i < u_end && head < (is_q ? p.num_q_heads : p.num_kv_heads);
+            raw[i][0] = there ? T::load(src + map.off_a) : T::zero();
+            raw[i][1] = there ? T::load(src + map.off_b) : T::zero();
         }
     };
-    run(static_cast<const Elem*>(p.q) + token * p.q_stride, static_cast<Elem*>(p.q_out) + token * p.q_out_stride,
-        static_cast<const Elem*>(p.q_weight), p.num_q_heads, u_begin, min(u_end, p.units_q));
-    run(static_cast<const Elem*>(p.k) + token * p.k_stride, static_cast<Elem*>(p.k_out) + token * p.k_out_stride,
-        static_cast<const Elem*>(p.k_weight), p.num_kv_heads, max(u_begin, p.units_q) - p.units_q, u_end - p.units_q);
+    load(now, u_begin);
+    if (u_begin < u_end) token_angles(p, token, lane, cs_all[warp]);
+    if (kNorm) stage_weights<T, D>(p, weight);
+    if (u_begin >= u_end) return;
+    float c[8], s[8];
+    if (map.turned) read_angles(cs_all[warp] + map.off_a, c, s);
+
+    for (int32_t u0 = u_begin; u0 < u_end; u0 += kUnroll) {
+        load(next, u0 + kUnroll);
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) {
+            if (u0 + i >= u_end) break;
+            const bool is_q = u0 + i < p.units_q;
+            const int32_t head = (u0 + i - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
+            float a[8], b[8];
+            T::unpack(now[i][0], a);
+            T::unpack(now[i][1], b);
+            if (kNorm) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+                const float r = rsqrtf(row_sum<Map::kLanes>(ss) * (1.f / D) + p.eps);
+                float w[8];
+                read8(weight[is_q ? 0 : 1] + map.off_a, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = a[e] * r * w[e];
+                read8(weight[is_q ? 0 : 1] + map.off_b, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[e] = b[e] * r * w[e];
+            }
+            if (map.turned) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = a[e], y = b[e];
+                    a[e] = fmaf(x, c[e], -y * s[e]);
+                    b[e] = fmaf(y, c[e], x * s[e]);
+                }
+            }
+            if (head < (is_q ? p.num_q_heads : p.num_kv_heads)) {
+                Elem* dst = (is_q ? static_cast<Elem*>(p.q_out) + token * p.q_out_stride : static_cast<Elem*>(p.k_out) + token * p.k_out_stride) + head * D;
+                T::store(dst + map.off_a, a);
+                T::store(dst + map.off_b, b);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kUnroll; ++i) {
+            now[i][0] = next[i][0];
+            now[i][1] = next[i][1];
+        }
+    }
 }
 
-// Backward.  The warps stride over (token, part) tasks and keep their sums of the weight gradient in registers; a CTA
-// leaves one partial row per tensor, which dw_reduce_kernel adds up in a fixed order: the same result from run to run.
+// Backward.  The warps stride over (token, part) tasks.  Their sums of the weight gradient stay with them: those of q in
+// registers, those of k (a fraction of the rows) in shared memory, a lane's own 16 values each.  A CTA leaves one partial
+// row per tensor, which dw_reduce_kernel adds up in a fixed order: the same result from run to run.
 template <class T, int D, bool kNorm>
-__global__ void __launch_bounds__(kWarps * 32) qk_rope_bwd_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kWarps * 32, 2) qk_rope_bwd_kernel(const __grid_constant__ Params p) {
     typedef LaneMap<D> Map;
     typedef typename T::Elem Elem;
-    constexpr int kUnroll = 2;
     __shared__ __align__(16) float2 cs_all[kWarps][kMaxPairs];
-    __shared__ float dw_all[kNorm ? kWarps : 1][2][D];
+    __shared__ __align__(16) float weight[kNorm ? 2 : 1][D];
+    __shared__ float4 dwk_all[kNorm ? kWarps : 1][4][32];  // [warp][quarter of the lane's 16 values][lane]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Map map(lane, p.rot);
     const int64_t n_tasks = p.n_tokens * p.warps_per_token;
-    float dwa[2][8], dwb[2][8];
+    float dwq[2][8];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < 8; ++i) dwq[0][i] = dwq[1][i] = 0.f;
+    if (kNorm) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dwa[t][i] = dwb[t][i] = 0.f;
-
+        for (int i = 0; i < 4; ++i) dwk_all[warp][i][lane] = make_float4(0.f, 0.f, 0.f, 0.f);
+        stage_weights<T, D>(p, weight);
+    }
     for (int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp; task < n_tasks;
          task += static_cast<int64_t>(gridDim.x) * kWarps) {
         const int64_t token = task / p.warps_per_token;
         const int32_t u_begin = static_cast<int32_t>(task - token * p.warps_per_token) * p.units_per_warp;
         const int32_t u_end = min(p.units, u_begin + p.units_per_warp);
-        float c[8], s[8];
-        __syncwarp();  // the previous task's angles have been read
-        token_angles(p, token, lane, cs_all[warp]);
-        map.angles(cs_all[warp], c, s);
-
-        auto run = [&](const Elem* src, const float* grad, Elem* dst, const Elem* weight, int32_t heads, int32_t u0, int32_t u1,
-                       float (&da)[8], float (&db)[8]) {
-            if (u0 >= u1) return;
-            float wa[8], wb[8];
+        const Elem* const q = static_cast<const Elem*>(p.q) + token * p.q_stride;
+        const Elem* const k = static_cast<const Elem*>(p.k) + token * p.k_stride;
+        const float* const dq = p.dq + token * p.num_q_heads * D;
+        const float* const dk = p.dk + token * p.num_kv_heads * D;
+        struct Batch {
+            typename T::Raw x[2];
+            F32::Raw g[2];
+        } now, next;
+        auto load = [&](Batch& r, int32_t u) {
+            const bool is_q = u < p.units_q;
+            const int32_t head = (u - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
+            const bool there = u < u_end && head < (is_q ? p.num_q_heads : p.num_kv_heads);
+            const Elem* x = (is_q ? q : k) + head * D;
+            const float* g = (is_q ? dq : dk) + head * D;
+            r.g[0] = there ? F32::load(g + map.off_a) : F32::zero();
+            r.g[1] = there ? F32::load(g + map.off_b) : F32::zero();
             if (kNorm) {
-                T::unpack(T::load(weight + map.off_a), wa);
-                T::unpack(T::load(weight + map.off_b), wb);
-            }
-            for (int32_t u = u0; u < u1; u += kUnroll) {
-                typename T::Raw ra[kUnroll], rb[kUnroll];
-                F32::Raw ga[kUnroll], gb[kUnroll];
-#pragma unroll
-                for (int k = 0; k < kUnroll; ++k) {
-                    const int32_t head = (u + k) * Map::kRows + map.row;
-                    const bool there = u + k < u1 && head < heads;
-                    if (kNorm) {
-                        ra[k] = there ? T::load(src + head * D + map.off_a) : T::zero();
-                        rb[k] = there ? T::load(src + head * D + map.off_b) : T::zero();
-                    }
-                    ga[k] = there ? F32::load(grad + head * D + map.off_a) : F32::zero();
-                    gb[k] = there ? F32::load(grad + head * D + map.off_b) : F32::zero();
-                }
-#pragma unroll
-                for (int k = 0; k < kUnroll; ++k) {
-                    if (u + k >= u1) break;
-                    const int32_t head = (u + k) * Map::kRows + map.row;
-                    float g[8], h[8];
-                    F32::unpack(ga[k], g);
-                    F32::unpack(gb[k], h);
-                    if (map.turned) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float x = g[i], y = h[i];
-                            g[i] = fmaf(x, c[i], y * s[i]);
-                            h[i] = fmaf(y, c[i], -x * s[i]);
-                        }
-                    }
-                    if (kNorm) {
-                        float a[8], b[8];
-                        T::unpack(ra[k], a);
-                        T::unpack(rb[k], b);
-                        float ss = 0.f, dot = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-                            dot = fmaf(g[i] * wa[i], a[i], fmaf(h[i] * wb[i], b[i], dot));
-                        }
-                        ss = row_sum<Map::kLanes>(ss);
-                        dot = row_sum<Map::kLanes>(dot);
-                        // a row past the last head has zero gradient and adds nothing; its r is not used (eps may be 0)
-                        const float r = head < heads ? rsqrtf(ss * (1.f / D) + p.eps) : 0.f;
-                        const float m = dot * r * (1.f / D);  // mean(g w u)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float ua = a[i] * r, ub = b[i] * r;
-                            da[i] = fmaf(g[i], ua, da[i]);
-                            db[i] = fmaf(h[i], ub, db[i]);
-                            g[i] = r * fmaf(-ua, m, g[i] * wa[i]);
-                            h[i] = r * fmaf(-ub, m, h[i] * wb[i]);
-                        }
-                    }
-                    if (head < heads) {
-                        T::store(dst + head * D + map.off_a, g);
-                        T::store(dst + head * D + map.off_b, h);
-                    }
-                }
+                r.x[0] = there ? T::load(x + map.off_a) : T::zero();
+                r.x[1] = there ? T::load(x + map.off_b) : T::zero();
             }
         };
-        run(static_cast<const Elem*>(p.q) + token * p.q_stride, p.dq + token * p.num_q_heads * D,
-            static_cast<Elem*>(p.q_out) + token * p.q_out_stride, static_cast<const Elem*>(p.q_weight), p.num_q_heads, u_begin,
-            min(u_end, p.units_q), dwa[0], dwb[0]);
-        run(static_cast<const Elem*>(p.k) + token * p.k_stride, p.dk + token * p.num_kv_heads * D,
-            static_cast<Elem*>(p.k_out) + token * p.k_out_stride, static_cast<const Elem*>(p.k_weight), p.num_kv_heads,
-            max(u_begin, p.units_q) - p.units_q, u_end - p.units_q, dwa[1], dwb[1]);
+        load(now, u_begin);
+        __syncwarp();  // the previous task's angles have been read
+        token_angles(p, token, lane, cs_all[warp]);
+        for (int32_t u = u_begin; u < u_end; ++u) {
+            load(next, u + 1);
+            const bool is_q = u < p.units_q;
+            const int32_t head = (u - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
+            const bool there = head < (is_q ? p.num_q_heads : p.num_kv_heads);
+            float g[8], h[8];
+            F32::unpack(now.g[0], g);
+            F32::unpack(now.g[1], h);
+            if (map.turned) {
+                float c[8], s[8];
+                read_angles(cs_all[warp] + map.off_a, c, s);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = g[i], y = h[i];
+                    g[i] = fmaf(x, c[i], y * s[i]);
+                    h[i] = fmaf(y, c[i], -x * s[i]);
+                }
+            }
+            if (kNorm) {
+                float a[8], b[8], wa[8], wb[8];
+                T::unpack(now.x[0], a);
+                T::unpack(now.x[1], b);
+                read8(weight[is_q ? 0 : 1] + map.off_a, wa);
+                read8(weight[is_q ? 0 : 1] + map.off_b, wb);
+                float ss = 0.f, dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+                    dot = fmaf(g[i] * wa[i], a[i], fmaf(h[i] * wb[i], b[i], dot));
+                }
+                ss = row_sum<Map::kLanes>(ss);
+                dot = row_sum<Map::kLanes>(dot);
+                // a row past the last head has zero gradient and adds nothing; its r is not used (eps may be 0)
+                const float r = there ? rsqrtf(ss * (1.f / D) + p.eps) : 0.f;
+                const float m = dot * r * (1.f / D);  // mean(g w u)
+                float da[8], db[8];  // what this row adds to the weight's gradient
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float ua = a[i] * r, ub = b[i] * r;
+                    da[i] = g[i] * ua;
+                    db[i] = h[i] * ub;
+                    g[i] = r * fmaf(-ua, m, g[i] * wa[i]);
+                    h[i] = r * fmaf(-ub, m, h[i] * wb[i]);
+                }
+                if (is_q) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dwq[0][i] += da[i];
+                        dwq[1][i] += db[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float4 v = dwk_all[warp][i][lane];
+                        const float* d = i < 2 ? da + 4 * i : db + 4 * (i - 2);
+                        v.x += d[0];
+                        v.y += d[1];
+                        v.z += d[2];
+                        v.w += d[3];
+                        dwk_all[warp][i][lane] = v;
+                    }
+                }
+            }
+            if (there) {
+                Elem* dst = (is_q ? static_cast<Elem*>(p.q_out) + token * p.q_out_stride : static_cast<Elem*>(p.k_out) + token * p.k_out_stride) + head * D;
+                T::store(dst + map.off_a, g);
+                T::store(dst + map.off_b, h);
+            }
+            now = next;
+        }
     }
     if (kNorm && p.dw_partial != nullptr) {
+        __shared__ float dw_all[kNorm ? kWarps : 1][2][D];
         // over the rows of the warp, then over the warps of the CTA
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float x = dwa[t][i], y = dwb[t][i];
+                const float* own = reinterpret_cast<const float*>(&dwk_all[warp][0][lane]);
+                float x = t == 0 ? dwq[0][i] : own[(i / 4) * 128 + i % 4];
+                float y = t == 0 ? dwq[1][i] : own[(2 + i / 4) * 128 + i % 4];
 #pragma unroll
                 for (int off = Map::kLanes; off < 32; off <<= 1) {
                     x += __shfl_xor_sync(0xffffffffu, x, off);
