@@ -211,7 +211,7 @@ struct RopeArgs {
     void* workspace = nullptr;           // backward: one partial row per CTA
     cudaStream_t stream;
 };
-constexpr int kRopeBwdCtasPerSm = 2, kRopeBwdMaxCtas = 512;
+constexpr int kRopeBwdCtasPerSm = 4, kRopeBwdMaxCtas = 1024;
 size_t rope_backward_workspace(int32_t head_dim);
 rpx_status_t launch_qk_rope(const RopeArgs& a);
 rpx_status_t launch_qk_rope_backward(const RopeArgs& a);

@@ -464,6 +464,11 @@ __device__ __forceinline__ void poly_exp2_pair(uint64_t x, float& e0, float& e1)
 }
 
 // 32-byte global store (sm_100): `p` must be 32-byte aligned.
+__device__ __forceinline__ void ld_global_v8(const void* p, float (&r)[8]) {  // 32-byte aligned
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+                 : "l"(p) : "memory");
+}
 __device__ __forceinline__ void st_global_v8(void* p, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t a4,
                                              uint32_t a5, uint32_t a6, uint32_t a7) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a0), "r"(a1), "r"(a2), "r"(a3),

@@ -15,12 +15,13 @@
 #include <cuda_bf16.h>
 
 #include "rpx_internal.h"
+#include "rpx_ptx.cuh"
 
 namespace rpx {
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;
 constexpr int kMaxPairs = 64;
 
 struct Params {
@@ -35,6 +36,7 @@ struct Params {
     int32_t num_q_heads, num_kv_heads, rot;
     int32_t units_q, units, units_per_warp, warps_per_token;  // a unit = the rows one warp holds at once
     float eps;
+    bool wide;                        // every float32 tensor starts on 32 bytes
     const float *dq, *dk;             // backward: [tokens][heads][D] contiguous
     float* dw_partial;                // backward: [grid][2][D], or NULL
     uint8_t axis[kMaxPairs];
@@ -49,7 +51,7 @@ __device__ __forceinline__ void token_angles(const Params& p, int64_t token, int
         const float x = static_cast<float>(half_turns - 2.0 * rint(half_turns * 0.5));
         float s, c;
         sincospif(x, &s, &c);
-        cs[i] = make_float2(c, s);
+        cs[((i & 7) >> 1) * (kMaxPairs / 4) + (i >> 3) * 2 + (i & 1)] = make_float2(c, s);
     }
     __syncwarp();
 }
@@ -57,7 +59,7 @@ __device__ __forceinline__ void token_angles(const Params& p, int64_t token, int
 struct Bf16 {
     typedef __nv_bfloat16 Elem;
     typedef uint4 Raw;  // 8 elements
-    static __device__ __forceinline__ Raw load(const Elem* p) { return *reinterpret_cast<const uint4*>(p); }
+    static __device__ __forceinline__ Raw load(const Elem* p, bool) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
     static __device__ __forceinline__ Raw zero() { return make_uint4(0u, 0u, 0u, 0u); }
     static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -68,35 +70,46 @@ struct Bf16 {
         }
     }
     // the one rounding of the pass: results to bf16, nearest-even
-    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8]) {
+    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8], bool) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
             w[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
     }
 };
 
+// A lane's eight floats are one 32-byte access: as two of 16 bytes, every request of a warp would touch all of its sectors
+// by halves, and the L1's request rate would bound the backward pass (79 % busy at 215 us per 34816 tokens).
 struct F32 {
     typedef float Elem;
-    struct Raw { float4 a, b; };
-    static __device__ __forceinline__ Raw load(const Elem* p) {
-        const float4* v = reinterpret_cast<const float4*>(p);
-        return Raw{v[0], v[1]};
+    struct Raw { float v[8]; };
+    static __device__ __forceinline__ Raw load(const Elem* p, bool wide) {
+        Raw r;
+        if (wide) {
+            ld_global_v8(p, r.v);
+        } else {
+            const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+            r.v[0] = a.x; r.v[1] = a.y; r.v[2] = a.z; r.v[3] = a.w;
+            r.v[4] = b.x; r.v[5] = b.y; r.v[6] = b.z; r.v[7] = b.w;
+        }
+        return r;
     }
-    static __device__ __forceinline__ Raw zero() {
-        return Raw{make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    }
+    static __device__ __forceinline__ Raw zero() { return Raw{{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}}; }
     static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
-        x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
-        x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = r.v[i];
     }
-    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8]) {
-        float4* v = reinterpret_cast<float4*>(p);
-        v[0] = make_float4(x[0], x[1], x[2], x[3]);
-        v[1] = make_float4(x[4], x[5], x[6], x[7]);
+    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8], bool wide) {
+        if (wide) {
+            st_global_v8(p, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]),
+                         __float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+        } else {
+            reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        }
     }
 };
 
@@ -124,17 +137,17 @@ struct LaneMap {
     }
 };
 
-// Eight consecutive (cos, sin) pairs, or eight floats, out of shared memory.
-__device__ __forceinline__ void read_angles(const float2* cs, float (&c)[8], float (&s)[8]) {
-    const float4* v = reinterpret_cast<const float4*>(cs);
+// A lane's eight (cos, sin) pairs, and a chunk of eight weights, out of shared memory.
+__device__ __forceinline__ void read_angles(const float2* cs, int chunk, float (&c)[8], float (&s)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float4 w = v[i];
+        const float4 w = *reinterpret_cast<const float4*>(cs + i * (kMaxPairs / 4) + chunk * 2);
         c[2 * i] = w.x; s[2 * i] = w.y; c[2 * i + 1] = w.z; s[2 * i + 1] = w.w;
     }
 }
-__device__ __forceinline__ void read8(const float* p, float (&x)[8]) {
-    const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
+template <int D>
+__device__ __forceinline__ void read_weights(const float* w, int chunk, float (&x)[8]) {  // [half of a chunk][chunk][4]
+    const float4 u = *reinterpret_cast<const float4*>(w + chunk * 4), v = *reinterpret_cast<const float4*>(w + D / 2 + chunk * 4);
     x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
     x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
 }
@@ -144,16 +157,16 @@ template <class T, int D>
 __device__ __forceinline__ void stage_weights(const Params& p, float (*w)[D]) {
     for (int i = threadIdx.x; i < 2 * D / 8; i += kWarps * 32) {
         float x[8];
-        T::unpack(T::load(static_cast<const typename T::Elem*>(i < D / 8 ? p.q_weight : p.k_weight) + (i % (D / 8)) * 8), x);
+        T::unpack(T::load(static_cast<const typename T::Elem*>(i < D / 8 ? p.q_weight : p.k_weight) + (i % (D / 8)) * 8, false), x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[i / (D / 8)][(i % (D / 8)) * 8 + e] = x[e];
+        for (int e = 0; e < 8; ++e) w[i / (D / 8)][(e >> 2) * (D / 2) + (i % (D / 8)) * 4 + (e & 3)] = x[e];
     }
     __syncthreads();
 }
 
 // The loads run a batch ahead of the arithmetic, the first batch in front of the angles: a warp always has rows in flight.
 template <class T, int D, bool kNorm>
-__global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3 : 2) qk_rope_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6 : 4) qk_rope_kernel(const __grid_constant__ Params p) {
     typedef LaneMap<D> Map;
     typedef typename T::Elem Elem;
     constexpr int kUnroll = sizeof(Elem) == 2 ? 2 : 1;  // units of a batch
@@ -176,8 +189,8 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3
             const int32_t head = (u0 + i - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
             const Elem* src = (is_q ? q : k) + head * D;
             const bool there = u0 + i < u_end && head < (is_q ? p.num_q_heads : p.num_kv_heads);
-            raw[i][0] = there ? T::load(src + map.off_a) : T::zero();
-            raw[i][1] = there ? T::load(src + map.off_b) : T::zero();
+            raw[i][0] = there ? T::load(src + map.off_a, p.wide) : T::zero();
+            raw[i][1] = there ? T::load(src + map.off_b, p.wide) : T::zero();
         }
     };
     load(now, u_begin);
@@ -185,7 +198,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3
     if (kNorm) stage_weights<T, D>(p, weight);
     if (u_begin >= u_end) return;
     float c[8], s[8];
-    if (map.turned) read_angles(cs_all[warp] + map.off_a, c, s);
+    if (map.turned) read_angles(cs_all[warp], map.off_a >> 3, c, s);
 
     for (int32_t u0 = u_begin; u0 < u_end; u0 += kUnroll) {
         load(next, u0 + kUnroll);
@@ -203,10 +216,10 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3
                 for (int e = 0; e < 8; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
                 const float r = rsqrtf(row_sum<Map::kLanes>(ss) * (1.f / D) + p.eps);
                 float w[8];
-                read8(weight[is_q ? 0 : 1] + map.off_a, w);
+                read_weights<D>(weight[is_q ? 0 : 1], map.off_a >> 3, w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a[e] = a[e] * r * w[e];
-                read8(weight[is_q ? 0 : 1] + map.off_b, w);
+                read_weights<D>(weight[is_q ? 0 : 1], map.off_b >> 3, w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) b[e] = b[e] * r * w[e];
             }
@@ -220,8 +233,8 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3
             }
             if (head < (is_q ? p.num_q_heads : p.num_kv_heads)) {
                 Elem* dst = (is_q ? static_cast<Elem*>(p.q_out) + token * p.q_out_stride : static_cast<Elem*>(p.k_out) + token * p.k_out_stride) + head * D;
-                T::store(dst + map.off_a, a);
-                T::store(dst + map.off_b, b);
+                T::store(dst + map.off_a, a, p.wide);
+                T::store(dst + map.off_b, b, p.wide);
             }
         }
 #pragma unroll
@@ -236,7 +249,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 3
 // registers, those of k (a fraction of the rows) in shared memory, a lane's own 16 values each.  A CTA leaves one partial
 // row per tensor, which dw_reduce_kernel adds up in a fixed order: the same result from run to run.
 template <class T, int D, bool kNorm>
-__global__ void __launch_bounds__(kWarps * 32, 2) qk_rope_bwd_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kWarps * 32, 4) qk_rope_bwd_kernel(const __grid_constant__ Params p) {
     typedef LaneMap<D> Map;
     typedef typename T::Elem Elem;
     __shared__ __align__(16) float2 cs_all[kWarps][kMaxPairs];
@@ -272,11 +285,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qk_rope_bwd_kernel(const __gri
             const bool there = u < u_end && head < (is_q ? p.num_q_heads : p.num_kv_heads);
             const Elem* x = (is_q ? q : k) + head * D;
             const float* g = (is_q ? dq : dk) + head * D;
-            r.g[0] = there ? F32::load(g + map.off_a) : F32::zero();
-            r.g[1] = there ? F32::load(g + map.off_b) : F32::zero();
+            r.g[0] = there ? F32::load(g + map.off_a, p.wide) : F32::zero();
+            r.g[1] = there ? F32::load(g + map.off_b, p.wide) : F32::zero();
             if (kNorm) {
-                r.x[0] = there ? T::load(x + map.off_a) : T::zero();
-                r.x[1] = there ? T::load(x + map.off_b) : T::zero();
+                r.x[0] = there ? T::load(x + map.off_a, p.wide) : T::zero();
+                r.x[1] = there ? T::load(x + map.off_b, p.wide) : T::zero();
             }
         };
         load(now, u_begin);
@@ -292,7 +305,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qk_rope_bwd_kernel(const __gri
             F32::unpack(now.g[1], h);
             if (map.turned) {
                 float c[8], s[8];
-                read_angles(cs_all[warp] + map.off_a, c, s);
+                read_angles(cs_all[warp], map.off_a >> 3, c, s);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float x = g[i], y = h[i];
@@ -304,8 +317,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qk_rope_bwd_kernel(const __gri
                 float a[8], b[8], wa[8], wb[8];
                 T::unpack(now.x[0], a);
                 T::unpack(now.x[1], b);
-                read8(weight[is_q ? 0 : 1] + map.off_a, wa);
-                read8(weight[is_q ? 0 : 1] + map.off_b, wb);
+                read_weights<D>(weight[is_q ? 0 : 1], map.off_a >> 3, wa);
+                read_weights<D>(weight[is_q ? 0 : 1], map.off_b >> 3, wb);
                 float ss = 0.f, dot = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -347,8 +360,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) qk_rope_bwd_kernel(const __gri
             }
             if (there) {
                 Elem* dst = (is_q ? static_cast<Elem*>(p.q_out) + token * p.q_out_stride : static_cast<Elem*>(p.k_out) + token * p.k_out_stride) + head * D;
-                T::store(dst + map.off_a, g);
-                T::store(dst + map.off_b, h);
+                T::store(dst + map.off_a, g, p.wide);
+                T::store(dst + map.off_b, h, p.wide);
             }
             now = next;
         }
@@ -460,6 +473,10 @@ Params make_params(const RopeArgs& a, int sms) {
     p.eps = a.desc->eps;
     p.dq = a.dq;
     p.dk = a.dk;
+    p.wide = true;
+    for (const void* t : {a.q, a.k, static_cast<const void*>(a.q_out), static_cast<const void*>(a.k_out), static_cast<const void*>(a.dq),
+                          static_cast<const void*>(a.dk)})
+        p.wide = p.wide && (reinterpret_cast<uintptr_t>(t) & 31u) == 0;
     p.dw_partial = a.dq_weight != nullptr ? static_cast<float*>(a.workspace) : nullptr;
     for (int i = 0; i < kMaxPairs; ++i)
         p.axis[i] = a.desc->pair_axis != nullptr && i < p.rot / 2 ? a.desc->pair_axis[i] : 0;
