@@ -243,10 +243,10 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream_ptr(stream) -> int:
-    torch = _torch()
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    c = _torch()._C  # the raw handles: torch.cuda's own functions take ten times as long
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def _tok_stride(t) -> int:
@@ -263,7 +263,7 @@ def _tok_stride(t) -> int:
 def _workspace(nbytes: int, device, workspace):
     torch = _torch()
     if workspace is not None:
-        if workspace.numel() * workspace.element_size() < nbytes:
+        if workspace.nbytes < nbytes:
             raise ValueError(f"workspace too small: need {nbytes} bytes")
         return workspace
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
@@ -280,7 +280,7 @@ def _in_call_context(fn):
         torch = _torch()
         first = args[0] if args else next(iter(kwargs.values()))
         stream = kwargs.get("stream")
-        if stream is None and first.device.index == torch.cuda.current_device():
+        if stream is None and first.is_cuda and first.get_device() == torch._C._cuda_getDevice():
             return fn(*args, **kwargs)  # the usual case, without the cost of entering a context
         with torch.cuda.device(first.device):
             if stream is None:
@@ -748,29 +748,30 @@ def qk_norm_rope_backward(q, k, dq, dk, positions, inv_freq, q_weight=None, k_we
     ``accumulate_dw``).  Returns (dq_in, dk_in, dq_weight, dk_weight), the last two None without weights."""
     torch = _torch()
     lib = load_library()
-    desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)
+    desc = ctypes.byref(_rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps))
     for g, x in ((dq, q), (dk, k)):
         if g.dtype != torch.float32 or g.shape != x.shape or not g.is_contiguous():
             raise ValueError("dq and dk are contiguous float32 tensors of the shapes of q and k")
     dq_in, dk_in = _rope_out(dq_in, q), _rope_out(dk_in, k)
-    d = q.shape[2]
-    ws = None
+    tokens, _, d = q.shape
+    ws, ws_bytes = None, 0
     if q_weight is not None:
         if accumulate_dw and (dq_weight is None or dk_weight is None):
             raise ValueError("accumulate_dw needs the dq_weight and dk_weight buffers to add to")
         if dq_weight is None:
-            dq_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+            dq_weight = torch.empty(d, dtype=torch.float32, device=q.device)
         if dk_weight is None:
-            dk_weight = torch.empty((d,), dtype=torch.float32, device=q.device)
+            dk_weight = torch.empty(d, dtype=torch.float32, device=q.device)
         for w in (dq_weight, dk_weight):
-            if w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous():
+            if w.dtype != torch.float32 or w.dim() != 1 or w.shape[0] != d or not w.is_contiguous():
                 raise ValueError("weight gradients are contiguous float32 [head_dim] tensors")
-        ws = _workspace(int(lib.rpx_qk_norm_rope_backward_workspace_bytes(ctypes.byref(desc), q.shape[0])), q.device, workspace)
-    rc = lib.rpx_qk_norm_rope_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
-                                       _ptr(k_weight), _ptr(positions), _axis_stride(positions), _ptr(inv_freq), _ptr(dq),
-                                       _ptr(dk), q.shape[0], _ptr(dq_in), _ptr(dk_in), _tok_stride(dq_in), _tok_stride(dk_in),
-                                       _ptr(dq_weight), _ptr(dk_weight), 1 if accumulate_dw else 0, _ptr(ws),
-                                       ws.numel() * ws.element_size() if ws is not None else 0, _stream_ptr(stream))
+        ws = _workspace(lib.rpx_qk_norm_rope_backward_workspace_bytes(desc, tokens), q.device, workspace)
+        ws_bytes = ws.nbytes
+    rc = lib.rpx_qk_norm_rope_backward(desc, q.data_ptr(), k.data_ptr(), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
+                                       _ptr(k_weight), positions.data_ptr(), _axis_stride(positions), inv_freq.data_ptr(),
+                                       dq.data_ptr(), dk.data_ptr(), tokens, dq_in.data_ptr(), dk_in.data_ptr(),
+                                       _tok_stride(dq_in), _tok_stride(dk_in), _ptr(dq_weight), _ptr(dk_weight),
+                                       1 if accumulate_dw else 0, _ptr(ws), ws_bytes, _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_qk_norm_rope_backward")
     return dq_in, dk_in, dq_weight, dk_weight
@@ -778,17 +779,20 @@ def qk_norm_rope_backward(q, k, dq, dk, positions, inv_freq, q_weight=None, k_we
 
 # ------------------------------------------------------------------ pages of the cache
 def _page_pool(block_table, lens, ref_counts) -> PagePool:
-    torch = _torch()
-    for t in (block_table, lens, ref_counts):
-        if t is not None and t.dtype != torch.int32:
-            raise TypeError("block_table, lens and ref_counts are int32")
-    if block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+    i32 = _torch().int32
+    if block_table.dtype != i32 or ref_counts.dtype != i32 or (lens is not None and lens.dtype != i32):
+        raise TypeError("block_table, lens and ref_counts are int32")
+    shape = block_table.shape
+    if len(shape) != 2:
         raise ValueError("block_table is [rows, pages] with contiguous rows")
-    if not ref_counts.is_contiguous() or (lens is not None and (not lens.is_contiguous() or lens.shape[0] != block_table.shape[0])):
+    rows, cols = shape
+    stride = block_table.stride()
+    if cols > 1 and stride[1] != 1:
+        raise ValueError("block_table is [rows, pages] with contiguous rows")
+    if not ref_counts.is_contiguous() or (lens is not None and (lens.numel() != rows or not lens.is_contiguous())):
         raise ValueError("ref_counts [num_blocks] and lens [rows] are contiguous")
-    rows, cols = block_table.shape
-    return PagePool(block_table.data_ptr(), block_table.stride(0) if rows > 1 else cols, cols, rows, _ptr(lens),
-                    ref_counts.data_ptr(), ref_counts.shape[0])
+    return PagePool(block_table.data_ptr(), stride[0] if rows > 1 else cols, cols, rows, _ptr(lens), ref_counts.data_ptr(),
+                    ref_counts.numel())
 
 
 def _row_list(t):
@@ -800,9 +804,8 @@ def _row_list(t):
 @_in_call_context
 def pages_free(block_table, lens, ref_counts, rows, device_status=None, stream=None) -> None:
     """rpx_pages_free: the listed rows give up their pages (reference counts go down, entries become -1, lens 0)."""
-    pool = _page_pool(block_table, lens, ref_counts)
-    rc = load_library().rpx_pages_free(ctypes.byref(pool), _ptr(_row_list(rows)), rows.shape[0], _ptr(device_status),
-                                       _stream_ptr(stream))
+    pool = ctypes.byref(_page_pool(block_table, lens, ref_counts))
+    rc = load_library().rpx_pages_free(pool, _row_list(rows).data_ptr(), rows.numel(), _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_pages_free")
 
@@ -816,19 +819,21 @@ def pages_fork(block_table, lens, ref_counts, src_rows, dst_rows, extra_tokens: 
     Returns (copy_src, copy_dst) int32 [n]: the partial pages to copy in every layer (``cache_copy_pages``), -1 where none."""
     torch = _torch()
     lib = load_library()
-    pool = _page_pool(block_table, lens, ref_counts)
-    n = _row_list(src_rows).shape[0]
-    if _row_list(dst_rows).shape[0] != n:
+    pool = ctypes.byref(_page_pool(block_table, lens, ref_counts))
+    n = _row_list(src_rows).numel()
+    if _row_list(dst_rows).numel() != n:
         raise ValueError("src_rows and dst_rows have one entry per request")
     if copy_src is None:
-        copy_src = torch.empty((n,), dtype=torch.int32, device=block_table.device)
-    if copy_dst is None:
-        copy_dst = torch.empty((n,), dtype=torch.int32, device=block_table.device)
-    if _row_list(copy_src).shape[0] < n or _row_list(copy_dst).shape[0] < n:
+        copy_src = torch.empty_like(src_rows)
+    elif _row_list(copy_src).numel() < n:
         raise ValueError("copy_src and copy_dst have one entry per request")
-    ws = _workspace(int(lib.rpx_pages_fork_workspace_bytes(ctypes.byref(pool), n)), block_table.device, workspace)
-    rc = lib.rpx_pages_fork(ctypes.byref(pool), _ptr(src_rows), _ptr(dst_rows), n, int(extra_tokens), _ptr(copy_src),
-                            _ptr(copy_dst), _ptr(ws), ws.numel() * ws.element_size(), _ptr(device_status), _stream_ptr(stream))
+    if copy_dst is None:
+        copy_dst = torch.empty_like(src_rows)
+    elif _row_list(copy_dst).numel() < n:
+        raise ValueError("copy_src and copy_dst have one entry per request")
+    ws = _workspace(lib.rpx_pages_fork_workspace_bytes(pool, n), block_table.device, workspace)
+    rc = lib.rpx_pages_fork(pool, src_rows.data_ptr(), dst_rows.data_ptr(), n, extra_tokens, copy_src.data_ptr(),
+                            copy_dst.data_ptr(), ws.data_ptr(), ws.nbytes, _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_pages_fork")
     return copy_src, copy_dst
@@ -844,24 +849,25 @@ def pages_compact(block_table, ref_counts, table_out=None, ref_counts_out=None, 
     the number of live pages (int32 [1])."""
     torch = _torch()
     lib = load_library()
-    pool = _page_pool(block_table, None, ref_counts)
+    pool = ctypes.byref(_page_pool(block_table, None, ref_counts))
+    blocks = ref_counts.numel()
     table_out = block_table if table_out is None else table_out
     ref_counts_out = ref_counts if ref_counts_out is None else ref_counts_out
     out = _page_pool(table_out, None, ref_counts_out)
-    if table_out.shape != block_table.shape or ref_counts_out.shape != ref_counts.shape:
+    if table_out.shape != block_table.shape or ref_counts_out.numel() != blocks:
         raise ValueError("table_out and ref_counts_out have the shapes of block_table and ref_counts")
-    moves, dev = ref_counts.shape[0] // 2, block_table.device
+    moves, dev = blocks // 2, block_table.device
     if copy_src is None:
-        copy_src = torch.empty((moves,), dtype=torch.int32, device=dev)
+        copy_src = torch.empty(moves, dtype=torch.int32, device=dev)
     if copy_dst is None:
-        copy_dst = torch.empty((moves,), dtype=torch.int32, device=dev)
+        copy_dst = torch.empty(moves, dtype=torch.int32, device=dev)
     if n_live is None:
-        n_live = torch.empty((1,), dtype=torch.int32, device=dev)
-    if _row_list(copy_src).shape[0] < moves or _row_list(copy_dst).shape[0] < moves or _row_list(n_live).shape[0] < 1:
+        n_live = torch.empty(1, dtype=torch.int32, device=dev)
+    if _row_list(copy_src).numel() < moves or _row_list(copy_dst).numel() < moves or _row_list(n_live).numel() < 1:
         raise ValueError("copy_src and copy_dst have num_blocks // 2 entries, n_live one")
-    ws = _workspace(int(lib.rpx_pages_compact_workspace_bytes(ctypes.byref(pool))), dev, workspace)
-    rc = lib.rpx_pages_compact(ctypes.byref(pool), out.block_table, out.block_table_stride, out.ref_counts, _ptr(copy_src),
-                               _ptr(copy_dst), _ptr(n_live), _ptr(ws), ws.numel() * ws.element_size(), _ptr(device_status),
+    ws = _workspace(lib.rpx_pages_compact_workspace_bytes(pool), dev, workspace)
+    rc = lib.rpx_pages_compact(pool, out.block_table, out.block_table_stride, out.ref_counts, copy_src.data_ptr(),
+                               copy_dst.data_ptr(), n_live.data_ptr(), ws.data_ptr(), ws.nbytes, _ptr(device_status),
                                _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_pages_compact")
@@ -873,20 +879,21 @@ def cache_copy_pages(k_cache, v_cache, src, dst, device_status=None, stream=None
     """rpx_cache_copy_pages: page src[i] -> page dst[i] of both pools (pairs of -1 skipped).
 
     Pools bfloat16 [num_blocks, H_kv, 16, d], or [layers, num_blocks, H_kv, 16, d] for all layers at once."""
-    torch = _torch()
-    if k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16:
+    bf16 = _torch().bfloat16
+    if k_cache.dtype != bf16 or v_cache.dtype != bf16:
         raise TypeError("cache pools are bfloat16")
-    if k_cache.shape != v_cache.shape or k_cache.dim() not in (4, 5) or k_cache.shape[-2] != BLOCK_SIZE:
+    shape = k_cache.shape
+    if v_cache.shape != shape or len(shape) not in (4, 5) or shape[-2] != BLOCK_SIZE:
         raise ValueError("cache pools are [(layers,) blocks, kv_heads, 16, head_dim], K and V alike")
     if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise ValueError("cache pools must be contiguous")
-    layers = k_cache.shape[0] if k_cache.dim() == 5 else 1
-    blocks, heads, _, d = k_cache.shape[-4:]
-    n = _row_list(src).shape[0]
-    if _row_list(dst).shape[0] != n:
+    blocks, heads, _, d = shape[-4:]
+    n = _row_list(src).numel()
+    if _row_list(dst).numel() != n:
         raise ValueError("src and dst have one entry per pair")
-    rc = load_library().rpx_cache_copy_pages(_ptr(k_cache), _ptr(v_cache), layers, blocks * heads * BLOCK_SIZE * d, blocks, heads,
-                                             d, _ptr(src), _ptr(dst), n, _ptr(device_status), _stream_ptr(stream))
+    rc = load_library().rpx_cache_copy_pages(k_cache.data_ptr(), v_cache.data_ptr(), shape[0] if len(shape) == 5 else 1,
+                                             blocks * heads * BLOCK_SIZE * d, blocks, heads, d, src.data_ptr(), dst.data_ptr(), n,
+                                             _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_cache_copy_pages")
 
@@ -897,16 +904,20 @@ def cache_append(k, v, cu_append, cached_lens, max_append: int, cache: Tuple, to
     """rpx_cache_append: K and V of tokens ``token_ids[cu_append[s]:cu_append[s + 1]]`` (or of the tokens of that range
     themselves) are stored at positions cached_lens[s], cached_lens[s] + 1, .. of sequence s; cached_lens stays as it is."""
     cs = _cache_struct(cache)
-    if v.shape != k.shape or v.dtype != k.dtype or tuple(cache[0].shape[1:]) != (k.shape[1], BLOCK_SIZE, k.shape[2]):
+    shape = k.shape
+    if len(shape) != 3:
         raise ValueError("k and v are [tokens, kv_heads, head_dim] tensors that fit the cache pools")
-    batch = _row_list(cached_lens).shape[0]
-    if _row_list(cu_append).shape[0] != batch + 1 or cache[2].shape[0] < batch:
+    tokens, heads, d = shape
+    if v.shape != shape or v.dtype != k.dtype or cache[0].shape[1:] != (heads, BLOCK_SIZE, d):
+        raise ValueError("k and v are [tokens, kv_heads, head_dim] tensors that fit the cache pools")
+    batch = _row_list(cached_lens).numel()
+    if _row_list(cu_append).numel() != batch + 1 or cache[2].shape[0] < batch:
         raise ValueError("cu_append has one entry more than cached_lens, and the block table a row for each sequence")
+    ids, n_ids = None, 0
     if token_ids is not None:
-        _row_list(token_ids)
-    rc = load_library().rpx_cache_append(_ptr(k), _ptr(v), _tok_stride(k), _tok_stride(v), k.shape[0], k.shape[1], k.shape[2],
-                                         _dtype_code(k), _ptr(token_ids), token_ids.shape[0] if token_ids is not None else 0,
-                                         _ptr(cu_append), _ptr(cached_lens), batch, int(max_append), ctypes.byref(cs),
-                                         _ptr(device_status), _stream_ptr(stream))
+        ids, n_ids = _row_list(token_ids).data_ptr(), token_ids.numel()
+    rc = load_library().rpx_cache_append(k.data_ptr(), v.data_ptr(), _tok_stride(k), _tok_stride(v), tokens, heads, d,
+                                         _dtype_code(k), ids, n_ids, cu_append.data_ptr(), cached_lens.data_ptr(), batch,
+                                         max_append, ctypes.byref(cs), _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_cache_append")
