@@ -119,8 +119,13 @@ __device__ __forceinline__ int32_t fresh_pages(const ForkRequest& r) {
     return max(0, r.need - (r.src == r.dst ? r.held : r.whole));
 }
 
-__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(PageArgs a, const int32_t* __restrict__ src_rows,
-                                                                 const int32_t* __restrict__ dst_rows, int32_t n, int32_t extra, ForkPlan plan) {
+__device__ __forceinline__ void apply_request(const PageArgs& a, const int32_t* src_rows, const int32_t* dst_rows, int32_t extra, const ForkPlan& plan,
+                                              int32_t i, int32_t self, int32_t threads, int32_t* copy_src, int32_t* copy_dst);
+
+// One block.  kApply: it also carries the requests out, a warp each (few of them: see launch_pages_fork).
+template <bool kApply>
+__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(PageArgs a, const int32_t* __restrict__ src_rows, const int32_t* __restrict__ dst_rows,
+                                                                 int32_t n, int32_t extra, ForkPlan plan, int32_t* copy_src, int32_t* copy_dst) {
     __shared__ int64_t sums[32];
     for (int32_t r = threadIdx.x; r < a.rows; r += kPlanThreads) plan.owner[r] = kNobody;
     __syncthreads();
@@ -170,16 +175,20 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(PageArgs a, con
         found += all;
     }
     if (threadIdx.x == 0) *plan.found = static_cast<int32_t>(min(found, wanted));
+    if (kApply) {
+        __syncthreads();
+        for (int32_t i = threadIdx.x >> 5; i < n; i += kPlanThreads / 32)
+            apply_request(a, src_rows, dst_rows, extra, plan, i, threadIdx.x & 31, 32, copy_src, copy_dst);
+    }
 }
 
-// One block per request: its row of the table, the counts, the pair of pages to copy.
-__global__ void __launch_bounds__(256) fork_apply_kernel(PageArgs a, const int32_t* __restrict__ src_rows, const int32_t* __restrict__ dst_rows,
-                                                         int32_t extra, ForkPlan plan, int32_t* copy_src, int32_t* copy_dst) {
-    const int32_t i = blockIdx.x;
+// One request's row of the table, the counts, the pair of pages to copy; by `threads` threads, of which this is number `self`.
+__device__ __forceinline__ void apply_request(const PageArgs& a, const int32_t* src_rows, const int32_t* dst_rows, int32_t extra, const ForkPlan& plan,
+                                              int32_t i, int32_t self, int32_t threads, int32_t* copy_src, int32_t* copy_dst) {
     const int32_t fresh = plan.fresh[i], start = plan.start[i];
     int32_t from_page = -1, to_page = -1;
     if (fresh > 0 && static_cast<int64_t>(start) + fresh > *plan.found) {
-        if (threadIdx.x == 0) report(a.device_status, RPX_ERR_NO_PAGES);
+        if (self == 0) report(a.device_status, RPX_ERR_NO_PAGES);
     } else if (fresh >= 0) {
         const int32_t src = __ldg(src_rows + i), dst = __ldg(dst_rows + i);
         const int32_t len = src >= 0 ? a.lens[src] : 0;
@@ -190,19 +199,19 @@ __global__ void __launch_bounds__(256) fork_apply_kernel(PageArgs a, const int32
         int32_t* to = a.block_table + static_cast<int64_t>(dst) * a.block_table_stride;
         bool bad = false;
         if (!grows)
-            for (int32_t j = threadIdx.x; j < whole; j += blockDim.x) {
+            for (int32_t j = self; j < whole; j += threads) {
                 const int32_t page = from[j];
                 to[j] = page;
                 if (page >= 0 && page < a.num_blocks) atomicAdd(a.ref_counts + page, 1);
                 else bad = true;
             }
-        for (int32_t j = threadIdx.x; j < fresh; j += blockDim.x) {
+        for (int32_t j = self; j < fresh; j += threads) {
             const int32_t page = plan.pages[start + j];
             to[first + j] = page;
             a.ref_counts[page] = 1;
         }
         if (bad) report(a.device_status, RPX_ERR_DEVICE_DATA);
-        if (threadIdx.x == 0 && !grows) {
+        if (self == 0 && !grows) {
             a.lens[dst] = len;
             if (len % kPage != 0) {
                 from_page = from[whole];
@@ -211,10 +220,15 @@ __global__ void __launch_bounds__(256) fork_apply_kernel(PageArgs a, const int32
             }
         }
     }
-    if (threadIdx.x == 0) {
+    if (self == 0) {
         copy_src[i] = from_page;
         copy_dst[i] = to_page;
     }
+}
+
+__global__ void __launch_bounds__(256) fork_apply_kernel(PageArgs a, const int32_t* __restrict__ src_rows, const int32_t* __restrict__ dst_rows,
+                                                         int32_t extra, ForkPlan plan, int32_t* copy_src, int32_t* copy_dst) {
+    apply_request(a, src_rows, dst_rows, extra, plan, blockIdx.x, threadIdx.x, blockDim.x, copy_src, copy_dst);
 }
 
 // ------------------------------------------------------------------ compact
@@ -320,6 +334,66 @@ compact_table_kernel(PageArgs a, int32_t* table_out, int64_t table_out_stride, i
         table_out[row * table_out_stride + col] = page;
     }
     if (bad) report(a.device_status, RPX_ERR_DEVICE_DATA);
+}
+
+// The same in one block and one launch, for small pools and tables.
+constexpr int kSmallThreads = 1024, kSmallPages = 4 * kSmallThreads, kSmallEntries = 8 * kSmallThreads;
+__global__ void __launch_bounds__(kSmallThreads)
+compact_small_kernel(PageArgs a, int32_t* table_out, int64_t table_out_stride, int32_t* ref_counts_out, int32_t* copy_src, int32_t* copy_dst, int32_t* n_live) {
+    __shared__ int32_t sums[32];
+    __shared__ int32_t place[kSmallPages];    // of every page: itself, where it goes, or -1 (free)
+    __shared__ int32_t hole[kSmallPages / 2]; // free numbers below L
+    constexpr int kPer = kSmallPages / kSmallThreads;
+    int32_t count[kPer], rank[kPer], live = 0, all;  // rank: live pages before this one
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int32_t id = k * kSmallThreads + static_cast<int32_t>(threadIdx.x);
+        count[k] = id < a.num_blocks ? a.ref_counts[id] : 0;
+        const int32_t one = count[k] > 0 ? 1 : 0;
+        rank[k] = live + block_scan<kSmallThreads, int32_t>(one, sums, &all) - one;
+        live += all;
+    }
+    int32_t mine = 0, below;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int32_t id = k * kSmallThreads + static_cast<int32_t>(threadIdx.x);
+        if (id < live && count[k] > 0) ++mine;
+        if (id < live && count[k] <= 0) hole[id - rank[k]] = id;
+    }
+    block_scan<kSmallThreads, int32_t>(mine, sums, &below);  // (its barriers also order `hole`)
+    const int32_t moves = live - below, max_moves = a.num_blocks / 2;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int32_t id = k * kSmallThreads + static_cast<int32_t>(threadIdx.x);
+        if (id >= a.num_blocks) continue;
+        int32_t to = count[k] > 0 ? id : -1;
+        if (count[k] > 0 && id >= live) {
+            const int32_t m = rank[k] - below;
+            to = hole[m];
+            copy_src[m] = id;
+            copy_dst[m] = to;
+            ref_counts_out[to] = count[k];
+        }
+        place[id] = to;
+        // a hole that a page moves into was written by that page (every one is); all else keeps its count or is free
+        if (id >= live || count[k] > 0) ref_counts_out[id] = to == id ? count[k] : 0;
+        if (id >= moves && id < max_moves) copy_src[id] = copy_dst[id] = -1;
+    }
+    __syncthreads();
+    bool bad = false;
+    const int32_t entries = a.rows * a.table_cols;
+    for (int32_t e = threadIdx.x; e < entries; e += kSmallThreads) {
+        const int32_t row = e / a.table_cols, col = e - row * a.table_cols;
+        int32_t page = a.block_table[static_cast<int64_t>(row) * a.block_table_stride + col];
+        if (page >= 0) {
+            page = page < a.num_blocks ? place[page] : -1;
+            bad |= page < 0;
+        }
+        table_out[row * table_out_stride + col] = page;
+    }
+    if (bad) report(a.device_status, RPX_ERR_DEVICE_DATA);
+    if (threadIdx.x == 0) *n_live = live;
 }
 
 // ------------------------------------------------------------------ copying pages
@@ -439,7 +513,12 @@ rpx_status_t launch_pages_fork(const PageArgs& a, const int32_t* src_rows, const
     plan.owner = plan.fresh + n;
     plan.pages = plan.owner + a.rows;
     plan.found = plan.pages + a.num_blocks;
-    fork_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(a, src_rows, dst_rows, n, extra, plan);
+    // a block of its own per request takes a launch more (2.5 us), which up to some thousand table entries is the longer way
+    if (static_cast<int64_t>(n) * a.table_cols <= 8192) {
+        fork_plan_kernel<true><<<1, kPlanThreads, 0, a.stream>>>(a, src_rows, dst_rows, n, extra, plan, copy_src, copy_dst);
+        return launched();
+    }
+    fork_plan_kernel<false><<<1, kPlanThreads, 0, a.stream>>>(a, src_rows, dst_rows, n, extra, plan, copy_src, copy_dst);
     if (rpx_status_t rc = launched()) return rc;
     fork_apply_kernel<<<static_cast<unsigned>(n), 256, 0, a.stream>>>(a, src_rows, dst_rows, extra, plan, copy_src, copy_dst);
     return launched();
@@ -451,6 +530,10 @@ size_t pages_compact_workspace(int32_t num_blocks) {
 
 rpx_status_t launch_pages_compact(const PageArgs& a, int32_t* table_out, int64_t table_out_stride, int32_t* ref_counts_out,
                                   int32_t* copy_src, int32_t* copy_dst, int32_t* n_live, void* workspace) {
+    if (a.num_blocks <= kSmallPages && static_cast<int64_t>(a.rows) * a.table_cols <= kSmallEntries) {
+        compact_small_kernel<<<1, kSmallThreads, 0, a.stream>>>(a, table_out, table_out_stride, ref_counts_out, copy_src, copy_dst, n_live);
+        return launched();
+    }
     const int32_t chunks = (a.num_blocks + kChunk - 1) / kChunk;
     int32_t* place = static_cast<int32_t*>(workspace);
     int32_t* counts = place + a.num_blocks;

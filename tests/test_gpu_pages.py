@@ -219,11 +219,11 @@ def test_double_counted_entries_are_reported(cuda_device):
     assert p.refs.tolist() == [0] * 12 and bool((p.table[0] == -1).all())
 
 
-@pytest.mark.parametrize("nb,seed", [(1, 0), (7, 1), (1000, 2), (1024, 3), (5000, 4), (40000, 5)])
+@pytest.mark.parametrize("nb,seed", [(1, 0), (7, 1), (1000, 2), (1024, 3), (4096, 6), (4097, 7), (5000, 4), (40000, 5)])
 @pytest.mark.parametrize("in_place", [True, False])
 def test_compaction(cuda_device, nb, seed, in_place):
     rng = np.random.default_rng(seed)
-    rows, cols = 9, max(1, nb // 4)
+    rows, cols = 9, max(1, min(nb // 4, 900 if nb == 4096 else nb))
     p = Pool(cuda_device, nb, rows, cols, pad=2, hkv=1)
     for r in range(rows - 1):
         take = rng.permutation(nb)[:rng.integers(0, max(1, nb // 10) + 1)][:cols]
