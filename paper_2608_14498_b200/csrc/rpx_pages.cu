@@ -400,6 +400,20 @@ compact_small_kernel(PageArgs a, int32_t* table_out, int64_t table_out_stride, i
 // A unit is one page of one tensor of one layer.  Lists may be mostly -1 (a compaction's list is as long as the most it
 // could move), so a block first gathers the valid ones among 256 of its units, then streams them.
 constexpr int kCopyThreads = 256;
+
+// Chunks c, c + kCopyThreads, .. of a page, kAhead loads in flight; returns the first that is left.
+template <int kAhead>
+__device__ __forceinline__ int32_t copy_run(const uint4* a, uint4* b, int32_t c, int32_t n) {
+    for (; c + (kAhead - 1) * kCopyThreads < n; c += kAhead * kCopyThreads) {
+        uint4 x[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) x[e] = __ldcs(a + c + e * kCopyThreads);
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) __stcs(b + c + e * kCopyThreads, x[e]);
+    }
+    return c;
+}
+
 __global__ void __launch_bounds__(kCopyThreads)
 copy_pages_kernel(uint4* k_cache, uint4* v_cache, int64_t layer_stride, int32_t layers, int32_t num_blocks, int32_t page_chunks,
                   const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int64_t n, int32_t* status) {
@@ -430,15 +444,10 @@ copy_pages_kernel(uint4* k_cache, uint4* v_cache, int64_t layer_stride, int32_t 
             uint4* pool = ((part[i] & 1) != 0 ? v_cache : k_cache) + (part[i] >> 1) * layer_stride;
             const uint4* a = pool + static_cast<int64_t>(from[i]) * page_chunks;
             uint4* b = pool + static_cast<int64_t>(to[i]) * page_chunks;
-            int32_t c = threadIdx.x;
-            for (; c + 3 * kCopyThreads < page_chunks; c += 4 * kCopyThreads) {
-                uint4 x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = a[c + e * kCopyThreads];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b[c + e * kCopyThreads] = x[e];
-            }
-            for (; c < page_chunks; c += kCopyThreads) b[c] = a[c];
+            // (8 loads ahead copy 24000-page pools at 91 % of the copy rate, 4 at 90)
+            int32_t c = copy_run<8>(a, b, threadIdx.x, page_chunks);
+            c = copy_run<4>(a, b, c, page_chunks);
+            copy_run<1>(a, b, c, page_chunks);
         }
         __syncthreads();
     }
