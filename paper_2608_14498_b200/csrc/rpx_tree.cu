@@ -178,7 +178,7 @@ tree_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
             // Probabilities are rounded to bf16 for the P V product.  Over few keys that rounding is not averaged away, so
             // short segments carry P as two bf16 terms (2^-17).
-            const bool two_terms = q.tiles <= 4;
+            const bool two_terms = kRowTiles <= 2 || q.tiles <= 4;
             float o[D / 8][4];
 #pragma unroll
             for (int i = 0; i < D / 8; ++i)
