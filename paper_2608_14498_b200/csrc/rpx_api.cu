@@ -58,7 +58,7 @@ TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t b
     w.sets_off = align_up(own, kWsAlign);
     w.values_off = w.sets_off + align_up(static_cast<size_t>(tokens) * tree_set_words(max_tree) * sizeof(uint32_t), kWsAlign);
     w.bytes = w.values_off;
-    if (d->dtype == RPX_BF16) w.bytes += align_up(static_cast<size_t>(tokens) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
+    if (d->dtype == RPX_BF16) w.bytes += align_up((static_cast<size_t>(tokens) + 8 * static_cast<size_t>(batch)) * d->num_kv_heads * d->head_dim * 2, kWsAlign);
     return w;
 }
 

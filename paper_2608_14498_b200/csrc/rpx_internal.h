@@ -147,7 +147,8 @@ size_t tree_tile_workspace(int32_t batch, int32_t head_dim, int32_t max_tree, in
 // bf16; sets and values as launch_tree_sets leaves them, launched directly before on the same stream
 rpx_status_t launch_tree_tile(const TreeArgs& a, const uint32_t* sets, const void* values);
 int32_t tree_set_words(int32_t max_tree);            // 32-bit words of one ancestor set, a multiple of 4
-// Ancestor sets [tokens][tree_set_words] and, unless NULL, the values with unused rows cleared, bf16 [tokens][H_kv][d].
+// Ancestor sets [tokens][tree_set_words] and, unless NULL, the values with unused rows cleared, bf16
+// [tokens + 8 batch][H_kv][d]: token t of sequence s in row t + 8 s.
 rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy);
 
 struct PageArgs {

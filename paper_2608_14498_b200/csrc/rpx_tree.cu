@@ -431,7 +431,8 @@ rpx_status_t launch_stream_d(const TreeArgs& a) {
 // ------------------------------------------------------------------ ancestor sets and values for the other forms
 // One warp per token: its ancestor set as mask words (lane w holds word w while all lanes walk the path to the root), all
 // zero for a node that is not in use or a token of no sequence; and, for the tensor-core form, a copy of the
-// tree's V with those rows cleared (a probability of 0 must not meet what they hold).
+// tree's V with those rows cleared (a probability of 0 must not meet what they hold), 8 rows more for every sequence before it
+// and zeros behind its last node: what is copied 8 rows at a time then never holds another sequence's values.
 constexpr int kSetWarps = 8;
 __global__ void __launch_bounds__(kSetWarps * 32)
 tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ parents, int32_t batch, int64_t total_tokens,
@@ -461,10 +462,10 @@ tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ par
         for (int32_t i = threadIdx.x; i < n0; i += kSetWarps * 32) staged[i] = __ldg(parents + begin0 + i);
     __syncthreads();
     if (token >= total_tokens) return;
-    int32_t tok0 = begin0;
+    int32_t tok0 = begin0, s = s0;
     int64_t n = n0;
     if (token >= begin0 + n0) {
-        const int32_t s = sequence_of(token);
+        s = sequence_of(token);
         tok0 = __ldg(cu + s);
         n = static_cast<int64_t>(__ldg(cu + s + 1)) - tok0;
     }
@@ -484,10 +485,12 @@ tree_sets_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ par
     if (!good && lane == 0 && status != nullptr) atomicCAS(status, 0, RPX_ERR_DEVICE_DATA);
     used = used && good;
     if (lane < words) sets[token * words + lane] = used ? bits : 0u;
-    if (v_copy != nullptr) {
+    if (v_copy != nullptr && inside) {
         const uint4* src = reinterpret_cast<const uint4*>(v + token * v_stride);
-        uint4* dst = reinterpret_cast<uint4*>(v_copy) + token * v_chunks;
+        uint4* dst = reinterpret_cast<uint4*>(v_copy) + (token + 8ll * s) * v_chunks;
         for (int32_t i = lane; i < v_chunks; i += 32) dst[i] = used ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+        if (token == tok0 + n - 1)  // zeros up to the next 8 rows of the sequence
+            for (int32_t i = lane; i < static_cast<int32_t>(-n & 7) * v_chunks; i += 32) dst[v_chunks + i] = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 

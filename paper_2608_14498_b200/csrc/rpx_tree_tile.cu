@@ -14,7 +14,7 @@
 //                    held up behind a V slot), one TMA box per 16-token page
 //   warp  9        : issues S_t = Q K^T (smem x smem -> TMEM) and O_t += P_t V (P as bf16 over S_t's first 64 columns)
 //   warps 10, 11   : only take part in the register hand-over
-// The tree's own V tiles come from a copy in which rows of unused nodes are zero, and ancestor sets as bit masks; a small
+// The tree's own V tiles come from a copy in which rows of unused nodes are zero (and no other sequence's rows follow), and ancestor sets as bit masks; a small
 // kernel writes both (tree_sets_kernel).  This kernel is launched on top of that one and waits for it only where it first
 // needs its results, behind the cached tiles.
 #include <type_traits>
@@ -160,10 +160,18 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         wait_for_sets();
                         have_sets = true;
                     }
-                    if (lane == 0) mbar_arrive_expect_tx(full, L::kTensorBytes);
+                    const int32_t boxes = min(kTile / 8, (q.n - own * kTile + 7) / 8);  // tokens start anywhere: a box per 8
+                    if (is_v && boxes < kTile / 8) {  // zeros behind the tree's last rows (what K holds there is masked)
+                        for (int32_t i = lane; i < (kTile - boxes * 8) * (D / 8); i += 32)
+                            *reinterpret_cast<uint4*>(dst + key_off<D>(boxes * 8 + i / (D / 8), i % (D / 8))) = make_uint4(0u, 0u, 0u, 0u);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    if (lane == 0) mbar_arrive_expect_tx(full, boxes * 8 * D * 2);
                     __syncwarp();
-                    if (lane < kTile / 8)  // tokens start anywhere: a box per 8
-                        tma_load_4d(dst + lane * (8 * D * 2), is_v ? &tmap_v : &tmap_k, full, 0, q.tok0 + own * kTile + lane * 8, 0, walk.head);
+                    if (lane < boxes)
+                        tma_load_4d(dst + lane * (8 * D * 2), is_v ? &tmap_v : &tmap_k, full, 0,
+                                    q.tok0 + own * kTile + lane * 8 + (is_v ? 8 * walk.s : 0), 0, walk.head);
                     return;
                 }
                 // K behind the last key may be anything (its scores are masked); V may not: what a probability of 0 meets
@@ -624,11 +632,11 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* va
         if (rpx_status_t rc = encode_tmap_bf16(&tq, a.q, 3, dims, strides, box)) return rc;
     }
     {
-        const uint64_t dims[4] = {64, tokens, D / 64, heads};
+        const uint64_t dims[4] = {64, tokens, D / 64, heads}, vdims[4] = {64, tokens + 8ull * a.batch, D / 64, heads};
         const uint64_t ks[3] = {static_cast<uint64_t>(a.k_tok_stride) * 2, 128, D * 2ull}, vs[3] = {heads * D * 2ull, 128, D * 2ull};
         const uint32_t box[4] = {64, 8, D / 64, 1};
         if (rpx_status_t rc = encode_tmap_bf16(&tk, a.k, 4, dims, ks, box)) return rc;
-        if (rpx_status_t rc = encode_tmap_bf16(&tv, values, 4, dims, vs, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&tv, values, 4, vdims, vs, box)) return rc;
     }
     {
         // the pool as groups of 8 keys: two per page and head

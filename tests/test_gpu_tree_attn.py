@@ -201,6 +201,21 @@ def test_rows_behind_the_last_sequence_stay(cuda_device, nodes):
     assert bool((out[-9:] == 7.0).all()) and bool((lse[-9:] == 7.0).all())
 
 
+@pytest.mark.parametrize("nodes", [[9, 5], [140, 30], [33, 129]])
+def test_a_sequence_does_not_meet_its_neighbours_values(cuda_device, nodes):
+    """Non-finite values in one sequence's nodes and cache leave every other sequence as it was."""
+    c = Case(cuda_device, [200, 77], nodes, 28, 4, 128)
+    want, want_lse = c.run()
+    a = nodes[0]
+    for own, other in ((slice(a, None), slice(0, a)), (slice(0, a), slice(a, None))):
+        k, v = c.k.clone(), c.v.clone()
+        c.k[own], c.v[own] = NAN, float("inf")
+        out, lse = c.run()
+        assert torch.equal(out[other], want[other]) and torch.equal(lse[other], want_lse[other])
+        assert not bool(torch.isfinite(out[own]).any())
+        c.k.copy_(k), c.v.copy_(v)
+
+
 @pytest.mark.parametrize("nodes", [[20], [160]])
 def test_peaked_scores_and_scale(cuda_device, nodes):
     """Scores up to hundreds: the running maximum moves by more than its threshold many times."""

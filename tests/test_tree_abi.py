@@ -51,12 +51,12 @@ def test_workspace_sizes(lib):
     small = B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 64, 8, 8)
     assert 0 < small < 32 << 20 and small % 256 == 0
     # 8 x 200 nodes in two-tile blocks: 9 first units, 148 pieces of 2 x 256 rows with (maximum, sum) and 128 floats each, then
-    # ancestor sets of 8 words and a copy of the values
+    # ancestor sets of 8 words and a copy of the values (8 rows more a sequence)
     wide = B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 8 * 200, 8, 200)
-    assert wide == 256 + 148 * 512 * 8 + 148 * 512 * 128 * 4 + 1600 * 8 * 4 + 1600 * 4 * 128 * 2
+    assert wide == 256 + 148 * 512 * 8 + 148 * 512 * 128 * 4 + 1600 * 8 * 4 + (1600 + 64) * 4 * 128 * 2
     # 16 nodes of 5 heads fit one 128-row tile
     one = B.tree_attn_workspace_bytes(40, 8, 128, B.RPX_BF16, 16, 1, 16)
-    assert one == 256 + 148 * 256 * 8 + 148 * 256 * 128 * 4 + 16 * 4 * 4 + 16 * 8 * 128 * 2
+    assert one == 256 + 148 * 256 * 8 + 148 * 256 * 128 * 4 + 16 * 4 * 4 + (16 + 8) * 8 * 128 * 2
     f32 = B.tree_attn_workspace_bytes(4, 2, 64, B.RPX_F32, 10, 2, 5)
     assert f32 == 256 + 256  # the attention call's piece, and 10 sets of 4 words
     assert B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 0, 8, 8) == 0
