@@ -103,30 +103,6 @@ rpx_status_t check_arch() {
     return major == 10 ? RPX_OK : RPX_ERR_ARCH;
 }
 
-rpx_status_t allow_smem(const void* kernel, size_t bytes) {
-    // a small table of (kernel, device) pairs already asked for; each kernel always asks for the same size
-    struct Seen {
-        std::atomic<const void*> kernel{nullptr};
-        std::atomic<uint64_t> devices{0};
-    };
-    static Seen seen[32];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return RPX_ERR_CUDA;
-    Seen* mine = nullptr;
-    for (Seen& s : seen) {
-        const void* k = s.kernel.load(std::memory_order_acquire);
-        if (k == nullptr && s.kernel.compare_exchange_strong(k, kernel, std::memory_order_acq_rel)) k = kernel;
-        if (k == kernel) {
-            mine = &s;
-            break;
-        }
-    }
-    if (mine != nullptr && dev < 64 && ((mine->devices.load(std::memory_order_acquire) >> dev) & 1u) != 0u) return RPX_OK;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return RPX_ERR_CUDA;
-    if (mine != nullptr && dev < 64) mine->devices.fetch_or(1ull << dev, std::memory_order_acq_rel);
-    return RPX_OK;
-}
-
 rpx_status_t launch_cast_f32_bf16(const float* src, int64_t src_row_stride, __nv_bfloat16_raw* dst, int64_t rows,
                                   int64_t cols, cudaStream_t stream) {
     const int64_t total = rows * cols;

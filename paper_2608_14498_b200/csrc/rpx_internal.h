@@ -23,8 +23,6 @@ void set_sm_budget(int sms);
 int lm_head_pairing();          // process-wide: 1 = the LM head runs its CTA-pair (cta_group::2) kernel
 void set_lm_head_pairing(int on);
 rpx_status_t check_arch();      // RPX_OK on compute capability 10.x
-// Lets a kernel use `bytes` of dynamic shared memory on the current device; asked of the runtime once per kernel and device.
-rpx_status_t allow_smem(const void* kernel, size_t bytes);
 
 // f32 -> bf16 (round to nearest even) of `rows` rows of `cols` contiguous elements.
 rpx_status_t launch_cast_f32_bf16(const float* src, int64_t src_row_stride, __nv_bfloat16_raw* dst, int64_t rows,

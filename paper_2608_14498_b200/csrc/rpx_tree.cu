@@ -387,7 +387,8 @@ rpx_status_t launch_stream(const TreeArgs& a, const CUtensorMap& tk, const CUten
     using L = Layout<D>;
     using Cut = RowCut<16 * kRowTiles>;
     auto* kernel = tree_stream_kernel<D, kRowTiles>;
-    if (rpx_status_t rc = allow_smem(reinterpret_cast<const void*>(kernel), L::kSmemBytes)) return rc;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess)
+        return RPX_ERR_CUDA;
     carve_workspace<Cut>(p, a.workspace);
     const int64_t whole = whole_grid<Cut>(p, a.max_cached);
     kernel<<<static_cast<unsigned>(whole > 0 ? whole : p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);

@@ -651,7 +651,7 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* va
     constexpr size_t smem = L::kCtlOff + sizeof(Ctl);
     static_assert(smem <= 232448, "shared memory of one CTA");
     auto* kernel = tree_tile_kernel<D, kPaired>;
-    if (rpx_status_t rc = allow_smem(reinterpret_cast<const void*>(kernel), smem)) return rc;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return RPX_ERR_CUDA;
     const int64_t whole = whole_grid<Cut>(p, a.max_cached);
     if (rpx_status_t rc = launch_on_top(kernel, static_cast<unsigned>(whole > 0 ? whole : p.ctas), kThreads, smem, a.stream, tq, tk, tv, tkc, tvc, p))
         return rc;
