@@ -48,7 +48,7 @@ struct Params {
 // first unit.  All blocks but a sequence's last have the same weight.
 template <int kRows_>
 struct RowCut {  // blocks of kRows rows, row = node * group + head within the KV head's group
-    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 2, kWholeTiles = 12;
+    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 2, kWholeTiles = kRows_ == 64 ? 3 : 6;
     static __device__ __forceinline__ int32_t weight(const Params&, int32_t, int32_t) { return 1; }
     static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) { return (n * p.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ void place(const Params& p, int32_t node, int32_t h, int32_t* block, int32_t* row) {
@@ -59,7 +59,7 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
 };
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
-    static constexpr int kTile = 128, kRows = 128 * kTiles, kWholeTiles = 6;
+    static constexpr int kTile = 128, kRows = 128 * kTiles, kWholeTiles = 8;
     // a key tile against two query tiles takes about 3500 clocks, against one 2600
     static constexpr int kPairWeight = 4, kOneWeight = 3;
     static constexpr int kMinUnits = kTiles == 1 ? 2 : 2 * kPairWeight;
@@ -408,8 +408,9 @@ inline void carve_workspace(Params& p, void* workspace) {
     p.part_o = reinterpret_cast<float*>(ws);
 }
 
-// Short sequences are not cut: one CTA walks a segment of up to kWholeTiles key tiles in less time than the join takes.  Goes
-// by the caller's bound; a longer sequence is only slower.  Returns the grid (and sets whole_blocks), or 0.
+// Short sequences are not cut: one CTA walks a segment of up to kWholeTiles key tiles in less time than cutting and joining
+// take (4 x 1 nodes, streaming: 200 cached tokens 8.4 us whole and 10.0 cut, 400: 10.9 and 8.8; 2 x 16 nodes, tensor cores:
+// 700 tokens 19.0 and 22.4, 1100: 23.2 and 19.0).  Goes by the caller's bound; a longer sequence is only slower.  Returns the grid (and sets whole_blocks), or 0.
 template <class Cut>
 inline int64_t whole_grid(Params& p, int32_t max_cached) {
     const int64_t tiles = (static_cast<int64_t>(max_cached) + Cut::kTile - 1) / Cut::kTile + (p.max_tree + Cut::kTile - 1) / Cut::kTile;
