@@ -44,11 +44,12 @@ struct Params {
 };
 
 // How a form cuts: keys per tile, rows of a block (in the workspace), blocks of a sequence, a row's place in its block, and
-// the weight of a block's key tiles: the line is measured in units of these, and a tile belongs to the piece that holds its
-// first unit.  All blocks but a sequence's last have the same weight.
+// the weight of a block's key tiles: the line is measured in units of these, with kSegment units in front of every segment
+// for going over to it (its Q, the outputs of the one before), and a tile belongs to the piece that holds its first unit.
+// All blocks but a sequence's last have the same weight.
 template <int kRows_>
 struct RowCut {  // blocks of kRows rows, row = node * group + head within the KV head's group
-    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 2, kWholeTiles = kRows_ == 64 ? 3 : 6;
+    static constexpr int kTile = 64, kRows = kRows_, kMinUnits = 3, kSegment = 1, kWholeTiles = kRows_ == 64 ? 3 : 6;
     static __device__ __forceinline__ int32_t weight(const Params&, int32_t, int32_t) { return 1; }
     static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) { return (n * p.group + kRows - 1) / kRows; }
     static __device__ __forceinline__ void place(const Params& p, int32_t node, int32_t h, int32_t* block, int32_t* row) {
@@ -60,11 +61,12 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
     static constexpr int kTile = 128, kRows = 128 * kTiles, kWholeTiles = 8;
-    // a key tile against two query tiles takes about 3500 clocks, against one 2600
-    static constexpr int kPairWeight = 4, kOneWeight = 3;
-    static constexpr int kMinUnits = kTiles == 1 ? 2 : 2 * kPairWeight;
+    // by a fit over the CTAs of a ragged batch, a key tile against two query tiles takes 2.15 us, against one 1.65, and going
+    // over to another segment about as long as two tiles
+    static constexpr int kPairWeight = 4, kOneWeight = 3, kSegment = 7;
+    static constexpr int kMinUnits = kSegment + 2 * (kTiles == 1 ? kOneWeight : kPairWeight);
     static __device__ __forceinline__ int32_t weight(const Params& p, int32_t n, int32_t block) {
-        if (kTiles == 1) return 1;
+        if (kTiles == 1) return kOneWeight;
         return n - block * kTiles * p.tile_nodes > p.tile_nodes ? kPairWeight : kOneWeight;
     }
     static __host__ __device__ __forceinline__ int32_t blocks(const Params& p, int32_t n) {
@@ -82,21 +84,40 @@ struct Seq {
     int32_t cached_tiles, tiles;  // key tiles of one segment: cached ones, then the tree's own
     int32_t blocks;               // row blocks
     int32_t weight, last_weight;  // of the key tiles of all blocks but the last, and of the last
-    __device__ __forceinline__ int64_t head_work() const {
-        return static_cast<int64_t>(tiles) * (static_cast<int64_t>(blocks - 1) * weight + last_weight);
-    }
-    __device__ __forceinline__ int64_t work(const Params& p) const { return n > 0 ? head_work() * p.num_kv_heads : 0; }
     __device__ __forceinline__ int32_t block_weight(int32_t block) const { return block + 1 < blocks ? weight : last_weight; }
 };
+
+// What is read of a sequence.
+struct SeqRaw {
+    int32_t begin, end, len;
+};
+__device__ __forceinline__ SeqRaw load_seq(const Params& p, int32_t s) { return SeqRaw{__ldg(p.cu + s), __ldg(p.cu + s + 1), __ldg(p.lens + s)}; }
+
+// Units of a whole segment, of a head's segments, of a sequence.
+template <class Cut>
+__device__ __forceinline__ int64_t segment_units(const Seq& q, int32_t block) {
+    return static_cast<int64_t>(q.tiles) * q.block_weight(block) + Cut::kSegment;
+}
+template <class Cut>
+__device__ __forceinline__ int64_t head_units(const Seq& q) {
+    return (q.blocks - 1) * segment_units<Cut>(q, 0) + segment_units<Cut>(q, q.blocks - 1);
+}
+template <class Cut>
+__device__ __forceinline__ int64_t seq_units(const Params& p, const Seq& q) { return q.n > 0 ? head_units<Cut>(q) * p.num_kv_heads : 0; }
+// A tile's first unit, counted from the start of its segment.
+template <class Cut>
+__device__ __forceinline__ int64_t tile_unit(const Seq& q, int32_t block, int32_t tile) {
+    return Cut::kSegment + static_cast<int64_t>(tile) * q.block_weight(block);
+}
 
 // Offsets that leave the packed tensors or the block table, and a tree larger than the caller's bound, make a sequence
 // count as empty (its rows are left as they were) and are reported.
 template <class Cut>
-__device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* data_error) {
+__device__ __forceinline__ Seq make_seq(const Params& p, const SeqRaw& raw, uint32_t* data_error) {
     Seq q;
-    q.tok0 = __ldg(p.cu + s);
-    q.n = __ldg(p.cu + s + 1) - q.tok0;
-    q.len = __ldg(p.lens + s);
+    q.tok0 = raw.begin;
+    q.n = raw.end - raw.begin;
+    q.len = raw.len;
     const bool bad = q.tok0 < 0 || q.n < 0 || static_cast<int64_t>(q.tok0) + q.n > p.total_tokens || q.n > p.max_tree ||
                      (q.n > 0 && (q.len < 0 || (static_cast<int64_t>(q.len) + kPage - 1) / kPage > p.block_table_stride));
     if (bad) {
@@ -109,15 +130,19 @@ __device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* da
     q.blocks = Cut::blocks(p, q.n);
     q.weight = Cut::weight(p, q.n, 0);
     q.last_weight = q.n > 0 ? Cut::weight(p, q.n, q.blocks - 1) : q.weight;
-    if (q.work(p) > INT32_MAX) {  // beyond any memory; the walk counts a sequence's units in 32 bits
+    if (seq_units<Cut>(p, q) > INT32_MAX) {  // beyond any memory; the walk counts a sequence's units in 32 bits
         if (data_error != nullptr) *data_error = 1;
         q.n = q.len = q.cached_tiles = q.tiles = q.blocks = 0;
     }
     return q;
 }
+template <class Cut>
+__device__ __forceinline__ Seq read_seq(const Params& p, int32_t s, uint32_t* data_error) {
+    return make_seq<Cut>(p, load_seq(p, s), data_error);
+}
 
-// The line of `total` units is cut into pieces of piece_units() units (the last ones may be short or empty; none is shorter
-// than a tile's weight otherwise, so each of a segment's pieces holds a tile).
+// The line of `total` units is cut into pieces of piece_units() units (the last ones may be short or empty; none is
+// otherwise shorter than a tile's weight, so every piece between a segment's first and last holds a tile).
 template <class Cut>
 __device__ __forceinline__ int64_t piece_units(int64_t total, int32_t ctas) {
     const int64_t even = (total >> 31) == 0 ? (static_cast<uint32_t>(total) + ctas - 1u) / static_cast<uint32_t>(ctas) : (total + ctas - 1) / ctas;
@@ -154,14 +179,14 @@ __device__ __forceinline__ Piece find_piece(const Params& p, uint32_t* data_erro
         const Seq q = read_seq<Cut>(p, s, i == 0 ? data_error : nullptr);
         if (q.n > 0 && block < q.blocks) {
             piece.seq = s;
-            piece.off = static_cast<int32_t>(head * q.head_work()) + block * q.tiles * q.weight;
-            piece.units = q.tiles * q.block_weight(block);
+            piece.off = static_cast<int32_t>(head * head_units<Cut>(q) + block * segment_units<Cut>(q, 0));
+            piece.units = static_cast<int32_t>(segment_units<Cut>(q, block));
         }
         return piece;
     }
     int64_t total = 0, first_work = 0, first_sum = 0;
     for (int32_t base = 0; base < p.batch; base += 32) {
-        const int64_t w = base + lane < p.batch ? read_seq<Cut>(p, base + lane, scribe ? data_error : nullptr).work(p) : 0;
+        const int64_t w = base + lane < p.batch ? seq_units<Cut>(p, read_seq<Cut>(p, base + lane, scribe ? data_error : nullptr)) : 0;
         const int64_t sum = total + warp_scan(w, lane);
         if (base == 0) {
             first_work = w;
@@ -175,7 +200,7 @@ __device__ __forceinline__ Piece find_piece(const Params& p, uint32_t* data_erro
     for (int32_t base = 0; base < p.batch; base += 32) {
         int64_t w = first_work, sum = first_sum;
         if (base > 0) {
-            w = base + lane < p.batch ? read_seq<Cut>(p, base + lane, nullptr).work(p) : 0;
+            w = base + lane < p.batch ? seq_units<Cut>(p, read_seq<Cut>(p, base + lane, nullptr)) : 0;
             sum = carry + warp_scan(w, lane);
         }
         const int64_t before = sum - w;
@@ -198,19 +223,27 @@ __device__ __forceinline__ Piece find_piece(const Params& p, uint32_t* data_erro
 template <class Cut>
 struct Walk {
     int32_t s, head, block, t0, t1;  // current segment: sequence, KV head, row block, key tiles [t0, t1)
-    int32_t left;                    // units of the piece behind t1
+    int32_t left;                    // units of the piece behind t1's first
     Seq q;
-    __device__ __forceinline__ Walk(const Params& p, const Piece& piece) : s(piece.seq), head(0), block(0), t0(0), t1(0), left(piece.units), q() {
+    int32_t next_begin, next_end, next_len;  // the sequence behind, read a sequence ahead
+    __device__ __forceinline__ void look_ahead(const Params& p) {
+        next_end = s + 1 < p.batch ? __ldg(p.cu + s + 2) : 0;
+        next_len = s + 1 < p.batch ? __ldg(p.lens + s + 1) : 0;
+    }
+    __device__ __forceinline__ Walk(const Params& p, const Piece& piece) : s(piece.seq), head(0), block(0), t0(0), t1(0), left(piece.units), q(), next_begin(0), next_end(0), next_len(0) {
         if (left == 0) return;
-        q = read_seq<Cut>(p, s, nullptr);
-        const int32_t per_head = static_cast<int32_t>(q.head_work()), per_block = q.tiles * q.weight;
+        const SeqRaw raw = load_seq(p, s);
+        look_ahead(p);
+        q = make_seq<Cut>(p, raw, nullptr);
+        next_begin = raw.end;
+        const int32_t per_head = static_cast<int32_t>(head_units<Cut>(q)), per_block = static_cast<int32_t>(segment_units<Cut>(q, 0));
         head = piece.off / per_head;
         int32_t off = piece.off - head * per_head;
         block = min(off / per_block, q.blocks - 1);
         off -= block * per_block;
         const int32_t w = q.block_weight(block);
-        t1 = (off + w - 1) / w;
-        left -= t1 * w - off;
+        t1 = max(0, (off - Cut::kSegment + w - 1) / w);
+        left -= Cut::kSegment + t1 * w - off;
     }
     __device__ __forceinline__ bool next(const Params& p) {
         if (left <= 0) return false;
@@ -221,11 +254,16 @@ struct Walk {
                 if (++head == p.num_kv_heads) {
                     head = 0;
                     do {
-                        if (++s >= p.batch) return false;  // (not reached: the piece ends before the line does)
-                        q = read_seq<Cut>(p, s, nullptr);
+                        if (++s >= p.batch) return false;
+                        const SeqRaw raw = {next_begin, next_end, next_len};
+                        look_ahead(p);
+                        q = make_seq<Cut>(p, raw, nullptr);
+                        next_begin = raw.end;
                     } while (q.n == 0);
                 }
             }
+            left -= Cut::kSegment;
+            if (left <= 0) return false;  // not even the first tile starts in this piece
         }
         const int32_t w = q.block_weight(block);
         t0 = t1;
@@ -262,9 +300,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kSplit > 1 ? 2 : 4) tree_join
                 const int32_t node = (row_begin + k) / p.num_q_heads, head = row_begin + k - node * p.num_q_heads, kv_head = head / p.group;
                 int32_t block;
                 Cut::place(p, node, head - kv_head * p.group, &block, &row[k]);
-                const int64_t unit0 = seq0 + kv_head * q.head_work() + static_cast<int64_t>(block) * q.tiles * q.weight;
-                c0[k] = piece_of(unit0, size);
-                n[k] = piece_of(unit0 + static_cast<int64_t>(q.tiles - 1) * q.block_weight(block), size) - c0[k] + 1;
+                const int64_t unit0 = seq0 + kv_head * head_units<Cut>(q) + block * segment_units<Cut>(q, 0);
+                c0[k] = piece_of(unit0 + tile_unit<Cut>(q, block, 0), size);
+                n[k] = piece_of(unit0 + tile_unit<Cut>(q, block, q.tiles - 1), size) - c0[k] + 1;
                 if (n[k] == 1) n[k] = 0;  // written whole
                 most = max(most, n[k]);
             }

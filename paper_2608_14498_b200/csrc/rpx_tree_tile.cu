@@ -377,7 +377,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             const int32_t head = walk.head * p.group + (row - in_tile * p.group);
             // ---- ancestor set, where this piece reaches the tree's own keys
             const uint32_t* set = nullptr;
-            bool row_used = true;  // known to the pieces that hold the last tile, which is one of the tree's own
+            uint32_t own_word = ~0u;  // holds the node's own bit; looked at by the pieces with the last tile, one of the tree's own
             if (walk.t1 > q.cached_tiles) {
                 if (!have_sets) {
                     wait_for_sets();
@@ -385,7 +385,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 }
                 if (row_valid) {
                     set = p.sets + (static_cast<int64_t>(q.tok0) + node) * p.set_words;
-                    row_used = ((set[node >> 5] >> (node & 31)) & 1u) != 0u;
+                    own_word = set[node >> 5];
                 }
             }
             float run_max = -CUDART_INF_F, run_sum = 0.f;
@@ -540,7 +540,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             const uint32_t o_addr = tmem_base + 256 + (paired ? t * 128 : 0) + lane_addr;
             const int c_begin = paired || t == 0 ? 0 : D / 64, c_end = paired || t == 1 ? D / 32 : D / 64;
             const bool whole = walk.t0 == 0 && walk.t1 == q.tiles;
-            const bool unused = walk.t1 == q.tiles && !row_used;
+            const bool unused = walk.t1 == q.tiles && ((own_word >> (node & 31)) & 1u) == 0u;
             const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
             const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * Cut::kRows + (paired ? t * 128 : 0) + row;
             const float inv = 1.f / sum;
