@@ -39,7 +39,7 @@ struct Params {
     float* lse;            // nullable
     int64_t* seq_unit0;    // workspace [batch + 1]: number of the sequence's first unit; the last entry is the total
     float2* part_ml;       // workspace [ctas][2][rows per block]; a negative sum marks a node that is not in use
-    float* part_o;         // workspace [ctas][2][rows per block][D]
+    float* part_o;         // workspace [ctas][2][rows per block][D], each form in an order of its own (part_at)
     int32_t* status;
 };
 
@@ -57,6 +57,8 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
         *block = r / kRows;
         *row = r % kRows;
     }
+    template <int D>
+    static __device__ __forceinline__ int64_t part_at(int64_t row, int32_t col) { return row * D + col; }
 };
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
@@ -76,6 +78,12 @@ struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
         const int32_t tile = node / p.tile_nodes;
         *block = tile / kTiles;
         *row = (tile % kTiles) * 128 + (node - tile * p.tile_nodes) * p.group + h;
+    }
+    // [32 rows][8 columns of each], so that what the 32 lanes of a warp hold of their rows goes out as whole lines: with a row's
+    // columns in one run every store touched 32 lines, and the next load waited 4000 clocks behind them
+    template <int D>
+    static __device__ __forceinline__ int64_t part_at(int64_t row, int32_t col) {
+        return ((row >> 5) * (D / 8) + (col >> 3)) * 256 + (row & 31) * 8 + (col & 7);
     }
 };
 
@@ -331,9 +339,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kSplit > 1 ? 2 : 4) tree_join
                     const int64_t at = (static_cast<int64_t>(c0[k] + j) * 2 + (j == 0 ? 1 : 0)) * Cut::kRows + row[k];
                     ml[k] = p.part_ml[at];
                     if (kCols == 4) {
-                        v[k] = *reinterpret_cast<const float4*>(p.part_o + at * D + lane * kCols);
+                        v[k] = *reinterpret_cast<const float4*>(p.part_o + Cut::template part_at<D>(at, lane * kCols));
                     } else {
-                        const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + lane * kCols);
+                        const float2 x = *reinterpret_cast<const float2*>(p.part_o + Cut::template part_at<D>(at, lane * kCols));
                         v[k].x = x.x;
                         v[k].y = x.y;
                     }

@@ -60,6 +60,8 @@ struct Ctl {
     uint64_t drain;
     uint32_t tmem_base, abort_flag, drain_flag, data_error;
     float2 ml[2][kTile];
+    int32_t walk[8][20];  // the softmax warps' walks: in registers they spill, and local memory is hundreds of clocks away
+    int32_t more[8];
 };
 
 // Key tiles lie as [group of 8 keys][half][8 rows][128 bytes], swizzled: a 16-token page (two groups, both halves) is one
@@ -116,19 +118,20 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = ctl->tmem_base;  // S_t at columns 128 t, O_t at 256 + 128 t
-    Walk<Cut> walk(p, find_piece<Cut>(p, &ctl->data_error));
+    const Piece piece = find_piece<Cut>(p, &ctl->data_error);
     // Every role walks the piece's segments alike.  A block whose nodes fit one query tile lets the buffers take turns.
-    auto nodes_in_block = [&]() { return min(walk.q.n - walk.block * L::kQTiles * p.tile_nodes, L::kQTiles * p.tile_nodes); };
+    auto nodes_in_block = [&](const Walk<Cut>& walk) { return min(walk.q.n - walk.block * L::kQTiles * p.tile_nodes, L::kQTiles * p.tile_nodes); };
 
     if (warp == kProducerWarp) {
         // =========================================================== producer
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        Walk<Cut> walk(p, piece);
         bool ok = true, have_sets = false;
         uint32_t nk = 0, nv = 0, segments = 0;
         while (ok && walk.next(p)) {
             const Seq q = walk.q;
             const int32_t node0 = walk.block * L::kQTiles * p.tile_nodes;
-            const bool paired = kPaired && nodes_in_block() > p.tile_nodes;
+            const bool paired = kPaired && nodes_in_block(walk) > p.tile_nodes;
             if (segments > 0 && !mbar_wait(&ctl->q_empty, (segments - 1) & 1u, abort_flag)) {
                 ok = false;
                 break;
@@ -240,6 +243,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         // =========================================================== tcgen05 issuer (one thread)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (elect_one()) {
+            Walk<Cut> walk(p, piece);
             constexpr uint32_t idesc_qk = make_idesc_bf16(kTile, kTile, false, false);
             constexpr uint32_t idesc_pv = make_idesc_bf16(kTile, D, false, true);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem), 16, 1024);
@@ -279,7 +283,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             };
             while (ok && walk.next(p)) {
                 const int32_t n = walk.t1 - walk.t0;
-                const bool paired = kPaired && nodes_in_block() > p.tile_nodes;
+                const bool paired = kPaired && nodes_in_block(walk) > p.tile_nodes;
                 const bool two_terms = walk.q.tiles <= 2;
                 ok = mbar_wait(&ctl->q_full, segments & 1u, abort_flag);
                 if (paired) {
@@ -366,25 +370,32 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         uint32_t used[2] = {0, 0};       // segments in which each buffer took part
         uint32_t turns = 0;              // segments in which the buffers took turns
         bool ok = true, have_sets = false;
-        while (ok && walk.next(p)) {
-            const Seq q = walk.q;
-            const int32_t n = walk.t1 - walk.t0;
-            const bool paired = kPaired && nodes_in_block() > p.tile_nodes;
-            const bool two_terms = q.tiles <= 2;
+        static_assert(sizeof(Walk<Cut>) <= sizeof(ctl->walk[0]), "room for a walk");
+        Walk<Cut>& walk = *reinterpret_cast<Walk<Cut>*>(ctl->walk[warp]);
+        if (lane == 0) walk = Walk<Cut>(p, piece);
+        while (ok) {
+            __syncwarp();  // the segment before has been read
+            if (lane == 0) ctl->more[warp] = walk.next(p) ? 1 : 0;
+            __syncwarp();
+            if (ctl->more[warp] == 0) break;
+            const int32_t tok0 = walk.q.tok0, len = walk.q.len, cached_tiles = walk.q.cached_tiles, t0 = walk.t0, n = walk.t1 - walk.t0;
+            const bool has_last = walk.t1 == walk.q.tiles, whole = has_last && t0 == 0;
+            const bool paired = kPaired && nodes_in_block(walk) > p.tile_nodes;
+            const bool two_terms = walk.q.tiles <= 2;
             const int32_t in_tile = row / p.group;  // rows beyond tile_nodes * group are padding
             const int32_t node = walk.block * L::kQTiles * p.tile_nodes + (paired ? t * p.tile_nodes : 0) + in_tile;
-            const bool row_valid = in_tile < p.tile_nodes && node < q.n;
+            const bool row_valid = in_tile < p.tile_nodes && node < walk.q.n;
             const int32_t head = walk.head * p.group + (row - in_tile * p.group);
             // ---- ancestor set, where this piece reaches the tree's own keys
             const uint32_t* set = nullptr;
             uint32_t own_word = ~0u;  // holds the node's own bit; looked at by the pieces with the last tile, one of the tree's own
-            if (walk.t1 > q.cached_tiles) {
+            if (t0 + n > cached_tiles) {
                 if (!have_sets) {
                     wait_for_sets();
                     have_sets = true;
                 }
                 if (row_valid) {
-                    set = p.sets + (static_cast<int64_t>(q.tok0) + node) * p.set_words;
+                    set = p.sets + (static_cast<int64_t>(tok0) + node) * p.set_words;
                     own_word = set[node >> 5];
                 }
             }
@@ -404,18 +415,18 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(my_s + c * 32, sc[c]);
                 tmem_ld_wait();
-                const int32_t tile = walk.t0 + j;
-                if (tile >= q.cached_tiles) {
+                const int32_t tile = t0 + j;
+                if (tile >= cached_tiles) {
                     uint4 m = make_uint4(0u, 0u, 0u, 0u);
-                    if (set != nullptr) m = reinterpret_cast<const uint4*>(set)[tile - q.cached_tiles];
+                    if (set != nullptr) m = reinterpret_cast<const uint4*>(set)[tile - cached_tiles];
                     const uint32_t bits[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (((bits[c] >> i) & 1u) == 0u) sc[c][i] = 0xff800000u;  // -inf
-                } else if (q.len - tile * kTile < kTile) {
-                    const int32_t keys = q.len - tile * kTile;
+                } else if (len - tile * kTile < kTile) {
+                    const int32_t keys = len - tile * kTile;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -539,10 +550,9 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             const bool adds = !paired && with_1;
             const uint32_t o_addr = tmem_base + 256 + (paired ? t * 128 : 0) + lane_addr;
             const int c_begin = paired || t == 0 ? 0 : D / 64, c_end = paired || t == 1 ? D / 32 : D / 64;
-            const bool whole = walk.t0 == 0 && walk.t1 == q.tiles;
-            const bool unused = walk.t1 == q.tiles && ((own_word >> (node & 31)) & 1u) == 0u;
-            const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + head;
-            const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * Cut::kRows + (paired ? t * 128 : 0) + row;
+            const bool unused = has_last && ((own_word >> (node & 31)) & 1u) == 0u;
+            const int64_t out_row = (static_cast<int64_t>(tok0) + node) * p.num_q_heads + head;
+            const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (t0 == 0 ? 1 : 0)) * Cut::kRows + (paired ? t * 128 : 0) + row;
             const float inv = 1.f / sum;
             const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0u;
 #pragma unroll 1
@@ -569,8 +579,13 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     for (int i = 0; i < 32; ++i)
                         a[i] = __float_as_uint(fmaf(f0, __uint_as_float(a[i]), f1 * __uint_as_float(b[i])));
                 }
-                if (!row_valid) continue;
-                if (whole) {
+                if (!whole) {  // (rows that are padding go along: they are nobody's)
+                    float* dst = p.part_o + Cut::template part_at<D>(slot, c * 32);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        st_global_v8(dst + 256 * i, a[8 * i], a[8 * i + 1], a[8 * i + 2], a[8 * i + 3], a[8 * i + 4], a[8 * i + 5],
+                                     a[8 * i + 6], a[8 * i + 7]);
+                } else if (row_valid) {
                     uint32_t w[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
@@ -584,12 +599,6 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         for (int i = 0; i < 4; ++i)
                             reinterpret_cast<uint4*>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                     }
-                } else {
-                    float* dst = p.part_o + slot * D + c * 32;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        st_global_v8(dst + 8 * i, a[8 * i], a[8 * i + 1], a[8 * i + 2], a[8 * i + 3], a[8 * i + 4], a[8 * i + 5],
-                                     a[8 * i + 6], a[8 * i + 7]);
                 }
             }
             if (row_valid && (paired || t == 0)) {
