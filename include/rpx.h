@@ -425,7 +425,7 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *   desc->pair_axis: HOST array of rot_dim / 2 axis numbers < num_axes (1 .. 8), or NULL: every pair takes axis 0
  *   q [n_tokens][num_q_heads][head_dim], k [n_tokens][num_kv_heads][head_dim] with token strides in elements, such as
  *       views of one fused projection; q_weight, k_weight: element type of q and k, both or neither NULL
- *   positions device int32 [num_axes][pos_axis_stride], pos_axis_stride >= n_tokens; inv_freq device float32 [rot_dim / 2]
+ *   positions device int32 [num_axes][pos_axis_stride], pos_axis_stride >= n_tokens, or 0: one row for all axes; inv_freq device float32 [rot_dim / 2]
  *   q_out, k_out with token strides; each may be its input itself (same pointer and stride), otherwise no output
  *       overlaps an input or the other output
  */

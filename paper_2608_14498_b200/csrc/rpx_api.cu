@@ -478,7 +478,7 @@ rpx_status_t check_rope(const RopeArgs& a) {
     const int64_t q_row = static_cast<int64_t>(d->num_q_heads) * d->head_dim;
     const int64_t kv_row = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
     if (a.q_tok_stride < q_row || a.k_tok_stride < kv_row || a.q_out_tok_stride < q_row || a.k_out_tok_stride < kv_row ||
-        a.pos_axis_stride < a.n_tokens)
+        (a.pos_axis_stride != 0 && a.pos_axis_stride < a.n_tokens))
         return RPX_ERR_SHAPE;
     if (a.q_tok_stride % 8 || a.k_tok_stride % 8 || a.q_out_tok_stride % 8 || a.k_out_tok_stride % 8) return RPX_ERR_ALIGN;
     if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.q_weight) || !aligned16(a.k_weight) || !aligned16(a.q_out) ||

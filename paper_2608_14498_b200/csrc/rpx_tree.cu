@@ -508,9 +508,10 @@ rpx_status_t launch_tree_sets(const TreeArgs& a, uint32_t* sets, void* v_copy) {
     return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
 }
 
-// The streaming form is bound by reading the cache up to 32 rows per block (94 % of that bound at 15 rows, 80 % at 30,
-// 8192 cached tokens); 64-row blocks are bound by mma.sync (41 us against 13 % of it for 56 rows over 8 x 4096 tokens), and
-// the tensor-core form is faster from there on.  It takes trees of any size but groups of at most 128 heads.
+// The streaming form reads the cache at 95 % of the copy rate with one row tile (32 x 3 nodes of 5 heads over 8192 tokens: 173
+// us) and 82 % with two (32 x 6 nodes: 200 us); with four, mma.sync bounds it, and the tensor-core form is faster at every
+// length (2 x 8 nodes of 7 heads over 600 tokens 17 us against 35, 8 x 16 over 1000 22 against 32).  That one takes trees of
+// any size, but groups of at most 128 heads.
 bool tree_streams(int32_t max_tree, int32_t group) {
     return max_tree <= kMaxNodes && (static_cast<int64_t>(max_tree) * group <= 32 || group > 128);
 }

@@ -3,19 +3,21 @@
 // Same mathematics and the same cut as the streaming form (rpx_tree.cuh), with 128-key tiles and tcgen05.  A query tile is
 // tile_nodes = 128 / group nodes times the query heads of one KV head (row = node * group + head), so a key tile is
 // fetched once for all of them.  A block holds one query tile, or two where trees need more rows (kPaired).  Per 128 keys
-// a query tile costs 1024 clocks of tensor pipe, 1024 of exponentials and the tile itself 64 KB, about 2800 clocks of this
-// SM's share of HBM: with one or two query tiles the cache's bytes bound, provided that the softmax of one step hides
-// behind the products of another.  So there are always two score buffers in flight:
+// a query tile costs 1024 clocks of tensor pipe, 768 of exponentials, and the tile itself 64 KB, 1.48 us (2500 clocks) of this
+// SM's share of HBM: with one query tile the cache's bytes bound, provided that the softmax of one step hides behind the
+// products of another.  So there are always two score buffers in flight:
 //   two query tiles  the buffers are the query tiles, both walk every key tile;
 //   one query tile   the buffers take turns: buffer t walks the key tiles t, t + 2, .. with a running maximum, sum and
 //                    output of its own, and both buffers' warps add the two up straight out of TMEM at the end.
+// Measured by a fit over the CTAs: a key tile against one query tile 1.6 us (the bytes: 1.48), against two 2.15 us (their
+// chain of product, softmax and product), going over to another segment 4 us.
 //   warps 0-3, 4-7 : softmax of buffer 0, 1: thread = row = TMEM lane
 //   warp  8        : producer: Q once per segment, K and V through rings of their own (K runs a tile ahead, so it is not
 //                    held up behind a V slot), one TMA box per 16-token page
 //   warp  9        : issues S_t = Q K^T (smem x smem -> TMEM) and O_t += P_t V (P as bf16 over S_t's first 64 columns)
 //   warps 10, 11   : only take part in the register hand-over
-// The tree's own V tiles come from a copy in which rows of unused nodes are zero (and no other sequence's rows follow), and ancestor sets as bit masks; a small
-// kernel writes both (tree_sets_kernel).  This kernel is launched on top of that one and waits for it only where it first
+// The tree's own V tiles come from a copy in which rows of unused nodes are zero (and no other sequence's rows follow), and
+// ancestor sets as bit masks; a small kernel writes both (tree_sets_kernel).  This kernel is launched on top of that one and waits for it only where it first
 // needs its results, behind the cached tiles.
 #include <type_traits>
 

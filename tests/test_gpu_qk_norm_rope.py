@@ -159,6 +159,30 @@ def test_far_positions(cuda_device, dtype):
     close(out, ref, HALF_STEP[dtype] * ref.abs() + 2.0 ** -18 * size, "far positions")
 
 
+def test_one_row_of_positions_for_all_axes(cuda_device):
+    q, k, pos, inv, axis, w = make(20, 4, 2, 64, 64, 3, "bf16", True, cuda_device)
+    want = rpx.qk_norm_rope(q, k, pos[:1].repeat(3, 1), inv, w[0], w[1], axis)
+    got = rpx.qk_norm_rope(q, k, pos[0].expand(3, -1), inv, w[0], w[1], axis)
+    also = rpx.qk_norm_rope(q, k, pos[0], inv, w[0], w[1])  # text: one axis
+    for x in (got, also):
+        assert torch.equal(x[0], want[0]) and torch.equal(x[1], want[1])
+
+
+def test_unaligned_float32_rows(cuda_device):
+    """float32 tensors that start on 16 bytes only take the narrower accesses and give the same bits."""
+    q, k, pos, inv, axis, w = make(30, 4, 2, 64, 64, 1, "f32", True, cuda_device)
+    dq, dk = torch.randn(30, 4, 64, device=cuda_device), torch.randn(30, 2, 64, device=cuda_device)
+    room = torch.zeros(30 * 4 * 64 + 4, device=cuda_device)
+    q2 = room[4:].view(30, 4, 64)
+    q2.copy_(q)
+    assert q2.data_ptr() % 32 == 16
+    q = q.contiguous()
+    assert all(torch.equal(a, b) for a, b in zip(rpx.qk_norm_rope(q2, k, pos, inv, w[0], w[1], axis),
+                                                 rpx.qk_norm_rope(q, k, pos, inv, w[0], w[1], axis)))
+    assert all(torch.equal(a, b) for a, b in zip(rpx.qk_norm_rope_backward(q2, k, dq, dk, pos, inv, w[0], w[1], axis),
+                                                 rpx.qk_norm_rope_backward(q, k, dq, dk, pos, inv, w[0], w[1], axis)))
+
+
 def test_in_place_strided_and_padded(cuda_device):
     q, k, pos, inv, axis, w = make(50, 6, 2, 128, 96, 3, "bf16", True, cuda_device, extra=24)
     base = q._base if q._base is not None else q
