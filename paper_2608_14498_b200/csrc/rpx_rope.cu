@@ -12,6 +12,9 @@
 // pairs up (p and p + rot/16; beyond rot two neighbours), so neither half ever moves between lanes and the only
 // exchange is the sum of squares.  A warp keeps one token: its rot/2 angles are computed once, two per lane, and read
 // back from shared memory as the lane's eight (cos, sin) pairs for all of the token's heads.
+//
+// Measured with 28 + 4 heads of 128, bf16, inputs beyond L2: forward of 32768 tokens 86 us, backward of 34816 tokens 183 us,
+// both 95 % of the copy bandwidth.  float32 forward of 8192 tokens 48 us, 86 %.
 #include <cuda_bf16.h>
 
 #include "rpx_internal.h"
@@ -61,28 +64,27 @@ struct Bf16 {
     typedef uint4 Raw;  // 8 elements
     static __device__ __forceinline__ Raw load(const Elem* p, bool) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
     static __device__ __forceinline__ Raw zero() { return make_uint4(0u, 0u, 0u, 0u); }
-    static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
+    static __device__ __forceinline__ void unpack(const Raw& r, uint64_t (&x)[4]) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) x[i] = f2_pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
     // the one rounding of the pass: results to bf16, nearest-even
-    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8], bool) {
+    static __device__ __forceinline__ void store(Elem* p, const uint64_t (&x)[4], bool) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&v);
+            float lo, hi;
+            f2_unpack(x[i], lo, hi);
+            w[i] = pack_bf16x2(lo, hi);
         }
         __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
     }
 };
 
 // A lane's eight floats are one 32-byte access: as two of 16 bytes, every request of a warp would touch all of its sectors
-// by halves, and the L1's request rate would bound the backward pass (79 % busy at 215 us per 34816 tokens).
+// by halves, and the L1's request rate would bound the backward pass (it was 79 % busy when measured so, at 215 us for
+// 34816 tokens of 28 + 4 heads of 128; see the top for what the pass takes now).
 struct F32 {
     typedef float Elem;
     struct Raw { float v[8]; };
@@ -98,11 +100,14 @@ struct F32 {
         return r;
     }
     static __device__ __forceinline__ Raw zero() { return Raw{{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}}; }
-    static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) {
+    static __device__ __forceinline__ void unpack(const Raw& r, uint64_t (&x)[4]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = r.v[i];
+        for (int i = 0; i < 4; ++i) x[i] = f2_pack(r.v[2 * i], r.v[2 * i + 1]);
     }
-    static __device__ __forceinline__ void store(Elem* p, const float (&x)[8], bool wide) {
+    static __device__ __forceinline__ void store(Elem* p, const uint64_t (&packed)[4], bool wide) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f2_unpack(packed[i], x[2 * i], x[2 * i + 1]);
         if (wide) {
             st_global_v8(p, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]),
                          __float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
@@ -137,29 +142,41 @@ struct LaneMap {
     }
 };
 
-// A lane's eight (cos, sin) pairs, and a chunk of eight weights, out of shared memory.
-__device__ __forceinline__ void read_angles(const float2* cs, int chunk, float (&c)[8], float (&s)[8]) {
+// All arithmetic runs on packed pairs of floats, one instruction for two: the backward pass was short of issue slots
+// (207 us with single floats, 183 with pairs).
+__device__ __forceinline__ uint64_t f2_negate(uint64_t x) { return x ^ 0x8000000080000000ull; }
+__device__ __forceinline__ float f2_sum(uint64_t x) {
+    float lo, hi;
+    f2_unpack(x, lo, hi);
+    return lo + hi;
+}
+
+// A lane's eight cosines and sines, and a chunk of eight weights, out of shared memory.
+__device__ __forceinline__ void read_angles(const float2* cs, int chunk, uint64_t (&c)[4], uint64_t (&s)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float4 w = *reinterpret_cast<const float4*>(cs + i * (kMaxPairs / 4) + chunk * 2);
-        c[2 * i] = w.x; s[2 * i] = w.y; c[2 * i + 1] = w.z; s[2 * i + 1] = w.w;
+        c[i] = f2_pack(w.x, w.z);
+        s[i] = f2_pack(w.y, w.w);
     }
 }
 template <int D>
-__device__ __forceinline__ void read_weights(const float* w, int chunk, float (&x)[8]) {  // [half of a chunk][chunk][4]
+__device__ __forceinline__ void read_weights(const float* w, int chunk, uint64_t (&x)[4]) {  // [half of a chunk][chunk][4]
     const float4 u = *reinterpret_cast<const float4*>(w + chunk * 4), v = *reinterpret_cast<const float4*>(w + D / 2 + chunk * 4);
-    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-    x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+    x[0] = f2_pack(u.x, u.y);
+    x[1] = f2_pack(u.z, u.w);
+    x[2] = f2_pack(v.x, v.y);
+    x[3] = f2_pack(v.z, v.w);
 }
 
 // The weights as float32 in shared memory; called by the whole block, ends with a barrier.
 template <class T, int D>
 __device__ __forceinline__ void stage_weights(const Params& p, float (*w)[D]) {
     for (int i = threadIdx.x; i < 2 * D / 8; i += kWarps * 32) {
-        float x[8];
+        uint64_t x[4];
         T::unpack(T::load(static_cast<const typename T::Elem*>(i < D / 8 ? p.q_weight : p.k_weight) + (i % (D / 8)) * 8, false), x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[i / (D / 8)][(e >> 2) * (D / 2) + (i % (D / 8)) * 4 + (e & 3)] = x[e];
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint64_t*>(&w[i / (D / 8)][(e >> 1) * (D / 2) + (i % (D / 8)) * 4 + 2 * (e & 1)]) = x[e];
     }
     __syncthreads();
 }
@@ -197,7 +214,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
     if (u_begin < u_end) token_angles(p, token, lane, cs_all[warp]);
     if (kNorm) stage_weights<T, D>(p, weight);
     if (u_begin >= u_end) return;
-    float c[8], s[8];
+    uint64_t c[4], s[4];
     if (map.turned) read_angles(cs_all[warp], map.off_a >> 3, c, s);
 
     for (int32_t u0 = u_begin; u0 < u_end; u0 += kUnroll) {
@@ -207,28 +224,32 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
             if (u0 + i >= u_end) break;
             const bool is_q = u0 + i < p.units_q;
             const int32_t head = (u0 + i - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
-            float a[8], b[8];
+            uint64_t a[4], b[4];
             T::unpack(now[i][0], a);
             T::unpack(now[i][1], b);
             if (kNorm) {
-                float ss = 0.f;
+                uint64_t ss = 0ull, st = 0ull;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
-                const float r = rsqrtf(row_sum<Map::kLanes>(ss) * (1.f / D) + p.eps);
-                float w[8];
+                for (int e = 0; e < 4; ++e) {
+                    ss = f2_fma(a[e], a[e], ss);
+                    st = f2_fma(b[e], b[e], st);
+                }
+                const float r = rsqrtf(row_sum<Map::kLanes>(f2_sum(f2_add(ss, st))) * (1.f / D) + p.eps);
+                const uint64_t r2 = f2_pack(r, r);
+                uint64_t w[4];
                 read_weights<D>(weight[is_q ? 0 : 1], map.off_a >> 3, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = a[e] * r * w[e];
+                for (int e = 0; e < 4; ++e) a[e] = f2_mul(f2_mul(a[e], r2), w[e]);
                 read_weights<D>(weight[is_q ? 0 : 1], map.off_b >> 3, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) b[e] = b[e] * r * w[e];
+                for (int e = 0; e < 4; ++e) b[e] = f2_mul(f2_mul(b[e], r2), w[e]);
             }
             if (map.turned) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = a[e], y = b[e];
-                    a[e] = fmaf(x, c[e], -y * s[e]);
-                    b[e] = fmaf(y, c[e], x * s[e]);
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t x = a[e], y = b[e];
+                    a[e] = f2_fma(x, c[e], f2_negate(f2_mul(y, s[e])));
+                    b[e] = f2_fma(y, c[e], f2_mul(x, s[e]));
                 }
             }
             if (head < (is_q ? p.num_q_heads : p.num_kv_heads)) {
@@ -254,16 +275,16 @@ __global__ void __launch_bounds__(kWarps * 32, 4) qk_rope_bwd_kernel(const __gri
     typedef typename T::Elem Elem;
     __shared__ __align__(16) float2 cs_all[kWarps][kMaxPairs];
     __shared__ __align__(16) float weight[kNorm ? 2 : 1][D];
-    __shared__ float4 dwk_all[kNorm ? kWarps : 1][4][32];  // [warp][quarter of the lane's 16 values][lane]
+    __shared__ ulonglong2 dwk_all[kNorm ? kWarps : 1][4][32];  // [warp][quarter of the lane's 16 values][lane]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Map map(lane, p.rot);
     const int64_t n_tasks = p.n_tokens * p.warps_per_token;
-    float dwq[2][8];
+    uint64_t dwq[2][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dwq[0][i] = dwq[1][i] = 0.f;
+    for (int i = 0; i < 4; ++i) dwq[0][i] = dwq[1][i] = 0ull;
     if (kNorm) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dwk_all[warp][i][lane] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < 4; ++i) dwk_all[warp][i][lane] = make_ulonglong2(0ull, 0ull);
         stage_weights<T, D>(p, weight);
     }
     for (int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp; task < n_tasks;
@@ -300,62 +321,68 @@ __global__ void __launch_bounds__(kWarps * 32, 4) qk_rope_bwd_kernel(const __gri
             const bool is_q = u < p.units_q;
             const int32_t head = (u - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
             const bool there = head < (is_q ? p.num_q_heads : p.num_kv_heads);
-            float g[8], h[8];
+            uint64_t g[4], h[4];
             F32::unpack(now.g[0], g);
             F32::unpack(now.g[1], h);
             if (map.turned) {
-                float c[8], s[8];
+                uint64_t c[4], s[4];
                 read_angles(cs_all[warp], map.off_a >> 3, c, s);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x = g[i], y = h[i];
-                    g[i] = fmaf(x, c[i], y * s[i]);
-                    h[i] = fmaf(y, c[i], -x * s[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t x = g[i], y = h[i];
+                    g[i] = f2_fma(x, c[i], f2_mul(y, s[i]));
+                    h[i] = f2_fma(y, c[i], f2_negate(f2_mul(x, s[i])));
                 }
             }
             if (kNorm) {
-                float a[8], b[8], wa[8], wb[8];
+                uint64_t a[4], b[4], gw[4], hw[4];
                 T::unpack(now.x[0], a);
                 T::unpack(now.x[1], b);
-                read_weights<D>(weight[is_q ? 0 : 1], map.off_a >> 3, wa);
-                read_weights<D>(weight[is_q ? 0 : 1], map.off_b >> 3, wb);
-                float ss = 0.f, dot = 0.f;
+                read_weights<D>(weight[is_q ? 0 : 1], map.off_a >> 3, gw);
+                read_weights<D>(weight[is_q ? 0 : 1], map.off_b >> 3, hw);
+                uint64_t ss = 0ull, st = 0ull, dot = 0ull, dou = 0ull;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-                    dot = fmaf(g[i] * wa[i], a[i], fmaf(h[i] * wb[i], b[i], dot));
+                for (int i = 0; i < 4; ++i) {
+                    gw[i] = f2_mul(g[i], gw[i]);
+                    hw[i] = f2_mul(h[i], hw[i]);
+                    ss = f2_fma(a[i], a[i], ss);
+                    st = f2_fma(b[i], b[i], st);
+                    dot = f2_fma(gw[i], a[i], dot);
+                    dou = f2_fma(hw[i], b[i], dou);
                 }
-                ss = row_sum<Map::kLanes>(ss);
-                dot = row_sum<Map::kLanes>(dot);
+                const float sum = row_sum<Map::kLanes>(f2_sum(f2_add(ss, st))), prod = row_sum<Map::kLanes>(f2_sum(f2_add(dot, dou)));
                 // a row past the last head has zero gradient and adds nothing; its r is not used (eps may be 0)
-                const float r = there ? rsqrtf(ss * (1.f / D) + p.eps) : 0.f;
-                const float m = dot * r * (1.f / D);  // mean(g w u)
-                float da[8], db[8];  // what this row adds to the weight's gradient
+                const float r = there ? rsqrtf(sum * (1.f / D) + p.eps) : 0.f;
+                const float m = prod * r * (1.f / D);  // mean(g w u)
+                const uint64_t r2 = f2_pack(r, r), m2 = f2_pack(-m, -m);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float ua = a[i] * r, ub = b[i] * r;
-                    da[i] = g[i] * ua;
-                    db[i] = h[i] * ub;
-                    g[i] = r * fmaf(-ua, m, g[i] * wa[i]);
-                    h[i] = r * fmaf(-ub, m, h[i] * wb[i]);
+                for (int i = 0; i < 4; ++i) {  // a, b become u; g, h what the row adds to the weight's gradient; gw, hw dx
+                    a[i] = f2_mul(a[i], r2);
+                    b[i] = f2_mul(b[i], r2);
+                    g[i] = f2_mul(g[i], a[i]);
+                    h[i] = f2_mul(h[i], b[i]);
+                    gw[i] = f2_mul(r2, f2_fma(a[i], m2, gw[i]));
+                    hw[i] = f2_mul(r2, f2_fma(b[i], m2, hw[i]));
                 }
                 if (is_q) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dwq[0][i] += da[i];
-                        dwq[1][i] += db[i];
+                    for (int i = 0; i < 4; ++i) {
+                        dwq[0][i] = f2_add(dwq[0][i], g[i]);
+                        dwq[1][i] = f2_add(dwq[1][i], h[i]);
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float4 v = dwk_all[warp][i][lane];
-                        const float* d = i < 2 ? da + 4 * i : db + 4 * (i - 2);
-                        v.x += d[0];
-                        v.y += d[1];
-                        v.z += d[2];
-                        v.w += d[3];
+                        ulonglong2 v = dwk_all[warp][i][lane];
+                        v.x = f2_add(v.x, i < 2 ? g[2 * i] : h[2 * (i - 2)]);
+                        v.y = f2_add(v.y, i < 2 ? g[2 * i + 1] : h[2 * (i - 2) + 1]);
                         dwk_all[warp][i][lane] = v;
                     }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    g[i] = gw[i];
+                    h[i] = hw[i];
                 }
             }
             if (there) {
@@ -374,8 +401,14 @@ __global__ void __launch_bounds__(kWarps * 32, 4) qk_rope_bwd_kernel(const __gri
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float* own = reinterpret_cast<const float*>(&dwk_all[warp][0][lane]);
-                float x = t == 0 ? dwq[0][i] : own[(i / 4) * 128 + i % 4];
-                float y = t == 0 ? dwq[1][i] : own[(2 + i / 4) * 128 + i % 4];
+                float x = own[(i / 4) * 128 + i % 4], y = own[(2 + i / 4) * 128 + i % 4];
+                if (t == 0) {
+                    float lo, hi;
+                    f2_unpack(dwq[0][i / 2], lo, hi);
+                    x = i & 1 ? hi : lo;
+                    f2_unpack(dwq[1][i / 2], lo, hi);
+                    y = i & 1 ? hi : lo;
+                }
 #pragma unroll
                 for (int off = Map::kLanes; off < 32; off <<= 1) {
                     x += __shfl_xor_sync(0xffffffffu, x, off);
