@@ -98,7 +98,8 @@ __global__ void __launch_bounds__(kRowsPerCta * 32) attn_f32_kernel(const Params
         for (int u = 0; u < U; ++u) s = fmaf(qv[u], kr[u], s);
         s = warp_sum(s);
         const float m_new = fmaxf(m, s);
-        const float corr = exp2f(m - m_new), pj = exp2f(s - m_new);
+        const float base = m_new == -CUDART_INF_F ? 0.f : m_new;  // nothing but scores of -inf so far
+        const float corr = exp2f(m - base), pj = exp2f(s - base);
         l = fmaf(l, corr, pj);
 #pragma unroll
         for (int u = 0; u < U; ++u) acc[u] = fmaf(acc[u], corr, pj * vr[u]);

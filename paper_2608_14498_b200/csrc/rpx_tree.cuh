@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kSplit > 1 ? 2 : 4) tree_join
 #pragma unroll
             for (int k = 0; k < kJoinRows; ++k) {
                 unused[k] |= ml[k].y < 0.f;
-                if (ml[k].x == -CUDART_INF_F) continue;  // no key seen
+                if (ml[k].x == -CUDART_INF_F && ml[k].y == ml[k].y) continue;  // no key seen (a NaN sum: nothing but NaN, and goes on)
                 const float to = fmaxf(top[k], ml[k].x);
                 const float keep = fast_exp2(top[k] - to), f = fast_exp2(ml[k].x - to);
                 top[k] = to;

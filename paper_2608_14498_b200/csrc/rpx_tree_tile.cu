@@ -438,19 +438,23 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 auto score = [&](int e) { return __uint_as_float(sc[e >> 5][e & 31]); };
                 float mx[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) mx[u] = fmaxf(score(u), score(8 + u));
+                for (int u = 0; u < 8; ++u) mx[u] = fmax3_nan(score(u), score(8 + u), score(16 + u));
 #pragma unroll
-                for (int e = 16; e < kTile; e += 16)
+                for (int e = 24; e < kTile - 8; e += 16)
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) mx[u] = fmax3(mx[u], score(e + u), score(e + 8 + u));
-                const float m = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * p.scale_log2;
+                    for (int u = 0; u < 8; ++u) mx[u] = fmax3_nan(mx[u], score(e + u), score(e + 8 + u));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) mx[u] = fmax3_nan(mx[u], score(kTile - 8 + u), score(kTile - 4 + u));
+                const float m = fmax3_nan(fmax3_nan(mx[0], mx[1], mx[2]), fmax3_nan(mx[3], mx[4], mx[5]), fmax3_nan(mx[6], mx[7], mx[7])) * p.scale_log2;
                 const bool grow = m > run_max + kRaise;
                 const float new_max = grow ? m : run_max;
                 const float alpha = grow ? fast_exp2(run_max - new_max) : 1.f;
                 const bool rescale = !first && __any_sync(0xffffffffu, grow);
                 run_sum *= alpha;
                 run_max = new_max;
-                const float base = run_max == -CUDART_INF_F ? 0.f : run_max;  // a row that has seen no key yet
+                // what the scores are taken off: 0 in a row that has seen no key yet, and NaN for a score of NaN or +inf, which makes
+                // the row NaN as the definition does (the quartic's clamp alone would drop it)
+                const float base = !(m < CUDART_INF_F) ? CUDART_NAN_F : run_max == -CUDART_INF_F ? 0.f : run_max;
                 // ---- P = 2^(x - max): bf16 pairs over the first 64 columns of S_t, for short segments (one or two tiles,
                 // where the rounding is not averaged over many keys) a second term in the other 64.  A quarter of the
                 // exponentials is taken off the special-function unit (16 a clock, as long as the two products of a query
@@ -555,7 +559,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             const bool unused = has_last && ((own_word >> (node & 31)) & 1u) == 0u;
             const int64_t out_row = (static_cast<int64_t>(tok0) + node) * p.num_q_heads + head;
             const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (t0 == 0 ? 1 : 0)) * Cut::kRows + (paired ? t * 128 : 0) + row;
-            const float inv = 1.f / sum;
+            const float inv = top == -CUDART_INF_F ? CUDART_NAN_F : 1.f / sum;  // (every score -inf: 0 / 0)
             const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0u;
 #pragma unroll 1
             for (int c = c_begin; c < c_end; ++c) {

@@ -325,3 +325,42 @@ def test_far_pages_pass_32_bits(cuda_device):
     c.cache = (k, v, table)
     got = c.run()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# streaming, one query tile, two query tiles; float32 - each with sequences that are not cut and with cut ones
+@pytest.mark.parametrize("lens", [[300, 40], [2900, 700]])
+@pytest.mark.parametrize("nodes,dtype", [([3, 2], torch.bfloat16), ([40, 9], torch.bfloat16), ([150, 20], torch.bfloat16),
+                                         ([5, 2], torch.float32)])
+def test_a_score_that_is_no_number_reaches_its_rows(cuda_device, lens, nodes, dtype):
+    """NaN, and +inf (inf - inf in the softmax), make a row NaN as the definition does; -inf only takes its key out."""
+    c = Case(cuda_device, lens, nodes, 4, 2, 64, dtype=dtype, seed=3)
+    clean, clean_lse = c.run()
+    k_cache, table = c.cache[0], c.cache[2]
+
+    def place(s, key):
+        return int(table[s, key // PAGE]), key % PAGE
+
+    spots = [[(0, j)] for j in (*range(9), 130, lens[0] - 1)] + [[(1, 3)]] + [[(0, j) for j in range(n)] for n in (lens[0], lens[0] * 2 // 3)]
+    for spot in spots:
+        saved = k_cache.clone()
+        for s, key in spot:
+            page, at = place(s, key)
+            k_cache[page, 0, at] = NAN
+        out, lse = c.run()
+        k_cache.copy_(saved)
+        seq = torch.zeros(len(c.parents), dtype=torch.bool, device=cuda_device)
+        lo = sum(nodes[:spot[0][0]])
+        seq[lo:lo + nodes[spot[0][0]]] = True
+        assert out[seq][:, :2].isnan().all() and lse[seq][:, :2].isnan().all(), spot
+        assert torch.equal(out[:, 2:], clean[:, 2:]) and torch.equal(lse[:, 2:], clean_lse[:, 2:])
+        assert torch.equal(out[~seq], clean[~seq]) and torch.equal(lse[~seq], clean_lse[~seq])
+    for key in range(8):
+        saved = k_cache.clone()
+        page, at = place(0, key)
+        k_cache[page, 0, at, 0] = float("inf")
+        out, lse = c.run()
+        k_cache.copy_(saved)
+        up = c.q[:nodes[0], :2, 0] > 0
+        assert torch.equal(out[:nodes[0], :2].isnan().all(-1), up) and torch.equal(out[:nodes[0], :2].isnan().any(-1), up), key
+        assert torch.equal(lse[:nodes[0], :2].isnan(), up)
+    assert c.status.item() == 0
