@@ -360,8 +360,9 @@ RPX_API rpx_status_t rpx_pages_free(const rpx_page_pool_t* pool, const int32_t* 
  *               request, both are -1.
  *   src == dst  the row keeps its pages and gets fresh ones up to lens + extra_tokens.
  * All rows are read as they were before the call: a row is dst of one request only, and a row that is branched into is no
- * request's src.  Requests that break this, rows outside the table, a dst that holds pages, a src that does not hold what
- * its lens says, or more pages than table_cols are reported (RPX_ERR_DEVICE_DATA) and change nothing.  Fresh pages are taken
+ * request's src.  Requests that break this, rows outside the table, a dst that holds pages, a src without the last page that
+ * its lens counts, or more pages than table_cols are reported (RPX_ERR_DEVICE_DATA) and change nothing.  Any other entry of
+ * src that is no page of the pool is reported, copied as it is and not counted.  Fresh pages are taken
  * in the order of the requests; one that needs more than are left, and every later one that needs any, is reported
  * (RPX_ERR_NO_PAGES) and changes nothing.
  *   workspace: rpx_pages_fork_workspace_bytes, 256-byte aligned
@@ -374,7 +375,7 @@ RPX_API size_t rpx_pages_fork_workspace_bytes(const rpx_page_pool_t* pool, int32
 /*
  * Moves the live pages to the low end of the pool: with L of them, the live pages numbered L and above go, in order, to the
  * free numbers below L, and everything from L on is free.  Writes the new table and counts (block_table_out with its own
- * stride, ref_counts_out: the pool's own arrays, or others that do not overlap them; columns beyond table_cols are not
+ * stride, ref_counts_out: the pool's own arrays with their stride, or others that do not overlap them; columns beyond table_cols are not
  * written), the list of moves copy_src, copy_dst (device int32 [num_blocks / 2], -1 behind the last move) for
  * rpx_cache_copy_pages, and L to *n_live (device int32).  pool->lens is not used.  A table entry that names a free page, or
  * none of the pool's, is reported (RPX_ERR_DEVICE_DATA) and becomes -1.
@@ -425,7 +426,8 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *   desc->pair_axis: HOST array of rot_dim / 2 axis numbers < num_axes (1 .. 8), or NULL: every pair takes axis 0
  *   q [n_tokens][num_q_heads][head_dim], k [n_tokens][num_kv_heads][head_dim] with token strides in elements, such as
  *       views of one fused projection; q_weight, k_weight: element type of q and k, both or neither NULL
- *   positions device int32 [num_axes][pos_axis_stride], pos_axis_stride >= n_tokens, or 0: one row for all axes; inv_freq device float32 [rot_dim / 2]
+ *   positions device int32 [num_axes][pos_axis_stride], pos_axis_stride >= n_tokens, or 0: one row for all axes
+ *   inv_freq device float32 [rot_dim / 2]
  *   q_out, k_out with token strides; each may be its input itself (same pointer and stride), otherwise no output
  *       overlaps an input or the other output
  */

@@ -457,8 +457,16 @@ def tree_attn(q, k, v, cu_seqlens_tree, parents, cached_lens, max_tree_len: int,
             raise TypeError("cu_seqlens_tree, parents and cached_lens are contiguous int32 tensors")
     if parents.shape[0] != total or cached_lens.shape[0] != batch:
         raise ValueError("parents has one entry per token and cached_lens one per sequence")
+    if v.shape != k.shape or k.dtype != q.dtype or v.dtype != q.dtype or k.shape[0] != total:
+        raise ValueError("k and v are [tokens, kv_heads, head_dim] tensors with the tokens and the element type of q")
+    if cache[0].shape[1:] != (k.shape[1], BLOCK_SIZE, k.shape[2]) or cache[1].shape != cache[0].shape or cache[2].shape[0] < batch:
+        raise ValueError("the cache pools are [blocks, kv_heads, 16, head_dim], the block table has a row for each sequence")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out is a contiguous tensor of the shape and element type of q")
+    if lse is not None and (lse.shape != (total, heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise ValueError("lse is a contiguous float32 [tokens, q_heads] tensor")
     if lse is None and return_lse:
         lse = torch.empty((total, heads), dtype=torch.float32, device=q.device)
     need = lib.rpx_tree_attn_workspace_bytes(desc, total, batch, max_tree_len)

@@ -640,6 +640,8 @@ rpx_status_t rpx_pages_compact(const rpx_page_pool_t* pool, int32_t* block_table
     if (rpx_status_t rc = check_pool(pool, false)) return rc;
     if (pool->num_blocks == 0) return RPX_ERR_SHAPE;
     if (block_table_out_stride < pool->table_cols) return RPX_ERR_SHAPE;
+    // in place means entry by entry
+    if (pool->rows > 1 && block_table_out == pool->block_table && block_table_out_stride != pool->block_table_stride) return RPX_ERR_SHAPE;
     if (pool->rows > 0 && pool->table_cols > 0 && block_table_out == nullptr) return RPX_ERR_NULL;
     if (ref_counts_out == nullptr || n_live == nullptr) return RPX_ERR_NULL;
     if (pool->num_blocks > 1 && (copy_src == nullptr || copy_dst == nullptr)) return RPX_ERR_NULL;

@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
     }
     if (i >= n) return;
     const int64_t token = a.token_ids != nullptr ? __ldg(a.token_ids + tok0 + i) : tok0 + i;
-    const int32_t pos = len + i;
+    const int64_t pos = static_cast<int64_t>(len) + i;
     const int32_t page = __ldg(a.cache.block_table + s * a.cache.block_table_stride + pos / kPage);
     if (token < 0 || token >= a.total_tokens || page < 0 || page >= a.cache.num_blocks) {
         if (lane == 0) report(a.device_status, RPX_ERR_DEVICE_DATA);

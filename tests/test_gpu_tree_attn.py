@@ -364,3 +364,21 @@ def test_a_score_that_is_no_number_reaches_its_rows(cuda_device, lens, nodes, dt
         assert torch.equal(out[:nodes[0], :2].isnan().all(-1), up) and torch.equal(out[:nodes[0], :2].isnan().any(-1), up), key
         assert torch.equal(lse[:nodes[0], :2].isnan(), up)
     assert c.status.item() == 0
+
+
+def test_tensors_that_do_not_fit_are_refused(cuda_device):
+    c = Case(cuda_device, [20, 40], [3, 2], 4, 2, 64)
+    k_cache, v_cache, table = c.cache
+    for cache in ((k_cache[:, :1].contiguous(), v_cache[:, :1].contiguous(), table), (k_cache, v_cache[:-1], table),
+                  (k_cache, v_cache, table[:1])):
+        with pytest.raises(ValueError):
+            c.run(cache=cache)
+    with pytest.raises(ValueError):
+        c.run(out=torch.empty(5, 4, 64, device=cuda_device))
+    with pytest.raises(ValueError):
+        c.run(out=torch.empty(5, 8, 64, dtype=torch.bfloat16, device=cuda_device)[:, ::2])
+    with pytest.raises(ValueError):
+        c.run(lse=torch.empty(4, 5, device=cuda_device).t())
+    for k, v in ((c.k, c.v[:, :1]), (c.k.float(), c.v), (c.k[:-1], c.v[:-1])):
+        with pytest.raises(ValueError):
+            rpx.tree_attn(c.q, k, v, c.cu, c.parents_dev, c.lens_dev, 3, 40, c.cache)

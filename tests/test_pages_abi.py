@@ -62,6 +62,7 @@ def test_compact(lib):
     for bad in (dict(out=None), dict(refs=None), dict(cs=None), dict(cd=None), dict(live=None)):
         assert call(**bad) == -1
     assert call(stride=7) == -2 and call(pool(nb=0)) == -2
+    assert call(out=pool().block_table, stride=9) == -2  # in place with another stride
     assert call(ws=None) == -5 and call(ws_bytes=16) == -5 and call(ws=0x1040) == -4
     assert lib.rpx_pages_compact_workspace_bytes(ref(pool())) == 512  # 64 places, 1 chunk, 1 count of moves
 
