@@ -394,7 +394,7 @@ rpx_status_t launch_stream(const TreeArgs& a, const CUtensorMap& tk, const CUten
     kernel<<<static_cast<unsigned>(whole > 0 ? whole : p.ctas), kThreads, L::kSmemBytes, a.stream>>>(tk, tv, tkc, tvc, p);
     if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
     if (whole > 0) return RPX_OK;
-    return launch_join<D, Cut>(p, a.stream);
+    return launch_join_rows<D, Cut>(p, a.stream);
 }
 
 template <int D>

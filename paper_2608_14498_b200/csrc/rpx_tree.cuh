@@ -406,6 +406,61 @@ __global__ void __launch_bounds__(kJoinWarps * 32, kSplit > 1 ? 2 : 4) tree_join
     }
 }
 
+// The same for the tensor-core form with a few pieces to a segment: its rows lie 32 side by side (part_at), so a lane takes a
+// row and a warp 32 rows of one segment and kCols of their columns: what it loads are whole kilobytes, and the segment's
+// pieces are worked out once.  (8 x 192 nodes over 8192 tokens: 10 us behind the attention kernel; with a warp a row every load
+// touched 16 lines, 20 us.  Half the columns a warp, twice the warps: no difference.)
+template <int D, int kTiles>
+__global__ void __launch_bounds__(kJoinWarps * 32, 2) tree_join_tiles_kernel(const Params p, int32_t blocks) {
+    using Cut = NodeCut<kTiles>;
+    constexpr int kCols = 32, kParts = D / kCols, kPerSegment = Cut::kRows / 32 * kParts / kJoinWarps;  // CTAs to a segment
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int32_t segment = blockIdx.x / kPerSegment, unit = (blockIdx.x - segment * kPerSegment) * kJoinWarps + warp;
+    const int32_t row = unit / kParts * 32 + lane, col0 = unit % kParts * kCols;
+    const int32_t block = segment % blocks, kv_head = segment / blocks % p.num_kv_heads, s = segment / blocks / p.num_kv_heads;
+    const int32_t tile = row >> 7, in_tile = (row & 127) / p.group, node = (block * kTiles + tile) * p.tile_nodes + in_tile;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t total = p.seq_unit0[p.batch], seq0 = p.seq_unit0[s];  // (in flight together with the lengths)
+    const Seq q = read_seq<Cut>(p, s, nullptr);
+    const bool valid = in_tile < p.tile_nodes && node < q.n;
+    if (block >= q.blocks || __ballot_sync(0xffffffffu, valid) == 0u) return;
+    const int64_t size = piece_units<Cut>(total, p.ctas);
+    const int64_t unit0 = seq0 + kv_head * head_units<Cut>(q) + block * segment_units<Cut>(q, 0);
+    const int32_t c0 = piece_of(unit0 + tile_unit<Cut>(q, block, 0), size);
+    const int32_t n = piece_of(unit0 + tile_unit<Cut>(q, block, q.tiles - 1), size) - c0 + 1;
+    if (n == 1 || !valid) return;  // written whole; a row that is nobody's
+    float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
+    bool unused = false;
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
+#pragma unroll 2
+    for (int32_t j = 0; j < n; ++j) {
+        // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
+        const int64_t at = (static_cast<int64_t>(c0 + j) * 2 + (j == 0 ? 1 : 0)) * Cut::kRows + row;
+        const float2 ml = p.part_ml[at];
+        float v[kCols / 8][8];
+#pragma unroll
+        for (int c = 0; c < kCols / 8; ++c) ld_global_v8(p.part_o + Cut::template part_at<D>(at, col0 + 8 * c), v[c]);
+        unused |= ml.y < 0.f;
+        if (ml.x == -CUDART_INF_F && ml.y == ml.y) continue;  // no key seen (a NaN sum: nothing but NaN, and goes on)
+        const float to = fmaxf(top, ml.x);
+        const float keep = fast_exp2(top - to), f = fast_exp2(ml.x - to);
+        top = to;
+        sum = fmaf(sum, keep, f * ml.y);
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) acc[e] = fmaf(acc[e], keep, f * v[e / 8][e % 8]);
+    }
+    const float inv = unused ? 0.f : 1.f / sum;
+    const int64_t out_row = (static_cast<int64_t>(q.tok0) + node) * p.num_q_heads + kv_head * p.group + ((row & 127) - in_tile * p.group);
+    uint32_t w[kCols / 2];
+#pragma unroll
+    for (int e = 0; e < kCols / 2; ++e) w[e] = unused ? 0u : pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    uint4* dst = reinterpret_cast<uint4*>(p.out + out_row * D + col0);
+#pragma unroll
+    for (int i = 0; i < kCols / 8; ++i) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    if (col0 == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
+}
+
 // Launches a kernel that may start before the one in front of it has ended (it waits by itself where it has to).
 template <class Kernel, class... Args>
 rpx_status_t launch_on_top(Kernel* kernel, unsigned grid, unsigned threads, size_t smem, cudaStream_t stream, const Args&... args) {
@@ -430,9 +485,19 @@ rpx_status_t launch_join_split(const Params& p, cudaStream_t stream) {
     return launch_on_top(tree_join_kernel<D, Cut, kSplit, kJoinRows>, static_cast<unsigned>(chunks * p.batch), kJoinWarps * 32, 0, stream, p,
                          static_cast<int32_t>(chunks));
 }
+// More than 8 pieces per segment: a block a row.  Else 32 rows a warp (tensor-core form), or a row, or where there are more
+// rows than the SMs hold warps, two.
+template <int D, int kTiles>
+rpx_status_t launch_join_tiles(const Params& p, cudaStream_t stream) {
+    using Cut = NodeCut<kTiles>;
+    const int32_t blocks = Cut::blocks(p, p.max_tree);
+    const int64_t segments = static_cast<int64_t>(p.batch) * p.num_kv_heads * blocks, grid = segments * (Cut::kRows / 32 * (D / 32) / kJoinWarps);
+    if (p.ctas > 8 * segments) return launch_join_split<D, Cut, kJoinWarps, 1>(p, stream);
+    if (grid > INT32_MAX) return RPX_ERR_SHAPE;
+    return launch_on_top(tree_join_tiles_kernel<D, kTiles>, static_cast<unsigned>(grid), kJoinWarps * 32, 0, stream, p, blocks);
+}
 template <int D, class Cut>
-rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
-    // more than 8 pieces per segment: a block a row; more rows than the SMs hold warps: two rows a warp
+rpx_status_t launch_join_rows(const Params& p, cudaStream_t stream) {
     const int64_t segments = static_cast<int64_t>(p.batch) * p.num_kv_heads * Cut::blocks(p, p.max_tree);
     if (p.ctas > 8 * segments) return launch_join_split<D, Cut, kJoinWarps, 1>(p, stream);
     return p.total_tokens * p.num_q_heads > 6144 ? launch_join_split<D, Cut, 1, 2>(p, stream) : launch_join_split<D, Cut, 1, 1>(p, stream);

@@ -671,7 +671,7 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* va
     if (rpx_status_t rc = launch_on_top(kernel, static_cast<unsigned>(whole > 0 ? whole : p.ctas), kThreads, smem, a.stream, tq, tk, tv, tkc, tvc, p))
         return rc;
     if (whole > 0) return RPX_OK;
-    return launch_join<D, Cut>(p, a.stream);
+    return launch_join_tiles<D, L::kQTiles>(p, a.stream);
 }
 
 // One query tile holds the rows of every tree: the buffers take turns throughout and the second Q tile's room goes to V.
