@@ -148,16 +148,9 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             ++segments;
             const int32_t* table = p.block_table + static_cast<int64_t>(walk.s) * p.block_table_stride;
             const int32_t pages = (q.len + kPage - 1) / kPage;
-            // lane pg fetches page pg of a tile; block ids are read a tile ahead
+            // lane pg fetches page pg of a tile; block ids are read a tile ahead and looked at only then
             const int pg = lane & 7;
-            auto read_block = [&](int32_t t) {
-                int32_t b = t < q.cached_tiles && t * kPages + pg < pages ? __ldg(table + t * kPages + pg) : 0;
-                if (b < 0 || b >= p.num_blocks) {
-                    ctl->data_error = 1;
-                    b = 0;
-                }
-                return b;
-            };
+            auto read_block = [&](int32_t t) { return t < q.cached_tiles && t * kPages + pg < pages ? __ldg(table + t * kPages + pg) : 0; };
             auto load = [&](int32_t t, int32_t block, bool is_v, uint8_t* dst, uint64_t* full) {
                 if (t >= q.cached_tiles) {  // the tree's own keys
                     const int32_t own = t - q.cached_tiles;
@@ -218,6 +211,10 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     const uint32_t st = nk % L::kSlotsK;
                     ok = mbar_wait(&ctl->k_empty[st], ((nk / L::kSlotsK) & 1u) ^ 1u, abort_flag);
                     if (!ok) break;
+                    if (block_now < 0 || block_now >= p.num_blocks) {
+                        ctl->data_error = 1;
+                        block_now = 0;
+                    }
                     load(walk.t0 + j, block_now, false, smem + L::kKOff + st * L::kTensorBytes, &ctl->k_full[st]);
                     ++nk;
                     __syncwarp();
