@@ -63,9 +63,9 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
     static constexpr int kTile = 128, kRows = 128 * kTiles, kWholeTiles = 8;
-    // by a fit over the CTAs of a ragged batch, a key tile against two query tiles takes 2.15 us, against one 1.65, and going
-    // over to another segment about as long as two tiles
-    static constexpr int kPairWeight = 4, kOneWeight = 3, kSegment = 7;
+    // by a fit over the CTAs of ragged batches, a key tile against two query tiles takes 2.09 us, against one 1.43, and going
+    // over to another segment 4.8 - 5.6
+    static constexpr int kPairWeight = 7, kOneWeight = 5, kSegment = 17;
     static constexpr int kMinUnits = kSegment + 2 * (kTiles == 1 ? kOneWeight : kPairWeight);
     static __device__ __forceinline__ int32_t weight(const Params& p, int32_t n, int32_t block) {
         if (kTiles == 1) return kOneWeight;
