@@ -521,7 +521,8 @@ inline void carve_workspace(Params& p, void* workspace) {
 
 // Short sequences are not cut: one CTA walks a segment of up to kWholeTiles key tiles in less time than cutting and joining
 // take (4 x 1 nodes, streaming: 200 cached tokens 8.4 us whole and 10.0 cut, 400: 10.9 and 8.8; 2 x 16 nodes, tensor cores:
-// 700 tokens 19.0 and 22.4, 1100: 23.2 and 19.0).  Goes by the caller's bound; a longer sequence is only slower.  Returns the grid (and sets whole_blocks), or 0.
+// 700 tokens 19.0 and 22.4, 1100: 23.2 and 19.0).  Goes by the caller's bound; a longer sequence is only slower.  Returns the
+// grid (and sets whole_blocks), or 0.
 template <class Cut>
 inline int64_t whole_grid(Params& p, int32_t max_cached) {
     const int64_t tiles = (static_cast<int64_t>(max_cached) + Cut::kTile - 1) / Cut::kTile + (p.max_tree + Cut::kTile - 1) / Cut::kTile;

@@ -19,8 +19,8 @@
 //   warp  9        : issues S_t = Q K^T (smem x smem -> TMEM) and O_t += P_t V (P as bf16 over S_t's first 64 columns)
 //   warps 10, 11   : only take part in the register hand-over
 // The tree's own V tiles come from a copy in which rows of unused nodes are zero (and no other sequence's rows follow), and
-// ancestor sets as bit masks; a small kernel writes both (tree_sets_kernel).  This kernel is launched on top of that one and waits for it only where it first
-// needs its results, behind the cached tiles.
+// ancestor sets as bit masks; a small kernel writes both (tree_sets_kernel).  This kernel is launched on top of that one and
+// waits for it only where it first needs its results, behind the cached tiles.
 #include <type_traits>
 
 #include "rpx_tree.cuh"
