@@ -685,6 +685,20 @@ def mrope_pair_axis(sections, interleaved: bool = False):
     return axes
 
 
+def _axis_bytes(pair_axis, pairs: int) -> bytes:
+    if not isinstance(pair_axis, (list, tuple, bytes)):
+        # an array's numbers and not its memory, which is what bytes() takes from anything with a buffer
+        if getattr(pair_axis, "is_cuda", False):
+            raise TypeError("pair_axis is read on the host")
+        pair_axis = pair_axis.tolist() if hasattr(pair_axis, "tolist") else list(pair_axis)
+    if len(pair_axis) != pairs:
+        raise ValueError("pair_axis has one axis number per entry of inv_freq")
+    try:
+        return bytes(pair_axis)
+    except ValueError:
+        raise ValueError("axis numbers of pair_axis are 0 .. num_axes - 1") from None
+
+
 def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) -> RopeDesc:
     torch = _torch()
     dtype = q.dtype
@@ -710,9 +724,7 @@ def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) ->
                 raise ValueError("norm weights are contiguous [head_dim] tensors")
     pairs = inv_freq.shape[0]
     if pair_axis is not None:
-        if len(pair_axis) != pairs:
-            raise ValueError("pair_axis has one axis number per entry of inv_freq")
-        pair_axis = bytes(pair_axis)
+        pair_axis = _axis_bytes(pair_axis, pairs)
     return RopeDesc(hq, k_shape[1], d, 2 * pairs, axes, pair_axis, eps, code)
 
 
@@ -734,7 +746,7 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, pair_a
     """rpx_qk_norm_rope: RMS norm per head (with weights) and rotation by position of queries and keys, in one pass.
 
     q [T, H_q, d], k [T, H_kv, d]; positions int32 [T] or [axes, T]; inv_freq float32 [rot_dim / 2]; pair_axis: the axis of
-    each pair (see ``mrope_pair_axis``), None = axis 0; weights [d] or both None (rotation only).  ``q_out`` / ``k_out``
+    each pair, a sequence or array on the host (see ``mrope_pair_axis``), None = axis 0; weights [d] or both None (rotation only).  ``q_out`` / ``k_out``
     may be q / k themselves.  Returns (q_out, k_out)."""
     lib = load_library()
     desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)

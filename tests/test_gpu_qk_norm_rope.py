@@ -293,3 +293,14 @@ def test_attention_backward_feeds_it(cuda_device):
     for name, x, y in zip(("dq", "dk", "dwq", "dwk"), got, ref):
         rel = float((x.double().cpu() - y).abs().max() / y.abs().max())
         assert rel <= 2e-2, (name, rel)
+
+
+@pytest.mark.parametrize("as_kind", [np.array, lambda a: np.array(a, dtype=np.int32), tuple, torch.tensor])
+def test_pair_axis_of_any_kind(cuda_device, as_kind):
+    """The axes as an array, a tuple or a CPU tensor give the bits that a list gives, both ways."""
+    q, k, pos, inv, axis, w = make(20, 4, 2, 64, 64, 3, "bf16", True, cuda_device)
+    dq, dk = torch.randn(20, 4, 64, device=cuda_device), torch.randn(20, 2, 64, device=cuda_device)
+    assert all(torch.equal(a, b) for a, b in zip(rpx.qk_norm_rope(q, k, pos, inv, w[0], w[1], as_kind(axis)),
+                                                 rpx.qk_norm_rope(q, k, pos, inv, w[0], w[1], axis)))
+    assert all(torch.equal(a, b) for a, b in zip(rpx.qk_norm_rope_backward(q, k, dq, dk, pos, inv, w[0], w[1], as_kind(axis)),
+                                                 rpx.qk_norm_rope_backward(q, k, dq, dk, pos, inv, w[0], w[1], axis)))

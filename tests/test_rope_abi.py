@@ -1,6 +1,7 @@
 """Host-only checks of the norm + rotation entry points: refusals before any launch, legal no-ops, the axis helper."""
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -84,3 +85,30 @@ def test_wrapper_checks():
                 dict(q_weight=torch.ones(32).bfloat16()), dict(positions=torch.zeros(3, 2, dtype=torch.int32))):
         with pytest.raises(ValueError):
             make(**bad)
+
+
+@pytest.mark.parametrize("make", [list, tuple, bytes, bytearray, iter, np.array, lambda a: np.array(a, dtype=np.int32),
+                                  lambda a: np.array(a, dtype=np.uint8), lambda a: np.array(sum(([x, 9] for x in a), []))[::2],
+                                  torch.tensor, lambda a: torch.tensor(a, dtype=torch.uint8),
+                                  lambda a: [np.int64(x) for x in a]])
+def test_pair_axis_means_its_numbers(make):
+    """Every kind of sequence gives the kernel the same axis per pair (an array's memory holds more bytes than numbers)."""
+    q, k = torch.zeros(3, 4, 64).bfloat16(), torch.zeros(3, 2, 64).bfloat16()
+    want = B.mrope_pair_axis([8, 12, 12])
+    desc = B._rope_desc(q, k, torch.zeros(3, 3, dtype=torch.int32), torch.ones(32), None, None, make(want), 1e-6)
+    at = ctypes.c_void_p.from_buffer(desc, B.RopeDesc.pair_axis.offset).value
+    assert list(ctypes.string_at(at, 32)) == want
+
+
+def test_pair_axis_refusals():
+    q, k = torch.zeros(3, 4, 64).bfloat16(), torch.zeros(3, 2, 64).bfloat16()
+
+    def make(axes):
+        return B._rope_desc(q, k, torch.zeros(3, 3, dtype=torch.int32), torch.ones(32), None, None, axes, 1e-6)
+
+    for bad in ([-1] + [0] * 31, np.full(32, -1), np.full(32, 256), np.zeros(31, np.int64), torch.zeros(64, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            make(bad)
+    for bad in ([0.5] * 32, np.zeros(32), np.zeros((32, 2), np.int64), "a" * 32):
+        with pytest.raises(TypeError):
+            make(bad)
