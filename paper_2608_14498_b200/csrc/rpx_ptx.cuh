@@ -449,12 +449,6 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// The same with a NaN for a result where an input is one.
-__device__ __forceinline__ float fmax3_nan(float a, float b, float c) {
-    float d;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
 // poly_exp2 on a pair; see poly_exp2 for the method.
 __device__ __forceinline__ void poly_exp2_pair(uint64_t x, float& e0, float& e1) {
     float x0, x1;

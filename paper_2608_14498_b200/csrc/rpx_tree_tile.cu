@@ -3,7 +3,7 @@
 // Same mathematics and the same cut as the streaming form (rpx_tree.cuh), with 128-key tiles and tcgen05.  A query tile is
 // tile_nodes = 128 / group nodes times the query heads of one KV head (row = node * group + head), so a key tile is
 // fetched once for all of them.  A block holds one query tile, or two where trees need more rows (kPaired).  Per 128 keys
-// a query tile costs 1024 clocks of tensor pipe, 768 of exponentials, and the tile itself 64 KB, 1.48 us (2500 clocks) of this
+// a query tile costs 1024 clocks of tensor pipe, 1024 of exponentials, and the tile itself 64 KB, 1.48 us (2500 clocks) of this
 // SM's share of HBM: with one query tile the cache's bytes bound, provided that the softmax of one step hides behind the
 // products of another.  So there are always two score buffers in flight:
 //   two query tiles  the buffers are the query tiles, both walk every key tile;
@@ -36,9 +36,6 @@ constexpr int kThreads = 32 * 12;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;  // 256 * 208 + 128 * 88 <= 384 * 168, what the launch has
 constexpr uint32_t kTmemCols = 512;
-constexpr int kPolyPairsOf4 = 1;  // of every 4 pairs of exponentials, how many go to the FMA pipe
-// 2^f on [-1/2, 1/2], least maximum of the relative error among quartics (2.6e-6; iteratively reweighted least squares)
-constexpr float kExp2_0 = 0.99999926f, kExp2_1 = 0.69312181f, kExp2_2 = 0.24024745f, kExp2_3 = 0.05591786f, kExp2_4 = 0.0095701f;
 constexpr int kMaxCtas = 148;
 
 template <int D, bool kPaired>
@@ -437,29 +434,27 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 auto score = [&](int e) { return __uint_as_float(sc[e >> 5][e & 31]); };
                 float mx[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) mx[u] = fmax3_nan(score(u), score(8 + u), score(16 + u));
+                for (int u = 0; u < 8; ++u) mx[u] = fmax3(score(u), score(8 + u), score(16 + u));
 #pragma unroll
                 for (int e = 24; e < kTile - 8; e += 16)
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) mx[u] = fmax3_nan(mx[u], score(e + u), score(e + 8 + u));
+                    for (int u = 0; u < 8; ++u) mx[u] = fmax3(mx[u], score(e + u), score(e + 8 + u));
 #pragma unroll
-                for (int u = 0; u < 4; ++u) mx[u] = fmax3_nan(mx[u], score(kTile - 8 + u), score(kTile - 4 + u));
-                const float m = fmax3_nan(fmax3_nan(mx[0], mx[1], mx[2]), fmax3_nan(mx[3], mx[4], mx[5]), fmax3_nan(mx[6], mx[7], mx[7])) * p.scale_log2;
+                for (int u = 0; u < 4; ++u) mx[u] = fmax3(mx[u], score(kTile - 8 + u), score(kTile - 4 + u));
+                const float m = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmax3(mx[6], mx[7], mx[7])) * p.scale_log2;
                 const bool grow = m > run_max + kRaise;
                 const float new_max = grow ? m : run_max;
                 const float alpha = grow ? fast_exp2(run_max - new_max) : 1.f;
                 const bool rescale = !first && __any_sync(0xffffffffu, grow);
                 run_sum *= alpha;
                 run_max = new_max;
-                // what the scores are taken off: 0 in a row that has seen no key yet, and NaN for a score of NaN or +inf, which makes
-                // the row NaN as the definition does (the quartic's clamp alone would drop it)
-                const float base = !(m < CUDART_INF_F) ? CUDART_NAN_F : run_max == -CUDART_INF_F ? 0.f : run_max;
+                const float base = run_max == -CUDART_INF_F ? 0.f : run_max;  // a row that has seen no key yet
                 // ---- P = 2^(x - max): bf16 pairs over the first 64 columns of S_t, for short segments (one or two tiles,
-                // where the rounding is not averaged over many keys) a second term in the other 64.  A quarter of the
-                // exponentials is taken off the special-function unit (16 a clock, as long as the two products of a query
-                // tile take); a cubic would do for P, but its 1e-4 shows in the float32 lse.
+                // where the rounding is not averaged over many keys) a second term in the other 64.  All exponentials go to the
+                // special-function unit: 0 for a masked key (-inf), NaN for NaN and for +inf (inf - inf).  With a quarter of them
+                // as a polynomial on the FMA pipe, clamped at 2^-125, a masked key had that weight, which a value of 1e38 shows,
+                // and the pass was no faster (8 x 8 nodes 27.8 us against 26.5, 32 ragged trees 212 against 207.5, 8 x 192 the same).
                 const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2), base2 = f2_pack(-base, -base);
-                const uint64_t magic = f2_pack(12582912.f, 12582912.f);  // 1.5 * 2^23: adding it rounds to an integer
                 uint64_t part[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -469,25 +464,7 @@ tree_tile_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     for (int i = 0; i < 32; i += 2) {
                         float x0, x1;
                         f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[c][i]), __uint_as_float(sc[c][i + 1])), scale2, base2), x0, x1);
-                        float e0, e1;
-                        if (((i / 2) & 3) < kPolyPairsOf4) {
-                            // x = n + f, |f| <= 1/2; 2^f by a quartic, 2^n into the exponent field
-                            const uint64_t x = f2_pack(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
-                            const uint64_t shifted = f2_add(x, magic);
-                            const uint64_t f = f2_sub(x, f2_sub(shifted, magic));
-                            uint64_t y = f2_fma(f2_pack(kExp2_4, kExp2_4), f, f2_pack(kExp2_3, kExp2_3));
-                            y = f2_fma(y, f, f2_pack(kExp2_2, kExp2_2));
-                            y = f2_fma(y, f, f2_pack(kExp2_1, kExp2_1));
-                            y = f2_fma(y, f, f2_pack(kExp2_0, kExp2_0));
-                            float y0, y1, s0, s1;
-                            f2_unpack(y, y0, y1);
-                            f2_unpack(shifted, s0, s1);
-                            e0 = __uint_as_float(__float_as_uint(y0) + (__float_as_uint(s0) << 23));
-                            e1 = __uint_as_float(__float_as_uint(y1) + (__float_as_uint(s1) << 23));
-                        } else {
-                            e0 = fast_exp2(x0);
-                            e1 = fast_exp2(x1);
-                        }
+                        const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
                         part[(i / 2) % 4] = f2_add(part[(i / 2) % 4], f2_pack(e0, e1));
                         packed[i >> 1] = pack_bf16x2(e0, e1);
                         if constexpr (kTwoTerms) {  // what the first term dropped

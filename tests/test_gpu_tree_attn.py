@@ -382,3 +382,42 @@ def test_tensors_that_do_not_fit_are_refused(cuda_device):
     for k, v in ((c.k, c.v[:, :1]), (c.k.float(), c.v), (c.k[:-1], c.v[:-1])):
         with pytest.raises(ValueError):
             rpx.tree_attn(c.q, k, v, c.cu, c.parents_dev, c.lens_dev, 3, 40, c.cache)
+
+
+# streaming, one query tile, two query tiles; float32
+FORMS = [([3, 2], torch.bfloat16), ([40, 9], torch.bfloat16), ([150, 20], torch.bfloat16), ([5, 2], torch.float32)]
+
+
+@pytest.mark.parametrize("lens", [[300, 40], [2900, 700]])
+@pytest.mark.parametrize("nodes,dtype", FORMS)
+def test_masked_values_weigh_nothing(cuda_device, lens, nodes, dtype):
+    """A node's V, however large, leaves every row alone that it is no ancestor of: the same bits as with V of 0."""
+    c = Case(cuda_device, lens, nodes, 4, 2, 64, dtype=dtype, kind="star", seed=4)
+    for j in range(min(18, nodes[0])):  # wherever the key lies within 16
+        saved, got = c.v[j].clone(), []
+        for value in (1e38, 0.0):
+            c.v[j] = value
+            got.append(c.run())
+        c.v[j] = saved
+        others = torch.arange(len(c.parents), device=cuda_device) != j
+        assert torch.equal(got[0][0][others], got[1][0][others]) and torch.equal(got[0][1][others], got[1][1][others]), j
+    assert c.status.item() == 0
+
+
+@pytest.mark.parametrize("nodes,dtype", FORMS)
+def test_far_smaller_scores_weigh_nothing(cuda_device, nodes, dtype):
+    """Keys whose weight is 2^-300 and less add nothing, not even to values of 1e38 (2^126)."""
+    c = Case(cuda_device, [300, 40], nodes, 4, 2, 64, dtype=dtype, seed=6)
+    k, v, table = c.cache
+    c.q.fill_(4.0), c.k.fill_(4.0)
+    # scores of 64 * 4 * 8 / 8 = 256 against 0 at a third of the keys: e^-256 < 2^-300
+    low = [key for key in range(300) if key % 3 == 0]
+    for key in range(300):
+        k[int(table[0, key // PAGE]), :, key % PAGE] = 0.0 if key % 3 == 0 else 8.0
+    got = []
+    for value in (1e38, 0.0):
+        for key in low:
+            v[int(table[0, key // PAGE]), :, key % PAGE] = value
+        got.append(c.run())
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert c.status.item() == 0
