@@ -47,7 +47,8 @@ struct TreeWorkspace {
 };
 TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t max_tree) {
     TreeWorkspace w = {};
-    if (d == nullptr || tokens <= 0 || batch <= 0 || max_tree <= 0 || d->num_kv_heads <= 0) return w;
+    // (the query may come before the call that refuses the descriptor)
+    if (check_attn_desc(d) != RPX_OK || tokens <= 0 || batch <= 0 || max_tree <= 0 || max_tree > RPX_TREE_MAX_NODES) return w;
     const int32_t group = d->num_q_heads / d->num_kv_heads;
     w.streams = d->dtype == RPX_BF16 && tree_streams(max_tree, group);
     if (w.streams) {

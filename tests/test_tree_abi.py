@@ -1,5 +1,8 @@
 """Host-only checks of the tree attention entry point: refusals before any launch, legal no-ops, workspace sizes."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -60,3 +63,26 @@ def test_workspace_sizes(lib):
     f32 = B.tree_attn_workspace_bytes(4, 2, 64, B.RPX_F32, 10, 2, 5)
     assert f32 == 256 + 256  # the attention call's piece, and 10 sets of 4 words
     assert B.tree_attn_workspace_bytes(28, 4, 128, B.RPX_BF16, 0, 8, 8) == 0
+
+
+def test_a_size_query_ends_no_process(lib):
+    """Fewer query heads than KV heads and a tree for the tensor-core form: a division by zero once, so in a child."""
+    code = "import sys; from paper_2608_14498_b200 import binding as B; " \
+           "sys.exit(B.tree_attn_workspace_bytes(4, 8, 128, 0, 200, 1, 200) != 0)"
+    assert subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(B.__file__)), timeout=120).returncode == 0
+
+
+@pytest.mark.parametrize("heads", [(4, 8), (4, 3), (0, 1), (1, 0), (-4, 2), (4, -2), (0, 0)])
+@pytest.mark.parametrize("max_tree", [1, 8, 129, 200, 1024])
+def test_sizes_for_heads_that_are_refused(lib, heads, max_tree):
+    """The size query answers 0 where the call refuses, for whoever asks for the size first."""
+    assert B.tree_attn_workspace_bytes(*heads, 128, B.RPX_BF16, 200, 1, max_tree) == 0
+    assert B.tree_attn_workspace_bytes(*heads, 128, B.RPX_F32, 200, 1, max_tree) == 0
+    assert call(lib, desc=B.AttnDesc(*heads, 128, 0.0, B.RPX_BF16), max_tree=max_tree, strides=(1024, 1024, 1024)) == -2
+
+
+def test_sizes_of_other_refusals(lib):
+    assert B.tree_attn_workspace_bytes(4, 2, 80, B.RPX_BF16, 200, 1, 200) == 0
+    assert B.tree_attn_workspace_bytes(4, 2, 128, 7, 200, 1, 200) == 0
+    assert B.tree_attn_workspace_bytes(4, 2, 128, B.RPX_BF16, 2000, 1, B.TREE_MAX_NODES + 1) == 0
+    assert lib.rpx_tree_attn_workspace_bytes(None, 200, 1, 200) == 0
