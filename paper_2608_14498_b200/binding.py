@@ -290,6 +290,14 @@ def _in_call_context(fn):
     return call
 
 
+def _one_device(first, *others) -> None:
+    """Kernels take bare pointers: an index tensor left on the host, or on another GPU, would be read as this GPU's memory."""
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"all tensors of a call are on one device: {t.device} next to {first.device}")
+
+
 def _desc(q, k, softmax_scale: float) -> AttnDesc:
     return AttnDesc(q.shape[1], k.shape[1], q.shape[2], float(softmax_scale), _dtype_code(q))
 
@@ -449,6 +457,7 @@ def tree_attn(q, k, v, cu_seqlens_tree, parents, cached_lens, max_tree_len: int,
     (out 0, lse -inf).  Other arguments as in ``suffix_attn``."""
     torch = _torch()
     lib = load_library()
+    _one_device(q, k, v, cu_seqlens_tree, parents, cached_lens, *cache, out, lse, workspace, device_status)
     desc = ctypes.byref(_desc(q, k, softmax_scale))
     total, heads, _ = q.shape
     batch = cu_seqlens_tree.shape[0] - 1
@@ -749,6 +758,7 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, pair_a
     each pair, a sequence or array on the host (see ``mrope_pair_axis``), None = axis 0; weights [d] or both None (rotation only).  ``q_out`` / ``k_out``
     may be q / k themselves.  Returns (q_out, k_out)."""
     lib = load_library()
+    _one_device(q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out)
     desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)
     q_out, k_out = _rope_out(q_out, q), _rope_out(k_out, k)
     rc = lib.rpx_qk_norm_rope(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), _tok_stride(q), _tok_stride(k), _ptr(q_weight),
@@ -768,6 +778,7 @@ def qk_norm_rope_backward(q, k, dq, dk, positions, inv_freq, q_weight=None, k_we
     ``accumulate_dw``).  Returns (dq_in, dk_in, dq_weight, dk_weight), the last two None without weights."""
     torch = _torch()
     lib = load_library()
+    _one_device(q, k, dq, dk, positions, inv_freq, q_weight, k_weight, dq_in, dk_in, dq_weight, dk_weight, workspace)
     desc = ctypes.byref(_rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps))
     for g, x in ((dq, q), (dk, k)):
         if g.dtype != torch.float32 or g.shape != x.shape or not g.is_contiguous():
@@ -824,6 +835,7 @@ def _row_list(t):
 @_in_call_context
 def pages_free(block_table, lens, ref_counts, rows, device_status=None, stream=None) -> None:
     """rpx_pages_free: the listed rows give up their pages (reference counts go down, entries become -1, lens 0)."""
+    _one_device(block_table, lens, ref_counts, rows, device_status)
     pool = ctypes.byref(_page_pool(block_table, lens, ref_counts))
     rc = load_library().rpx_pages_free(pool, _row_list(rows).data_ptr(), rows.numel(), _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
@@ -839,6 +851,7 @@ def pages_fork(block_table, lens, ref_counts, src_rows, dst_rows, extra_tokens: 
     Returns (copy_src, copy_dst) int32 [n]: the partial pages to copy in every layer (``cache_copy_pages``), -1 where none."""
     torch = _torch()
     lib = load_library()
+    _one_device(block_table, lens, ref_counts, src_rows, dst_rows, copy_src, copy_dst, workspace, device_status)
     pool = ctypes.byref(_page_pool(block_table, lens, ref_counts))
     n = _row_list(src_rows).numel()
     if _row_list(dst_rows).numel() != n:
@@ -869,6 +882,7 @@ def pages_compact(block_table, ref_counts, table_out=None, ref_counts_out=None, 
     the number of live pages (int32 [1])."""
     torch = _torch()
     lib = load_library()
+    _one_device(block_table, ref_counts, table_out, ref_counts_out, copy_src, copy_dst, n_live, workspace, device_status)
     pool = ctypes.byref(_page_pool(block_table, None, ref_counts))
     blocks = ref_counts.numel()
     table_out = block_table if table_out is None else table_out
@@ -900,6 +914,7 @@ def cache_copy_pages(k_cache, v_cache, src, dst, device_status=None, stream=None
 
     Pools bfloat16 [num_blocks, H_kv, 16, d], or [layers, num_blocks, H_kv, 16, d] for all layers at once."""
     bf16 = _torch().bfloat16
+    _one_device(k_cache, v_cache, src, dst, device_status)
     if k_cache.dtype != bf16 or v_cache.dtype != bf16:
         raise TypeError("cache pools are bfloat16")
     shape = k_cache.shape
@@ -923,6 +938,7 @@ def cache_append(k, v, cu_append, cached_lens, max_append: int, cache: Tuple, to
                  stream=None) -> None:
     """rpx_cache_append: K and V of tokens ``token_ids[cu_append[s]:cu_append[s + 1]]`` (or of the tokens of that range
     themselves) are stored at positions cached_lens[s], cached_lens[s] + 1, .. of sequence s; cached_lens stays as it is."""
+    _one_device(k, v, cu_append, cached_lens, *cache, token_ids, device_status)
     cs = _cache_struct(cache)
     shape = k.shape
     if len(shape) != 3:
