@@ -951,7 +951,8 @@ def cache_append(k, v, cu_append, cached_lens, max_append: int, cache: Tuple, to
         raise ValueError("cu_append has one entry more than cached_lens, and the block table a row for each sequence")
     ids, n_ids = None, 0
     if token_ids is not None:
-        ids, n_ids = _row_list(token_ids).data_ptr(), token_ids.numel()
+        # (an empty list has no pointer, and NULL stands for no list)
+        ids, n_ids = _row_list(token_ids).data_ptr() or cu_append.data_ptr(), token_ids.numel()
     rc = load_library().rpx_cache_append(k.data_ptr(), v.data_ptr(), _tok_stride(k), _tok_stride(v), tokens, heads, d,
                                          _dtype_code(k), ids, n_ids, cu_append.data_ptr(), cached_lens.data_ptr(), batch,
                                          max_append, ctypes.byref(cs), _ptr(device_status), _stream_ptr(stream))

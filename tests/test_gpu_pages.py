@@ -516,3 +516,16 @@ def test_a_rollout_with_drafted_trees(cuda_device):
         # bf16 output half step 2^-8 |out| and the weights' error on values below 5
         assert float((out.double() - ref).abs().max()) <= 2.0 ** -8 * float(ref.abs().max()) + 5 * 2.0 ** -11
         assert float((lse.double() - torch.logsumexp(z, -1).t()).abs().max()) <= 5e-4
+
+
+def test_append_of_an_empty_list_stores_nothing(cuda_device):
+    """An empty list of accepted tokens is a list: nothing is stored, and offsets that reach into it are reported."""
+    p = Pool(cuda_device, 30, 2, 4)
+    p.fork([(-1, 0), (-1, 1)], 40)
+    k = torch.randn(10, 2, 64, device=cuda_device).bfloat16()
+    before = p.k.clone(), p.v.clone()
+    rpx.cache_append(k, k, p.ints([0, 0, 0]), p.ints([3, 5]), 4, (p.k, p.v, p.table), token_ids=p.ints([]), device_status=p.status)
+    p.expect(0)
+    rpx.cache_append(k, k, p.ints([0, 2, 2]), p.ints([3, 5]), 4, (p.k, p.v, p.table), token_ids=p.ints([]), device_status=p.status)
+    p.expect(-8)
+    assert torch.equal(p.k, before[0]) and torch.equal(p.v, before[1])
