@@ -832,6 +832,11 @@ def _row_list(t):
     return t
 
 
+def _first(t, n):
+    """What a call wrote of a caller's buffer that may be longer: what lies behind is of an earlier call."""
+    return t if t.numel() == n else t[:n]
+
+
 @_in_call_context
 def pages_free(block_table, lens, ref_counts, rows, device_status=None, stream=None) -> None:
     """rpx_pages_free: the listed rows give up their pages (reference counts go down, entries become -1, lens 0)."""
@@ -848,7 +853,8 @@ def pages_fork(block_table, lens, ref_counts, src_rows, dst_rows, extra_tokens: 
     """rpx_pages_fork: empty rows ``dst`` become branches of rows ``src`` (-1: new sequences; src == dst: the row grows), whole
     pages shared, with fresh pages for the partial last one and ``extra_tokens`` more.
 
-    Returns (copy_src, copy_dst) int32 [n]: the partial pages to copy in every layer (``cache_copy_pages``), -1 where none."""
+    Returns (copy_src, copy_dst) int32 [n], the first n entries of buffers that are given: the partial pages to copy in every
+    layer (``cache_copy_pages``), -1 where none."""
     torch = _torch()
     lib = load_library()
     _one_device(block_table, lens, ref_counts, src_rows, dst_rows, copy_src, copy_dst, workspace, device_status)
@@ -869,7 +875,7 @@ def pages_fork(block_table, lens, ref_counts, src_rows, dst_rows, extra_tokens: 
                             copy_dst.data_ptr(), ws.data_ptr(), ws.nbytes, _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_pages_fork")
-    return copy_src, copy_dst
+    return _first(copy_src, n), _first(copy_dst, n)
 
 
 @_in_call_context
@@ -878,8 +884,8 @@ def pages_compact(block_table, ref_counts, table_out=None, ref_counts_out=None, 
     """rpx_pages_compact: live pages move to the low end of the pool; the table and the counts are rewritten, in place unless
     outputs are given.
 
-    Returns (copy_src, copy_dst, n_live): the moves for ``cache_copy_pages`` (int32 [num_blocks // 2], -1 behind the last) and
-    the number of live pages (int32 [1])."""
+    Returns (copy_src, copy_dst, n_live): the moves for ``cache_copy_pages`` (int32 [num_blocks // 2], -1 behind the last; the
+    first entries of buffers that are given) and the number of live pages (int32 [1])."""
     torch = _torch()
     lib = load_library()
     _one_device(block_table, ref_counts, table_out, ref_counts_out, copy_src, copy_dst, n_live, workspace, device_status)
@@ -905,7 +911,7 @@ def pages_compact(block_table, ref_counts, table_out=None, ref_counts_out=None, 
                                _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_pages_compact")
-    return copy_src, copy_dst, n_live
+    return _first(copy_src, moves), _first(copy_dst, moves), _first(n_live, 1)
 
 
 @_in_call_context

@@ -529,3 +529,28 @@ def test_append_of_an_empty_list_stores_nothing(cuda_device):
     rpx.cache_append(k, k, p.ints([0, 2, 2]), p.ints([3, 5]), 4, (p.k, p.v, p.table), token_ids=p.ints([]), device_status=p.status)
     p.expect(-8)
     assert torch.equal(p.k, before[0]) and torch.equal(p.v, before[1])
+
+
+def test_pair_lists_in_longer_buffers(cuda_device):
+    """Buffers made for the most a program ever asks for: what comes back holds this call's pairs and none of an earlier one."""
+    p = Pool(cuda_device, 41, 6, 8)
+    room = [torch.full((50,), 3, dtype=torch.int32, device=cuda_device) for _ in range(2)]
+    p.fork([(-1, 0)], 60)
+    p.set_len(0, 37)
+    pairs = rpx.pages_fork(p.table, p.lens, p.refs, p.ints([0, 0]), p.ints([2, 3]), 5, copy_src=room[0], copy_dst=room[1],
+                           device_status=p.status)
+    want, _, _ = p.model.fork([(0, 2), (0, 3)], 5)
+    assert list(zip(*(x.tolist() for x in pairs))) == want
+    assert [x.data_ptr() for x in pairs] == [x.data_ptr() for x in room]
+    p.free([0])
+    before = p.k.clone()
+    src, dst, n_live = rpx.pages_compact(p.table, p.refs, copy_src=room[0], copy_dst=room[1], n_live=p.ints([9, 9]),
+                                         device_status=p.status)
+    moves, n = p.model.compact()
+    assert n_live.tolist() == [n] and list(zip(src.tolist(), dst.tolist())) == moves + [(-1, -1)] * (20 - len(moves))
+    rpx.cache_copy_pages(p.k, p.v, src, dst, device_status=p.status)
+    p.expect(0)
+    p.check()
+    for a, b in moves:
+        before[b] = before[a]
+    assert torch.equal(p.k, before)
