@@ -253,11 +253,11 @@ def _tok_stride(t) -> int:
     shape, stride = t.shape, t.stride()
     if len(shape) != 3:
         raise ValueError("expected a [tokens, heads, head_dim] tensor")
-    if shape[0] <= 1:
+    if shape[0] == 0:
         return shape[1] * shape[2]
-    if stride[2] != 1 or stride[1] != shape[2]:
+    if stride[2] != 1 or (stride[1] != shape[2] and shape[1] > 1):  # (one head has no neighbour)
         raise ValueError("expected a [tokens, heads, head_dim] tensor with contiguous heads")
-    return stride[0]
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _workspace(nbytes: int, device, workspace):

@@ -106,3 +106,31 @@ def test_host_tensors_are_refused(cuda_device, name):
         with pytest.raises(ValueError, match="one device"):
             getattr(rpx, name)(**bad)
     torch.cuda.synchronize()
+
+
+def test_token_strides():
+    """The heads of one token are looked at as those of many are: a single decoded token may be a view of anything."""
+    x = torch.zeros(1, 8, 128)
+    for t, stride in ((x, 1024), (x[:, 2:5], 384), (x[:, :1, :64], 64), (x[:, 3:4], 128), (x[:0, ::2], 512),
+                      (torch.zeros(5, 8, 64)[2:3], 512), (torch.zeros(5, 8, 64)[1:4, 2:4], 512)):
+        assert B._tok_stride(t) == stride, (t.shape, t.stride())
+    for t in (x[:, ::2], x[..., :64], x.transpose(1, 2), x[..., ::2], torch.zeros(5, 8, 64)[2:3, ::2], torch.zeros(5, 8, 64)[:, ::2]):
+        with pytest.raises(ValueError):
+            B._tok_stride(t)
+
+
+@pytest.mark.gpu
+def test_one_token_with_heads_apart_is_refused(cuda_device):
+    args = arguments(cuda_device)
+    wide = torch.randn(1, 8, 64, device=cuda_device).bfloat16()
+    rope = {n: args["qk_norm_rope"][n] for n in ("inv_freq", "q_weight", "k_weight")}
+    pos = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+    for q, k in ((wide[:, ::2], wide[:, :2]), (wide[:, :4], wide[:, ::4])):
+        with pytest.raises(ValueError):
+            rpx.qk_norm_rope(q, k, pos, **rope)
+        with pytest.raises(ValueError):
+            rpx.tree_attn(q, k, k, pos.new_tensor([0, 1]), pos - 1, pos, 1, 16, args["tree_attn"]["cache"])
+    with pytest.raises(ValueError):
+        rpx.qk_norm_rope(wide[:, :4], wide[:, :2], pos, **rope, q_out=wide.clone()[:, ::2])
+    with pytest.raises(ValueError):
+        rpx.cache_append(wide[:, ::4], wide[:, ::4], pos.new_tensor([0, 1]), pos, 1, args["tree_attn"]["cache"])
