@@ -63,6 +63,14 @@ TreeWorkspace tree_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t b
     return w;
 }
 
+// Sizes that a later launch of a tree pass cannot hold (grids; 32-bit coordinates of the pool's groups of eight keys):
+// refused before the first one.
+bool tree_too_large(const rpx_attn_desc_t* d, int32_t batch, int32_t max_tree, const rpx_kv_cache_t* cache, bool streams) {
+    if (d->dtype == RPX_F32) return batch > 65535 || d->num_q_heads > 65535;
+    if (!streams && cache->num_blocks * d->num_kv_heads > INT32_MAX / 2) return true;
+    return (static_cast<int64_t>(max_tree) * d->num_q_heads + 7) / 8 * batch > INT32_MAX;  // eight rows or more to a block of the join
+}
+
 // Shared body of the attention entry points.  prefix_lens == NULL selects the prefix pass, parents != NULL
 // (with is_suffix) a tree of drafted tokens.
 rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const void* k, const void* v,
@@ -96,6 +104,7 @@ rpx_status_t run_attention(const rpx_attn_desc_t* desc, const void* q, const voi
     if (q_tok_stride % 8 || k_tok_stride % 8 || v_tok_stride % 8) return RPX_ERR_ALIGN;
     const TreeWorkspace tree_ws = is_tree ? tree_workspace(desc, total_tokens, batch, max_q_len) : TreeWorkspace{};
     const size_t need = is_tree ? tree_ws.bytes : attn_workspace(desc, total_tokens, is_suffix);
+    if (is_tree && tree_too_large(desc, batch, max_q_len, cache, tree_ws.streams)) return RPX_ERR_SHAPE;
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return RPX_ERR_WORKSPACE;
     if (need > 0 && !aligned_ws(workspace)) return RPX_ERR_ALIGN;
     if (rpx_status_t rc = check_arch()) return rc;

@@ -631,8 +631,7 @@ rpx_status_t launch_tile(const TreeArgs& a, const uint32_t* sets, const void* va
     }
     {
         // the pool as groups of 8 keys: two per page and head
-        const uint64_t groups = static_cast<uint64_t>(a.cache->num_blocks) * heads * 2;
-        if (groups > INT32_MAX) return RPX_ERR_SHAPE;
+        const uint64_t groups = static_cast<uint64_t>(a.cache->num_blocks) * heads * 2;  // (fits 32 bits: checked by the caller)
         const uint64_t dims[4] = {64, 8, D / 64, groups};
         const uint64_t strides[3] = {D * 2ull, 128, 8 * D * 2ull};
         const uint32_t box[4] = {64, 8, D / 64, 2};

@@ -86,3 +86,12 @@ def test_sizes_of_other_refusals(lib):
     assert B.tree_attn_workspace_bytes(4, 2, 128, 7, 200, 1, 200) == 0
     assert B.tree_attn_workspace_bytes(4, 2, 128, B.RPX_BF16, 2000, 1, B.TREE_MAX_NODES + 1) == 0
     assert lib.rpx_tree_attn_workspace_bytes(None, 200, 1, 200) == 0
+
+
+def test_sizes_that_no_launch_holds(lib):
+    """Refused on the host, before the launches in front of the one that could not hold them."""
+    f32, big = B.AttnDesc(4, 2, 128, 0.0, B.RPX_F32), 1 << 40
+    assert call(lib, desc=f32, batch=65536, total=65536, max_tree=1, ws_bytes=big) == -2
+    assert call(lib, max_tree=64, cache=B.KvCache(0x1000, 0x1000, 1 << 29, 16, 0x1000, 4)) == -2  # 2^31 groups of eight keys
+    assert call(lib, desc=B.AttnDesc(128, 1, 64, 0.0, 0), strides=(128 * 64, 64, 64), batch=1 << 18, total=1 << 20, max_tree=1024,
+                ws_bytes=big) == -2
