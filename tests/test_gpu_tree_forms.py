@@ -230,3 +230,33 @@ def test_repeats_streams_graph_and_workspace(cuda_device, size, lens):
         graph.replay()
     check(c, first, first_lse)
     assert torch.equal(first, second) and torch.equal(first_lse, second_lse)
+
+
+# ------------------------------------------------------------------ many sequences, long contexts, large groups
+@pytest.mark.parametrize("form,nodes,hq,hkv,d", [("stream16", 2, 4, 2, 64), ("stream16", 1, 4, 2, 128), ("stream32", 12, 4, 2, 64),
+                                                 ("tile1", 40, 4, 2, 64), ("tile2", 150, 28, 4, 128)])
+@pytest.mark.parametrize("batch", [33, 64, 97])
+def test_many_sequences_are_cut(cuda_device, form, nodes, hq, hkv, d, batch):
+    """More sequences than a warp looks at in a step, and too long not to be cut: the line of tiles, the walk along it and
+    the join go over several rounds of 32, with long, short and empty sequences on both sides of each."""
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(0, 60, batch).tolist()
+    counts = rng.integers(0, nodes + 1, batch).tolist()
+    for s in (0, 30, 31, 32, 33, 63, 64, 65, 95, 96):
+        if s < batch:
+            lens[s], counts[s] = int(rng.integers(1100, 3000)), nodes
+    for s in (5, 34, 62, 70):
+        if s < batch:
+            lens[s], counts[s] = int(rng.integers(600, 1500)), max(1, nodes // 2)
+    for s in (29, 36, 66):
+        if s < batch:
+            lens[s], counts[s] = 0, 0
+    assert form_of(counts, hq, hkv, d, BF16) == form
+    c = Case(cuda_device, lens, counts, hq, hkv, d, unused=0.1, seed=batch)
+    check(c, *c.run())
+
+
+def test_a_batch_of_decoding_steps(cuda_device):
+    lens = np.random.default_rng(0).integers(0, 3000, 64).tolist()
+    c = Case(cuda_device, lens, [1] * 64, 16, 4, 64)
+    check(c, *c.run())
