@@ -260,3 +260,44 @@ def test_a_batch_of_decoding_steps(cuda_device):
     lens = np.random.default_rng(0).integers(0, 3000, 64).tolist()
     c = Case(cuda_device, lens, [1] * 64, 16, 4, 64)
     check(c, *c.run())
+
+
+@pytest.mark.parametrize("form,nodes,hq,hkv", [("stream16", 8, 16, 8), ("stream32", 16, 16, 8), ("tile1", 48, 16, 8), ("tile2", 100, 16, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_tile_of_a_long_context(cuda_device, form, nodes, hq, hkv, d):
+    """Each node looks for one key that matches it: its output is that key's value, so a tile that is missing, stale, taken
+    twice or read from another page shows.  4 sequences of 8000 tokens are 13 key tiles a piece and more, several times the
+    rings' stages; over the runs every tile of 64 keys is looked for by some node, the last key of a sequence too.
+
+    A matching key is 30 sqrt(d) q / |q|^2: its score is 30, other nodes' matches have N(0, 30^2 / d) and the 8000 other keys
+    N(0, 1) or so, whose weights add up to some e^10; up to 100 of the former reach 17.  The match has all but e^-12 of the
+    weight, and the output is its value to the roundings of the probability and of the output, 2^-8 each."""
+    lens, batch = [8000, 7993, 7936, 8001], 4
+    assert form_of([nodes], hq, hkv, d, BF16) == form
+    c = Case(cuda_device, lens, [nodes] * batch, hq, hkv, d, kind="star", seed=2)
+    gen = torch.Generator().manual_seed(3)
+    k_cache, v_cache, table = c.cache
+    pages = table.cpu().numpy()
+    tiles = -(-max(lens) // 64)
+    for run in range(-(-tiles // nodes)):
+        want = torch.randn(batch * nodes, d, generator=gen).bfloat16().to(cuda_device)
+        c.q.copy_(want[:, None].expand(-1, hq, -1))
+        block, slot, row = [], [], []
+        for s in range(batch):
+            for i in range(nodes):
+                tile = (run * nodes + i) % tiles
+                at = lens[s] - 1 if tile == tiles - 1 else min(lens[s] - 1, tile * 64 + int(torch.randint(0, 64, (1,), generator=gen)))
+                if (int(pages[s, at // PAGE]), at % PAGE) in zip(block, slot):
+                    continue  # (the runs' last nodes start over)
+                block.append(int(pages[s, at // PAGE])), slot.append(at % PAGE), row.append(s * nodes + i)
+        b, t, r = (torch.tensor(x, device=cuda_device) for x in (block, slot, row))
+        saved = k_cache[b, :, t].clone()
+        match = want[r].float()
+        match = match * (30 * d ** 0.5 / match.square().sum(-1, keepdim=True))
+        k_cache[b, :, t] = match.bfloat16()[:, None].expand(-1, hkv, -1)
+        out, lse = c.run()
+        check(c, out, lse)
+        # and directly: the output is the value of the key that matches
+        match = v_cache[b, :, t].float().repeat_interleave(hq // hkv, 1)
+        assert float((out[r].float() - match).abs().max()) <= (2.0 ** -7 + 1e-4) * float(match.abs().max())
+        k_cache[b, :, t] = saved
