@@ -301,3 +301,11 @@ def test_every_tile_of_a_long_context(cuda_device, form, nodes, hq, hkv, d):
         match = v_cache[b, :, t].float().repeat_interleave(hq // hkv, 1)
         assert float((out[r].float() - match).abs().max()) <= (2.0 ** -7 + 1e-4) * float(match.abs().max())
         k_cache[b, :, t] = saved
+
+
+@pytest.mark.parametrize("lens,nodes,hq,hkv", [([300, 60], [100, 128], 160, 1), ([2500, 0], [128, 37], 160, 1), ([700, 5], [9, 100], 258, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_groups_above_128_heads(cuda_device, lens, nodes, hq, hkv, d):
+    assert form_of(nodes, hq, hkv, d, BF16) == "stream64"
+    c = Case(cuda_device, lens, nodes, hq, hkv, d, unused=0.1, seed=8)
+    check(c, *c.run())
