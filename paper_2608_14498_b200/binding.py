@@ -290,6 +290,14 @@ def _in_call_context(fn):
     return call
 
 
+def _bound(x) -> int:
+    """A bound or a count for the C ABI: any whole number, and nothing that 32 bits would cut."""
+    x = int(x)
+    if not 0 <= x < 1 << 31:
+        raise ValueError(f"{x} is not a count of 32 bits")
+    return x
+
+
 def _one_device(first, *others) -> None:
     """Kernels take bare pointers: an index tensor left on the host, or on another GPU, would be read as this GPU's memory."""
     device = first.get_device()
@@ -458,6 +466,7 @@ def tree_attn(q, k, v, cu_seqlens_tree, parents, cached_lens, max_tree_len: int,
     torch = _torch()
     lib = load_library()
     _one_device(q, k, v, cu_seqlens_tree, parents, cached_lens, *cache, out, lse, workspace, device_status)
+    max_tree_len, max_cached_len = _bound(max_tree_len), _bound(max_cached_len)
     desc = ctypes.byref(_desc(q, k, softmax_scale))
     total, heads, _ = q.shape
     batch = cu_seqlens_tree.shape[0] - 1
@@ -871,7 +880,7 @@ def pages_fork(block_table, lens, ref_counts, src_rows, dst_rows, extra_tokens: 
     elif _row_list(copy_dst).numel() < n:
         raise ValueError("copy_src and copy_dst have one entry per request")
     ws = _workspace(lib.rpx_pages_fork_workspace_bytes(pool, n), block_table.device, workspace)
-    rc = lib.rpx_pages_fork(pool, src_rows.data_ptr(), dst_rows.data_ptr(), n, extra_tokens, copy_src.data_ptr(),
+    rc = lib.rpx_pages_fork(pool, src_rows.data_ptr(), dst_rows.data_ptr(), n, _bound(extra_tokens), copy_src.data_ptr(),
                             copy_dst.data_ptr(), ws.data_ptr(), ws.nbytes, _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_pages_fork")
@@ -961,6 +970,6 @@ def cache_append(k, v, cu_append, cached_lens, max_append: int, cache: Tuple, to
         ids, n_ids = _row_list(token_ids).data_ptr() or cu_append.data_ptr(), token_ids.numel()
     rc = load_library().rpx_cache_append(k.data_ptr(), v.data_ptr(), _tok_stride(k), _tok_stride(v), tokens, heads, d,
                                          _dtype_code(k), ids, n_ids, cu_append.data_ptr(), cached_lens.data_ptr(), batch,
-                                         max_append, ctypes.byref(cs), _ptr(device_status), _stream_ptr(stream))
+                                         _bound(max_append), ctypes.byref(cs), _ptr(device_status), _stream_ptr(stream))
     if rc != 0:
         raise RpxError(rc, "rpx_cache_append")

@@ -2,6 +2,7 @@
 bare pointers, and index tensors are often built on the host."""
 import inspect
 
+import numpy as np
 import pytest
 import torch
 
@@ -134,3 +135,25 @@ def test_one_token_with_heads_apart_is_refused(cuda_device):
         rpx.qk_norm_rope(wide[:, :4], wide[:, :2], pos, **rope, q_out=wide.clone()[:, ::2])
     with pytest.raises(ValueError):
         rpx.cache_append(wide[:, ::4], wide[:, ::4], pos.new_tensor([0, 1]), pos, 1, args["tree_attn"]["cache"])
+
+
+def test_bounds():
+    for x in (0, 7, np.int64(7), np.int32(7), torch.tensor(7), 2 ** 31 - 1):
+        assert B._bound(x) == int(x) and type(B._bound(x)) is int
+    for x in (-1, 2 ** 31, 2 ** 32 + 5):  # 2^32 + 5 arrived as 5
+        with pytest.raises(ValueError):
+            B._bound(x)
+
+
+@pytest.mark.gpu
+def test_bounds_of_any_kind(cuda_device):
+    args = arguments(cuda_device)
+    for name, bounds in (("tree_attn", ("max_tree_len", "max_cached_len")), ("pages_fork", ("extra_tokens",)), ("cache_append", ("max_append",))):
+        call = {**args[name], **{b: 3 for b in bounds}}
+        for kind in (np.int64, np.int32, torch.tensor):
+            getattr(rpx, name)(**{**call, **{b: kind(3) for b in bounds}})
+        for b in bounds:
+            for bad in (2 ** 32 + 3, -1):
+                with pytest.raises(ValueError):
+                    getattr(rpx, name)(**{**call, b: bad})
+    torch.cuda.synchronize()
