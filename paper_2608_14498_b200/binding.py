@@ -278,7 +278,7 @@ def _in_call_context(fn):
     @functools.wraps(fn)
     def call(*args, **kwargs):
         torch = _torch()
-        first = args[0] if args else next(iter(kwargs.values()))
+        first = args[0] if args else next(x for x in kwargs.values() if isinstance(x, torch.Tensor))
         stream = kwargs.get("stream")
         if stream is None and first.is_cuda and first.get_device() == torch._C._cuda_getDevice():
             return fn(*args, **kwargs)  # the usual case, without the cost of entering a context

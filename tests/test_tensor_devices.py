@@ -157,3 +157,14 @@ def test_bounds_of_any_kind(cuda_device):
                 with pytest.raises(ValueError):
                     getattr(rpx, name)(**{**call, b: bad})
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", CALLS)
+def test_keywords_in_any_order(cuda_device, name):
+    """Numbers, tuples and None may come before the first tensor."""
+    args = arguments(cuda_device)[name]
+    late = {n: x for n, x in args.items() if torch.is_tensor(x)}
+    early = {n: x for n, x in args.items() if n not in late}
+    getattr(rpx, name)(stream=None, **early, **late)
+    torch.cuda.synchronize()
