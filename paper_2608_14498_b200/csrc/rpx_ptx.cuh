@@ -468,8 +468,8 @@ __device__ __forceinline__ void poly_exp2_pair(uint64_t x, float& e0, float& e1)
     e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(s1) << 23));
 }
 
-// 32-byte global store (sm_100): `p` must be 32-byte aligned.
-__device__ __forceinline__ void ld_global_v8(const void* p, float (&r)[8]) {  // 32-byte aligned
+// 32-byte global load and store (sm_100): `p` must be 32-byte aligned.
+__device__ __forceinline__ void ld_global_v8(const void* p, float (&r)[8]) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
                  : "l"(p) : "memory");

@@ -63,8 +63,10 @@ struct RowCut {  // blocks of kRows rows, row = node * group + head within the K
 template <int kTiles>
 struct NodeCut {  // blocks of kTiles query tiles of tile_nodes nodes each
     static constexpr int kTile = 128, kRows = 128 * kTiles, kWholeTiles = 8;
-    // by a fit over the CTAs of ragged batches, a key tile against two query tiles takes 2.09 us, against one 1.43, and going
-    // over to another segment 4.8 - 5.6
+    // by a fit over the CTAs, a key tile against two query tiles takes 1.67 us, against one 1.0 - 1.35, and going over to
+    // another segment 4.5 - 6.5.  The times hardly turn on it: over five batches (8 x 8, 16 x 24, 32 ragged x 16, 12 x 60 and
+    // 8 x 192 nodes) weights of (6, 5, 17), (8, 5, 17), (7, 5, 11), (7, 5, 25), (7, 5, 34) and (6, 5, 30) are up to 1.5 % faster
+    // and up to 7 % slower with head_dim 64, where a tile has half the bytes, and within the noise or slower with 128.
     static constexpr int kPairWeight = 7, kOneWeight = 5, kSegment = 17;
     static constexpr int kMinUnits = kSegment + 2 * (kTiles == 1 ? kOneWeight : kPairWeight);
     static __device__ __forceinline__ int32_t weight(const Params& p, int32_t n, int32_t block) {
@@ -486,7 +488,8 @@ rpx_status_t launch_join_split(const Params& p, cudaStream_t stream) {
                          static_cast<int32_t>(chunks));
 }
 // More than 8 pieces per segment: a block a row.  Else 32 rows a warp (tensor-core form), or a row, or where there are more
-// rows than the SMs hold warps, two.
+// rows than the SMs hold warps, two (streaming form, whole call with a row and with two: 200 rows 15.3 and 15.7 us, 5120 rows
+// 38.2 and 38.9, 7680 rows 52.9 and 52.1, 12288 rows 78.6 and 77.1).
 template <int D, int kTiles>
 rpx_status_t launch_join_tiles(const Params& p, cudaStream_t stream) {
     using Cut = NodeCut<kTiles>;
@@ -520,9 +523,10 @@ inline void carve_workspace(Params& p, void* workspace) {
 }
 
 // Short sequences are not cut: one CTA walks a segment of up to kWholeTiles key tiles in less time than cutting and joining
-// take (4 x 1 nodes, streaming: 200 cached tokens 8.4 us whole and 10.0 cut, 400: 10.9 and 8.8; 2 x 16 nodes, tensor cores:
-// 700 tokens 19.0 and 22.4, 1100: 23.2 and 19.0).  Goes by the caller's bound; a longer sequence is only slower.  Returns the
-// grid (and sets whole_blocks), or 0.
+// take (head_dim 128; 4 x 1 nodes, streaming: 300 cached tokens 9.5 us whole and 10.3 cut, 400: 11.1 and 9.5; 2 x 16 nodes,
+// one query tile: 900 tokens 19.2 and 20.8, 1100: 20.2 and 20.7; 2 x 100 nodes, two: 700 tokens 22.6 and 24.2, 1100: 28.0 and
+// 24.6.  head_dim 64, in the same order: 7.5 and 8.8, 8.6 and 8.3; 17.4 and 18.8, 18.4 and 18.9; 19.5 and 20.9, 24.2 and 21.0).
+// Goes by the caller's bound; a longer sequence is only slower.  Returns the grid (and sets whole_blocks), or 0.
 template <class Cut>
 inline int64_t whole_grid(Params& p, int32_t max_cached) {
     const int64_t tiles = (static_cast<int64_t>(max_cached) + Cut::kTile - 1) / Cut::kTile + (p.max_tree + Cut::kTile - 1) / Cut::kTile;

@@ -9,10 +9,10 @@
 //   two query tiles  the buffers are the query tiles, both walk every key tile;
 //   one query tile   the buffers take turns: buffer t walks the key tiles t, t + 2, .. with a running maximum, sum and
 //                    output of its own, and both buffers' warps add the two up straight out of TMEM at the end.
-// Measured by a fit over the CTAs: a key tile against one query tile 1.43 us (the bytes), against two 2.09 us, going over to
-// another segment 5 us.  Of the 3800 clocks of a tile against two, the tensor core is busy for 2050, and its issuer waits 950
-// for probabilities and 850 for K and V; handing the probabilities over in two halves, or waiting for K behind the first
-// product instead of in front of it, changed nothing.
+// Measured by a fit over the CTAs (head_dim 128): a key tile against one query tile 1.35 us where the bytes bound it and 1.0
+// where they come from L2, against two 1.67 us, going over to another segment 4.5 - 6.5 us.  Of the 3200 clocks of a tile
+// against two, the tensor core is busy for 2050, and its issuer waits 1200 for probabilities and 800 for K and V; handing the
+// probabilities over in two halves, or waiting for K behind the first product instead of in front of it, changed nothing.
 //   warps 0-3, 4-7 : softmax of buffer 0, 1: thread = row = TMEM lane
 //   warp  8        : producer: Q once per segment, K and V through rings of their own (K runs a tile ahead, so it is not
 //                    held up behind a V slot), one TMA box per 16-token page
