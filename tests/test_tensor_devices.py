@@ -1,5 +1,5 @@
-"""Calls around the cache check that all of their tensors are on one device before anything is launched: their kernels take
-bare pointers, and index tensors are often built on the host."""
+"""Calls around the cache check what only the binding can see before anything is launched: that all tensors are on one device
+(kernels take bare pointers, and index tensors are often built on the host), strides of single tokens, bounds beyond 32 bits."""
 import inspect
 
 import numpy as np
