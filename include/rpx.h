@@ -292,6 +292,53 @@ RPX_API size_t rpx_token_logprobs_backward_workspace_bytes(int64_t n_tokens, int
                                                            rpx_dtype_t dtype);
 
 /*
+ * Clipped policy loss with a KL term, and its gradient (Section 2.1: the log-probabilities of the responses under the policy,
+ * the policy that sampled them and the reference enter the loss of the RL step): from rpx_token_logprobs to the `upstream` of
+ * rpx_token_logprobs_backward.  Sequence s owns the tokens cu_seqlens[s] .. cu_seqlens[s+1]-1; of them those with mask != 0
+ * (mask NULL: all) are counted, n_s of them; what lies at the others is not used.  With l, o, f the three log-probabilities:
+ *     d_t = l_t - o_t, or with RPX_RATIO_SEQUENCE its mean over the counted tokens of the sequence;   r_t = exp(d_t)
+ *     policy_t = -A r_t,            and where A > 0 and r_t > 1 + clip_high:                 -A (1 + clip_high)
+ *                                       where A < 0 and r_t < 1 - clip_low:                  -A (1 - clip_low)
+ *                                       where A < 0 and r_t > clip_dual (clip_dual > 0):     -A clip_dual
+ *     kl_t = l - f (kl = 1),  (l - f)^2 / 2 (kl = 2),  exp(f - l) - (f - l) - 1 (kl = 3),  0 (kl = 0)
+ *     w_t  = 1 / sum of all n_s (RPX_MEAN_TOKENS), or 1 / (n_s * sequences with n_s > 0) (RPX_MEAN_SEQUENCES); with
+ *            desc->count > 0 that number in place of the sum, or of the number of sequences (batches in parts)
+ *     loss = sum over the counted tokens of w_t (policy_t + kl_coef kl_t)
+ *     dlogprobs_t = upstream * w_t (-A r_t where not clipped, else 0, + kl_coef * d kl_t / d l_t);  0 where not counted
+ *   logprobs, old_logprobs, ref_logprobs device float32 [n_tokens]; old_logprobs NULL: d = 0 (a step on the policy itself);
+ *       ref_logprobs: needed with kl != 0, otherwise not read
+ *   advantages device float32: [n_tokens] with desc->adv_per_token, else [batch] (with RPX_RATIO_SEQUENCE always [batch])
+ *   mask device uint8 [n_tokens], or NULL.  These arrays may start at any element (16-byte accesses where all allow them).
+ *   upstream device float32 [1], the gradient that reaches the loss, or NULL: 1
+ *   stats device float32 [6]: loss, sum w policy, sum w kl, sum w [clipped], sum w r, the number of counted tokens
+ *   dlogprobs device float32 [n_tokens], or NULL: no gradient; overlaps no input.  Tokens of no sequence keep what it holds.
+ *   workspace: rpx_policy_loss_workspace_bytes
+ * Which side of a border a ratio is on is decided in 64 bits, sums are taken in 64 bits in a fixed order: the same call gives
+ * the same bits.  cu_seqlens that do not ascend from 0 or more to n_tokens at most are reported (RPX_ERR_DEVICE_DATA): a
+ * sequence that does not fit counts as empty, and the outputs of that call are undefined.
+ */
+enum { RPX_RATIO_TOKEN = 0, RPX_RATIO_SEQUENCE = 1 };
+enum { RPX_MEAN_TOKENS = 0, RPX_MEAN_SEQUENCES = 1 };
+typedef struct {
+    int32_t ratio;         /* RPX_RATIO_* */
+    int32_t mean;          /* RPX_MEAN_* */
+    int32_t kl;            /* 0 .. 3 */
+    int32_t adv_per_token; /* 0 or 1 */
+    double clip_low;       /* 0 <= clip_low < 1: doubles, so that a border is the caller's and not its float32 neighbour */
+    double clip_high;      /* >= 0 */
+    double clip_dual;      /* 0: off, else > 1 */
+    double kl_coef;
+    double count;          /* 0: the call's own */
+} rpx_policy_desc_t;
+
+RPX_API rpx_status_t rpx_policy_loss(const rpx_policy_desc_t* desc, const float* logprobs, const float* old_logprobs,
+                                     const float* ref_logprobs, const float* advantages, const uint8_t* mask,
+                                     const int32_t* cu_seqlens, int32_t batch, int64_t n_tokens, const float* upstream,
+                                     float* stats, float* dlogprobs, void* workspace, size_t workspace_bytes,
+                                     int32_t* device_status, void* cuda_stream);
+RPX_API size_t rpx_policy_loss_workspace_bytes(int32_t batch, int64_t n_tokens);
+
+/*
  * Backward of causal GQA attention over packed whole sequences (Section 3.2: the training actor differentiates both
  * its suffix pass and its prefix pass, and the suffix pass's gradient reaches the prompt through the prefix K/V it
  * attended to; Table 4, the row on the boundary KV that stays attached).  A sequence is prompt followed by response;
@@ -419,6 +466,37 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
                                       const rpx_kv_cache_t* cache, int32_t* device_status, void* cuda_stream);
 
 /*
+ * Attention of groups of sequences that share the pages of a prefix (an extension: the paper's workload samples several
+ * responses to every prompt, Section 4.1, and each of them attends to the one boundary KV of the prompt, Table 4).  All K
+ * and V lie in the cache, the queries' own among them (rpx_qk_norm_rope_append or rpx_cache_append has stored them): sequence
+ * s has kv_lens[s] cached tokens and owns the query tokens cu_seqlens_q[s] .. cu_seqlens_q[s+1]-1, the LAST n of its cached
+ * tokens; query i of n attends to the positions 0 .. kv_lens[s] - n + i.  n = 1 everywhere is a decoding step.
+ *   q [total_q_tokens][num_q_heads][head_dim], token stride in elements; out, lse as in rpx_suffix_attn
+ *   cu_groups device int32 [n_groups + 1]: group g is the sequences cu_groups[g] .. cu_groups[g+1]-1; every sequence is in
+ *       one group (alone, if it shares nothing)
+ *   shared_lens device int32 [n_groups]: tokens that the group's sequences have in common from position 0 on.  The table rows
+ *       of the group name the same pages for the whole pages among them (as rpx_pages_fork leaves them); those are read once
+ *       for the group, through its first row.  What is beyond is read through every sequence's own row.
+ *   A group is computed without sharing, and reported (RPX_ERR_DEVICE_DATA), if its bounds or shared length do not fit: the
+ *       shared tokens end in front of every member's first query.  A sequence whose offsets leave the packed tensors or the
+ *       table, that has more queries than cached tokens, or more than max_q_len, is reported and its rows are left as they are.
+ *   max_q_len, max_group_tokens: upper bounds of a sequence's and of a group's query tokens (a group with more is computed
+ *       without sharing, and reported); max_kv_len: upper bound of kv_lens (sizes the grid only)
+ *   num_q_heads / num_kv_heads: at most 128 (RPX_ERR_SHAPE)
+ *   workspace: rpx_group_attn_workspace_bytes with the same sizes
+ * The same call gives the same bits.  (Where the keys are cut goes by all lengths of the batch, so a sequence's sums may round
+ * otherwise beside other sequences.)  RPX_BF16: scores, maxima, sums and outputs are float32 until the output's rounding.
+ * RPX_F32 (for checking; a warp per row, nothing is shared): q, out and all products float32, K and V the cache's bf16.
+ */
+RPX_API rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t q_tok_stride, const int32_t* cu_seqlens_q,
+                                    const int32_t* kv_lens, int32_t batch, int64_t total_q_tokens, int32_t max_q_len,
+                                    int32_t max_kv_len, const int32_t* cu_groups, const int32_t* shared_lens, int32_t n_groups,
+                                    int32_t max_group_tokens, const rpx_kv_cache_t* cache, void* out, float* lse,
+                                    void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
+RPX_API size_t rpx_group_attn_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_q_tokens, int32_t batch,
+                                              int32_t n_groups, int32_t max_q_len, int32_t max_group_tokens);
+
+/*
  * Norm of queries and keys per head and rotation by position, in one pass (the attention calls of this library take q and
  * k with both already applied; the paper's video prompts are positioned on three axes: time, height, width).  For every
  * token t and head h, with the weight w of that tensor (q_weight or k_weight, [head_dim]):
@@ -452,6 +530,25 @@ RPX_API rpx_status_t rpx_qk_norm_rope(const rpx_rope_desc_t* desc, const void* q
                                       const int32_t* positions, int64_t pos_axis_stride, const float* inv_freq,
                                       int64_t n_tokens, void* q_out, void* k_out, int64_t q_out_tok_stride,
                                       int64_t k_out_tok_stride, void* cuda_stream);
+
+/*
+ * rpx_qk_norm_rope with K and V stored into the paged cache on the way, for generation steps and prompts: q_out as in
+ * rpx_qk_norm_rope; the normed and rotated k and the v of token cu_append[s] + i are stored, as bf16 rounded once, at position
+ * cached_lens[s] + i of sequence s (cached_lens is not changed).  The same slots as rpx_cache_append's, without k in between.
+ *   q, k, v [n_tokens][heads][head_dim] with token strides, such as views of one fused projection; element type desc->dtype
+ *   cu_append device int32 [batch + 1], ascending.  Tokens of no sequence are not stored and their q_out is left as it is.
+ *   positions as in rpx_qk_norm_rope, or NULL: every axis takes the token's place in its sequence, cached_lens[s] + i
+ *   max_append: upper bound of a sequence's tokens.  A sequence with more, or whose offsets or table do not fit, is reported
+ *       (RPX_ERR_DEVICE_DATA) and left out, its q_out too; a page number out of the pool is reported and that token's K, V are
+ *       not stored.  Two sequences must not store into the same slot.
+ */
+RPX_API rpx_status_t rpx_qk_norm_rope_append(const rpx_rope_desc_t* desc, const void* q, const void* k, const void* v,
+                                             int64_t q_tok_stride, int64_t k_tok_stride, int64_t v_tok_stride,
+                                             const void* q_weight, const void* k_weight, const int32_t* positions,
+                                             int64_t pos_axis_stride, const float* inv_freq, int64_t n_tokens,
+                                             const int32_t* cu_append, const int32_t* cached_lens, int32_t batch,
+                                             int32_t max_append, const rpx_kv_cache_t* cache, void* q_out,
+                                             int64_t q_out_tok_stride, int32_t* device_status, void* cuda_stream);
 
 /*
  * Backward of rpx_qk_norm_rope (Section 3.2: the training actor's passes are differentiated).  dq, dk are the gradients with

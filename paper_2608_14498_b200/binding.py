@@ -25,6 +25,8 @@ EXPORTS = (
     "rpx_chunk_attn",
     "rpx_tree_attn",
     "rpx_tree_attn_workspace_bytes",
+    "rpx_group_attn",
+    "rpx_group_attn_workspace_bytes",
     "rpx_token_logprobs",
     "rpx_token_logprobs_entropy",
     "rpx_token_logprobs_shard",
@@ -33,6 +35,8 @@ EXPORTS = (
     "rpx_token_logprobs_backward",
     "rpx_token_logprobs_backward_full",
     "rpx_token_logprobs_backward_workspace_bytes",
+    "rpx_policy_loss",
+    "rpx_policy_loss_workspace_bytes",
     "rpx_set_lm_head_pairing",
     "rpx_get_lm_head_pairing",
     "rpx_attn_backward",
@@ -45,6 +49,7 @@ EXPORTS = (
     "rpx_cache_copy_pages",
     "rpx_cache_append",
     "rpx_qk_norm_rope",
+    "rpx_qk_norm_rope_append",
     "rpx_qk_norm_rope_backward",
     "rpx_qk_norm_rope_backward_workspace_bytes",
     "rpx_prefix_attn_workspace_bytes",
@@ -110,6 +115,20 @@ class RopeDesc(ctypes.Structure):
     ]
 
 
+class PolicyDesc(ctypes.Structure):
+    _fields_ = [
+        ("ratio", ctypes.c_int32),
+        ("mean", ctypes.c_int32),
+        ("kl", ctypes.c_int32),
+        ("adv_per_token", ctypes.c_int32),
+        ("clip_low", ctypes.c_double),
+        ("clip_high", ctypes.c_double),
+        ("clip_dual", ctypes.c_double),
+        ("kl_coef", ctypes.c_double),
+        ("count", ctypes.c_double),
+    ]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -135,6 +154,18 @@ def load_library():
     lib.rpx_chunk_attn.restype = i32
     lib.rpx_chunk_attn.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, i64, i64, i64, vp, vp, i32, i64, i32,
                                     i32, ctypes.POINTER(KvCache), vp, vp, vp, sz, vp, vp]
+    lib.rpx_group_attn.restype = i32
+    lib.rpx_group_attn.argtypes = [ctypes.POINTER(AttnDesc), vp, i64, vp, vp, i32, i64, i32, i32, vp, vp, i32, i32,
+                                   ctypes.POINTER(KvCache), vp, vp, vp, sz, vp, vp]
+    lib.rpx_group_attn_workspace_bytes.restype = sz
+    lib.rpx_group_attn_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), i64, i32, i32, i32, i32]
+    lib.rpx_qk_norm_rope_append.restype = i32
+    lib.rpx_qk_norm_rope_append.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, vp, i64, i64, i64, vp, vp, vp, i64, vp, i64, vp, vp,
+                                            i32, i32, ctypes.POINTER(KvCache), vp, i64, vp, vp]
+    lib.rpx_policy_loss.restype = i32
+    lib.rpx_policy_loss.argtypes = [ctypes.POINTER(PolicyDesc), vp, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp, vp, sz, vp, vp]
+    lib.rpx_policy_loss_workspace_bytes.restype = sz
+    lib.rpx_policy_loss_workspace_bytes.argtypes = [i32, i64]
     lib.rpx_tree_attn.restype = i32
     lib.rpx_tree_attn.argtypes = [ctypes.POINTER(AttnDesc), vp, vp, vp, i64, i64, i64, vp, vp, vp, i32, i64, i32, i32,
                                   ctypes.POINTER(KvCache), vp, vp, vp, sz, vp, vp]
@@ -498,6 +529,57 @@ def tree_attn(q, k, v, cu_seqlens_tree, parents, cached_lens, max_tree_len: int,
     return (out, lse) if return_lse else out
 
 
+def group_attn_workspace_bytes(num_q_heads, num_kv_heads, head_dim, dtype_code, total_tokens, batch, n_groups, max_q_len,
+                               max_group_tokens) -> int:
+    d = AttnDesc(num_q_heads, num_kv_heads, head_dim, 0.0, dtype_code)
+    return int(load_library().rpx_group_attn_workspace_bytes(ctypes.byref(d), int(total_tokens), int(batch), int(n_groups),
+                                                             int(max_q_len), int(max_group_tokens)))
+
+
+@_in_call_context
+def group_attn(q, cu_seqlens_q, kv_lens, cu_groups, shared_lens, max_q_len: int, max_group_tokens: int, max_kv_len: int,
+               cache: Tuple, softmax_scale: float = 0.0, out=None, lse=None, return_lse: bool = False, workspace=None,
+               device_status=None, stream=None):
+    """rpx_group_attn: the last queries of every sequence over its cached keys, for groups that share the pages of a prefix.
+
+    q [T, H_q, d], packed by cu_seqlens_q int32 [B + 1]; kv_lens int32 [B]: cached tokens, the queries' own among them (store
+    them first); cu_groups int32 [G + 1]: sequences of every group; shared_lens int32 [G]: tokens that a group has in common
+    (whole pages of them are read once for the group, through its first row of the block table).  max_q_len and
+    max_group_tokens bound the query tokens of a sequence and of a group, max_kv_len kv_lens."""
+    torch = _torch()
+    lib = load_library()
+    _one_device(q, cu_seqlens_q, kv_lens, cu_groups, shared_lens, *cache, out, lse, workspace, device_status)
+    max_q_len, max_group_tokens, max_kv_len = _bound(max_q_len), _bound(max_group_tokens), _bound(max_kv_len)
+    shape, pool = q.shape, cache[0].shape
+    if len(shape) != 3 or len(pool) != 4 or pool[2:] != (BLOCK_SIZE, shape[2]) or cache[1].shape != pool:
+        raise ValueError("q is [tokens, q_heads, head_dim], the cache pools are [blocks, kv_heads, 16, head_dim]")
+    total, heads, d = shape
+    desc = ctypes.byref(AttnDesc(heads, pool[1], d, softmax_scale, _dtype_code(q)))
+    batch, groups = _row_list(kv_lens).numel(), _row_list(shared_lens).numel()
+    if _row_list(cu_seqlens_q).numel() != batch + 1 or cache[2].shape[0] < batch:
+        raise ValueError("cu_seqlens_q has one entry more than kv_lens, and the block table a row for each sequence")
+    if _row_list(cu_groups).numel() != groups + 1:
+        raise ValueError("cu_groups has one entry more than shared_lens")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out is a contiguous tensor of the shape and element type of q")
+    if lse is not None:
+        if lse.shape != (total, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("lse is a contiguous float32 [tokens, q_heads] tensor")
+    elif return_lse:
+        lse = torch.empty((total, heads), dtype=torch.float32, device=q.device)
+    need = lib.rpx_group_attn_workspace_bytes(desc, total, batch, groups, max_q_len, max_group_tokens)
+    ws = _workspace(need, q.device, workspace)
+    rc = lib.rpx_group_attn(desc, q.data_ptr(), _tok_stride(q), cu_seqlens_q.data_ptr(), kv_lens.data_ptr(), batch, total, max_q_len,
+                            max_kv_len, cu_groups.data_ptr(), shared_lens.data_ptr(), groups, max_group_tokens,
+                            ctypes.byref(_cache_struct(cache)), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
+                            _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_group_attn")
+    return (out, lse) if return_lse else out
+
+
 @_in_call_context
 def token_logprobs(hidden, w_vocab, target_ids, logprobs=None, lse=None, return_lse: bool = False, workspace=None,
                    device_status=None, stream=None, entropy=None):
@@ -575,6 +657,59 @@ def token_logprobs_backward(hidden, w_vocab, target_ids, lse, upstream, dhidden=
     if rc != 0:
         raise RpxError(rc, "rpx_token_logprobs_backward_full")
     return (dhidden, dw) if with_dw else dhidden
+
+
+_RATIOS = {"token": 0, "sequence": 1}
+_MEANS = {"tokens": 0, "sequences": 1}
+
+
+@_in_call_context
+def policy_loss(logprobs, old_logprobs, advantages, cu_seqlens, mask=None, ref_logprobs=None, clip_low: float = 0.2,
+                clip_high: float = 0.2, clip_dual: float = 0.0, kl_coef: float = 0.0, kl: int = 3, ratio: str = "token",
+                mean: str = "sequences", count: float = 0.0, upstream=None, want_grad: bool = True, stats=None, dlogprobs=None,
+                workspace=None, device_status=None, stream=None):
+    """rpx_policy_loss: clipped policy loss with a KL term over packed log-probs (as ``token_logprobs`` returns them) and its
+    gradient (the ``upstream`` of ``token_logprobs_backward``).
+
+    logprobs, old_logprobs (None: on the policy itself), ref_logprobs float32 [T], packed by cu_seqlens int32 [B + 1];
+    advantages float32 [B], or [T] (then one per token; where B == T, two dimensions [T, 1] ask for one per token); mask bool
+    or uint8 [T].  ``ratio`` "token" or "sequence", ``mean`` "tokens" or "sequences", ``kl`` 1, 2 or 3 (0, or no ref_logprobs:
+    none), clip_dual 0: off, ``count`` > 0: the denominator in place of the call's own.  Returns (stats, dlogprobs): float32
+    [6] (loss, policy term, KL term, clipped share, mean ratio, counted tokens) and [T], None without ``want_grad``."""
+    torch = _torch()
+    lib = load_library()
+    _one_device(logprobs, old_logprobs, advantages, cu_seqlens, mask, ref_logprobs, upstream, stats, dlogprobs, workspace,
+                device_status)
+    n, f32 = logprobs.numel(), torch.float32
+    for t in (logprobs, old_logprobs, ref_logprobs, dlogprobs):
+        if t is not None and (t.dtype != f32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("log-probs and their gradient are contiguous float32 [tokens] tensors")
+    if mask is not None and (mask.dtype not in (torch.bool, torch.uint8) or mask.dim() != 1 or mask.numel() != n or not mask.is_contiguous()):
+        raise ValueError("mask is a contiguous bool or uint8 [tokens] tensor")
+    batch = _row_list(cu_seqlens).numel() - 1
+    if batch < 0:
+        raise ValueError("cu_seqlens has one entry more than there are sequences")
+    per_token = advantages.dim() == 2 or (advantages.numel() == n and n != batch)
+    if advantages.dtype != f32 or not advantages.is_contiguous() or advantages.shape not in (((n, 1),) if advantages.dim() == 2 else ((n,) if per_token else (batch,),)):
+        raise ValueError("advantages are contiguous float32, one for each sequence or one for each token")
+    if ratio not in _RATIOS or mean not in _MEANS:
+        raise ValueError('ratio is "token" or "sequence", mean is "tokens" or "sequences"')
+    for t, k in ((upstream, 1), (stats, 6)):
+        if t is not None and (t.dtype != f32 or t.numel() != k or not t.is_contiguous()):
+            raise ValueError("upstream is float32 [1] and stats float32 [6]")
+    if dlogprobs is None and want_grad:
+        dlogprobs = torch.empty_like(logprobs)
+    if stats is None:
+        stats = torch.empty(6, dtype=f32, device=logprobs.device)
+    desc = PolicyDesc(_RATIOS[ratio], _MEANS[mean], kl if ref_logprobs is not None else 0, 1 if per_token else 0, clip_low, clip_high,
+                      clip_dual, kl_coef, count)
+    ws = _workspace(lib.rpx_policy_loss_workspace_bytes(batch, n), logprobs.device, workspace)
+    rc = lib.rpx_policy_loss(ctypes.byref(desc), logprobs.data_ptr(), _ptr(old_logprobs), _ptr(ref_logprobs), advantages.data_ptr(),
+                             _ptr(mask), cu_seqlens.data_ptr(), batch, n, _ptr(upstream), stats.data_ptr(),
+                             _ptr(dlogprobs), ws.data_ptr(), ws.nbytes, _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_policy_loss")
+    return stats, dlogprobs
 
 
 @_in_call_context
@@ -723,15 +858,18 @@ def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) ->
     code = _dtype_code(q)
     if k.dtype != dtype:
         raise TypeError("q, k and the norm weights must share an element type")
-    if positions.dtype != torch.int32 or inv_freq.dtype != torch.float32:
+    if (positions is not None and positions.dtype != torch.int32) or inv_freq.dtype != torch.float32:
         raise TypeError("positions are int32 and inv_freq float32")
-    q_shape, k_shape, pos_shape = q.shape, k.shape, positions.shape
+    q_shape, k_shape = q.shape, k.shape
     if len(q_shape) != 3 or len(k_shape) != 3 or k_shape[0] != q_shape[0] or k_shape[2] != q_shape[2]:
         raise ValueError("expected q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim]")
     n, hq, d = q_shape
-    axes = pos_shape[0] if len(pos_shape) == 2 else 1
-    if len(pos_shape) not in (1, 2) or pos_shape[-1] != n or (n > 1 and positions.stride(-1) != 1):
-        raise ValueError("positions are [tokens] or [axes, tokens] with contiguous tokens")
+    axes = 1
+    if positions is not None:
+        pos_shape = positions.shape
+        axes = pos_shape[0] if len(pos_shape) == 2 else 1
+        if len(pos_shape) not in (1, 2) or pos_shape[-1] != n or (n > 1 and positions.stride(-1) != 1):
+            raise ValueError("positions are [tokens] or [axes, tokens] with contiguous tokens")
     if inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq is a contiguous [rot_dim / 2] tensor")
     for w in (q_weight, k_weight):
@@ -776,6 +914,40 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, pair_a
     if rc != 0:
         raise RpxError(rc, "rpx_qk_norm_rope")
     return q_out, k_out
+
+
+@_in_call_context
+def qk_norm_rope_append(q, k, v, positions, inv_freq, cu_append, cached_lens, max_append: int, cache: Tuple, q_weight=None,
+                        k_weight=None, pair_axis=None, eps: float = 1e-6, q_out=None, device_status=None, stream=None):
+    """rpx_qk_norm_rope_append: ``qk_norm_rope`` with k and v stored into the paged cache on the way: token cu_append[s] + i at
+    position cached_lens[s] + i of sequence s, as ``cache_append`` does (cached_lens stays as it is).
+
+    q [T, H_q, d], k, v [T, H_kv, d], such as views of one fused projection; positions as in ``qk_norm_rope``, or None: the
+    token's place in its sequence.  ``q_out`` may be q itself.  Returns q_out."""
+    lib = load_library()
+    _one_device(q, k, v, positions, inv_freq, cu_append, cached_lens, *cache, q_weight, k_weight, q_out, device_status)
+    cs = _cache_struct(cache)
+    shape = k.shape
+    if len(shape) != 3 or v.shape != shape or v.dtype != k.dtype or cache[0].shape[1:] != (shape[1], BLOCK_SIZE, shape[2]) or cache[1].shape != cache[0].shape:
+        raise ValueError("k and v are [tokens, kv_heads, head_dim] tensors that fit the cache pools")
+    if positions is None:
+        if pair_axis is not None:
+            raise ValueError("pair_axis names axes of positions")
+        desc, pos, axis_stride = _rope_desc(q, k, None, inv_freq, q_weight, k_weight, None, eps), None, 0
+    else:
+        desc = _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps)
+        pos, axis_stride = positions.data_ptr(), _axis_stride(positions)
+    q_out = _rope_out(q_out, q)
+    batch = _row_list(cached_lens).numel()
+    if _row_list(cu_append).numel() != batch + 1 or cache[2].shape[0] < batch:
+        raise ValueError("cu_append has one entry more than cached_lens, and the block table a row for each sequence")
+    rc = lib.rpx_qk_norm_rope_append(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), _tok_stride(q), _tok_stride(k),
+                                     _tok_stride(v), _ptr(q_weight), _ptr(k_weight), pos, axis_stride, inv_freq.data_ptr(), shape[0],
+                                     cu_append.data_ptr(), cached_lens.data_ptr(), batch, _bound(max_append), ctypes.byref(cs),
+                                     q_out.data_ptr(), _tok_stride(q_out), _ptr(device_status), _stream_ptr(stream))
+    if rc != 0:
+        raise RpxError(rc, "rpx_qk_norm_rope_append")
+    return q_out
 
 
 @_in_call_context

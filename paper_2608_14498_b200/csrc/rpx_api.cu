@@ -467,8 +467,8 @@ rpx_status_t rpx_attn_backward(const rpx_attn_desc_t* desc, const void* q, const
 
 namespace {
 
-// Checks shared by rpx_qk_norm_rope and its backward; `out_*` are the tensors the call writes.
-rpx_status_t check_rope(const RopeArgs& a) {
+// Checks shared by rpx_qk_norm_rope, its append form (a.v given) and its backward; `out_*` are the tensors the call writes.
+rpx_status_t check_rope(const RopeArgs& a, bool append = false) {
     const rpx_rope_desc_t* d = a.desc;
     if (d == nullptr) return RPX_ERR_NULL;
     if (d->dtype != RPX_BF16 && d->dtype != RPX_F32) return RPX_ERR_DTYPE;
@@ -482,13 +482,13 @@ rpx_status_t check_rope(const RopeArgs& a) {
     if (a.n_tokens < 0 || a.n_tokens >= INT32_MAX) return RPX_ERR_SHAPE;
     if ((a.q_weight == nullptr) != (a.k_weight == nullptr)) return RPX_ERR_NULL;
     if (a.n_tokens == 0) return RPX_OK;
-    if (a.q == nullptr || a.k == nullptr || a.positions == nullptr || a.inv_freq == nullptr || a.q_out == nullptr ||
-        a.k_out == nullptr)
+    if (a.q == nullptr || a.k == nullptr || (a.positions == nullptr && !append) || a.inv_freq == nullptr || a.q_out == nullptr ||
+        (a.k_out == nullptr && !append))
         return RPX_ERR_NULL;
     const int64_t q_row = static_cast<int64_t>(d->num_q_heads) * d->head_dim;
     const int64_t kv_row = static_cast<int64_t>(d->num_kv_heads) * d->head_dim;
-    if (a.q_tok_stride < q_row || a.k_tok_stride < kv_row || a.q_out_tok_stride < q_row || a.k_out_tok_stride < kv_row ||
-        (a.pos_axis_stride != 0 && a.pos_axis_stride < a.n_tokens))
+    if (a.q_tok_stride < q_row || a.k_tok_stride < kv_row || a.q_out_tok_stride < q_row || (a.k_out_tok_stride < kv_row && !append) ||
+        (a.pos_axis_stride != 0 && a.pos_axis_stride < a.n_tokens && a.positions != nullptr))
         return RPX_ERR_SHAPE;
     if (a.q_tok_stride % 8 || a.k_tok_stride % 8 || a.q_out_tok_stride % 8 || a.k_out_tok_stride % 8) return RPX_ERR_ALIGN;
     if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.q_weight) || !aligned16(a.k_weight) || !aligned16(a.q_out) ||
@@ -526,6 +526,49 @@ rpx_status_t rpx_qk_norm_rope(const rpx_rope_desc_t* desc, const void* q, const 
     if (n_tokens == 0) return RPX_OK;
     if (rpx_status_t rc = check_arch()) return rc;
     return launch_qk_rope(a);
+}
+
+rpx_status_t rpx_qk_norm_rope_append(const rpx_rope_desc_t* desc, const void* q, const void* k, const void* v, int64_t q_tok_stride,
+                                     int64_t k_tok_stride, int64_t v_tok_stride, const void* q_weight, const void* k_weight,
+                                     const int32_t* positions, int64_t pos_axis_stride, const float* inv_freq, int64_t n_tokens,
+                                     const int32_t* cu_append, const int32_t* cached_lens, int32_t batch, int32_t max_append,
+                                     const rpx_kv_cache_t* cache, void* q_out, int64_t q_out_tok_stride, int32_t* device_status,
+                                     void* cuda_stream) {
+    RopeArgs a;
+    a.desc = desc;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_tok_stride = q_tok_stride;
+    a.k_tok_stride = k_tok_stride;
+    a.v_tok_stride = v_tok_stride;
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.positions = positions;
+    a.pos_axis_stride = pos_axis_stride;
+    a.inv_freq = inv_freq;
+    a.n_tokens = n_tokens;
+    a.q_out = q_out;
+    a.k_out = nullptr;
+    a.q_out_tok_stride = q_out_tok_stride;
+    a.k_out_tok_stride = 0;
+    a.cu = cu_append;
+    a.cached_lens = cached_lens;
+    a.batch = batch;
+    a.max_append = max_append;
+    a.device_status = device_status;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rpx_status_t rc = check_rope(a, true)) return rc;
+    if (cache == nullptr) return RPX_ERR_NULL;
+    if (batch < 0 || max_append < 0) return RPX_ERR_SHAPE;
+    if (n_tokens == 0 || batch == 0 || max_append == 0) return RPX_OK;  // (an empty table or pool has no pointer)
+    if (rpx_status_t rc = check_cache(cache, batch)) return rc;
+    if (v == nullptr || cu_append == nullptr || cached_lens == nullptr) return RPX_ERR_NULL;
+    if (v_tok_stride < static_cast<int64_t>(desc->num_kv_heads) * desc->head_dim) return RPX_ERR_SHAPE;
+    if (!aligned16(v) || v_tok_stride % 8) return RPX_ERR_ALIGN;
+    if (rpx_status_t rc = check_arch()) return rc;
+    a.cache = *cache;
+    return launch_qk_rope_append(a);
 }
 
 size_t rpx_qk_norm_rope_backward_workspace_bytes(const rpx_rope_desc_t* desc, int64_t n_tokens) {
@@ -724,6 +767,115 @@ rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_tok_stride
     a.device_status = device_status;
     a.stream = static_cast<cudaStream_t>(cuda_stream);
     return launch_append(a);
+}
+
+size_t rpx_policy_loss_workspace_bytes(int32_t batch, int64_t n_tokens) {
+    return batch <= 0 || n_tokens <= 0 || n_tokens >= INT32_MAX ? 0 : align_up(policy_workspace(batch, n_tokens), kWsAlign);
+}
+
+rpx_status_t rpx_policy_loss(const rpx_policy_desc_t* desc, const float* logprobs, const float* old_logprobs,
+                             const float* ref_logprobs, const float* advantages, const uint8_t* mask, const int32_t* cu_seqlens,
+                             int32_t batch, int64_t n_tokens, const float* upstream, float* stats, float* dlogprobs,
+                             void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream) {
+    if (desc == nullptr) return RPX_ERR_NULL;
+    if ((desc->ratio != RPX_RATIO_TOKEN && desc->ratio != RPX_RATIO_SEQUENCE) || desc->kl < 0 || desc->kl > 3 ||
+        (desc->mean != RPX_MEAN_TOKENS && desc->mean != RPX_MEAN_SEQUENCES) || (desc->adv_per_token != 0 && desc->adv_per_token != 1))
+        return RPX_ERR_SHAPE;
+    if (desc->adv_per_token != 0 && desc->ratio == RPX_RATIO_SEQUENCE) return RPX_ERR_SHAPE;
+    if (!(desc->clip_low >= 0.0 && desc->clip_low < 1.0) || !(desc->clip_high >= 0.0) || !(desc->count >= 0.0) ||
+        !(desc->clip_dual == 0.0 || desc->clip_dual > 1.0) || desc->kl_coef != desc->kl_coef)
+        return RPX_ERR_SHAPE;
+    if (batch < 0 || n_tokens < 0 || n_tokens >= INT32_MAX || batch == INT32_MAX) return RPX_ERR_SHAPE;
+    if (stats == nullptr) return RPX_ERR_NULL;
+    const bool empty = batch == 0 || n_tokens == 0;  // the statistics are zeros
+    if (!empty) {
+        if (logprobs == nullptr || advantages == nullptr || cu_seqlens == nullptr || (desc->kl != 0 && ref_logprobs == nullptr))
+            return RPX_ERR_NULL;
+        const size_t need = rpx_policy_loss_workspace_bytes(batch, n_tokens);
+        if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return RPX_ERR_WORKSPACE;
+        if (need > 0 && !aligned_ws(workspace)) return RPX_ERR_ALIGN;
+    }
+    for (const void* t : {static_cast<const void*>(logprobs), static_cast<const void*>(old_logprobs), static_cast<const void*>(ref_logprobs),
+                          static_cast<const void*>(advantages), static_cast<const void*>(dlogprobs), static_cast<const void*>(stats),
+                          static_cast<const void*>(upstream), static_cast<const void*>(cu_seqlens)})
+        if ((reinterpret_cast<uintptr_t>(t) & 3u) != 0) return RPX_ERR_ALIGN;
+    if (rpx_status_t rc = check_arch()) return rc;
+    PolicyArgs a;
+    a.desc = desc;
+    a.logprobs = logprobs;
+    a.old_logprobs = old_logprobs;
+    a.ref_logprobs = desc->kl != 0 ? ref_logprobs : nullptr;
+    a.advantages = advantages;
+    a.mask = mask;
+    a.cu = cu_seqlens;
+    a.batch = batch;
+    a.n_tokens = n_tokens;
+    a.upstream = upstream;
+    a.stats = stats;
+    a.dlogprobs = dlogprobs;
+    a.workspace = workspace;
+    a.device_status = device_status;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    return launch_policy_loss(a);
+}
+
+size_t rpx_group_attn_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_q_tokens, int32_t batch, int32_t n_groups,
+                                      int32_t max_q_len, int32_t max_group_tokens) {
+    // (the query may come before the call that refuses the descriptor)
+    if (check_attn_desc(desc) != RPX_OK || desc->num_q_heads / desc->num_kv_heads > 128 || total_q_tokens <= 0 || batch <= 0 ||
+        n_groups < 0 || max_q_len <= 0 || max_group_tokens < 0)
+        return 0;
+    return align_up(group_workspace(desc, total_q_tokens, batch, n_groups, max_q_len, max_group_tokens), kWsAlign);
+}
+
+rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t q_tok_stride, const int32_t* cu_seqlens_q,
+                            const int32_t* kv_lens, int32_t batch, int64_t total_q_tokens, int32_t max_q_len, int32_t max_kv_len,
+                            const int32_t* cu_groups, const int32_t* shared_lens, int32_t n_groups, int32_t max_group_tokens,
+                            const rpx_kv_cache_t* cache, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            int32_t* device_status, void* cuda_stream) {
+    if (rpx_status_t rc = check_attn_desc(desc)) return rc;
+    if (desc->num_q_heads / desc->num_kv_heads > 128) return RPX_ERR_SHAPE;
+    if (batch < 0 || total_q_tokens < 0 || total_q_tokens >= INT32_MAX || max_q_len < 0 || max_kv_len < 0 || n_groups < 0 ||
+        max_group_tokens < 0)
+        return RPX_ERR_SHAPE;
+    if (cache == nullptr) return RPX_ERR_NULL;
+    if (batch == 0 || total_q_tokens == 0 || max_q_len == 0) return RPX_OK;  // (an empty table or pool has no pointer)
+    if (rpx_status_t rc = check_cache(cache, batch)) return rc;
+    if (q == nullptr || out == nullptr || cu_seqlens_q == nullptr || kv_lens == nullptr) return RPX_ERR_NULL;
+    if (n_groups > 0 && (cu_groups == nullptr || shared_lens == nullptr)) return RPX_ERR_NULL;
+    if (!aligned16(q) || !aligned16(out)) return RPX_ERR_ALIGN;
+    if (q_tok_stride < static_cast<int64_t>(desc->num_q_heads) * desc->head_dim) return RPX_ERR_SHAPE;
+    if (q_tok_stride % 8) return RPX_ERR_ALIGN;
+    GroupArgs a;
+    a.num_q_heads = desc->num_q_heads;
+    a.num_kv_heads = desc->num_kv_heads;
+    a.head_dim = desc->head_dim;
+    a.softmax_scale = desc->softmax_scale;
+    a.dtype = desc->dtype;
+    a.q = q;
+    a.q_tok_stride = q_tok_stride;
+    a.cu = cu_seqlens_q;
+    a.kv_lens = kv_lens;
+    a.batch = batch;
+    a.total_tokens = total_q_tokens;
+    a.max_q = max_q_len;
+    a.max_kv = max_kv_len;
+    a.cu_groups = cu_groups;
+    a.shared_lens = shared_lens;
+    a.n_groups = n_groups;
+    a.max_group = max_group_tokens;
+    a.cache = cache;
+    a.out = out;
+    a.lse = lse;
+    a.workspace = workspace;
+    a.device_status = device_status;
+    a.stream = static_cast<cudaStream_t>(cuda_stream);
+    if (group_too_large(a)) return RPX_ERR_SHAPE;
+    const size_t need = rpx_group_attn_workspace_bytes(desc, total_q_tokens, batch, n_groups, max_q_len, max_group_tokens);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return RPX_ERR_WORKSPACE;
+    if (need > 0 && !aligned_ws(workspace)) return RPX_ERR_ALIGN;
+    if (rpx_status_t rc = check_arch()) return rc;
+    return launch_group_attn(a);
 }
 
 rpx_status_t rpx_selftest_bounded_wait(int64_t limit_cycles, int32_t* device_status, void* cuda_stream) {

@@ -208,14 +208,78 @@ struct RopeArgs {
     float *dq_weight = nullptr, *dk_weight = nullptr;  // backward only, nullable
     bool accumulate_dw = false;
     void* workspace = nullptr;           // backward: one partial row per CTA
+    // append only (k_out is not used, positions may be NULL)
+    const void* v = nullptr;
+    int64_t v_tok_stride = 0;
+    const int32_t *cu = nullptr, *cached_lens = nullptr;
+    int32_t batch = 0, max_append = 0;
+    rpx_kv_cache_t cache = {};
+    int32_t* device_status = nullptr;
     cudaStream_t stream;
 };
 constexpr int kRopeBwdCtasPerSm = 4, kRopeBwdMaxCtas = 1024;
 size_t rope_backward_workspace(int32_t head_dim);
 rpx_status_t launch_qk_rope(const RopeArgs& a);
+rpx_status_t launch_qk_rope_append(const RopeArgs& a);
 rpx_status_t launch_qk_rope_backward(const RopeArgs& a);
 
+struct PolicyArgs {
+    const rpx_policy_desc_t* desc;
+    const float *logprobs, *old_logprobs, *ref_logprobs, *advantages;
+    const uint8_t* mask;
+    const int32_t* cu;
+    int32_t batch;
+    int64_t n_tokens;
+    const float* upstream;
+    float *stats, *dlogprobs;
+    void* workspace;
+    int32_t* device_status;
+    cudaStream_t stream;
+};
+size_t policy_workspace(int32_t batch, int64_t n_tokens);
+rpx_status_t launch_policy_loss(const PolicyArgs& a);
+
+struct GroupArgs {
+    int32_t num_q_heads, num_kv_heads, head_dim;
+    float softmax_scale;
+    rpx_dtype_t dtype;
+    const void* q;
+    int64_t q_tok_stride;
+    const int32_t *cu, *kv_lens;         // [batch + 1], [batch]
+    int32_t batch;
+    int64_t total_tokens;
+    int32_t max_q, max_kv;
+    const int32_t *cu_groups, *shared_lens;  // [n_groups + 1], [n_groups]
+    int32_t n_groups, max_group;
+    const rpx_kv_cache_t* cache;
+    void* out;
+    float* lse;
+    void* workspace;
+    int32_t* device_status;
+    cudaStream_t stream;
+};
+size_t group_workspace(const rpx_attn_desc_t* desc, int64_t total_tokens, int32_t batch, int32_t n_groups, int32_t max_q,
+                       int32_t max_group);
+bool group_too_large(const GroupArgs& a);  // sizes that a launch of the pass cannot hold
+rpx_status_t launch_group_attn(const GroupArgs& a);
+
 rpx_status_t launch_bounded_wait_selftest(long long limit_cycles, int32_t* status, cudaStream_t stream);
+
+// Launches a kernel that may start before the one in front of it has ended (it waits by itself where it has to).
+template <class Kernel, class... Args>
+rpx_status_t launch_on_top(Kernel* kernel, unsigned grid, unsigned threads, size_t smem, cudaStream_t stream, const Args&... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(grid);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...) == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+}
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -16,6 +16,10 @@
 // Measured with 28 + 4 heads of 128, bf16, inputs beyond L2: forward of 32768 tokens 86 us, backward of 34816 tokens 183 us,
 // both 95 % of the copy bandwidth.  float32: forward of 8192 tokens 48 us (86 %), of 32768 172 us (95 %); backward 79 us
 // (78 %) and 270 us (91 %).
+//
+// The append form (rpx_qk_norm_rope_append) is the forward pass with two more destinations: a row of k goes to its token's
+// slot of the paged cache instead of k_out, and the rows of v follow as units of their own that are only copied there.  A warp
+// finds its token's sequence by itself, 32 offsets a step, while its first rows are on their way.
 #include <cuda_bf16.h>
 
 #include "rpx_internal.h"
@@ -27,6 +31,18 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kMaxPairs = 64;
+constexpr int kPage = 16;
+
+struct Append {
+    const void* v;
+    int64_t v_stride;
+    const int32_t *cu, *lens;         // [batch + 1], [batch]
+    int32_t batch, max_append;
+    const int32_t* table;
+    int32_t table_stride, num_blocks;
+    __nv_bfloat16 *k_cache, *v_cache;
+    int32_t* status;
+};
 
 struct Params {
     const void *q, *k;
@@ -38,19 +54,21 @@ struct Params {
     const float* inv_freq;            // [rot / 2]
     int64_t n_tokens;
     int32_t num_q_heads, num_kv_heads, rot;
-    int32_t units_q, units, units_per_warp, warps_per_token;  // a unit = the rows one warp holds at once
+    int32_t units_q, units_qk, units, units_per_warp, warps_per_token;  // a unit = the rows one warp holds at once
     float eps;
     bool wide;                        // every float32 tensor starts on 32 bytes
     const float *dq, *dk;             // backward: [tokens][heads][D] contiguous
     float* dw_partial;                // backward: [grid][2][D], or NULL
+    Append append;                    // append form only
     uint8_t axis[kMaxPairs];
 };
 
 // cos and sin of this token's angles.  The angle is reduced in 64 bits (position * frequency loses whole radians in 32
 // bits at far positions): in units of half a turn, brought into [-1, 1], which 32 bits hold to 2^-25 of a half turn.
-__device__ __forceinline__ void token_angles(const Params& p, int64_t token, int lane, float2* cs) {
+// `place`: the position on every axis where there are no positions (append form).
+__device__ __forceinline__ void token_angles(const Params& p, int64_t token, int lane, float2* cs, int32_t place = 0) {
     for (int i = lane; i < (p.rot >> 1); i += 32) {
-        const double pos = static_cast<double>(__ldg(p.positions + p.axis[i] * p.pos_stride + token));
+        const double pos = static_cast<double>(p.positions == nullptr ? place : __ldg(p.positions + p.axis[i] * p.pos_stride + token));
         const double half_turns = pos * (static_cast<double>(__ldg(p.inv_freq + i)) * 0.31830988618379067154);
         const float x = static_cast<float>(half_turns - 2.0 * rint(half_turns * 0.5));
         float s, c;
@@ -80,6 +98,17 @@ struct Bf16 {
             w[i] = pack_bf16x2(lo, hi);
         }
         __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    // into the cache, where the attention call reads it next (a value that came as bf16 is stored as it was)
+    static __device__ __forceinline__ void keep(Elem* p, const uint64_t (&x)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            f2_unpack(x[i], lo, hi);
+            w[i] = pack_bf16x2(lo, hi);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 
@@ -182,8 +211,50 @@ __device__ __forceinline__ void stage_weights(const Params& p, float (*w)[D]) {
     __syncthreads();
 }
 
+// Where the append form stores a token: its place in its sequence, and its page's first row for head 0 (-1: nowhere, the page
+// number is none of the pool's).  False: the token is in no sequence, or in one that does not fit.
+struct Slot {
+    int32_t place;
+    int64_t row;
+};
+__device__ __forceinline__ bool find_slot(const Append& a, int64_t token, int64_t n_tokens, int32_t num_kv_heads, int lane, Slot* slot) {
+    // the last sequence that starts at or before the token, 32 offsets a step: [lo, hi) holds it
+    int32_t lo = 0, hi = a.batch;
+    while (hi - lo > 1) {
+        const int32_t step = (hi - lo + 31) / 32;
+        const int64_t at = lo + static_cast<int64_t>(lane) * step;
+        const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(a.cu + at) <= token);
+        const int32_t last = before != 0u ? 31 - __clz(static_cast<int>(before)) : 0;
+        lo += last * step;
+        hi = hi - lo > step ? lo + step : hi;
+    }
+    const int32_t begin = __ldg(a.cu + lo), end = __ldg(a.cu + lo + 1), len = __ldg(a.lens + lo);
+    if (token < begin || token >= end || begin < 0 || end > n_tokens || end - begin > a.max_append || len < 0) return false;
+    const int64_t pos = len + (token - begin);
+    if ((static_cast<int64_t>(len) + (end - begin) + kPage - 1) / kPage > a.table_stride) return false;
+    const int32_t page = __ldg(a.table + static_cast<int64_t>(lo) * a.table_stride + pos / kPage);
+    slot->place = static_cast<int32_t>(pos);
+    slot->row = page >= 0 && page < a.num_blocks ? static_cast<int64_t>(page) * num_kv_heads * kPage + pos % kPage : -1;
+    return true;
+}
+// Offsets, lengths and bounds of all sequences, looked at by one block of the launch.
+__device__ __forceinline__ void check_sequences(const Append& a, int64_t n_tokens) {
+    bool bad = false;
+    for (int32_t s = threadIdx.x; s < a.batch; s += blockDim.x) {
+        const int32_t begin = __ldg(a.cu + s), end = __ldg(a.cu + s + 1), len = __ldg(a.lens + s);
+        if (begin == end) {
+            bad |= begin < 0 || begin > n_tokens;
+            continue;
+        }
+        bad |= begin < 0 || end < begin || end > n_tokens || static_cast<int64_t>(end) - begin > a.max_append || len < 0 ||
+               (static_cast<int64_t>(len) + end - begin + kPage - 1) / kPage > a.table_stride;
+    }
+    if (bad && a.status != nullptr) atomicCAS(a.status, 0, RPX_ERR_DEVICE_DATA);
+}
+
 // The loads run a batch ahead of the arithmetic, the first batch in front of the angles: a warp always has rows in flight.
-template <class T, int D, bool kNorm>
+// Units are the rows of q, then of k and, in the append form, of v.
+template <class T, int D, bool kNorm, bool kAppend>
 __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6 : 4) qk_rope_kernel(const __grid_constant__ Params p) {
     typedef LaneMap<D> Map;
     typedef typename T::Elem Elem;
@@ -194,7 +265,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
     const int64_t task = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
     const int64_t token = task / p.warps_per_token;
     const int32_t u_begin = static_cast<int32_t>(task - token * p.warps_per_token) * p.units_per_warp;
-    const int32_t u_end = token < p.n_tokens ? min(p.units, u_begin + p.units_per_warp) : 0;
+    int32_t u_end = token < p.n_tokens ? min(p.units, u_begin + p.units_per_warp) : 0;
     const Map map(lane, p.rot);
     const Elem* const q = static_cast<const Elem*>(p.q) + token * p.q_stride;
     const Elem* const k = static_cast<const Elem*>(p.k) + token * p.k_stride;
@@ -203,16 +274,25 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
     auto load = [&](typename T::Raw (&raw)[kUnroll][2], int32_t u0) {
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
-            const bool is_q = u0 + i < p.units_q;
-            const int32_t head = (u0 + i - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
+            const bool is_q = u0 + i < p.units_q, is_v = kAppend && u0 + i >= p.units_qk;
+            const int32_t head = (u0 + i - (is_q ? 0 : is_v ? p.units_qk : p.units_q)) * Map::kRows + map.row;
             const Elem* src = (is_q ? q : k) + head * D;
+            if (is_v) src = static_cast<const Elem*>(p.append.v) + token * p.append.v_stride + head * D;
             const bool there = u0 + i < u_end && head < (is_q ? p.num_q_heads : p.num_kv_heads);
             raw[i][0] = there ? T::load(src + map.off_a, p.wide) : T::zero();
             raw[i][1] = there ? T::load(src + map.off_b, p.wide) : T::zero();
         }
     };
     load(now, u_begin);
-    if (u_begin < u_end) token_angles(p, token, lane, cs_all[warp]);
+    [[maybe_unused]] Slot slot = {0, -1};
+    if constexpr (kAppend) {
+        if (blockIdx.x == 0) check_sequences(p.append, p.n_tokens);
+        if (u_begin < u_end) {
+            if (!find_slot(p.append, token, p.n_tokens, p.num_kv_heads, lane, &slot)) u_end = 0;
+            else if (slot.row < 0 && u_begin == 0 && lane == 0 && p.append.status != nullptr) atomicCAS(p.append.status, 0, RPX_ERR_DEVICE_DATA);
+        }
+    }
+    if (u_begin < u_end) token_angles(p, token, lane, cs_all[warp], slot.place);
     if (kNorm) stage_weights<T, D>(p, weight);
     if (u_begin >= u_end) return;
     uint64_t c[4], s[4];
@@ -223,12 +303,12 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
 #pragma unroll
         for (int i = 0; i < kUnroll; ++i) {
             if (u0 + i >= u_end) break;
-            const bool is_q = u0 + i < p.units_q;
-            const int32_t head = (u0 + i - (is_q ? 0 : p.units_q)) * Map::kRows + map.row;
+            const bool is_q = u0 + i < p.units_q, is_v = kAppend && u0 + i >= p.units_qk;
+            const int32_t head = (u0 + i - (is_q ? 0 : is_v ? p.units_qk : p.units_q)) * Map::kRows + map.row;
             uint64_t a[4], b[4];
             T::unpack(now[i][0], a);
             T::unpack(now[i][1], b);
-            if (kNorm) {
+            if (kNorm && !is_v) {
                 uint64_t ss = 0ull, st = 0ull;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -245,7 +325,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
 #pragma unroll
                 for (int e = 0; e < 4; ++e) b[e] = f2_mul(f2_mul(b[e], r2), w[e]);
             }
-            if (map.turned) {
+            if (map.turned && !is_v) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint64_t x = a[e], y = b[e];
@@ -254,9 +334,17 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
                 }
             }
             if (head < (is_q ? p.num_q_heads : p.num_kv_heads)) {
-                Elem* dst = (is_q ? static_cast<Elem*>(p.q_out) + token * p.q_out_stride : static_cast<Elem*>(p.k_out) + token * p.k_out_stride) + head * D;
-                T::store(dst + map.off_a, a, p.wide);
-                T::store(dst + map.off_b, b, p.wide);
+                if (kAppend && !is_q) {
+                    if (slot.row >= 0) {
+                        __nv_bfloat16* dst = (is_v ? p.append.v_cache : p.append.k_cache) + (slot.row + static_cast<int64_t>(head) * kPage) * D;
+                        Bf16::keep(dst + map.off_a, a);
+                        Bf16::keep(dst + map.off_b, b);
+                    }
+                } else {
+                    Elem* dst = (is_q ? static_cast<Elem*>(p.q_out) + token * p.q_out_stride : static_cast<Elem*>(p.k_out) + token * p.k_out_stride) + head * D;
+                    T::store(dst + map.off_a, a, p.wide);
+                    T::store(dst + map.off_b, b, p.wide);
+                }
             }
         }
 #pragma unroll
@@ -448,19 +536,20 @@ __global__ void dw_reduce_kernel(const float* __restrict__ partial, int n, int d
 void split_heads(Params& p, int head_dim, int sms) {
     const int rows = 32 / (head_dim / 16);
     p.units_q = (p.num_q_heads + rows - 1) / rows;
-    p.units = p.units_q + (p.num_kv_heads + rows - 1) / rows;
+    p.units_qk = p.units_q + (p.num_kv_heads + rows - 1) / rows;
+    p.units = p.append.v == nullptr ? p.units_qk : 2 * p.units_qk - p.units_q;
     int64_t want = p.n_tokens > 0 ? (static_cast<int64_t>(sms) * 16 + p.n_tokens - 1) / p.n_tokens : 1;
     if (want > p.units) want = p.units;
     p.units_per_warp = static_cast<int32_t>((p.units + want - 1) / want);
     p.warps_per_token = (p.units + p.units_per_warp - 1) / p.units_per_warp;
 }
 
-template <class T, int D>
+template <class T, int D, bool kAppend = false>
 rpx_status_t launch_forward(const Params& p, cudaStream_t stream) {
     const int64_t blocks = (p.n_tokens * p.warps_per_token + kWarps - 1) / kWarps;
     if (blocks > INT32_MAX) return RPX_ERR_SHAPE;
-    if (p.q_weight != nullptr) qk_rope_kernel<T, D, true><<<static_cast<unsigned>(blocks), kWarps * 32, 0, stream>>>(p);
-    else qk_rope_kernel<T, D, false><<<static_cast<unsigned>(blocks), kWarps * 32, 0, stream>>>(p);
+    if (p.q_weight != nullptr) qk_rope_kernel<T, D, true, kAppend><<<static_cast<unsigned>(blocks), kWarps * 32, 0, stream>>>(p);
+    else qk_rope_kernel<T, D, false, kAppend><<<static_cast<unsigned>(blocks), kWarps * 32, 0, stream>>>(p);
     return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
 }
 
@@ -509,11 +598,16 @@ Params make_params(const RopeArgs& a, int sms) {
     p.dk = a.dk;
     p.wide = true;
     for (const void* t : {a.q, a.k, static_cast<const void*>(a.q_out), static_cast<const void*>(a.k_out), static_cast<const void*>(a.dq),
-                          static_cast<const void*>(a.dk)})
+                          static_cast<const void*>(a.dk), a.v})
         p.wide = p.wide && (reinterpret_cast<uintptr_t>(t) & 31u) == 0;
     p.dw_partial = a.dq_weight != nullptr ? static_cast<float*>(a.workspace) : nullptr;
     for (int i = 0; i < kMaxPairs; ++i)
         p.axis[i] = a.desc->pair_axis != nullptr && i < p.rot / 2 ? a.desc->pair_axis[i] : 0;
+    p.append = {};
+    if (a.v != nullptr)
+        p.append = {a.v, a.v_tok_stride, a.cu, a.cached_lens, a.batch, a.max_append, a.cache.block_table, a.cache.block_table_stride,
+                    static_cast<int32_t>(a.cache.num_blocks), static_cast<__nv_bfloat16*>(a.cache.k_cache),
+                    static_cast<__nv_bfloat16*>(a.cache.v_cache), a.device_status};
     split_heads(p, a.desc->head_dim, sms);
     return p;
 }
@@ -531,6 +625,15 @@ rpx_status_t launch_qk_rope(const RopeArgs& a) {
     const bool bf16 = a.desc->dtype == RPX_BF16;
     if (a.desc->head_dim == 128) return bf16 ? launch_forward<Bf16, 128>(p, a.stream) : launch_forward<F32, 128>(p, a.stream);
     return bf16 ? launch_forward<Bf16, 64>(p, a.stream) : launch_forward<F32, 64>(p, a.stream);
+}
+
+rpx_status_t launch_qk_rope_append(const RopeArgs& a) {
+    const int sms = sm_count();
+    if (sms <= 0) return RPX_ERR_CUDA;
+    const Params p = make_params(a, sms);
+    const bool bf16 = a.desc->dtype == RPX_BF16;
+    if (a.desc->head_dim == 128) return bf16 ? launch_forward<Bf16, 128, true>(p, a.stream) : launch_forward<F32, 128, true>(p, a.stream);
+    return bf16 ? launch_forward<Bf16, 64, true>(p, a.stream) : launch_forward<F32, 64, true>(p, a.stream);
 }
 
 rpx_status_t launch_qk_rope_backward(const RopeArgs& a) {

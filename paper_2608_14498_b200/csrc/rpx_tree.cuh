@@ -463,22 +463,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32, 2) tree_join_tiles_kernel(con
     if (col0 == 0 && p.lse != nullptr) p.lse[out_row] = unused ? -CUDART_INF_F : (top + log2f(sum)) * kLn2;
 }
 
-// Launches a kernel that may start before the one in front of it has ended (it waits by itself where it has to).
-template <class Kernel, class... Args>
-rpx_status_t launch_on_top(Kernel* kernel, unsigned grid, unsigned threads, size_t smem, cudaStream_t stream, const Args&... args) {
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(grid);
-    config.blockDim = dim3(threads);
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    config.attrs = attr;
-    config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, kernel, args...) == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
-}
-
 template <int D, class Cut, int kSplit, int kJoinRows>
 rpx_status_t launch_join_split(const Params& p, cudaStream_t stream) {
     constexpr int per_block = kJoinWarps / kSplit * kJoinRows;
