@@ -476,7 +476,7 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *       one group (alone, if it shares nothing)
  *   shared_lens device int32 [n_groups]: tokens that the group's sequences have in common from position 0 on.  The table rows
  *       of the group name the same pages for the whole pages among them (as rpx_pages_fork leaves them); those are read once
- *       for the group, through its first row.  What is beyond is read through every sequence's own row.
+ *       for the group, through the row of its first sequence with queries.  What is beyond is read through every sequence's own.
  *   A group is computed without sharing, and reported (RPX_ERR_DEVICE_DATA), if its bounds or shared length do not fit: the
  *       shared tokens end in front of every member's first query.  A sequence whose offsets leave the packed tensors or the
  *       table, that has more queries than cached tokens, or more than max_q_len, is reported and its rows are left as they are.

@@ -1,117 +1,162 @@
-// Attention of groups of sequences over the paged cache, K and V of the queries' own tokens included.
+// Attention of groups of sequences over the paged cache, K and V of the queries' own tokens included: what runs in front of and
+// behind the kernel that walks the key tiles (rpx_group_tile.cu), and the float32 form.
 //
 // For query i of the n of a sequence with len cached tokens, query head h and KV head g = h / group:
 //     out = sum_{j <= len - n + i} softmax_j(scale * q . k_j) v_j
-//
-// This first form takes a warp per (token, head): four keys a step, eight lanes to a key with head_dim / 8 of its elements
-// each, and a running maximum and sum for each of the four; they are joined at the end of the row.
-#include <cuda_bf16.h>
-#include <math_constants.h>
-
-#include "rpx_internal.h"
-#include "rpx_ptx.cuh"
+// The keys of a group's shared pages and those of the sequence itself are summed apart, each with its own maximum m and sum l,
+// and joined: with M = max m,  l = sum l_i 2^(m_i - M),  out = sum o_i 2^(m_i - M) / l.
+#include "rpx_group.cuh"
 
 namespace rpx {
 
+namespace group {
+rpx_status_t launch_group_tile(const Params& p, int32_t head_dim, const rpx_kv_cache_t& cache, cudaStream_t stream);
+}
+
 namespace {
 
-constexpr int kPage = 16;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+using namespace group;
 
-struct Params {
-    const void* q;
-    int64_t q_stride;
-    const int32_t *cu, *lens;
-    int32_t batch;
-    int64_t total_tokens;
-    int32_t max_q, max_group;
-    const int32_t *cu_groups, *shared;
-    int32_t n_groups;
-    int32_t num_q_heads, num_kv_heads, group;
-    const int32_t* block_table;
-    int32_t block_table_stride, num_blocks;
-    const __nv_bfloat16 *k_cache, *v_cache;
-    float scale_log2;
-    void* out;
-    float* lse;
-    int32_t* status;
-};
+// ------------------------------------------------------------------ the plan
+// One block.  Every sequence gets its entry as if it were alone; groups that share are then given theirs, and their members'
+// keys begin behind it.  The first units are a running sum over all entries.
+constexpr int kPlanThreads = 1024;
 
-__device__ __forceinline__ void report(int32_t* status) {
-    if (status != nullptr) atomicCAS(status, 0, RPX_ERR_DEVICE_DATA);
-}
-
-// A sequence's queries and cached tokens; false where they do not fit (its rows are left as they are).
-struct Seq {
-    int32_t tok0, n, len;
-};
-__device__ __forceinline__ bool read_seq(const Params& p, int32_t s, Seq* q) {
-    const int32_t begin = __ldg(p.cu + s), end = __ldg(p.cu + s + 1);
-    q->tok0 = begin;
-    q->n = 0;
-    q->len = 0;
-    if (begin < 0 || end < begin || end > p.total_tokens) return false;
-    if (end == begin) return true;
-    q->len = __ldg(p.lens + s);
-    if (end - begin > p.max_q || q->len < end - begin || (static_cast<int64_t>(q->len) + kPage - 1) / kPage > p.block_table_stride) return false;
-    q->n = end - begin;
-    return true;
-}
-
-// The sequence that a token is in, or -1: the last that starts at or before it, 32 offsets a step (a warp together).
-__device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int lane, Seq* q) {
-    int32_t lo = 0, hi = p.batch;
-    while (hi - lo > 1) {
-        const int32_t step = (hi - lo + 31) / 32;
-        const int64_t at = lo + static_cast<int64_t>(lane) * step;
-        const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(p.cu + at) <= token);
-        lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
-        hi = hi - lo > step ? lo + step : hi;
+__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0) {
+    Entry e = {tok0, n, len, row, page0, 1, 0, 1};
+    if (n == 0 || len == 0) {
+        e.n = e.len = 0;
+        return e;
     }
-    return read_seq(p, lo, q) && token >= q->tok0 && token < static_cast<int64_t>(q->tok0) + q->n ? lo : -1;
+    e.tiles = len / kTile + (len % kTile != 0 ? 1 : 0);
+    // Blocks of at most `cap` rows; of at most 64 where the keys are few, so that probabilities keep their second term: over
+    // many keys the rounding averages out.
+    const int32_t rows = e.tiles <= 2 && p.cap > 64 ? 64 : p.cap, per = max(1, rows / p.group);
+    e.blocks = (n + per - 1) / per;
+    // A tile's 64 KB (D = 128) are 1.5 us of this SM's share of HBM once, or the work against a block.
+    const int32_t work = 4 + e.block_tokens() * p.group * 12 / 128;
+    e.weight = max((15 + e.blocks - 1) / e.blocks, work);
+    return e;
 }
 
-// Whether the bounds of all groups ascend (otherwise nothing is shared); by a whole block, which meets at a barrier here.
-__device__ __forceinline__ bool groups_ascend(const Params& p) {
-    bool good = true;
-    for (int32_t g = threadIdx.x; g < p.n_groups; g += blockDim.x) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
-    return __syncthreads_and(good) != 0;
-}
-
-// What a group shares: whole pages' tokens, 0 where it has nothing to share, -1 where it does not fit; its first and last
-// sequence and their query tokens.  A warp together.
-struct Group {
-    int32_t first, last, tok0, n, shared;
-};
-__device__ __forceinline__ Group read_group(const Params& p, int32_t g, int lane) {
-    Group r = {__ldg(p.cu_groups + g), __ldg(p.cu_groups + g + 1), 0, 0, -1};
-    const int32_t shared = __ldg(p.shared + g);
-    if (r.first < 0 || r.last < r.first || r.last > p.batch) return r;
-    if (shared < 0) return r;
-    bool fits = true;
-    for (int32_t s = r.first + lane; s < r.last; s += 32) {
+__global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_constant__ Params p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ int64_t sums[kPlanThreads / 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int32_t s = threadIdx.x; s < p.batch; s += kPlanThreads) {
         Seq q;
-        fits &= read_seq(p, s, &q) && (q.n == 0 || q.len - q.n >= shared);
+        if (!read_seq(p, s, &q)) report(p.status);
+        p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0);
+        p.seq_group[s] = -1;
     }
-    if (!__all_sync(0xffffffffu, fits)) return r;
-    if (r.first < r.last) {
-        r.tok0 = __ldg(p.cu + r.first);
-        r.n = __ldg(p.cu + r.last) - r.tok0;
+    const bool ascend = groups_ascend(p);  // (a barrier: the entries above are written)
+    for (int32_t g = warp; g < p.n_groups; g += kPlanThreads / 32) {
+        Group r = {0, 0, 0, 0, -1, 0, 0};
+        if (ascend) r = read_group(p, g, lane);
+        if (r.shared < 0 && lane == 0) report(p.status);
+        const bool shares = r.shared > 0 && r.members > 1;
+        if (lane == 0) p.entries[g] = make_entry(p, r.tok0, shares ? r.n : 0, r.shared, r.row, 0);
+        if (!shares) continue;
+        for (int32_t s = r.first + lane; s < r.last; s += 32) {
+            Seq q;
+            read_seq(p, s, &q);
+            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - r.shared : 0, s, r.shared / kPage);
+            p.seq_group[s] = g;
+        }
     }
-    if (r.n > p.max_group) return r;
-    r.shared = shared / kPage * kPage;
-    return r;
+    __syncthreads();
+    const int32_t count = p.n_groups + p.batch;
+    int64_t carry = 0;
+    for (int32_t base = 0; base < count; base += kPlanThreads) {
+        const int32_t e = base + threadIdx.x;
+        int64_t x = 0;
+        if (e < count) {
+            const Entry q = p.entries[e];
+            if (q.n > 0) x = q.segment_units() * q.blocks * p.num_kv_heads;
+        }
+        int64_t sum = x;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, sum, off);
+            if (lane >= off) sum += y;
+        }
+        __syncthreads();  // the sums of the round before have been read
+        if (lane == 31) sums[warp] = sum;
+        __syncthreads();
+        int64_t before = carry, total = carry;
+        for (int w = 0; w < kPlanThreads / 32; ++w) {
+            before += w < warp ? sums[w] : 0;
+            total += sums[w];
+        }
+        if (e < count) p.unit0[e] = before + sum - x;
+        carry = total;
+    }
+    if (threadIdx.x == 0) p.unit0[count] = carry;
 }
 
+// ------------------------------------------------------------------ the join
+// A warp per row (token, query head) that has more than one set to add up: the shared keys' pieces in order, then its own.
+constexpr int kJoinWarps = 8;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinWarps * 32) group_join_kernel(const __grid_constant__ Params p) {
+    constexpr int kCols = D / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t out_row = static_cast<int64_t>(blockIdx.x) * kJoinWarps + warp, token = out_row / p.num_q_heads;
+    if (token >= p.total_tokens) return;  // (never a whole block)
+    const int32_t h = static_cast<int32_t>(out_row - token * p.num_q_heads), kv_head = h / p.group, in_group = h - kv_head * p.group;
+    Seq seq;
+    const int32_t s = find_seq(p, token, lane, &seq);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // (of rows that are left out too: this grid never ends before that one)
+    if (s < 0) return;
+    const int32_t g = __ldcg(p.seq_group + s), count = p.n_groups + p.batch;
+    const int64_t size = piece_units(__ldcg(p.unit0 + count), p.ctas);
+    float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+    for (int kind = g < 0 ? 1 : 0; kind < 2; ++kind) {
+        const int32_t e = kind == 0 ? g : p.n_groups + s;
+        const Entry q = Walk::load(p, e);
+        const int32_t in = static_cast<int32_t>(token - q.tok0), per = q.block_tokens(), block = in / per;
+        const int32_t row = (in - block * per) * p.group + in_group;
+        const int64_t unit = __ldcg(p.unit0 + e) + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
+        const int64_t c0 = unit / size;
+        const int32_t pieces = static_cast<int32_t>((unit + static_cast<int64_t>(q.tiles - 1) * q.weight) / size - c0) + 1;
+        if (pieces == 1 && g < 0) return;  // written whole
+#pragma unroll 2
+        for (int32_t j = 0; j < pieces; ++j) {
+            // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
+            const int64_t slot = ((c0 + j) * 2 + (j == 0 ? 1 : 0)) * p.cap + row, own_row = kind * p.total_tokens * p.num_q_heads + out_row;
+            const float2 ml = pieces == 1 ? __ldcg(p.whole_ml + own_row) : __ldcg(p.part_ml + slot);
+            const float* o = (pieces == 1 ? p.whole_o + own_row * D : p.part_o + slot * D) + lane * kCols;
+            float v[kCols];
+            if constexpr (kCols == 4) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(o));
+            else *reinterpret_cast<float2*>(v) = __ldcg(reinterpret_cast<const float2*>(o));
+            if (ml.x == -CUDART_INF_F && ml.y == 0.f) continue;  // no key seen (a NaN sum, of nothing but NaN, goes on)
+            const float to = fmaxf(top, ml.x), keep = top == -CUDART_INF_F ? 0.f : fast_exp2(top - to);
+            const float f = ml.x == -CUDART_INF_F ? 1.f : fast_exp2(ml.x - to);
+            top = to;
+            sum = fmaf(sum, keep, f * ml.y);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) acc[i] = fmaf(acc[i], keep, f * v[i]);
+        }
+    }
+    const float inv = 1.f / sum;
+    uint32_t w[kCols / 2];
+#pragma unroll
+    for (int i = 0; i < kCols / 2; ++i) w[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + out_row * D + lane * kCols);
+    if constexpr (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    else *dst = w[0];
+    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = (top + log2f(sum)) * kLn2;
+}
+
+// ------------------------------------------------------------------ float32
+// For checking: a warp per (token, head); four keys a step, eight lanes to a key with D / 8 of its elements each, and a running
+// maximum and sum for each of the four, joined at the end of the row.  Bound by that walk.
 constexpr int kRowWarps = 4;
 
-__device__ __forceinline__ float load_q(const float* p) { return __ldg(p); }
-__device__ __forceinline__ float load_q(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void store_out(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_out(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
-
-template <class T, int D>
+template <int D>
 __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params p) {
     constexpr int U = D / 8;  // elements of a lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, part = lane & 7;
@@ -131,10 +176,10 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     const int32_t s = find_seq(p, token, lane, &seq);
     if (s < 0) return;
     float q[U], acc[U];
-    const T* src = static_cast<const T*>(p.q) + token * p.q_stride + static_cast<int64_t>(head) * D + part * U;
+    const float* src = static_cast<const float*>(p.q) + token * p.q_stride + static_cast<int64_t>(head) * D + part * U;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        q[u] = load_q(src + u) * p.scale_log2;
+        q[u] = __ldg(src + u) * p.scale_log2;
         acc[u] = 0.f;
     }
     float m = -CUDART_INF_F, l = 0.f;
@@ -189,58 +234,81 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     l *= f;
 #pragma unroll
     for (int off = 8; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-    T* dst = static_cast<T*>(p.out) + row * D + part * U;
+    float* dst = static_cast<float*>(p.out) + row * D + part * U;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         acc[u] *= f;
 #pragma unroll
         for (int off = 8; off < 32; off <<= 1) acc[u] += __shfl_xor_sync(0xffffffffu, acc[u], off);
-        if (sub == 0) store_out(dst + u, acc[u] / l);
+        if (sub == 0) dst[u] = acc[u] / l;
     }
     if (p.lse != nullptr && lane == 0) p.lse[row] = (top + log2f(l)) * kLn2;
 }
 
-template <class T>
-rpx_status_t launch_rows(const Params& p, const GroupArgs& a) {
-    const int64_t blocks = (a.total_tokens * a.num_q_heads + kRowWarps - 1) / kRowWarps;
-    if (a.head_dim == 128) group_rows_kernel<T, 128><<<static_cast<unsigned>(blocks), kRowWarps * 32, 0, a.stream>>>(p);
-    else group_rows_kernel<T, 64><<<static_cast<unsigned>(blocks), kRowWarps * 32, 0, a.stream>>>(p);
-    return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+int32_t rows_cap(int64_t rows, int32_t group) {
+    const int64_t most = rows > group ? rows : group;
+    return most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
+}
+int32_t cap_of(int32_t max_q, int32_t max_group, int32_t n_groups, int32_t group) {
+    const int32_t most = n_groups > 0 && max_group > max_q ? max_group : max_q;
+    return rows_cap(static_cast<int64_t>(most) * group, group);
+}
+constexpr int kMaxCtas = 148;
+
+// Carves the workspace (NULL: only measures it).
+size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t batch, int32_t cap, int32_t heads, int32_t head_dim, void* workspace) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        uint8_t* r = ws + at;
+        at += align_up(bytes, 256);
+        return r;
+    };
+    const size_t rows = static_cast<size_t>(tokens) * heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * cap;
+    p.entries = reinterpret_cast<Entry*>(take(static_cast<size_t>(entries) * sizeof(Entry)));
+    p.unit0 = reinterpret_cast<int64_t*>(take((static_cast<size_t>(entries) + 1) * sizeof(int64_t)));
+    p.seq_group = reinterpret_cast<int32_t*>(take(static_cast<size_t>(batch) * sizeof(int32_t)));
+    p.whole_ml = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
+    p.part_ml = reinterpret_cast<float2*>(take(slots * sizeof(float2)));
+    p.whole_o = reinterpret_cast<float*>(take(rows * head_dim * sizeof(float)));
+    p.part_o = reinterpret_cast<float*>(take(slots * head_dim * sizeof(float)));
+    return at;
 }
 
 }  // namespace
 
-size_t group_workspace(const rpx_attn_desc_t*, int64_t, int32_t, int32_t, int32_t, int32_t) { return 0; }
+size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t n_groups, int32_t max_q, int32_t max_group) {
+    if (d->dtype == RPX_F32 || batch > INT32_MAX - n_groups - 1) return 0;
+    Params p = {};
+    return carve(p, tokens, n_groups + batch, batch, cap_of(max_q, max_group, n_groups, d->num_q_heads / d->num_kv_heads), d->num_q_heads, d->head_dim, nullptr);
+}
 
-bool group_too_large(const GroupArgs& a) { return (a.total_tokens * a.num_q_heads + kRowWarps - 1) / kRowWarps > INT32_MAX; }
+bool group_too_large(const GroupArgs& a) {
+    if ((a.total_tokens * a.num_q_heads + kRowWarps - 1) / kRowWarps > INT32_MAX) return true;
+    return a.batch > INT32_MAX - a.n_groups - 1 || a.cache->num_blocks * a.num_kv_heads > INT32_MAX / 2;
+}
 
 rpx_status_t launch_group_attn(const GroupArgs& a) {
-    Params p = {};
-    p.q = a.q;
-    p.q_stride = a.q_tok_stride;
-    p.cu = a.cu;
-    p.lens = a.kv_lens;
-    p.batch = a.batch;
-    p.total_tokens = a.total_tokens;
-    p.max_q = a.max_q;
-    p.max_group = a.max_group;
-    p.cu_groups = a.cu_groups;
-    p.shared = a.shared_lens;
-    p.n_groups = a.n_groups;
-    p.num_q_heads = a.num_q_heads;
-    p.num_kv_heads = a.num_kv_heads;
-    p.group = a.num_q_heads / a.num_kv_heads;
-    p.block_table = a.cache->block_table;
-    p.block_table_stride = a.cache->block_table_stride;
-    p.num_blocks = static_cast<int32_t>(a.cache->num_blocks);
-    p.k_cache = static_cast<const __nv_bfloat16*>(a.cache->k_cache);
-    p.v_cache = static_cast<const __nv_bfloat16*>(a.cache->v_cache);
-    const float scale = a.softmax_scale > 0.f ? a.softmax_scale : 1.0f / sqrtf(static_cast<float>(a.head_dim));
-    p.scale_log2 = scale * kLog2e;
-    p.out = a.out;
-    p.lse = a.lse;
-    p.status = a.device_status;
-    return a.dtype == RPX_F32 ? launch_rows<float>(p, a) : launch_rows<__nv_bfloat16>(p, a);
+    Params p = make_params(a);
+    const int64_t rows = a.total_tokens * a.num_q_heads;
+    if (a.dtype == RPX_F32) {
+        const unsigned blocks = static_cast<unsigned>((rows + kRowWarps - 1) / kRowWarps);
+        if (a.head_dim == 128) group_rows_kernel<128><<<blocks, kRowWarps * 32, 0, a.stream>>>(p);
+        else group_rows_kernel<64><<<blocks, kRowWarps * 32, 0, a.stream>>>(p);
+        return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
+    }
+    const int sms = sm_count();
+    if (sms <= 0) return RPX_ERR_CUDA;
+    p.cap = cap_of(a.max_q, a.max_group, a.n_groups, p.group);
+    // (without the SM budget: where the line of tiles is cut decides the order of the sums)
+    p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
+    carve(p, a.total_tokens, a.n_groups + a.batch, a.batch, p.cap, a.num_q_heads, a.head_dim, a.workspace);
+    group_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
+    if (rpx_status_t rc = launch_group_tile(p, a.head_dim, *a.cache, a.stream)) return rc;
+    const unsigned blocks = static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps);
+    return a.head_dim == 128 ? launch_on_top(group_join_kernel<128>, blocks, kJoinWarps * 32, 0, a.stream, p)
+                             : launch_on_top(group_join_kernel<64>, blocks, kJoinWarps * 32, 0, a.stream, p);
 }
 
 }  // namespace rpx

@@ -1,0 +1,554 @@
+// Attention of groups of sequences over the paged cache: the kernel that walks the key tiles (bf16).
+//
+// Few query rows meet many keys here - 5 to 8 rows a sequence in a decoding step, some dozens where a group shares a prompt -
+// and every cached byte is read once, 512 bytes a key against rows * 512 flops.  So the KEYS are the tensor core's M: a key
+// tile's 128 keys are the 128 lanes of S^T = K Q^T, the rows are its columns, and what a tile costs grows with the rows that are
+// there (16 to 128 in steps of 16) instead of with a tile of 128 that holds them:
+//     S^T [128 keys x N rows]  = K [128 x D] (K-major, as it lies in the cache) * Q^T (K-major)
+//     O^T [D x N rows]        += V^T [D x 128] (V as it lies in the cache, read MN-major) * P^T [128 x N]
+// P goes through shared memory, as bf16 [row][key] (K-major B operand).  The scores are loaded from tensor memory in the fragment
+// that stmatrix takes (16 lanes x 256 bits: a thread holds two rows of one key), so a warp stores its 32 keys of eight rows
+// with one instruction.  While a block has at most half of P's room in rows, the other half takes what the rounding to bf16
+// dropped: probabilities enter the product as two terms (off by 2^-17) and not as one (2^-8), and the product is done twice,
+// which costs nothing where the cache's bytes bound.
+//
+// A row's running reference is raised only when a score passes it by 2^8: what is kept is exact whatever the reference, so all
+// the threads of a tile need to agree on is whether one of them has to (one barrier with a vote).
+//
+// Segments (a KV head's keys of a group's prompt or of one sequence) follow one another without a pause: two buffers each for S, P,
+// O and, but for the largest blocks, Q, so the tensor core is in the next segment while this one's output is written, and the
+// rings of K and V never drain.
+//   warps 0-3, 4-7 : softmax of the first and second half of the rows, lanes = keys; a segment's output, lanes = elements of D
+//   warp  8        : producer of K and V, one TMA box per 16-token page
+//   warp  9        : issues the products (one thread)
+//   warps 10, 11   : lay Q out
+#include "rpx_group.cuh"
+
+namespace rpx {
+
+namespace {
+
+using namespace group;
+
+constexpr int kThreads = 32 * 12;
+constexpr int kProducerWarp = 8, kMmaWarp = 9, kQWarp = 10, kQWarps = 2;
+constexpr int kPages = kTile / kPage;
+constexpr float kRaise = 8.0f;  // log2 units
+constexpr int kMaxSlots = 6;
+
+template <int D, int kCap>
+struct Layout {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTensorBytes = kTile * D * 2;             // a key tile of K or V
+    static constexpr int kPRows = kCap <= 64 ? 2 * kCap : 128;
+    static constexpr int kPHalfBytes = kPRows * 128;               // 64 keys of all rows
+    static constexpr int kPBytes = 2 * kPHalfBytes;
+    static constexpr int kQHalfBytes = kCap * 128;
+    static constexpr int kQBytes = kHalves * kQHalfBytes;
+    static constexpr int kQBufs = kQBytes <= 16384 ? 2 : 1;
+    static constexpr int kCtlBytes = 512 + 512 + 2048;             // barriers; references; exchange
+    static constexpr int kRoom = 232448 - kCtlBytes - 2 * kPBytes - kQBufs * kQBytes;
+    static constexpr int kFit = kRoom / kTensorBytes;
+    static constexpr int kSlotsK = (kFit + 1) / 2 < kMaxSlots ? (kFit + 1) / 2 : kMaxSlots;
+    static constexpr int kSlotsV = kFit / 2 < kMaxSlots ? kFit / 2 : kMaxSlots;
+    static constexpr int kVOff = kSlotsK * kTensorBytes;
+    static constexpr int kPOff = kVOff + kSlotsV * kTensorBytes;   // (V's last tile is followed by P: see the products)
+    static constexpr int kQOff = kPOff + 2 * kPBytes;
+    static constexpr int kCtlOff = kQOff + kQBufs * kQBytes;
+    static constexpr size_t kSmemBytes = kCtlOff + kCtlBytes;
+    static constexpr uint32_t kTmemCols = 4 * kCap;                // S twice, O twice
+};
+
+struct Ctl {
+    uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
+    uint64_t q_full[2], q_empty[2];
+    uint64_t s_full[2];   // tensor core -> softmax: scores of a tile (and the product two tiles before has read its P)
+    uint64_t p_ready[2];  // softmax -> tensor core
+    uint64_t pv_done;     // a tile's product with V has been added
+    uint64_t o_done[2];   // ... the last one of a segment
+    uint64_t o_free[2];   // softmax -> tensor core: the segment's output has been read
+    uint64_t drain;
+    uint32_t tmem_base, abort_flag, drain_flag, data_error;
+};
+static_assert(sizeof(Ctl) <= 512, "room of the barriers");
+
+// Key tiles lie as [group of 8 keys][half][8 rows][128 bytes], swizzled: a 16-token page is one TMA box.
+template <int D>
+__device__ __forceinline__ uint32_t key_off(int r, int c) {  // of 16-byte chunk c of key r
+    return static_cast<uint32_t>(((r >> 3) * (D / 64) + (c >> 3)) * 1024 + (r & 7) * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
+
+__device__ __forceinline__ void half_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool half_any(int id, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n"
+        " .reg .pred p, q;\n"
+        " setp.ne.u32 p, %2, 0;\n"
+        " bar.red.or.pred q, %1, 128, p;\n"
+        " selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(r) : "r"(id), "r"(x ? 1u : 0u) : "memory");
+    return r != 0u;
+}
+
+template <int D, int kCap>
+__global__ void __launch_bounds__(kThreads, 1)
+group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params p) {
+    using L = Layout<D, kCap>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    if ((smem_u32(smem) & 1023u) != 0u) {  // swizzled tiles need 1024-byte alignment; never expected
+        if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, RPX_ERR_CUDA);
+        return;
+    }
+    Ctl* ctl = reinterpret_cast<Ctl*>(smem + L::kCtlOff);
+    float* ref = reinterpret_cast<float*>(smem + L::kCtlOff + 512);        // [half][64]: (the halves may be in different segments)
+    float* exchange = reinterpret_cast<float*>(smem + L::kCtlOff + 1024);  // [half][warp][64]
+    volatile uint32_t* abort_flag = &ctl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kMaxSlots; ++i) {
+            mbar_init(&ctl->k_full[i], 1);
+            mbar_init(&ctl->k_empty[i], 1);
+            mbar_init(&ctl->v_full[i], 1);
+            mbar_init(&ctl->v_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&ctl->q_full[i], kQWarps);
+            mbar_init(&ctl->q_empty[i], 1);
+            mbar_init(&ctl->s_full[i], 1);
+            mbar_init(&ctl->p_ready[i], 8);
+            mbar_init(&ctl->o_done[i], 1);
+            mbar_init(&ctl->o_free[i], 8);
+        }
+        mbar_init(&ctl->pv_done, 1);
+        mbar_init(&ctl->drain, 1);
+        ctl->abort_flag = ctl->drain_flag = ctl->data_error = 0;
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(&ctl->tmem_base, L::kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = ctl->tmem_base;  // S at columns 0 and kCap, O at 2 kCap and 3 kCap
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
+    Walk walk;
+    walk.start(p);
+    auto rows16 = [&](const Walk& w) { return (w.tokens() * p.group + 15) & ~15; };
+
+    if (warp == kProducerWarp) {
+        // =========================================================== producer: K a tile ahead of V, through all segments
+        bool ok = true;
+        uint32_t nk = 0, nv = 0;
+        // the tile whose V comes next: page number of this lane's page, boxes, KV head
+        int32_t v_block = 0, v_boxes = 0, v_head = 0;
+        const int pg = lane & 7;
+        auto load = [&](const CUtensorMap* map, uint8_t* dst, uint64_t* full, int32_t block, int32_t boxes, int32_t head) {
+            if (lane == 0) mbar_arrive_expect_tx(full, static_cast<uint32_t>(boxes) * kPage * D * 2);
+            __syncwarp();  // the byte count is armed before any copy can complete
+            if (lane < boxes) tma_load_4d(dst + pg * (kPage * D * 2), map, full, 0, 0, 0, (block * p.num_kv_heads + head) * 2);
+            __syncwarp();
+        };
+        auto load_v = [&]() {
+            const uint32_t st = nv % L::kSlotsV;
+            if (!mbar_wait(&ctl->v_empty[st], ((nv / L::kSlotsV) & 1u) ^ 1u, abort_flag)) return false;
+            load(&tmap_v, smem + L::kVOff + st * L::kTensorBytes, &ctl->v_full[st], v_block, v_boxes, v_head);
+            ++nv;
+            return true;
+        };
+        while (ok && walk.next(p)) {
+            const int32_t* table = p.block_table + static_cast<int64_t>(walk.q.row) * p.block_table_stride + walk.q.page0;
+            const int32_t pages = (walk.q.len + kPage - 1) / kPage;
+            auto read_block = [&](int32_t t) { return t < walk.t1 && t * kPages + pg < pages ? __ldg(table + t * kPages + pg) : 0; };
+            int32_t next_block = read_block(walk.t0);
+            for (int32_t t = walk.t0; t < walk.t1; ++t) {
+                int32_t block = next_block;
+                next_block = read_block(t + 1);
+                if (block < 0 || block >= p.num_blocks) {
+                    ctl->data_error = 1;
+                    block = 0;
+                }
+                const int32_t boxes = min(kPages, pages - t * kPages);
+                const uint32_t st = nk % L::kSlotsK;
+                ok = mbar_wait(&ctl->k_empty[st], ((nk / L::kSlotsK) & 1u) ^ 1u, abort_flag);
+                if (!ok) break;
+                load(&tmap_k, smem + st * L::kTensorBytes, &ctl->k_full[st], block, boxes, walk.head);
+                ++nk;
+                if (nk > 1) ok = load_v();
+                if (!ok) break;
+                v_block = block;
+                v_boxes = boxes;
+                v_head = walk.head;
+            }
+        }
+        if (ok && nk > 0) ok = load_v();
+        if (!ok) {  // abort: copies still in flight get a moment to land before shared memory is released
+            for (uint32_t i = nk > L::kSlotsK ? nk - L::kSlotsK : 0u; i < nk; ++i)
+                mbar_wait(&ctl->k_full[i % L::kSlotsK], (i / L::kSlotsK) & 1u, &ctl->drain_flag, kDrainLimitCycles);
+            for (uint32_t i = nv > L::kSlotsV ? nv - L::kSlotsV : 0u; i < nv; ++i)
+                mbar_wait(&ctl->v_full[i % L::kSlotsV], (i / L::kSlotsV) & 1u, &ctl->drain_flag, kDrainLimitCycles);
+        }
+    } else if (warp == kMmaWarp) {
+        // =========================================================== tcgen05 issuer (one thread)
+        if (elect_one()) {
+            // D = 64: M stays 128, and the lanes 64 .. 127 of O^T, which nobody reads, are fed by whatever lies 1 KB on
+            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem), 16, L::kHalves * 1024);
+            const uint64_t v_desc = make_smem_desc_sw128(smem_u32(smem + L::kVOff), 1024, L::kHalves * 1024);
+            const uint64_t p_desc = make_smem_desc_sw128(smem_u32(smem + L::kPOff), 16, 1024);
+            const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem + L::kQOff), 16, 1024);
+            Walk ahead = walk;  // the scores run a tile ahead of the products with V, into the next segment too
+            bool ok = true, more = ahead.next(p);
+            int32_t at = ahead.t0;      // the tile whose scores come next
+            uint32_t q_segments = 0, segments = 0, tiles = 0, scored = 0;
+            auto issue_scores = [&]() {
+                const uint32_t st = scored % L::kSlotsK, b = scored & 1u, qb = q_segments % L::kQBufs;
+                if (at == ahead.t0 && !mbar_wait(&ctl->q_full[qb], (q_segments / L::kQBufs) & 1u, abort_flag)) return false;
+                if (!mbar_wait(&ctl->k_full[st], (scored / L::kSlotsK) & 1u, abort_flag)) return false;
+                tc_fence_after_sync();
+                const uint32_t idesc = make_idesc_bf16(128, rows16(ahead), false, false);
+                const uint64_t kd = k_desc + static_cast<uint64_t>(st * (L::kTensorBytes >> 4)), qd = q_desc + static_cast<uint64_t>(qb * (L::kQBytes >> 4));
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_bf16_ss(tmem_base + b * kCap, kd + (ks >> 2) * 64 + 2 * (ks & 3), qd + (ks >> 2) * (L::kQHalfBytes >> 4) + 2 * (ks & 3), idesc, ks != 0);
+                umma_commit(&ctl->s_full[b]);
+                umma_commit(&ctl->k_empty[st]);
+                ++scored;
+                if (++at == ahead.t1) {
+                    umma_commit(&ctl->q_empty[qb]);
+                    ++q_segments;
+                    more = ahead.next(p);
+                    at = ahead.t0;
+                }
+                return true;
+            };
+            if (more) ok = issue_scores();
+            while (ok && walk.next(p)) {
+                const int32_t n16 = rows16(walk);
+                const bool two_terms = 2 * n16 <= L::kPRows;
+                const uint32_t ob = segments & 1u;
+                const uint32_t idesc = make_idesc_bf16(128, n16, true, false);
+                for (int32_t t = walk.t0; t < walk.t1; ++t) {
+                    if (more) ok = issue_scores();
+                    const uint32_t b = tiles & 1u, st = tiles % L::kSlotsV;
+                    if (ok && t == walk.t0 && segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
+                    if (ok) ok = mbar_wait(&ctl->p_ready[b], (tiles >> 1) & 1u, abort_flag) && mbar_wait(&ctl->v_full[st], (tiles / L::kSlotsV) & 1u, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const int32_t steps = (min(kTile, walk.q.len - t * kTile) + 15) / 16;  // pages that were loaded
+                    const uint64_t vd = v_desc + static_cast<uint64_t>(st * (L::kTensorBytes >> 4)), pd = p_desc + static_cast<uint64_t>(b * (L::kPBytes >> 4));
+                    for (int32_t ks = 0; ks < steps; ++ks)
+                        umma_bf16_ss(tmem_base + (2 + ob) * kCap, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
+                                     pd + static_cast<uint64_t>((ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, t != walk.t0 || ks != 0);
+                    if (two_terms)
+                        for (int32_t ks = 0; ks < steps; ++ks)
+                            umma_bf16_ss(tmem_base + (2 + ob) * kCap, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
+                                         pd + static_cast<uint64_t>((L::kPRows / 2) * 8 + (ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, 1u);
+                    umma_commit(&ctl->v_empty[st]);
+                    umma_commit(&ctl->pv_done);
+                    if (t + 1 == walk.t1) umma_commit(&ctl->o_done[ob]);
+                    ++tiles;
+                }
+                ++segments;
+            }
+            if (!ok) {
+                umma_commit(&ctl->drain);
+                mbar_wait(&ctl->drain, 0, &ctl->drain_flag, kDrainLimitCycles);
+            }
+        }
+        __syncwarp();
+        // the join may start on the SMs that become free
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    } else if (warp >= kQWarp) {
+        // =========================================================== Q of a segment's rows, zeros up to the next 16
+        uint32_t segments = 0;
+        while (walk.next(p)) {
+            const uint32_t qb = segments % L::kQBufs;
+            if (segments >= L::kQBufs && !mbar_wait(&ctl->q_empty[qb], ((segments / L::kQBufs) - 1) & 1u, abort_flag)) break;
+            uint8_t* dst = smem + L::kQOff + qb * L::kQBytes;
+            const int32_t rows = walk.tokens() * p.group, n16 = rows16(walk);
+            const int64_t first = static_cast<int64_t>(walk.q.tok0) + walk.token0();
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + first * p.q_stride + static_cast<int64_t>(walk.head) * p.group * D;
+            constexpr int kBatch = 4, kChunks = D / 8;
+            for (int32_t i0 = threadIdx.x - kQWarp * 32; i0 < n16 * kChunks; i0 += kBatch * kQWarps * 32) {
+                uint4 x[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int32_t i = i0 + u * kQWarps * 32, r = i / kChunks, c = i % kChunks, token = r / p.group;
+                    x[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (r < rows) x[u] = __ldg(reinterpret_cast<const uint4*>(src + token * p.q_stride + (r - token * p.group) * D) + c);
+                }
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int32_t i = i0 + u * kQWarps * 32, r = i / kChunks, c = i % kChunks;
+                    if (r < n16) *reinterpret_cast<uint4*>(dst + (c >> 3) * L::kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = x[u];
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl->q_full[qb]);
+            ++segments;
+        }
+    } else {
+        // =========================================================== softmax and output
+        // After a wait that ran out (ok == false) a warp goes through the rest of its walk without waiting: every warp still meets
+        // the others at the same barriers, and the outputs of the call are undefined anyway.
+        constexpr int kBlocks = kCap / 16;  // 8-row blocks of a half at most
+        const int half = warp >> 2, quarter = warp & 3, bar = 1 + half;
+        const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
+        float* mine = exchange + (half * 4 + quarter) * 64;     // this warp's part of the exchange
+        const float* all = exchange + half * 4 * 64;
+        const int key0 = quarter * 32 + (lane >> 2);            // this thread's keys of a tile: key0 + 8 m
+        const int pair = 2 * (lane & 3);                        // its rows of an 8-row block: pair, pair + 1
+        uint32_t tiles = 0, segments = 0;
+        bool ok = true;
+        while (walk.next(p)) {
+            const int32_t len = walk.q.len, tokens = walk.tokens(), token0 = walk.token0(), rows = tokens * p.group, n16 = (rows + 15) & ~15;
+            const int32_t nb = n16 / 16, row0 = half * (n16 / 2);  // blocks and first row of this half
+            const bool two_terms = 2 * n16 <= L::kPRows;
+            const bool own = walk.e >= p.n_groups;
+            const int32_t seen_by_first = own ? len - walk.q.n + token0 + 1 : len;  // keys that the block's first token sees
+            float rf[2 * kBlocks], sum[2 * kBlocks];
+#pragma unroll
+            for (int i = 0; i < 2 * kBlocks; ++i) {
+                rf[i] = -CUDART_INF_F;
+                sum[i] = 0.f;
+            }
+            for (int32_t t = walk.t0; t < walk.t1; ++t, ++tiles) {
+                const uint32_t b = tiles & 1u;
+                const bool first = t == walk.t0;
+                if (ok) ok = mbar_wait(&ctl->s_full[b], (tiles >> 1) & 1u, abort_flag);
+                tc_fence_after_sync();
+                uint32_t sc[kBlocks][8];  // [block][2 m + row of the pair]: key m
+#pragma unroll
+                for (int k = 0; k < kBlocks; ++k)
+                    if (k < nb) {
+                        tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr, &sc[k][0]);
+                        tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr + (16u << 16), &sc[k][4]);
+                    }
+                tmem_ld_wait();
+                const int32_t left = len - t * kTile;  // keys from the tile's first on
+                if (left < kTile || (t + 1) * kTile > seen_by_first) {
+#pragma unroll
+                    for (int k = 0; k < kBlocks; ++k)
+                        if (k < nb) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int32_t token = min((row0 + 8 * k + pair + e) / p.group, tokens - 1);
+                                const int32_t seen = min(left, seen_by_first + token - t * kTile);
+#pragma unroll
+                                for (int m = 0; m < 4; ++m)
+                                    if (key0 + 8 * m >= seen) sc[k][2 * m + e] = 0xff800000u;  // -inf
+                            }
+                        }
+                }
+                // ---- does any row's reference have to be raised?
+                bool up = false;
+#pragma unroll
+                for (int k = 0; k < kBlocks; ++k)
+                    if (k < nb) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float top = fmaxf(fmaxf(__uint_as_float(sc[k][e]), __uint_as_float(sc[k][2 + e])),
+                                                    fmaxf(__uint_as_float(sc[k][4 + e]), __uint_as_float(sc[k][6 + e])));
+                            up |= top * p.scale_log2 > rf[2 * k + e] + kRaise;
+                        }
+                    }
+                if (half_any(bar, up || first)) {
+#pragma unroll
+                    for (int k = 0; k < kBlocks; ++k)
+                        if (k < nb) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float top = fmaxf(fmaxf(__uint_as_float(sc[k][e]), __uint_as_float(sc[k][2 + e])),
+                                                  fmaxf(__uint_as_float(sc[k][4 + e]), __uint_as_float(sc[k][6 + e])));
+#pragma unroll
+                                for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                                if (lane < 4) mine[8 * k + pair + e] = top;
+                            }
+                        }
+                    half_sync(bar);
+                    float keep[2 * kBlocks];
+#pragma unroll
+                    for (int k = 0; k < kBlocks; ++k)
+                        if (k < nb) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int r = 8 * k + pair + e;
+                                const float top = fmaxf(fmaxf(all[r], all[64 + r]), fmaxf(all[128 + r], all[192 + r])) * p.scale_log2;
+                                const float old = rf[2 * k + e];
+                                const bool raise = top > old + kRaise;
+                                rf[2 * k + e] = raise ? top : old;
+                                keep[2 * k + e] = raise ? fast_exp2(old - top) : 1.f;  // (from -inf: 0)
+                                sum[2 * k + e] *= keep[2 * k + e];
+                                if (quarter == 0 && lane < 4) ref[half * 64 + r] = rf[2 * k + e];
+                            }
+                        }
+                    if (!first) {  // what O holds goes along
+                        half_sync(bar);
+#pragma unroll
+                        for (int k = 0; k < kBlocks; ++k)
+                            if (k < nb && quarter == 0 && lane < 4) {
+                                exchange[half * 256 + 8 * k + pair] = keep[2 * k];
+                                exchange[half * 256 + 8 * k + pair + 1] = keep[2 * k + 1];
+                            }
+                        half_sync(bar);
+                        if (ok) ok = mbar_wait(&ctl->pv_done, (tiles - 1) & 1u, abort_flag);
+                        tc_fence_after_sync();
+#pragma unroll 1
+                        for (int32_t c = 0; c < 8 * nb; c += 8) {
+                            uint32_t o[8];
+                            const uint32_t at = tmem_base + (2 + (segments & 1u)) * kCap + row0 + c + lane_addr;
+                            tmem_ld8(at, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[c + i]);
+                            tmem_st8(at, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                // ---- P = 2^(s - reference): 0 for a masked key (-inf), NaN for NaN and for +inf (inf - inf)
+                uint8_t* pb = smem + L::kPOff + b * L::kPBytes + (quarter >> 1) * L::kPHalfBytes;
+                const int chunk = (quarter & 1) * 4 + (lane >> 3), prow = row0 + (lane & 7);
+                const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2);
+#pragma unroll
+                for (int k = 0; k < kBlocks; ++k)
+                    if (k < nb) {
+                        const float base0 = rf[2 * k] == -CUDART_INF_F ? 0.f : rf[2 * k];  // a row that has seen no key yet
+                        const float base1 = rf[2 * k + 1] == -CUDART_INF_F ? 0.f : rf[2 * k + 1];
+                        const uint64_t base2 = f2_pack(-base0, -base1);
+                        uint32_t hi[4], lo[4];
+                        uint64_t s2 = f2_pack(sum[2 * k], sum[2 * k + 1]);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            float x0, x1;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[k][2 * m]), __uint_as_float(sc[k][2 * m + 1])), scale2, base2), x0, x1);
+                            x0 = fast_exp2(x0);
+                            x1 = fast_exp2(x1);
+                            s2 = f2_add(s2, f2_pack(x0, x1));
+                            hi[m] = pack_bf16x2(x0, x1);
+                            lo[m] = pack_bf16x2(x0 - __uint_as_float(hi[m] << 16), x1 - __uint_as_float(hi[m] & 0xffff0000u));
+                        }
+                        f2_unpack(s2, sum[2 * k], sum[2 * k + 1]);
+                        const uint32_t at = smem_u32(pb) + (prow + 8 * k) * 128 + ((chunk ^ ((prow + 8 * k) & 7)) << 4);
+                        stsm_x4_trans(at, hi[0], hi[1], hi[2], hi[3]);
+                        if (two_terms) stsm_x4_trans(at + (L::kPRows / 2) * 128, lo[0], lo[1], lo[2], lo[3]);
+                    }
+                // ---- V's rows behind the last key of a page that was loaded may hold anything: a probability of 0 must not
+                // meet a NaN there
+                const int32_t ragged = left < kTile ? left & 15 : 0;
+                if (ragged != 0) {
+                    const uint32_t st = tiles % L::kSlotsV;
+                    if (ok) ok = mbar_wait(&ctl->v_full[st], (tiles / L::kSlotsV) & 1u, abort_flag);
+                    uint8_t* v = smem + L::kVOff + st * L::kTensorBytes;
+                    for (int32_t i = threadIdx.x; i < (16 - ragged) * (D / 8); i += 256)
+                        *reinterpret_cast<uint4*>(v + key_off<D>(left + i / (D / 8), i % (D / 8))) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                fence_proxy_async_smem();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->p_ready[b]);
+            }
+            // ---- the segment's sums and output
+            half_sync(bar);  // the exchange has been read
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k)
+                if (k < nb) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float x = sum[2 * k + e];
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+                        if (lane < 4) mine[8 * k + pair + e] = x;
+                    }
+                }
+            half_sync(bar);
+            const bool whole = walk.t0 == 0 && walk.t1 == walk.q.tiles;
+            const bool last_word = whole && own && walk.q.page0 == 0;  // nothing to add: this is the result
+            const uint32_t ob = segments & 1u;
+            if (ok) ok = mbar_wait(&ctl->o_done[ob], (segments >> 1) & 1u, abort_flag);
+            tc_fence_after_sync();
+            const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
+            const int64_t kind = own ? p.total_tokens * p.num_q_heads : 0;
+            const int32_t d = quarter * 32 + lane;
+#pragma unroll 1
+            for (int32_t c = 0; c < 8 * nb; c += 8) {
+                uint32_t o[8];
+                tmem_ld8(tmem_base + (2 + ob) * kCap + row0 + c + lane_addr, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t r = row0 + c + i;
+                    if (r >= rows) break;
+                    const float total = (all[c + i] + all[64 + c + i]) + (all[128 + c + i] + all[192 + c + i]), m = ref[half * 64 + c + i];
+                    const int32_t token = r / p.group;
+                    const int64_t out_row = (static_cast<int64_t>(walk.q.tok0) + token0 + token) * p.num_q_heads + walk.head * p.group + (r - token * p.group);
+                    if (last_word) {
+                        if (d < D) static_cast<__nv_bfloat16*>(p.out)[out_row * D + d] = __float2bfloat16_rn(__uint_as_float(o[i]) / total);
+                        if (d == 0 && p.lse != nullptr) p.lse[out_row] = (m + log2f(total)) * kLn2;
+                    } else {
+                        float* po = whole ? p.whole_o + (kind + out_row) * D : p.part_o + (slot + r) * D;
+                        float2* pm = whole ? p.whole_ml + kind + out_row : p.part_ml + slot + r;
+                        if (d < D) po[d] = __uint_as_float(o[i]);
+                        if (d == 0) *pm = make_float2(m, total);
+                    }
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl->o_free[ob]);
+            ++segments;
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, L::kTmemCols);
+    }
+    if (threadIdx.x == 0 && p.status != nullptr) {
+        if (ctl->abort_flag != 0u) atomicCAS(p.status, 0, RPX_ERR_TIMEOUT);
+        else if (ctl->data_error != 0u) atomicCAS(p.status, 0, RPX_ERR_DEVICE_DATA);
+    }
+}
+
+template <int D, int kCap>
+rpx_status_t launch(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
+    using L = Layout<D, kCap>;
+    static_assert(L::kSlotsK >= 2 && L::kSlotsV >= 2 && L::kSmemBytes <= 232448, "shared memory of one CTA");
+    static_assert(L::kTmemCols >= 32 && L::kTmemCols <= 512, "tensor memory");
+    CUtensorMap tk, tv;
+    // the pool as groups of 8 keys: two per page and head
+    const uint64_t groups = static_cast<uint64_t>(cache.num_blocks) * p.num_kv_heads * 2;  // (fits 32 bits: checked by the caller)
+    const uint64_t dims[4] = {64, 8, D / 64, groups};
+    const uint64_t strides[3] = {D * 2ull, 128, 8 * D * 2ull};
+    const uint32_t box[4] = {64, 8, D / 64, 2};
+    if (rpx_status_t rc = encode_tmap_bf16(&tk, cache.k_cache, 4, dims, strides, box)) return rc;
+    if (rpx_status_t rc = encode_tmap_bf16(&tv, cache.v_cache, 4, dims, strides, box)) return rc;
+    auto* kernel = group_tile_kernel<D, kCap>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess) return RPX_ERR_CUDA;
+    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), kThreads, L::kSmemBytes, stream, tk, tv, p);
+}
+
+template <int D>
+rpx_status_t launch_cap(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
+    switch (p.cap) {
+        case 16: return launch<D, 16>(p, cache, stream);
+        case 32: return launch<D, 32>(p, cache, stream);
+        case 64: return launch<D, 64>(p, cache, stream);
+        default: return launch<D, 128>(p, cache, stream);
+    }
+}
+
+}  // namespace
+
+namespace group {
+rpx_status_t launch_group_tile(const Params& p, int32_t head_dim, const rpx_kv_cache_t& cache, cudaStream_t stream) {
+    return head_dim == 128 ? launch_cap<128>(p, cache, stream) : launch_cap<64>(p, cache, stream);
+}
+}  // namespace group
+
+}  // namespace rpx
