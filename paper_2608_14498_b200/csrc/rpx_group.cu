@@ -18,127 +18,295 @@ namespace {
 using namespace group;
 
 // ------------------------------------------------------------------ the plan
-// One block.  Every sequence gets its entry as if it were alone; groups that share are then given theirs, and their members'
-// keys begin behind it.  The first units are a running sum over all entries.
+// One block, which also finds where every CTA's piece begins.
 constexpr int kPlanThreads = 1024;
 
-__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0) {
-    Entry e = {tok0, n, len, row, page0, 1, 0, 1};
+// Units of the line (20 ns): of a tile against no rows, against 128 more, and of what a segment costs besides its tiles.
+constexpr int kWorkUnits = 30, kRowUnits = 75, kSegmentWork = 130;
+
+__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t group = -1) {
+    Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, 0};
     if (n == 0 || len == 0) {
         e.n = e.len = 0;
         return e;
     }
-    e.tiles = len / kTile + (len % kTile != 0 ? 1 : 0);
     // Blocks of at most `cap` rows; of at most 64 where the keys are few, so that probabilities keep their second term: over
     // many keys the rounding averages out.
-    const int32_t rows = e.tiles <= 2 && p.cap > 64 ? 64 : p.cap, per = max(1, rows / p.group);
-    e.blocks = (n + per - 1) / per;
-    // A tile's 64 KB (D = 128) are 1.5 us of this SM's share of HBM once, or the work against a block.
-    const int32_t work = 4 + e.block_tokens() * p.group * 12 / 128;
-    e.weight = max((15 + e.blocks - 1) / e.blocks, work);
+    const int32_t rows = e.tiles() <= 2 && p.cap > 64 ? 64 : p.cap, per = max(1, rows / p.group);
+    e.blocks = n <= per ? 1 : (n + per - 1) / per;
+    e.block_tokens = e.blocks == 1 ? n : (n + e.blocks - 1) / e.blocks;
+    // A tile's bytes are kTileUnits of this SM's share of HBM, once for all blocks; the work against a block overlaps with that, but
+    // a segment's first scores and last output do not with each other.
+    const int32_t rows_now = e.block_tokens * p.group, work = kWorkUnits + rows_now * kRowUnits / 128;
+    const int32_t bytes = p.tile_units / e.blocks, beside = kSegmentWork / e.tiles();
+    e.weight = max(bytes, work + beside);
     return e;
 }
 
+__device__ __forceinline__ int64_t entry_units(const Params& p, const Entry& e) { return e.n > 0 ? e.segment_units() * e.blocks * p.num_kv_heads : 0; }
+
+// What the sequences of some groups have in common.
+struct GroupBooks {
+    int32_t first[kPlanThreads + 1];
+    int32_t room[kPlanThreads];     // tokens in front of a member's first query, the least of all members; -1: a member does not fit
+    int32_t members[kPlanThreads];  // sequences with queries
+    int32_t row[kPlanThreads];      // the first of them
+    int32_t shared[kPlanThreads];   // whole pages' tokens; 0: nothing, or nobody to share with
+    __device__ __forceinline__ void open(int32_t i, int32_t begin) {
+        first[i] = begin;
+        room[i] = row[i] = INT32_MAX;
+        members[i] = 0;
+    }
+    __device__ __forceinline__ void add(int32_t i, int32_t s, bool fits, const Seq& q) {
+        if (!fits) {
+            atomicMin(&room[i], -1);
+        } else if (q.n > 0) {
+            atomicMin(&room[i], q.len - q.n);
+            atomicAdd(&members[i], 1);
+            atomicMin(&row[i], s);
+        }
+    }
+    __device__ __forceinline__ int32_t find(int32_t s, int32_t groups) const {  // the last that begins at or before the sequence
+        int32_t lo = 0, hi = groups;
+        while (hi - lo > 1) {
+            const int32_t mid = (lo + hi) / 2;
+            if (first[mid] <= s) lo = mid;
+            else hi = mid;
+        }
+        return lo;
+    }
+};
+
+// The tokens that a group shares: 0 for nothing, or nobody to share with; reports what does not fit.  `first`, `last`: its
+// sequences, with their first token and the one behind their last; `ascend` false (some bounds descend): no group fits.
+__device__ __forceinline__ bool group_fits(const Params& p, bool ascend, int32_t first, int32_t last, int32_t shared, int32_t room) {
+    return ascend && first >= 0 && first <= last && last <= p.batch && shared >= 0 && shared <= room;
+}
+__device__ __forceinline__ int32_t shared_tokens(const Params& p, bool fits, int32_t n, int32_t shared, int32_t members) {
+    fits = fits && n <= p.max_group;
+    if (!fits) report(p.status);
+    return fits && members > 1 ? shared / kPage * kPage : 0;
+}
+
+// Running sum over the block's threads; *total: of all of them.
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* sums, int64_t* total) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t sum = x;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, sum, off);
+        if (lane >= off) sum += y;
+    }
+    __syncthreads();  // the sums of the round before have been read
+    if (lane == 31) sums[warp] = sum;
+    __syncthreads();
+    const int64_t w = sums[lane];
+    int64_t upto = w;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
+        if (lane >= off) upto += y;
+    }
+    *total = __shfl_sync(0xffffffffu, upto, 31);
+    return __shfl_sync(0xffffffffu, upto - w, warp) + sum;
+}
+
+// Up to as many entries as threads: a thread an entry, groups first, everything read once (8 prompts of 8: 3 us; with the form
+// below 6).
+__global__ void __launch_bounds__(kPlanThreads) group_plan_small_kernel(const __grid_constant__ Params p) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ int64_t sums[kPlanThreads / 32];
+    __shared__ int64_t unit0[kPlanThreads];
+    __shared__ int32_t cu[kPlanThreads + 1];
+    __shared__ GroupBooks books;
+    const int32_t g = threadIdx.x, s = g - p.n_groups, count = p.n_groups + p.batch;
+    const bool is_group = g < p.n_groups, is_seq = !is_group && g < count;
+    int32_t first = 0, last = 0, shared = 0;
+    Seq q = {0, 0, 0};
+    bool fits = true;
+    if (is_group) {
+        first = __ldg(p.cu_groups + g);
+        last = __ldg(p.cu_groups + g + 1);
+        shared = __ldg(p.shared + g);
+        books.open(g, first);
+        if (g + 1 == p.n_groups) books.first[p.n_groups] = last;
+    } else if (is_seq) {
+        fits = read_seq(p, s, &q);
+        if (!fits) report(p.status);
+        cu[s] = q.tok0;
+        if (s + 1 == p.batch) cu[p.batch] = __ldg(p.cu + p.batch);
+    }
+    const bool ascend = __syncthreads_and(!is_group || first <= last) != 0;
+    const bool member = is_seq && ascend && p.n_groups > 0 && s >= books.first[0] && s < books.first[p.n_groups];
+    const int32_t of = member ? books.find(s, p.n_groups) : -1;
+    if (member) books.add(of, s, fits, q);
+    __syncthreads();
+    Entry e = {};
+    if (is_group) {
+        fits = group_fits(p, ascend, first, last, shared, books.room[g]);
+        const int32_t n = fits ? cu[last] - cu[first] : 0;
+        shared = shared_tokens(p, fits, n, shared, books.members[g]);
+        books.shared[g] = shared;
+        e = make_entry(p, shared > 0 ? cu[first] : 0, shared > 0 ? n : 0, shared, books.row[g], 0);
+    }
+    __syncthreads();
+    if (is_seq) {
+        shared = member ? books.shared[of] : 0;
+        e = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, shared > 0 ? of : -1);
+    }
+    const int64_t units = entry_units(p, e);
+    int64_t total;
+    e.unit0 = block_sum(units, sums, &total) - units;
+    unit0[threadIdx.x] = e.unit0;
+    if (g < count) p.entries[g] = e;
+    if (g == 0) *p.total = total;
+    __syncthreads();
+    if (g < p.ctas) p.starts[g] = find_start(p, total, g, [&](int32_t i) { return unit0[i]; });
+}
+
+// Any number: every sequence gets its entry as if it were alone; groups that share are then given theirs, kPlanThreads at a time,
+// and their members' keys begin behind it.
 __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_constant__ Params p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ int64_t sums[kPlanThreads / 32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ GroupBooks books;
+    bool good = true;
+    for (int32_t g = threadIdx.x; g < p.n_groups; g += kPlanThreads) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
     for (int32_t s = threadIdx.x; s < p.batch; s += kPlanThreads) {
         Seq q;
         if (!read_seq(p, s, &q)) report(p.status);
         p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0);
-        p.seq_group[s] = -1;
     }
-    const bool ascend = groups_ascend(p);  // (a barrier: the entries above are written)
-    for (int32_t g = warp; g < p.n_groups; g += kPlanThreads / 32) {
-        Group r = {0, 0, 0, 0, -1, 0, 0};
-        if (ascend) r = read_group(p, g, lane);
-        if (r.shared < 0 && lane == 0) report(p.status);
-        const bool shares = r.shared > 0 && r.members > 1;
-        if (lane == 0) p.entries[g] = make_entry(p, r.tok0, shares ? r.n : 0, r.shared, r.row, 0);
-        if (!shares) continue;
-        for (int32_t s = r.first + lane; s < r.last; s += 32) {
+    const bool ascend = __syncthreads_and(good) != 0;
+    for (int32_t g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
+        const int32_t groups = min(kPlanThreads, p.n_groups - g0), g = g0 + threadIdx.x;
+        const bool is_group = threadIdx.x < groups;
+        if (is_group) books.open(threadIdx.x, __ldg(p.cu_groups + g));
+        if (threadIdx.x == 0) books.first[groups] = __ldg(p.cu_groups + g0 + groups);
+        __syncthreads();
+        // the members of these groups (nobody, where the bounds descend)
+        const int32_t begin = max(books.first[0], 0), end = ascend ? min(books.first[groups], p.batch) : 0;
+        for (int32_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
+            Seq q;
+            const bool fits = read_seq(p, s, &q);
+            books.add(books.find(s, groups), s, fits, q);
+        }
+        __syncthreads();
+        if (is_group) {
+            const int32_t first = books.first[threadIdx.x], last = books.first[threadIdx.x + 1];
+            int32_t shared = __ldg(p.shared + g);
+            const bool fits = group_fits(p, ascend, first, last, shared, books.room[threadIdx.x]);
+            const int32_t tok0 = fits ? __ldg(p.cu + first) : 0, n = fits ? __ldg(p.cu + last) - tok0 : 0;
+            shared = shared_tokens(p, fits, n, shared, books.members[threadIdx.x]);
+            books.shared[threadIdx.x] = shared;
+            p.entries[g] = make_entry(p, tok0, shared > 0 ? n : 0, shared, books.row[threadIdx.x], 0);
+        }
+        __syncthreads();
+        for (int32_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
+            const int32_t i = books.find(s, groups), shared = books.shared[i];
+            if (shared == 0) continue;
             Seq q;
             read_seq(p, s, &q);
-            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - r.shared : 0, s, r.shared / kPage);
-            p.seq_group[s] = g;
+            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, g0 + i);
         }
+        __syncthreads();
     }
-    __syncthreads();
     const int32_t count = p.n_groups + p.batch;
     int64_t carry = 0;
     for (int32_t base = 0; base < count; base += kPlanThreads) {
         const int32_t e = base + threadIdx.x;
-        int64_t x = 0;
-        if (e < count) {
-            const Entry q = p.entries[e];
-            if (q.n > 0) x = q.segment_units() * q.blocks * p.num_kv_heads;
-        }
-        int64_t sum = x;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, sum, off);
-            if (lane >= off) sum += y;
-        }
-        __syncthreads();  // the sums of the round before have been read
-        if (lane == 31) sums[warp] = sum;
-        __syncthreads();
-        int64_t before = carry, total = carry;
-        for (int w = 0; w < kPlanThreads / 32; ++w) {
-            before += w < warp ? sums[w] : 0;
-            total += sums[w];
-        }
-        if (e < count) p.unit0[e] = before + sum - x;
-        carry = total;
+        const int64_t x = e < count ? entry_units(p, p.entries[e]) : 0;
+        int64_t total;
+        const int64_t upto = block_sum(x, sums, &total);
+        if (e < count) p.entries[e].unit0 = carry + upto - x;
+        carry += total;
     }
-    if (threadIdx.x == 0) p.unit0[count] = carry;
+    if (threadIdx.x == 0) *p.total = carry;
+    __syncthreads();
+    if (threadIdx.x < p.ctas) p.starts[threadIdx.x] = find_start(p, carry, threadIdx.x, [&](int32_t i) { return p.entries[i].unit0; });
 }
 
 // ------------------------------------------------------------------ the join
 // A warp per row (token, query head) that has more than one set to add up: the shared keys' pieces in order, then its own.
 constexpr int kJoinWarps = 8;
 
+// The sets of a row against one entry: where the first lies, how far on the others, and how many.
+struct Sets {
+    int64_t first, step;
+    int32_t n;
+    bool whole;
+};
+__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int64_t size, int32_t kv_head, int32_t in_group, int64_t token, int64_t own_row) {
+    const int32_t in = static_cast<int32_t>(token - q.tok0), block = q.blocks == 1 ? 0 : in / q.block_tokens;
+    const int64_t unit = q.unit0 + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
+    const int64_t c0 = quotient(unit, size);
+    Sets r;
+    r.n = static_cast<int32_t>(quotient(unit + static_cast<int64_t>(q.tiles() - 1) * q.weight, size) - c0) + 1;
+    r.whole = r.n == 1;
+    // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
+    r.first = r.whole ? own_row : (c0 * 2 + 1) * p.cap + (in - block * q.block_tokens) * p.group + in_group;
+    r.step = p.cap;  // from the second slot of a piece to the first of the next; 2 cap from there on
+    return r;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kJoinWarps * 32) group_join_kernel(const __grid_constant__ Params p) {
     constexpr int kCols = D / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t out_row = static_cast<int64_t>(blockIdx.x) * kJoinWarps + warp, token = out_row / p.num_q_heads;
+    const int64_t out_row = static_cast<int64_t>(blockIdx.x) * kJoinWarps + warp, token = quotient(out_row, p.num_q_heads);
     if (token >= p.total_tokens) return;  // (never a whole block)
-    const int32_t h = static_cast<int32_t>(out_row - token * p.num_q_heads), kv_head = h / p.group, in_group = h - kv_head * p.group;
-    Seq seq;
-    const int32_t s = find_seq(p, token, lane, &seq);
+    const int32_t h = static_cast<int32_t>(out_row - token * p.num_q_heads), kv_head = over_group(p, h), in_group = h - kv_head * p.group;
+    const int32_t s = find_seq(p, token, lane);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // (of rows that are left out too: this grid never ends before that one)
-    if (s < 0) return;
-    const int32_t g = __ldcg(p.seq_group + s), count = p.n_groups + p.batch;
-    const int64_t size = piece_units(__ldcg(p.unit0 + count), p.ctas);
+    const Entry own = load_entry(p.entries + p.n_groups + s);
+    const int64_t size = piece_units(__ldcg(p.total), p.ctas), all_rows = p.total_tokens * p.num_q_heads;
+    if (token < own.tok0 || token - own.tok0 >= own.n) return;  // in no sequence, or in one that does not fit
+    Sets sets[2];
+    sets[0] = Sets{0, 0, 0, false};
+    sets[1] = find_sets(p, own, size, kv_head, in_group, token, all_rows + out_row);
+    if (own.group < 0 && sets[1].whole) return;  // written whole
+    if (own.group >= 0) sets[0] = find_sets(p, load_entry(p.entries + own.group), size, kv_head, in_group, token, out_row);
     float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
 #pragma unroll
     for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
-    for (int kind = g < 0 ? 1 : 0; kind < 2; ++kind) {
-        const int32_t e = kind == 0 ? g : p.n_groups + s;
-        const Entry q = Walk::load(p, e);
-        const int32_t in = static_cast<int32_t>(token - q.tok0), per = q.block_tokens(), block = in / per;
-        const int32_t row = (in - block * per) * p.group + in_group;
-        const int64_t unit = __ldcg(p.unit0 + e) + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
-        const int64_t c0 = unit / size;
-        const int32_t pieces = static_cast<int32_t>((unit + static_cast<int64_t>(q.tiles - 1) * q.weight) / size - c0) + 1;
-        if (pieces == 1 && g < 0) return;  // written whole
-#pragma unroll 2
-        for (int32_t j = 0; j < pieces; ++j) {
-            // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
-            const int64_t slot = ((c0 + j) * 2 + (j == 0 ? 1 : 0)) * p.cap + row, own_row = kind * p.total_tokens * p.num_q_heads + out_row;
-            const float2 ml = pieces == 1 ? __ldcg(p.whole_ml + own_row) : __ldcg(p.part_ml + slot);
-            const float* o = (pieces == 1 ? p.whole_o + own_row * D : p.part_o + slot * D) + lane * kCols;
-            float v[kCols];
-            if constexpr (kCols == 4) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(o));
-            else *reinterpret_cast<float2*>(v) = __ldcg(reinterpret_cast<const float2*>(o));
-            if (ml.x == -CUDART_INF_F && ml.y == 0.f) continue;  // no key seen (a NaN sum, of nothing but NaN, goes on)
-            const float to = fmaxf(top, ml.x), keep = top == -CUDART_INF_F ? 0.f : fast_exp2(top - to);
-            const float f = ml.x == -CUDART_INF_F ? 1.f : fast_exp2(ml.x - to);
-            top = to;
-            sum = fmaf(sum, keep, f * ml.y);
+    // kBatch sets at a time, all of them on their way together (one after the other, 17 sets took 6 us)
+    constexpr int kBatch = 8;
+    const int32_t n = sets[0].n + sets[1].n;
+    for (int32_t j0 = 0; j0 < n; j0 += kBatch) {
+        float2 ml[kBatch];
+        float v[kBatch][kCols];
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) acc[i] = fmaf(acc[i], keep, f * v[i]);
+        for (int u = 0; u < kBatch; ++u) {
+            const bool shared = j0 + u < sets[0].n;
+            const int32_t j = j0 + u - (shared ? 0 : sets[0].n);
+            const int64_t at = (shared ? sets[0].first : sets[1].first) + (j == 0 ? 0 : (2 * j - 1) * (shared ? sets[0].step : sets[1].step));
+            const bool whole = shared ? sets[0].whole : sets[1].whole;
+            ml[u] = make_float2(-CUDART_INF_F, 0.f);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) v[u][i] = 0.f;
+            if (j0 + u < n) {
+                ml[u] = __ldcg((whole ? p.whole_ml : p.part_ml) + at);
+                const float* o = (whole ? p.whole_o : p.part_o) + at * D + lane * kCols;
+                if constexpr (kCols == 4) *reinterpret_cast<float4*>(v[u]) = __ldcg(reinterpret_cast<const float4*>(o));
+                else *reinterpret_cast<float2*>(v[u]) = __ldcg(reinterpret_cast<const float2*>(o));
+            }
+        }
+        float to = top;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) to = fmaxf(to, ml[u].x);
+        const float base = to == -CUDART_INF_F ? 0.f : to;  // (no key seen so far)
+        const float keep = fast_exp2(top - base);
+        top = to;
+        sum *= keep;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[i] *= keep;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            // a set that saw no key has a sum and outputs of 0; one of nothing but NaN goes on with a factor of 1
+            const float f = ml[u].x == -CUDART_INF_F ? 1.f : fast_exp2(ml[u].x - base);
+            sum = fmaf(f, ml[u].y, sum);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) acc[i] = fmaf(f, v[u][i], acc[i]);
         }
     }
     const float inv = 1.f / sum;
@@ -164,17 +332,31 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
         Seq q;
         for (int32_t s = threadIdx.x; s < p.batch; s += blockDim.x)
             if (!read_seq(p, s, &q)) report(p.status);
-        const bool ascend = groups_ascend(p);
-        for (int32_t g = warp; g < p.n_groups; g += kRowWarps)
-            if (!ascend || read_group(p, g, lane).shared < 0) report(p.status);
+        bool good = true;
+        for (int32_t g = threadIdx.x; g < p.n_groups; g += blockDim.x) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
+        const bool ascend = __syncthreads_and(good) != 0;
+        for (int32_t g = warp; g < p.n_groups; g += kRowWarps) {
+            const int32_t first = max(__ldg(p.cu_groups + g), 0), last = ascend ? min(__ldg(p.cu_groups + g + 1), p.batch) : 0;
+            int32_t room = INT32_MAX;
+            for (int32_t s = first + lane; s < last; s += 32) {
+                if (!read_seq(p, s, &q)) room = -1;
+                else if (q.n > 0) room = min(room, q.len - q.n);
+            }
+            room = __reduce_min_sync(0xffffffffu, room);
+            if (lane == 0) {
+                const int32_t end = __ldg(p.cu_groups + g + 1);
+                const bool fits = group_fits(p, ascend, __ldg(p.cu_groups + g), end, __ldg(p.shared + g), room);
+                shared_tokens(p, fits, fits ? __ldg(p.cu + end) - __ldg(p.cu + first) : 0, 0, 0);
+            }
+        }
     }
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kRowWarps + warp;
     const int64_t token = row / p.num_q_heads;
     const int32_t head = static_cast<int32_t>(row - token * p.num_q_heads);
     if (token >= p.total_tokens) return;
+    const int32_t s = find_seq(p, token, lane);
     Seq seq;
-    const int32_t s = find_seq(p, token, lane, &seq);
-    if (s < 0) return;
+    if (!read_seq(p, s, &seq) || token < seq.tok0 || token - seq.tok0 >= seq.n) return;
     float q[U], acc[U];
     const float* src = static_cast<const float*>(p.q) + token * p.q_stride + static_cast<int64_t>(head) * D + part * U;
 #pragma unroll
@@ -245,18 +427,15 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     if (p.lse != nullptr && lane == 0) p.lse[row] = (top + log2f(l)) * kLn2;
 }
 
-int32_t rows_cap(int64_t rows, int32_t group) {
-    const int64_t most = rows > group ? rows : group;
-    return most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
-}
-int32_t cap_of(int32_t max_q, int32_t max_group, int32_t n_groups, int32_t group) {
-    const int32_t most = n_groups > 0 && max_group > max_q ? max_group : max_q;
-    return rows_cap(static_cast<int64_t>(most) * group, group);
+// Rows per block: the smallest of 16, 32, 64 and the most that a form takes that holds a group's rows of one KV head.
+int32_t cap_of(int32_t max_q, int32_t max_group, int32_t n_groups, int32_t group, int32_t head_dim) {
+    const int64_t rows = static_cast<int64_t>(n_groups > 0 && max_group > max_q ? max_group : max_q) * group;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : group_most_rows(head_dim);
 }
 constexpr int kMaxCtas = 148;
 
 // Carves the workspace (NULL: only measures it).
-size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t batch, int32_t cap, int32_t heads, int32_t head_dim, void* workspace) {
+size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t cap, int32_t heads, int32_t head_dim, void* workspace) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -264,10 +443,10 @@ size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t batch, int32_t 
         at += align_up(bytes, 256);
         return r;
     };
+    p.starts = reinterpret_cast<Start*>(take(kMaxCtas * sizeof(Start)));
     const size_t rows = static_cast<size_t>(tokens) * heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * cap;
     p.entries = reinterpret_cast<Entry*>(take(static_cast<size_t>(entries) * sizeof(Entry)));
-    p.unit0 = reinterpret_cast<int64_t*>(take((static_cast<size_t>(entries) + 1) * sizeof(int64_t)));
-    p.seq_group = reinterpret_cast<int32_t*>(take(static_cast<size_t>(batch) * sizeof(int32_t)));
+    p.total = reinterpret_cast<int64_t*>(take(sizeof(int64_t)));
     p.whole_ml = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
     p.part_ml = reinterpret_cast<float2*>(take(slots * sizeof(float2)));
     p.whole_o = reinterpret_cast<float*>(take(rows * head_dim * sizeof(float)));
@@ -277,10 +456,12 @@ size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t batch, int32_t 
 
 }  // namespace
 
+int32_t group_most_rows(int32_t head_dim) { return head_dim == 128 ? 112 : 128; }
+
 size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t n_groups, int32_t max_q, int32_t max_group) {
     if (d->dtype == RPX_F32 || batch > INT32_MAX - n_groups - 1) return 0;
     Params p = {};
-    return carve(p, tokens, n_groups + batch, batch, cap_of(max_q, max_group, n_groups, d->num_q_heads / d->num_kv_heads), d->num_q_heads, d->head_dim, nullptr);
+    return carve(p, tokens, n_groups + batch, cap_of(max_q, max_group, n_groups, d->num_q_heads / d->num_kv_heads, d->head_dim), d->num_q_heads, d->head_dim, nullptr);
 }
 
 bool group_too_large(const GroupArgs& a) {
@@ -299,11 +480,13 @@ rpx_status_t launch_group_attn(const GroupArgs& a) {
     }
     const int sms = sm_count();
     if (sms <= 0) return RPX_ERR_CUDA;
-    p.cap = cap_of(a.max_q, a.max_group, a.n_groups, p.group);
+    p.cap = cap_of(a.max_q, a.max_group, a.n_groups, p.group, a.head_dim);
+    p.tile_units = a.head_dim == 128 ? 75 : 38;  // 64 KB or 32 at 6.5 TB/s over 148 SMs
     // (without the SM budget: where the line of tiles is cut decides the order of the sums)
     p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
-    carve(p, a.total_tokens, a.n_groups + a.batch, a.batch, p.cap, a.num_q_heads, a.head_dim, a.workspace);
-    group_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
+    carve(p, a.total_tokens, a.n_groups + a.batch, p.cap, a.num_q_heads, a.head_dim, a.workspace);
+    if (a.n_groups + a.batch <= kPlanThreads) group_plan_small_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
+    else group_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
     if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
     if (rpx_status_t rc = launch_group_tile(p, a.head_dim, *a.cache, a.stream)) return rc;
     const unsigned blocks = static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps);

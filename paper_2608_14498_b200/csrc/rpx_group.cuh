@@ -22,17 +22,30 @@ constexpr int kTile = 128;  // keys of a tile
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// The line is measured in units; going over to another segment counts kSegment of them.
-constexpr int kSegment = 10, kMinUnits = 40;
+// The line is measured in units of some 20 ns; going over to another segment counts kSegment of them (what more it costs is in
+// the weight of its tiles).  A piece has kMinUnits at least: as long as the heaviest tile, so every piece between a segment's
+// first and last holds one.
+constexpr int kSegment = 25, kMinUnits = 256;
 
-struct __align__(32) Entry {
+struct __align__(16) Entry {
     int32_t tok0, n, len;   // first query token, query tokens, keys
     int32_t row, page0;     // the table row that names the keys' pages, and the first of them
-    int32_t blocks, tiles;  // row blocks, key tiles
+    int32_t blocks, block_tokens;  // row blocks, and the tokens of each but the last
     int32_t weight;         // units of a key tile against one block
-    __device__ __forceinline__ int32_t block_tokens() const { return (n + blocks - 1) / blocks; }
-    __device__ __forceinline__ int64_t segment_units() const { return static_cast<int64_t>(tiles) * weight + kSegment; }
+    int64_t unit0;          // its first unit
+    int32_t group;          // of a sequence: the group whose shared pages it reads as well, or -1
+    int32_t unused;
+    __device__ __forceinline__ int32_t tiles() const { return len / kTile + (len % kTile != 0 ? 1 : 0); }
+    __device__ __forceinline__ int64_t segment_units() const { return static_cast<int64_t>(tiles()) * weight + kSegment; }
 };
+
+__device__ __forceinline__ Entry load_entry(const Entry* at) {
+    const int4 a = __ldcg(reinterpret_cast<const int4*>(at)), b = __ldcg(reinterpret_cast<const int4*>(at) + 1);
+    const longlong2 c = __ldcg(reinterpret_cast<const longlong2*>(at) + 2);
+    return Entry{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, static_cast<int32_t>(c.y), 0};
+}
+
+struct Start;
 
 struct Params {
     const void* q;
@@ -44,6 +57,7 @@ struct Params {
     const int32_t *cu_groups, *shared;
     int32_t n_groups;
     int32_t num_q_heads, num_kv_heads, group;
+    uint32_t group_magic;  // 2^32 / group, rounded up: row / group for rows below 2^16 (group 1: 0)
     const int32_t* block_table;
     int32_t block_table_stride, num_blocks;
     const __nv_bfloat16 *k_cache, *v_cache;
@@ -53,15 +67,20 @@ struct Params {
     int32_t* status;
     // bf16 only
     int32_t cap;           // rows per block at most
+    int32_t tile_units;    // of a tile's bytes
     int32_t ctas;          // pieces at most
     Entry* entries;        // workspace [n_groups + batch]
-    int64_t* unit0;        // workspace [n_groups + batch + 1]: an entry's first unit; the last is the total
-    int32_t* seq_group;    // workspace [batch]: the group whose shared pages a sequence reads, or -1
+    struct Start* starts;  // workspace [ctas]
+    int64_t* total;        // workspace: units of the line
     float2* whole_ml;      // workspace [2][total_tokens][H_q]: of segments that are not cut: shared, own
     float* whole_o;        // workspace [2][total_tokens][H_q][D]
     float2* part_ml;       // workspace [ctas][2][cap]: of segments that are
     float* part_o;         // workspace [ctas][2][cap][D]
 };
+
+__device__ __forceinline__ int32_t over_group(const Params& p, int32_t row) {
+    return p.group == 1 ? row : static_cast<int32_t>(__umulhi(static_cast<uint32_t>(row), p.group_magic));
+}
 
 __device__ __forceinline__ void report(int32_t* status) {
     if (status != nullptr) atomicCAS(status, 0, RPX_ERR_DEVICE_DATA);
@@ -84,8 +103,8 @@ __device__ __forceinline__ bool read_seq(const Params& p, int32_t s, Seq* q) {
     return true;
 }
 
-// The sequence that a token is in, or -1: the last that starts at or before it, 32 offsets a step (a warp together).
-__device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int lane, Seq* q) {
+// The last sequence that starts at or before a token, 32 offsets a step (a warp together).
+__device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int lane) {
     int32_t lo = 0, hi = p.batch;
     while (hi - lo > 1) {
         const int32_t step = (hi - lo + 31) / 32;
@@ -94,44 +113,7 @@ __device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int 
         lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
         hi = hi - lo > step ? lo + step : hi;
     }
-    return read_seq(p, lo, q) && token >= q->tok0 && token < static_cast<int64_t>(q->tok0) + q->n ? lo : -1;
-}
-
-// Whether the bounds of all groups ascend (otherwise nothing is shared); by a whole block, which meets at a barrier here.
-__device__ __forceinline__ bool groups_ascend(const Params& p) {
-    bool good = true;
-    for (int32_t g = threadIdx.x; g < p.n_groups; g += blockDim.x) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
-    return __syncthreads_and(good) != 0;
-}
-
-// What a group shares: whole pages' tokens, -1 where it does not fit; its first and last sequence, their query tokens, how many
-// sequences have any, and the first that does (its table row names the shared pages).  A warp together.
-struct Group {
-    int32_t first, last, tok0, n, shared, members, row;
-};
-__device__ __forceinline__ Group read_group(const Params& p, int32_t g, int lane) {
-    Group r = {__ldg(p.cu_groups + g), __ldg(p.cu_groups + g + 1), 0, 0, -1, 0, INT32_MAX};
-    const int32_t shared = __ldg(p.shared + g);
-    if (r.first < 0 || r.last < r.first || r.last > p.batch || shared < 0) return r;
-    bool fits = true;
-    for (int32_t s = r.first + lane; s < r.last; s += 32) {
-        Seq q;
-        fits &= read_seq(p, s, &q) && (q.n == 0 || q.len - q.n >= shared);
-        if (q.n > 0) {
-            ++r.members;
-            r.row = min(r.row, s);
-        }
-    }
-    r.members = __reduce_add_sync(0xffffffffu, r.members);
-    r.row = __reduce_min_sync(0xffffffffu, r.row);
-    if (!__all_sync(0xffffffffu, fits)) return r;
-    if (r.first < r.last) {
-        r.tok0 = __ldg(p.cu + r.first);
-        r.n = __ldg(p.cu + r.last) - r.tok0;
-    }
-    if (r.n > p.max_group) return r;
-    r.shared = shared / kPage * kPage;
-    return r;
+    return lo;
 }
 
 // Pieces: the line of `total` units in runs of piece_units() (the last ones may be short or empty).
@@ -140,51 +122,61 @@ __device__ __forceinline__ int64_t piece_units(int64_t total, int32_t ctas) {
     return even > kMinUnits ? even : kMinUnits;
 }
 
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // (64-bit division takes ten times as long)
+    if ((a >> 31) == 0 && (b >> 31) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
+// Where a CTA's piece begins: its entry, KV head, row block and first tile (as Walk keeps them), and the units behind that.
+struct __align__(16) Start {
+    Entry q;
+    int32_t e, head, block, t1;
+    int64_t left, unused;
+};
+// By one thread for one CTA; unit0(e) gives an entry's first unit.
+template <class Unit0>
+__device__ __forceinline__ Start find_start(const Params& p, int64_t total, int32_t cta, Unit0 unit0) {
+    const int64_t size = piece_units(total, p.ctas), begin = min(total, size * static_cast<int64_t>(cta)), end = min(total, begin + size);
+    Start r = {};
+    r.left = end - begin;
+    if (r.left == 0) return r;
+    int32_t lo = 0, hi = p.n_groups + p.batch;  // the last entry that starts at or before `begin`
+    while (hi - lo > 1) {
+        const int32_t mid = lo + (hi - lo) / 2;
+        if (unit0(mid) <= begin) lo = mid;
+        else hi = mid;
+    }
+    r.e = lo;
+    r.q = p.entries[lo];
+    int64_t off = begin - r.q.unit0;
+    const int64_t seg = r.q.segment_units(), i = quotient(off, seg);
+    r.head = static_cast<int32_t>(quotient(i, r.q.blocks));
+    r.block = static_cast<int32_t>(i - static_cast<int64_t>(r.head) * r.q.blocks);
+    off -= i * seg;
+    r.t1 = off <= kSegment ? 0 : static_cast<int32_t>(quotient(off - kSegment + r.q.weight - 1, r.q.weight));
+    r.left -= kSegment + static_cast<int64_t>(r.t1) * r.q.weight - off;
+    return r;
+}
+
 // Walks the pieces of segments inside a CTA's part of the line; every role walks it alike.
 struct Walk {
     int32_t e, head, block, t0, t1;  // current segment: entry, KV head, row block, key tiles [t0, t1)
     int64_t left;                    // units of the piece behind t1's first
-    Entry q, ahead;                  // the entry, and the one behind it
-    static __device__ __forceinline__ Entry load(const Params& p, int32_t e) {
-        Entry r = {};
-        if (e < p.n_groups + p.batch) {
-            const int4 a = __ldcg(reinterpret_cast<const int4*>(p.entries + e)), b = __ldcg(reinterpret_cast<const int4*>(p.entries + e) + 1);
-            r = Entry{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        }
-        return r;
-    }
-    // (a whole warp together)
+    Entry q;
     __device__ __forceinline__ void start(const Params& p) {
-        const int lane = threadIdx.x & 31;
-        const int32_t count = p.n_groups + p.batch;
-        const int64_t total = __ldcg(p.unit0 + count), size = piece_units(total, p.ctas);
-        const int64_t begin = min(total, size * static_cast<int64_t>(blockIdx.x)), end = min(total, begin + size);
-        e = head = block = t0 = t1 = 0;
-        left = end - begin;
-        q = ahead = Entry{};
-        if (left == 0) return;
-        int32_t lo = 0, hi = count;  // the last entry that starts at or before `begin`, 32 a step
-        while (hi - lo > 1) {
-            const int32_t step = (hi - lo + 31) / 32;
-            const int64_t at = lo + static_cast<int64_t>(lane) * step;
-            const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldcg(p.unit0 + at) <= begin);
-            lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
-            hi = hi - lo > step ? lo + step : hi;
-        }
-        e = lo;
-        q = load(p, e);
-        ahead = load(p, e + 1);
-        int64_t off = begin - __ldcg(p.unit0 + e);
-        const int64_t seg = q.segment_units(), i = off / seg;
-        head = static_cast<int32_t>(i / q.blocks);
-        block = static_cast<int32_t>(i - static_cast<int64_t>(head) * q.blocks);
-        off -= i * seg;
-        t1 = off <= kSegment ? 0 : static_cast<int32_t>((off - kSegment + q.weight - 1) / q.weight);
-        left -= kSegment + static_cast<int64_t>(t1) * q.weight - off;
+        const Start* s = p.starts + blockIdx.x;
+        const int4 a = __ldcg(reinterpret_cast<const int4*>(&s->e));
+        left = __ldcg(&s->left);
+        q = load_entry(&s->q);
+        e = a.x;
+        head = a.y;
+        block = a.z;
+        t1 = a.w;
+        t0 = 0;
     }
     __device__ __forceinline__ bool next(const Params& p) {
         if (left <= 0) return false;
-        if (t1 == q.tiles) {
+        if (t1 == q.tiles()) {
             t1 = 0;
             if (++block == q.blocks) {
                 block = 0;
@@ -192,8 +184,7 @@ struct Walk {
                     head = 0;
                     do {
                         if (++e >= p.n_groups + p.batch) return false;
-                        q = ahead;
-                        ahead = load(p, e + 1);
+                        q = load_entry(p.entries + e);
                     } while (q.n == 0);
                 }
             }
@@ -201,13 +192,13 @@ struct Walk {
             if (left <= 0) return false;  // not even the first tile starts in this piece
         }
         t0 = t1;
-        const int64_t tiles = (left + q.weight - 1) / q.weight;
-        t1 = tiles < q.tiles - t0 ? t0 + static_cast<int32_t>(tiles) : q.tiles;
+        t1 = q.tiles();
+        if (static_cast<int64_t>(t1 - t0) * q.weight > left) t1 = t0 + static_cast<int32_t>(min(quotient(left + q.weight - 1, q.weight), static_cast<int64_t>(t1 - t0)));
         left -= static_cast<int64_t>(t1 - t0) * q.weight;
         return true;
     }
-    __device__ __forceinline__ int32_t token0() const { return block * q.block_tokens(); }
-    __device__ __forceinline__ int32_t tokens() const { return min(q.block_tokens(), q.n - token0()); }
+    __device__ __forceinline__ int32_t token0() const { return block * q.block_tokens; }
+    __device__ __forceinline__ int32_t tokens() const { return min(q.block_tokens, q.n - token0()); }
 };
 
 inline Params make_params(const GroupArgs& a) {
@@ -226,6 +217,7 @@ inline Params make_params(const GroupArgs& a) {
     p.num_q_heads = a.num_q_heads;
     p.num_kv_heads = a.num_kv_heads;
     p.group = a.num_q_heads / a.num_kv_heads;
+    p.group_magic = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
     p.block_table = a.cache->block_table;
     p.block_table_stride = a.cache->block_table_stride;
     p.num_blocks = static_cast<int32_t>(a.cache->num_blocks);

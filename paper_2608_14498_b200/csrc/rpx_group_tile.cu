@@ -15,13 +15,14 @@
 // A row's running reference is raised only when a score passes it by 2^8: what is kept is exact whatever the reference, so all
 // the threads of a tile need to agree on is whether one of them has to (one barrier with a vote).
 //
-// Segments (a KV head's keys of a group's prompt or of one sequence) follow one another without a pause: two buffers each for S, P,
-// O and, but for the largest blocks, Q, so the tensor core is in the next segment while this one's output is written, and the
-// rings of K and V never drain.
-//   warps 0-3, 4-7 : softmax of the first and second half of the rows, lanes = keys; a segment's output, lanes = elements of D
-//   warp  8        : producer of K and V, one TMA box per 16-token page
-//   warp  9        : issues the products (one thread)
-//   warps 10, 11   : lay Q out
+// Segments (a KV head's keys of a group's prompt or of one sequence) follow one another without a pause: there are two buffers
+// each of S, P, O and (but for more than 64 rows) Q, every product has a thread of its own that waits for its own operands only, and
+// a segment's output is written by warps that do nothing else, while the softmax warps are in the next one.
+//   4 x 2 or 4 warps : two (up to 16 rows) or four teams with a share of the rows each: softmax, lanes = keys
+//   1 warp each      : producer of K and V (one TMA box per 16-token page); S^T = K Q^T; O^T += V^T P^T; laying Q out
+//   4 warps          : output, lanes = elements of D
+#include <type_traits>
+
 #include "rpx_group.cuh"
 
 namespace rpx {
@@ -30,47 +31,66 @@ namespace {
 
 using namespace group;
 
-constexpr int kThreads = 32 * 12;
-constexpr int kProducerWarp = 8, kMmaWarp = 9, kQWarp = 10, kQWarps = 2;
+constexpr int kSoftmaxRegs = 96, kOtherRegs = 48;  // 512 * 96 + 256 * 48 = 768 * 80, what a launch of 768 threads has
 constexpr int kPages = kTile / kPage;
 constexpr float kRaise = 8.0f;  // log2 units
 constexpr int kMaxSlots = 6;
 
 template <int D, int kCap>
 struct Layout {
+    static constexpr int kTeams = kCap == 16 ? 2 : 4;              // of four softmax warps
+    static constexpr int kProducerWarp = 4 * kTeams, kScoreWarp = kProducerWarp + 1, kValueWarp = kProducerWarp + 2, kQWarp = kProducerWarp + 3;
+    static constexpr int kOutWarp = kProducerWarp + 4;             // the first of four
+    static constexpr int kThreads = 32 * (kOutWarp + 4);
+    static constexpr bool kSplitRegs = kTeams == 4;
+    static constexpr int kBlocks = (kCap / 8 + kTeams - 1) / kTeams;  // 8-row blocks of a team at most
     static constexpr int kHalves = D / 64;
     static constexpr int kTensorBytes = kTile * D * 2;             // a key tile of K or V
     static constexpr int kPRows = kCap <= 64 ? 2 * kCap : 128;
     static constexpr int kPHalfBytes = kPRows * 128;               // 64 keys of all rows
     static constexpr int kPBytes = 2 * kPHalfBytes;
-    static constexpr int kQHalfBytes = kCap * 128;
+    static constexpr int kQRows = kCap <= 64 ? 2 * kCap : kCap;    // two blocks' Q, or one of more rows than half of these
+    static constexpr int kQHalfBytes = kQRows * 128;
     static constexpr int kQBytes = kHalves * kQHalfBytes;
-    static constexpr int kQBufs = kQBytes <= 16384 ? 2 : 1;
-    static constexpr int kCtlBytes = 512 + 512 + 2048;             // barriers; references; exchange
-    static constexpr int kRoom = 232448 - kCtlBytes - 2 * kPBytes - kQBufs * kQBytes;
+    static constexpr int kCtlBytes = 512 + 10 * kCap * 4;          // barriers; two segments' references and sums
+    static constexpr int kRoom = 232448 - kCtlBytes - 2 * kPBytes - kQBytes;
     static constexpr int kFit = kRoom / kTensorBytes;
     static constexpr int kSlotsK = (kFit + 1) / 2 < kMaxSlots ? (kFit + 1) / 2 : kMaxSlots;
     static constexpr int kSlotsV = kFit / 2 < kMaxSlots ? kFit / 2 : kMaxSlots;
     static constexpr int kVOff = kSlotsK * kTensorBytes;
     static constexpr int kPOff = kVOff + kSlotsV * kTensorBytes;   // (V's last tile is followed by P: see the products)
     static constexpr int kQOff = kPOff + 2 * kPBytes;
-    static constexpr int kCtlOff = kQOff + kQBufs * kQBytes;
+    static constexpr int kCtlOff = kQOff + kQBytes;
     static constexpr size_t kSmemBytes = kCtlOff + kCtlBytes;
-    static constexpr uint32_t kTmemCols = 4 * kCap;                // S twice, O twice
+    static constexpr uint32_t kTmemCols = kCap > 64 ? 512 : 4 * kCap;  // S twice, O twice (a power of two)
 };
 
 struct Ctl {
     uint64_t k_full[kMaxSlots], k_empty[kMaxSlots], v_full[kMaxSlots], v_empty[kMaxSlots];
     uint64_t q_full[2], q_empty[2];
-    uint64_t s_full[2];   // tensor core -> softmax: scores of a tile (and the product two tiles before has read its P)
-    uint64_t p_ready[2];  // softmax -> tensor core
-    uint64_t pv_done;     // a tile's product with V has been added
+    uint64_t s_full[2];   // tensor core -> softmax: scores of a tile
+    uint64_t p_ready[2];  // softmax -> tensor core: P is there, and the scores have been read
+    uint64_t pv_done[2];  // a tile's product with V has been added (and its P read)
     uint64_t o_done[2];   // ... the last one of a segment
-    uint64_t o_free[2];   // softmax -> tensor core: the segment's output has been read
-    uint64_t drain;
+    uint64_t ml_ready[2]; // softmax -> output: the segment's maxima and sums are there
+    uint64_t o_free[2];   // output -> tensor core and softmax: output, maxima and sums have been read
+    uint64_t drain[2];
     uint32_t tmem_base, abort_flag, drain_flag, data_error;
 };
 static_assert(sizeof(Ctl) <= 512, "room of the barriers");
+
+// The two halves of Q's room are used in turn by blocks that fit one, and together by larger ones.
+struct QTurn {
+    uint32_t uses0 = 0, uses1 = 0, at = 0, next = 0;
+    __device__ __forceinline__ bool take(bool both) {  // the half a block starts in: `at`; whether it has both
+        at = both ? 0 : next;
+        if (!both) next ^= 1;
+        if (at == 0) ++uses0;
+        if (at == 1 || both) ++uses1;
+        return both;
+    }
+    __device__ __forceinline__ uint32_t uses() const { return at == 0 ? uses0 : uses1; }
+};
 
 // Key tiles lie as [group of 8 keys][half][8 rows][128 bytes], swizzled: a 16-token page is one TMA box.
 template <int D>
@@ -78,8 +98,8 @@ __device__ __forceinline__ uint32_t key_off(int r, int c) {  // of 16-byte chunk
     return static_cast<uint32_t>(((r >> 3) * (D / 64) + (c >> 3)) * 1024 + (r & 7) * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
-__device__ __forceinline__ void half_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ bool half_any(int id, bool x) {
+__device__ __forceinline__ void team_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool team_any(int id, bool x) {
     uint32_t r;
     asm volatile(
         "{\n"
@@ -93,17 +113,18 @@ __device__ __forceinline__ bool half_any(int id, bool x) {
 }
 
 template <int D, int kCap>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1)
 group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params p) {
     using L = Layout<D, kCap>;
+    constexpr int kTeams = L::kTeams, kProducerWarp = L::kProducerWarp, kScoreWarp = L::kScoreWarp, kValueWarp = L::kValueWarp, kQWarp = L::kQWarp, kOutWarp = L::kOutWarp;
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0u) {  // swizzled tiles need 1024-byte alignment; never expected
         if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, RPX_ERR_CUDA);
         return;
     }
     Ctl* ctl = reinterpret_cast<Ctl*>(smem + L::kCtlOff);
-    float* ref = reinterpret_cast<float*>(smem + L::kCtlOff + 512);        // [half][64]: (the halves may be in different segments)
-    float* exchange = reinterpret_cast<float*>(smem + L::kCtlOff + 1024);  // [half][warp][64]
+    // [O buffer][4 quarters' sums, reference][row] of a segment
+    float* ml = reinterpret_cast<float*>(smem + L::kCtlOff + 512);
     volatile uint32_t* abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -114,19 +135,20 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             mbar_init(&ctl->v_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&ctl->q_full[i], kQWarps);
+            mbar_init(&ctl->q_full[i], 1);
             mbar_init(&ctl->q_empty[i], 1);
             mbar_init(&ctl->s_full[i], 1);
-            mbar_init(&ctl->p_ready[i], 8);
+            mbar_init(&ctl->p_ready[i], 4 * kTeams);
+            mbar_init(&ctl->pv_done[i], 1);
+            mbar_init(&ctl->drain[i], 1);
             mbar_init(&ctl->o_done[i], 1);
-            mbar_init(&ctl->o_free[i], 8);
+            mbar_init(&ctl->ml_ready[i], 4 * kTeams);
+            mbar_init(&ctl->o_free[i], 4);
         }
-        mbar_init(&ctl->pv_done, 1);
-        mbar_init(&ctl->drain, 1);
         ctl->abort_flag = ctl->drain_flag = ctl->data_error = 0;
         fence_barrier_init();
     }
-    if (warp == kMmaWarp) {
+    if (warp == kValueWarp) {
         tmem_alloc(&ctl->tmem_base, L::kTmemCols);
         tmem_relinquish();
     }
@@ -135,12 +157,13 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     tc_fence_after_sync();
     const uint32_t tmem_base = ctl->tmem_base;  // S at columns 0 and kCap, O at 2 kCap and 3 kCap
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
-    Walk walk;
-    walk.start(p);
-    auto rows16 = [&](const Walk& w) { return (w.tokens() * p.group + 15) & ~15; };
+    auto rows16 = [&](const auto& w) { return (w.tokens() * p.group + 15) & ~15; };
 
     if (warp == kProducerWarp) {
         // =========================================================== producer: K a tile ahead of V, through all segments
+        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        Walk walk;
+        walk.start(p);
         bool ok = true;
         uint32_t nk = 0, nv = 0;
         // the tile whose V comes next: page number of this lane's page, boxes, KV head
@@ -191,252 +214,340 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             for (uint32_t i = nv > L::kSlotsV ? nv - L::kSlotsV : 0u; i < nv; ++i)
                 mbar_wait(&ctl->v_full[i % L::kSlotsV], (i / L::kSlotsV) & 1u, &ctl->drain_flag, kDrainLimitCycles);
         }
-    } else if (warp == kMmaWarp) {
-        // =========================================================== tcgen05 issuer (one thread)
+    } else if (warp == kScoreWarp) {
+        // =========================================================== S^T = K Q^T, by one thread
+        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        Walk walk;
+        walk.start(p);
+        if (elect_one()) {
+            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem), 16, L::kHalves * 1024);
+            const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem + L::kQOff), 16, 1024);
+            bool ok = true;
+            uint32_t tiles = 0;
+            QTurn turn;
+            while (ok && walk.next(p)) {
+                const int32_t n16 = rows16(walk);
+                const bool both = turn.take(n16 > L::kQRows / 2);
+                const uint32_t idesc = make_idesc_bf16(128, n16, false, false);
+                const uint64_t qd = q_desc + static_cast<uint64_t>(turn.at * (L::kQRows / 2) * 8);
+                ok = mbar_wait(&ctl->q_full[turn.at], (turn.uses() - 1) & 1u, abort_flag) &&
+                     (!both || mbar_wait(&ctl->q_full[1], (turn.uses1 - 1) & 1u, abort_flag));
+                for (int32_t t = walk.t0; ok && t < walk.t1; ++t, ++tiles) {
+                    const uint32_t st = tiles % L::kSlotsK, b = tiles & 1u;
+                    ok = (tiles < 2 || mbar_wait(&ctl->p_ready[b], ((tiles >> 1) - 1) & 1u, abort_flag)) &&
+                         mbar_wait(&ctl->k_full[st], (tiles / L::kSlotsK) & 1u, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint64_t kd = k_desc + static_cast<uint64_t>(st * (L::kTensorBytes >> 4));
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        umma_bf16_ss(tmem_base + b * kCap, kd + (ks >> 2) * 64 + 2 * (ks & 3), qd + (ks >> 2) * (L::kQHalfBytes >> 4) + 2 * (ks & 3), idesc, ks != 0);
+                    umma_commit(&ctl->s_full[b]);
+                    umma_commit(&ctl->k_empty[st]);
+                    if (t + 1 == walk.t1) {
+                        umma_commit(&ctl->q_empty[turn.at]);
+                        if (both) umma_commit(&ctl->q_empty[1]);
+                    }
+                }
+            }
+            if (!ok) {
+                umma_commit(&ctl->drain[0]);
+                mbar_wait(&ctl->drain[0], 0, &ctl->drain_flag, kDrainLimitCycles);
+            }
+        }
+    } else if (warp == kValueWarp) {
+        // =========================================================== O^T += V^T P^T, by one thread
+        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        Walk walk;
+        walk.start(p);
         if (elect_one()) {
             // D = 64: M stays 128, and the lanes 64 .. 127 of O^T, which nobody reads, are fed by whatever lies 1 KB on
-            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem), 16, L::kHalves * 1024);
             const uint64_t v_desc = make_smem_desc_sw128(smem_u32(smem + L::kVOff), 1024, L::kHalves * 1024);
             const uint64_t p_desc = make_smem_desc_sw128(smem_u32(smem + L::kPOff), 16, 1024);
-            const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem + L::kQOff), 16, 1024);
-            Walk ahead = walk;  // the scores run a tile ahead of the products with V, into the next segment too
-            bool ok = true, more = ahead.next(p);
-            int32_t at = ahead.t0;      // the tile whose scores come next
-            uint32_t q_segments = 0, segments = 0, tiles = 0, scored = 0;
-            auto issue_scores = [&]() {
-                const uint32_t st = scored % L::kSlotsK, b = scored & 1u, qb = q_segments % L::kQBufs;
-                if (at == ahead.t0 && !mbar_wait(&ctl->q_full[qb], (q_segments / L::kQBufs) & 1u, abort_flag)) return false;
-                if (!mbar_wait(&ctl->k_full[st], (scored / L::kSlotsK) & 1u, abort_flag)) return false;
-                tc_fence_after_sync();
-                const uint32_t idesc = make_idesc_bf16(128, rows16(ahead), false, false);
-                const uint64_t kd = k_desc + static_cast<uint64_t>(st * (L::kTensorBytes >> 4)), qd = q_desc + static_cast<uint64_t>(qb * (L::kQBytes >> 4));
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    umma_bf16_ss(tmem_base + b * kCap, kd + (ks >> 2) * 64 + 2 * (ks & 3), qd + (ks >> 2) * (L::kQHalfBytes >> 4) + 2 * (ks & 3), idesc, ks != 0);
-                umma_commit(&ctl->s_full[b]);
-                umma_commit(&ctl->k_empty[st]);
-                ++scored;
-                if (++at == ahead.t1) {
-                    umma_commit(&ctl->q_empty[qb]);
-                    ++q_segments;
-                    more = ahead.next(p);
-                    at = ahead.t0;
-                }
-                return true;
-            };
-            if (more) ok = issue_scores();
+            bool ok = true;
+            uint32_t segments = 0, tiles = 0;
             while (ok && walk.next(p)) {
                 const int32_t n16 = rows16(walk);
                 const bool two_terms = 2 * n16 <= L::kPRows;
-                const uint32_t ob = segments & 1u;
-                const uint32_t idesc = make_idesc_bf16(128, n16, true, false);
-                for (int32_t t = walk.t0; t < walk.t1; ++t) {
-                    if (more) ok = issue_scores();
+                const uint32_t ob = segments & 1u, idesc = make_idesc_bf16(128, n16, true, false);
+                if (segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
+                for (int32_t t = walk.t0; ok && t < walk.t1; ++t, ++tiles) {
                     const uint32_t b = tiles & 1u, st = tiles % L::kSlotsV;
-                    if (ok && t == walk.t0 && segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
-                    if (ok) ok = mbar_wait(&ctl->p_ready[b], (tiles >> 1) & 1u, abort_flag) && mbar_wait(&ctl->v_full[st], (tiles / L::kSlotsV) & 1u, abort_flag);
+                    ok = mbar_wait(&ctl->v_full[st], (tiles / L::kSlotsV) & 1u, abort_flag) && mbar_wait(&ctl->p_ready[b], (tiles >> 1) & 1u, abort_flag);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const int32_t steps = (min(kTile, walk.q.len - t * kTile) + 15) / 16;  // pages that were loaded
                     const uint64_t vd = v_desc + static_cast<uint64_t>(st * (L::kTensorBytes >> 4)), pd = p_desc + static_cast<uint64_t>(b * (L::kPBytes >> 4));
-                    for (int32_t ks = 0; ks < steps; ++ks)
-                        umma_bf16_ss(tmem_base + (2 + ob) * kCap, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
-                                     pd + static_cast<uint64_t>((ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, t != walk.t0 || ks != 0);
-                    if (two_terms)
-                        for (int32_t ks = 0; ks < steps; ++ks)
-                            umma_bf16_ss(tmem_base + (2 + ob) * kCap, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
-                                         pd + static_cast<uint64_t>((L::kPRows / 2) * 8 + (ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, 1u);
+                    auto issue = [&](uint64_t pd, bool add) {
+#pragma unroll
+                        for (int32_t ks = 0; ks < kTile / 16; ++ks)
+                            if (ks < steps)
+                                umma_bf16_ss(tmem_base + (2 + ob) * kCap, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
+                                             pd + static_cast<uint64_t>((ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, add || ks != 0);
+                    };
+                    issue(pd, t != walk.t0);
+                    if (two_terms) issue(pd + static_cast<uint64_t>((L::kPRows / 2) * 8), true);
                     umma_commit(&ctl->v_empty[st]);
-                    umma_commit(&ctl->pv_done);
+                    umma_commit(&ctl->pv_done[b]);
                     if (t + 1 == walk.t1) umma_commit(&ctl->o_done[ob]);
-                    ++tiles;
                 }
                 ++segments;
             }
             if (!ok) {
-                umma_commit(&ctl->drain);
-                mbar_wait(&ctl->drain, 0, &ctl->drain_flag, kDrainLimitCycles);
+                umma_commit(&ctl->drain[1]);
+                mbar_wait(&ctl->drain[1], 0, &ctl->drain_flag, kDrainLimitCycles);
             }
         }
         __syncwarp();
         // the join may start on the SMs that become free
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    } else if (warp >= kQWarp) {
+    } else if (warp == kQWarp) {
         // =========================================================== Q of a segment's rows, zeros up to the next 16
-        uint32_t segments = 0;
+        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        Walk walk;
+        walk.start(p);
+        QTurn turn;
         while (walk.next(p)) {
-            const uint32_t qb = segments % L::kQBufs;
-            if (segments >= L::kQBufs && !mbar_wait(&ctl->q_empty[qb], ((segments / L::kQBufs) - 1) & 1u, abort_flag)) break;
-            uint8_t* dst = smem + L::kQOff + qb * L::kQBytes;
+            const bool both = turn.take(rows16(walk) > L::kQRows / 2);
+            if ((turn.uses() > 1 && !mbar_wait(&ctl->q_empty[turn.at], turn.uses() & 1u, abort_flag)) ||
+                (both && turn.uses1 > 1 && !mbar_wait(&ctl->q_empty[1], turn.uses1 & 1u, abort_flag)))
+                break;
+            uint8_t* dst = smem + L::kQOff + turn.at * (L::kQRows / 2) * 128;
             const int32_t rows = walk.tokens() * p.group, n16 = rows16(walk);
             const int64_t first = static_cast<int64_t>(walk.q.tok0) + walk.token0();
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + first * p.q_stride + static_cast<int64_t>(walk.head) * p.group * D;
-            constexpr int kBatch = 4, kChunks = D / 8;
-            for (int32_t i0 = threadIdx.x - kQWarp * 32; i0 < n16 * kChunks; i0 += kBatch * kQWarps * 32) {
-                uint4 x[kBatch];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const int32_t i = i0 + u * kQWarps * 32, r = i / kChunks, c = i % kChunks, token = r / p.group;
-                    x[u] = make_uint4(0u, 0u, 0u, 0u);
-                    if (r < rows) x[u] = __ldg(reinterpret_cast<const uint4*>(src + token * p.q_stride + (r - token * p.group) * D) + c);
-                }
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const int32_t i = i0 + u * kQWarps * 32, r = i / kChunks, c = i % kChunks;
-                    if (r < n16) *reinterpret_cast<uint4*>(dst + (c >> 3) * L::kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = x[u];
-                }
+            // a thread copies 16-byte chunk c of every kStep-th row
+            constexpr int kChunks = D / 8, kStep = 32 / kChunks;
+            const int32_t c = lane % kChunks;
+            int32_t r = lane / kChunks, in_group = r - over_group(p, r) * p.group;
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + (first + over_group(p, r)) * p.q_stride + static_cast<int64_t>(walk.head) * p.group * D + c * 8;
+            for (; r < n16; r += kStep) {
+                uint8_t* to = dst + (c >> 3) * L::kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+                if (r < rows) cp_async_16(to, src + in_group * D);
+                else *reinterpret_cast<uint4*>(to) = make_uint4(0u, 0u, 0u, 0u);
+                for (in_group += kStep; in_group >= p.group; in_group -= p.group) src += p.q_stride;
             }
+            cp_async_wait_all();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl->q_full[qb]);
+            if (lane == 0) {
+                mbar_arrive(&ctl->q_full[turn.at]);
+                if (both) mbar_arrive(&ctl->q_full[1]);
+            }
+        }
+    } else if (warp >= kOutWarp) {
+        // =========================================================== output: a warp 32 elements of D of all rows
+        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        Walk walk;
+        walk.start(p);
+        const int quarter = warp & 3;
+        const int32_t d = quarter * 32 + lane;
+        uint32_t segments = 0;
+        while (walk.next(p)) {
+            const uint32_t ob = segments & 1u;
+            const int32_t rows = walk.tokens() * p.group;
+            const bool own = walk.e >= p.n_groups, whole = walk.t0 == 0 && walk.t1 == walk.q.tiles();
+            const bool last_word = whole && own && walk.q.page0 == 0;  // nothing to add: this is the result
+            const float* now = ml + ob * 5 * kCap;
+            auto sum_of = [&](int32_t r) { return (now[r] + now[kCap + r]) + (now[2 * kCap + r] + now[3 * kCap + r]); };
+            // where the block's rows go: in order in a slot, or each in its own place
+            const int64_t first_row = (static_cast<int64_t>(walk.q.tok0) + walk.token0()) * p.num_q_heads + walk.head * p.group;
+            const int64_t base = whole ? (own ? p.total_tokens * p.num_q_heads : 0) + first_row : (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
+            const int32_t skip = whole ? p.num_q_heads - p.group : 0;  // rows between a token's last and the next one's first
+            if (!mbar_wait(&ctl->ml_ready[ob], (segments >> 1) & 1u, abort_flag)) break;
+            if (quarter == 0)
+                for (int32_t r = lane; r < rows; r += 32) {
+                    const int32_t at = r + over_group(p, r) * skip;
+                    const float2 x = make_float2(now[4 * kCap + r], sum_of(r));
+                    if (!whole) p.part_ml[base + at] = x;
+                    else if (!last_word) p.whole_ml[base + at] = x;
+                    else if (p.lse != nullptr) p.lse[first_row + at] = (x.x + log2f(x.y)) * kLn2;
+                }
+            if (!mbar_wait(&ctl->o_done[ob], (segments >> 1) & 1u, abort_flag)) break;
+            tc_fence_after_sync();
+            const uint32_t o_addr = tmem_base + (2 + ob) * kCap + (static_cast<uint32_t>(quarter * 32) << 16);
+            if (d < D || D == 128) {
+                float* dst = (whole ? p.whole_o : p.part_o) + base * D + d;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + first_row * D + d;
+                int32_t in_group = 0;
+                int64_t at = 0;
+#pragma unroll 1
+                for (int32_t c = 0; c < rows; c += 8) {
+                    uint32_t o[8];
+                    tmem_ld8(o_addr + c, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < rows) {
+                            if (last_word) out[at] = __float2bfloat16_rn(__uint_as_float(o[i]) / sum_of(c + i));
+                            else dst[at] = __uint_as_float(o[i]);
+                            at += D;
+                            if (++in_group == p.group) {
+                                in_group = 0;
+                                at += static_cast<int64_t>(skip) * D;
+                            }
+                        }
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl->o_free[ob]);
             ++segments;
         }
     } else {
-        // =========================================================== softmax and output
+        // =========================================================== softmax
         // After a wait that ran out (ok == false) a warp goes through the rest of its walk without waiting: every warp still meets
         // the others at the same barriers, and the outputs of the call are undefined anyway.
-        constexpr int kBlocks = kCap / 16;  // 8-row blocks of a half at most
-        const int half = warp >> 2, quarter = warp & 3, bar = 1 + half;
+        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        Walk walk;
+        walk.start(p);
+        constexpr int kBlocks = L::kBlocks;
+        const int team = warp >> 2, quarter = warp & 3, bar = 1 + team;
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
-        float* mine = exchange + (half * 4 + quarter) * 64;     // this warp's part of the exchange
-        const float* all = exchange + half * 4 * 64;
         const int key0 = quarter * 32 + (lane >> 2);            // this thread's keys of a tile: key0 + 8 m
         const int pair = 2 * (lane & 3);                        // its rows of an 8-row block: pair, pair + 1
         uint32_t tiles = 0, segments = 0;
         bool ok = true;
         while (walk.next(p)) {
             const int32_t len = walk.q.len, tokens = walk.tokens(), token0 = walk.token0(), rows = tokens * p.group, n16 = (rows + 15) & ~15;
-            const int32_t nb = n16 / 16, row0 = half * (n16 / 2);  // blocks and first row of this half
+            const int32_t per_team = (n16 / 8 + kTeams - 1) / kTeams;  // blocks; this team's, and its first row
+            const int32_t nb = max(0, min(per_team, n16 / 8 - team * per_team)), row0 = 8 * team * per_team;
             const bool two_terms = 2 * n16 <= L::kPRows;
             const bool own = walk.e >= p.n_groups;
             const int32_t seen_by_first = own ? len - walk.q.n + token0 + 1 : len;  // keys that the block's first token sees
-            float rf[2 * kBlocks], sum[2 * kBlocks];
+            // of the pairs of rows that this thread holds: what a score has to pass for the reference to be raised, the reference
+            // with its sign turned (0 for a row that has seen no key), and the sum over the thread's keys
+            float limit[2 * kBlocks], base[2 * kBlocks], sum[2 * kBlocks];
 #pragma unroll
             for (int i = 0; i < 2 * kBlocks; ++i) {
-                rf[i] = -CUDART_INF_F;
-                sum[i] = 0.f;
+                limit[i] = -CUDART_INF_F;
+                base[i] = sum[i] = 0.f;
             }
+            auto reference = [&](int i) { return limit[i] == -CUDART_INF_F ? -CUDART_INF_F : -base[i]; };
+            // (a form for every number of blocks: with the count looked at inside, the blocks follow one another instead of
+            // overlapping)
+            auto run_tiles = [&](auto blocks_tag) {
+            constexpr int kNow = decltype(blocks_tag)::value;
             for (int32_t t = walk.t0; t < walk.t1; ++t, ++tiles) {
                 const uint32_t b = tiles & 1u;
                 const bool first = t == walk.t0;
                 if (ok) ok = mbar_wait(&ctl->s_full[b], (tiles >> 1) & 1u, abort_flag);
                 tc_fence_after_sync();
-                uint32_t sc[kBlocks][8];  // [block][2 m + row of the pair]: key m
-#pragma unroll
-                for (int k = 0; k < kBlocks; ++k)
-                    if (k < nb) {
-                        tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr, &sc[k][0]);
-                        tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr + (16u << 16), &sc[k][4]);
-                    }
-                tmem_ld_wait();
                 const int32_t left = len - t * kTile;  // keys from the tile's first on
+                if constexpr (kNow > 0) {
+                uint32_t sc[kNow][8];  // [block][2 m + row of the pair]: key m
+#pragma unroll
+                for (int k = 0; k < kNow; ++k) {
+                    tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr, &sc[k][0]);
+                    tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr + (16u << 16), &sc[k][4]);
+                }
+                tmem_ld_wait();
                 if (left < kTile || (t + 1) * kTile > seen_by_first) {
 #pragma unroll
-                    for (int k = 0; k < kBlocks; ++k)
-                        if (k < nb) {
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int32_t token = min((row0 + 8 * k + pair + e) / p.group, tokens - 1);
-                                const int32_t seen = min(left, seen_by_first + token - t * kTile);
-#pragma unroll
-                                for (int m = 0; m < 4; ++m)
-                                    if (key0 + 8 * m >= seen) sc[k][2 * m + e] = 0xff800000u;  // -inf
-                            }
-                        }
-                }
-                // ---- does any row's reference have to be raised?
-                bool up = false;
-#pragma unroll
-                for (int k = 0; k < kBlocks; ++k)
-                    if (k < nb) {
+                    for (int k = 0; k < kNow; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float top = fmaxf(fmaxf(__uint_as_float(sc[k][e]), __uint_as_float(sc[k][2 + e])),
-                                                    fmaxf(__uint_as_float(sc[k][4 + e]), __uint_as_float(sc[k][6 + e])));
-                            up |= top * p.scale_log2 > rf[2 * k + e] + kRaise;
+                            const int32_t token = min(over_group(p, row0 + 8 * k + pair + e), tokens - 1);
+                            const int32_t seen = min(left, seen_by_first + token - t * kTile);
+#pragma unroll
+                            for (int m = 0; m < 4; ++m)
+                                if (key0 + 8 * m >= seen) sc[k][2 * m + e] = 0xff800000u;  // -inf
                         }
-                    }
-                if (half_any(bar, up || first)) {
+                }
+                // its P has been read: until P is written, its place is where the team's warps exchange numbers, [5][rows]
+                if (ok && tiles >= 2) ok = mbar_wait(&ctl->pv_done[b], ((tiles >> 1) - 1) & 1u, abort_flag);
+                float* all = reinterpret_cast<float*>(smem + L::kPOff + b * L::kPBytes + row0 * 128);
+                auto top_of = [&](int k, int e) {
+                    return fmaxf(fmax3(__uint_as_float(sc[k][e]), __uint_as_float(sc[k][2 + e]), __uint_as_float(sc[k][4 + e])), __uint_as_float(sc[k][6 + e]));
+                };
+                // ---- does any row's reference have to be raised?
+                bool up = first;
 #pragma unroll
-                    for (int k = 0; k < kBlocks; ++k)
-                        if (k < nb) {
+                for (int k = 0; k < kNow; ++k)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float top = fmaxf(fmaxf(__uint_as_float(sc[k][e]), __uint_as_float(sc[k][2 + e])),
-                                                  fmaxf(__uint_as_float(sc[k][4 + e]), __uint_as_float(sc[k][6 + e])));
+                    for (int e = 0; e < 2; ++e) up |= top_of(k, e) > limit[2 * k + e];
+                if (team_any(bar, up)) {
 #pragma unroll
-                                for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                                if (lane < 4) mine[8 * k + pair + e] = top;
-                            }
+                    for (int k = 0; k < kNow; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float top = top_of(k, e);
+#pragma unroll
+                            for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                            if (lane < 4) all[(quarter * kNow + k) * 8 + pair + e] = top;
                         }
-                    half_sync(bar);
-                    float keep[2 * kBlocks];
+                    team_sync(bar);
+                    float keep[2 * kNow];
 #pragma unroll
-                    for (int k = 0; k < kBlocks; ++k)
-                        if (k < nb) {
+                    for (int k = 0; k < kNow; ++k)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int r = 8 * k + pair + e;
-                                const float top = fmaxf(fmaxf(all[r], all[64 + r]), fmaxf(all[128 + r], all[192 + r])) * p.scale_log2;
-                                const float old = rf[2 * k + e];
-                                const bool raise = top > old + kRaise;
-                                rf[2 * k + e] = raise ? top : old;
-                                keep[2 * k + e] = raise ? fast_exp2(old - top) : 1.f;  // (from -inf: 0)
-                                sum[2 * k + e] *= keep[2 * k + e];
-                                if (quarter == 0 && lane < 4) ref[half * 64 + r] = rf[2 * k + e];
-                            }
+                        for (int e = 0; e < 2; ++e) {
+                            const int r = 8 * k + pair + e;
+                            const float top = fmaxf(fmaxf(all[r], all[8 * kNow + r]), fmaxf(all[16 * kNow + r], all[24 * kNow + r])) * p.scale_log2;
+                            const float old = reference(2 * k + e);
+                            const bool raise = top > old + kRaise;
+                            const float now = raise ? top : old;
+                            keep[2 * k + e] = raise ? fast_exp2(old - top) : 1.f;  // (from -inf: 0)
+                            sum[2 * k + e] *= keep[2 * k + e];
+                            base[2 * k + e] = now == -CUDART_INF_F ? 0.f : -now;
+                            limit[2 * k + e] = (now + kRaise) / p.scale_log2;
                         }
                     if (!first) {  // what O holds goes along
-                        half_sync(bar);
+                        if (quarter == 0 && lane < 4) {
 #pragma unroll
-                        for (int k = 0; k < kBlocks; ++k)
-                            if (k < nb && quarter == 0 && lane < 4) {
-                                exchange[half * 256 + 8 * k + pair] = keep[2 * k];
-                                exchange[half * 256 + 8 * k + pair + 1] = keep[2 * k + 1];
-                            }
-                        half_sync(bar);
-                        if (ok) ok = mbar_wait(&ctl->pv_done, (tiles - 1) & 1u, abort_flag);
+                            for (int k = 0; k < kNow; ++k)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) all[32 * kNow + 8 * k + pair + e] = keep[2 * k + e];
+                        }
+                        team_sync(bar);
+                        if (ok) ok = mbar_wait(&ctl->pv_done[b ^ 1u], ((tiles - 1) >> 1) & 1u, abort_flag);
                         tc_fence_after_sync();
 #pragma unroll 1
-                        for (int32_t c = 0; c < 8 * nb; c += 8) {
+                        for (int c = 0; c < 8 * kNow; c += 8) {
                             uint32_t o[8];
                             const uint32_t at = tmem_base + (2 + (segments & 1u)) * kCap + row0 + c + lane_addr;
                             tmem_ld8(at, o);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[c + i]);
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kNow + c + i]);
                             tmem_st8(at, o);
                         }
                         tmem_st_wait();
                     }
+                    team_sync(bar);  // the exchange has been read
                 }
                 // ---- P = 2^(s - reference): 0 for a masked key (-inf), NaN for NaN and for +inf (inf - inf)
-                uint8_t* pb = smem + L::kPOff + b * L::kPBytes + (quarter >> 1) * L::kPHalfBytes;
+                const uint32_t pb = smem_u32(smem + L::kPOff + b * L::kPBytes + (quarter >> 1) * L::kPHalfBytes);
                 const int chunk = (quarter & 1) * 4 + (lane >> 3), prow = row0 + (lane & 7);
+                const uint32_t at0 = pb + prow * 128 + ((chunk ^ (prow & 7)) << 4);  // (row0 is a multiple of 8)
                 const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2);
+                auto store_p = [&](auto two_tag) {
 #pragma unroll
-                for (int k = 0; k < kBlocks; ++k)
-                    if (k < nb) {
-                        const float base0 = rf[2 * k] == -CUDART_INF_F ? 0.f : rf[2 * k];  // a row that has seen no key yet
-                        const float base1 = rf[2 * k + 1] == -CUDART_INF_F ? 0.f : rf[2 * k + 1];
-                        const uint64_t base2 = f2_pack(-base0, -base1);
-                        uint32_t hi[4], lo[4];
+                    for (int k = 0; k < kNow; ++k) {
+                        const uint64_t base2 = f2_pack(base[2 * k], base[2 * k + 1]);
+                        uint32_t hi[4];
+                        float x[8];
                         uint64_t s2 = f2_pack(sum[2 * k], sum[2 * k + 1]);
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
-                            float x0, x1;
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[k][2 * m]), __uint_as_float(sc[k][2 * m + 1])), scale2, base2), x0, x1);
-                            x0 = fast_exp2(x0);
-                            x1 = fast_exp2(x1);
-                            s2 = f2_add(s2, f2_pack(x0, x1));
-                            hi[m] = pack_bf16x2(x0, x1);
-                            lo[m] = pack_bf16x2(x0 - __uint_as_float(hi[m] << 16), x1 - __uint_as_float(hi[m] & 0xffff0000u));
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[k][2 * m]), __uint_as_float(sc[k][2 * m + 1])), scale2, base2), x[2 * m], x[2 * m + 1]);
+                            x[2 * m] = fast_exp2(x[2 * m]);
+                            x[2 * m + 1] = fast_exp2(x[2 * m + 1]);
+                            hi[m] = pack_bf16x2(x[2 * m], x[2 * m + 1]);
                         }
+                        s2 = f2_add(s2, f2_add(f2_add(f2_pack(x[0], x[1]), f2_pack(x[2], x[3])), f2_add(f2_pack(x[4], x[5]), f2_pack(x[6], x[7]))));
                         f2_unpack(s2, sum[2 * k], sum[2 * k + 1]);
-                        const uint32_t at = smem_u32(pb) + (prow + 8 * k) * 128 + ((chunk ^ ((prow + 8 * k) & 7)) << 4);
-                        stsm_x4_trans(at, hi[0], hi[1], hi[2], hi[3]);
-                        if (two_terms) stsm_x4_trans(at + (L::kPRows / 2) * 128, lo[0], lo[1], lo[2], lo[3]);
+                        stsm_x4_trans(at0 + 8 * k * 128, hi[0], hi[1], hi[2], hi[3]);
+                        if constexpr (decltype(two_tag)::value) {
+#pragma unroll
+                            for (int m = 0; m < 4; ++m)
+                                hi[m] = pack_bf16x2(x[2 * m] - __uint_as_float(hi[m] << 16), x[2 * m + 1] - __uint_as_float(hi[m] & 0xffff0000u));
+                            stsm_x4_trans(at0 + (8 * k + L::kPRows / 2) * 128, hi[0], hi[1], hi[2], hi[3]);
+                        }
                     }
+                };
+                if (kCap <= 64 || two_terms) store_p(std::true_type{});
+                else store_p(std::false_type{});
+                }
                 // ---- V's rows behind the last key of a page that was loaded may hold anything: a probability of 0 must not
                 // meet a NaN there
                 const int32_t ragged = left < kTile ? left & 15 : 0;
@@ -444,7 +555,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                     const uint32_t st = tiles % L::kSlotsV;
                     if (ok) ok = mbar_wait(&ctl->v_full[st], (tiles / L::kSlotsV) & 1u, abort_flag);
                     uint8_t* v = smem + L::kVOff + st * L::kTensorBytes;
-                    for (int32_t i = threadIdx.x; i < (16 - ragged) * (D / 8); i += 256)
+                    for (int32_t i = threadIdx.x; i < (16 - ragged) * (D / 8); i += 128 * kTeams)
                         *reinterpret_cast<uint4*>(v + key_off<D>(left + i / (D / 8), i % (D / 8))) = make_uint4(0u, 0u, 0u, 0u);
                 }
                 fence_proxy_async_smem();
@@ -452,8 +563,16 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl->p_ready[b]);
             }
-            // ---- the segment's sums and output
-            half_sync(bar);  // the exchange has been read
+            };
+            if (nb == kBlocks) run_tiles(std::integral_constant<int, kBlocks>{});
+            else if (nb == 0) run_tiles(std::integral_constant<int, 0>{});
+            else if (nb == 1) run_tiles(std::integral_constant<int, 1>{});
+            else if (nb == 2) run_tiles(std::integral_constant<int, (kBlocks > 2 ? 2 : 1)>{});
+            else run_tiles(std::integral_constant<int, (kBlocks > 3 ? 3 : 1)>{});
+            // ---- the segment's references and this warp's sums, for the output warps
+            const uint32_t ob = segments & 1u;
+            if (ok && segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
+            float* mine = ml + (ob * 5 + quarter) * kCap + row0;
 #pragma unroll
             for (int k = 0; k < kBlocks; ++k)
                 if (k < nb) {
@@ -463,49 +582,17 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll
                         for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
                         if (lane < 4) mine[8 * k + pair + e] = x;
+                        if (quarter == 0 && lane < 4) mine[4 * kCap + 8 * k + pair + e] = reference(2 * k + e);
                     }
                 }
-            half_sync(bar);
-            const bool whole = walk.t0 == 0 && walk.t1 == walk.q.tiles;
-            const bool last_word = whole && own && walk.q.page0 == 0;  // nothing to add: this is the result
-            const uint32_t ob = segments & 1u;
-            if (ok) ok = mbar_wait(&ctl->o_done[ob], (segments >> 1) & 1u, abort_flag);
-            tc_fence_after_sync();
-            const int64_t slot = (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
-            const int64_t kind = own ? p.total_tokens * p.num_q_heads : 0;
-            const int32_t d = quarter * 32 + lane;
-#pragma unroll 1
-            for (int32_t c = 0; c < 8 * nb; c += 8) {
-                uint32_t o[8];
-                tmem_ld8(tmem_base + (2 + ob) * kCap + row0 + c + lane_addr, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int32_t r = row0 + c + i;
-                    if (r >= rows) break;
-                    const float total = (all[c + i] + all[64 + c + i]) + (all[128 + c + i] + all[192 + c + i]), m = ref[half * 64 + c + i];
-                    const int32_t token = r / p.group;
-                    const int64_t out_row = (static_cast<int64_t>(walk.q.tok0) + token0 + token) * p.num_q_heads + walk.head * p.group + (r - token * p.group);
-                    if (last_word) {
-                        if (d < D) static_cast<__nv_bfloat16*>(p.out)[out_row * D + d] = __float2bfloat16_rn(__uint_as_float(o[i]) / total);
-                        if (d == 0 && p.lse != nullptr) p.lse[out_row] = (m + log2f(total)) * kLn2;
-                    } else {
-                        float* po = whole ? p.whole_o + (kind + out_row) * D : p.part_o + (slot + r) * D;
-                        float2* pm = whole ? p.whole_ml + kind + out_row : p.part_ml + slot + r;
-                        if (d < D) po[d] = __uint_as_float(o[i]);
-                        if (d == 0) *pm = make_float2(m, total);
-                    }
-                }
-            }
-            tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl->o_free[ob]);
+            if (lane == 0) mbar_arrive(&ctl->ml_ready[ob]);
             ++segments;
         }
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == kMmaWarp) {
+    if (warp == kValueWarp) {
         tc_fence_after_sync();
         tmem_dealloc(tmem_base, L::kTmemCols);
     }
@@ -530,7 +617,7 @@ rpx_status_t launch(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t s
     if (rpx_status_t rc = encode_tmap_bf16(&tv, cache.v_cache, 4, dims, strides, box)) return rc;
     auto* kernel = group_tile_kernel<D, kCap>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess) return RPX_ERR_CUDA;
-    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), kThreads, L::kSmemBytes, stream, tk, tv, p);
+    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, L::kSmemBytes, stream, tk, tv, p);
 }
 
 template <int D>
@@ -539,7 +626,7 @@ rpx_status_t launch_cap(const Params& p, const rpx_kv_cache_t& cache, cudaStream
         case 16: return launch<D, 16>(p, cache, stream);
         case 32: return launch<D, 32>(p, cache, stream);
         case 64: return launch<D, 64>(p, cache, stream);
-        default: return launch<D, 128>(p, cache, stream);
+        default: return launch<D, (D == 128 ? 112 : 128)>(p, cache, stream);
     }
 }
 
