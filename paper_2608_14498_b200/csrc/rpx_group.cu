@@ -25,20 +25,20 @@ constexpr int kPlanThreads = 1024;
 constexpr int kWorkUnits = 30, kRowUnits = 75, kSegmentWork = 130;
 
 __device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t group = -1) {
-    Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, 0};
+    Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, len / kTile + (len % kTile != 0 ? 1 : 0)};
     if (n == 0 || len == 0) {
         e.n = e.len = 0;
         return e;
     }
     // Blocks of at most `cap` rows; of at most 64 where the keys are few, so that probabilities keep their second term: over
     // many keys the rounding averages out.
-    const int32_t rows = e.tiles() <= 2 && p.cap > 64 ? 64 : p.cap, per = max(1, rows / p.group);
+    const int32_t rows = e.tiles <= 2 && p.cap > 64 ? 64 : p.cap, per = max(1, rows / p.group);  // (at most p.cap / group: Q's box)
     e.blocks = n <= per ? 1 : (n + per - 1) / per;
     e.block_tokens = e.blocks == 1 ? n : (n + e.blocks - 1) / e.blocks;
     // A tile's bytes are kTileUnits of this SM's share of HBM, once for all blocks; the work against a block overlaps with that, but
     // a segment's first scores and last output do not with each other.
     const int32_t rows_now = e.block_tokens * p.group, work = kWorkUnits + rows_now * kRowUnits / 128;
-    const int32_t bytes = p.tile_units / e.blocks, beside = kSegmentWork / e.tiles();
+    const int32_t bytes = p.tile_units / e.blocks, beside = kSegmentWork / e.tiles;
     e.weight = max(bytes, work + beside);
     return e;
 }
@@ -241,7 +241,7 @@ __device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int64
     const int64_t unit = q.unit0 + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
     const int64_t c0 = quotient(unit, size);
     Sets r;
-    r.n = static_cast<int32_t>(quotient(unit + static_cast<int64_t>(q.tiles() - 1) * q.weight, size) - c0) + 1;
+    r.n = static_cast<int32_t>(quotient(unit + static_cast<int64_t>(q.tiles - 1) * q.weight, size) - c0) + 1;
     r.whole = r.n == 1;
     // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
     r.first = r.whole ? own_row : (c0 * 2 + 1) * p.cap + (in - block * q.block_tokens) * p.group + in_group;

@@ -34,15 +34,14 @@ struct __align__(16) Entry {
     int32_t weight;         // units of a key tile against one block
     int64_t unit0;          // its first unit
     int32_t group;          // of a sequence: the group whose shared pages it reads as well, or -1
-    int32_t unused;
-    __device__ __forceinline__ int32_t tiles() const { return len / kTile + (len % kTile != 0 ? 1 : 0); }
-    __device__ __forceinline__ int64_t segment_units() const { return static_cast<int64_t>(tiles()) * weight + kSegment; }
+    int32_t tiles;          // key tiles
+    __device__ __forceinline__ int64_t segment_units() const { return static_cast<int64_t>(tiles) * weight + kSegment; }
 };
 
 __device__ __forceinline__ Entry load_entry(const Entry* at) {
     const int4 a = __ldcg(reinterpret_cast<const int4*>(at)), b = __ldcg(reinterpret_cast<const int4*>(at) + 1);
     const longlong2 c = __ldcg(reinterpret_cast<const longlong2*>(at) + 2);
-    return Entry{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, static_cast<int32_t>(c.y), 0};
+    return Entry{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, static_cast<int32_t>(c.y), static_cast<int32_t>(c.y >> 32)};
 }
 
 struct Start;
@@ -161,12 +160,12 @@ __device__ __forceinline__ Start find_start(const Params& p, int64_t total, int3
 // Walks the pieces of segments inside a CTA's part of the line; every role walks it alike.
 struct Walk {
     int32_t e, head, block, t0, t1;  // current segment: entry, KV head, row block, key tiles [t0, t1)
-    int64_t left;                    // units of the piece behind t1's first
+    int32_t left;                    // units of the piece behind t1's first
     Entry q;
     __device__ __forceinline__ void start(const Params& p) {
         const Start* s = p.starts + blockIdx.x;
         const int4 a = __ldcg(reinterpret_cast<const int4*>(&s->e));
-        left = __ldcg(&s->left);
+        left = static_cast<int32_t>(__ldcg(&s->left));  // (2^31 units are 40 s)
         q = load_entry(&s->q);
         e = a.x;
         head = a.y;
@@ -176,7 +175,7 @@ struct Walk {
     }
     __device__ __forceinline__ bool next(const Params& p) {
         if (left <= 0) return false;
-        if (t1 == q.tiles()) {
+        if (t1 == q.tiles) {
             t1 = 0;
             if (++block == q.blocks) {
                 block = 0;
@@ -192,9 +191,14 @@ struct Walk {
             if (left <= 0) return false;  // not even the first tile starts in this piece
         }
         t0 = t1;
-        t1 = q.tiles();
-        if (static_cast<int64_t>(t1 - t0) * q.weight > left) t1 = t0 + static_cast<int32_t>(min(quotient(left + q.weight - 1, q.weight), static_cast<int64_t>(t1 - t0)));
-        left -= static_cast<int64_t>(t1 - t0) * q.weight;
+        t1 = q.tiles;
+        const int64_t all = static_cast<int64_t>(t1 - t0) * q.weight;
+        if (all > left) {
+            t1 = t0 + (left + q.weight - 1) / q.weight;
+            left = 0;
+        } else {
+            left -= static_cast<int32_t>(all);
+        }
         return true;
     }
     __device__ __forceinline__ int32_t token0() const { return block * q.block_tokens; }

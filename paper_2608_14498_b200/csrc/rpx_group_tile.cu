@@ -9,8 +9,9 @@
 // P goes through shared memory, as bf16 [row][key] (K-major B operand).  The scores are loaded from tensor memory in the fragment
 // that stmatrix takes (16 lanes x 256 bits: a thread holds two rows of one key), so a warp stores its 32 keys of eight rows
 // with one instruction.  While a block has at most half of P's room in rows, the other half takes what the rounding to bf16
-// dropped: probabilities enter the product as two terms (off by 2^-17) and not as one (2^-8), and the product is done twice,
-// which costs nothing where the cache's bytes bound.
+// dropped, as so many more rows of the same product: probabilities enter it as two terms (off by 2^-17) and not as one (2^-8),
+// and the two outputs are added when they are read.  That costs nothing where the cache's bytes bound: V, the larger operand, is
+// read once.
 //
 // A row's running reference is raised only when a score passes it by 2^8: what is kept is exact whatever the reference, so all
 // the threads of a tile need to agree on is whether one of them has to (one barrier with a vote).
@@ -51,6 +52,10 @@ struct Layout {
     static constexpr int kPBytes = 2 * kPHalfBytes;
     static constexpr int kQRows = kCap <= 64 ? 2 * kCap : kCap;    // two blocks' Q, or one of more rows than half of these
     static constexpr int kQHalfBytes = kQRows * 128;
+    // tokens of the box that a block of several lands in; a block that one half holds has at most as many
+    static __host__ __device__ constexpr int32_t q_box_tokens(bool both, int32_t group) {
+        return (both ? kQRows : kQRows / 2) / group > 1 ? (both ? kQRows : kQRows / 2) / group : 1;
+    }
     static constexpr int kQBytes = kHalves * kQHalfBytes;
     static constexpr int kCtlBytes = 512 + 10 * kCap * 4;          // barriers; two segments' references and sums
     static constexpr int kRoom = 232448 - kCtlBytes - 2 * kPBytes - kQBytes;
@@ -62,7 +67,8 @@ struct Layout {
     static constexpr int kQOff = kPOff + 2 * kPBytes;
     static constexpr int kCtlOff = kQOff + kQBytes;
     static constexpr size_t kSmemBytes = kCtlOff + kCtlBytes;
-    static constexpr uint32_t kTmemCols = kCap > 64 ? 512 : 4 * kCap;  // S twice, O twice (a power of two)
+    static constexpr int kOCol = 2 * kCap;                         // O twice, kPRows columns each, behind S twice
+    static constexpr uint32_t kTmemCols = kCap >= 64 ? 512 : 8 * kCap;  // (a power of two)
 };
 
 struct Ctl {
@@ -114,7 +120,8 @@ __device__ __forceinline__ bool team_any(int id, bool x) {
 
 template <int D, int kCap>
 __global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1)
-group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params p) {
+group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_constant__ CUtensorMap tmap_qh, const __grid_constant__ CUtensorMap tmap_qb,
+                  const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params p) {
     using L = Layout<D, kCap>;
     constexpr int kTeams = L::kTeams, kProducerWarp = L::kProducerWarp, kScoreWarp = L::kScoreWarp, kValueWarp = L::kValueWarp, kQWarp = L::kQWarp, kOutWarp = L::kOutWarp;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -155,7 +162,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem_base = ctl->tmem_base;  // S at columns 0 and kCap, O at 2 kCap and 3 kCap
+    const uint32_t tmem_base = ctl->tmem_base;  // S at columns 0 and kCap, O at kOCol
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
     auto rows16 = [&](const auto& w) { return (w.tokens() * p.group + 15) & ~15; };
 
@@ -269,7 +276,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             while (ok && walk.next(p)) {
                 const int32_t n16 = rows16(walk);
                 const bool two_terms = 2 * n16 <= L::kPRows;
-                const uint32_t ob = segments & 1u, idesc = make_idesc_bf16(128, n16, true, false);
+                const uint32_t ob = segments & 1u, idesc = make_idesc_bf16(128, two_terms ? 2 * n16 : n16, true, false);
                 if (segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
                 for (int32_t t = walk.t0; ok && t < walk.t1; ++t, ++tiles) {
                     const uint32_t b = tiles & 1u, st = tiles % L::kSlotsV;
@@ -278,15 +285,11 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                     tc_fence_after_sync();
                     const int32_t steps = (min(kTile, walk.q.len - t * kTile) + 15) / 16;  // pages that were loaded
                     const uint64_t vd = v_desc + static_cast<uint64_t>(st * (L::kTensorBytes >> 4)), pd = p_desc + static_cast<uint64_t>(b * (L::kPBytes >> 4));
-                    auto issue = [&](uint64_t pd, bool add) {
 #pragma unroll
-                        for (int32_t ks = 0; ks < kTile / 16; ++ks)
-                            if (ks < steps)
-                                umma_bf16_ss(tmem_base + (2 + ob) * kCap, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
-                                             pd + static_cast<uint64_t>((ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, add || ks != 0);
-                    };
-                    issue(pd, t != walk.t0);
-                    if (two_terms) issue(pd + static_cast<uint64_t>((L::kPRows / 2) * 8), true);
+                    for (int32_t ks = 0; ks < kTile / 16; ++ks)
+                        if (ks < steps)
+                            umma_bf16_ss(tmem_base + L::kOCol + ob * L::kPRows, vd + static_cast<uint64_t>(ks * (L::kHalves * 128)),
+                                         pd + static_cast<uint64_t>((ks >> 2) * (L::kPHalfBytes >> 4) + 2 * (ks & 3)), idesc, t != walk.t0 || ks != 0);
                     umma_commit(&ctl->v_empty[st]);
                     umma_commit(&ctl->pv_done[b]);
                     if (t + 1 == walk.t1) umma_commit(&ctl->o_done[ob]);
@@ -302,36 +305,31 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         // the join may start on the SMs that become free
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     } else if (warp == kQWarp) {
-        // =========================================================== Q of a segment's rows, zeros up to the next 16
+        // =========================================================== Q of a segment's block
+        // One box lands as consecutive 128-byte rows: of one token, of as many as a half of Q's room holds, or of as many as both do.
+        // (What lies behind the block's rows is another token's, or was there before: those rows are nobody's.)
         if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
         walk.start(p);
-        QTurn turn;
-        while (walk.next(p)) {
-            const bool both = turn.take(rows16(walk) > L::kQRows / 2);
-            if ((turn.uses() > 1 && !mbar_wait(&ctl->q_empty[turn.at], turn.uses() & 1u, abort_flag)) ||
-                (both && turn.uses1 > 1 && !mbar_wait(&ctl->q_empty[1], turn.uses1 & 1u, abort_flag)))
-                break;
-            uint8_t* dst = smem + L::kQOff + turn.at * (L::kQRows / 2) * 128;
-            const int32_t rows = walk.tokens() * p.group, n16 = rows16(walk);
-            const int64_t first = static_cast<int64_t>(walk.q.tok0) + walk.token0();
-            // a thread copies 16-byte chunk c of every kStep-th row
-            constexpr int kChunks = D / 8, kStep = 32 / kChunks;
-            const int32_t c = lane % kChunks;
-            int32_t r = lane / kChunks, in_group = r - over_group(p, r) * p.group;
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + (first + over_group(p, r)) * p.q_stride + static_cast<int64_t>(walk.head) * p.group * D + c * 8;
-            for (; r < n16; r += kStep) {
-                uint8_t* to = dst + (c >> 3) * L::kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-                if (r < rows) cp_async_16(to, src + in_group * D);
-                else *reinterpret_cast<uint4*>(to) = make_uint4(0u, 0u, 0u, 0u);
-                for (in_group += kStep; in_group >= p.group; in_group -= p.group) src += p.q_stride;
-            }
-            cp_async_wait_all();
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&ctl->q_full[turn.at]);
+        if (elect_one()) {
+            QTurn turn;
+            bool ok = true;
+            while (walk.next(p)) {
+                const bool both = turn.take(rows16(walk) > L::kQRows / 2);
+                ok = (turn.uses() <= 1 || mbar_wait(&ctl->q_empty[turn.at], turn.uses() & 1u, abort_flag)) &&
+                     (!both || turn.uses1 <= 1 || mbar_wait(&ctl->q_empty[1], turn.uses1 & 1u, abort_flag));
+                if (!ok) break;
+                const bool one = walk.tokens() == 1;
+                const int32_t box_tokens = one ? 1 : L::q_box_tokens(both, p.group);
+                mbar_arrive_expect_tx(&ctl->q_full[turn.at], static_cast<uint32_t>(box_tokens * p.group * L::kHalves) * 128);
                 if (both) mbar_arrive(&ctl->q_full[1]);
+                for (int hf = 0; hf < L::kHalves; ++hf)
+                    tma_load_3d(smem + L::kQOff + hf * L::kQHalfBytes + turn.at * (L::kQRows / 2) * 128, one ? &tmap_q1 : both ? &tmap_qb : &tmap_qh, &ctl->q_full[turn.at], hf * 64,
+                                walk.head * p.group, walk.q.tok0 + walk.token0());
+            }
+            if (!ok) {  // abort: the copies in flight get a moment to land
+                if (turn.uses0 > 0) mbar_wait(&ctl->q_full[0], (turn.uses0 - 1) & 1u, &ctl->drain_flag, kDrainLimitCycles);
+                if (turn.uses1 > 0) mbar_wait(&ctl->q_full[1], (turn.uses1 - 1) & 1u, &ctl->drain_flag, kDrainLimitCycles);
             }
         }
     } else if (warp >= kOutWarp) {
@@ -342,52 +340,65 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         const int quarter = warp & 3;
         const int32_t d = quarter * 32 + lane;
         uint32_t segments = 0;
+        bool ok = true;
         while (walk.next(p)) {
             const uint32_t ob = segments & 1u;
             const int32_t rows = walk.tokens() * p.group;
-            const bool own = walk.e >= p.n_groups, whole = walk.t0 == 0 && walk.t1 == walk.q.tiles();
+            const bool own = walk.e >= p.n_groups, whole = walk.t0 == 0 && walk.t1 == walk.q.tiles;
             const bool last_word = whole && own && walk.q.page0 == 0;  // nothing to add: this is the result
-            const float* now = ml + ob * 5 * kCap;
-            auto sum_of = [&](int32_t r) { return (now[r] + now[kCap + r]) + (now[2 * kCap + r] + now[3 * kCap + r]); };
             // where the block's rows go: in order in a slot, or each in its own place
             const int64_t first_row = (static_cast<int64_t>(walk.q.tok0) + walk.token0()) * p.num_q_heads + walk.head * p.group;
-            const int64_t base = whole ? (own ? p.total_tokens * p.num_q_heads : 0) + first_row : (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
+            const int64_t base = whole ? (own && !last_word ? p.total_tokens * p.num_q_heads : 0) + first_row : (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
             const int32_t skip = whole ? p.num_q_heads - p.group : 0;  // rows between a token's last and the next one's first
+            float* dst = (whole ? p.whole_o : p.part_o) + base * D + d;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + base * D + d;
+            float2* dst_ml = (whole ? p.whole_ml : p.part_ml) + base;
+            const float* now = ml + ob * 5 * kCap + lane;
+            const int32_t n16 = rows16(walk);
+            const bool two_terms = 2 * n16 <= L::kPRows;
+            const uint32_t o_addr = tmem_base + L::kOCol + ob * L::kPRows + (static_cast<uint32_t>(quarter * 32) << 16);
             if (!mbar_wait(&ctl->ml_ready[ob], (segments >> 1) & 1u, abort_flag)) break;
-            if (quarter == 0)
-                for (int32_t r = lane; r < rows; r += 32) {
-                    const int32_t at = r + over_group(p, r) * skip;
-                    const float2 x = make_float2(now[4 * kCap + r], sum_of(r));
-                    if (!whole) p.part_ml[base + at] = x;
-                    else if (!last_word) p.whole_ml[base + at] = x;
-                    else if (p.lse != nullptr) p.lse[first_row + at] = (x.x + log2f(x.y)) * kLn2;
+            for (int32_t r0 = 0; r0 < rows; r0 += 32, now += 32) {  // 32 rows a turn, a lane's numbers are those of row r0 + lane
+                const int32_t here = min(32, rows - r0);
+                int32_t at = 0;
+                float inv = 0.f;
+                if (lane < here) {
+                    const float total = (now[0] + now[kCap]) + (now[2 * kCap] + now[3 * kCap]), m = now[4 * kCap];
+                    at = r0 + lane + over_group(p, r0 + lane) * skip;
+                    inv = 1.f / total;
+                    if (quarter == 0) {
+                        if (!last_word) dst_ml[at] = make_float2(m, total);
+                        else if (p.lse != nullptr) p.lse[base + at] = (m + log2f(total)) * kLn2;
+                    }
                 }
-            if (!mbar_wait(&ctl->o_done[ob], (segments >> 1) & 1u, abort_flag)) break;
-            tc_fence_after_sync();
-            const uint32_t o_addr = tmem_base + (2 + ob) * kCap + (static_cast<uint32_t>(quarter * 32) << 16);
-            if (d < D || D == 128) {
-                float* dst = (whole ? p.whole_o : p.part_o) + base * D + d;
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + first_row * D + d;
-                int32_t in_group = 0;
-                int64_t at = 0;
+                if (r0 == 0) {
+                    if (!mbar_wait(&ctl->o_done[ob], (segments >> 1) & 1u, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after_sync();
+                }
 #pragma unroll 1
-                for (int32_t c = 0; c < rows; c += 8) {
-                    uint32_t o[8];
-                    tmem_ld8(o_addr + c, o);
+                for (int32_t c = 0; c < here; c += 8) {
+                    uint32_t o[8], lo[8];
+                    tmem_ld8(o_addr + r0 + c, o);
+                    if (two_terms) tmem_ld8(o_addr + n16 + r0 + c, lo);
                     tmem_ld_wait();
+                    if (two_terms)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (c + i < rows) {
-                            if (last_word) out[at] = __float2bfloat16_rn(__uint_as_float(o[i]) / sum_of(c + i));
-                            else dst[at] = __uint_as_float(o[i]);
-                            at += D;
-                            if (++in_group == p.group) {
-                                in_group = 0;
-                                at += static_cast<int64_t>(skip) * D;
-                            }
+                        for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) + __uint_as_float(lo[i]));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int64_t to = static_cast<int64_t>(__shfl_sync(0xffffffffu, at, c + i)) * D;
+                        const float f = __shfl_sync(0xffffffffu, inv, c + i);
+                        if (c + i < here && d < D) {
+                            if (last_word) out[to] = __float2bfloat16_rn(__uint_as_float(o[i]) * f);
+                            else dst[to] = __uint_as_float(o[i]);
                         }
+                    }
                 }
             }
+            if (!ok) break;
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl->o_free[ob]);
@@ -406,11 +417,15 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         const int key0 = quarter * 32 + (lane >> 2);            // this thread's keys of a tile: key0 + 8 m
         const int pair = 2 * (lane & 3);                        // its rows of an 8-row block: pair, pair + 1
         uint32_t tiles = 0, segments = 0;
+        int32_t turn = 0;
         bool ok = true;
         while (walk.next(p)) {
             const int32_t len = walk.q.len, tokens = walk.tokens(), token0 = walk.token0(), rows = tokens * p.group, n16 = (rows + 15) & ~15;
-            const int32_t per_team = (n16 / 8 + kTeams - 1) / kTeams;  // blocks; this team's, and its first row
-            const int32_t nb = max(0, min(per_team, n16 / 8 - team * per_team)), row0 = 8 * team * per_team;
+            // the block's rows by eights, so many of these to a team; a segment begins with the team behind the last one's, so
+            // that small segments go to the teams in turn.  (Nobody writes P's rows beyond: their outputs are nobody's.)
+            const int32_t eights = (rows + 7) / 8, per_team = (eights + kTeams - 1) / kTeams, mine = (team - turn) & (kTeams - 1);
+            const int32_t nb = max(0, min(per_team, eights - mine * per_team)), row0 = 8 * mine * per_team;
+            turn += per_team == 1 ? eights : (eights + per_team - 1) / per_team;
             const bool two_terms = 2 * n16 <= L::kPRows;
             const bool own = walk.e >= p.n_groups;
             const int32_t seen_by_first = own ? len - walk.q.n + token0 + 1 : len;  // keys that the block's first token sees
@@ -489,7 +504,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                             keep[2 * k + e] = raise ? fast_exp2(old - top) : 1.f;  // (from -inf: 0)
                             sum[2 * k + e] *= keep[2 * k + e];
                             base[2 * k + e] = now == -CUDART_INF_F ? 0.f : -now;
-                            limit[2 * k + e] = (now + kRaise) / p.scale_log2;
+                            limit[2 * k + e] = row0 + r < rows ? (now + kRaise) / p.scale_log2 : CUDART_INF_F;  // (nobody's rows never do)
                         }
                     if (!first) {  // what O holds goes along
                         if (quarter == 0 && lane < 4) {
@@ -504,12 +519,19 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll 1
                         for (int c = 0; c < 8 * kNow; c += 8) {
                             uint32_t o[8];
-                            const uint32_t at = tmem_base + (2 + (segments & 1u)) * kCap + row0 + c + lane_addr;
+                            const uint32_t at = tmem_base + L::kOCol + (segments & 1u) * L::kPRows + row0 + c + lane_addr;
                             tmem_ld8(at, o);
                             tmem_ld_wait();
 #pragma unroll
                             for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kNow + c + i]);
                             tmem_st8(at, o);
+                            if (two_terms) {
+                                tmem_ld8(at + n16, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kNow + c + i]);
+                                tmem_st8(at + n16, o);
+                            }
                         }
                         tmem_st_wait();
                     }
@@ -541,7 +563,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll
                             for (int m = 0; m < 4; ++m)
                                 hi[m] = pack_bf16x2(x[2 * m] - __uint_as_float(hi[m] << 16), x[2 * m + 1] - __uint_as_float(hi[m] & 0xffff0000u));
-                            stsm_x4_trans(at0 + (8 * k + L::kPRows / 2) * 128, hi[0], hi[1], hi[2], hi[3]);
+                            stsm_x4_trans(at0 + (8 * k + n16) * 128, hi[0], hi[1], hi[2], hi[3]);
                         }
                     }
                 };
@@ -572,7 +594,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             // ---- the segment's references and this warp's sums, for the output warps
             const uint32_t ob = segments & 1u;
             if (ok && segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
-            float* mine = ml + (ob * 5 + quarter) * kCap + row0;
+            float* to = ml + (ob * 5 + quarter) * kCap + row0;
 #pragma unroll
             for (int k = 0; k < kBlocks; ++k)
                 if (k < nb) {
@@ -581,8 +603,8 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                         float x = sum[2 * k + e];
 #pragma unroll
                         for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-                        if (lane < 4) mine[8 * k + pair + e] = x;
-                        if (quarter == 0 && lane < 4) mine[4 * kCap + 8 * k + pair + e] = reference(2 * k + e);
+                        if (lane < 4) to[8 * k + pair + e] = x;
+                        if (quarter == 0 && lane < 4) to[4 * kCap + 8 * k + pair + e] = reference(2 * k + e);
                     }
                 }
             __syncwarp();
@@ -607,7 +629,18 @@ rpx_status_t launch(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t s
     using L = Layout<D, kCap>;
     static_assert(L::kSlotsK >= 2 && L::kSlotsV >= 2 && L::kSmemBytes <= 232448, "shared memory of one CTA");
     static_assert(L::kTmemCols >= 32 && L::kTmemCols <= 512, "tensor memory");
-    CUtensorMap tk, tv;
+    CUtensorMap tq1, tqh, tqb, tk, tv;
+    {
+        // a block's rows as (64 elements, heads of a KV head, tokens)
+        const uint64_t dims[3] = {D, static_cast<uint64_t>(p.num_q_heads), static_cast<uint64_t>(p.total_tokens)};
+        const uint64_t strides[2] = {D * 2ull, static_cast<uint64_t>(p.q_stride) * 2};
+        uint32_t box[3] = {64, static_cast<uint32_t>(p.group), 1};
+        if (rpx_status_t rc = encode_tmap_bf16(&tq1, p.q, 3, dims, strides, box)) return rc;
+        box[2] = static_cast<uint32_t>(L::q_box_tokens(false, p.group));
+        if (rpx_status_t rc = encode_tmap_bf16(&tqh, p.q, 3, dims, strides, box)) return rc;
+        box[2] = static_cast<uint32_t>(L::q_box_tokens(true, p.group));
+        if (rpx_status_t rc = encode_tmap_bf16(&tqb, p.q, 3, dims, strides, box)) return rc;
+    }
     // the pool as groups of 8 keys: two per page and head
     const uint64_t groups = static_cast<uint64_t>(cache.num_blocks) * p.num_kv_heads * 2;  // (fits 32 bits: checked by the caller)
     const uint64_t dims[4] = {64, 8, D / 64, groups};
@@ -617,7 +650,7 @@ rpx_status_t launch(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t s
     if (rpx_status_t rc = encode_tmap_bf16(&tv, cache.v_cache, 4, dims, strides, box)) return rc;
     auto* kernel = group_tile_kernel<D, kCap>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess) return RPX_ERR_CUDA;
-    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, L::kSmemBytes, stream, tk, tv, p);
+    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, L::kSmemBytes, stream, tq1, tqh, tqb, tk, tv, p);
 }
 
 template <int D>
