@@ -421,44 +421,43 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
         bool ok = true;
         while (walk.next(p)) {
             const int32_t len = walk.q.len, tokens = walk.tokens(), token0 = walk.token0(), rows = tokens * p.group, n16 = (rows + 15) & ~15;
-            // the block's rows by eights, so many of these to a team; a segment begins with the team behind the last one's, so
-            // that small segments go to the teams in turn.  (Nobody writes P's rows beyond: their outputs are nobody's.)
-            const int32_t eights = (rows + 7) / 8, per_team = (eights + kTeams - 1) / kTeams, mine = (team - turn) & (kTeams - 1);
-            const int32_t nb = max(0, min(per_team, eights - mine * per_team)), row0 = 8 * mine * per_team;
-            turn += per_team == 1 ? eights : (eights + per_team - 1) / per_team;
+            // the block's rows by eights, kBlocks of these to a team; a segment begins with the team behind the last one's, so that
+            // small segments go to the teams in turn.  (Nobody writes P's rows beyond: their outputs are nobody's.)
+            const int32_t eights = (rows + 7) / 8, mine = (team - turn) & (kTeams - 1);
+            const int32_t nb = min(kBlocks, eights - mine * kBlocks), row0 = 8 * mine * kBlocks;
+            turn += (eights + kBlocks - 1) / kBlocks;
             const bool two_terms = 2 * n16 <= L::kPRows;
             const bool own = walk.e >= p.n_groups;
             const int32_t seen_by_first = own ? len - walk.q.n + token0 + 1 : len;  // keys that the block's first token sees
-            // of the pairs of rows that this thread holds: what a score has to pass for the reference to be raised, the reference
-            // with its sign turned (0 for a row that has seen no key), and the sum over the thread's keys
+            // of the pairs of rows that this thread holds: what a score has to pass for the reference to be raised (rows that are
+            // nobody's never do), the reference with its sign turned (0 for a row that has seen no key), and the sum over the
+            // thread's keys
             float limit[2 * kBlocks], base[2 * kBlocks], sum[2 * kBlocks];
 #pragma unroll
             for (int i = 0; i < 2 * kBlocks; ++i) {
-                limit[i] = -CUDART_INF_F;
+                limit[i] = row0 + 8 * (i >> 1) + pair + (i & 1) < rows ? -CUDART_INF_F : CUDART_INF_F;
                 base[i] = sum[i] = 0.f;
             }
             auto reference = [&](int i) { return limit[i] == -CUDART_INF_F ? -CUDART_INF_F : -base[i]; };
-            // (a form for every number of blocks: with the count looked at inside, the blocks follow one another instead of
-            // overlapping)
-            auto run_tiles = [&](auto blocks_tag) {
-            constexpr int kNow = decltype(blocks_tag)::value;
+            // (All kBlocks are gone through whether they have rows or not: a form for every number of them is more code than the
+            // instruction cache holds beside the other roles', and took twice as long.)
             for (int32_t t = walk.t0; t < walk.t1; ++t, ++tiles) {
                 const uint32_t b = tiles & 1u;
                 const bool first = t == walk.t0;
                 if (ok) ok = mbar_wait(&ctl->s_full[b], (tiles >> 1) & 1u, abort_flag);
                 tc_fence_after_sync();
                 const int32_t left = len - t * kTile;  // keys from the tile's first on
-                if constexpr (kNow > 0) {
-                uint32_t sc[kNow][8];  // [block][2 m + row of the pair]: key m
+                if (nb > 0) {
+                uint32_t sc[kBlocks][8];  // [block][2 m + row of the pair]: key m
 #pragma unroll
-                for (int k = 0; k < kNow; ++k) {
+                for (int k = 0; k < kBlocks; ++k) {
                     tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr, &sc[k][0]);
                     tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr + (16u << 16), &sc[k][4]);
                 }
                 tmem_ld_wait();
                 if (left < kTile || (t + 1) * kTile > seen_by_first) {
 #pragma unroll
-                    for (int k = 0; k < kNow; ++k)
+                    for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int32_t token = min(over_group(p, row0 + 8 * k + pair + e), tokens - 1);
@@ -477,59 +476,59 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
                 // ---- does any row's reference have to be raised?
                 bool up = first;
 #pragma unroll
-                for (int k = 0; k < kNow; ++k)
+                for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) up |= top_of(k, e) > limit[2 * k + e];
                 if (team_any(bar, up)) {
 #pragma unroll
-                    for (int k = 0; k < kNow; ++k)
+                    for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             float top = top_of(k, e);
 #pragma unroll
                             for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                            if (lane < 4) all[(quarter * kNow + k) * 8 + pair + e] = top;
+                            if (lane < 4) all[(quarter * kBlocks + k) * 8 + pair + e] = top;
                         }
                     team_sync(bar);
-                    float keep[2 * kNow];
+                    float keep[2 * kBlocks];
 #pragma unroll
-                    for (int k = 0; k < kNow; ++k)
+                    for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int r = 8 * k + pair + e;
-                            const float top = fmaxf(fmaxf(all[r], all[8 * kNow + r]), fmaxf(all[16 * kNow + r], all[24 * kNow + r])) * p.scale_log2;
+                            const float top = fmaxf(fmaxf(all[r], all[8 * kBlocks + r]), fmaxf(all[16 * kBlocks + r], all[24 * kBlocks + r])) * p.scale_log2;
                             const float old = reference(2 * k + e);
                             const bool raise = top > old + kRaise;
                             const float now = raise ? top : old;
                             keep[2 * k + e] = raise ? fast_exp2(old - top) : 1.f;  // (from -inf: 0)
                             sum[2 * k + e] *= keep[2 * k + e];
                             base[2 * k + e] = now == -CUDART_INF_F ? 0.f : -now;
-                            limit[2 * k + e] = row0 + r < rows ? (now + kRaise) / p.scale_log2 : CUDART_INF_F;  // (nobody's rows never do)
+                            if (row0 + r < rows) limit[2 * k + e] = (now + kRaise) / p.scale_log2;
                         }
                     if (!first) {  // what O holds goes along
                         if (quarter == 0 && lane < 4) {
 #pragma unroll
-                            for (int k = 0; k < kNow; ++k)
+                            for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) all[32 * kNow + 8 * k + pair + e] = keep[2 * k + e];
+                                for (int e = 0; e < 2; ++e) all[32 * kBlocks + 8 * k + pair + e] = keep[2 * k + e];
                         }
                         team_sync(bar);
                         if (ok) ok = mbar_wait(&ctl->pv_done[b ^ 1u], ((tiles - 1) >> 1) & 1u, abort_flag);
                         tc_fence_after_sync();
 #pragma unroll 1
-                        for (int c = 0; c < 8 * kNow; c += 8) {
+                        for (int c = 0; c < 8 * nb; c += 8) {
                             uint32_t o[8];
                             const uint32_t at = tmem_base + L::kOCol + (segments & 1u) * L::kPRows + row0 + c + lane_addr;
                             tmem_ld8(at, o);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kNow + c + i]);
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kBlocks + c + i]);
                             tmem_st8(at, o);
                             if (two_terms) {
                                 tmem_ld8(at + n16, o);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kNow + c + i]);
+                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kBlocks + c + i]);
                                 tmem_st8(at + n16, o);
                             }
                         }
@@ -542,33 +541,38 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
                 const int chunk = (quarter & 1) * 4 + (lane >> 3), prow = row0 + (lane & 7);
                 const uint32_t at0 = pb + prow * 128 + ((chunk ^ (prow & 7)) << 4);  // (row0 is a multiple of 8)
                 const uint64_t scale2 = f2_pack(p.scale_log2, p.scale_log2);
-                auto store_p = [&](auto two_tag) {
 #pragma unroll
-                    for (int k = 0; k < kNow; ++k) {
-                        const uint64_t base2 = f2_pack(base[2 * k], base[2 * k + 1]);
-                        uint32_t hi[4];
-                        float x[8];
-                        uint64_t s2 = f2_pack(sum[2 * k], sum[2 * k + 1]);
+                for (int k = 0; k < kBlocks; ++k) {
+                    const uint64_t base2 = f2_pack(base[2 * k], base[2 * k + 1]);
+                    uint32_t hi[4];
+                    uint64_t x[4];
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        float x0, x1;
+                        f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[k][2 * m]), __uint_as_float(sc[k][2 * m + 1])), scale2, base2), x0, x1);
+                        x0 = fast_exp2(x0);
+                        x1 = fast_exp2(x1);
+                        x[m] = f2_pack(x0, x1);
+                        hi[m] = pack_bf16x2(x0, x1);
+                        sc[k][2 * m] = __float_as_uint(x0);
+                        sc[k][2 * m + 1] = __float_as_uint(x1);
+                    }
+                    f2_unpack(f2_add(f2_pack(sum[2 * k], sum[2 * k + 1]), f2_add(f2_add(x[0], x[1]), f2_add(x[2], x[3]))), sum[2 * k], sum[2 * k + 1]);
+                    if (kBlocks == 1 || k < nb) stsm_x4_trans(at0 + 8 * k * 128, hi[0], hi[1], hi[2], hi[3]);
+                }
+                if (kCap <= 64 || two_terms) {  // what that rounding dropped
+#pragma unroll
+                    for (int k = 0; k < kBlocks; ++k) {
+                        uint32_t lo[4];
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[k][2 * m]), __uint_as_float(sc[k][2 * m + 1])), scale2, base2), x[2 * m], x[2 * m + 1]);
-                            x[2 * m] = fast_exp2(x[2 * m]);
-                            x[2 * m + 1] = fast_exp2(x[2 * m + 1]);
-                            hi[m] = pack_bf16x2(x[2 * m], x[2 * m + 1]);
+                            const float x0 = __uint_as_float(sc[k][2 * m]), x1 = __uint_as_float(sc[k][2 * m + 1]);
+                            const uint32_t hi = pack_bf16x2(x0, x1);
+                            lo[m] = pack_bf16x2(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
                         }
-                        s2 = f2_add(s2, f2_add(f2_add(f2_pack(x[0], x[1]), f2_pack(x[2], x[3])), f2_add(f2_pack(x[4], x[5]), f2_pack(x[6], x[7]))));
-                        f2_unpack(s2, sum[2 * k], sum[2 * k + 1]);
-                        stsm_x4_trans(at0 + 8 * k * 128, hi[0], hi[1], hi[2], hi[3]);
-                        if constexpr (decltype(two_tag)::value) {
-#pragma unroll
-                            for (int m = 0; m < 4; ++m)
-                                hi[m] = pack_bf16x2(x[2 * m] - __uint_as_float(hi[m] << 16), x[2 * m + 1] - __uint_as_float(hi[m] & 0xffff0000u));
-                            stsm_x4_trans(at0 + (8 * k + n16) * 128, hi[0], hi[1], hi[2], hi[3]);
-                        }
+                        if (kBlocks == 1 || k < nb) stsm_x4_trans(at0 + (8 * k + n16) * 128, lo[0], lo[1], lo[2], lo[3]);
                     }
-                };
-                if (kCap <= 64 || two_terms) store_p(std::true_type{});
-                else store_p(std::false_type{});
+                }
                 }
                 // ---- V's rows behind the last key of a page that was loaded may hold anything: a probability of 0 must not
                 // meet a NaN there
@@ -585,12 +589,6 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl->p_ready[b]);
             }
-            };
-            if (nb == kBlocks) run_tiles(std::integral_constant<int, kBlocks>{});
-            else if (nb == 0) run_tiles(std::integral_constant<int, 0>{});
-            else if (nb == 1) run_tiles(std::integral_constant<int, 1>{});
-            else if (nb == 2) run_tiles(std::integral_constant<int, (kBlocks > 2 ? 2 : 1)>{});
-            else run_tiles(std::integral_constant<int, (kBlocks > 3 ? 3 : 1)>{});
             // ---- the segment's references and this warp's sums, for the output warps
             const uint32_t ob = segments & 1u;
             if (ok && segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
