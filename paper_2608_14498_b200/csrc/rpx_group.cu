@@ -22,9 +22,9 @@ using namespace group;
 constexpr int kPlanThreads = 1024;
 
 // Units of the line (20 ns): of a tile against no rows, against 128 more, and of what a segment costs besides its tiles.
-constexpr int kWorkUnits = 30, kRowUnits = 75, kSegmentWork = 130;
+constexpr int kWorkUnits = 10, kRowUnits = 61, kSegmentWork = 15;
 
-__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t group = -1) {
+__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t cap, int32_t group = -1) {
     Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, len / kTile + (len % kTile != 0 ? 1 : 0)};
     if (n == 0 || len == 0) {
         e.n = e.len = 0;
@@ -32,14 +32,14 @@ __device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32
     }
     // Blocks of at most `cap` rows; of at most 64 where the keys are few, so that probabilities keep their second term: over
     // many keys the rounding averages out.
-    const int32_t rows = e.tiles <= 2 && p.cap > 64 ? 64 : p.cap, per = max(1, rows / p.group);  // (at most p.cap / group: Q's box)
+    const int32_t rows = e.tiles <= 2 && cap > 64 ? 64 : cap, per = max(1, rows / p.group);  // (at most cap / group: Q's box)
     e.blocks = n <= per ? 1 : (n + per - 1) / per;
     e.block_tokens = e.blocks == 1 ? n : (n + e.blocks - 1) / e.blocks;
-    // A tile's bytes are kTileUnits of this SM's share of HBM, once for all blocks; the work against a block overlaps with that, but
-    // a segment's first scores and last output do not with each other.
+    // A tile's bytes are tile_units of this SM's share of HBM, once for all blocks; the work against a block overlaps with that, what
+    // a segment costs besides does not quite.
     const int32_t rows_now = e.block_tokens * p.group, work = kWorkUnits + rows_now * kRowUnits / 128;
     const int32_t bytes = p.tile_units / e.blocks, beside = kSegmentWork / e.tiles;
-    e.weight = max(bytes, work + beside);
+    e.weight = max(bytes, work) + beside;
     return e;
 }
 
@@ -111,6 +111,17 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* sums, int64_t* 
     return __shfl_sync(0xffffffffu, upto - w, warp) + sum;
 }
 
+// Every CTA's start, and the lines' totals.
+template <class Unit0>
+__device__ __forceinline__ void leave_starts(const Params& p, int64_t line1, int64_t total, Unit0 unit0) {
+    const int32_t i = threadIdx.x;
+    if (i < p.lines) p.total[i] = p.lines == 1 ? total : i == 0 ? line1 : total - line1;
+    if (i < p.lines * p.ctas) {
+        const int32_t line = i / p.ctas;
+        p.starts[i] = find_start(p, line, line == 0 ? 0 : line1, p.lines == 1 ? total : line == 0 ? line1 : total - line1, i - line * p.ctas, unit0);
+    }
+}
+
 // Up to as many entries as threads: a thread an entry, groups first, everything read once (8 prompts of 8: 3 us; with the form
 // below 6).
 __global__ void __launch_bounds__(kPlanThreads) group_plan_small_kernel(const __grid_constant__ Params p) {
@@ -147,21 +158,23 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_small_kernel(const __
         const int32_t n = fits ? cu[last] - cu[first] : 0;
         shared = shared_tokens(p, fits, n, shared, books.members[g]);
         books.shared[g] = shared;
-        e = make_entry(p, shared > 0 ? cu[first] : 0, shared > 0 ? n : 0, shared, books.row[g], 0);
+        e = make_entry(p, shared > 0 ? cu[first] : 0, shared > 0 ? n : 0, shared, books.row[g], 0, p.cap[0]);
     }
     __syncthreads();
     if (is_seq) {
         shared = member ? books.shared[of] : 0;
-        e = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, shared > 0 ? of : -1);
+        e = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, p.cap[p.lines - 1], shared > 0 ? of : -1);
     }
     const int64_t units = entry_units(p, e);
     int64_t total;
-    e.unit0 = block_sum(units, sums, &total) - units;
-    unit0[threadIdx.x] = e.unit0;
-    if (g < count) p.entries[g] = e;
-    if (g == 0) *p.total = total;
+    const int64_t first_unit = block_sum(units, sums, &total) - units;
+    unit0[threadIdx.x] = first_unit;
     __syncthreads();
-    if (g < p.ctas) p.starts[g] = find_start(p, total, g, [&](int32_t i) { return unit0[i]; });
+    const int64_t line1 = p.lines == 2 ? (p.n_groups < kPlanThreads ? unit0[p.n_groups] : total) : 0;  // where the second line starts
+    e.unit0 = first_unit - (is_group ? 0 : line1);
+    if (g < count) p.entries[g] = e;
+    __syncthreads();
+    leave_starts(p, line1, total, [&](int32_t i) { return unit0[i]; });
 }
 
 // Any number: every sequence gets its entry as if it were alone; groups that share are then given theirs, kPlanThreads at a time,
@@ -175,7 +188,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     for (int32_t s = threadIdx.x; s < p.batch; s += kPlanThreads) {
         Seq q;
         if (!read_seq(p, s, &q)) report(p.status);
-        p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0);
+        p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0, p.cap[p.lines - 1]);
     }
     const bool ascend = __syncthreads_and(good) != 0;
     for (int32_t g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
@@ -199,7 +212,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
             const int32_t tok0 = fits ? __ldg(p.cu + first) : 0, n = fits ? __ldg(p.cu + last) - tok0 : 0;
             shared = shared_tokens(p, fits, n, shared, books.members[threadIdx.x]);
             books.shared[threadIdx.x] = shared;
-            p.entries[g] = make_entry(p, tok0, shared > 0 ? n : 0, shared, books.row[threadIdx.x], 0);
+            p.entries[g] = make_entry(p, tok0, shared > 0 ? n : 0, shared, books.row[threadIdx.x], 0, p.cap[0]);
         }
         __syncthreads();
         for (int32_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
@@ -207,36 +220,46 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
             if (shared == 0) continue;
             Seq q;
             read_seq(p, s, &q);
-            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, g0 + i);
+            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, p.cap[p.lines - 1], g0 + i);
         }
         __syncthreads();
     }
     const int32_t count = p.n_groups + p.batch;
+    __shared__ int64_t line1;
     int64_t carry = 0;
+    if (threadIdx.x == 0) line1 = 0;
     for (int32_t base = 0; base < count; base += kPlanThreads) {
         const int32_t e = base + threadIdx.x;
         const int64_t x = e < count ? entry_units(p, p.entries[e]) : 0;
         int64_t total;
-        const int64_t upto = block_sum(x, sums, &total);
-        if (e < count) p.entries[e].unit0 = carry + upto - x;
+        const int64_t upto = carry + block_sum(x, sums, &total);
+        if (e < count) p.entries[e].unit0 = upto - x;
+        if (p.lines == 2 && e == p.n_groups) line1 = upto - x;
         carry += total;
     }
-    if (threadIdx.x == 0) *p.total = carry;
     __syncthreads();
-    if (threadIdx.x < p.ctas) p.starts[threadIdx.x] = find_start(p, carry, threadIdx.x, [&](int32_t i) { return p.entries[i].unit0; });
+    leave_starts(p, line1, carry, [&](int32_t i) { return p.entries[i].unit0; });
+    if (p.lines == 2) {
+        __syncthreads();
+        for (int32_t e = p.n_groups + threadIdx.x; e < count; e += kPlanThreads) p.entries[e].unit0 -= line1;
+        // (the starts keep an entry's first unit too, but nobody reads it there)
+    }
 }
 
 // ------------------------------------------------------------------ the join
-// A warp per row (token, query head) that has more than one set to add up: the shared keys' pieces in order, then its own.
+// A warp takes kRows rows of a KV head's group of one token (the sets of all of them lie alike) and kBatch sets of each at a time,
+// all of them on their way together: the shared keys' pieces in order, then its own.  Many sets and few rows: 1 x 8; many rows
+// have few sets each: 4 x 2.
 constexpr int kJoinWarps = 8;
 
-// The sets of a row against one entry: where the first lies, how far on the others, and how many.
+// The sets of a row against one entry: where the first one lies, how far on the next (twice as far on all others), and how many.
 struct Sets {
-    int64_t first, step;
-    int32_t n;
+    int64_t first;
+    int32_t step, n;
     bool whole;
 };
-__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int64_t size, int32_t kv_head, int32_t in_group, int64_t token, int64_t own_row) {
+__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int32_t line, int64_t total, int32_t kv_head, int32_t in_group, int64_t token, int64_t own_row) {
+    const int64_t size = piece_units(total, p.ctas);
     const int32_t in = static_cast<int32_t>(token - q.tok0), block = q.blocks == 1 ? 0 : in / q.block_tokens;
     const int64_t unit = q.unit0 + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
     const int64_t c0 = quotient(unit, size);
@@ -244,79 +267,108 @@ __device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int64
     r.n = static_cast<int32_t>(quotient(unit + static_cast<int64_t>(q.tiles - 1) * q.weight, size) - c0) + 1;
     r.whole = r.n == 1;
     // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
-    r.first = r.whole ? own_row : (c0 * 2 + 1) * p.cap + (in - block * q.block_tokens) * p.group + in_group;
-    r.step = p.cap;  // from the second slot of a piece to the first of the next; 2 cap from there on
+    r.step = p.cap[line];
+    r.first = r.whole ? own_row : p.slot0(line) + (c0 * 2 + 1) * r.step + (in - block * q.block_tokens) * p.group + in_group;
     return r;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kJoinWarps * 32) group_join_kernel(const __grid_constant__ Params p) {
+template <int D, int kRows, int kBatch>
+__global__ void __launch_bounds__(kJoinWarps * 32, 4) group_join_kernel(const __grid_constant__ Params p, int32_t per_group) {
     constexpr int kCols = D / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t out_row = static_cast<int64_t>(blockIdx.x) * kJoinWarps + warp, token = quotient(out_row, p.num_q_heads);
-    if (token >= p.total_tokens) return;  // (never a whole block)
-    const int32_t h = static_cast<int32_t>(out_row - token * p.num_q_heads), kv_head = over_group(p, h), in_group = h - kv_head * p.group;
-    const int32_t s = find_seq(p, token, lane);
+    // task = (token, KV head, run of kRows rows)
+    const int64_t task = static_cast<int64_t>(blockIdx.x) * kJoinWarps + warp, pair = quotient(task, per_group), token = quotient(pair, p.num_kv_heads);
+    const int32_t kv_head = static_cast<int32_t>(pair - token * p.num_kv_heads), in_group = static_cast<int32_t>(task - pair * per_group) * kRows;
+    const bool there = token < p.total_tokens;
+    const int32_t s = find_seq(p, there ? token : 0, lane);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // (of rows that are left out too: this grid never ends before that one)
+    if (!there) return;
     const Entry own = load_entry(p.entries + p.n_groups + s);
-    const int64_t size = piece_units(__ldcg(p.total), p.ctas), all_rows = p.total_tokens * p.num_q_heads;
+    const int64_t total0 = __ldcg(p.total), total1 = p.lines == 2 ? __ldcg(p.total + 1) : total0, all_rows = p.total_tokens * p.num_q_heads;
     if (token < own.tok0 || token - own.tok0 >= own.n) return;  // in no sequence, or in one that does not fit
-    Sets sets[2];
-    sets[0] = Sets{0, 0, 0, false};
-    sets[1] = find_sets(p, own, size, kv_head, in_group, token, all_rows + out_row);
-    if (own.group < 0 && sets[1].whole) return;  // written whole
-    if (own.group >= 0) sets[0] = find_sets(p, load_entry(p.entries + own.group), size, kv_head, in_group, token, out_row);
-    float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
+    const int64_t row0 = token * p.num_q_heads + kv_head * p.group + in_group;
+    const int32_t rows = min(kRows, p.group - in_group);
+    const Sets of_own = find_sets(p, own, p.lines - 1, total1, kv_head, in_group, token, all_rows + row0);
+    if (own.group < 0 && of_own.whole) return;  // written whole
+    Sets of_group = {0, 0, 0, false};
+    if (own.group >= 0) of_group = find_sets(p, load_entry(p.entries + own.group), 0, total0, kv_head, in_group, token, row0);
+    float top[kRows], sum[kRows], acc[kRows][kCols];
 #pragma unroll
-    for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
-    // kBatch sets at a time, all of them on their way together (one after the other, 17 sets took 6 us)
-    constexpr int kBatch = 8;
-    const int32_t n = sets[0].n + sets[1].n;
+    for (int k = 0; k < kRows; ++k) {
+        top[k] = -CUDART_INF_F;
+        sum[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) acc[k][i] = 0.f;
+    }
+    const int32_t n = of_group.n + of_own.n;
     for (int32_t j0 = 0; j0 < n; j0 += kBatch) {
-        float2 ml[kBatch];
-        float v[kBatch][kCols];
+        float2 ml[kRows][kBatch];
+        float v[kRows][kBatch][kCols];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const bool shared = j0 + u < sets[0].n;
-            const int32_t j = j0 + u - (shared ? 0 : sets[0].n);
-            const int64_t at = (shared ? sets[0].first : sets[1].first) + (j == 0 ? 0 : (2 * j - 1) * (shared ? sets[0].step : sets[1].step));
-            const bool whole = shared ? sets[0].whole : sets[1].whole;
-            ml[u] = make_float2(-CUDART_INF_F, 0.f);
+            const bool shared = j0 + u < of_group.n;
+            const int32_t j = j0 + u - (shared ? 0 : of_group.n);
+            const bool whole = shared ? of_group.whole : of_own.whole;
+            const int64_t at = (shared ? of_group.first : of_own.first) + (j == 0 ? 0 : static_cast<int64_t>(2 * j - 1) * (shared ? of_group.step : of_own.step));
+            const float2* from_ml = (whole ? p.whole_ml : p.part_ml) + at;
+            const float* from = (whole ? p.whole_o : p.part_o) + at * D + lane * kCols;
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) v[u][i] = 0.f;
-            if (j0 + u < n) {
-                ml[u] = __ldcg((whole ? p.whole_ml : p.part_ml) + at);
-                const float* o = (whole ? p.whole_o : p.part_o) + at * D + lane * kCols;
-                if constexpr (kCols == 4) *reinterpret_cast<float4*>(v[u]) = __ldcg(reinterpret_cast<const float4*>(o));
-                else *reinterpret_cast<float2*>(v[u]) = __ldcg(reinterpret_cast<const float2*>(o));
+            for (int k = 0; k < kRows; ++k) {
+                ml[k][u] = make_float2(-CUDART_INF_F, 0.f);
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) v[k][u][i] = 0.f;
+                if (j0 + u < n && k < rows) {
+                    ml[k][u] = __ldcg(from_ml + k);
+                    if constexpr (kCols == 4) *reinterpret_cast<float4*>(v[k][u]) = __ldcg(reinterpret_cast<const float4*>(from + k * D));
+                    else *reinterpret_cast<float2*>(v[k][u]) = __ldcg(reinterpret_cast<const float2*>(from + k * D));
+                }
             }
         }
-        float to = top;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) to = fmaxf(to, ml[u].x);
-        const float base = to == -CUDART_INF_F ? 0.f : to;  // (no key seen so far)
-        const float keep = fast_exp2(top - base);
-        top = to;
-        sum *= keep;
+        for (int k = 0; k < kRows; ++k) {
+            float to = top[k];
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) acc[i] *= keep;
+            for (int u = 0; u < kBatch; ++u) to = fmaxf(to, ml[k][u].x);
+            const float base = to == -CUDART_INF_F ? 0.f : to;  // (no key seen so far)
+            const float keep = fast_exp2(top[k] - base);
+            top[k] = to;
+            sum[k] *= keep;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            // a set that saw no key has a sum and outputs of 0; one of nothing but NaN goes on with a factor of 1
-            const float f = ml[u].x == -CUDART_INF_F ? 1.f : fast_exp2(ml[u].x - base);
-            sum = fmaf(f, ml[u].y, sum);
+            for (int i = 0; i < kCols; ++i) acc[k][i] *= keep;
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) acc[i] = fmaf(f, v[u][i], acc[i]);
+            for (int u = 0; u < kBatch; ++u) {
+                // a set that saw no key has a sum and outputs of 0; one of nothing but NaN goes on with a factor of 1
+                const float f = ml[k][u].x == -CUDART_INF_F ? 1.f : fast_exp2(ml[k][u].x - base);
+                sum[k] = fmaf(f, ml[k][u].y, sum[k]);
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) acc[k][i] = fmaf(f, v[k][u][i], acc[k][i]);
+            }
         }
     }
-    const float inv = 1.f / sum;
-    uint32_t w[kCols / 2];
 #pragma unroll
-    for (int i = 0; i < kCols / 2; ++i) w[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + out_row * D + lane * kCols);
-    if constexpr (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    else *dst = w[0];
-    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = (top + log2f(sum)) * kLn2;
+    for (int k = 0; k < kRows; ++k)
+        if (k < rows) {
+            const float inv = 1.f / sum[k];
+            uint32_t w[kCols / 2];
+#pragma unroll
+            for (int i = 0; i < kCols / 2; ++i) w[i] = pack_bf16x2(acc[k][2 * i] * inv, acc[k][2 * i + 1] * inv);
+            uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + (row0 + k) * D + lane * kCols);
+            if constexpr (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+            else *dst = w[0];
+            if (lane == 0 && p.lse != nullptr) p.lse[row0 + k] = (top[k] + log2f(sum[k])) * kLn2;
+        }
+}
+
+template <int D, int kRows, int kBatch>
+rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
+    const int32_t per_group = (p.group + kRows - 1) / kRows;
+    const int64_t tasks = p.total_tokens * p.num_kv_heads * per_group;
+    return launch_on_top(group_join_kernel<D, kRows, kBatch>, static_cast<unsigned>((tasks + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0, stream, p, per_group);
+}
+template <int D>
+rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
+    // as many rows as warps that run at once, or more
+    return p.total_tokens * p.num_q_heads > 148 * 4 * kJoinWarps ? launch_join<D, 4, 2>(p, stream) : launch_join<D, 1, 8>(p, stream);
 }
 
 // ------------------------------------------------------------------ float32
@@ -427,15 +479,23 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     if (p.lse != nullptr && lane == 0) p.lse[row] = (top + log2f(l)) * kLn2;
 }
 
-// Rows per block: the smallest of 16, 32, 64 and the most that a form takes that holds a group's rows of one KV head.
-int32_t cap_of(int32_t max_q, int32_t max_group, int32_t n_groups, int32_t group, int32_t head_dim) {
-    const int64_t rows = static_cast<int64_t>(n_groups > 0 && max_group > max_q ? max_group : max_q) * group;
+// Rows per block: the smallest of 16, 32, 64 and the most that a form takes that holds so many tokens' rows of one KV head.
+int32_t cap_of(int32_t tokens, int32_t group, int32_t head_dim) {
+    const int64_t rows = static_cast<int64_t>(tokens) * group;
     return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : group_most_rows(head_dim);
+}
+// One line, or where groups need the largest form and single sequences do not, a line each: that form's rings are short, and
+// small segments take it 4900 clocks a tile against 2500 (4 x 64 sequences with 500 tokens of their own: 180 us in one line).
+void choose_lines(Params& p, int32_t head_dim) {
+    const int32_t seq = cap_of(p.max_q, p.group, head_dim), group = p.n_groups > 0 && p.max_group > p.max_q ? cap_of(p.max_group, p.group, head_dim) : seq;
+    p.lines = group > 64 && seq <= 64 ? 2 : 1;
+    p.cap[0] = group;
+    p.cap[1] = seq;
 }
 constexpr int kMaxCtas = 148;
 
 // Carves the workspace (NULL: only measures it).
-size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t cap, int32_t heads, int32_t head_dim, void* workspace) {
+size_t carve(Params& p, int32_t head_dim, void* workspace) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -443,10 +503,10 @@ size_t carve(Params& p, int64_t tokens, int32_t entries, int32_t cap, int32_t he
         at += align_up(bytes, 256);
         return r;
     };
-    p.starts = reinterpret_cast<Start*>(take(kMaxCtas * sizeof(Start)));
-    const size_t rows = static_cast<size_t>(tokens) * heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * cap;
-    p.entries = reinterpret_cast<Entry*>(take(static_cast<size_t>(entries) * sizeof(Entry)));
-    p.total = reinterpret_cast<int64_t*>(take(sizeof(int64_t)));
+    const size_t rows = static_cast<size_t>(p.total_tokens) * p.num_q_heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * (p.cap[0] + (p.lines == 2 ? p.cap[1] : 0));
+    p.entries = reinterpret_cast<Entry*>(take((static_cast<size_t>(p.n_groups) + p.batch) * sizeof(Entry)));
+    p.total = reinterpret_cast<int64_t*>(take(2 * sizeof(int64_t)));
+    p.starts = reinterpret_cast<Start*>(take(2 * kMaxCtas * sizeof(Start)));
     p.whole_ml = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
     p.part_ml = reinterpret_cast<float2*>(take(slots * sizeof(float2)));
     p.whole_o = reinterpret_cast<float*>(take(rows * head_dim * sizeof(float)));
@@ -461,7 +521,15 @@ int32_t group_most_rows(int32_t head_dim) { return head_dim == 128 ? 112 : 128; 
 size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t n_groups, int32_t max_q, int32_t max_group) {
     if (d->dtype == RPX_F32 || batch > INT32_MAX - n_groups - 1) return 0;
     Params p = {};
-    return carve(p, tokens, n_groups + batch, cap_of(max_q, max_group, n_groups, d->num_q_heads / d->num_kv_heads, d->head_dim), d->num_q_heads, d->head_dim, nullptr);
+    p.total_tokens = tokens;
+    p.batch = batch;
+    p.n_groups = n_groups;
+    p.max_q = max_q;
+    p.max_group = max_group;
+    p.num_q_heads = d->num_q_heads;
+    p.group = d->num_q_heads / d->num_kv_heads;
+    choose_lines(p, d->head_dim);
+    return carve(p, d->head_dim, nullptr);
 }
 
 bool group_too_large(const GroupArgs& a) {
@@ -480,18 +548,16 @@ rpx_status_t launch_group_attn(const GroupArgs& a) {
     }
     const int sms = sm_count();
     if (sms <= 0) return RPX_ERR_CUDA;
-    p.cap = cap_of(a.max_q, a.max_group, a.n_groups, p.group, a.head_dim);
+    choose_lines(p, a.head_dim);
     p.tile_units = a.head_dim == 128 ? 75 : 38;  // 64 KB or 32 at 6.5 TB/s over 148 SMs
     // (without the SM budget: where the line of tiles is cut decides the order of the sums)
     p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
-    carve(p, a.total_tokens, a.n_groups + a.batch, p.cap, a.num_q_heads, a.head_dim, a.workspace);
+    carve(p, a.head_dim, a.workspace);
     if (a.n_groups + a.batch <= kPlanThreads) group_plan_small_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
     else group_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
     if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
     if (rpx_status_t rc = launch_group_tile(p, a.head_dim, *a.cache, a.stream)) return rc;
-    const unsigned blocks = static_cast<unsigned>((rows + kJoinWarps - 1) / kJoinWarps);
-    return a.head_dim == 128 ? launch_on_top(group_join_kernel<128>, blocks, kJoinWarps * 32, 0, a.stream, p)
-                             : launch_on_top(group_join_kernel<64>, blocks, kJoinWarps * 32, 0, a.stream, p);
+    return a.head_dim == 128 ? launch_join<128>(p, a.stream) : launch_join<64>(p, a.stream);
 }
 
 }  // namespace rpx

@@ -2,7 +2,8 @@
 //
 // All key tiles of all segments lie in a line: first the groups' shared pages (an entry per group), then every sequence's own
 // keys (an entry per sequence).  A segment is one KV head of an entry and one block of its rows (row = token * group + head
-// within the KV head's group).  The line is cut into equal pieces, one per CTA.  A segment that lies in one piece leaves its
+// within the KV head's group).  The line is cut into equal pieces, one per CTA; where groups have more rows than one
+// kernel form does well beside single sequences, the two parts of the line are cut apart, for CTAs of two forms in one launch.  A segment that lies in one piece leaves its
 // rows' (maximum in log2 units, sum) and un-normalised outputs in the rows' own place in the workspace (or, where its sequence
 // shares nothing, the result in `out`), a segment that is cut one set per piece; the join adds them up in the order of the keys.
 // The cut goes by lengths alone, so the same call gives the same bits.
@@ -32,7 +33,7 @@ struct __align__(16) Entry {
     int32_t row, page0;     // the table row that names the keys' pages, and the first of them
     int32_t blocks, block_tokens;  // row blocks, and the tokens of each but the last
     int32_t weight;         // units of a key tile against one block
-    int64_t unit0;          // its first unit
+    int64_t unit0;          // its first unit, counted from the start of its line
     int32_t group;          // of a sequence: the group whose shared pages it reads as well, or -1
     int32_t tiles;          // key tiles
     __device__ __forceinline__ int64_t segment_units() const { return static_cast<int64_t>(tiles) * weight + kSegment; }
@@ -65,16 +66,19 @@ struct Params {
     float* lse;
     int32_t* status;
     // bf16 only
-    int32_t cap;           // rows per block at most
     int32_t tile_units;    // of a tile's bytes
-    int32_t ctas;          // pieces at most
+    int32_t ctas;          // pieces of a line at most
+    int32_t lines;         // 1: groups and sequences are one line; 2: a line each
+    int32_t cap[2];        // rows per block at most, of each line
     Entry* entries;        // workspace [n_groups + batch]
-    struct Start* starts;  // workspace [ctas]
-    int64_t* total;        // workspace: units of the line
+    struct Start* starts;  // workspace [lines][ctas]
+    int64_t* total;        // workspace [lines]: units of each line
     float2* whole_ml;      // workspace [2][total_tokens][H_q]: of segments that are not cut: shared, own
     float* whole_o;        // workspace [2][total_tokens][H_q][D]
-    float2* part_ml;       // workspace [ctas][2][cap]: of segments that are
-    float* part_o;         // workspace [ctas][2][cap][D]
+    float2* part_ml;       // workspace [lines][ctas][2][cap of the line]: of segments that are
+    float* part_o;         // workspace, rows as those, [D]
+    __host__ __device__ __forceinline__ int32_t line_of(int32_t entry) const { return lines == 2 && entry >= n_groups ? 1 : 0; }
+    __host__ __device__ __forceinline__ int64_t slot0(int32_t line) const { return line == 0 ? 0 : static_cast<int64_t>(ctas) * 2 * cap[0]; }
 };
 
 __device__ __forceinline__ int32_t over_group(const Params& p, int32_t row) {
@@ -132,14 +136,15 @@ struct __align__(16) Start {
     int32_t e, head, block, t1;
     int64_t left, unused;
 };
-// By one thread for one CTA; unit0(e) gives an entry's first unit.
+// By one thread for one CTA; unit0(e) gives an entry's first unit, counted from the start of the first line.
 template <class Unit0>
-__device__ __forceinline__ Start find_start(const Params& p, int64_t total, int32_t cta, Unit0 unit0) {
-    const int64_t size = piece_units(total, p.ctas), begin = min(total, size * static_cast<int64_t>(cta)), end = min(total, begin + size);
+__device__ __forceinline__ Start find_start(const Params& p, int32_t line, int64_t line0, int64_t total, int32_t cta, Unit0 unit0) {
+    const int64_t size = piece_units(total, p.ctas), from = min(total, size * static_cast<int64_t>(cta)), end = min(total, from + size);
     Start r = {};
-    r.left = end - begin;
+    r.left = end - from;
     if (r.left == 0) return r;
-    int32_t lo = 0, hi = p.n_groups + p.batch;  // the last entry that starts at or before `begin`
+    const int64_t begin = line0 + from;
+    int32_t lo = line == 0 ? 0 : p.n_groups, hi = line == 0 && p.lines == 2 ? p.n_groups : p.n_groups + p.batch;  // the last entry that starts at or before `begin`
     while (hi - lo > 1) {
         const int32_t mid = lo + (hi - lo) / 2;
         if (unit0(mid) <= begin) lo = mid;
@@ -147,7 +152,7 @@ __device__ __forceinline__ Start find_start(const Params& p, int64_t total, int3
     }
     r.e = lo;
     r.q = p.entries[lo];
-    int64_t off = begin - r.q.unit0;
+    int64_t off = begin - unit0(lo);
     const int64_t seg = r.q.segment_units(), i = quotient(off, seg);
     r.head = static_cast<int32_t>(quotient(i, r.q.blocks));
     r.block = static_cast<int32_t>(i - static_cast<int64_t>(r.head) * r.q.blocks);
@@ -162,8 +167,8 @@ struct Walk {
     int32_t e, head, block, t0, t1;  // current segment: entry, KV head, row block, key tiles [t0, t1)
     int32_t left;                    // units of the piece behind t1's first
     Entry q;
-    __device__ __forceinline__ void start(const Params& p) {
-        const Start* s = p.starts + blockIdx.x;
+    __device__ __forceinline__ void start(const Params& p, int32_t piece) {
+        const Start* s = p.starts + piece;
         const int4 a = __ldcg(reinterpret_cast<const int4*>(&s->e));
         left = static_cast<int32_t>(__ldcg(&s->left));  // (2^31 units are 40 s)
         q = load_entry(&s->q);

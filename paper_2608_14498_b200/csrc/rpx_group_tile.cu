@@ -32,7 +32,6 @@ namespace {
 
 using namespace group;
 
-constexpr int kSoftmaxRegs = 96, kOtherRegs = 48;  // 512 * 96 + 256 * 48 = 768 * 80, what a launch of 768 threads has
 constexpr int kPages = kTile / kPage;
 constexpr float kRaise = 8.0f;  // log2 units
 constexpr int kMaxSlots = 6;
@@ -43,7 +42,6 @@ struct Layout {
     static constexpr int kProducerWarp = 4 * kTeams, kScoreWarp = kProducerWarp + 1, kValueWarp = kProducerWarp + 2, kQWarp = kProducerWarp + 3;
     static constexpr int kOutWarp = kProducerWarp + 4;             // the first of four
     static constexpr int kThreads = 32 * (kOutWarp + 4);
-    static constexpr bool kSplitRegs = kTeams == 4;
     static constexpr int kBlocks = (kCap / 8 + kTeams - 1) / kTeams;  // 8-row blocks of a team at most
     static constexpr int kHalves = D / 64;
     static constexpr int kTensorBytes = kTile * D * 2;             // a key tile of K or V
@@ -118,12 +116,16 @@ __device__ __forceinline__ bool team_any(int id, bool x) {
     return r != 0u;
 }
 
-template <int D, int kCap>
-__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1)
-group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_constant__ CUtensorMap tmap_qh, const __grid_constant__ CUtensorMap tmap_qb,
-                  const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Params p) {
+struct Maps {  // Q (boxes of one token, of a half of its room, of both), K, V
+    CUtensorMap q1, qh, qb, k, v;
+};
+
+// One CTA's piece of a line.  (kThreads: of the block; warps beyond this form's only meet the others at its barriers.)
+template <int D, int kCap, int kThreads>
+__device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_t line, int32_t cta) {
     using L = Layout<D, kCap>;
     constexpr int kTeams = L::kTeams, kProducerWarp = L::kProducerWarp, kScoreWarp = L::kScoreWarp, kValueWarp = L::kValueWarp, kQWarp = L::kQWarp, kOutWarp = L::kOutWarp;
+    constexpr int kSoftmaxRegs = kThreads == 768 ? 96 : 0, kOtherRegs = 48;  // 512 * 96 + 256 * 48 = 768 * 80, what a launch of 768 threads has
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0u) {  // swizzled tiles need 1024-byte alignment; never expected
         if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, RPX_ERR_CUDA);
@@ -168,9 +170,9 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
 
     if (warp == kProducerWarp) {
         // =========================================================== producer: K a tile ahead of V, through all segments
-        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p);
+        walk.start(p, line * p.ctas + cta);
         bool ok = true;
         uint32_t nk = 0, nv = 0;
         // the tile whose V comes next: page number of this lane's page, boxes, KV head
@@ -185,7 +187,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
         auto load_v = [&]() {
             const uint32_t st = nv % L::kSlotsV;
             if (!mbar_wait(&ctl->v_empty[st], ((nv / L::kSlotsV) & 1u) ^ 1u, abort_flag)) return false;
-            load(&tmap_v, smem + L::kVOff + st * L::kTensorBytes, &ctl->v_full[st], v_block, v_boxes, v_head);
+            load(&maps.v, smem + L::kVOff + st * L::kTensorBytes, &ctl->v_full[st], v_block, v_boxes, v_head);
             ++nv;
             return true;
         };
@@ -205,7 +207,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
                 const uint32_t st = nk % L::kSlotsK;
                 ok = mbar_wait(&ctl->k_empty[st], ((nk / L::kSlotsK) & 1u) ^ 1u, abort_flag);
                 if (!ok) break;
-                load(&tmap_k, smem + st * L::kTensorBytes, &ctl->k_full[st], block, boxes, walk.head);
+                load(&maps.k, smem + st * L::kTensorBytes, &ctl->k_full[st], block, boxes, walk.head);
                 ++nk;
                 if (nk > 1) ok = load_v();
                 if (!ok) break;
@@ -223,9 +225,9 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
         }
     } else if (warp == kScoreWarp) {
         // =========================================================== S^T = K Q^T, by one thread
-        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p);
+        walk.start(p, line * p.ctas + cta);
         if (elect_one()) {
             const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem), 16, L::kHalves * 1024);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem + L::kQOff), 16, 1024);
@@ -264,9 +266,9 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
         }
     } else if (warp == kValueWarp) {
         // =========================================================== O^T += V^T P^T, by one thread
-        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p);
+        walk.start(p, line * p.ctas + cta);
         if (elect_one()) {
             // D = 64: M stays 128, and the lanes 64 .. 127 of O^T, which nobody reads, are fed by whatever lies 1 KB on
             const uint64_t v_desc = make_smem_desc_sw128(smem_u32(smem + L::kVOff), 1024, L::kHalves * 1024);
@@ -308,9 +310,9 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
         // =========================================================== Q of a segment's block
         // One box lands as consecutive 128-byte rows: of one token, of as many as a half of Q's room holds, or of as many as both do.
         // (What lies behind the block's rows is another token's, or was there before: those rows are nobody's.)
-        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p);
+        walk.start(p, line * p.ctas + cta);
         if (elect_one()) {
             QTurn turn;
             bool ok = true;
@@ -324,7 +326,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
                 mbar_arrive_expect_tx(&ctl->q_full[turn.at], static_cast<uint32_t>(box_tokens * p.group * L::kHalves) * 128);
                 if (both) mbar_arrive(&ctl->q_full[1]);
                 for (int hf = 0; hf < L::kHalves; ++hf)
-                    tma_load_3d(smem + L::kQOff + hf * L::kQHalfBytes + turn.at * (L::kQRows / 2) * 128, one ? &tmap_q1 : both ? &tmap_qb : &tmap_qh, &ctl->q_full[turn.at], hf * 64,
+                    tma_load_3d(smem + L::kQOff + hf * L::kQHalfBytes + turn.at * (L::kQRows / 2) * 128, one ? &maps.q1 : both ? &maps.qb : &maps.qh, &ctl->q_full[turn.at], hf * 64,
                                 walk.head * p.group, walk.q.tok0 + walk.token0());
             }
             if (!ok) {  // abort: the copies in flight get a moment to land
@@ -332,11 +334,11 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
                 if (turn.uses1 > 0) mbar_wait(&ctl->q_full[1], (turn.uses1 - 1) & 1u, &ctl->drain_flag, kDrainLimitCycles);
             }
         }
-    } else if (warp >= kOutWarp) {
+    } else if (warp >= kOutWarp && warp < kOutWarp + 4) {
         // =========================================================== output: a warp 32 elements of D of all rows
-        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p);
+        walk.start(p, line * p.ctas + cta);
         const int quarter = warp & 3;
         const int32_t d = quarter * 32 + lane;
         uint32_t segments = 0;
@@ -348,7 +350,7 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
             const bool last_word = whole && own && walk.q.page0 == 0;  // nothing to add: this is the result
             // where the block's rows go: in order in a slot, or each in its own place
             const int64_t first_row = (static_cast<int64_t>(walk.q.tok0) + walk.token0()) * p.num_q_heads + walk.head * p.group;
-            const int64_t base = whole ? (own && !last_word ? p.total_tokens * p.num_q_heads : 0) + first_row : (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
+            const int64_t base = whole ? (own && !last_word ? p.total_tokens * p.num_q_heads : 0) + first_row : p.slot0(line) + (static_cast<int64_t>(cta) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
             const int32_t skip = whole ? p.num_q_heads - p.group : 0;  // rows between a token's last and the next one's first
             float* dst = (whole ? p.whole_o : p.part_o) + base * D + d;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + base * D + d;
@@ -404,13 +406,13 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
             if (lane == 0) mbar_arrive(&ctl->o_free[ob]);
             ++segments;
         }
-    } else {
+    } else if (warp < kProducerWarp) {
         // =========================================================== softmax
         // After a wait that ran out (ok == false) a warp goes through the rest of its walk without waiting: every warp still meets
         // the others at the same barriers, and the outputs of the call are undefined anyway.
-        if constexpr (L::kSplitRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         Walk walk;
-        walk.start(p);
+        walk.start(p, line * p.ctas + cta);
         constexpr int kBlocks = L::kBlocks;
         const int team = warp >> 2, quarter = warp & 3, bar = 1 + team;
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
@@ -622,42 +624,81 @@ group_tile_kernel(const __grid_constant__ CUtensorMap tmap_q1, const __grid_cons
     }
 }
 
+// One line: every CTA a piece of it.
 template <int D, int kCap>
-rpx_status_t launch(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
+__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1) group_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
+    attend<D, kCap, Layout<D, kCap>::kThreads>(maps, p, 0, blockIdx.x);
+}
+// Two lines: the first CTAs take the groups' shared keys, the others, as these end, the sequences' own.
+template <int D, int kCap, int kSeqCap>
+__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1)
+group_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Maps seq_maps, const __grid_constant__ Params p) {
+    constexpr int kThreads = Layout<D, kCap>::kThreads;
+    if (blockIdx.x < p.ctas) attend<D, kCap, kThreads>(maps, p, 0, blockIdx.x);
+    else attend<D, kSeqCap, kThreads>(seq_maps, p, 1, blockIdx.x - p.ctas);
+}
+
+template <int D, int kCap>
+rpx_status_t make_maps(Maps* m, const Params& p, const rpx_kv_cache_t& cache) {
     using L = Layout<D, kCap>;
     static_assert(L::kSlotsK >= 2 && L::kSlotsV >= 2 && L::kSmemBytes <= 232448, "shared memory of one CTA");
     static_assert(L::kTmemCols >= 32 && L::kTmemCols <= 512, "tensor memory");
-    CUtensorMap tq1, tqh, tqb, tk, tv;
     {
         // a block's rows as (64 elements, heads of a KV head, tokens)
         const uint64_t dims[3] = {D, static_cast<uint64_t>(p.num_q_heads), static_cast<uint64_t>(p.total_tokens)};
         const uint64_t strides[2] = {D * 2ull, static_cast<uint64_t>(p.q_stride) * 2};
         uint32_t box[3] = {64, static_cast<uint32_t>(p.group), 1};
-        if (rpx_status_t rc = encode_tmap_bf16(&tq1, p.q, 3, dims, strides, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&m->q1, p.q, 3, dims, strides, box)) return rc;
         box[2] = static_cast<uint32_t>(L::q_box_tokens(false, p.group));
-        if (rpx_status_t rc = encode_tmap_bf16(&tqh, p.q, 3, dims, strides, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&m->qh, p.q, 3, dims, strides, box)) return rc;
         box[2] = static_cast<uint32_t>(L::q_box_tokens(true, p.group));
-        if (rpx_status_t rc = encode_tmap_bf16(&tqb, p.q, 3, dims, strides, box)) return rc;
+        if (rpx_status_t rc = encode_tmap_bf16(&m->qb, p.q, 3, dims, strides, box)) return rc;
     }
     // the pool as groups of 8 keys: two per page and head
     const uint64_t groups = static_cast<uint64_t>(cache.num_blocks) * p.num_kv_heads * 2;  // (fits 32 bits: checked by the caller)
     const uint64_t dims[4] = {64, 8, D / 64, groups};
     const uint64_t strides[3] = {D * 2ull, 128, 8 * D * 2ull};
     const uint32_t box[4] = {64, 8, D / 64, 2};
-    if (rpx_status_t rc = encode_tmap_bf16(&tk, cache.k_cache, 4, dims, strides, box)) return rc;
-    if (rpx_status_t rc = encode_tmap_bf16(&tv, cache.v_cache, 4, dims, strides, box)) return rc;
+    if (rpx_status_t rc = encode_tmap_bf16(&m->k, cache.k_cache, 4, dims, strides, box)) return rc;
+    return encode_tmap_bf16(&m->v, cache.v_cache, 4, dims, strides, box);
+}
+
+template <int D, int kCap>
+rpx_status_t launch_one(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
+    using L = Layout<D, kCap>;
+    Maps maps;
+    if (rpx_status_t rc = make_maps<D, kCap>(&maps, p, cache)) return rc;
     auto* kernel = group_tile_kernel<D, kCap>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess) return RPX_ERR_CUDA;
-    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, L::kSmemBytes, stream, tq1, tqh, tqb, tk, tv, p);
+    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, L::kSmemBytes, stream, maps, p);
+}
+template <int D, int kCap, int kSeqCap>
+rpx_status_t launch_two(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
+    using L = Layout<D, kCap>;
+    constexpr size_t bytes = L::kSmemBytes > Layout<D, kSeqCap>::kSmemBytes ? L::kSmemBytes : Layout<D, kSeqCap>::kSmemBytes;
+    Maps maps, seq_maps;
+    if (rpx_status_t rc = make_maps<D, kCap>(&maps, p, cache)) return rc;
+    if (rpx_status_t rc = make_maps<D, kSeqCap>(&seq_maps, p, cache)) return rc;
+    auto* kernel = group_tiles_kernel<D, kCap, kSeqCap>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return RPX_ERR_CUDA;
+    return launch_on_top(kernel, static_cast<unsigned>(2 * p.ctas), L::kThreads, bytes, stream, maps, seq_maps, p);
 }
 
 template <int D>
 rpx_status_t launch_cap(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
-    switch (p.cap) {
-        case 16: return launch<D, 16>(p, cache, stream);
-        case 32: return launch<D, 32>(p, cache, stream);
-        case 64: return launch<D, 64>(p, cache, stream);
-        default: return launch<D, (D == 128 ? 112 : 128)>(p, cache, stream);
+    constexpr int kMost = D == 128 ? 112 : 128;
+    if (p.lines == 2) {
+        switch (p.cap[1]) {
+            case 16: return launch_two<D, kMost, 16>(p, cache, stream);
+            case 32: return launch_two<D, kMost, 32>(p, cache, stream);
+            default: return launch_two<D, kMost, 64>(p, cache, stream);
+        }
+    }
+    switch (p.cap[0]) {
+        case 16: return launch_one<D, 16>(p, cache, stream);
+        case 32: return launch_one<D, 32>(p, cache, stream);
+        case 64: return launch_one<D, 64>(p, cache, stream);
+        default: return launch_one<D, kMost>(p, cache, stream);
     }
 }
 
