@@ -21,8 +21,8 @@ using namespace group;
 // One block, which also finds where every CTA's piece begins.
 constexpr int kPlanThreads = 1024;
 
-// Units of the line (20 ns): of a tile against no rows, against 128 more, and of what a segment costs besides its tiles.
-constexpr int kWorkUnits = 10, kRowUnits = 61, kSegmentWork = 15;
+// Units of the line (20 ns): of a tile's work, rows that add one, and what a segment costs besides.
+constexpr int kWorkUnits = 48, kRowsAUnit = 8, kSegmentWork = 10;
 
 __device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t cap, int32_t group = -1) {
     Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, len / kTile + (len % kTile != 0 ? 1 : 0)};
@@ -35,11 +35,10 @@ __device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32
     const int32_t rows = e.tiles <= 2 && cap > 64 ? 64 : cap, per = max(1, rows / p.group);  // (at most cap / group: Q's box)
     e.blocks = n <= per ? 1 : (n + per - 1) / per;
     e.block_tokens = e.blocks == 1 ? n : (n + e.blocks - 1) / e.blocks;
-    // A tile's bytes are tile_units of this SM's share of HBM, once for all blocks; the work against a block overlaps with that, what
-    // a segment costs besides does not quite.
-    const int32_t rows_now = e.block_tokens * p.group, work = kWorkUnits + rows_now * kRowUnits / 128;
-    const int32_t bytes = p.tile_units / e.blocks, beside = kSegmentWork / e.tiles;
-    e.weight = max(bytes, work) + beside;
+    // A tile's bytes are tile_units of this SM's share of HBM, once for all blocks (on a line of their own, sequences do not meet all
+    // SMs there); the work against a block overlaps with that, what a segment costs besides does not quite.
+    const int32_t bytes = (p.lines == 2 && cap == p.cap[1] ? p.tile_units * 2 / 3 : p.tile_units) / e.blocks;
+    e.weight = max(bytes, kWorkUnits + e.block_tokens * p.group / kRowsAUnit) + kSegmentWork / e.tiles;
     return e;
 }
 
@@ -111,14 +110,24 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* sums, int64_t* 
     return __shfl_sync(0xffffffffu, upto - w, warp) + sum;
 }
 
-// Every CTA's start, and the lines' totals.
+// The cut, and every CTA's start.  Two lines get CTAs by what they cost.
 template <class Unit0>
 __device__ __forceinline__ void leave_starts(const Params& p, int64_t line1, int64_t total, Unit0 unit0) {
     const int32_t i = threadIdx.x;
-    if (i < p.lines) p.total[i] = p.lines == 1 ? total : i == 0 ? line1 : total - line1;
-    if (i < p.lines * p.ctas) {
-        const int32_t line = i / p.ctas;
-        p.starts[i] = find_start(p, line, line == 0 ? 0 : line1, p.lines == 1 ? total : line == 0 ? line1 : total - line1, i - line * p.ctas, unit0);
+    if (i >= p.ctas) return;
+    int32_t first = p.ctas;  // CTAs of the first line
+    if (p.lines == 2) {
+        first = static_cast<int32_t>(static_cast<double>(line1) / static_cast<double>(max(total, static_cast<int64_t>(1))) * p.ctas + 0.5);
+        first = min(max(first, line1 > 0 ? 1 : 0), p.ctas - (line1 < total ? 1 : 0));
+    }
+    const int32_t line = i < first ? 0 : 1, ctas = line == 0 ? first : p.ctas - first;
+    const int64_t units = p.lines == 1 ? total : line == 0 ? line1 : total - line1, size = piece_units(units, ctas);
+    p.starts[i] = find_start(p, line, line == 0 ? 0 : line1, units, size, line == 0 ? i : i - first, unit0);
+    if (i == 0 || i == first) {
+        p.cut->ctas[line] = ctas;
+        p.cut->size[line] = size;
+        p.cut->inverse[line] = 1.0 / static_cast<double>(size);
+        if (ctas == p.ctas) p.cut->ctas[1 - line] = 0;
     }
 }
 
@@ -247,128 +256,147 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------ the join
-// A warp takes kRows rows of a KV head's group of one token (the sets of all of them lie alike) and kBatch sets of each at a time,
-// all of them on their way together: the shared keys' pieces in order, then its own.  Many sets and few rows: 1 x 8; many rows
-// have few sets each: 4 x 2.
-constexpr int kJoinWarps = 8;
+// A warp per row (token, query head), or where there are few rows with many sets, the eight warps of a block: the shared keys'
+// pieces in order, then its own, kBatch sets a warp at a time, all of them on their way together (one after the other, 17 sets
+// took 6 us).  The code is kept short: at this length a kernel waits for its instructions first; and what all warps read alike -
+// the cut, the entries - comes through L1 (10240 warps that asked L2 for the same line waited 3 us for it).
+constexpr int kJoinWarps = 8, kBatch = 4;
 
 // The sets of a row against one entry: where the first one lies, how far on the next (twice as far on all others), and how many.
 struct Sets {
     int64_t first;
     int32_t step, n;
-    bool whole;
 };
-__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int32_t line, int64_t total, int32_t kv_head, int32_t in_group, int64_t token, int64_t own_row) {
-    const int64_t size = piece_units(total, p.ctas);
-    const int32_t in = static_cast<int32_t>(token - q.tok0), block = q.blocks == 1 ? 0 : in / q.block_tokens;
+__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int32_t line, int32_t kv_head, int32_t in_group, int32_t in) {
+    const int64_t size = p.cut->size[line];
+    const double inverse = p.cut->inverse[line];
+    const int32_t block = q.blocks == 1 ? 0 : in / q.block_tokens;
     const int64_t unit = q.unit0 + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
-    const int64_t c0 = quotient(unit, size);
+    const int32_t c0 = piece_of(unit, size, inverse);
     Sets r;
-    r.n = static_cast<int32_t>(quotient(unit + static_cast<int64_t>(q.tiles - 1) * q.weight, size) - c0) + 1;
-    r.whole = r.n == 1;
+    r.n = piece_of(unit + static_cast<int64_t>(q.tiles - 1) * q.weight, size, inverse) - c0 + 1;
     // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
     r.step = p.cap[line];
-    r.first = r.whole ? own_row : p.slot0(line) + (c0 * 2 + 1) * r.step + (in - block * q.block_tokens) * p.group + in_group;
+    r.first = p.slot0(line) + (static_cast<int64_t>(c0) * 2 + 1) * r.step + (in - block * q.block_tokens) * p.group + in_group;
     return r;
 }
 
-template <int D, int kRows, int kBatch>
-__global__ void __launch_bounds__(kJoinWarps * 32, 4) group_join_kernel(const __grid_constant__ Params p, int32_t per_group) {
+template <int D, int kSplit>
+__global__ void __launch_bounds__(kJoinWarps * 32, 5) group_join_kernel(const __grid_constant__ Params p) {
     constexpr int kCols = D / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // task = (token, KV head, run of kRows rows)
-    const int64_t task = static_cast<int64_t>(blockIdx.x) * kJoinWarps + warp, pair = quotient(task, per_group), token = quotient(pair, p.num_kv_heads);
-    const int32_t kv_head = static_cast<int32_t>(pair - token * p.num_kv_heads), in_group = static_cast<int32_t>(task - pair * per_group) * kRows;
+    __shared__ float part_acc[kSplit > 1 ? kSplit : 1][D];
+    __shared__ float2 part_ml[kSplit > 1 ? kSplit : 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % kSplit;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / kSplit) + warp / kSplit;
+    const int32_t in_group = blockIdx.y, kv_head = blockIdx.z;
     const bool there = token < p.total_tokens;
     const int32_t s = find_seq(p, there ? token : 0, lane);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // (of rows that are left out too: this grid never ends before that one)
     if (!there) return;
-    const Entry own = load_entry(p.entries + p.n_groups + s);
-    const int64_t total0 = __ldcg(p.total), total1 = p.lines == 2 ? __ldcg(p.total + 1) : total0, all_rows = p.total_tokens * p.num_q_heads;
+    const Entry own = p.entries[p.n_groups + s];
     if (token < own.tok0 || token - own.tok0 >= own.n) return;  // in no sequence, or in one that does not fit
-    const int64_t row0 = token * p.num_q_heads + kv_head * p.group + in_group;
-    const int32_t rows = min(kRows, p.group - in_group);
-    const Sets of_own = find_sets(p, own, p.lines - 1, total1, kv_head, in_group, token, all_rows + row0);
-    if (own.group < 0 && of_own.whole) return;  // written whole
-    Sets of_group = {0, 0, 0, false};
-    if (own.group >= 0) of_group = find_sets(p, load_entry(p.entries + own.group), 0, total0, kv_head, in_group, token, row0);
-    float top[kRows], sum[kRows], acc[kRows][kCols];
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-        top[k] = -CUDART_INF_F;
-        sum[k] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) acc[k][i] = 0.f;
+    const int64_t out_row = token * p.num_q_heads + kv_head * p.group + in_group;
+    Sets of_own = find_sets(p, own, p.lines - 1, kv_head, in_group, static_cast<int32_t>(token - own.tok0)), of_group = {0, 0, 0};
+    if (own.group < 0 && of_own.n == 1) return;  // written whole
+    if (own.group >= 0) {
+        const Entry g = p.entries[own.group];
+        of_group = find_sets(p, g, 0, kv_head, in_group, static_cast<int32_t>(token - g.tok0));
     }
+    float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
     const int32_t n = of_group.n + of_own.n;
-    for (int32_t j0 = 0; j0 < n; j0 += kBatch) {
-        float2 ml[kRows][kBatch];
-        float v[kRows][kBatch][kCols];
+#pragma unroll 1
+    for (int32_t j0 = sub; j0 < n; j0 += kSplit * kBatch) {
+        float2 ml[kBatch];
+        float v[kBatch][kCols];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const bool shared = j0 + u < of_group.n;
-            const int32_t j = j0 + u - (shared ? 0 : of_group.n);
-            const bool whole = shared ? of_group.whole : of_own.whole;
-            const int64_t at = (shared ? of_group.first : of_own.first) + (j == 0 ? 0 : static_cast<int64_t>(2 * j - 1) * (shared ? of_group.step : of_own.step));
-            const float2* from_ml = (whole ? p.whole_ml : p.part_ml) + at;
-            const float* from = (whole ? p.whole_o : p.part_o) + at * D + lane * kCols;
+            const bool shared = j0 + kSplit * u < of_group.n;
+            const Sets& of = shared ? of_group : of_own;
+            const int32_t j = j0 + kSplit * u - (shared ? 0 : of_group.n);
+            int64_t at = of.first + (j == 0 ? 0 : static_cast<int64_t>(2 * j - 1) * of.step);
+            const float2* mls = p.part_ml;
+            const float* os = p.part_o;
+            if (of.n == 1) {  // a segment that is whole: the row's own place
+                at = out_row + (shared ? 0 : p.total_tokens * p.num_q_heads);
+                mls = p.whole_ml;
+                os = p.whole_o;
+            }
+            ml[u] = make_float2(-CUDART_INF_F, 0.f);
 #pragma unroll
-            for (int k = 0; k < kRows; ++k) {
-                ml[k][u] = make_float2(-CUDART_INF_F, 0.f);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) v[k][u][i] = 0.f;
-                if (j0 + u < n && k < rows) {
-                    ml[k][u] = __ldcg(from_ml + k);
-                    if constexpr (kCols == 4) *reinterpret_cast<float4*>(v[k][u]) = __ldcg(reinterpret_cast<const float4*>(from + k * D));
-                    else *reinterpret_cast<float2*>(v[k][u]) = __ldcg(reinterpret_cast<const float2*>(from + k * D));
-                }
+            for (int i = 0; i < kCols; ++i) v[u][i] = 0.f;
+            if (j0 + kSplit * u < n) {
+                ml[u] = __ldcg(mls + at);
+                if constexpr (kCols == 4) *reinterpret_cast<float4*>(v[u]) = __ldcg(reinterpret_cast<const float4*>(os + at * D) + lane);
+                else *reinterpret_cast<float2*>(v[u]) = __ldcg(reinterpret_cast<const float2*>(os + at * D) + lane);
             }
         }
+        float to = top;
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            float to = top[k];
+        for (int u = 0; u < kBatch; ++u) to = fmaxf(to, ml[u].x);
+        const float base = to == -CUDART_INF_F ? 0.f : to;  // (no key seen so far)
+        const float keep = fast_exp2(top - base);
+        top = to;
+        sum *= keep;
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) to = fmaxf(to, ml[k][u].x);
-            const float base = to == -CUDART_INF_F ? 0.f : to;  // (no key seen so far)
-            const float keep = fast_exp2(top[k] - base);
-            top[k] = to;
-            sum[k] *= keep;
+        for (int i = 0; i < kCols; ++i) acc[i] *= keep;
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) acc[k][i] *= keep;
+        for (int u = 0; u < kBatch; ++u) {
+            // a set that saw no key has a sum and outputs of 0; one of nothing but NaN goes on with a factor of 1
+            const float f = ml[u].x == -CUDART_INF_F ? 1.f : fast_exp2(ml[u].x - base);
+            sum = fmaf(f, ml[u].y, sum);
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                // a set that saw no key has a sum and outputs of 0; one of nothing but NaN goes on with a factor of 1
-                const float f = ml[k][u].x == -CUDART_INF_F ? 1.f : fast_exp2(ml[k][u].x - base);
-                sum[k] = fmaf(f, ml[k][u].y, sum[k]);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) acc[k][i] = fmaf(f, v[k][u][i], acc[k][i]);
-            }
+            for (int i = 0; i < kCols; ++i) acc[i] = fmaf(f, v[u][i], acc[i]);
         }
     }
+    if constexpr (kSplit > 1) {
 #pragma unroll
-    for (int k = 0; k < kRows; ++k)
-        if (k < rows) {
-            const float inv = 1.f / sum[k];
-            uint32_t w[kCols / 2];
+        for (int i = 0; i < kCols; ++i) part_acc[warp][lane * kCols + i] = acc[i];
+        if (lane == 0) part_ml[warp] = make_float2(top, sum);
+        __syncthreads();  // (the warps of a block are of one row)
+        if (warp != 0) return;
+        top = -CUDART_INF_F;
+        sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < kCols / 2; ++i) w[i] = pack_bf16x2(acc[k][2 * i] * inv, acc[k][2 * i + 1] * inv);
-            uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + (row0 + k) * D + lane * kCols);
-            if constexpr (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-            else *dst = w[0];
-            if (lane == 0 && p.lse != nullptr) p.lse[row0 + k] = (top[k] + log2f(sum[k])) * kLn2;
+        for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+        for (int w = 0; w < kSplit; ++w) top = fmaxf(top, part_ml[w].x);
+        for (int w = 0; w < kSplit; ++w) {
+            const float2 ml = part_ml[w];
+            const float f = ml.x == -CUDART_INF_F ? 1.f : fast_exp2(ml.x - top);  // (as above)
+            sum = fmaf(f, ml.y, sum);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) acc[i] = fmaf(f, part_acc[w][lane * kCols + i], acc[i]);
         }
+    }
+    const float inv = 1.f / sum;
+    uint32_t w[kCols / 2];
+#pragma unroll
+    for (int i = 0; i < kCols / 2; ++i) w[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + out_row * D + lane * kCols);
+    if constexpr (kCols == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    else *dst = w[0];
+    if (lane == 0 && p.lse != nullptr) p.lse[out_row] = (top + log2f(sum)) * kLn2;
 }
 
-template <int D, int kRows, int kBatch>
+template <int D, int kSplit>
 rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
-    const int32_t per_group = (p.group + kRows - 1) / kRows;
-    const int64_t tasks = p.total_tokens * p.num_kv_heads * per_group;
-    return launch_on_top(group_join_kernel<D, kRows, kBatch>, static_cast<unsigned>((tasks + kJoinWarps - 1) / kJoinWarps), kJoinWarps * 32, 0, stream, p, per_group);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    constexpr int kTokens = kJoinWarps / kSplit;
+    config.gridDim = dim3(static_cast<unsigned>((p.total_tokens + kTokens - 1) / kTokens), static_cast<unsigned>(p.group), static_cast<unsigned>(p.num_kv_heads));
+    config.blockDim = dim3(kJoinWarps * 32);
+    config.stream = stream;
+    config.attrs = attr;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, group_join_kernel<D, kSplit>, p) == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
 }
 template <int D>
 rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
-    // as many rows as warps that run at once, or more
-    return p.total_tokens * p.num_q_heads > 148 * 4 * kJoinWarps ? launch_join<D, 4, 2>(p, stream) : launch_join<D, 1, 8>(p, stream);
+    // while a block a row is at most one wave of blocks
+    return p.total_tokens * p.num_q_heads <= 148 * 5 ? launch_join<D, kJoinWarps>(p, stream) : launch_join<D, 1>(p, stream);
 }
 
 // ------------------------------------------------------------------ float32
@@ -505,8 +533,8 @@ size_t carve(Params& p, int32_t head_dim, void* workspace) {
     };
     const size_t rows = static_cast<size_t>(p.total_tokens) * p.num_q_heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * (p.cap[0] + (p.lines == 2 ? p.cap[1] : 0));
     p.entries = reinterpret_cast<Entry*>(take((static_cast<size_t>(p.n_groups) + p.batch) * sizeof(Entry)));
-    p.total = reinterpret_cast<int64_t*>(take(2 * sizeof(int64_t)));
-    p.starts = reinterpret_cast<Start*>(take(2 * kMaxCtas * sizeof(Start)));
+    p.cut = reinterpret_cast<Cut*>(take(sizeof(Cut)));
+    p.starts = reinterpret_cast<Start*>(take(kMaxCtas * sizeof(Start)));
     p.whole_ml = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
     p.part_ml = reinterpret_cast<float2*>(take(slots * sizeof(float2)));
     p.whole_o = reinterpret_cast<float*>(take(rows * head_dim * sizeof(float)));
@@ -534,6 +562,7 @@ size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, 
 
 bool group_too_large(const GroupArgs& a) {
     if ((a.total_tokens * a.num_q_heads + kRowWarps - 1) / kRowWarps > INT32_MAX) return true;
+    if (a.num_kv_heads > 65535) return true;  // (a dimension of the join's grid)
     return a.batch > INT32_MAX - a.n_groups - 1 || a.cache->num_blocks * a.num_kv_heads > INT32_MAX / 2;
 }
 

@@ -3,7 +3,7 @@
 // All key tiles of all segments lie in a line: first the groups' shared pages (an entry per group), then every sequence's own
 // keys (an entry per sequence).  A segment is one KV head of an entry and one block of its rows (row = token * group + head
 // within the KV head's group).  The line is cut into equal pieces, one per CTA; where groups have more rows than one
-// kernel form does well beside single sequences, the two parts of the line are cut apart, for CTAs of two forms in one launch.  A segment that lies in one piece leaves its
+// kernel form does well beside single sequences, the two parts are a line each, for CTAs of two forms side by side in one launch.  A segment that lies in one piece leaves its
 // rows' (maximum in log2 units, sum) and un-normalised outputs in the rows' own place in the workspace (or, where its sequence
 // shares nothing, the result in `out`), a segment that is cut one set per piece; the join adds them up in the order of the keys.
 // The cut goes by lengths alone, so the same call gives the same bits.
@@ -26,7 +26,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // The line is measured in units of some 20 ns; going over to another segment counts kSegment of them (what more it costs is in
 // the weight of its tiles).  A piece has kMinUnits at least: as long as the heaviest tile, so every piece between a segment's
 // first and last holds one.
-constexpr int kSegment = 25, kMinUnits = 256;
+constexpr int kSegment = 10, kMinUnits = 128;
 
 struct __align__(16) Entry {
     int32_t tok0, n, len;   // first query token, query tokens, keys
@@ -46,6 +46,7 @@ __device__ __forceinline__ Entry load_entry(const Entry* at) {
 }
 
 struct Start;
+struct Cut;
 
 struct Params {
     const void* q;
@@ -71,11 +72,11 @@ struct Params {
     int32_t lines;         // 1: groups and sequences are one line; 2: a line each
     int32_t cap[2];        // rows per block at most, of each line
     Entry* entries;        // workspace [n_groups + batch]
-    struct Start* starts;  // workspace [lines][ctas]
-    int64_t* total;        // workspace [lines]: units of each line
+    struct Start* starts;  // workspace [ctas]: those of the first line's pieces, then the second's
+    struct Cut* cut;       // workspace
     float2* whole_ml;      // workspace [2][total_tokens][H_q]: of segments that are not cut: shared, own
     float* whole_o;        // workspace [2][total_tokens][H_q][D]
-    float2* part_ml;       // workspace [lines][ctas][2][cap of the line]: of segments that are
+    float2* part_ml;       // workspace [ctas][2][cap of the first line], [ctas][2][cap of the second]: of segments that are
     float* part_o;         // workspace, rows as those, [D]
     __host__ __device__ __forceinline__ int32_t line_of(int32_t entry) const { return lines == 2 && entry >= n_groups ? 1 : 0; }
     __host__ __device__ __forceinline__ int64_t slot0(int32_t line) const { return line == 0 ? 0 : static_cast<int64_t>(ctas) * 2 * cap[0]; }
@@ -119,10 +120,22 @@ __device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int 
     return lo;
 }
 
-// Pieces: the line of `total` units in runs of piece_units() (the last ones may be short or empty).
+// How each line is cut: its pieces, the units of one (the last ones may be short or empty), and 1 / units.
+struct Cut {
+    int32_t ctas[2];
+    int64_t size[2];
+    double inverse[2];
+};
 __device__ __forceinline__ int64_t piece_units(int64_t total, int32_t ctas) {
     const int64_t even = (total + ctas - 1) / ctas;
     return even > kMinUnits ? even : kMinUnits;
+}
+// The piece that a unit is in.  (A division takes more instructions than the join has otherwise.)
+__device__ __forceinline__ int32_t piece_of(int64_t unit, int64_t size, double inverse) {
+    int64_t q = static_cast<int64_t>(static_cast<double>(unit) * inverse);
+    const int64_t rest = unit - q * size;
+    q += rest < 0 ? -1 : rest >= size ? 1 : 0;
+    return static_cast<int32_t>(q);
 }
 
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // (64-bit division takes ten times as long)
@@ -138,8 +151,8 @@ struct __align__(16) Start {
 };
 // By one thread for one CTA; unit0(e) gives an entry's first unit, counted from the start of the first line.
 template <class Unit0>
-__device__ __forceinline__ Start find_start(const Params& p, int32_t line, int64_t line0, int64_t total, int32_t cta, Unit0 unit0) {
-    const int64_t size = piece_units(total, p.ctas), from = min(total, size * static_cast<int64_t>(cta)), end = min(total, from + size);
+__device__ __forceinline__ Start find_start(const Params& p, int32_t line, int64_t line0, int64_t total, int64_t size, int32_t cta, Unit0 unit0) {
+    const int64_t from = min(total, size * static_cast<int64_t>(cta)), end = min(total, from + size);
     Start r = {};
     r.left = end - from;
     if (r.left == 0) return r;

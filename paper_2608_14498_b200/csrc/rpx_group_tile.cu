@@ -120,12 +120,14 @@ struct Maps {  // Q (boxes of one token, of a half of its room, of both), K, V
     CUtensorMap q1, qh, qb, k, v;
 };
 
-// One CTA's piece of a line.  (kThreads: of the block; warps beyond this form's only meet the others at its barriers.)
-template <int D, int kCap, int kThreads>
+// One CTA's piece of a line.  (kThreads: of the block; warps beyond this form's only meet the others at its barriers.  kPlanned: the
+// plan has been waited for.)
+template <int D, int kCap, int kThreads, bool kPlanned>
 __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_t line, int32_t cta) {
     using L = Layout<D, kCap>;
     constexpr int kTeams = L::kTeams, kProducerWarp = L::kProducerWarp, kScoreWarp = L::kScoreWarp, kValueWarp = L::kValueWarp, kQWarp = L::kQWarp, kOutWarp = L::kOutWarp;
-    constexpr int kSoftmaxRegs = kThreads == 768 ? 96 : 0, kOtherRegs = 48;  // 512 * 96 + 256 * 48 = 768 * 80, what a launch of 768 threads has
+    // 512 * 96 + 256 * 48 = 512 * 88 + 256 * 64 = 768 * 80, what a launch of 768 threads has
+    constexpr int kSoftmaxRegs = kThreads != 768 ? 0 : L::kBlocks > 2 ? 96 : 88, kOtherRegs = L::kBlocks > 2 ? 48 : 64;
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0u) {  // swizzled tiles need 1024-byte alignment; never expected
         if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, RPX_ERR_CUDA);
@@ -165,14 +167,14 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = ctl->tmem_base;  // S at columns 0 and kCap, O at kOCol
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
+    if constexpr (!kPlanned) asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
     auto rows16 = [&](const auto& w) { return (w.tokens() * p.group + 15) & ~15; };
 
     if (warp == kProducerWarp) {
         // =========================================================== producer: K a tile ahead of V, through all segments
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p, line * p.ctas + cta);
+        walk.start(p, blockIdx.x);
         bool ok = true;
         uint32_t nk = 0, nv = 0;
         // the tile whose V comes next: page number of this lane's page, boxes, KV head
@@ -227,7 +229,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
         // =========================================================== S^T = K Q^T, by one thread
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p, line * p.ctas + cta);
+        walk.start(p, blockIdx.x);
         if (elect_one()) {
             const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem), 16, L::kHalves * 1024);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem + L::kQOff), 16, 1024);
@@ -268,7 +270,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
         // =========================================================== O^T += V^T P^T, by one thread
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p, line * p.ctas + cta);
+        walk.start(p, blockIdx.x);
         if (elect_one()) {
             // D = 64: M stays 128, and the lanes 64 .. 127 of O^T, which nobody reads, are fed by whatever lies 1 KB on
             const uint64_t v_desc = make_smem_desc_sw128(smem_u32(smem + L::kVOff), 1024, L::kHalves * 1024);
@@ -312,7 +314,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
         // (What lies behind the block's rows is another token's, or was there before: those rows are nobody's.)
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p, line * p.ctas + cta);
+        walk.start(p, blockIdx.x);
         if (elect_one()) {
             QTurn turn;
             bool ok = true;
@@ -338,7 +340,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
         // =========================================================== output: a warp 32 elements of D of all rows
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
-        walk.start(p, line * p.ctas + cta);
+        walk.start(p, blockIdx.x);
         const int quarter = warp & 3;
         const int32_t d = quarter * 32 + lane;
         uint32_t segments = 0;
@@ -380,22 +382,27 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
                     }
                     tc_fence_after_sync();
                 }
+                if (d >= D) continue;
+                int32_t place = r0 + over_group(p, r0) * skip, in_group = r0 - over_group(p, r0) * p.group;  // of the next row
 #pragma unroll 1
                 for (int32_t c = 0; c < here; c += 8) {
                     uint32_t o[8], lo[8];
                     tmem_ld8(o_addr + r0 + c, o);
                     if (two_terms) tmem_ld8(o_addr + n16 + r0 + c, lo);
                     tmem_ld_wait();
-                    if (two_terms)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) + __uint_as_float(lo[i]));
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const int64_t to = static_cast<int64_t>(__shfl_sync(0xffffffffu, at, c + i)) * D;
-                        const float f = __shfl_sync(0xffffffffu, inv, c + i);
-                        if (c + i < here && d < D) {
-                            if (last_word) out[to] = __float2bfloat16_rn(__uint_as_float(o[i]) * f);
-                            else dst[to] = __uint_as_float(o[i]);
+                        float x = __uint_as_float(o[i]);
+                        if (two_terms) x += __uint_as_float(lo[i]);
+                        const float f = last_word ? __shfl_sync(0xffffffffu, inv, c + i) : 1.f;
+                        if (c + i < here) {
+                            if (last_word) out[static_cast<int64_t>(place) * D] = __float2bfloat16_rn(x * f);
+                            else dst[static_cast<int64_t>(place) * D] = x;
+                        }
+                        ++place;
+                        if (++in_group == p.group) {
+                            in_group = 0;
+                            place += skip;
                         }
                     }
                 }
@@ -412,7 +419,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
         // the others at the same barriers, and the outputs of the call are undefined anyway.
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         Walk walk;
-        walk.start(p, line * p.ctas + cta);
+        walk.start(p, blockIdx.x);
         constexpr int kBlocks = L::kBlocks;
         const int team = warp >> 2, quarter = warp & 3, bar = 1 + team;
         const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
@@ -627,15 +634,17 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
 // One line: every CTA a piece of it.
 template <int D, int kCap>
 __global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1) group_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
-    attend<D, kCap, Layout<D, kCap>::kThreads>(maps, p, 0, blockIdx.x);
+    attend<D, kCap, Layout<D, kCap>::kThreads, false>(maps, p, 0, blockIdx.x);
 }
-// Two lines: the first CTAs take the groups' shared keys, the others, as these end, the sequences' own.
+// Two lines: so many CTAs take the groups' shared keys, the others the sequences' own.
 template <int D, int kCap, int kSeqCap>
 __global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1)
 group_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Maps seq_maps, const __grid_constant__ Params p) {
     constexpr int kThreads = Layout<D, kCap>::kThreads;
-    if (blockIdx.x < p.ctas) attend<D, kCap, kThreads>(maps, p, 0, blockIdx.x);
-    else attend<D, kSeqCap, kThreads>(seq_maps, p, 1, blockIdx.x - p.ctas);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
+    const int32_t first = __ldcg(&p.cut->ctas[0]), cta = blockIdx.x;
+    if (cta < first) attend<D, kCap, kThreads, true>(maps, p, 0, cta);
+    else attend<D, kSeqCap, kThreads, true>(seq_maps, p, 1, cta - first);
 }
 
 template <int D, int kCap>
@@ -681,7 +690,7 @@ rpx_status_t launch_two(const Params& p, const rpx_kv_cache_t& cache, cudaStream
     if (rpx_status_t rc = make_maps<D, kSeqCap>(&seq_maps, p, cache)) return rc;
     auto* kernel = group_tiles_kernel<D, kCap, kSeqCap>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return RPX_ERR_CUDA;
-    return launch_on_top(kernel, static_cast<unsigned>(2 * p.ctas), L::kThreads, bytes, stream, maps, seq_maps, p);
+    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, bytes, stream, maps, seq_maps, p);
 }
 
 template <int D>
