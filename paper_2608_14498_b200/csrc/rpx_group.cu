@@ -21,8 +21,9 @@ using namespace group;
 // One block, which also finds where every CTA's piece begins.
 constexpr int kPlanThreads = 1024;
 
-// Units of the line (20 ns): of a tile's work, rows that add one, and what a segment costs besides.
-constexpr int kWorkUnits = 48, kRowsAUnit = 8, kSegmentWork = 10;
+// Units of the line (20 ns): of a tile's work, rows that add one; and what a segment costs besides: two a row, at most kSegmentWork
+// (its rows go out one after the other).
+constexpr int kWorkUnits = 48, kRowsAUnit = 8, kSegmentWork = 100;
 
 __device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t cap, int32_t group = -1) {
     Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, len / kTile + (len % kTile != 0 ? 1 : 0)};
@@ -38,7 +39,8 @@ __device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32
     // A tile's bytes are tile_units of this SM's share of HBM, once for all blocks (on a line of their own, sequences do not meet all
     // SMs there); the work against a block overlaps with that, what a segment costs besides does not quite.
     const int32_t bytes = (p.lines == 2 && cap == p.cap[1] ? p.tile_units * 2 / 3 : p.tile_units) / e.blocks;
-    e.weight = max(bytes, kWorkUnits + e.block_tokens * p.group / kRowsAUnit) + kSegmentWork / e.tiles;
+    const int32_t block_rows = e.block_tokens * p.group;
+    e.weight = max(bytes, kWorkUnits + block_rows / kRowsAUnit) + min(2 * block_rows, kSegmentWork) / e.tiles;
     return e;
 }
 

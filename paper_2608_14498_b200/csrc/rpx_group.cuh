@@ -26,7 +26,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // The line is measured in units of some 20 ns; going over to another segment counts kSegment of them (what more it costs is in
 // the weight of its tiles).  A piece has kMinUnits at least: as long as the heaviest tile, so every piece between a segment's
 // first and last holds one.
-constexpr int kSegment = 10, kMinUnits = 128;
+constexpr int kSegment = 10, kMinUnits = 192;
 
 struct __align__(16) Entry {
     int32_t tok0, n, len;   // first query token, query tokens, keys

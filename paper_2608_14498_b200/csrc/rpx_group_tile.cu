@@ -588,6 +588,9 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
                 const int32_t ragged = left < kTile ? left & 15 : 0;
                 if (ragged != 0) {
                     const uint32_t st = tiles % L::kSlotsV;
+                    // (The product two tiles before has been waited for by teams with rows; without that wait the slot may still be an
+                    // earlier tile's, and the barrier's parity cannot tell the two.)
+                    if (ok && tiles >= 2) ok = mbar_wait(&ctl->pv_done[b], ((tiles >> 1) - 1) & 1u, abort_flag);
                     if (ok) ok = mbar_wait(&ctl->v_full[st], (tiles / L::kSlotsV) & 1u, abort_flag);
                     uint8_t* v = smem + L::kVOff + st * L::kTensorBytes;
                     for (int32_t i = threadIdx.x; i < (16 - ragged) * (D / 8); i += 128 * kTeams)

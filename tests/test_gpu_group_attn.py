@@ -88,9 +88,11 @@ def exact(s, softmax_scale=None):
     return out, lse, pv, big
 
 
-def check(s, got, one_term=True, softmax_scale=None):
+def check(s, got, softmax_scale=None):
+    """P is one bf16 term only where a block may have more than 64 rows."""
     out, lse, pv, big = exact(s, softmax_scale)
     d = s["q"].shape[2]
+    one_term = max(s["max_q"], s["max_group"]) * s["q"].shape[1] // s["kc"].shape[1] > 64
     bf16 = s["q"].dtype == torch.bfloat16
     score = (d + 4) * 2.0 ** -24 * big
     w = score + 2.0 ** -21 + ((2.0 ** -8 if one_term else 2.0 ** -16) if bf16 else 0.0)
@@ -131,6 +133,19 @@ def test_against_the_definition(cuda_device, name, hq, hkv, d):
     check(s, got)
     again = call(s)
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+@pytest.mark.parametrize("groups", [[(0, [(1000, 1)])] * 256, [(4090, [(509 + i, 1) for i in range(8)])] * 32,
+                                    [(0, [(1 + 17 * i % 999, 1)]) for i in range(300)], [(3000, [(40 + 13 * i, 3) for i in range(5)])] * 20],
+                         ids=["alone", "groups", "many_lengths", "three_tokens"])
+@pytest.mark.parametrize("hq,hkv,d", [(40, 8, 128), (28, 4, 128), (40, 8, 64)])
+def test_many_sequences_that_end_inside_a_page(cuda_device, groups, hq, hkv, d):
+    """Every SM goes through dozens of segments whose last page is partly empty (and holds anything)."""
+    s = make(groups, hq, hkv, d, cuda_device, fill=float("inf"))
+    for bounds in (dict(), dict(max_group_tokens=s["max_group"] + 8), dict(max_group_tokens=s["max_group"] + 40)):
+        for _ in range(2):
+            check(s, call(s, **bounds))
+    assert int(s["status"]) == 0
 
 
 @pytest.mark.parametrize("name", ["one_token", "group_of_8", "mixed", "several_tokens", "long_chunks"])
