@@ -19,7 +19,10 @@
 //
 // The append form (rpx_qk_norm_rope_append) is the forward pass with two more destinations: a row of k goes to its token's
 // slot of the paged cache instead of k_out, and the rows of v follow as units of their own that are only copied there.  A warp
-// finds its token's sequence by itself, 32 offsets a step, while its first rows are on their way.
+// finds its token's sequence by itself, 32 offsets a step, while its first rows and positions are on their way; what is read of
+// the page table is waited for behind the angles.  Bound by memory as well, 28 + 4 + 4 heads of 128 in bf16: 8 x 4096 tokens
+// 105 us (88 % of the copy bandwidth; rows stored page by page cost 5 us more than rows in a line, finding the pages 3).
+// Runs of tokens that share a search, or v copied ahead by the warp, take registers and are slower (120 us).
 #include <cuda_bf16.h>
 
 #include "rpx_internal.h"
@@ -63,18 +66,17 @@ struct Params {
     uint8_t axis[kMaxPairs];
 };
 
-// cos and sin of this token's angles.  The angle is reduced in 64 bits (position * frequency loses whole radians in 32
+// cos and sin of an angle.  The angle is reduced in 64 bits (position * frequency loses whole radians in 32
 // bits at far positions): in units of half a turn, brought into [-1, 1], which 32 bits hold to 2^-25 of a half turn.
-// `place`: the position on every axis where there are no positions (append form).
-__device__ __forceinline__ void token_angles(const Params& p, int64_t token, int lane, float2* cs, int32_t place = 0) {
-    for (int i = lane; i < (p.rot >> 1); i += 32) {
-        const double pos = static_cast<double>(p.positions == nullptr ? place : __ldg(p.positions + p.axis[i] * p.pos_stride + token));
-        const double half_turns = pos * (static_cast<double>(__ldg(p.inv_freq + i)) * 0.31830988618379067154);
-        const float x = static_cast<float>(half_turns - 2.0 * rint(half_turns * 0.5));
-        float s, c;
-        sincospif(x, &s, &c);
-        cs[((i & 7) >> 1) * (kMaxPairs / 4) + (i >> 3) * 2 + (i & 1)] = make_float2(c, s);
-    }
+__device__ __forceinline__ void write_angle(const Params& p, int i, int32_t position, float2* cs) {
+    const double half_turns = static_cast<double>(position) * (static_cast<double>(__ldg(p.inv_freq + i)) * 0.31830988618379067154);
+    const float x = static_cast<float>(half_turns - 2.0 * rint(half_turns * 0.5));
+    float s, c;
+    sincospif(x, &s, &c);
+    cs[((i & 7) >> 1) * (kMaxPairs / 4) + (i >> 3) * 2 + (i & 1)] = make_float2(c, s);
+}
+__device__ __forceinline__ void token_angles(const Params& p, int64_t token, int lane, float2* cs) {
+    for (int i = lane; i < (p.rot >> 1); i += 32) write_angle(p, i, __ldg(p.positions + p.axis[i] * p.pos_stride + token), cs);
     __syncwarp();
 }
 
@@ -108,7 +110,7 @@ struct Bf16 {
             f2_unpack(x[i], lo, hi);
             w[i] = pack_bf16x2(lo, hi);
         }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
     }
 };
 
@@ -211,30 +213,36 @@ __device__ __forceinline__ void stage_weights(const Params& p, float (*w)[D]) {
     __syncthreads();
 }
 
-// Where the append form stores a token: its place in its sequence, and its page's first row for head 0 (-1: nowhere, the page
-// number is none of the pool's).  False: the token is in no sequence, or in one that does not fit.
+// Where the append form stores a token: its place in its sequence, and its page (-1: nowhere, the page number is none of the
+// pool's).  False: the token is in no sequence, or in one that does not fit.
 struct Slot {
-    int32_t place;
-    int64_t row;
+    int32_t place, page;
 };
-__device__ __forceinline__ bool find_slot(const Append& a, int64_t token, int64_t n_tokens, int32_t num_kv_heads, int lane, Slot* slot) {
-    // the last sequence that starts at or before the token, 32 offsets a step: [lo, hi) holds it
+__device__ __forceinline__ bool find_slot(const Append& a, int64_t token, int64_t n_tokens, int lane, Slot* slot) {
+    // the last sequence that starts at or before the token, 32 offsets a step: [lo, hi) holds it.  A lane of the last step has
+    // its sequence's numbers at hand.
     int32_t lo = 0, hi = a.batch;
-    while (hi - lo > 1) {
+    while (hi - lo > 32) {
         const int32_t step = (hi - lo + 31) / 32;
         const int64_t at = lo + static_cast<int64_t>(lane) * step;
         const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(a.cu + at) <= token);
-        const int32_t last = before != 0u ? 31 - __clz(static_cast<int>(before)) : 0;
-        lo += last * step;
+        lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
         hi = hi - lo > step ? lo + step : hi;
     }
-    const int32_t begin = __ldg(a.cu + lo), end = __ldg(a.cu + lo + 1), len = __ldg(a.lens + lo);
+    const int32_t mine = min(lo + lane, hi - 1);
+    int32_t begin = __ldg(a.cu + mine), end = __ldg(a.cu + mine + 1), len = __ldg(a.lens + mine);
+    const uint32_t before = __ballot_sync(0xffffffffu, lo + lane < hi && begin <= token);
+    const int32_t last = before != 0u ? 31 - __clz(static_cast<int>(before)) : 0;
+    lo += last;
+    begin = __shfl_sync(0xffffffffu, begin, last);
+    end = __shfl_sync(0xffffffffu, end, last);
+    len = __shfl_sync(0xffffffffu, len, last);
     if (token < begin || token >= end || begin < 0 || end > n_tokens || end - begin > a.max_append || len < 0) return false;
     const int64_t pos = len + (token - begin);
     if ((static_cast<int64_t>(len) + (end - begin) + kPage - 1) / kPage > a.table_stride) return false;
     const int32_t page = __ldg(a.table + static_cast<int64_t>(lo) * a.table_stride + pos / kPage);
     slot->place = static_cast<int32_t>(pos);
-    slot->row = page >= 0 && page < a.num_blocks ? static_cast<int64_t>(page) * num_kv_heads * kPage + pos % kPage : -1;
+    slot->page = page >= 0 && page < a.num_blocks ? page : -1;
     return true;
 }
 // Offsets, lengths and bounds of all sequences, looked at by one block of the launch.
@@ -255,7 +263,9 @@ __device__ __forceinline__ void check_sequences(const Append& a, int64_t n_token
 // The loads run a batch ahead of the arithmetic, the first batch in front of the angles: a warp always has rows in flight.
 // Units are the rows of q, then of k and, in the append form, of v.
 template <class T, int D, bool kNorm, bool kAppend>
-__global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6 : 4) qk_rope_kernel(const __grid_constant__ Params p) {
+// Six CTAs an SM, the append form with norm five: held to 80 registers it spills (8 x 4096 tokens 123 us for 105; without norm
+// six are the faster, 97 us for 100).
+__global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? (kAppend && kNorm ? 5 : 6) : 4) qk_rope_kernel(const __grid_constant__ Params p) {
     typedef LaneMap<D> Map;
     typedef typename T::Elem Elem;
     constexpr int kUnroll = sizeof(Elem) == 2 ? 2 : 1;  // units of a batch
@@ -285,18 +295,31 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
     };
     load(now, u_begin);
     [[maybe_unused]] Slot slot = {0, -1};
+    [[maybe_unused]] int32_t pos[2] = {0, 0};  // of this lane's pairs; under way during the search
     if constexpr (kAppend) {
+        if (p.positions != nullptr && u_begin < u_end) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane + 32 * i < (p.rot >> 1)) pos[i] = __ldg(p.positions + p.axis[lane + 32 * i] * p.pos_stride + token);
+        }
         if (blockIdx.x == 0) check_sequences(p.append, p.n_tokens);
         if (u_begin < u_end) {
-            if (!find_slot(p.append, token, p.n_tokens, p.num_kv_heads, lane, &slot)) u_end = 0;
-            else if (slot.row < 0 && u_begin == 0 && lane == 0 && p.append.status != nullptr) atomicCAS(p.append.status, 0, RPX_ERR_DEVICE_DATA);
+            if (!find_slot(p.append, token, p.n_tokens, lane, &slot)) u_end = 0;
+            if (p.positions == nullptr) pos[0] = pos[1] = slot.place;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane + 32 * i < (p.rot >> 1)) write_angle(p, lane + 32 * i, pos[i], cs_all[warp]);
+            __syncwarp();
         }
+    } else if (u_begin < u_end) {
+        token_angles(p, token, lane, cs_all[warp]);
     }
-    if (u_begin < u_end) token_angles(p, token, lane, cs_all[warp], slot.place);
     if (kNorm) stage_weights<T, D>(p, weight);
     if (u_begin >= u_end) return;
     uint64_t c[4], s[4];
     if (map.turned) read_angles(cs_all[warp], map.off_a >> 3, c, s);
+    if constexpr (kAppend)  // (here the page number has come)
+        if (slot.page < 0 && u_begin == 0 && lane == 0 && p.append.status != nullptr) atomicCAS(p.append.status, 0, RPX_ERR_DEVICE_DATA);
 
     for (int32_t u0 = u_begin; u0 < u_end; u0 += kUnroll) {
         load(next, u0 + kUnroll);
@@ -335,8 +358,8 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? 6
             }
             if (head < (is_q ? p.num_q_heads : p.num_kv_heads)) {
                 if (kAppend && !is_q) {
-                    if (slot.row >= 0) {
-                        __nv_bfloat16* dst = (is_v ? p.append.v_cache : p.append.k_cache) + (slot.row + static_cast<int64_t>(head) * kPage) * D;
+                    if (slot.page >= 0) {
+                        __nv_bfloat16* dst = (is_v ? p.append.v_cache : p.append.k_cache) + ((static_cast<int64_t>(slot.page) * p.num_kv_heads + head) * kPage + slot.place % kPage) * D;
                         Bf16::keep(dst + map.off_a, a);
                         Bf16::keep(dst + map.off_b, b);
                     }
