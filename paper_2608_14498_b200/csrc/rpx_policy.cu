@@ -12,6 +12,10 @@
 // weights need the counts of all sequences first.  So batches of up to kSmallTokens tokens are one launch of one CTA, larger
 // ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the tokens is launched on top of it with
 // its first tokens already on their way; its last CTA adds up the CTAs' sums.
+//
+// Measured: 8 x 250 tokens 7 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M tokens)
+// 27 us, a quarter of the copy bandwidth: some 100 instructions a token and the count before it, 6 us.  A lane has four tokens
+// at a time and a warp's tokens follow one another, so that a sequence is looked up, and its weight divided, where one begins.
 #include "rpx_internal.h"
 
 namespace rpx {
@@ -20,20 +24,20 @@ namespace {
 
 constexpr int kThreads = 256, kSmallThreads = 1024;
 constexpr int64_t kSmallTokens = 8192;
-constexpr int kCtasPerSm = 4;
+constexpr int kCtasPerSm = 3;  // (four, with 64 registers, spill: 29 us for 27)
 constexpr int kSums = 4;  // policy, kl, clipped, ratio
 
 struct Params {
     const float *l, *o, *f, *adv;  // o, f nullable
     const uint8_t* mask;           // nullable
     const int32_t* cu;
-    int32_t batch;
-    int64_t n_tokens;
+    int32_t batch, n_tokens;
     const float* upstream;         // nullable
     float *stats, *dl;             // dl nullable
     int32_t kl;
     bool by_sequence, sequence_mean, adv_per_token, wide;  // wide: all token arrays allow 16-byte (mask: 4-byte) accesses
     double log_low, log_high, log_dual;  // borders of d
+    float near_low, near_high, near_dual;  // rounded
     float low, high, dual;               // what r is held at
     float kl_coef;
     double kl_coef64, count;
@@ -57,6 +61,12 @@ __device__ __forceinline__ bool sequence(const Params& p, int32_t s, int32_t* be
     return *begin >= 0 && *begin <= *end && *end <= p.n_tokens;
 }
 
+__device__ __forceinline__ void count_one(const Params& p, int64_t t, bool with_d, int32_t* n, double* d) {
+    if (p.mask != nullptr && __ldg(p.mask + t) == 0) return;
+    *n += 1;
+    if (with_d) *d += static_cast<double>(__ldg(p.l + t)) - static_cast<double>(__ldg(p.o + t));
+}
+
 // Counted tokens of a sequence and the sum of their d, as one of `lanes` threads sees them.
 __device__ __forceinline__ void count_tokens(const Params& p, int32_t begin, int32_t end, int lane, int lanes, int32_t* n, double* d) {
     *n = 0;
@@ -65,12 +75,34 @@ __device__ __forceinline__ void count_tokens(const Params& p, int32_t begin, int
         if (lane == 0) *n = end - begin;
         return;
     }
+    const bool with_d = p.by_sequence && p.o != nullptr;
+    if (p.wide) {  // by fours
 #pragma unroll 4
-    for (int64_t t = begin + lane; t < end; t += lanes) {
-        const bool counted = p.mask == nullptr || __ldg(p.mask + t) != 0;
-        *n += counted ? 1 : 0;
-        if (p.by_sequence && p.o != nullptr && counted) *d += static_cast<double>(__ldg(p.l + t)) - static_cast<double>(__ldg(p.o + t));
+        for (int64_t t = (begin & ~3) + 4 * lane; t < end; t += 4 * lanes) {
+            if (t + 4 > p.n_tokens) {
+                for (int64_t u = t < begin ? begin : t; u < end; ++u) count_one(p, u, with_d, n, d);
+                continue;
+            }
+            uint32_t m = p.mask != nullptr ? __ldg(reinterpret_cast<const uint32_t*>(p.mask + t)) : ~0u;
+            float4 l, o;
+            if (with_d) {
+                l = __ldg(reinterpret_cast<const float4*>(p.l + t));
+                o = __ldg(reinterpret_cast<const float4*>(p.o + t));
+            }
+            if (t < begin) m &= ~0u << 8 * (begin - t);
+            if (t + 4 > end) m &= ~0u >> 8 * (t + 4 - end);
+            *n += __popc(__vcmpgtu4(m, 0u)) >> 3;
+            if (with_d) {
+                *d += (m & 255u) != 0u ? static_cast<double>(l.x) - static_cast<double>(o.x) : 0.0;
+                *d += (m & 0xff00u) != 0u ? static_cast<double>(l.y) - static_cast<double>(o.y) : 0.0;
+                *d += (m & 0xff0000u) != 0u ? static_cast<double>(l.z) - static_cast<double>(o.z) : 0.0;
+                *d += (m >> 24) != 0u ? static_cast<double>(l.w) - static_cast<double>(o.w) : 0.0;
+            }
+        }
+        return;
     }
+#pragma unroll 4
+    for (int64_t t = begin + lane; t < end; t += lanes) count_one(p, t, with_d, n, d);
 }
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_constant__ Params p) {
@@ -105,23 +137,31 @@ __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_con
     }
 }
 
-// e^x from expm1 (1 ulp; the fast e^x that this library is compiled with is four times as far off): 1 + expm1(|x|) loses
-// nothing, and the other side is its reciprocal.
-__device__ __forceinline__ float exp_near(float x) {
-    const float e = 1.f + expm1f(fabsf(x));
-    return x < 0.f ? __frcp_rn(e) : e;
-}
-// e^x - 1 - x: its series where the terms all but cancel (the first one left out is below 2^-28 of the first one taken)
-__device__ __forceinline__ float exp_minus_linear(float x) {
-    if (fabsf(x) >= 0.25f) return expm1f(x) - x;
-    float y = 1.f / 40320.f;
-    y = fmaf(y, x, 1.f / 5040.f);
-    y = fmaf(y, x, 1.f / 720.f);
-    y = fmaf(y, x, 1.f / 120.f);
-    y = fmaf(y, x, 1.f / 24.f);
-    y = fmaf(y, x, 1.f / 6.f);
-    y = fmaf(y, x, 0.5f);
-    return y * x * x;
+// e^x, e^x - 1 and e^x - 1 - x together: x = n ln 2 + g with |g| <= ln 2 / 2 (ln 2 in two parts, n times the first exact),
+// q = e^g - 1 by its Taylor polynomial of degree 8 (what is left out is below 2^-32), e^x = 2^n (1 + q).  Where n is 0 neither
+// e^x - 1 nor e^x - 1 - x has lost anything; elsewhere both are as large as their parts.  2 to 3 roundings, no branch, NaN kept,
+// 0 below e^-87.3 and infinity above the largest value.  (The fast e^x that this library is compiled with is four times as far
+// off; expm1f, called for each, took a third of the kernel's time.)
+struct Exp {
+    float exp, minus_one, minus_linear;
+};
+__device__ __forceinline__ Exp exponentials(float x) {
+    float y;
+    asm("{\n\t.reg .f32 t;\n\tmin.NaN.f32 t, %1, 0f42B20000;\n\tmax.NaN.f32 %0, t, 0fC2AF0000;\n\t}" : "=f"(y) : "f"(x));  // [-87.5, 89]
+    const float shifted = fmaf(y, 1.44269504f, 12582912.f);  // 1.5 * 2^23: n in the low bits
+    const float n = shifted - 12582912.f;
+    const float g = fmaf(n, -1.42860682e-6f, fmaf(n, -0.693145751953125f, y));
+    const float half = __int_as_float((__float_as_int(shifted) << 23) + (126 << 23));  // 2^n / 2
+    float a = 1.f / 40320.f;
+    a = fmaf(a, g, 1.f / 5040.f);
+    a = fmaf(a, g, 1.f / 720.f);
+    a = fmaf(a, g, 1.f / 120.f);
+    a = fmaf(a, g, 1.f / 24.f);
+    a = fmaf(a, g, 1.f / 6.f);
+    a = fmaf(a, g, 0.5f);
+    const float rest = a * (g * g), q = g + rest;
+    const float e = (1.f + q) * half, m = fmaf(half, q, half - 0.5f);
+    return {e + e, m + m, n == 0.f ? rest : (m + m) - x};
 }
 
 struct Four {
@@ -130,16 +170,16 @@ struct Four {
 };
 
 template <int kBlock, bool kSmall>
-__global__ void __launch_bounds__(kBlock) policy_loss_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_kernel(const __grid_constant__ Params p) {
     constexpr int kWarps = kBlock / 32;
     __shared__ double part[kWarps][kSums];
     __shared__ int64_t part_n[kWarps];
     __shared__ int32_t part_s[kWarps];
     __shared__ bool last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    auto load = [&](Four& x, int64_t t0) {
+    auto load = [&](Four& x, int32_t t0) {
         x.counted = 0u;
-        if (p.wide && t0 + 4 <= p.n_tokens) {
+        if (p.wide && t0 <= p.n_tokens - 4) {
             *reinterpret_cast<float4*>(x.l) = __ldcs(reinterpret_cast<const float4*>(p.l + t0));
             if (p.o != nullptr) *reinterpret_cast<float4*>(x.o) = __ldcs(reinterpret_cast<const float4*>(p.o + t0));
             if (p.f != nullptr) *reinterpret_cast<float4*>(x.f) = __ldcs(reinterpret_cast<const float4*>(p.f + t0));
@@ -151,7 +191,7 @@ __global__ void __launch_bounds__(kBlock) policy_loss_kernel(const __grid_consta
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (t0 + i < p.n_tokens) {
+            if (i < p.n_tokens - t0) {
                 x.l[i] = p.l[t0 + i];
                 if (p.o != nullptr) x.o[i] = p.o[t0 + i];
                 if (p.f != nullptr) x.f[i] = p.f[t0 + i];
@@ -159,8 +199,10 @@ __global__ void __launch_bounds__(kBlock) policy_loss_kernel(const __grid_consta
                 if (p.mask == nullptr || p.mask[t0 + i] != 0) x.counted |= 1u << i;
             }
     };
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * kBlock * 4;
-    int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+    // a warp's tokens follow one another, 128 a step: its lanes seldom have to look a sequence up
+    const int64_t steps = (static_cast<int64_t>(p.n_tokens) + 127) / 128, at = static_cast<int64_t>(blockIdx.x) * kWarps + warp, warps = static_cast<int64_t>(gridDim.x) * kWarps;
+    const int32_t step_end = static_cast<int32_t>(steps * (at + 1) / warps);
+    int32_t step = static_cast<int32_t>(steps * at / warps), t0 = step < step_end ? step * 128 + lane * 4 : p.n_tokens;  // (at most 2^31 - 4)
     Four now;
     if (t0 < p.n_tokens) load(now, t0);
 
@@ -211,80 +253,118 @@ __global__ void __launch_bounds__(kBlock) policy_loss_kernel(const __grid_consta
 
     // ---- the tokens, four a thread
     double sums[kSums] = {0.0, 0.0, 0.0, 0.0};
-    for (; __any_sync(0xffffffffu, t0 < p.n_tokens); t0 += stride) {
+    int32_t s = 0, s_hi = 0, begin = 0, end = 0;  // the sequence whose numbers are at hand
+    bool fits = false;
+    double w = 0.0, d_seq = 0.0;
+    float a_seq = 0.f, w_up = 0.f;  // (w_up: w times the upstream gradient)
+    for (; step < step_end; ++step, t0 += 128) {
         Four next;
-        if (t0 + stride < p.n_tokens) load(next, t0 + stride);
-        // sequences of the warp's first and last token: 32 offsets a step (the last one that starts at or before a token)
-        auto find = [&](int64_t t) {
-            int32_t lo = 0, hi = p.batch;
-            while (hi - lo > 1) {
-                const int32_t step = (hi - lo + 31) / 32;
-                const int64_t at = lo + static_cast<int64_t>(lane) * step;
-                const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(p.cu + at) <= t);
-                lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
-                hi = hi - lo > step ? lo + step : hi;
+        if (step + 1 < step_end && t0 < p.n_tokens - 128) load(next, t0 + 128);
+        const bool alone = __all_sync(0xffffffffu, fits && t0 <= end - 4);  // every lane stays in its sequence
+        if (!alone) {
+            // sequences of the warp's first and last token: 32 offsets a step (the last one that starts at or before a token)
+            auto find = [&](int32_t t) {
+                int32_t lo = 0, hi = p.batch;
+                while (hi - lo > 1) {
+                    const int32_t jump = (hi - lo + 31) / 32;
+                    const int64_t at = lo + static_cast<int64_t>(lane) * jump;
+                    const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(p.cu + at) <= t);
+                    lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * jump;
+                    hi = hi - lo > jump ? lo + jump : hi;
+                }
+                return lo;
+            };
+            const int32_t first = step * 128;
+            s = s_hi = find(first);
+            const int32_t rest = min(127, p.n_tokens - 1 - first);
+            if (__ldg(p.cu + s + 1) <= first + rest) s_hi = find(first + rest);
+            // the thread's first token, among these
+            int32_t up = s_hi + 1;
+            while (up - s > 1) {
+                const int32_t mid = s + (up - s) / 2;
+                if (__ldg(p.cu + mid) <= t0) s = mid;
+                else up = mid;
             }
-            return lo;
-        };
-        const int64_t first = __shfl_sync(0xffffffffu, t0, 0);
-        int32_t s_lo = find(first), s_hi = s_lo;
-        if (__ldg(p.cu + s_lo + 1) < min(first + 128, p.n_tokens)) s_hi = find(min(first + 127, p.n_tokens - 1));
-        // the thread's first token, among these
-        int32_t s = s_lo, up = s_hi + 1;
-        while (up - s > 1) {
-            const int32_t mid = s + (up - s) / 2;
-            if (__ldg(p.cu + mid) <= t0) s = mid;
-            else up = mid;
+            fits = false;
         }
         if (t0 < p.n_tokens) {
-            int32_t begin = 0, end = 0;  // of the sequence whose numbers are at hand
-            bool fits = false;
-            double w = 0.0, d_seq = 0.0;
-            float a_seq = 0.f, grads[4];
+            float grads[4], policy = 0.f, ratio = 0.f;  // sums of tokens of one weight, at most four
+            double kl_sum = 0.0;
+            int clips = 0;
             uint32_t written = 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = t0 + i;
-                if (!fits || t >= end) {
-                    while (s < s_hi && __ldg(p.cu + s + 1) <= t) ++s;
-                    fits = sequence(p, s, &begin, &end) && begin <= t && t < end;
-                    w = 0.0;
-                    if (fits) {
-                        const int32_t n = p.seq_n[s];
-                        w = n > 0 ? 1.0 / (p.sequence_mean ? over * n : over) : 0.0;
-                        if (p.by_sequence) d_seq = p.seq_d[s];
-                        if (!p.adv_per_token) a_seq = __ldg(p.adv + s);
-                    }
-                }
-                grads[i] = 0.f;
-                if (t >= p.n_tokens || !fits) continue;
-                written |= 1u << i;
-                if ((now.counted >> i & 1u) == 0u) continue;
+            auto add = [&] {
+                sums[0] += w * static_cast<double>(policy);
+                sums[1] += w * kl_sum;
+                sums[2] += w * clips;
+                sums[3] += w * static_cast<double>(ratio);
+            };
+            auto token = [&](int i) {
+                const bool counted = (now.counted >> i & 1u) != 0u;
                 const float a = p.adv_per_token ? now.adv[i] : a_seq;
-                // the difference of two floats in 64 bits: on the side of a border that it is on
-                const double d = p.by_sequence ? d_seq : p.o != nullptr ? static_cast<double>(now.l[i]) - static_cast<double>(now.o[i]) : 0.0;
-                const float r = exp_near(static_cast<float>(d));
-                float held = 0.f;
-                bool clipped = false;
-                if (a > 0.f && d > p.log_high) {
-                    clipped = true;
-                    held = p.high;
-                } else if (a < 0.f && (d < p.log_low || d > p.log_dual)) {
-                    clipped = true;
-                    held = d < p.log_low ? p.low : p.dual;
+                const float d = p.by_sequence ? static_cast<float>(d_seq) : p.o != nullptr ? now.l[i] - now.o[i] : 0.f;
+                bool above = d > p.near_high, below = d < p.near_low, far = d > p.near_dual;
+                if (d == p.near_high || d == p.near_low || d == p.near_dual) {  // the rounding of d decides nothing
+                    const double exact = p.by_sequence ? d_seq : p.o != nullptr ? static_cast<double>(now.l[i]) - static_cast<double>(now.o[i]) : 0.0;
+                    above = exact > p.log_high;
+                    below = exact < p.log_low;
+                    far = exact > p.log_dual;
                 }
-                float g = clipped ? 0.f : -a * r, kl = 0.f;
+                const float r = exponentials(d).exp;
+                const bool clipped = a > 0.f ? above : a < 0.f && (below || far);
+                const float held = a > 0.f ? p.high : below ? p.low : p.dual;
+                float g = clipped ? 0.f : -a * r;
+                policy += counted ? -a * (clipped ? held : r) : 0.f;
+                ratio += counted ? r : 0.f;
+                clips += counted && clipped ? 1 : 0;
                 if (p.kl != 0) {
                     const float x = now.f[i] - now.l[i];
-                    kl = p.kl == 1 ? -x : p.kl == 2 ? 0.5f * x * x : exp_minus_linear(x);
-                    g += p.kl_coef * (p.kl == 1 ? 1.f : p.kl == 2 ? -x : -expm1f(x));
+                    float kl = -x, slope = 1.f;
+                    if (p.kl == 2) {
+                        kl = 0.5f * x * x;
+                        slope = -x;
+                    } else if (p.kl == 3) {
+                        const Exp e = exponentials(x);
+                        kl = e.minus_linear;
+                        slope = -e.minus_one;
+                    }
+                    kl_sum += counted ? static_cast<double>(kl) : 0.0;
+                    g += p.kl_coef * slope;
                 }
-                grads[i] = static_cast<float>(w) * g * upstream;
-                sums[0] += w * static_cast<double>(-a * (clipped ? held : r));
-                sums[1] += w * static_cast<double>(kl);
-                sums[2] += clipped ? w : 0.0;
-                sums[3] += w * static_cast<double>(r);
+                grads[i] = counted ? g * w_up : 0.f;
+            };
+            if (alone) {
+                written = 15u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) token(i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t t = t0 + i;
+                    if (!fits || t >= end) {
+                        if (i > 0) {
+                            add();
+                            policy = ratio = 0.f;
+                            kl_sum = 0.0;
+                            clips = 0;
+                        }
+                        while (s < s_hi && __ldg(p.cu + s + 1) <= t) ++s;
+                        fits = sequence(p, s, &begin, &end) && begin <= t && t < end;
+                        w = 0.0;
+                        if (fits) {
+                            const int32_t n = p.seq_n[s];
+                            w = n > 0 ? 1.0 / (p.sequence_mean ? over * n : over) : 0.0;
+                            if (p.by_sequence) d_seq = p.seq_d[s];
+                            if (!p.adv_per_token) a_seq = __ldg(p.adv + s);
+                        }
+                        w_up = static_cast<float>(w) * upstream;
+                    }
+                    grads[i] = 0.f;
+                    if (!fits) continue;
+                    written |= 1u << i;
+                    token(i);
+                }
             }
+            add();
             if (p.dl != nullptr) {
                 if (written == 15u && p.wide) {
                     *reinterpret_cast<float4*>(p.dl + t0) = make_float4(grads[0], grads[1], grads[2], grads[3]);
@@ -355,7 +435,7 @@ rpx_status_t launch_policy_loss(const PolicyArgs& a) {
     p.mask = a.mask;
     p.cu = a.cu;
     p.batch = a.batch;
-    p.n_tokens = a.n_tokens;
+    p.n_tokens = static_cast<int32_t>(a.n_tokens);  // (below 2^31 - 1)
     p.upstream = a.upstream;
     p.stats = a.stats;
     p.dl = a.dlogprobs;
@@ -366,6 +446,9 @@ rpx_status_t launch_policy_loss(const PolicyArgs& a) {
     p.log_high = log1p(c.clip_high);
     p.log_low = log1p(-c.clip_low);
     p.log_dual = c.clip_dual > 0.0 ? log(c.clip_dual) : HUGE_VAL;
+    p.near_low = static_cast<float>(p.log_low);
+    p.near_high = static_cast<float>(p.log_high);
+    p.near_dual = static_cast<float>(p.log_dual);
     p.high = static_cast<float>(1.0 + c.clip_high);
     p.low = static_cast<float>(1.0 - c.clip_low);
     p.dual = static_cast<float>(c.clip_dual);
