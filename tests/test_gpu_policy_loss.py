@@ -284,3 +284,33 @@ def test_stream_graph_and_two_workspaces(cuda_device):
         want = call(s, coef=0.1)
         graph.replay()
         assert torch.equal(stats, want[0]) and torch.equal(grad, want[1])
+
+
+def test_exponentials_over_their_range(cuda_device):
+    """The ratio and the KL term alone, one token a call's sequence, at differences that float32 holds: 8 e relative for the
+    ratio's gradient (four roundings of its own, three products); e^x - 1 and e^x - 1 - x to 8 e of themselves below 1/4, of their
+    parts above.  Out of range: 0 and infinity."""
+    x = torch.cat([torch.linspace(-80, 88, 4001), torch.linspace(-0.4, 0.4, 2001), 2.0 ** torch.arange(-40, 0), -2.0 ** torch.arange(-40, 0)]).float()
+    n, zero = x.numel(), torch.zeros(x.numel(), device=cuda_device)
+    d = x.to(cuda_device)
+    cu = torch.arange(n + 1, dtype=torch.int32, device=cuda_device)
+    kw = dict(clip_low=1 - 2.0 ** -50, clip_high=0.0, count=1.0)
+    _, dl = rpx.policy_loss(d, zero, -torch.ones(n, device=cuda_device), cu, **kw)
+    e = torch.exp(x.double())
+    held = x < math.log(2.0 ** -50)
+    err, r = (dl.double().cpu() - e).abs(), torch.where(held, 0.0, e)
+    assert bool((dl.cpu()[held] == 0).all()) and bool((err[~held] <= 8 * E * r[~held]).all()), float((err / e)[~held].max() / E)
+    _, dl = rpx.policy_loss(-d, None, zero, cu, ref_logprobs=zero, kl_coef=1.0, kl=3, **kw)
+    want, small = -torch.expm1(x.double()), x.abs() < 0.25
+    err = (dl.double().cpu() - want).abs()
+    assert bool((err <= 8 * E * torch.where(small, want.abs(), e + 1)).all()), float((err / (e + 1)).max() / E)
+    for i in [*range(4001, n, 97), *range(0, 4001, 400)]:
+        stats, _ = rpx.policy_loss(-d[i:i + 1], None, zero[:1], cu[:2], ref_logprobs=zero[:1], kl_coef=0.0, kl=3, want_grad=False, **kw)
+        t = float(x[i])
+        want = t * t / 2 * (1 + t / 3 + t * t / 12 + t ** 3 / 60 + t ** 4 / 360) if abs(t) < 0.01 else math.expm1(t) - t
+        size = abs(want) if abs(t) < 0.25 else math.exp(t) + 1 + abs(t)
+        assert abs(float(stats[2]) - want) <= 8 * E * size + 2.0 ** -126, (t, float(stats[2]), want)
+    far = torch.tensor([89.0, 1e30, math.inf, -200.0, -math.inf, math.nan], device=cuda_device)
+    z = torch.zeros(6, device=cuda_device)
+    _, dl = rpx.policy_loss(-far, None, z, torch.arange(7, dtype=torch.int32, device=cuda_device), ref_logprobs=z, kl_coef=1.0, kl=3, **kw)
+    assert dl.tolist()[:5] == [-math.inf, -math.inf, -math.inf, 1.0, 1.0] and math.isnan(float(dl[5]))

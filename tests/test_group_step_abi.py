@@ -66,6 +66,7 @@ def test_group_refusals(lib):
                 dict(max_group=-1), dict(c=cache(size=8)), dict(c=cache(blocks=2 ** 32)), dict(desc=B.AttnDesc(4, 3, 128, 0.0, 0)),
                 dict(desc=B.AttnDesc(4, 2, 80, 0.0, 0)), dict(desc=B.AttnDesc(258, 2, 64, 0.0, 0)), dict(desc=B.AttnDesc(0, 2, 64, 0.0, 0))):
         assert group(lib, **bad) == -2, bad
+    assert group(lib, desc=B.AttnDesc(226, 2, 128, 0.0, 0)) == -2  # 113 heads a KV head of 128 values
     assert group(lib, desc=B.AttnDesc(4, 2, 128, 0.0, 7)) == -3
     for bad in (dict(qs=516), dict(q=P + 8), dict(out=P + 2), dict(c=cache(k=P + 8))):
         assert group(lib, **bad) == -4, bad
