@@ -481,7 +481,8 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *       shared tokens end in front of every member's first query.  A sequence whose offsets leave the packed tensors or the
  *       table, that has more queries than cached tokens, or more than max_q_len, is reported and its rows are left as they are.
  *   max_q_len, max_group_tokens: upper bounds of a sequence's and of a group's query tokens (a group with more is computed
- *       without sharing, and reported); max_kv_len: upper bound of kv_lens (sizes the grid only)
+ *       without sharing, and reported); max_kv_len: upper bound of kv_lens (>= 0; nothing is
+ *       sized by it, the work is laid out from kv_lens themselves)
  *   num_q_heads / num_kv_heads: at most 112 with head_dim 128, 128 with 64 (RPX_ERR_SHAPE)
  *   workspace: rpx_group_attn_workspace_bytes with the same sizes
  * The same call gives the same bits.  (Where the keys are cut goes by all lengths of the batch, so a sequence's sums may round

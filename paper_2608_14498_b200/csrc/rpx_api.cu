@@ -859,7 +859,6 @@ rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t 
     a.batch = batch;
     a.total_tokens = total_q_tokens;
     a.max_q = max_q_len;
-    a.max_kv = max_kv_len;
     a.cu_groups = cu_groups;
     a.shared_lens = shared_lens;
     a.n_groups = n_groups;

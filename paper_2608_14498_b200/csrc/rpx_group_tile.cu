@@ -22,7 +22,6 @@
 //   4 x 2 or 4 warps : two (up to 16 rows) or four teams with a share of the rows each: softmax, lanes = keys
 //   1 warp each      : producer of K and V (one TMA box per 16-token page); S^T = K Q^T; O^T += V^T P^T; laying Q out
 //   4 warps          : output, lanes = elements of D
-#include <type_traits>
 
 #include "rpx_group.cuh"
 

@@ -248,7 +248,7 @@ struct GroupArgs {
     const int32_t *cu, *kv_lens;         // [batch + 1], [batch]
     int32_t batch;
     int64_t total_tokens;
-    int32_t max_q, max_kv;
+    int32_t max_q;
     const int32_t *cu_groups, *shared_lens;  // [n_groups + 1], [n_groups]
     int32_t n_groups, max_group;
     const rpx_kv_cache_t* cache;
