@@ -13,8 +13,8 @@
 // ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the tokens is launched on top of it with
 // its first tokens already on their way; its last CTA adds up the CTAs' sums.
 //
-// Measured: 8 x 250 tokens 7 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M tokens)
-// 27 us, a quarter of the copy bandwidth: some 100 instructions a token and the count before it, 6 us.  A lane has four tokens
+// Measured: 8 x 250 tokens 6.6 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M
+// tokens) 26 us, 28 % of the copy bandwidth: the chains of some 100 instructions a token; without the count 24.5 us.  A lane has four tokens
 // at a time and a warp's tokens follow one another, so that a sequence is looked up, and its weight divided, where one begins.
 #include "rpx_internal.h"
 
@@ -35,6 +35,7 @@ struct Params {
     const float* upstream;         // nullable
     float *stats, *dl;             // dl nullable
     int32_t kl;
+    int32_t steps, more;           // 128 tokens each: of every warp, and the first warps that have one more
     bool by_sequence, sequence_mean, adv_per_token, wide;  // wide: all token arrays allow 16-byte (mask: 4-byte) accesses
     double log_low, log_high, log_dual;  // borders of d
     float near_low, near_high, near_dual;  // rounded
@@ -200,9 +201,10 @@ __global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_k
             }
     };
     // a warp's tokens follow one another, 128 a step: its lanes seldom have to look a sequence up
-    const int64_t steps = (static_cast<int64_t>(p.n_tokens) + 127) / 128, at = static_cast<int64_t>(blockIdx.x) * kWarps + warp, warps = static_cast<int64_t>(gridDim.x) * kWarps;
-    const int32_t step_end = static_cast<int32_t>(steps * (at + 1) / warps);
-    int32_t step = static_cast<int32_t>(steps * at / warps), t0 = step < step_end ? step * 128 + lane * 4 : p.n_tokens;  // (at most 2^31 - 4)
+    const int32_t at = static_cast<int32_t>(blockIdx.x) * kWarps + warp;
+    int32_t step = p.steps * at + min(at, p.more);
+    const int32_t step_end = step + p.steps + (at < p.more ? 1 : 0);
+    int32_t t0 = step < step_end ? step * 128 + lane * 4 : p.n_tokens;  // (at most 2^31 - 4)
     Four now;
     if (t0 < p.n_tokens) load(now, t0);
 
@@ -468,7 +470,13 @@ rpx_status_t launch_policy_loss(const PolicyArgs& a) {
     ws += kMaxCtas * kSums * sizeof(double);
     p.ticket = reinterpret_cast<uint32_t*>(ws);
     p.status = a.device_status;
+    auto share_out = [&](int64_t warps) {
+        const int64_t steps = (a.n_tokens + 127) / 128;
+        p.steps = static_cast<int32_t>(steps / warps);
+        p.more = static_cast<int32_t>(steps % warps);
+    };
     if (a.n_tokens <= kSmallTokens) {
+        share_out(kSmallThreads / 32);
         policy_loss_kernel<kSmallThreads, true><<<1, kSmallThreads, 0, a.stream>>>(p);
         return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;
     }
@@ -480,6 +488,7 @@ rpx_status_t launch_policy_loss(const PolicyArgs& a) {
     int64_t ctas = (a.n_tokens + kThreads * 4 - 1) / (kThreads * 4);
     const int64_t cap = sms * kCtasPerSm < kMaxCtas ? sms * kCtasPerSm : kMaxCtas;
     if (ctas > cap) ctas = cap;
+    share_out(ctas * (kThreads / 32));
     return launch_on_top(policy_loss_kernel<kThreads, false>, static_cast<unsigned>(ctas), kThreads, 0, a.stream, p);
 }
 
