@@ -344,12 +344,14 @@ def _desc(q, k, softmax_scale: float) -> AttnDesc:
 def _cache_struct(cache) -> KvCache:
     k_cache, v_cache, block_table = cache
     torch = _torch()
-    if k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16 or block_table.dtype != torch.int32:
+    bf16 = torch.bfloat16
+    if k_cache.dtype != bf16 or v_cache.dtype != bf16 or block_table.dtype != torch.int32:
         raise TypeError("cache pools are bfloat16 and the block table is int32")
-    if not (k_cache.is_contiguous() and v_cache.is_contiguous()) or block_table.stride(1) != 1:
+    row_stride, col_stride = block_table.stride()
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()) or col_stride != 1:
         raise ValueError("cache pools must be contiguous [blocks, kv_heads, 16, head_dim]")
-    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[0], k_cache.shape[2],
-                   block_table.data_ptr(), block_table.stride(0))
+    shape = k_cache.shape
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), shape[0], shape[2], block_table.data_ptr(), row_stride)
 
 
 def prefix_attn_workspace_bytes(num_q_heads, num_kv_heads, head_dim, dtype_code, total_tokens) -> int:
@@ -868,7 +870,7 @@ def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) ->
     if positions is not None:
         pos_shape = positions.shape
         axes = pos_shape[0] if len(pos_shape) == 2 else 1
-        if len(pos_shape) not in (1, 2) or pos_shape[-1] != n or (n > 1 and positions.stride(-1) != 1):
+        if len(pos_shape) not in (1, 2) or pos_shape[-1] != n or (n > 1 and positions.stride()[-1] != 1):
             raise ValueError("positions are [tokens] or [axes, tokens] with contiguous tokens")
     if inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq is a contiguous [rot_dim / 2] tensor")
@@ -876,21 +878,23 @@ def _rope_desc(q, k, positions, inv_freq, q_weight, k_weight, pair_axis, eps) ->
         if w is not None:
             if w.dtype != dtype:
                 raise TypeError("q, k and the norm weights must share an element type")
-            if w.dim() != 1 or w.shape[0] != d or not w.is_contiguous():
+            if w.dim() != 1 or w.numel() != d or not w.is_contiguous():
                 raise ValueError("norm weights are contiguous [head_dim] tensors")
-    pairs = inv_freq.shape[0]
+    pairs = inv_freq.numel()
     if pair_axis is not None:
         pair_axis = _axis_bytes(pair_axis, pairs)
     return RopeDesc(hq, k_shape[1], d, 2 * pairs, axes, pair_axis, eps, code)
 
 
 def _axis_stride(positions) -> int:
-    return positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else positions.shape[-1]
+    shape = positions.shape
+    return positions.stride()[0] if len(shape) == 2 and shape[0] > 1 else shape[-1]
 
 
 def _rope_out(given, like):
     if given is None:
-        return _torch().empty_like(like, memory_format=_torch().contiguous_format)
+        torch = _torch()
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     if given.shape != like.shape or given.dtype != like.dtype:
         raise ValueError("an output has the shape and element type of its input")
     return given
@@ -927,8 +931,8 @@ def qk_norm_rope_append(q, k, v, positions, inv_freq, cu_append, cached_lens, ma
     lib = load_library()
     _one_device(q, k, v, positions, inv_freq, cu_append, cached_lens, *cache, q_weight, k_weight, q_out, device_status)
     cs = _cache_struct(cache)
-    shape = k.shape
-    if len(shape) != 3 or v.shape != shape or v.dtype != k.dtype or cache[0].shape[1:] != (shape[1], BLOCK_SIZE, shape[2]) or cache[1].shape != cache[0].shape:
+    shape, pool = k.shape, cache[0].shape
+    if len(shape) != 3 or v.shape != shape or v.dtype != k.dtype or len(pool) != 4 or pool != (pool[0], shape[1], BLOCK_SIZE, shape[2]) or cache[1].shape != pool:
         raise ValueError("k and v are [tokens, kv_heads, head_dim] tensors that fit the cache pools")
     if positions is None:
         if pair_axis is not None:
