@@ -314,3 +314,15 @@ def test_exponentials_over_their_range(cuda_device):
     z = torch.zeros(6, device=cuda_device)
     _, dl = rpx.policy_loss(-far, None, z, torch.arange(7, dtype=torch.int32, device=cuda_device), ref_logprobs=z, kl_coef=1.0, kl=3, **kw)
     assert dl.tolist()[:5] == [-math.inf, -math.inf, -math.inf, 1.0, 1.0] and math.isnan(float(dl[5]))
+
+
+@pytest.mark.parametrize("batch", [31, 33, 1024, 1025, 5000])
+@pytest.mark.parametrize("ratio,per_token", [("token", True), ("sequence", False)])
+def test_sequences_that_end_inside_a_lanes_tokens(cuda_device, batch, ratio, per_token):
+    """Lengths of 0 to 9 and a few long ones: weights change inside a lane's four tokens and inside a warp's."""
+    gen = np.random.default_rng(batch)
+    lens = gen.integers(0, 10, batch)
+    lens[:: 29] = 400
+    s = make(lens.tolist(), cuda_device, seed=batch, mask=0.7, per_token=per_token)
+    kw = dict(ratio=ratio, mean="sequences", kl=3, coef=0.05, dual=3.0)
+    check(s, call(s, **kw), **kw)

@@ -216,3 +216,19 @@ def test_empty_calls(cuda_device):
     call(s, max_append=0)
     call(s, cu_append=torch.zeros(1, dtype=torch.int32, device=cuda_device), cached_lens=torch.zeros(0, dtype=torch.int32, device=cuda_device))
     assert torch.equal(s["kc"], kc0) and int(s["status"]) == 0
+
+
+@pytest.mark.parametrize("batch", [31, 32, 33, 63, 64, 65, 1023, 1024, 1025, 4000])
+@pytest.mark.parametrize("norm", [True, False])
+def test_any_number_of_sequences(cuda_device, batch, norm):
+    """Which sequence a token is in, some of them empty: as cache_append finds it."""
+    gen = np.random.default_rng(batch)
+    new = gen.integers(0, 4, batch).tolist()
+    new[0], new[-1] = (0, 2) if batch % 2 else (1, 0)
+    s = make(new, gen.integers(0, 40, batch).tolist(), 4, 2, 64, 64, 2, "bf16", norm, cuda_device)
+    q_two, k_two = rpx.qk_norm_rope(s["q"], s["k"], s["pos"], s["inv"], q_weight=s["w"][0], k_weight=s["w"][1], pair_axis=s["axis"], eps=1e-6)
+    kc, vc = s["kc"].clone(), s["vc"].clone()
+    rpx.cache_append(k_two, s["v"].contiguous(), s["cu"], s["lens"], s["max_new"], (kc, vc, s["table"]))
+    q = call(s)
+    assert int(s["status"]) == 0
+    assert torch.equal(q, q_two) and torch.equal(s["kc"], kc) and torch.equal(s["vc"], vc)
