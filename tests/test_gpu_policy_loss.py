@@ -2,8 +2,8 @@
 
 Tolerances, with e = 2^-24.  A ratio: d rounded once (|d| e), expm1 (2 e), the sum and the reciprocal (2 e); its product with
 the advantage and with the weight, itself rounded, and with upstream: (|d| + 8) e relative.  A KL term: f - l rounded once moves
-e^x by |x| e^x e, expm1 2 e of itself, series or difference 4 e of |x| e^|x|; coefficient and products 4 e.  The sums are of
-64-bit products of such terms, and rounded once (e).
+e^x by |x| e^x e, expm1 2 e of itself, series or difference 4 e of |x| e^|x|; coefficient and products 4 e.  The sums of
+ratios and of policy terms are by fours in float32 (3 e, of the 8), and all of them in 64 bits beyond, rounded once (e).
 """
 import math
 
