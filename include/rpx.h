@@ -483,10 +483,11 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *   max_q_len, max_group_tokens: upper bounds of a sequence's and of a group's query tokens (a group with more is computed
  *       without sharing, and reported); max_kv_len: upper bound of kv_lens (>= 0; nothing is
  *       sized by it, the work is laid out from kv_lens themselves)
- *   num_q_heads / num_kv_heads: at most 112 with head_dim 128, 128 with 64 (RPX_ERR_SHAPE)
+ *   num_q_heads / num_kv_heads: at most 112 with head_dim 128, 128 with 64 (RPX_ERR_SHAPE); more than 64 go over the keys twice
  *   workspace: rpx_group_attn_workspace_bytes with the same sizes
  * The same call gives the same bits.  (Where the keys are cut goes by all lengths of the batch, so a sequence's sums may round
- * otherwise beside other sequences.)  RPX_BF16: scores, maxima, sums and outputs are float32 until the output's rounding.
+ * otherwise beside other sequences.)  RPX_BF16: scores, maxima, sums and outputs are float32 until the output's rounding;
+ * probabilities enter the product with V as two bf16 terms (off by 2^-17), whatever the group.
  * RPX_F32 (for checking; a warp per row, nothing is shared): q, out and all products float32, K and V the cache's bf16.
  */
 RPX_API rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t q_tok_stride, const int32_t* cu_seqlens_q,

@@ -822,7 +822,7 @@ rpx_status_t rpx_policy_loss(const rpx_policy_desc_t* desc, const float* logprob
 size_t rpx_group_attn_workspace_bytes(const rpx_attn_desc_t* desc, int64_t total_q_tokens, int32_t batch, int32_t n_groups,
                                       int32_t max_q_len, int32_t max_group_tokens) {
     // (the query may come before the call that refuses the descriptor)
-    if (check_attn_desc(desc) != RPX_OK || desc->num_q_heads / desc->num_kv_heads > group_most_rows(desc->head_dim) || total_q_tokens <= 0 || batch <= 0 ||
+    if (check_attn_desc(desc) != RPX_OK || desc->num_q_heads / desc->num_kv_heads > group_most_heads(desc->head_dim) || total_q_tokens <= 0 || batch <= 0 ||
         n_groups < 0 || max_q_len <= 0 || max_group_tokens < 0)
         return 0;
     return align_up(group_workspace(desc, total_q_tokens, batch, n_groups, max_q_len, max_group_tokens), kWsAlign);
@@ -834,7 +834,7 @@ rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t 
                             const rpx_kv_cache_t* cache, void* out, float* lse, void* workspace, size_t workspace_bytes,
                             int32_t* device_status, void* cuda_stream) {
     if (rpx_status_t rc = check_attn_desc(desc)) return rc;
-    if (desc->num_q_heads / desc->num_kv_heads > group_most_rows(desc->head_dim)) return RPX_ERR_SHAPE;
+    if (desc->num_q_heads / desc->num_kv_heads > group_most_heads(desc->head_dim)) return RPX_ERR_SHAPE;
     if (batch < 0 || total_q_tokens < 0 || total_q_tokens >= INT32_MAX || max_q_len < 0 || max_kv_len < 0 || n_groups < 0 ||
         max_group_tokens < 0)
         return RPX_ERR_SHAPE;

@@ -5,6 +5,8 @@
 //     out = sum_{j <= len - n + i} softmax_j(scale * q . k_j) v_j
 // The keys of a group's shared pages and those of the sequence itself are summed apart, each with its own maximum m and sum l,
 // and joined: with M = max m,  l = sum l_i 2^(m_i - M),  out = sum o_i 2^(m_i - M) / l.
+#include <algorithm>
+
 #include "rpx_group.cuh"
 
 namespace rpx {
@@ -25,21 +27,18 @@ constexpr int kPlanThreads = 1024;
 // (its rows go out one after the other).
 constexpr int kWorkUnits = 48, kRowsAUnit = 8, kSegmentWork = 100;
 
-__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t cap, int32_t group = -1) {
+__device__ __forceinline__ Entry make_entry(const Params& p, int32_t tok0, int32_t n, int32_t len, int32_t row, int32_t page0, int32_t group = -1) {
     Entry e = {tok0, n, len, row, page0, 1, 1, 1, 0, group, len / kTile + (len % kTile != 0 ? 1 : 0)};
     if (n == 0 || len == 0) {
         e.n = e.len = 0;
         return e;
     }
-    // Blocks of at most `cap` rows; of at most 64 where the keys are few, so that probabilities keep their second term: over
-    // many keys the rounding averages out.
-    const int32_t rows = e.tiles <= 2 && cap > 64 ? 64 : cap, per = max(1, rows / p.group);  // (at most cap / group: Q's box)
+    const int32_t per = p.cap / p.group;  // (at least one token, and no more than Q's box holds)
     e.blocks = n <= per ? 1 : (n + per - 1) / per;
     e.block_tokens = e.blocks == 1 ? n : (n + e.blocks - 1) / e.blocks;
-    // A tile's bytes are tile_units of this SM's share of HBM, once for all blocks (on a line of their own, sequences do not meet all
-    // SMs there); the work against a block overlaps with that, what a segment costs besides does not quite.
-    const int32_t bytes = (p.lines == 2 && cap == p.cap[1] ? p.tile_units * 2 / 3 : p.tile_units) / e.blocks;
-    const int32_t block_rows = e.block_tokens * p.group;
+    // A tile's bytes are tile_units of this SM's share of HBM, once for all blocks; the work against a block overlaps with that, what
+    // a segment costs besides does not quite.
+    const int32_t bytes = p.tile_units / e.blocks, block_rows = e.block_tokens * p.group;
     e.weight = max(bytes, kWorkUnits + block_rows / kRowsAUnit) + min(2 * block_rows, kSegmentWork) / e.tiles;
     return e;
 }
@@ -112,24 +111,16 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* sums, int64_t* 
     return __shfl_sync(0xffffffffu, upto - w, warp) + sum;
 }
 
-// The cut, and every CTA's start.  Two lines get CTAs by what they cost.
+// The cut, and every CTA's start.
 template <class Unit0>
-__device__ __forceinline__ void leave_starts(const Params& p, int64_t line1, int64_t total, Unit0 unit0) {
+__device__ __forceinline__ void leave_starts(const Params& p, int64_t total, Unit0 unit0) {
     const int32_t i = threadIdx.x;
     if (i >= p.ctas) return;
-    int32_t first = p.ctas;  // CTAs of the first line
-    if (p.lines == 2) {
-        first = static_cast<int32_t>(static_cast<double>(line1) / static_cast<double>(max(total, static_cast<int64_t>(1))) * p.ctas + 0.5);
-        first = min(max(first, line1 > 0 ? 1 : 0), p.ctas - (line1 < total ? 1 : 0));
-    }
-    const int32_t line = i < first ? 0 : 1, ctas = line == 0 ? first : p.ctas - first;
-    const int64_t units = p.lines == 1 ? total : line == 0 ? line1 : total - line1, size = piece_units(units, ctas);
-    p.starts[i] = find_start(p, line, line == 0 ? 0 : line1, units, size, line == 0 ? i : i - first, unit0);
-    if (i == 0 || i == first) {
-        p.cut->ctas[line] = ctas;
-        p.cut->size[line] = size;
-        p.cut->inverse[line] = 1.0 / static_cast<double>(size);
-        if (ctas == p.ctas) p.cut->ctas[1 - line] = 0;
+    const int64_t size = piece_units(total, p.ctas);
+    p.starts[i] = find_start(p, total, size, i, unit0);
+    if (i == 0) {
+        p.cut->size = size;
+        p.cut->inverse = 1.0 / static_cast<double>(size);
     }
 }
 
@@ -169,23 +160,19 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_small_kernel(const __
         const int32_t n = fits ? cu[last] - cu[first] : 0;
         shared = shared_tokens(p, fits, n, shared, books.members[g]);
         books.shared[g] = shared;
-        e = make_entry(p, shared > 0 ? cu[first] : 0, shared > 0 ? n : 0, shared, books.row[g], 0, p.cap[0]);
+        e = make_entry(p, shared > 0 ? cu[first] : 0, shared > 0 ? n : 0, shared, books.row[g], 0);
     }
     __syncthreads();
     if (is_seq) {
         shared = member ? books.shared[of] : 0;
-        e = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, p.cap[p.lines - 1], shared > 0 ? of : -1);
+        e = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, shared > 0 ? of : -1);
     }
     const int64_t units = entry_units(p, e);
     int64_t total;
-    const int64_t first_unit = block_sum(units, sums, &total) - units;
-    unit0[threadIdx.x] = first_unit;
-    __syncthreads();
-    const int64_t line1 = p.lines == 2 ? (p.n_groups < kPlanThreads ? unit0[p.n_groups] : total) : 0;  // where the second line starts
-    e.unit0 = first_unit - (is_group ? 0 : line1);
+    e.unit0 = unit0[threadIdx.x] = block_sum(units, sums, &total) - units;
     if (g < count) p.entries[g] = e;
     __syncthreads();
-    leave_starts(p, line1, total, [&](int32_t i) { return unit0[i]; });
+    leave_starts(p, total, [&](int32_t i) { return unit0[i]; });
 }
 
 // Any number: every sequence gets its entry as if it were alone; groups that share are then given theirs, kPlanThreads at a time,
@@ -199,7 +186,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     for (int32_t s = threadIdx.x; s < p.batch; s += kPlanThreads) {
         Seq q;
         if (!read_seq(p, s, &q)) report(p.status);
-        p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0, p.cap[p.lines - 1]);
+        p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0);
     }
     const bool ascend = __syncthreads_and(good) != 0;
     for (int32_t g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
@@ -223,7 +210,7 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
             const int32_t tok0 = fits ? __ldg(p.cu + first) : 0, n = fits ? __ldg(p.cu + last) - tok0 : 0;
             shared = shared_tokens(p, fits, n, shared, books.members[threadIdx.x]);
             books.shared[threadIdx.x] = shared;
-            p.entries[g] = make_entry(p, tok0, shared > 0 ? n : 0, shared, books.row[threadIdx.x], 0, p.cap[0]);
+            p.entries[g] = make_entry(p, tok0, shared > 0 ? n : 0, shared, books.row[threadIdx.x], 0);
         }
         __syncthreads();
         for (int32_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
@@ -231,30 +218,22 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
             if (shared == 0) continue;
             Seq q;
             read_seq(p, s, &q);
-            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, p.cap[p.lines - 1], g0 + i);
+            p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.n > 0 ? q.len - shared : 0, s, shared / kPage, g0 + i);
         }
         __syncthreads();
     }
     const int32_t count = p.n_groups + p.batch;
-    __shared__ int64_t line1;
     int64_t carry = 0;
-    if (threadIdx.x == 0) line1 = 0;
     for (int32_t base = 0; base < count; base += kPlanThreads) {
         const int32_t e = base + threadIdx.x;
         const int64_t x = e < count ? entry_units(p, p.entries[e]) : 0;
         int64_t total;
         const int64_t upto = carry + block_sum(x, sums, &total);
         if (e < count) p.entries[e].unit0 = upto - x;
-        if (p.lines == 2 && e == p.n_groups) line1 = upto - x;
         carry += total;
     }
     __syncthreads();
-    leave_starts(p, line1, carry, [&](int32_t i) { return p.entries[i].unit0; });
-    if (p.lines == 2) {
-        __syncthreads();
-        for (int32_t e = p.n_groups + threadIdx.x; e < count; e += kPlanThreads) p.entries[e].unit0 -= line1;
-        // (the starts keep an entry's first unit too, but nobody reads it there)
-    }
+    leave_starts(p, carry, [&](int32_t i) { return p.entries[i].unit0; });
 }
 
 // ------------------------------------------------------------------ the join
@@ -269,17 +248,17 @@ struct Sets {
     int64_t first;
     int32_t step, n;
 };
-__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int32_t line, int32_t kv_head, int32_t in_group, int32_t in) {
-    const int64_t size = p.cut->size[line];
-    const double inverse = p.cut->inverse[line];
+__device__ __forceinline__ Sets find_sets(const Params& p, const Entry& q, int32_t kv_head, int32_t in_group, int32_t in) {
+    const int64_t size = p.cut->size;
+    const double inverse = p.cut->inverse;
     const int32_t block = q.blocks == 1 ? 0 : in / q.block_tokens;
     const int64_t unit = q.unit0 + (static_cast<int64_t>(kv_head) * q.blocks + block) * q.segment_units() + kSegment;
     const int32_t c0 = piece_of(unit, size, inverse);
     Sets r;
     r.n = piece_of(unit + static_cast<int64_t>(q.tiles - 1) * q.weight, size, inverse) - c0 + 1;
     // a piece keeps the segment it starts in the middle of in its first slot, the one it breaks off in its second
-    r.step = p.cap[line];
-    r.first = p.slot0(line) + (static_cast<int64_t>(c0) * 2 + 1) * r.step + (in - block * q.block_tokens) * p.group + in_group;
+    r.step = p.cap;
+    r.first = (static_cast<int64_t>(c0) * 2 + 1) * r.step + (in - block * q.block_tokens) * p.group + in_group;
     return r;
 }
 
@@ -297,12 +276,12 @@ __global__ void __launch_bounds__(kJoinWarps * 32, 5) group_join_kernel(const __
     if (!there) return;
     const Entry own = p.entries[p.n_groups + s];
     if (token < own.tok0 || token - own.tok0 >= own.n) return;  // in no sequence, or in one that does not fit
-    const int64_t out_row = token * p.num_q_heads + kv_head * p.group + in_group;
-    Sets of_own = find_sets(p, own, p.lines - 1, kv_head, in_group, static_cast<int32_t>(token - own.tok0)), of_group = {0, 0, 0};
+    const int64_t out_row = token * p.num_q_heads + kv_head * p.step + in_group;
+    Sets of_own = find_sets(p, own, kv_head, in_group, static_cast<int32_t>(token - own.tok0)), of_group = {0, 0, 0};
     if (own.group < 0 && of_own.n == 1) return;  // written whole
     if (own.group >= 0) {
         const Entry g = p.entries[own.group];
-        of_group = find_sets(p, g, 0, kv_head, in_group, static_cast<int32_t>(token - g.tok0));
+        of_group = find_sets(p, g, kv_head, in_group, static_cast<int32_t>(token - g.tok0));
     }
     float top = -CUDART_INF_F, sum = 0.f, acc[kCols];
 #pragma unroll
@@ -398,7 +377,7 @@ rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
 template <int D>
 rpx_status_t launch_join(const Params& p, cudaStream_t stream) {
     // while a block a row is at most one wave of blocks
-    return p.total_tokens * p.num_q_heads <= 148 * 5 ? launch_join<D, kJoinWarps>(p, stream) : launch_join<D, 1>(p, stream);
+    return p.total_tokens * p.num_kv_heads * p.group <= 148 * 5 ? launch_join<D, kJoinWarps>(p, stream) : launch_join<D, 1>(p, stream);
 }
 
 // ------------------------------------------------------------------ float32
@@ -509,18 +488,16 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     if (p.lse != nullptr && lane == 0) p.lse[row] = (top + log2f(l)) * kLn2;
 }
 
-// Rows per block: the smallest of 16, 32, 64 and the most that a form takes that holds so many tokens' rows of one KV head.
-int32_t cap_of(int32_t tokens, int32_t group, int32_t head_dim) {
-    const int64_t rows = static_cast<int64_t>(tokens) * group;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : group_most_rows(head_dim);
+// A KV head's query heads are taken in as few equal parts as a block has rows for, one after the other: more than 64 are rare.
+int32_t part_heads(int32_t step) {
+    const int32_t parts = (step + kMostRows - 1) / kMostRows;
+    return (step + parts - 1) / parts;
 }
-// One line, or where groups need the largest form and single sequences do not, a line each: that form's rings are short, and
-// small segments take it 4900 clocks a tile against 2500 (4 x 64 sequences with 500 tokens of their own: 180 us in one line).
-void choose_lines(Params& p, int32_t head_dim) {
-    const int32_t seq = cap_of(p.max_q, p.group, head_dim), group = p.n_groups > 0 && p.max_group > p.max_q ? cap_of(p.max_group, p.group, head_dim) : seq;
-    p.lines = group > 64 && seq <= 64 ? 2 : 1;
-    p.cap[0] = group;
-    p.cap[1] = seq;
+// Rows per block: the smallest of 16, 32 and 64 that holds the rows of a KV head of the longest sequence and the largest group, or
+// 64, and such blocks side by side.
+int32_t choose_cap(const Params& p) {
+    const int64_t rows = static_cast<int64_t>(p.n_groups > 0 ? std::max(p.max_q, p.max_group) : p.max_q) * part_heads(p.step);
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : kMostRows;
 }
 constexpr int kMaxCtas = 148;
 
@@ -533,7 +510,7 @@ size_t carve(Params& p, int32_t head_dim, void* workspace) {
         at += align_up(bytes, 256);
         return r;
     };
-    const size_t rows = static_cast<size_t>(p.total_tokens) * p.num_q_heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * (p.cap[0] + (p.lines == 2 ? p.cap[1] : 0));
+    const size_t rows = static_cast<size_t>(p.total_tokens) * p.num_q_heads * 2, slots = static_cast<size_t>(kMaxCtas) * 2 * p.cap;
     p.entries = reinterpret_cast<Entry*>(take((static_cast<size_t>(p.n_groups) + p.batch) * sizeof(Entry)));
     p.cut = reinterpret_cast<Cut*>(take(sizeof(Cut)));
     p.starts = reinterpret_cast<Start*>(take(kMaxCtas * sizeof(Start)));
@@ -546,7 +523,7 @@ size_t carve(Params& p, int32_t head_dim, void* workspace) {
 
 }  // namespace
 
-int32_t group_most_rows(int32_t head_dim) { return head_dim == 128 ? 112 : 128; }
+int32_t group_most_heads(int32_t head_dim) { return head_dim == 128 ? 112 : 128; }
 
 size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t n_groups, int32_t max_q, int32_t max_group) {
     if (d->dtype == RPX_F32 || batch > INT32_MAX - n_groups - 1) return 0;
@@ -557,8 +534,8 @@ size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, 
     p.max_q = max_q;
     p.max_group = max_group;
     p.num_q_heads = d->num_q_heads;
-    p.group = d->num_q_heads / d->num_kv_heads;
-    choose_lines(p, d->head_dim);
+    p.step = d->num_q_heads / d->num_kv_heads;
+    p.cap = choose_cap(p);
     return carve(p, d->head_dim, nullptr);
 }
 
@@ -579,16 +556,24 @@ rpx_status_t launch_group_attn(const GroupArgs& a) {
     }
     const int sms = sm_count();
     if (sms <= 0) return RPX_ERR_CUDA;
-    choose_lines(p, a.head_dim);
+    p.cap = choose_cap(p);
     p.tile_units = a.head_dim == 128 ? 75 : 38;  // 64 KB or 32 at 6.5 TB/s over 148 SMs
     // (without the SM budget: where the line of tiles is cut decides the order of the sums)
     p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
     carve(p, a.head_dim, a.workspace);
-    if (a.n_groups + a.batch <= kPlanThreads) group_plan_small_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
-    else group_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
-    if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
-    if (rpx_status_t rc = launch_group_tile(p, a.head_dim, *a.cache, a.stream)) return rc;
-    return a.head_dim == 128 ? launch_join<128>(p, a.stream) : launch_join<64>(p, a.stream);
+    for (int32_t head = 0; head < p.step; head += part_heads(p.step)) {
+        p.group = std::min(part_heads(p.step), p.step - head);
+        p.group_magic = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
+        p.q = static_cast<const __nv_bfloat16*>(a.q) + static_cast<int64_t>(head) * a.head_dim;
+        p.out = static_cast<__nv_bfloat16*>(a.out) + static_cast<int64_t>(head) * a.head_dim;
+        p.lse = a.lse != nullptr ? a.lse + head : nullptr;
+        if (a.n_groups + a.batch <= kPlanThreads) group_plan_small_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
+        else group_plan_kernel<<<1, kPlanThreads, 0, a.stream>>>(p);
+        if (cudaGetLastError() != cudaSuccess) return RPX_ERR_CUDA;
+        if (rpx_status_t rc = launch_group_tile(p, a.head_dim, *a.cache, a.stream)) return rc;
+        if (rpx_status_t rc = a.head_dim == 128 ? launch_join<128>(p, a.stream) : launch_join<64>(p, a.stream)) return rc;
+    }
+    return RPX_OK;
 }
 
 }  // namespace rpx

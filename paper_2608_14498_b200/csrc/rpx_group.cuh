@@ -2,10 +2,9 @@
 //
 // All key tiles of all segments lie in a line: first the groups' shared pages (an entry per group), then every sequence's own
 // keys (an entry per sequence).  A segment is one KV head of an entry and one block of its rows (row = token * group + head
-// within the KV head's group).  The line is cut into equal pieces, one per CTA; where groups have more rows than one
-// kernel form does well beside single sequences, the two parts are a line each, for CTAs of two forms side by side in one launch.  A segment that lies in one piece leaves its
-// rows' (maximum in log2 units, sum) and un-normalised outputs in the rows' own place in the workspace (or, where its sequence
-// shares nothing, the result in `out`), a segment that is cut one set per piece; the join adds them up in the order of the keys.
+// within the KV head's group).  The line is cut into equal pieces, one per CTA.  A segment that lies in one piece leaves its rows' (maximum in log2 units, sum) and
+// un-normalised outputs in the rows' own place in the workspace (or, where its sequence shares nothing, the result in `out`), a
+// segment that is cut one set per piece; the join adds them up in the order of the keys.
 // The cut goes by lengths alone, so the same call gives the same bits.
 #pragma once
 
@@ -20,6 +19,7 @@ namespace group {
 
 constexpr int kPage = 16;
 constexpr int kTile = 128;  // keys of a tile
+constexpr int kMostRows = 64;  // of a block
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -33,7 +33,7 @@ struct __align__(16) Entry {
     int32_t row, page0;     // the table row that names the keys' pages, and the first of them
     int32_t blocks, block_tokens;  // row blocks, and the tokens of each but the last
     int32_t weight;         // units of a key tile against one block
-    int64_t unit0;          // its first unit, counted from the start of its line
+    int64_t unit0;          // its first unit, counted from the start of the line
     int32_t group;          // of a sequence: the group whose shared pages it reads as well, or -1
     int32_t tiles;          // key tiles
     __device__ __forceinline__ int64_t segment_units() const { return static_cast<int64_t>(tiles) * weight + kSegment; }
@@ -57,7 +57,8 @@ struct Params {
     int32_t max_q, max_group;
     const int32_t *cu_groups, *shared;
     int32_t n_groups;
-    int32_t num_q_heads, num_kv_heads, group;
+    int32_t num_q_heads, num_kv_heads, step;  // step: query heads to a KV head
+    int32_t group;         // those of them that this pass takes: all, or a part (q, out and lse begin with its first)
     uint32_t group_magic;  // 2^32 / group, rounded up: row / group for rows below 2^16 (group 1: 0)
     const int32_t* block_table;
     int32_t block_table_stride, num_blocks;
@@ -68,18 +69,15 @@ struct Params {
     int32_t* status;
     // bf16 only
     int32_t tile_units;    // of a tile's bytes
-    int32_t ctas;          // pieces of a line at most
-    int32_t lines;         // 1: groups and sequences are one line; 2: a line each
-    int32_t cap[2];        // rows per block at most, of each line
+    int32_t ctas;          // pieces of the line at most
+    int32_t cap;           // rows per block at most
     Entry* entries;        // workspace [n_groups + batch]
-    struct Start* starts;  // workspace [ctas]: those of the first line's pieces, then the second's
+    struct Start* starts;  // workspace [ctas]
     struct Cut* cut;       // workspace
     float2* whole_ml;      // workspace [2][total_tokens][H_q]: of segments that are not cut: shared, own
     float* whole_o;        // workspace [2][total_tokens][H_q][D]
-    float2* part_ml;       // workspace [ctas][2][cap of the first line], [ctas][2][cap of the second]: of segments that are
-    float* part_o;         // workspace, rows as those, [D]
-    __host__ __device__ __forceinline__ int32_t line_of(int32_t entry) const { return lines == 2 && entry >= n_groups ? 1 : 0; }
-    __host__ __device__ __forceinline__ int64_t slot0(int32_t line) const { return line == 0 ? 0 : static_cast<int64_t>(ctas) * 2 * cap[0]; }
+    float2* part_ml;       // workspace [ctas][2][cap]: of segments that are
+    float* part_o;         // workspace [ctas][2][cap][D]
 };
 
 __device__ __forceinline__ int32_t over_group(const Params& p, int32_t row) {
@@ -120,11 +118,10 @@ __device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int 
     return lo;
 }
 
-// How each line is cut: its pieces, the units of one (the last ones may be short or empty), and 1 / units.
+// How the line is cut: the units of a piece (the last ones may be short or empty), and 1 / units.
 struct Cut {
-    int32_t ctas[2];
-    int64_t size[2];
-    double inverse[2];
+    int64_t size;
+    double inverse;
 };
 __device__ __forceinline__ int64_t piece_units(int64_t total, int32_t ctas) {
     const int64_t even = (total + ctas - 1) / ctas;
@@ -149,15 +146,14 @@ struct __align__(16) Start {
     int32_t e, head, block, t1;
     int64_t left, unused;
 };
-// By one thread for one CTA; unit0(e) gives an entry's first unit, counted from the start of the first line.
+// By one thread for one CTA; unit0(e) gives an entry's first unit.
 template <class Unit0>
-__device__ __forceinline__ Start find_start(const Params& p, int32_t line, int64_t line0, int64_t total, int64_t size, int32_t cta, Unit0 unit0) {
-    const int64_t from = min(total, size * static_cast<int64_t>(cta)), end = min(total, from + size);
+__device__ __forceinline__ Start find_start(const Params& p, int64_t total, int64_t size, int32_t cta, Unit0 unit0) {
+    const int64_t begin = min(total, size * static_cast<int64_t>(cta)), end = min(total, begin + size);
     Start r = {};
-    r.left = end - from;
+    r.left = end - begin;
     if (r.left == 0) return r;
-    const int64_t begin = line0 + from;
-    int32_t lo = line == 0 ? 0 : p.n_groups, hi = line == 0 && p.lines == 2 ? p.n_groups : p.n_groups + p.batch;  // the last entry that starts at or before `begin`
+    int32_t lo = 0, hi = p.n_groups + p.batch;  // the last entry that starts at or before `begin`
     while (hi - lo > 1) {
         const int32_t mid = lo + (hi - lo) / 2;
         if (unit0(mid) <= begin) lo = mid;
@@ -238,8 +234,7 @@ inline Params make_params(const GroupArgs& a) {
     p.n_groups = a.n_groups;
     p.num_q_heads = a.num_q_heads;
     p.num_kv_heads = a.num_kv_heads;
-    p.group = a.num_q_heads / a.num_kv_heads;
-    p.group_magic = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
+    p.step = p.group = a.num_q_heads / a.num_kv_heads;
     p.block_table = a.cache->block_table;
     p.block_table_stride = a.cache->block_table_stride;
     p.num_blocks = static_cast<int32_t>(a.cache->num_blocks);

@@ -3,21 +3,21 @@
 // Few query rows meet many keys here - 5 to 8 rows a sequence in a decoding step, some dozens where a group shares a prompt -
 // and every cached byte is read once, 512 bytes a key against rows * 512 flops.  So the KEYS are the tensor core's M: a key
 // tile's 128 keys are the 128 lanes of S^T = K Q^T, the rows are its columns, and what a tile costs grows with the rows that are
-// there (16 to 128 in steps of 16) instead of with a tile of 128 that holds them:
+// there (16 to 64 in steps of 16) instead of with a tile of 128 that holds them:
 //     S^T [128 keys x N rows]  = K [128 x D] (K-major, as it lies in the cache) * Q^T (K-major)
 //     O^T [D x N rows]        += V^T [D x 128] (V as it lies in the cache, read MN-major) * P^T [128 x N]
 // P goes through shared memory, as bf16 [row][key] (K-major B operand).  The scores are loaded from tensor memory in the fragment
 // that stmatrix takes (16 lanes x 256 bits: a thread holds two rows of one key), so a warp stores its 32 keys of eight rows
-// with one instruction.  While a block has at most half of P's room in rows, the other half takes what the rounding to bf16
-// dropped, as so many more rows of the same product: probabilities enter it as two terms (off by 2^-17) and not as one (2^-8),
-// and the two outputs are added when they are read.  That costs nothing where the cache's bytes bound: V, the larger operand, is
-// read once.
+// with one instruction.  Half of P's room takes what the rounding to bf16 dropped, as so many more rows of the same product:
+// probabilities enter it as two terms (off by 2^-17) and not as one (2^-8), and the two outputs are added when they are read.  That
+// costs nothing where the cache's bytes bound: V, the larger operand, is read once.  (Blocks of 112 rows with one term took 102 us
+// where blocks of 64 with both take 130, 4 prompts of 64 responses, and were twice as far off.)
 //
 // A row's running reference is raised only when a score passes it by 2^8: what is kept is exact whatever the reference, so all
 // the threads of a tile need to agree on is whether one of them has to (one barrier with a vote).
 //
 // Segments (a KV head's keys of a group's prompt or of one sequence) follow one another without a pause: there are two buffers
-// each of S, P, O and (but for more than 64 rows) Q, every product has a thread of its own that waits for its own operands only, and
+// each of S, P, O and Q, every product has a thread of its own that waits for its own operands only, and
 // a segment's output is written by warps that do nothing else, while the softmax warps are in the next one.
 //   4 x 2 or 4 warps : two (up to 16 rows) or four teams with a share of the rows each: softmax, lanes = keys
 //   1 warp each      : producer of K and V (one TMA box per 16-token page); S^T = K Q^T; O^T += V^T P^T; laying Q out
@@ -44,15 +44,10 @@ struct Layout {
     static constexpr int kBlocks = (kCap / 8 + kTeams - 1) / kTeams;  // 8-row blocks of a team at most
     static constexpr int kHalves = D / 64;
     static constexpr int kTensorBytes = kTile * D * 2;             // a key tile of K or V
-    static constexpr int kPRows = kCap <= 64 ? 2 * kCap : 128;
+    static constexpr int kPRows = 2 * kCap;                        // of both terms
     static constexpr int kPHalfBytes = kPRows * 128;               // 64 keys of all rows
     static constexpr int kPBytes = 2 * kPHalfBytes;
-    static constexpr int kQRows = kCap <= 64 ? 2 * kCap : kCap;    // two blocks' Q, or one of more rows than half of these
-    static constexpr int kQHalfBytes = kQRows * 128;
-    // tokens of the box that a block of several lands in; a block that one half holds has at most as many
-    static __host__ __device__ constexpr int32_t q_box_tokens(bool both, int32_t group) {
-        return (both ? kQRows : kQRows / 2) / group > 1 ? (both ? kQRows : kQRows / 2) / group : 1;
-    }
+    static constexpr int kQHalfBytes = 2 * kCap * 128;             // 64 elements of D of two blocks' rows
     static constexpr int kQBytes = kHalves * kQHalfBytes;
     static constexpr int kCtlBytes = 512 + 10 * kCap * 4;          // barriers; two segments' references and sums
     static constexpr int kRoom = 232448 - kCtlBytes - 2 * kPBytes - kQBytes;
@@ -65,7 +60,7 @@ struct Layout {
     static constexpr int kCtlOff = kQOff + kQBytes;
     static constexpr size_t kSmemBytes = kCtlOff + kCtlBytes;
     static constexpr int kOCol = 2 * kCap;                         // O twice, kPRows columns each, behind S twice
-    static constexpr uint32_t kTmemCols = kCap >= 64 ? 512 : 8 * kCap;  // (a power of two)
+    static constexpr uint32_t kTmemCols = 8 * kCap;                // (a power of two)
 };
 
 struct Ctl {
@@ -81,19 +76,6 @@ struct Ctl {
     uint32_t tmem_base, abort_flag, drain_flag, data_error;
 };
 static_assert(sizeof(Ctl) <= 512, "room of the barriers");
-
-// The two halves of Q's room are used in turn by blocks that fit one, and together by larger ones.
-struct QTurn {
-    uint32_t uses0 = 0, uses1 = 0, at = 0, next = 0;
-    __device__ __forceinline__ bool take(bool both) {  // the half a block starts in: `at`; whether it has both
-        at = both ? 0 : next;
-        if (!both) next ^= 1;
-        if (at == 0) ++uses0;
-        if (at == 1 || both) ++uses1;
-        return both;
-    }
-    __device__ __forceinline__ uint32_t uses() const { return at == 0 ? uses0 : uses1; }
-};
 
 // Key tiles lie as [group of 8 keys][half][8 rows][128 bytes], swizzled: a 16-token page is one TMA box.
 template <int D>
@@ -115,18 +97,17 @@ __device__ __forceinline__ bool team_any(int id, bool x) {
     return r != 0u;
 }
 
-struct Maps {  // Q (boxes of one token, of a half of its room, of both), K, V
-    CUtensorMap q1, qh, qb, k, v;
+struct Maps {  // Q (boxes of one token, of as many as a block holds), K, V
+    CUtensorMap q1, qb, k, v;
 };
 
-// One CTA's piece of a line.  (kThreads: of the block; warps beyond this form's only meet the others at its barriers.  kPlanned: the
-// plan has been waited for.)
-template <int D, int kCap, int kThreads, bool kPlanned>
-__device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_t line, int32_t cta) {
+// One CTA's piece of the line.
+template <int D, int kCap>
+__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1) group_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
     using L = Layout<D, kCap>;
     constexpr int kTeams = L::kTeams, kProducerWarp = L::kProducerWarp, kScoreWarp = L::kScoreWarp, kValueWarp = L::kValueWarp, kQWarp = L::kQWarp, kOutWarp = L::kOutWarp;
-    // 512 * 96 + 256 * 48 = 512 * 88 + 256 * 64 = 768 * 80, what a launch of 768 threads has
-    constexpr int kSoftmaxRegs = kThreads != 768 ? 0 : L::kBlocks > 2 ? 96 : 88, kOtherRegs = L::kBlocks > 2 ? 48 : 64;
+    // 512 * 88 + 256 * 64 = 768 * 80, what a launch of 768 threads has
+    constexpr int kSoftmaxRegs = L::kThreads == 768 ? 88 : 0, kOtherRegs = 64;
     extern __shared__ __align__(1024) uint8_t smem[];
     if ((smem_u32(smem) & 1023u) != 0u) {  // swizzled tiles need 1024-byte alignment; never expected
         if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, RPX_ERR_CUDA);
@@ -166,7 +147,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem_base = ctl->tmem_base;  // S at columns 0 and kCap, O at kOCol
-    if constexpr (!kPlanned) asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
     auto rows16 = [&](const auto& w) { return (w.tokens() * p.group + 15) & ~15; };
 
     if (warp == kProducerWarp) {
@@ -233,15 +214,11 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
             const uint64_t k_desc = make_smem_desc_sw128(smem_u32(smem), 16, L::kHalves * 1024);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(smem + L::kQOff), 16, 1024);
             bool ok = true;
-            uint32_t tiles = 0;
-            QTurn turn;
-            while (ok && walk.next(p)) {
-                const int32_t n16 = rows16(walk);
-                const bool both = turn.take(n16 > L::kQRows / 2);
-                const uint32_t idesc = make_idesc_bf16(128, n16, false, false);
-                const uint64_t qd = q_desc + static_cast<uint64_t>(turn.at * (L::kQRows / 2) * 8);
-                ok = mbar_wait(&ctl->q_full[turn.at], (turn.uses() - 1) & 1u, abort_flag) &&
-                     (!both || mbar_wait(&ctl->q_full[1], (turn.uses1 - 1) & 1u, abort_flag));
+            uint32_t segments = 0, tiles = 0;
+            for (; ok && walk.next(p); ++segments) {
+                const uint32_t qb = segments & 1u, idesc = make_idesc_bf16(128, rows16(walk), false, false);
+                const uint64_t qd = q_desc + static_cast<uint64_t>(qb * kCap * 8);
+                ok = mbar_wait(&ctl->q_full[qb], (segments >> 1) & 1u, abort_flag);
                 for (int32_t t = walk.t0; ok && t < walk.t1; ++t, ++tiles) {
                     const uint32_t st = tiles % L::kSlotsK, b = tiles & 1u;
                     ok = (tiles < 2 || mbar_wait(&ctl->p_ready[b], ((tiles >> 1) - 1) & 1u, abort_flag)) &&
@@ -254,10 +231,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
                         umma_bf16_ss(tmem_base + b * kCap, kd + (ks >> 2) * 64 + 2 * (ks & 3), qd + (ks >> 2) * (L::kQHalfBytes >> 4) + 2 * (ks & 3), idesc, ks != 0);
                     umma_commit(&ctl->s_full[b]);
                     umma_commit(&ctl->k_empty[st]);
-                    if (t + 1 == walk.t1) {
-                        umma_commit(&ctl->q_empty[turn.at]);
-                        if (both) umma_commit(&ctl->q_empty[1]);
-                    }
+                    if (t + 1 == walk.t1) umma_commit(&ctl->q_empty[qb]);
                 }
             }
             if (!ok) {
@@ -277,9 +251,7 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
             bool ok = true;
             uint32_t segments = 0, tiles = 0;
             while (ok && walk.next(p)) {
-                const int32_t n16 = rows16(walk);
-                const bool two_terms = 2 * n16 <= L::kPRows;
-                const uint32_t ob = segments & 1u, idesc = make_idesc_bf16(128, two_terms ? 2 * n16 : n16, true, false);
+                const uint32_t ob = segments & 1u, idesc = make_idesc_bf16(128, 2 * rows16(walk), true, false);
                 if (segments >= 2) ok = mbar_wait(&ctl->o_free[ob], ((segments >> 1) - 1) & 1u, abort_flag);
                 for (int32_t t = walk.t0; ok && t < walk.t1; ++t, ++tiles) {
                     const uint32_t b = tiles & 1u, st = tiles % L::kSlotsV;
@@ -309,31 +281,27 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     } else if (warp == kQWarp) {
         // =========================================================== Q of a segment's block
-        // One box lands as consecutive 128-byte rows: of one token, of as many as a half of Q's room holds, or of as many as both do.
+        // One box lands as consecutive 128-byte rows: of one token, or of as many as a block holds.
         // (What lies behind the block's rows is another token's, or was there before: those rows are nobody's.)
         if constexpr (kSoftmaxRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         Walk walk;
         walk.start(p, blockIdx.x);
         if (elect_one()) {
-            QTurn turn;
+            uint32_t segments = 0;
             bool ok = true;
-            while (walk.next(p)) {
-                const bool both = turn.take(rows16(walk) > L::kQRows / 2);
-                ok = (turn.uses() <= 1 || mbar_wait(&ctl->q_empty[turn.at], turn.uses() & 1u, abort_flag)) &&
-                     (!both || turn.uses1 <= 1 || mbar_wait(&ctl->q_empty[1], turn.uses1 & 1u, abort_flag));
+            for (; walk.next(p); ++segments) {
+                const uint32_t qb = segments & 1u;
+                ok = segments < 2 || mbar_wait(&ctl->q_empty[qb], ((segments >> 1) - 1) & 1u, abort_flag);
                 if (!ok) break;
                 const bool one = walk.tokens() == 1;
-                const int32_t box_tokens = one ? 1 : L::q_box_tokens(both, p.group);
-                mbar_arrive_expect_tx(&ctl->q_full[turn.at], static_cast<uint32_t>(box_tokens * p.group * L::kHalves) * 128);
-                if (both) mbar_arrive(&ctl->q_full[1]);
+                mbar_arrive_expect_tx(&ctl->q_full[qb], static_cast<uint32_t>((one ? 1 : kCap / p.group) * p.group * L::kHalves) * 128);
                 for (int hf = 0; hf < L::kHalves; ++hf)
-                    tma_load_3d(smem + L::kQOff + hf * L::kQHalfBytes + turn.at * (L::kQRows / 2) * 128, one ? &maps.q1 : both ? &maps.qb : &maps.qh, &ctl->q_full[turn.at], hf * 64,
-                                walk.head * p.group, walk.q.tok0 + walk.token0());
+                    tma_load_3d(smem + L::kQOff + hf * L::kQHalfBytes + qb * kCap * 128, one ? &maps.q1 : &maps.qb, &ctl->q_full[qb], hf * 64, walk.head * p.step,
+                                walk.q.tok0 + walk.token0());
             }
-            if (!ok) {  // abort: the copies in flight get a moment to land
-                if (turn.uses0 > 0) mbar_wait(&ctl->q_full[0], (turn.uses0 - 1) & 1u, &ctl->drain_flag, kDrainLimitCycles);
-                if (turn.uses1 > 0) mbar_wait(&ctl->q_full[1], (turn.uses1 - 1) & 1u, &ctl->drain_flag, kDrainLimitCycles);
-            }
+            if (!ok)  // abort: the copies in flight get a moment to land
+                for (uint32_t i = segments > 2 ? segments - 2 : 0u; i < segments; ++i)
+                    mbar_wait(&ctl->q_full[i & 1u], (i >> 1) & 1u, &ctl->drain_flag, kDrainLimitCycles);
         }
     } else if (warp >= kOutWarp && warp < kOutWarp + 4) {
         // =========================================================== output: a warp 32 elements of D of all rows
@@ -350,15 +318,14 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
             const bool own = walk.e >= p.n_groups, whole = walk.t0 == 0 && walk.t1 == walk.q.tiles;
             const bool last_word = whole && own && walk.q.page0 == 0;  // nothing to add: this is the result
             // where the block's rows go: in order in a slot, or each in its own place
-            const int64_t first_row = (static_cast<int64_t>(walk.q.tok0) + walk.token0()) * p.num_q_heads + walk.head * p.group;
-            const int64_t base = whole ? (own && !last_word ? p.total_tokens * p.num_q_heads : 0) + first_row : p.slot0(line) + (static_cast<int64_t>(cta) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
+            const int64_t first_row = (static_cast<int64_t>(walk.q.tok0) + walk.token0()) * p.num_q_heads + walk.head * p.step;
+            const int64_t base = whole ? (own && !last_word ? p.total_tokens * p.num_q_heads : 0) + first_row : (static_cast<int64_t>(blockIdx.x) * 2 + (walk.t0 == 0 ? 1 : 0)) * kCap;
             const int32_t skip = whole ? p.num_q_heads - p.group : 0;  // rows between a token's last and the next one's first
             float* dst = (whole ? p.whole_o : p.part_o) + base * D + d;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + base * D + d;
             float2* dst_ml = (whole ? p.whole_ml : p.part_ml) + base;
             const float* now = ml + ob * 5 * kCap + lane;
             const int32_t n16 = rows16(walk);
-            const bool two_terms = 2 * n16 <= L::kPRows;
             const uint32_t o_addr = tmem_base + L::kOCol + ob * L::kPRows + (static_cast<uint32_t>(quarter * 32) << 16);
             if (!mbar_wait(&ctl->ml_ready[ob], (segments >> 1) & 1u, abort_flag)) break;
             for (int32_t r0 = 0; r0 < rows; r0 += 32, now += 32) {  // 32 rows a turn, a lane's numbers are those of row r0 + lane
@@ -387,12 +354,11 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
                 for (int32_t c = 0; c < here; c += 8) {
                     uint32_t o[8], lo[8];
                     tmem_ld8(o_addr + r0 + c, o);
-                    if (two_terms) tmem_ld8(o_addr + n16 + r0 + c, lo);
+                    tmem_ld8(o_addr + n16 + r0 + c, lo);
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        float x = __uint_as_float(o[i]);
-                        if (two_terms) x += __uint_as_float(lo[i]);
+                        const float x = __uint_as_float(o[i]) + __uint_as_float(lo[i]);
                         const float f = last_word ? __shfl_sync(0xffffffffu, inv, c + i) : 1.f;
                         if (c + i < here) {
                             if (last_word) out[static_cast<int64_t>(place) * D] = __float2bfloat16_rn(x * f);
@@ -434,7 +400,6 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
             const int32_t eights = (rows + 7) / 8, mine = (team - turn) & (kTeams - 1);
             const int32_t nb = min(kBlocks, eights - mine * kBlocks), row0 = 8 * mine * kBlocks;
             turn += (eights + kBlocks - 1) / kBlocks;
-            const bool two_terms = 2 * n16 <= L::kPRows;
             const bool own = walk.e >= p.n_groups;
             const int32_t seen_by_first = own ? len - walk.q.n + token0 + 1 : len;  // keys that the block's first token sees
             // of the pairs of rows that this thread holds: what a score has to pass for the reference to be raised (rows that are
@@ -532,13 +497,11 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
 #pragma unroll
                             for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kBlocks + c + i]);
                             tmem_st8(at, o);
-                            if (two_terms) {
-                                tmem_ld8(at + n16, o);
-                                tmem_ld_wait();
+                            tmem_ld8(at + n16, o);
+                            tmem_ld_wait();
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kBlocks + c + i]);
-                                tmem_st8(at + n16, o);
-                            }
+                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * all[32 * kBlocks + c + i]);
+                            tmem_st8(at + n16, o);
                         }
                         tmem_st_wait();
                     }
@@ -568,18 +531,16 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
                     f2_unpack(f2_add(f2_pack(sum[2 * k], sum[2 * k + 1]), f2_add(f2_add(x[0], x[1]), f2_add(x[2], x[3]))), sum[2 * k], sum[2 * k + 1]);
                     if (kBlocks == 1 || k < nb) stsm_x4_trans(at0 + 8 * k * 128, hi[0], hi[1], hi[2], hi[3]);
                 }
-                if (kCap <= 64 || two_terms) {  // what that rounding dropped
 #pragma unroll
-                    for (int k = 0; k < kBlocks; ++k) {
-                        uint32_t lo[4];
+                for (int k = 0; k < kBlocks; ++k) {  // what that rounding dropped
+                    uint32_t lo[4];
 #pragma unroll
-                        for (int m = 0; m < 4; ++m) {
-                            const float x0 = __uint_as_float(sc[k][2 * m]), x1 = __uint_as_float(sc[k][2 * m + 1]);
-                            const uint32_t hi = pack_bf16x2(x0, x1);
-                            lo[m] = pack_bf16x2(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
-                        }
-                        if (kBlocks == 1 || k < nb) stsm_x4_trans(at0 + (8 * k + n16) * 128, lo[0], lo[1], lo[2], lo[3]);
+                    for (int m = 0; m < 4; ++m) {
+                        const float x0 = __uint_as_float(sc[k][2 * m]), x1 = __uint_as_float(sc[k][2 * m + 1]);
+                        const uint32_t hi = pack_bf16x2(x0, x1);
+                        lo[m] = pack_bf16x2(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));
                     }
+                    if (kBlocks == 1 || k < nb) stsm_x4_trans(at0 + (8 * k + n16) * 128, lo[0], lo[1], lo[2], lo[3]);
                 }
                 }
                 // ---- V's rows behind the last key of a page that was loaded may hold anything: a probability of 0 must not
@@ -633,36 +594,18 @@ __device__ __forceinline__ void attend(const Maps& maps, const Params& p, int32_
     }
 }
 
-// One line: every CTA a piece of it.
-template <int D, int kCap>
-__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1) group_tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
-    attend<D, kCap, Layout<D, kCap>::kThreads, false>(maps, p, 0, blockIdx.x);
-}
-// Two lines: so many CTAs take the groups' shared keys, the others the sequences' own.
-template <int D, int kCap, int kSeqCap>
-__global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1)
-group_tiles_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Maps seq_maps, const __grid_constant__ Params p) {
-    constexpr int kThreads = Layout<D, kCap>::kThreads;
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the plan
-    const int32_t first = __ldcg(&p.cut->ctas[0]), cta = blockIdx.x;
-    if (cta < first) attend<D, kCap, kThreads, true>(maps, p, 0, cta);
-    else attend<D, kSeqCap, kThreads, true>(seq_maps, p, 1, cta - first);
-}
-
 template <int D, int kCap>
 rpx_status_t make_maps(Maps* m, const Params& p, const rpx_kv_cache_t& cache) {
     using L = Layout<D, kCap>;
     static_assert(L::kSlotsK >= 2 && L::kSlotsV >= 2 && L::kSmemBytes <= 232448, "shared memory of one CTA");
     static_assert(L::kTmemCols >= 32 && L::kTmemCols <= 512, "tensor memory");
     {
-        // a block's rows as (64 elements, heads of a KV head, tokens)
-        const uint64_t dims[3] = {D, static_cast<uint64_t>(p.num_q_heads), static_cast<uint64_t>(p.total_tokens)};
+        // a block's rows as (64 elements, heads of a KV head, tokens); a part's last KV head has p.group heads left
+        const uint64_t dims[3] = {D, static_cast<uint64_t>((p.num_kv_heads - 1) * p.step + p.group), static_cast<uint64_t>(p.total_tokens)};
         const uint64_t strides[2] = {D * 2ull, static_cast<uint64_t>(p.q_stride) * 2};
         uint32_t box[3] = {64, static_cast<uint32_t>(p.group), 1};
         if (rpx_status_t rc = encode_tmap_bf16(&m->q1, p.q, 3, dims, strides, box)) return rc;
-        box[2] = static_cast<uint32_t>(L::q_box_tokens(false, p.group));
-        if (rpx_status_t rc = encode_tmap_bf16(&m->qh, p.q, 3, dims, strides, box)) return rc;
-        box[2] = static_cast<uint32_t>(L::q_box_tokens(true, p.group));
+        box[2] = static_cast<uint32_t>(kCap / p.group);
         if (rpx_status_t rc = encode_tmap_bf16(&m->qb, p.q, 3, dims, strides, box)) return rc;
     }
     // the pool as groups of 8 keys: two per page and head
@@ -683,33 +626,12 @@ rpx_status_t launch_one(const Params& p, const rpx_kv_cache_t& cache, cudaStream
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kSmemBytes)) != cudaSuccess) return RPX_ERR_CUDA;
     return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, L::kSmemBytes, stream, maps, p);
 }
-template <int D, int kCap, int kSeqCap>
-rpx_status_t launch_two(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
-    using L = Layout<D, kCap>;
-    constexpr size_t bytes = L::kSmemBytes > Layout<D, kSeqCap>::kSmemBytes ? L::kSmemBytes : Layout<D, kSeqCap>::kSmemBytes;
-    Maps maps, seq_maps;
-    if (rpx_status_t rc = make_maps<D, kCap>(&maps, p, cache)) return rc;
-    if (rpx_status_t rc = make_maps<D, kSeqCap>(&seq_maps, p, cache)) return rc;
-    auto* kernel = group_tiles_kernel<D, kCap, kSeqCap>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) != cudaSuccess) return RPX_ERR_CUDA;
-    return launch_on_top(kernel, static_cast<unsigned>(p.ctas), L::kThreads, bytes, stream, maps, seq_maps, p);
-}
-
 template <int D>
 rpx_status_t launch_cap(const Params& p, const rpx_kv_cache_t& cache, cudaStream_t stream) {
-    constexpr int kMost = D == 128 ? 112 : 128;
-    if (p.lines == 2) {
-        switch (p.cap[1]) {
-            case 16: return launch_two<D, kMost, 16>(p, cache, stream);
-            case 32: return launch_two<D, kMost, 32>(p, cache, stream);
-            default: return launch_two<D, kMost, 64>(p, cache, stream);
-        }
-    }
-    switch (p.cap[0]) {
+    switch (p.cap) {
         case 16: return launch_one<D, 16>(p, cache, stream);
         case 32: return launch_one<D, 32>(p, cache, stream);
-        case 64: return launch_one<D, 64>(p, cache, stream);
-        default: return launch_one<D, kMost>(p, cache, stream);
+        default: return launch_one<D, kMostRows>(p, cache, stream);
     }
 }
 

@@ -260,7 +260,7 @@ struct GroupArgs {
 };
 size_t group_workspace(const rpx_attn_desc_t* desc, int64_t total_tokens, int32_t batch, int32_t n_groups, int32_t max_q,
                        int32_t max_group);
-int32_t group_most_rows(int32_t head_dim);  // rows of a block at most: query heads of a KV head that the pass takes
+int32_t group_most_heads(int32_t head_dim);  // query heads to a KV head that the call takes at most
 bool group_too_large(const GroupArgs& a);  // sizes that a launch of the pass cannot hold
 rpx_status_t launch_group_attn(const GroupArgs& a);
 

@@ -1,0 +1,62 @@
+"""Further GPU tests of group attention: what its first ones do not reach.
+
+Tolerances as in test_gpu_group_attn.py (u = 2^-8, e = 2^-24, S the largest scale * sum |q_i k_i| of a row), with the 2^-16 of two
+bf16 terms of P for every batch: out  u |out| + (2 w + 2^-13) sum p |v|,  w = (d + 4) e S + 2^-21 + 2^-16.
+"""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_group_attn import call, exact, make
+
+pytestmark = pytest.mark.gpu
+
+
+def check_two_terms(s, got, softmax_scale=None):
+    out, lse, pv, big = exact(s, softmax_scale)
+    score = (s["q"].shape[2] + 4) * 2.0 ** -24 * big
+    tol = 2.0 ** -8 * out.abs() + (2 * (score + 2.0 ** -21 + 2.0 ** -16) + 2.0 ** -13)[..., None] * pv
+    err = (got[0].double() - out).abs()
+    assert bool((err <= tol).all()), (float(err.max()), float((err / tol).max()))
+    assert bool(((got[1].double() - lse).abs() <= score + 2.0 ** -13 + 2.0 ** -20 * lse.abs()).all())
+
+
+# ------------------------------------------------------------------ probabilities in two terms, whoever else is in the group
+MANY_ROWS = {
+    "members": [(1500, [(1 + i % 40, 1) for i in range(70)])],
+    "tokens": [(900, [(40, 5), (600, 13), (5, 5), (200, 1)] * 3)],
+    "chunks": [(500, [(150, 150), (260, 200)]), (0, [(1029, 129)])],
+}
+
+
+@pytest.mark.parametrize("name", list(MANY_ROWS))
+@pytest.mark.parametrize("hq,hkv,d", [(28, 4, 128), (16, 2, 64), (64, 1, 128), (5, 5, 128)])
+@pytest.mark.parametrize("factor", [1.0, 6.0])
+def test_probabilities_are_two_terms_in_large_blocks(cuda_device, name, hq, hkv, d, factor):
+    """Groups and chunks of far more rows than a block holds; with the larger scale few keys hold a row's weight, so that a
+    probability of one bf16 term is off by many times the tolerance."""
+    scale = factor * d ** -0.5
+    s = make(MANY_ROWS[name], hq, hkv, d, cuda_device)
+    got = call(s, softmax_scale=scale)
+    assert int(s["status"]) == 0
+    check_two_terms(s, got, scale)
+
+
+def test_bounds_do_not_change_how_exact_a_row_is(cuda_device):
+    s = make([(700, [(20 + i, 1) for i in range(6)]), (0, [(400, 1)])], 28, 4, 128, cuda_device)
+    for bounds in (dict(), dict(max_group_tokens=40), dict(max_group_tokens=5000), dict(max_q_len=300)):
+        check_two_terms(s, call(s, softmax_scale=0.6, **bounds), 0.6)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(65, 1, 128), (112, 1, 128), (222, 2, 128), (224, 2, 128), (128, 1, 64), (381, 3, 64), (200, 2, 64)])
+def test_more_heads_to_a_kv_head_than_a_block_has_rows(cuda_device, hq, hkv, d):
+    """Parts of a KV head's query heads, equal and unequal ones, with several tokens, shared keys, cut segments and rows of nobody."""
+    for groups in (MANY_ROWS["tokens"], [(700, [(1 + i % 40, 1) for i in range(9)]), (0, [(3000, 2), (1, 1)])], [(0, [(129, 129)])], [(0, [(20000, 1)])]):
+        s = make(groups, hq, hkv, d, cuda_device, fill=float("nan"))
+        out = torch.full((s["q"].shape[0] + 2, hq, d), 9.0, dtype=torch.bfloat16, device=cuda_device)
+        got = call(s, out=out[1:-1])
+        assert int(s["status"]) == 0
+        check_two_terms(s, got)
+        assert bool((out[[0, -1]] == 9).all())
+        again = call(s)
+        assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
