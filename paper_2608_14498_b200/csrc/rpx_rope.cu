@@ -68,8 +68,8 @@ struct Params {
 
 // cos and sin of an angle.  The angle is reduced in 64 bits (position * frequency loses whole radians in 32
 // bits at far positions): in units of half a turn, brought into [-1, 1], which 32 bits hold to 2^-25 of a half turn.
-__device__ __forceinline__ void write_angle(const Params& p, int i, int32_t position, float2* cs) {
-    const double half_turns = static_cast<double>(position) * (static_cast<double>(__ldg(p.inv_freq + i)) * 0.31830988618379067154);
+__device__ __forceinline__ void write_angle(const Params& p, int i, double position, float2* cs) {
+    const double half_turns = position * (static_cast<double>(__ldg(p.inv_freq + i)) * 0.31830988618379067154);
     const float x = static_cast<float>(half_turns - 2.0 * rint(half_turns * 0.5));
     float s, c;
     sincospif(x, &s, &c);
@@ -213,10 +213,11 @@ __device__ __forceinline__ void stage_weights(const Params& p, float (*w)[D]) {
     __syncthreads();
 }
 
-// Where the append form stores a token: its place in its sequence, and its page (-1: nowhere, the page number is none of the
-// pool's).  False: the token is in no sequence, or in one that does not fit.
+// Where the append form stores a token: its place in its sequence (which may pass 31 bits behind a long one), the place in its
+// page, and the page (-1: nowhere, the page number is none of the pool's).  False: the token is in no sequence, or in one that does not fit.
 struct Slot {
-    int32_t place, page;
+    int64_t place;
+    int32_t in_page, page;
 };
 __device__ __forceinline__ bool find_slot(const Append& a, int64_t token, int64_t n_tokens, int lane, Slot* slot) {
     // the last sequence that starts at or before the token, 32 offsets a step: [lo, hi) holds it.  A lane of the last step has
@@ -241,7 +242,8 @@ __device__ __forceinline__ bool find_slot(const Append& a, int64_t token, int64_
     const int64_t pos = len + (token - begin);
     if ((static_cast<int64_t>(len) + (end - begin) + kPage - 1) / kPage > a.table_stride) return false;
     const int32_t page = __ldg(a.table + static_cast<int64_t>(lo) * a.table_stride + pos / kPage);
-    slot->place = static_cast<int32_t>(pos);
+    slot->place = pos;
+    slot->in_page = static_cast<int32_t>(pos % kPage);
     slot->page = page >= 0 && page < a.num_blocks ? page : -1;
     return true;
 }
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? (
         }
     };
     load(now, u_begin);
-    [[maybe_unused]] Slot slot = {0, -1};
+    [[maybe_unused]] Slot slot = {0, 0, -1};
     [[maybe_unused]] int32_t pos[2] = {0, 0};  // of this lane's pairs; under way during the search
     if constexpr (kAppend) {
         if (p.positions != nullptr && u_begin < u_end) {
@@ -305,10 +307,10 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? (
         if (blockIdx.x == 0) check_sequences(p.append, p.n_tokens);
         if (u_begin < u_end) {
             if (!find_slot(p.append, token, p.n_tokens, lane, &slot)) u_end = 0;
-            if (p.positions == nullptr) pos[0] = pos[1] = slot.place;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (lane + 32 * i < (p.rot >> 1)) write_angle(p, lane + 32 * i, pos[i], cs_all[warp]);
+                if (lane + 32 * i < (p.rot >> 1))
+                    write_angle(p, lane + 32 * i, p.positions == nullptr ? static_cast<double>(slot.place) : static_cast<double>(pos[i]), cs_all[warp]);
             __syncwarp();
         }
     } else if (u_begin < u_end) {
@@ -359,7 +361,7 @@ __global__ void __launch_bounds__(kWarps * 32, sizeof(typename T::Elem) == 2 ? (
             if (head < (is_q ? p.num_q_heads : p.num_kv_heads)) {
                 if (kAppend && !is_q) {
                     if (slot.page >= 0) {
-                        __nv_bfloat16* dst = (is_v ? p.append.v_cache : p.append.k_cache) + ((static_cast<int64_t>(slot.page) * p.num_kv_heads + head) * kPage + slot.place % kPage) * D;
+                        __nv_bfloat16* dst = (is_v ? p.append.v_cache : p.append.k_cache) + ((static_cast<int64_t>(slot.page) * p.num_kv_heads + head) * kPage + slot.in_page) * D;
                         Bf16::keep(dst + map.off_a, a);
                         Bf16::keep(dst + map.off_b, b);
                     }
