@@ -79,7 +79,7 @@ __device__ __forceinline__ void count_tokens(const Params& p, int32_t begin, int
     const bool with_d = p.by_sequence && p.o != nullptr;
     if (p.wide) {  // by fours
 #pragma unroll 4
-        for (int64_t t = (begin & ~3) + 4 * lane; t < end; t += 4 * lanes) {
+        for (int64_t t = static_cast<int64_t>(begin & ~3) + 4 * lane; t < end; t += 4 * lanes) {  // (up to 2^31 tokens: 64 bits before the sum)
             if (t + 4 > p.n_tokens) {
                 for (int64_t u = t < begin ? begin : t; u < end; ++u) count_one(p, u, with_d, n, d);
                 continue;
@@ -103,7 +103,7 @@ __device__ __forceinline__ void count_tokens(const Params& p, int32_t begin, int
         return;
     }
 #pragma unroll 4
-    for (int64_t t = begin + lane; t < end; t += lanes) count_one(p, t, with_d, n, d);
+    for (int64_t t = static_cast<int64_t>(begin) + lane; t < end; t += lanes) count_one(p, t, with_d, n, d);
 }
 
 __global__ void __launch_bounds__(kThreads) policy_count_kernel(const __grid_constant__ Params p) {
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_k
     bool fits = false;
     double w = 0.0, d_seq = 0.0;
     float a_seq = 0.f, w_up = 0.f;  // (w_up: w times the upstream gradient)
-    for (; step < step_end; ++step, t0 += 128) {
+    for (; step < step_end; ++step, t0 = step < step_end ? t0 + 128 : t0) {  // (128 more than the last ones may not fit 32 bits)
         Four next;
         if (step + 1 < step_end && t0 < p.n_tokens - 128) load(next, t0 + 128);
         const bool alone = __all_sync(0xffffffffu, fits && t0 <= end - 4);  // every lane stays in its sequence
