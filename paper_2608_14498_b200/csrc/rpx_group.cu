@@ -429,8 +429,8 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     bool bad_page = false;
     const int32_t keys = seq.len - seq.n + static_cast<int32_t>(token - seq.tok0) + 1;
     const int32_t* table = p.block_table + static_cast<int64_t>(s) * p.block_table_stride;
-    for (int32_t j0 = 0; j0 < keys; j0 += 4) {
-        const int32_t j = j0 + sub;
+    for (int64_t j0 = 0; j0 < keys; j0 += 4) {
+        const int64_t j = j0 + sub;
         const int32_t block = j < keys ? __ldg(table + j / kPage) : 0;
         const bool there = j < keys && block >= 0 && block < p.num_blocks;
         bad_page |= j < keys && !there;

@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1) group_tile_kerne
         };
         while (ok && walk.next(p)) {
             const int32_t* table = p.block_table + static_cast<int64_t>(walk.q.row) * p.block_table_stride + walk.q.page0;
-            const int32_t pages = (walk.q.len + kPage - 1) / kPage;
+            const int32_t pages = (walk.q.len - 1) / kPage + 1;  // (len + 15 may not fit 32 bits)
             auto read_block = [&](int32_t t) { return t < walk.t1 && t * kPages + pg < pages ? __ldg(table + t * kPages + pg) : 0; };
             int32_t next_block = read_block(walk.t0);
             for (int32_t t = walk.t0; t < walk.t1; ++t) {
@@ -428,13 +428,13 @@ __global__ void __launch_bounds__(Layout<D, kCap>::kThreads, 1) group_tile_kerne
                     tmem_ld_16x256(tmem_base + b * kCap + row0 + 8 * k + lane_addr + (16u << 16), &sc[k][4]);
                 }
                 tmem_ld_wait();
-                if (left < kTile || (t + 1) * kTile > seen_by_first) {
+                if (left < kTile || seen_by_first - t * kTile < kTile) {
 #pragma unroll
                     for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const int32_t token = min(over_group(p, row0 + 8 * k + pair + e), tokens - 1);
-                            const int32_t seen = min(left, seen_by_first + token - t * kTile);
+                            const int32_t seen = min(left, seen_by_first - t * kTile + token);  // (in this order: the sum of the first two may not fit)
 #pragma unroll
                             for (int m = 0; m < 4; ++m)
                                 if (key0 + 8 * m >= seen) sc[k][2 * m + e] = 0xff800000u;  // -inf

@@ -60,3 +60,34 @@ def test_more_heads_to_a_kv_head_than_a_block_has_rows(cuda_device, hq, hkv, d):
         assert bool((out[[0, -1]] == 9).all())
         again = call(s)
         assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+
+
+# ------------------------------------------------------------------ caches as long as kv_lens can say
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("kv", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 100])
+def test_lengths_next_to_31_bits(cuda_device, kv, shared):
+    """Every key weighs 1 but the last, whose weight is about that of all others together; behind it lies one that would outweigh
+    everything.  All pages but the last are the same one.  Sums of ones are exact (2^24 a piece), so the outputs are off by their
+    own rounding, 2^-8, and the joins', 2^-16 at most."""
+    hq, d, n, last, far = 2, 64, 5, 5.0, 400.0
+    seqs = 4 if shared else 1
+    pages = -(-kv // 16)
+    kc, vc = torch.zeros(2, 1, 16, d, device=cuda_device).bfloat16(), torch.ones(2, 1, 16, d, device=cuda_device).bfloat16()
+    place = (kv - 1) % 16
+    kc[1, 0, place, 0], vc[1, 0, place] = 172.0, last  # score 21.5
+    kc[1, 0, place + 1:, 0], vc[1, 0, place + 1:] = far, 100.0
+    table = torch.zeros(seqs, pages, dtype=torch.int32, device=cuda_device)
+    table[:, -1] = 1
+    whole = (kv - n) // 16 * 16 if shared else 0
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=cuda_device)
+    s = dict(q=torch.ones(seqs * n, hq, d, device=cuda_device).bfloat16(), kc=kc, vc=vc, table=table, cu=n * torch.arange(seqs + 1, dtype=torch.int32, device=cuda_device),
+             kv=i32(*[kv] * seqs), cg=i32(0, seqs), shared=i32(whole), max_q=n, max_group=seqs * n, max_kv=kv, status=i32(0))
+    out, lse = call(s)
+    assert int(s["status"]) == 0
+    ones, w = float(kv - 1), np.exp(21.5)
+    want = torch.ones(n, dtype=torch.float64)
+    want[-1] = (ones + last * w) / (ones + w)
+    total = torch.tensor([np.log(kv - n + 1.0 + i) for i in range(n - 1)] + [np.log(ones + w)])
+    err = (out.double().cpu().view(seqs, n, hq, d) - want[None, :, None, None]).abs()
+    assert bool((err <= (2.0 ** -8 + 2.0 ** -16) * want[None, :, None, None]).all()), err.amax((0, 2, 3))
+    assert bool(((lse.double().cpu().view(seqs, n, hq) - total[None, :, None]).abs() <= 2.0 ** -13 + 2.0 ** -20 * total[-1]).all())
