@@ -311,7 +311,8 @@ RPX_API size_t rpx_token_logprobs_backward_workspace_bytes(int64_t n_tokens, int
  *   mask device uint8 [n_tokens], or NULL.  These arrays may start at any element (16-byte accesses where all allow them).
  *   upstream device float32 [1], the gradient that reaches the loss, or NULL: 1
  *   stats device float32 [6]: loss, sum w policy, sum w kl, sum w [clipped], sum w r, the number of counted tokens
- *   dlogprobs device float32 [n_tokens], or NULL: no gradient; overlaps no input.  Tokens of no sequence keep what it holds.
+ *   dlogprobs device float32 [n_tokens], or NULL: no gradient; overlaps no input.  Tokens of no sequence keep what it holds, or
+ *       with desc->zero_rest get 0 (a buffer that holds nothing yet, on its way to rpx_token_logprobs_backward)
  *   workspace: rpx_policy_loss_workspace_bytes
  * Which side of a border a ratio is on is decided in 64 bits; ratios and policy terms are added up by fours in float32, and those
  * sums, the KL terms and the means of d in 64 bits, in a fixed order: the same call gives the same bits.  cu_seqlens that do not ascend from 0 or more to n_tokens at most are reported (RPX_ERR_DEVICE_DATA): a
@@ -329,6 +330,7 @@ typedef struct {
     double clip_dual;      /* 0: off, else > 1 */
     double kl_coef;
     double count;          /* 0: the call's own */
+    int32_t zero_rest;     /* not 0: dlogprobs of tokens of no sequence is 0 */
 } rpx_policy_desc_t;
 
 RPX_API rpx_status_t rpx_policy_loss(const rpx_policy_desc_t* desc, const float* logprobs, const float* old_logprobs,

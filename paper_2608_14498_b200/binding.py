@@ -126,6 +126,7 @@ class PolicyDesc(ctypes.Structure):
         ("clip_dual", ctypes.c_double),
         ("kl_coef", ctypes.c_double),
         ("count", ctypes.c_double),
+        ("zero_rest", ctypes.c_int32),
     ]
 
 
@@ -677,7 +678,8 @@ def policy_loss(logprobs, old_logprobs, advantages, cu_seqlens, mask=None, ref_l
     advantages float32 [B], or [T] (then one per token; where B == T, two dimensions [T, 1] ask for one per token); mask bool
     or uint8 [T].  ``ratio`` "token" or "sequence", ``mean`` "tokens" or "sequences", ``kl`` 1, 2 or 3 (0, or no ref_logprobs:
     none), clip_dual 0: off, ``count`` > 0: the denominator in place of the call's own.  Returns (stats, dlogprobs): float32
-    [6] (loss, policy term, KL term, clipped share, mean ratio, counted tokens) and [T], None without ``want_grad``."""
+    [6] (loss, policy term, KL term, clipped share, mean ratio, counted tokens) and [T], None without ``want_grad``.  Tokens of
+    no sequence (padding) have a gradient of 0; a given ``dlogprobs`` keeps what it holds there."""
     torch = _torch()
     lib = load_library()
     _one_device(logprobs, old_logprobs, advantages, cu_seqlens, mask, ref_logprobs, upstream, stats, dlogprobs, workspace,
@@ -699,12 +701,13 @@ def policy_loss(logprobs, old_logprobs, advantages, cu_seqlens, mask=None, ref_l
     for t, k in ((upstream, 1), (stats, 6)):
         if t is not None and (t.dtype != f32 or t.numel() != k or not t.is_contiguous()):
             raise ValueError("upstream is float32 [1] and stats float32 [6]")
-    if dlogprobs is None and want_grad:
+    zero_rest = dlogprobs is None and want_grad
+    if zero_rest:
         dlogprobs = torch.empty_like(logprobs)
     if stats is None:
         stats = torch.empty(6, dtype=f32, device=logprobs.device)
     desc = PolicyDesc(_RATIOS[ratio], _MEANS[mean], kl if ref_logprobs is not None else 0, 1 if per_token else 0, clip_low, clip_high,
-                      clip_dual, kl_coef, count)
+                      clip_dual, kl_coef, count, 1 if zero_rest else 0)
     ws = _workspace(lib.rpx_policy_loss_workspace_bytes(batch, n), logprobs.device, workspace)
     rc = lib.rpx_policy_loss(ctypes.byref(desc), logprobs.data_ptr(), _ptr(old_logprobs), _ptr(ref_logprobs), advantages.data_ptr(),
                              _ptr(mask), cu_seqlens.data_ptr(), batch, n, _ptr(upstream), stats.data_ptr(),

@@ -35,3 +35,47 @@ def test_sequences_next_to_31_bits(cuda_device, lens, shift):
         assert float(out[at - 1]) == 3.0
         del big, room, out, got
         torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ tokens of no sequence
+def _dirty(n, dev):
+    """Leaves NaN in the blocks that the allocator hands out next."""
+    for _ in range(4):
+        rooms = [torch.full((n,), float("nan"), device=dev) for _ in range(3)]
+        del rooms
+
+
+@pytest.mark.parametrize("lens", [[], [30, 41], [0, 0], [3000, 0, 7001], [1] * 900, [8192]], ids=lambda x: f"{len(x)}x{max(x + [0])}")
+@pytest.mark.parametrize("lead,tail", [(5, 9), (0, 1), (3, 20000), (129, 0)])
+def test_padding_has_a_gradient_of_zero(cuda_device, lens, lead, tail):
+    """A gradient that the call allocates itself goes to token_logprobs_backward as it is."""
+    s = make(lens, cuda_device, lead=lead, tail=tail, mask=0.7)
+    for ratio in ("token", "sequence"):
+        n = s["lp"].shape[0]
+        _dirty(n, cuda_device)
+        got = call(s, coef=0.1, ratio=ratio)
+        check(s, got, coef=0.1, ratio=ratio)
+        end = n - tail
+        assert bool((got[1][:lead] == 0).all()) and bool((got[1][end:] == 0).all())
+        out = torch.full_like(s["lp"], 3.0)
+        kept = call(s, coef=0.1, ratio=ratio, dlogprobs=out)
+        assert torch.equal(out[lead:end], got[1][lead:end]) and torch.equal(kept[0], got[0])
+        assert bool((out[:lead] == 3).all()) and bool((out[end:] == 3).all())
+
+
+def test_padded_training_step(cuda_device):
+    """hidden -> log-probs -> loss -> dW with padding behind the sequences: what lies there reaches no weight."""
+    gen = torch.Generator().manual_seed(1)
+    lens, t, hdim, vocab = [50, 0, 1, 93, 40], 250, 256, 1000
+    hidden = torch.randn(t, hdim, generator=gen).bfloat16().to(cuda_device)
+    w = (torch.randn(vocab, hdim, generator=gen) / 16).bfloat16().to(cuda_device)
+    ids, adv = torch.randint(vocab, (t,), generator=gen).int().to(cuda_device), torch.randn(len(lens), generator=gen).to(cuda_device)
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32).to(cuda_device)
+    lp, lse = rpx.token_logprobs(hidden, w, ids, return_lse=True)
+    old = lp - 0.05
+    _dirty(t, cuda_device)
+    _, dl = rpx.policy_loss(lp, old, adv, cu)
+    dh, dw = rpx.token_logprobs_backward(hidden, w, ids, lse, dl, want_dw=True)
+    _, dl = rpx.policy_loss(lp, old, adv, cu, dlogprobs=torch.zeros(t, device=cuda_device))
+    dh0, dw0 = rpx.token_logprobs_backward(hidden, w, ids, lse, dl, want_dw=True)
+    assert torch.equal(dh, dh0) and torch.equal(dw, dw0) and bool((dh[sum(lens):] == 0).all())
