@@ -314,9 +314,9 @@ RPX_API size_t rpx_token_logprobs_backward_workspace_bytes(int64_t n_tokens, int
  *   dlogprobs device float32 [n_tokens], or NULL: no gradient; overlaps no input.  Tokens of no sequence keep what it holds, or
  *       with desc->zero_rest get 0 (a buffer that holds nothing yet, on its way to rpx_token_logprobs_backward)
  *   workspace: rpx_policy_loss_workspace_bytes
- * Which side of a border a ratio is on is decided in 64 bits; ratios and policy terms are added up by fours in float32, and those
- * sums, the KL terms and the means of d in 64 bits, in a fixed order: the same call gives the same bits.  cu_seqlens that do not ascend from 0 or more to n_tokens at most are reported (RPX_ERR_DEVICE_DATA): a
- * sequence that does not fit counts as empty, and the outputs of that call are undefined.
+ * Which side of a border a ratio is on is decided in 64 bits, and all sums (of ratios, policy and KL terms, and the means of d) are
+ * in 64 bits, in a fixed order: the same call gives the same bits.  cu_seqlens that do not ascend from 0 or more to n_tokens at
+ * most are reported (RPX_ERR_DEVICE_DATA): a sequence that does not fit counts as empty, and the outputs of that call are undefined.
  */
 enum { RPX_RATIO_TOKEN = 0, RPX_RATIO_SEQUENCE = 1 };
 enum { RPX_MEAN_TOKENS = 0, RPX_MEAN_SEQUENCES = 1 };

@@ -291,15 +291,15 @@ __global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_k
             fits = false;
         }
         if (t0 < p.n_tokens) {
-            float grads[4], policy = 0.f, ratio = 0.f;  // sums of tokens of one weight, at most four
-            double kl_sum = 0.0;
+            float grads[4];
+            double policy = 0.0, ratio = 0.0, kl_sum = 0.0;  // sums of tokens of one weight
             int clips = 0;
             uint32_t written = 0u;
             auto add = [&] {
-                sums[0] += w * static_cast<double>(policy);
+                sums[0] += w * policy;
                 sums[1] += w * kl_sum;
                 sums[2] += w * clips;
-                sums[3] += w * static_cast<double>(ratio);
+                sums[3] += w * ratio;
             };
             auto token = [&](int i) {
                 const bool counted = (now.counted >> i & 1u) != 0u;
@@ -316,8 +316,8 @@ __global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_k
                 const bool clipped = a > 0.f ? above : a < 0.f && (below || far);
                 const float held = a > 0.f ? p.high : below ? p.low : p.dual;
                 float g = clipped ? 0.f : -a * r;
-                policy += counted ? -a * (clipped ? held : r) : 0.f;
-                ratio += counted ? r : 0.f;
+                policy += counted ? static_cast<double>(-a * (clipped ? held : r)) : 0.0;
+                ratio += counted ? static_cast<double>(r) : 0.0;
                 clips += counted && clipped ? 1 : 0;
                 if (p.kl != 0) {
                     const float x = now.f[i] - now.l[i];
@@ -346,8 +346,7 @@ __global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_k
                     if (!fits || t >= end) {
                         if (i > 0) {
                             add();
-                            policy = ratio = 0.f;
-                            kl_sum = 0.0;
+                            policy = ratio = kl_sum = 0.0;
                             clips = 0;
                         }
                         while (s < s_hi && __ldg(p.cu + s + 1) <= t) ++s;

@@ -79,3 +79,20 @@ def test_padded_training_step(cuda_device):
     _, dl = rpx.policy_loss(lp, old, adv, cu, dlogprobs=torch.zeros(t, device=cuda_device))
     dh0, dw0 = rpx.token_logprobs_backward(hidden, w, ids, lse, dl, want_dw=True)
     assert torch.equal(dh, dh0) and torch.equal(dw, dw0) and bool((dh[sum(lens):] == 0).all())
+
+
+# ------------------------------------------------------------------ ratios whose sum passes float32
+@pytest.mark.parametrize("lens", [[4], [4, 1, 7], [3000, 0, 7001]], ids=str)
+@pytest.mark.parametrize("mean", ["tokens", "sequences"])
+def test_large_ratios_have_a_finite_mean(cuda_device, lens, mean):
+    """Ratios up to 3.3e38: four of them add up to more than float32 holds, their weighted sum does not.  Differences lie on a grid
+    of 2^-10, so that they are exact; the advantage holds nothing (below 0, no dual clip) or makes the term small."""
+    s = make(lens, cuda_device, seed=2)
+    gen = torch.Generator().manual_seed(3)
+    d = torch.round((88.0 + 0.7 * torch.rand(sum(lens), generator=gen)) * 1024) / 1024
+    s["lp"], s["old"], s["ref"] = -torch.ones(sum(lens), device=cuda_device), -1 - d.to(cuda_device), None
+    for size in (1.0, 2.0 ** -20):
+        s["adv"] = -size * torch.ones(len(lens), device=cuda_device)
+        got = call(s, mean=mean)
+        assert bool(got[0].isfinite().all()) and float(got[0][4]) > 1.6e38
+        check(s, got, mean=mean)
