@@ -9,8 +9,8 @@
 // same r, and n terms of weight w with dr/dl = r / n each add up to the one w r.
 //
 // Bound by memory in principle (at most 21 bytes a token: l, o, f, mask, an advantage, dl) and by launches in truth: the
-// weights need the counts of all sequences first.  So batches of up to kSmallTokens tokens are one launch of one CTA, larger
-// ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the tokens is launched on top of it with
+// weights need the counts of all sequences first.  So batches of up to kSmallTokens tokens in up to kSmallBatch sequences (a warp
+// each) are one launch of one CTA, larger ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the tokens is launched on top of it with
 // its first tokens already on their way; its last CTA adds up the CTAs' sums.
 //
 // Measured: 8 x 250 tokens 6.6 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M
@@ -23,7 +23,11 @@ namespace rpx {
 namespace {
 
 constexpr int kThreads = 256, kSmallThreads = 1024;
-constexpr int64_t kSmallTokens = 8192;
+// One CTA against two launches, 8 x 250 tokens: 7.0 us in a graph for 7.4, and 15.8 for 18.0 a call from Python; masked 7.5 for 7.7,
+// one sequence of 2000 9.0 for 7.4.  Beyond, the one CTA loses: 8 x 1024 masked 12.2 us for 7.5; 48 x 41 9.4 for 9.1, 400 x 2 17.3
+// for 9.6, 8192 x 1 208 for 22.
+constexpr int64_t kSmallTokens = 2048;
+constexpr int32_t kSmallBatch = 32;
 constexpr int kCtasPerSm = 3;  // (four, with 64 registers, spill: 29 us for 27)
 constexpr int kSums = 4;  // policy, kl, clipped, ratio
 
@@ -480,7 +484,7 @@ rpx_status_t launch_policy_loss(const PolicyArgs& a) {
         p.steps = static_cast<int32_t>(steps / warps);
         p.more = static_cast<int32_t>(steps % warps);
     };
-    if (a.n_tokens <= kSmallTokens) {
+    if (a.n_tokens <= kSmallTokens && a.batch <= kSmallBatch) {
         share_out(kSmallThreads / 32);
         policy_loss_kernel<kSmallThreads, true><<<1, kSmallThreads, 0, a.stream>>>(p);
         return cudaGetLastError() == cudaSuccess ? RPX_OK : RPX_ERR_CUDA;

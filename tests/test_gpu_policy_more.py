@@ -96,3 +96,49 @@ def test_large_ratios_have_a_finite_mean(cuda_device, lens, mean):
         got = call(s, mean=mean)
         assert bool(got[0].isfinite().all()) and float(got[0][4]) > 1.6e38
         check(s, got, mean=mean)
+
+
+# ------------------------------------------------------------------ many short sequences
+@pytest.mark.parametrize("lens", [[1] * 8192, [2] * 4096, [0, 3] * 2000, [100] + [0] * 20000, [64] * 32, [64] * 33, [2048], [2049], [0] * 31 + [2048], [0] * 32 + [2048]],
+                         ids=lambda x: f"{len(x)}x{x[-1]}")
+@pytest.mark.parametrize("ratio,mean", [("token", "sequences"), ("sequence", "tokens"), ("sequence", "sequences")])
+@pytest.mark.parametrize("mask", [None, 0.6])
+def test_few_tokens_in_many_sequences(cuda_device, lens, ratio, mean, mask):
+    """Few tokens in many sequences, and both sides of what one launch of one CTA takes."""
+    s = make(lens, cuda_device, mask=mask, lead=1, tail=2)
+    kw = dict(ratio=ratio, mean=mean, kl=3, coef=0.05, dual=2.0)
+    got = call(s, **kw)
+    check(s, got, **kw)
+    again = call(s, **kw)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+def test_time_of_few_tokens_in_many_sequences(cuda_device):
+    """One-token sequences are spread over the GPU: three times as long as the same tokens in eight sequences, and by no
+    means eight times (one CTA that goes through them all takes seventeen times as long)."""
+    n = 8192
+    lp = -torch.rand(n, device=cuda_device)
+    mask = torch.ones(n, dtype=torch.bool, device=cuda_device)
+    times = []
+    for batch in (8, n):
+        cu = (torch.arange(batch + 1, device=cuda_device) * (n // batch)).int()
+        adv = torch.ones(batch, device=cuda_device)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            rpx.policy_loss(lp, lp, adv, cu, mask=mask)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                for _ in range(20):
+                    rpx.policy_loss(lp, lp, adv, cu, mask=mask)
+        best = float("inf")
+        for _ in range(10):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            graph.replay()
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        times.append(best)
+    assert times[1] <= 8 * times[0], times
