@@ -676,10 +676,11 @@ def policy_loss(logprobs, old_logprobs, advantages, cu_seqlens, mask=None, ref_l
 
     logprobs, old_logprobs (None: on the policy itself), ref_logprobs float32 [T], packed by cu_seqlens int32 [B + 1];
     advantages float32 [B], or [T] (then one per token; where B == T, two dimensions [T, 1] ask for one per token); mask bool
-    or uint8 [T].  ``ratio`` "token" or "sequence", ``mean`` "tokens" or "sequences", ``kl`` 1, 2 or 3 (0, or no ref_logprobs:
-    none), clip_dual 0: off, ``count`` > 0: the denominator in place of the call's own.  Returns (stats, dlogprobs): float32
-    [6] (loss, policy term, KL term, clipped share, mean ratio, counted tokens) and [T], None without ``want_grad``.  Tokens of
-    no sequence (padding) have a gradient of 0; a given ``dlogprobs`` keeps what it holds there."""
+    or uint8 [T].  ``ratio`` "token" or "sequence", ``mean`` "tokens" or "sequences", ``kl`` 1, 2 or 3, or 0: none (without
+    ref_logprobs there is none either, and a kl_coef that asks for one is refused), clip_dual 0: off, ``count`` > 0: the
+    denominator in place of the call's own.  Returns (stats, dlogprobs): float32 [6] (loss, policy term, KL term, clipped share,
+    mean ratio, counted tokens) and [T], None without ``want_grad``.  Tokens of no sequence (padding) have a gradient of 0; a
+    given ``dlogprobs`` keeps what it holds there."""
     torch = _torch()
     lib = load_library()
     _one_device(logprobs, old_logprobs, advantages, cu_seqlens, mask, ref_logprobs, upstream, stats, dlogprobs, workspace,
@@ -698,6 +699,10 @@ def policy_loss(logprobs, old_logprobs, advantages, cu_seqlens, mask=None, ref_l
         raise ValueError("advantages are contiguous float32, one for each sequence or one for each token")
     if ratio not in _RATIOS or mean not in _MEANS:
         raise ValueError('ratio is "token" or "sequence", mean is "tokens" or "sequences"')
+    if kl not in (0, 1, 2, 3):
+        raise ValueError("kl is 0, 1, 2 or 3")
+    if ref_logprobs is None and kl != 0 and kl_coef != 0:
+        raise ValueError("a KL term needs ref_logprobs (kl or kl_coef 0: none)")
     for t, k in ((upstream, 1), (stats, 6)):
         if t is not None and (t.dtype != f32 or t.numel() != k or not t.is_contiguous()):
             raise ValueError("upstream is float32 [1] and stats float32 [6]")
