@@ -311,8 +311,9 @@ RPX_API size_t rpx_token_logprobs_backward_workspace_bytes(int64_t n_tokens, int
  *   mask device uint8 [n_tokens], or NULL.  These arrays may start at any element (16-byte accesses where all allow them).
  *   upstream device float32 [1], the gradient that reaches the loss, or NULL: 1
  *   stats device float32 [6]: loss, sum w policy, sum w kl, sum w [clipped], sum w r, the number of counted tokens
- *   dlogprobs device float32 [n_tokens], or NULL: no gradient; overlaps no input.  Tokens of no sequence keep what it holds, or
- *       with desc->zero_rest get 0 (a buffer that holds nothing yet, on its way to rpx_token_logprobs_backward)
+ *   dlogprobs device float32 [n_tokens], or NULL: no gradient; overlaps neither inputs, stats nor workspace (RPX_ERR_SHAPE).
+ *       Tokens of no sequence keep what it holds, or with desc->zero_rest get 0 (for a buffer that holds nothing yet: it goes on to
+ *       rpx_token_logprobs_backward)
  *   workspace: rpx_policy_loss_workspace_bytes
  * Which side of a border a ratio is on is decided in 64 bits, and all sums (of ratios, policy and KL terms, and the means of d) are
  * in 64 bits, in a fixed order: the same call gives the same bits.  cu_seqlens that do not ascend from 0 or more to n_tokens at

@@ -799,6 +799,18 @@ rpx_status_t rpx_policy_loss(const rpx_policy_desc_t* desc, const float* logprob
                           static_cast<const void*>(advantages), static_cast<const void*>(dlogprobs), static_cast<const void*>(stats),
                           static_cast<const void*>(upstream), static_cast<const void*>(cu_seqlens)})
         if ((reinterpret_cast<uintptr_t>(t) & 3u) != 0) return RPX_ERR_ALIGN;
+    if (dlogprobs != nullptr && n_tokens > 0) {  // tokens are read ahead, and the offsets and means by all CTAs
+        const uintptr_t first = reinterpret_cast<uintptr_t>(dlogprobs), bytes = static_cast<uintptr_t>(n_tokens) * 4;
+        const uintptr_t tokens = static_cast<uintptr_t>(n_tokens), sequences = static_cast<uintptr_t>(batch);
+        const struct { const void* at; uintptr_t bytes; } others[] = {
+            {logprobs, tokens * 4}, {old_logprobs, tokens * 4}, {desc->kl != 0 ? ref_logprobs : nullptr, tokens * 4},
+            {advantages, (desc->adv_per_token != 0 ? tokens : sequences) * 4}, {mask, tokens}, {cu_seqlens, (sequences + 1) * 4}, {upstream, 4},
+            {stats, 24}, {workspace, empty ? 0 : rpx_policy_loss_workspace_bytes(batch, n_tokens)}};
+        for (const auto& o : others) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(o.at);
+            if (at != 0 && o.bytes > 0 && at < first + bytes && first < at + o.bytes) return RPX_ERR_SHAPE;
+        }
+    }
     if (rpx_status_t rc = check_arch()) return rc;
     PolicyArgs a;
     a.desc = desc;

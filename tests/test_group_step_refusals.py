@@ -39,3 +39,37 @@ def test_a_kl_term_without_reference_is_refused(stubbed):
     for good in (dict(), dict(kl=0, kl_coef=0.1), dict(kl=1), dict(kl_coef=0.1, ref_logprobs=torch.zeros(6)), dict(kl=0, ref_logprobs=torch.zeros(6))):
         with pytest.raises(Reached):
             stubbed(**good)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2608_14498_b200 import build
+
+    build.build()
+    return B.load_library()
+
+
+def test_a_gradient_that_overlaps_another_array_is_refused(lib):
+    """Addresses that nothing is launched with: the refusal comes before the device is asked."""
+    n, batch = 16, 2
+    at = {k: 0x10000 * (i + 1) for i, k in enumerate(("lp", "old", "ref", "adv", "mask", "cu", "up", "stats", "ws", "dl"))}
+    size = dict(lp=4 * n, old=4 * n, ref=4 * n, adv=4 * batch, mask=n, cu=4 * (batch + 1), up=4, stats=24, ws=B.load_library().rpx_policy_loss_workspace_bytes(batch, n))
+
+    def policy(kl=3, **kw):
+        a = dict(at, **kw)
+        d = B.PolicyDesc(0, 1, kl, 0, 0.2, 0.2, 0.0, 0.1, 0.0)
+        if torch.cuda.is_available():
+            return None  # (these addresses would be launched with)
+        return lib.rpx_policy_loss(ctypes.byref(d), a["lp"], a["old"], a["ref"], a["adv"], a["mask"], a["cu"], batch, n, a["up"], a["stats"],
+                                   a["dl"], a["ws"], 1 << 20, None, None)
+
+    if torch.cuda.is_available():
+        pytest.skip("host-only")
+    passed = policy()
+    assert passed in (-6, -7)  # no such device
+    for k, bytes_ in size.items():
+        assert policy(dl=at[k]) == -2, k
+        assert policy(dl=at[k] + bytes_ - 4 + bytes_ % 4) == -2, k
+        assert policy(dl=at[k] - 4 * n + 4) == -2, k
+        assert policy(dl=at[k] + (bytes_ + 3) // 4 * 4) == passed and policy(dl=at[k] - 4 * n) == passed, k
+    assert policy(kl=0, dl=at["ref"]) == passed and policy(dl=None) == passed
