@@ -143,10 +143,11 @@ __global__ void __launch_bounds__(kThreads, 5) policy_count_kernel(const __grid_
     }
 }
 
-// e^x, e^x - 1 and e^x - 1 - x together: x = n ln 2 + g with |g| <= ln 2 / 2 (ln 2 in two parts, n times the first exact),
-// q = e^g - 1 by its Taylor polynomial of degree 8 (what is left out is below 2^-32), e^x = 2^n (1 + q).  Where n is 0 neither
-// e^x - 1 nor e^x - 1 - x has lost anything; elsewhere both are as large as their parts.  2 to 3 roundings, no branch, NaN kept,
-// 0 below e^-87.3 and infinity above the largest value.  (The fast e^x that this library is compiled with is four times as far
+// e^x, e^x - 1 and e^x - 1 - x together: x = n ln 2 + g with |g| <= ln 2 / 2 (the reduction of Cody and Waite: ln 2 in two parts,
+// n times the first exact), q = e^g - 1 by its Taylor polynomial of degree 8 (what is left out is below 2^-32), e^x = 2^n (1 + q).
+// Where n is 0 neither e^x - 1 nor e^x - 1 - x has lost anything; elsewhere both are as large as their parts.  2 to 3 roundings, no
+// branch, NaN kept, infinity above the largest value, 0 from n = -126 on: below 2^-125.5, x < -86.99, where 2^n / 2 is none of
+// float32's normal numbers.  (The fast e^x that this library is compiled with is four times as far
 // off; expm1f, called for each, took a third of the kernel's time.)
 struct Exp {
     float exp, minus_one, minus_linear;
@@ -166,8 +167,8 @@ __device__ __forceinline__ Exp exponentials(float x) {
     a = fmaf(a, g, 1.f / 6.f);
     a = fmaf(a, g, 0.5f);
     const float rest = a * (g * g), q = g + rest;
-    const float e = (1.f + q) * half, m = fmaf(half, q, half - 0.5f);
-    return {e + e, m + m, n == 0.f ? rest : (m + m) - x};
+    const float one = 1.f + q, m = fmaf(half, q, half - 0.5f);
+    return {(one + one) * half, m + m, n == 0.f ? rest : (m + m) - x};
 }
 
 struct Four {

@@ -142,3 +142,21 @@ def test_time_of_few_tokens_in_many_sequences(cuda_device):
             best = min(best, a.elapsed_time(b))
         times.append(best)
     assert times[1] <= 8 * times[0], times
+
+
+# ------------------------------------------------------------------ exponentials down to where they end
+def test_ratios_down_to_the_smallest(cuda_device):
+    """The ratio alone (advantage 1, one token a sequence, weight 1), in units of e = 2^-24: x = n ln 2 + g leaves g off by e / 2,
+    q = e^g - 1 is a sum of g and less than 0.07, rounded once (e / 2), 1 + q once more (e), scaling by 2^n is exact, all against
+    1 + q >= 0.7: 3 e, and e each for the products with the advantage and the weight.  0 below 2^-125.5; 2^-126 holds 2 roundings
+    of the border."""
+    x = torch.cat([torch.linspace(-87.5, -86.5, 4001), torch.linspace(-87.0, -40.0, 4001), torch.tensor([-88.0, -100.0, -1e30, -float("inf")])]).float()
+    n = x.numel()
+    cu = torch.arange(n + 1, dtype=torch.int32, device=cuda_device)
+    stats, dl = rpx.policy_loss(x.to(cuda_device), torch.zeros(n, device=cuda_device), torch.ones(n, device=cuda_device), cu, count=1.0)
+    r = -dl.double().cpu()
+    want = torch.exp(x.double())
+    border = -125.5 * np.log(2.0)
+    over, under = x.double() > border + 2.0 ** -16, x.double() < border - 2.0 ** -16
+    assert bool(((r - want).abs() <= 5 * E * want)[over].all()), float(((r - want).abs() / want)[over].max() / E)
+    assert bool((r[under] == 0).all()) and int(under.sum()) > 2000
