@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32, 5) group_join_kernel(const __
 #pragma unroll 1
     for (int32_t j0 = sub; j0 < n; j0 += kSplit * kBatch) {
         float2 ml[kBatch];
-        float v[kBatch][kCols];
+        alignas(16) float v[kBatch][kCols];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             const bool shared = j0 + kSplit * u < of_group.n;

@@ -172,7 +172,7 @@ __device__ __forceinline__ Exp exponentials(float x) {
 }
 
 struct Four {
-    float l[4], o[4], f[4], adv[4];
+    alignas(16) float l[4], o[4], f[4], adv[4];  // (read as 16 bytes, also where they have left the registers)
     uint32_t counted;  // a bit each
 };
 
