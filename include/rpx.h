@@ -490,7 +490,8 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *   workspace: rpx_group_attn_workspace_bytes with the same sizes
  * The same call gives the same bits.  (Where the keys are cut goes by all lengths of the batch, so a sequence's sums may round
  * otherwise beside other sequences.)  RPX_BF16: scores, maxima, sums and outputs are float32 until the output's rounding;
- * probabilities enter the product with V as two bf16 terms (off by 2^-17), whatever the group.
+ * probabilities enter the product with V as two bf16 terms (off by 2^-17), whatever the group.  RPX_BF16 calls are not capped by
+ * rpx_set_sm_budget: the pieces that the keys are cut into, and with them the order of the sums, are those of a whole GPU.
  * RPX_F32 (for checking; a warp per row, nothing is shared): q, out and all products float32, K and V the cache's bf16.
  */
 RPX_API rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t q_tok_stride, const int32_t* cu_seqlens_q,
@@ -626,7 +627,8 @@ RPX_API rpx_status_t rpx_selftest_bounded_wait(int64_t limit_cycles, int32_t* de
  * slowdown Delta_D for sharing the GPU with prefix work; how large it is depends on how much of
  * the GPU the prefix kernels leave free.  The LM-head and attention kernels are persistent (one
  * CTA per SM, all shared memory of the SM), so left alone they leave nothing.  rpx_set_sm_budget(n)
- * caps their grids at n CTAs for every later call of this process (all devices, all streams);
+ * caps their grids at n CTAs for every later call of this process (all devices, all streams; rpx_tree_attn and rpx_group_attn
+ * are not capped: a caller who holds SMs back for a co-runner does not run them beside it);
  * 0 removes the cap, n < 0 returns RPX_ERR_SHAPE and changes nothing.  Results do not depend on
  * the budget bit for bit.  Host-only state: no CUDA call, no allocation, nothing set on the GPU.
  */

@@ -558,7 +558,7 @@ rpx_status_t launch_group_attn(const GroupArgs& a) {
     if (sms <= 0) return RPX_ERR_CUDA;
     p.cap = choose_cap(p);
     p.tile_units = a.head_dim == 128 ? 75 : 38;  // 64 KB or 32 at 6.5 TB/s over 148 SMs
-    // (without the SM budget: where the line of tiles is cut decides the order of the sums)
+    // (without the SM budget, as the header says: where the line of tiles is cut decides the order of the sums)
     p.ctas = sms < kMaxCtas ? sms : kMaxCtas;
     carve(p, a.head_dim, a.workspace);
     for (int32_t head = 0; head < p.step; head += part_heads(p.step)) {

@@ -7,7 +7,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_group_attn import call, exact, make
+import paper_2608_14498_b200 as rpx
+from test_gpu_group_attn import GROUPS, call, exact, make
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +92,18 @@ def test_lengths_next_to_31_bits(cuda_device, kv, shared):
     err = (out.double().cpu().view(seqs, n, hq, d) - want[None, :, None, None]).abs()
     assert bool((err <= (2.0 ** -8 + 2.0 ** -16) * want[None, :, None, None]).all()), err.amax((0, 2, 3))
     assert bool(((lse.double().cpu().view(seqs, n, hq) - total[None, :, None]).abs() <= 2.0 ** -13 + 2.0 ** -20 * total[-1]).all())
+
+
+# ------------------------------------------------------------------ the SM budget
+@pytest.mark.parametrize("name", ["mixed", "several_tokens"])
+def test_the_sm_budget_changes_no_bit(cuda_device, name):
+    s = make(GROUPS[name], 28, 4, 128, cuda_device)
+    want = call(s)
+    before = rpx.get_sm_budget()
+    try:
+        for budget in (1, 40, 147):
+            rpx.set_sm_budget(budget)
+            got = call(s)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    finally:
+        rpx.set_sm_budget(before)
