@@ -195,8 +195,8 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
         if (is_group) books.open(threadIdx.x, __ldg(p.cu_groups + g));
         if (threadIdx.x == 0) books.first[groups] = __ldg(p.cu_groups + g0 + groups);
         __syncthreads();
-        // the members of these groups (nobody, where the bounds descend)
-        const int32_t begin = max(books.first[0], 0), end = ascend ? min(books.first[groups], p.batch) : 0;
+        // the members of these groups (nobody, where the bounds descend; no bound goes into a sum as it came)
+        const int32_t begin = min(max(books.first[0], 0), p.batch), end = ascend ? min(books.first[groups], p.batch) : 0;
         for (int32_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
             Seq q;
             const bool fits = read_seq(p, s, &q);
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
         for (int32_t g = threadIdx.x; g < p.n_groups; g += blockDim.x) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
         const bool ascend = __syncthreads_and(good) != 0;
         for (int32_t g = warp; g < p.n_groups; g += kRowWarps) {
-            const int32_t first = max(__ldg(p.cu_groups + g), 0), last = ascend ? min(__ldg(p.cu_groups + g + 1), p.batch) : 0;
+            const int32_t first = min(max(__ldg(p.cu_groups + g), 0), p.batch), last = ascend ? min(__ldg(p.cu_groups + g + 1), p.batch) : 0;
             int32_t room = INT32_MAX;
             for (int32_t s = first + lane; s < last; s += 32) {
                 if (!read_seq(p, s, &q)) room = -1;

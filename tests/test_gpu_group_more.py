@@ -107,3 +107,74 @@ def test_the_sm_budget_changes_no_bit(cuda_device, name):
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     finally:
         rpx.set_sm_budget(before)
+
+
+# ------------------------------------------------------------------ data that does not fit, in every form
+BATCH = [(500, [(40, 1), (60, 1), (5, 1)]), (64, [(9, 2), (200, 2)])]
+FORMS = {"bf16": (torch.bfloat16, 0), "f32": (torch.float32, 0), "bf16_many": (torch.bfloat16, 1100)}  # type, sequences of their own behind
+
+
+def _longer(s, key, first, behind):
+    """The first entries of one of the batch's arrays replaced; those of the sequences behind as they were."""
+    old = s[key]
+    s[key] = torch.cat([torch.tensor(first, dtype=torch.int32, device=old.device), old[len(first):]])
+    assert s[key].shape == old.shape and behind == old.shape[0] - len(first)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("change", [
+    dict(cg=[0, 3, 2]), dict(cg=[-1, 3, 5]), dict(cg=[1, 0, 5]), dict(cg=[0, 2 ** 31 - 1, 5]), dict(cg=[0, -2 ** 31, 5]),
+    dict(cg=[2 ** 31 - 1] * 3), dict(cg=[2 ** 31 - 20, 2 ** 31 - 20, 2 ** 31 - 1]), dict(cg=[-2 ** 31, -1, 5]), dict(shared=[-1, 64]),
+    dict(shared=[505, 64]), dict(shared=[500, 2 ** 31 - 1]), dict(max_group=2), dict(shared=[500, 72])], ids=str)
+def test_groups_that_do_not_fit(cuda_device, form, change):
+    """Reported, and computed without sharing: whatever the form, the rows are right."""
+    dtype, behind = FORMS[form]
+    s = make(BATCH + [(0, [(3 + i % 30, 1)]) for i in range(behind)], 8, 2, 128, cuda_device, dtype=dtype)
+    good = call(s)
+    assert int(s["status"]) == 0
+    for k, v in change.items():
+        if k == "max_group":
+            s[k] = v
+        else:
+            _longer(s, k, v, behind)
+    got = call(s)
+    assert int(s["status"]) == -8
+    if dtype == torch.float32:
+        assert torch.equal(got[0], good[0]) and torch.equal(got[1], good[1])  # (never shared)
+    else:
+        check_two_terms(s, got)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("change,gone", [
+    (dict(kv=[540, 560, 505, 1, 264]), [3, 4]), (dict(kv=[540, -1, 505, 73, 264]), [1]), (dict(kv=[540, 2 ** 31 - 1, 505, 73, 264]), [1]),
+    (dict(max_q=1), [3, 4, 5, 6]), (dict(cu=[-1, 1, 2, 3, 5, 7]), [0]), (dict(cu=[0, 1, 2, 3, 5, 8]), [5, 6, 7])], ids=str)
+def test_sequences_that_do_not_fit(cuda_device, form, change, gone):
+    """Reported, and their rows left as they were; the other sequences' are right."""
+    dtype, behind = FORMS[form]
+    s = make(BATCH + [(0, [(3 + i % 30, 1)]) for i in range(behind)], 8, 2, 128, cuda_device, dtype=dtype)
+    want, lse = exact(s)[:2]
+    for k, v in change.items():
+        if k == "max_q":
+            s[k] = v
+        else:
+            _longer(s, k, v, behind)
+    out = torch.full_like(s["q"], 9.0)
+    out_lse = torch.full(s["q"].shape[:2], 9.0, device=cuda_device)
+    call(s, out=out, lse=out_lse)
+    assert int(s["status"]) == -8
+    gone = [t for t in gone if t < out.shape[0]]  # (the last sequence of the batch takes the next one's token, or one that is not there)
+    kept = [t for t in range(out.shape[0]) if t not in gone]
+    assert bool((out[gone] == 9).all()) and bool((out_lse[gone] == 9).all())
+    # values of size 1 to 4: rounded to 2^-8 of themselves, and 2^-13 of the terms' sum
+    assert float((out[kept].double() - want[kept]).abs().max()) < 0.03 and float((out_lse[kept].double() - lse[kept]).abs().max()) < 1e-3
+
+
+def test_bounds_of_later_groups_that_do_not_fit(cuda_device):
+    """More groups than the plan takes at a time, the later ones' bounds far behind the last sequence but ascending."""
+    for first, last in ((1024, 2 ** 31 - 1), (1024, 2 ** 31 - 500), (1, 2 ** 31 - 1), (1030, 2 ** 31 - 1)):
+        s = make(BATCH + [(0, [(3 + i % 30, 1)]) for i in range(1100)], 8, 2, 128, cuda_device)
+        s["cg"][first:] = last
+        got = call(s)
+        assert int(s["status"]) == -8
+        check_two_terms(s, got)
