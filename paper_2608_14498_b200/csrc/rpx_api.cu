@@ -560,7 +560,7 @@ rpx_status_t rpx_qk_norm_rope_append(const rpx_rope_desc_t* desc, const void* q,
     a.stream = static_cast<cudaStream_t>(cuda_stream);
     if (rpx_status_t rc = check_rope(a, true)) return rc;
     if (cache == nullptr) return RPX_ERR_NULL;
-    if (batch < 0 || max_append < 0) return RPX_ERR_SHAPE;
+    if (batch < 0 || batch > kMostSequences || max_append < 0) return RPX_ERR_SHAPE;
     if (n_tokens == 0 || batch == 0 || max_append == 0) return RPX_OK;  // (an empty table or pool has no pointer)
     if (rpx_status_t rc = check_cache(cache, batch)) return rc;
     if (v == nullptr || cu_append == nullptr || cached_lens == nullptr) return RPX_ERR_NULL;
@@ -785,7 +785,7 @@ rpx_status_t rpx_policy_loss(const rpx_policy_desc_t* desc, const float* logprob
     if (!(desc->clip_low >= 0.0 && desc->clip_low < 1.0) || !(desc->clip_high >= 0.0) || !(desc->count >= 0.0) ||
         !(desc->clip_dual == 0.0 || desc->clip_dual > 1.0) || desc->kl_coef != desc->kl_coef)
         return RPX_ERR_SHAPE;
-    if (batch < 0 || n_tokens < 0 || n_tokens >= INT32_MAX || batch == INT32_MAX) return RPX_ERR_SHAPE;
+    if (batch < 0 || n_tokens < 0 || n_tokens >= INT32_MAX || batch > kMostSequences) return RPX_ERR_SHAPE;
     if (stats == nullptr) return RPX_ERR_NULL;
     const bool empty = batch == 0 || n_tokens == 0;  // the statistics are zeros
     if (!empty) {

@@ -526,7 +526,7 @@ size_t carve(Params& p, int32_t head_dim, void* workspace) {
 int32_t group_most_heads(int32_t head_dim) { return head_dim == 128 ? 112 : 128; }
 
 size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, int32_t n_groups, int32_t max_q, int32_t max_group) {
-    if (d->dtype == RPX_F32 || batch > INT32_MAX - n_groups - 1) return 0;
+    if (d->dtype == RPX_F32 || batch > kMostSequences - n_groups) return 0;
     Params p = {};
     p.total_tokens = tokens;
     p.batch = batch;
@@ -542,7 +542,7 @@ size_t group_workspace(const rpx_attn_desc_t* d, int64_t tokens, int32_t batch, 
 bool group_too_large(const GroupArgs& a) {
     if ((a.total_tokens * a.num_q_heads + kRowWarps - 1) / kRowWarps > INT32_MAX) return true;
     if (a.num_kv_heads > 65535) return true;  // (a dimension of the join's grid)
-    return a.batch > INT32_MAX - a.n_groups - 1 || a.cache->num_blocks * a.num_kv_heads > INT32_MAX / 2;
+    return a.batch > kMostSequences - a.n_groups || a.cache->num_blocks * a.num_kv_heads > INT32_MAX / 2;
 }
 
 rpx_status_t launch_group_attn(const GroupArgs& a) {

@@ -223,6 +223,9 @@ rpx_status_t launch_qk_rope(const RopeArgs& a);
 rpx_status_t launch_qk_rope_append(const RopeArgs& a);
 rpx_status_t launch_qk_rope_backward(const RopeArgs& a);
 
+// Sequences of a call (with its groups) at most: loops over them step by a grid or a block beyond the last one, in 32 bits.
+constexpr int32_t kMostSequences = INT32_MAX - 65536;
+
 struct PolicyArgs {
     const rpx_policy_desc_t* desc;
     const float *logprobs, *old_logprobs, *ref_logprobs, *advantages;

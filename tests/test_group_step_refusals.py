@@ -73,3 +73,21 @@ def test_a_gradient_that_overlaps_another_array_is_refused(lib):
         assert policy(dl=at[k] - 4 * n + 4) == -2, k
         assert policy(dl=at[k] + (bytes_ + 3) // 4 * 4) == passed and policy(dl=at[k] - 4 * n) == passed, k
     assert policy(kl=0, dl=at["ref"]) == passed and policy(dl=None) == passed
+
+
+def test_more_sequences_than_32_bits_can_step_over_are_refused(lib):
+    """Loops over sequences go a grid beyond the last one."""
+    if torch.cuda.is_available():
+        pytest.skip("host-only")
+    P, most = 0x1000, 2 ** 31 - 1 - 65536
+    cache = B.KvCache(P, P, 8, 16, P, 4)
+    for batch in (most + 1, 2 ** 31 - 2, 2 ** 31 - 1):
+        d = B.PolicyDesc(0, 1, 0, 0, 0.2, 0.2, 0.0, 0.0, 0.0)
+        assert lib.rpx_policy_loss(ctypes.byref(d), P, P, None, P, None, P, batch, 16, None, P, None, P, 1 << 60, None, None) == -2
+        d = B.RopeDesc(4, 2, 128, 128, 1, None, 1e-6, B.RPX_BF16)
+        assert lib.rpx_qk_norm_rope_append(ctypes.byref(d), P, P, P, 512, 256, 256, P, P, P, 16, P, 16, P, P, batch, 8, ctypes.byref(cache), P, 512,
+                                           None, None) == -2
+        d = B.AttnDesc(4, 2, 128, 0.0, B.RPX_BF16)
+        for b, groups in ((batch, 0), (batch - 5, 5), (2, batch), (batch, batch)):
+            assert lib.rpx_group_attn(ctypes.byref(d), P, 512, P, P, b, 2, 1, 100, P, P, groups, 2, ctypes.byref(cache), P, None, P, 1 << 62, None, None) == -2
+            assert lib.rpx_group_attn_workspace_bytes(ctypes.byref(d), 2, b, groups, 1, 2) == 0
