@@ -482,7 +482,8 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *       for the group, through the row of its first sequence with queries.  What is beyond is read through every sequence's own.
  *   A group is computed without sharing, and reported (RPX_ERR_DEVICE_DATA), if its bounds or shared length do not fit: the
  *       shared tokens end in front of every member's first query.  A sequence whose offsets leave the packed tensors or the
- *       table, that has more queries than cached tokens, or more than max_q_len, is reported and its rows are left as they are.
+ *       table, that has more queries than cached tokens, or more than max_q_len, is reported and its rows are left as they are;
+ *       where cu_seqlens_q runs backwards, all rows are.
  *   max_q_len, max_group_tokens: upper bounds of a sequence's and of a group's query tokens (a group with more is computed
  *       without sharing, and reported); max_kv_len: upper bound of kv_lens (>= 0; nothing is
  *       sized by it, the work is laid out from kv_lens themselves)

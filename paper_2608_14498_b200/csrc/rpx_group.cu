@@ -153,10 +153,12 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_small_kernel(const __
     const bool member = is_seq && ascend && p.n_groups > 0 && s >= books.first[0] && s < books.first[p.n_groups];
     const int32_t of = member ? books.find(s, p.n_groups) : -1;
     if (member) books.add(of, s, fits, q);
-    __syncthreads();
+    // (offsets that run backwards: a row's sequence cannot be looked up, and nothing is computed)
+    const bool ordered = __syncthreads_and(!is_seq || cu[s] <= cu[s + 1]) != 0;
+    if (!ordered) q.n = 0;
     Entry e = {};
     if (is_group) {
-        fits = group_fits(p, ascend, first, last, shared, books.room[g]);
+        fits = ordered && group_fits(p, ascend, first, last, shared, books.room[g]);
         const int32_t n = fits ? cu[last] - cu[first] : 0;
         shared = shared_tokens(p, fits, n, shared, books.members[g]);
         books.shared[g] = shared;
@@ -181,14 +183,17 @@ __global__ void __launch_bounds__(kPlanThreads) group_plan_kernel(const __grid_c
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ int64_t sums[kPlanThreads / 32];
     __shared__ GroupBooks books;
-    bool good = true;
+    bool good = true, in_order = true;
     for (int32_t g = threadIdx.x; g < p.n_groups; g += kPlanThreads) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
     for (int32_t s = threadIdx.x; s < p.batch; s += kPlanThreads) {
         Seq q;
         if (!read_seq(p, s, &q)) report(p.status);
         p.entries[p.n_groups + s] = make_entry(p, q.tok0, q.n, q.len, s, 0);
+        in_order &= __ldg(p.cu + s) <= __ldg(p.cu + s + 1);
     }
-    const bool ascend = __syncthreads_and(good) != 0;
+    const bool ordered = __syncthreads_and(in_order) != 0, ascend = __syncthreads_and(good) != 0 && ordered;
+    if (!ordered)  // (as above)
+        for (int32_t s = threadIdx.x; s < p.batch; s += kPlanThreads) p.entries[p.n_groups + s] = make_entry(p, 0, 0, 0, s, 0);
     for (int32_t g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
         const int32_t groups = min(kPlanThreads, p.n_groups - g0), g = g0 + threadIdx.x;
         const bool is_group = threadIdx.x < groups;
@@ -389,11 +394,14 @@ template <int D>
 __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params p) {
     constexpr int U = D / 8;  // elements of a lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, part = lane & 7;
+    bool good = true;
+    for (int32_t s = threadIdx.x; s < p.batch; s += blockDim.x) good &= __ldg(p.cu + s) <= __ldg(p.cu + s + 1);
+    const bool ordered = __syncthreads_and(good) != 0;
     if (blockIdx.x == 0) {  // what does not fit is reported once
         Seq q;
         for (int32_t s = threadIdx.x; s < p.batch; s += blockDim.x)
             if (!read_seq(p, s, &q)) report(p.status);
-        bool good = true;
+        good = ordered;
         for (int32_t g = threadIdx.x; g < p.n_groups; g += blockDim.x) good &= __ldg(p.cu_groups + g) <= __ldg(p.cu_groups + g + 1);
         const bool ascend = __syncthreads_and(good) != 0;
         for (int32_t g = warp; g < p.n_groups; g += kRowWarps) {
@@ -414,7 +422,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kRowWarps + warp;
     const int64_t token = row / p.num_q_heads;
     const int32_t head = static_cast<int32_t>(row - token * p.num_q_heads);
-    if (token >= p.total_tokens) return;
+    if (token >= p.total_tokens || !ordered) return;
     const int32_t s = find_seq(p, token, lane);
     Seq seq;
     if (!read_seq(p, s, &seq) || token < seq.tok0 || token - seq.tok0 >= seq.n) return;

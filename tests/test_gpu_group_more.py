@@ -178,3 +178,17 @@ def test_bounds_of_later_groups_that_do_not_fit(cuda_device):
         got = call(s)
         assert int(s["status"]) == -8
         check_two_terms(s, got)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("cu", [[0, 1, 2, 3, 2, 7], [0, 1, 2 ** 31 - 1, 3, 5, 7], [0, 1, -2 ** 31, 3, 5, 7], [2, 1, 2, 3, 5, 7]], ids=str)
+def test_offsets_that_run_backwards(cuda_device, form, cu):
+    """A row's sequence is looked up in offsets that ascend: where they do not, no row is written."""
+    dtype, behind = FORMS[form]
+    s = make(BATCH + [(0, [(3 + i % 30, 1)]) for i in range(behind)], 8, 2, 128, cuda_device, dtype=dtype)
+    _longer(s, "cu", cu, behind)
+    out = torch.full_like(s["q"], 9.0)
+    lse = torch.full(s["q"].shape[:2], 9.0, device=cuda_device)
+    call(s, out=out, lse=lse)
+    assert int(s["status"]) == -8
+    assert bool((out == 9).all()) and bool((lse == 9).all())
