@@ -474,7 +474,8 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  * and V lie in the cache, the queries' own among them (rpx_qk_norm_rope_append or rpx_cache_append has stored them): sequence
  * s has kv_lens[s] cached tokens and owns the query tokens cu_seqlens_q[s] .. cu_seqlens_q[s+1]-1, the LAST n of its cached
  * tokens; query i of n attends to the positions 0 .. kv_lens[s] - n + i.  n = 1 everywhere is a decoding step.
- *   q [total_q_tokens][num_q_heads][head_dim], token stride in elements; out, lse as in rpx_suffix_attn
+ *   q [total_q_tokens][num_q_heads][head_dim], token stride in elements; out, lse as in rpx_suffix_attn; out may be q
+ *       itself (contiguous), otherwise it does not overlap q (RPX_ERR_SHAPE)
  *   cu_groups device int32 [n_groups + 1]: group g is the sequences cu_groups[g] .. cu_groups[g+1]-1; every sequence is in
  *       one group (alone, if it shares nothing)
  *   shared_lens device int32 [n_groups]: tokens that the group's sequences have in common from position 0 on.  The table rows
@@ -489,6 +490,8 @@ RPX_API rpx_status_t rpx_cache_append(const void* k, const void* v, int64_t k_to
  *       sized by it, the work is laid out from kv_lens themselves)
  *   num_q_heads / num_kv_heads: at most 112 with head_dim 128, 128 with 64 (RPX_ERR_SHAPE); more than 64 go over the keys twice
  *   workspace: rpx_group_attn_workspace_bytes with the same sizes
+ * What lies behind kv_lens in a page is not used.  V of a sequence's later query tokens has weight 0 for its earlier ones in the
+ * same product: an infinity or NaN there makes those rows NaN too.
  * The same call gives the same bits.  (Where the keys are cut goes by all lengths of the batch, so a sequence's sums may round
  * otherwise beside other sequences.)  RPX_BF16: scores, maxima, sums and outputs are float32 until the output's rounding;
  * probabilities enter the product with V as two bf16 terms (off by 2^-17), whatever the group.  RPX_BF16 calls are not capped by
@@ -543,7 +546,8 @@ RPX_API rpx_status_t rpx_qk_norm_rope(const rpx_rope_desc_t* desc, const void* q
  * rpx_qk_norm_rope; the normed and rotated k and the v of token cu_append[s] + i are stored, as bf16 rounded once, at position
  * cached_lens[s] + i of sequence s (cached_lens is not changed).  The same slots as rpx_cache_append's, without k in between.
  *   q, k, v [n_tokens][heads][head_dim] with token strides, such as views of one fused projection; element type desc->dtype
- *   cu_append device int32 [batch + 1], ascending.  Tokens of no sequence are not stored and their q_out is left as it is.
+ *   cu_append device int32 [batch + 1], ascending (where it runs backwards, which is reported, tokens of other sequences may be
+ *       left out as well).  Tokens of no sequence are not stored and their q_out is left as it is.
  *   positions as in rpx_qk_norm_rope, or NULL: every axis takes the token's place in its sequence, cached_lens[s] + i
  *   max_append: upper bound of a sequence's tokens.  A sequence with more, or whose offsets or table do not fit, is reported
  *       (RPX_ERR_DEVICE_DATA) and left out, its q_out too; a page number out of the pool is reported and that token's K, V are

@@ -885,6 +885,13 @@ rpx_status_t rpx_group_attn(const rpx_attn_desc_t* desc, const void* q, int64_t 
     const size_t need = rpx_group_attn_workspace_bytes(desc, total_q_tokens, batch, n_groups, max_q_len, max_group_tokens);
     if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return RPX_ERR_WORKSPACE;
     if (need > 0 && !aligned_ws(workspace)) return RPX_ERR_ALIGN;
+    {  // a row's queries have been read for the last time when its output is written: q itself may take it, nothing that lies across it
+        const int64_t row = static_cast<int64_t>(desc->num_q_heads) * desc->head_dim, element = desc->dtype == RPX_BF16 ? 2 : 4;
+        const uintptr_t first = reinterpret_cast<uintptr_t>(q), to = reinterpret_cast<uintptr_t>(out);
+        if ((to != first || q_tok_stride != row) && to < first + static_cast<uintptr_t>((total_q_tokens - 1) * q_tok_stride + row) * element &&
+            first < to + static_cast<uintptr_t>(total_q_tokens * row) * element)
+            return RPX_ERR_SHAPE;
+    }
     if (rpx_status_t rc = check_arch()) return rc;
     return launch_group_attn(a);
 }

@@ -192,3 +192,16 @@ def test_offsets_that_run_backwards(cuda_device, form, cu):
     call(s, out=out, lse=lse)
     assert int(s["status"]) == -8
     assert bool((out == 9).all()) and bool((lse == 9).all())
+
+
+# ------------------------------------------------------------------ outputs in the place of the queries
+@pytest.mark.parametrize("name", list(GROUPS))
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(28, 4, 128, torch.bfloat16), (4, 2, 64, torch.bfloat16), (100, 1, 128, torch.bfloat16), (4, 2, 64, torch.float32)])
+def test_outputs_in_the_place_of_the_queries(cuda_device, name, hq, hkv, d, dtype):
+    s = make(GROUPS[name], hq, hkv, d, cuda_device, dtype=dtype)
+    want = call(s)
+    for _ in range(3):
+        q = s["q"].clone()
+        got = call(s, q=q, out=q)
+        assert got[0].data_ptr() == q.data_ptr() and torch.equal(q, want[0]) and torch.equal(got[1], want[1])
+    assert int(s["status"]) == 0

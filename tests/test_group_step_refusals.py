@@ -91,3 +91,21 @@ def test_more_sequences_than_32_bits_can_step_over_are_refused(lib):
         for b, groups in ((batch, 0), (batch - 5, 5), (2, batch), (batch, batch)):
             assert lib.rpx_group_attn(ctypes.byref(d), P, 512, P, P, b, 2, 1, 100, P, P, groups, 2, ctypes.byref(cache), P, None, P, 1 << 62, None, None) == -2
             assert lib.rpx_group_attn_workspace_bytes(ctypes.byref(d), 2, b, groups, 1, 2) == 0
+
+
+def test_outputs_across_the_queries_are_refused(lib):
+    if torch.cuda.is_available():
+        pytest.skip("host-only")
+    P, q, t = 0x1000, 0x100000, 3
+    cache = B.KvCache(P, P, 8, 16, P, 4)
+
+    def group(out, stride=512, dtype=B.RPX_BF16):
+        d = B.AttnDesc(4, 2, 128, 0.0, dtype)
+        return lib.rpx_group_attn(ctypes.byref(d), q, stride, P, P, 2, t, 2, 100, P, P, 1, 3, ctypes.byref(cache), out, None, P, 1 << 40, None, None)
+
+    for stride, dtype, size in ((512, B.RPX_BF16, 2), (1536, B.RPX_BF16, 2), (512, B.RPX_F32, 4)):
+        end, room = q + (2 * stride + 512) * size, t * 512 * size
+        for out in (q + 16, end - 16, q - room + 16) + (() if stride == 512 else (q,)):
+            assert group(out, stride, dtype) == -2, (stride, out)
+        for out in (end, q - room) + ((q,) if stride == 512 else ()):
+            assert group(out, stride, dtype) in (-6, -7), (stride, out)  # no such device
