@@ -22,10 +22,11 @@ namespace rpx {
 
 namespace {
 
-constexpr int kThreads = 256, kSmallThreads = 1024;
-// One CTA against two launches, 8 x 250 tokens: 7.0 us in a graph for 7.4, and 15.8 for 18.0 a call from Python; masked 7.5 for 7.7,
-// one sequence of 2000 9.0 for 7.4.  Beyond, the one CTA loses: 8 x 1024 masked 12.2 us for 7.5; 48 x 41 9.4 for 9.1, 400 x 2 17.3
-// for 9.6, 8192 x 1 208 for 22.
+constexpr int kThreads = 256, kSmallThreads = 512;
+// One CTA (of 512 threads, four tokens each: with 1024 it spills, 7.1 us for 5.8) against two launches, 8 x 250 tokens: 5.8 us in a
+// graph for 7.6, and 16.2 for 18.4 a call from Python; masked 6.3 for 7.8, 32 x 60 6.8 for 7.9, one sequence of 2000 7.4 for 7.7.
+// Beyond, the one CTA loses (with 1024 threads): 8 x 1024 masked 12.2 us for 7.5; 48 x 41 9.4 for 9.1, 400 x 2 17.3 for 9.6, 8192 x
+// 1 208 for 22.
 constexpr int64_t kSmallTokens = 2048;
 constexpr int32_t kSmallBatch = 32;
 constexpr int kCtasPerSm = 3;  // (four, with 64 registers, spill: 29 us for 27)
