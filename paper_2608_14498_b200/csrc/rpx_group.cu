@@ -125,7 +125,7 @@ __device__ __forceinline__ void leave_starts(const Params& p, int64_t total, Uni
 }
 
 // Up to as many entries as threads: a thread an entry, groups first, everything read once (8 prompts of 8 with 5 tokens
-// each: the call takes 59 us, with the form below 62; one prompt of 8: 18 and 20).
+// each: the call takes 53 us, with the form below 55; one prompt of 8: 17.1 and 18.7).
 __global__ void __launch_bounds__(kPlanThreads) group_plan_small_kernel(const __grid_constant__ Params p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ int64_t sums[kPlanThreads / 32];

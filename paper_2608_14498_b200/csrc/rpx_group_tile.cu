@@ -11,7 +11,7 @@
 // with one instruction.  Half of P's room takes what the rounding to bf16 dropped, as so many more rows of the same product:
 // probabilities enter it as two terms (off by 2^-17) and not as one (2^-8), and the two outputs are added when they are read.  That
 // costs nothing where the cache's bytes bound: V, the larger operand, is read once.  (Blocks of 112 rows with one term took 102 us
-// where blocks of 64 with both take 130, 4 prompts of 64 responses, and were twice as far off.)
+// where blocks of 64 with both take 130, 4 prompts of 64 responses, and were off by 0.0023 of the largest output for 0.0017.)
 //
 // A row's running reference is raised only when a score passes it by 2^8: what is kept is exact whatever the reference, so all
 // the threads of a tile need to agree on is whether one of them has to (one barrier with a vote).

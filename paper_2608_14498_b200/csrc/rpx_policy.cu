@@ -13,9 +13,9 @@
 // each) are one launch of one CTA, larger ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the tokens is launched on top of it with
 // its first tokens already on their way; its last CTA adds up the CTAs' sums.
 //
-// Measured: 8 x 250 tokens 6.6 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M
-// tokens) 26 us, 28 % of the copy bandwidth: the chains of some 100 instructions a token; without the count 24.5 us.  A lane has four tokens
-// at a time and a warp's tokens follow one another, so that a sequence is looked up, and its weight divided, where one begins.
+// Measured: 8 x 250 tokens 5.4 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M
+// tokens) 28 us, 27 % of the copy bandwidth: the chains of some 100 instructions a token.  A lane has four tokens at a time and a
+// warp's tokens follow one another, so that a sequence is looked up, and its weight divided, where one begins.
 #include "rpx_internal.h"
 
 namespace rpx {
@@ -29,7 +29,7 @@ constexpr int kThreads = 256, kSmallThreads = 512;
 // 1 208 for 22.
 constexpr int64_t kSmallTokens = 2048;
 constexpr int32_t kSmallBatch = 32;
-constexpr int kCtasPerSm = 3;  // (four, with 64 registers, spill: 29 us for 27)
+constexpr int kCtasPerSm = 3;  // (four, with 64 registers, spill: 31 us for 28)
 constexpr int kSums = 4;  // policy, kl, clipped, ratio
 
 struct Params {
