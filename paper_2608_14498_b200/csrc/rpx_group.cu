@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32, 5) group_join_kernel(const __
     const int64_t token = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / kSplit) + warp / kSplit;
     const int32_t in_group = blockIdx.y, kv_head = blockIdx.z;
     const bool there = token < p.total_tokens;
-    const int32_t s = find_seq(p, there ? token : 0, lane);
+    const int32_t s = last_at_or_before(p.cu, p.batch, there ? token : 0, lane);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // (of rows that are left out too: this grid never ends before that one)
     if (!there) return;
     const Entry own = p.entries[p.n_groups + s];
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) group_rows_kernel(const Params
     const int64_t token = row / p.num_q_heads;
     const int32_t head = static_cast<int32_t>(row - token * p.num_q_heads);
     if (token >= p.total_tokens || !ordered) return;
-    const int32_t s = find_seq(p, token, lane);
+    const int32_t s = last_at_or_before(p.cu, p.batch, token, lane);
     Seq seq;
     if (!read_seq(p, s, &seq) || token < seq.tok0 || token - seq.tok0 >= seq.n) return;
     float q[U], acc[U];

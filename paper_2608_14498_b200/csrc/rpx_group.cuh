@@ -105,19 +105,6 @@ __device__ __forceinline__ bool read_seq(const Params& p, int32_t s, Seq* q) {
     return true;
 }
 
-// The last sequence that starts at or before a token, 32 offsets a step (a warp together).
-__device__ __forceinline__ int32_t find_seq(const Params& p, int64_t token, int lane) {
-    int32_t lo = 0, hi = p.batch;
-    while (hi - lo > 1) {
-        const int32_t step = (hi - lo + 31) / 32;
-        const int64_t at = lo + static_cast<int64_t>(lane) * step;
-        const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(p.cu + at) <= token);
-        lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
-        hi = hi - lo > step ? lo + step : hi;
-    }
-    return lo;
-}
-
 // How the line is cut: the units of a piece (the last ones may be short or empty), and 1 / units.
 struct Cut {
     int64_t size;

@@ -17,6 +17,7 @@
 // tokens) 28 us, 27 % of the copy bandwidth: the chains of some 100 instructions a token.  A lane has four tokens at a time and a
 // warp's tokens follow one another, so that a sequence is looked up, and its weight divided, where one begins.
 #include "rpx_internal.h"
+#include "rpx_ptx.cuh"
 
 namespace rpx {
 
@@ -271,22 +272,11 @@ __global__ void __launch_bounds__(kBlock, kSmall ? 1 : kCtasPerSm) policy_loss_k
         if (step + 1 < step_end && t0 < p.n_tokens - 128) load(next, t0 + 128);
         const bool alone = __all_sync(0xffffffffu, fits && t0 <= end - 4);  // every lane stays in its sequence
         if (!alone) {
-            // sequences of the warp's first and last token: 32 offsets a step (the last one that starts at or before a token)
-            auto find = [&](int32_t t) {
-                int32_t lo = 0, hi = p.batch;
-                while (hi - lo > 1) {
-                    const int32_t jump = (hi - lo + 31) / 32;
-                    const int64_t at = lo + static_cast<int64_t>(lane) * jump;
-                    const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(p.cu + at) <= t);
-                    lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * jump;
-                    hi = hi - lo > jump ? lo + jump : hi;
-                }
-                return lo;
-            };
+            // sequences of the warp's first and last token
             const int32_t first = step * 128;
-            s = s_hi = find(first);
+            s = s_hi = last_at_or_before(p.cu, p.batch, first, lane);
             const int32_t rest = min(127, p.n_tokens - 1 - first);
-            if (__ldg(p.cu + s + 1) <= first + rest) s_hi = find(first + rest);
+            if (__ldg(p.cu + s + 1) <= first + rest) s_hi = last_at_or_before(p.cu, p.batch, first + rest, lane);
             // the thread's first token, among these
             int32_t up = s_hi + 1;
             while (up - s > 1) {

@@ -145,6 +145,18 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+// The last of n ascending offsets that is at or before a token, 32 of them a step (a warp together).
+__device__ __forceinline__ int32_t last_at_or_before(const int32_t* offsets, int32_t n, int64_t token, int lane) {
+    int32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int32_t step = (hi - lo + 31) / 32;
+        const int64_t at = lo + static_cast<int64_t>(lane) * step;
+        const uint32_t before = __ballot_sync(0xffffffffu, at < hi && __ldg(offsets + at) <= token);
+        lo += (before != 0u ? 31 - __clz(static_cast<int>(before)) : 0) * step;
+        hi = hi - lo > step ? lo + step : hi;
+    }
+    return lo;
+}
 // Stores four 8x8 bf16 matrices transposed: thread t holds (row t / 4, columns 2 (t % 4), + 1) of each, lane l gives the address
 // where column l % 8 of matrix l / 8 goes as 16 bytes.
 __device__ __forceinline__ void stsm_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
