@@ -10,8 +10,8 @@
 //
 // Bound by memory in principle (at most 21 bytes a token: l, o, f, mask, an advantage, dl) and by launches in truth: the
 // weights need the counts of all sequences first.  So batches of up to kSmallTokens tokens in up to kSmallBatch sequences (a warp
-// each) are one launch of one CTA, larger ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the tokens is launched on top of it with
-// its first tokens already on their way; its last CTA adds up the CTAs' sums.
+// each) are one launch of one CTA, larger ones two: one CTA per sequence counts (and takes the mean of d), and the pass over the
+// tokens is launched on top of it with its first tokens already on their way; its last CTA adds up the CTAs' sums.
 //
 // Measured: 8 x 250 tokens 5.4 us, 256 ragged sequences of up to 2048 10 us, 1024 of up to 4096 with every input (2.3 M
 // tokens) 28 us, 27 % of the copy bandwidth: the chains of some 100 instructions a token.  A lane has four tokens at a time and a
